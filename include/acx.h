@@ -74,7 +74,10 @@ typedef enum acx_op {
   ACX_OP_BWD_BUILTIN_SCRATCH = 3, /* bytes of built-in scratch acx_linear_bwd_factor_builtin_scratch would use */
   ACX_OP_RSVD = 4,
   ACX_OP_BIAS_GRAD = 5,
-  ACX_OP_BWD_BIAS = 6
+  ACX_OP_BWD_BIAS = 6,
+  ACX_OP_NORM_BWD = 7, /* for acx_rows_workspace_bytes */
+  ACX_OP_CE_FWD = 8,   /* for acx_ce_workspace_bytes */
+  ACX_OP_CE_BWD = 9
 } acx_op;
 
 /* Problem descriptor: plain data, filled by the caller, read-only for the library. */
@@ -251,6 +254,69 @@ ACX_API acx_status acx_lowrank_adamw(const acx_desc* desc, const float* dW_A, fl
  * acx_reconstruct_v or acx_lowrank_adamw with this Vt.  d_out and seed of desc are not read. */
 ACX_API acx_status acx_rsvd_factor(const acx_desc* desc, const void* X, const void* U, void* Vt, void* ws, size_t ws_bytes,
                                    void* cuda_stream);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * What stands between the linears of a training step and behind the last one.  The nonlinear operators keep what their
+ * backward needs in 8 bits; the loss never writes the logits of the whole vocabulary.
+ * --------------------------------------------------------------------------------------------------------------- */
+
+/* A matrix of rows x cols elements: cols a multiple of 8 and >= 8; rows >= 0 (0 is a no-op; gradients of vectors are then
+ * set to zero).  Matrices with an explicit row stride (ldX, in elements) may be column slices of wider ones: the stride
+ * is a multiple of 8 and at least cols; all other matrices are dense. */
+typedef struct acx_rows_desc {
+  uint32_t struct_size; /* sizeof(acx_rows_desc) */
+  int32_t io_dtype;     /* acx_dtype of the matrices and of the weight vectors */
+  int64_t rows, cols;
+} acx_rows_desc;
+
+/* Workspace of the row operators: ACX_OP_NORM_BWD; 0 for anything else. */
+ACX_API size_t acx_rows_workspace_bytes(const acx_rows_desc* desc, int op);
+
+/* 8-bit checkpoint of a matrix: codes [rows x cols] int8, dense, and one fp32 scale per row and group of ACX_Q8_GROUP
+ * columns, scales [rows x ceil(cols / ACX_Q8_GROUP)].  With a = max |x| of a group:
+ *     scale = a / 127,  code = rint(x * (127 * (1 / a))),  value = code * scale,
+ * each step one binary32 operation (so the codes are reproducible bit for bit), the scale at most the largest float whose
+ * 127-fold is finite; the value is within a / 254 of x (and a
+ * few units in the last place).  Groups with a < 2^-100 are stored as zeros.  A group that holds an infinity or a NaN
+ * reads back as NaN.
+ *   acx_q8_store:  X [rows x cols, stride ldx] io_dtype, in;  codes, scales out.
+ *   acx_q8_load:   codes, scales in;  X [rows x cols, stride ldx] io_dtype, out (each value rounded once). */
+#define ACX_Q8_GROUP 128
+ACX_API acx_status acx_q8_store(const acx_rows_desc* desc, const void* X, int64_t ldx, int8_t* codes, float* scales, void* cuda_stream);
+ACX_API acx_status acx_q8_load(const acx_rows_desc* desc, const int8_t* codes, const float* scales, void* X, int64_t ldx,
+                               void* cuda_stream);
+
+/* Gated activation of an MLP:  H = silu(G) * U,  silu(g) = g / (1 + exp(-g)).
+ *   acx_swiglu_fwd:  G, U [rows x cols, strides ldg, ldu] in (the halves of a stacked gate/up output, for instance);
+ *      H [rows x cols] out;  Gq, Gs, Uq, Us: 8-bit checkpoints of G and U, out, or all NULL (nothing is kept).
+ *   acx_swiglu_bwd:  dH [rows x cols] in;  the checkpoints in;  dG, dU [rows x cols, strides lddg, lddu] out:
+ *      dU = dH G s,  dG = dH U s (1 + G (1 - s)),  s = 1 / (1 + exp(-G)),  at the checkpointed G and U. */
+ACX_API acx_status acx_swiglu_fwd(const acx_rows_desc* desc, const void* G, int64_t ldg, const void* U, int64_t ldu, void* H, int8_t* Gq,
+                                  float* Gs, int8_t* Uq, float* Us, void* cuda_stream);
+ACX_API acx_status acx_swiglu_bwd(const acx_rows_desc* desc, const void* dH, const int8_t* Gq, const float* Gs, const int8_t* Uq,
+                                  const float* Us, void* dG, int64_t lddg, void* dU, int64_t lddu, void* cuda_stream);
+
+/* Residual join between two blocks, with the RMS norm behind the first and the one in front of the second:
+ *     t = h + alpha * gate * (w_post * b * r_b),   h_out = t,   y = w_pre * t * r_t,   r_x = 1 / sqrt(mean(x^2) + eps),
+ * the means over the columns of a row; t is not rounded before y is taken from it.
+ *   h [rows x cols] in: the residual stream;  b [rows x cols] in: the block's output, or NULL: the norm alone (then
+ *   w_post, gate and h_out are NULL too);  w_post [cols] or NULL: no norm behind the block (r_b = w_post = 1);
+ *   gate [cols] or NULL: one;  w_pre [cols];  h_out, y [rows x cols] out.
+ *   Hq, Hs, Bq, Bs: 8-bit checkpoints of h and b, out;  rstd_post, rstd_pre [rows] fp32, out: r_b and r_t.  Either all that
+ *   apply are given (Bq, Bs with b, rstd_post with w_post) or none.
+ * acx_norm_join_bwd recomputes t from the checkpoints.  With that = t r_t, bhat = b r_b, k = alpha gate w_post:
+ *     dh = dh_next + r_t (dy w_pre - that mean(dy w_pre that)),     db = r_b (k dh - bhat mean(k dh bhat))  (k dh without w_post)
+ *     dw_pre = sum over the rows of dy that,   dw_post = alpha gate c,   dgate = alpha w_post c,   c = sum of dh bhat.
+ *   dy, dh_next [rows x cols] in: gradients of y and of h_out (dh_next may be NULL: zero);  dh, db [rows x cols] out (db with b);
+ *   dw_post, dgate, dw_pre [cols] fp32, out, each may be NULL;  ws/ws_bytes: acx_rows_workspace_bytes(desc, ACX_OP_NORM_BWD).
+ *   Fixed summation order: reproducible bits.  cols <= 32768 (else ACX_ERR_UNSUPPORTED_SHAPE). */
+ACX_API acx_status acx_norm_join_fwd(const acx_rows_desc* desc, const void* h, const void* b, const void* w_post, const void* gate,
+                                     const void* w_pre, void* h_out, void* y, int8_t* Hq, float* Hs, int8_t* Bq, float* Bs,
+                                     float* rstd_post, float* rstd_pre, float eps, float alpha, void* cuda_stream);
+ACX_API acx_status acx_norm_join_bwd(const acx_rows_desc* desc, const void* dy, const void* dh_next, const void* w_post, const void* gate,
+                                     const void* w_pre, const int8_t* Hq, const float* Hs, const int8_t* Bq, const float* Bs,
+                                     const float* rstd_post, const float* rstd_pre, void* dh, void* db, float* dw_post, float* dgate,
+                                     float* dw_pre, float alpha, void* ws, size_t ws_bytes, void* cuda_stream);
 
 /* Synchronises the stream and returns ACX_ERR_TIMEOUT if any kernel on this device since the last call gave up on
  * a bounded wait (its outputs are then undefined), ACX_ERR_CUDA on a CUDA error, else ACX_OK.  Clears the flag.  The

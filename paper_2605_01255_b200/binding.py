@@ -22,12 +22,15 @@ ACX_BUILTIN_SCRATCH_BYTES = 16 << 20
 ACX_F32, ACX_BF16 = 0, 1
 ACX_OP_FWD, ACX_OP_BWD, ACX_OP_RECONSTRUCT, ACX_OP_BWD_BUILTIN_SCRATCH, ACX_OP_RSVD, ACX_OP_BIAS_GRAD = 0, 1, 2, 3, 4, 5
 ACX_OP_BWD_BIAS = 6
+ACX_OP_NORM_BWD, ACX_OP_CE_FWD, ACX_OP_CE_BWD = 7, 8, 9
+ACX_Q8_GROUP = 128
 
 EXPORTS = (
     "acx_workspace_bytes", "acx_linear_fwd", "acx_linear_bwd", "acx_reconstruct",
     "acx_sketch_materialize", "acx_last_device_status", "acx_kernel_launches", "acx_status_string", "acx_version",
     "acx_linear_bwd_factor_builtin_scratch", "acx_reconstruct_adamw", "acx_debug_expired_wait",
     "acx_debug_force_gemm_mode", "acx_linear_fwd_v", "acx_reconstruct_v", "acx_lowrank_adamw", "acx_rsvd_factor", "acx_linear_fwd_bias", "acx_bias_grad", "acx_linear_bwd_bias",
+    "acx_rows_workspace_bytes", "acx_q8_store", "acx_q8_load", "acx_swiglu_fwd", "acx_swiglu_bwd", "acx_norm_join_fwd", "acx_norm_join_bwd",
 )
 
 
@@ -48,6 +51,10 @@ class acx_desc(ctypes.Structure):
         ("tokens", ctypes.c_int64), ("d_in", ctypes.c_int64), ("d_out", ctypes.c_int64),
         ("r", ctypes.c_int32), ("io_dtype", ctypes.c_int32), ("seed", ctypes.c_uint64),
     ]
+
+
+class acx_rows_desc(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("io_dtype", ctypes.c_int32), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64)]
 
 
 _lib = None
@@ -78,6 +85,14 @@ def lib() -> ctypes.CDLL:
         L.acx_linear_fwd_bias.restype, L.acx_linear_fwd_bias.argtypes = ctypes.c_int, [dp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.acx_bias_grad.restype, L.acx_bias_grad.argtypes = ctypes.c_int, [dp, vp, vp, vp, sz, vp]
         L.acx_linear_bwd_bias.restype, L.acx_linear_bwd_bias.argtypes = ctypes.c_int, [dp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        rp, i64, f32 = ctypes.POINTER(acx_rows_desc), ctypes.c_int64, ctypes.c_float
+        L.acx_rows_workspace_bytes.restype, L.acx_rows_workspace_bytes.argtypes = sz, [rp, ctypes.c_int]
+        L.acx_q8_store.restype, L.acx_q8_store.argtypes = ctypes.c_int, [rp, vp, i64, vp, vp, vp]
+        L.acx_q8_load.restype, L.acx_q8_load.argtypes = ctypes.c_int, [rp, vp, vp, vp, i64, vp]
+        L.acx_swiglu_fwd.restype, L.acx_swiglu_fwd.argtypes = ctypes.c_int, [rp, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp]
+        L.acx_swiglu_bwd.restype, L.acx_swiglu_bwd.argtypes = ctypes.c_int, [rp, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp]
+        L.acx_norm_join_fwd.restype, L.acx_norm_join_fwd.argtypes = ctypes.c_int, [rp] + [vp] * 13 + [f32, f32, vp]
+        L.acx_norm_join_bwd.restype, L.acx_norm_join_bwd.argtypes = ctypes.c_int, [rp] + [vp] * 16 + [f32, vp, sz, vp]
         L.acx_sketch_materialize.restype, L.acx_sketch_materialize.argtypes = ctypes.c_int, [dp, vp, vp]
         L.acx_last_device_status.restype, L.acx_last_device_status.argtypes = ctypes.c_int, [vp]
         L.acx_debug_expired_wait.restype, L.acx_debug_expired_wait.argtypes = ctypes.c_int, [ctypes.c_uint64, vp]
@@ -293,3 +308,112 @@ def acx_debug_force_gemm_mode(mode: int) -> None:
 
 def acx_last_device_status(stream=None) -> int:
     return int(lib().acx_last_device_status(_stream(stream)))
+
+
+# ---- what stands between the linears: 8-bit checkpoints, gated activation, residual join -------------------------------
+def make_rows_desc(rows: int, cols: int, dtype) -> acx_rows_desc:
+    """dtype: torch.float32 / torch.bfloat16 or "f32" / "bf16"."""
+    code = {torch.float32: ACX_F32, torch.bfloat16: ACX_BF16, "f32": ACX_F32, "bf16": ACX_BF16}[dtype]
+    return acx_rows_desc(ctypes.sizeof(acx_rows_desc), code, rows, cols)
+
+
+def acx_rows_workspace_bytes(desc: acx_rows_desc, op: int) -> int:
+    return int(lib().acx_rows_workspace_bytes(ctypes.byref(desc), op))
+
+
+def alloc_rows_workspace(desc: acx_rows_desc, op: int, device="cuda") -> Optional[torch.Tensor]:
+    n = acx_rows_workspace_bytes(desc, op)
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def q8_empty(rows: int, cols: int, device="cuda") -> Tuple[torch.Tensor, torch.Tensor]:
+    """Room for the 8-bit checkpoint of a rows x cols matrix: codes (int8) and scales (fp32)."""
+    return (torch.empty(rows, cols, dtype=torch.int8, device=device),
+            torch.empty(rows, -(-cols // ACX_Q8_GROUP), dtype=torch.float32, device=device))
+
+
+def _dense(t: Optional[torch.Tensor], shape: Tuple[int, ...], dtype, name: str) -> Optional[int]:
+    """Address of a dense CUDA tensor, checked like _ptr."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous CUDA tensor of shape %s and dtype %s (got %s %s on %s)"
+                         % (name, tuple(shape), dtype, tuple(t.shape), t.dtype, t.device))
+    return t.data_ptr()
+
+
+def _strided(t: torch.Tensor, shape: Tuple[int, int], dtype, name: str) -> Tuple[int, int]:
+    """Address and row stride of a CUDA matrix whose rows are dense (a column slice of a wider one is fine)."""
+    if t is None or t.dtype is not dtype or t.shape != shape or not t.is_cuda or t.stride(1) != 1:
+        raise ValueError("%s must be a CUDA matrix of shape %s and dtype %s with unit column stride" % (name, tuple(shape), dtype))
+    return t.data_ptr(), (t.stride(0) if shape[0] > 1 else shape[1])
+
+
+def _stream_arg(stream) -> int:
+    if stream is not None:
+        return stream.cuda_stream
+    return _raw_stream(torch.cuda.current_device()) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+
+
+def _q8_ptrs(desc: acx_rows_desc, codes, scales, name: str) -> Tuple[Optional[int], Optional[int]]:
+    rows, cols = desc.rows, desc.cols
+    return (_dense(codes, (rows, cols), torch.int8, name + " codes"),
+            _dense(scales, (rows, -(-cols // ACX_Q8_GROUP)), torch.float32, name + " scales"))
+
+
+def _rows_dtype(desc: acx_rows_desc):
+    return torch.bfloat16 if desc.io_dtype == ACX_BF16 else torch.float32
+
+
+def acx_q8_store(desc: acx_rows_desc, X, codes, scales, stream=None) -> None:
+    """Codes and scales of X (rows x cols; its rows may be strided)."""
+    xp, ldx = _strided(X, (desc.rows, desc.cols), _rows_dtype(desc), "X")
+    _check(lib().acx_q8_store(desc, xp, ldx, *_q8_ptrs(desc, codes, scales, "X"), _stream_arg(stream)), "acx_q8_store")
+
+
+def acx_q8_load(desc: acx_rows_desc, codes, scales, X, stream=None) -> None:
+    """The values of an 8-bit checkpoint into X (rows x cols; its rows may be strided)."""
+    xp, ldx = _strided(X, (desc.rows, desc.cols), _rows_dtype(desc), "X")
+    _check(lib().acx_q8_load(desc, *_q8_ptrs(desc, codes, scales, "X"), xp, ldx, _stream_arg(stream)), "acx_q8_load")
+
+
+def acx_swiglu_fwd(desc: acx_rows_desc, G, U, H, Gq=None, Gs=None, Uq=None, Us=None, stream=None) -> None:
+    """H = silu(G) * U; with Gq, Gs, Uq, Us also the 8-bit checkpoints of G and U."""
+    shape, dt = (desc.rows, desc.cols), _rows_dtype(desc)
+    gp, ldg = _strided(G, shape, dt, "G")
+    up, ldu = _strided(U, shape, dt, "U")
+    _check(lib().acx_swiglu_fwd(desc, gp, ldg, up, ldu, _dense(H, shape, dt, "H"), *_q8_ptrs(desc, Gq, Gs, "G"), *_q8_ptrs(desc, Uq, Us, "U"),
+                                _stream_arg(stream)), "acx_swiglu_fwd")
+
+
+def acx_swiglu_bwd(desc: acx_rows_desc, dH, Gq, Gs, Uq, Us, dG, dU, stream=None) -> None:
+    """dG, dU of H = silu(G) * U at the checkpointed G and U."""
+    shape, dt = (desc.rows, desc.cols), _rows_dtype(desc)
+    gp, ldg = _strided(dG, shape, dt, "dG")
+    up, ldu = _strided(dU, shape, dt, "dU")
+    _check(lib().acx_swiglu_bwd(desc, _dense(dH, shape, dt, "dH"), *_q8_ptrs(desc, Gq, Gs, "G"), *_q8_ptrs(desc, Uq, Us, "U"), gp, ldg, up, ldu,
+                                _stream_arg(stream)), "acx_swiglu_bwd")
+
+
+def acx_norm_join_fwd(desc: acx_rows_desc, h, b, w_post, gate, w_pre, h_out, y, Hq=None, Hs=None, Bq=None, Bs=None, rstd_post=None,
+                      rstd_pre=None, *, eps: float = 1e-5, alpha: float = 1.0, stream=None) -> None:
+    """h_out = h + alpha * gate * RMSNorm(b) * w_post and y = RMSNorm(h_out) * w_pre; b, w_post, gate may be None (see acx.h)."""
+    shape, vec, row, dt = (desc.rows, desc.cols), (desc.cols,), (desc.rows,), _rows_dtype(desc)
+    _check(lib().acx_norm_join_fwd(desc, _dense(h, shape, dt, "h"), _dense(b, shape, dt, "b"), _dense(w_post, vec, dt, "w_post"),
+                                   _dense(gate, vec, dt, "gate"), _dense(w_pre, vec, dt, "w_pre"), _dense(h_out, shape, dt, "h_out"),
+                                   _dense(y, shape, dt, "y"), *_q8_ptrs(desc, Hq, Hs, "h"), *_q8_ptrs(desc, Bq, Bs, "b"),
+                                   _dense(rstd_post, row, torch.float32, "rstd_post"), _dense(rstd_pre, row, torch.float32, "rstd_pre"),
+                                   eps, alpha, _stream_arg(stream)), "acx_norm_join_fwd")
+
+
+def acx_norm_join_bwd(desc: acx_rows_desc, dy, dh_next, w_post, gate, w_pre, Hq, Hs, Bq, Bs, rstd_post, rstd_pre, dh, db, dw_post, dgate,
+                      dw_pre, *, alpha: float = 1.0, ws=None, stream=None) -> None:
+    """Gradients of acx_norm_join_fwd at its checkpoints; ws: alloc_rows_workspace(desc, ACX_OP_NORM_BWD)."""
+    shape, vec, row, dt, f32 = (desc.rows, desc.cols), (desc.cols,), (desc.rows,), _rows_dtype(desc), torch.float32
+    wp, wn = _ws(ws)
+    _check(lib().acx_norm_join_bwd(desc, _dense(dy, shape, dt, "dy"), _dense(dh_next, shape, dt, "dh_next"), _dense(w_post, vec, dt, "w_post"),
+                                   _dense(gate, vec, dt, "gate"), _dense(w_pre, vec, dt, "w_pre"), *_q8_ptrs(desc, Hq, Hs, "h"),
+                                   *_q8_ptrs(desc, Bq, Bs, "b"), _dense(rstd_post, row, f32, "rstd_post"),
+                                   _dense(rstd_pre, row, f32, "rstd_pre"), _dense(dh, shape, dt, "dh"), _dense(db, shape, dt, "db"),
+                                   _dense(dw_post, vec, f32, "dw_post"), _dense(dgate, vec, f32, "dgate"), _dense(dw_pre, vec, f32, "dw_pre"),
+                                   alpha, wp, wn, _stream_arg(stream)), "acx_norm_join_bwd")

@@ -18,6 +18,18 @@ struct Problem {
   SketchParams sp;
 };
 
+// A validated acx_rows_desc.
+struct Rows {
+  int64_t rows, cols;
+  bool bf16;
+};
+
+// A validated acx_ce_desc.
+struct CeProblem {
+  int64_t m, d, vocab;
+  float logit_scale;
+};
+
 // Device-side status word values (written by kernels whose bounded waits expire).
 constexpr int kDevOk = 0;
 constexpr int kDevTimeout = 1;
@@ -92,6 +104,32 @@ size_t sm100_factor_scratch_bytes(const Problem& p);  // split-K partials throug
 // kMaxFactorSplits ranges) and *db_splits receives the number of ranges.
 cudaError_t sm100_factor(const Problem& p, const void* G, const void* XS, float* A, void* ws, int* status, cudaStream_t st,
                          bool allow_cluster, float* db_part = nullptr, int* db_splits = nullptr, bool after_dx = false);
+
+// ---- row operators (bf16 or fp32) -----------------------------------------------------------------
+cudaError_t q8_store(const Rows& d, const void* X, int64_t ldx, int8_t* codes, float* scales, cudaStream_t st);
+cudaError_t q8_load(const Rows& d, const int8_t* codes, const float* scales, void* X, int64_t ldx, cudaStream_t st);
+// Gq == nullptr: no checkpoints (then Gs, Uq, Us are not read either).
+cudaError_t swiglu_fwd(const Rows& d, const void* G, int64_t ldg, const void* U, int64_t ldu, void* H, int8_t* Gq, float* Gs, int8_t* Uq,
+                       float* Us, cudaStream_t st);
+cudaError_t swiglu_bwd(const Rows& d, const void* dH, const int8_t* Gq, const float* Gs, const int8_t* Uq, const float* Us, void* dG,
+                       int64_t lddg, void* dU, int64_t lddu, cudaStream_t st);
+constexpr int64_t kMaxNormCols = 32768;
+cudaError_t norm_join_fwd(const Rows& d, const void* h, const void* b, const void* w_post, const void* gate, const void* w_pre, void* h_out,
+                          void* y, int8_t* Hq, float* Hs, int8_t* Bq, float* Bs, float* rstd_post, float* rstd_pre, float eps, float alpha,
+                          cudaStream_t st);
+size_t norm_join_bwd_workspace_bytes(const Rows& d);
+cudaError_t norm_join_bwd(const Rows& d, const void* dy, const void* dh_next, const void* w_post, const void* gate, const void* w_pre,
+                          const int8_t* Hq, const float* Hs, const int8_t* Bq, const float* Bs, const float* rstd_post,
+                          const float* rstd_pre, void* dh, void* db, float* dw_post, float* dgate, float* dw_pre, float alpha, void* ws,
+                          cudaStream_t st);
+
+// ---- softmax cross entropy over a vocabulary (bf16 X and W) ---------------------------------------
+size_t ce_fwd_workspace_bytes(const CeProblem& p);
+cudaError_t ce_fwd(const CeProblem& p, const void* X, const void* W, const int64_t* targets, const float* weight, float* loss, float* lse,
+                   float* total, void* ws, int* status, cudaStream_t st);
+size_t ce_bwd_workspace_bytes(const CeProblem& p);
+cudaError_t ce_bwd(const CeProblem& p, const void* X, const void* W, const int64_t* targets, const float* weight, const float* lse,
+                   const float* denom, float scale, void* dX, void* dW, void* ws, int* status, cudaStream_t st);
 
 // Test/debug: overrides the tile-shape cost models of the forward and dX (0 = off, 1..4 = a GEMM mode).
 void sm100_force_gemm_mode(int mode);

@@ -1,0 +1,100 @@
+// Device helpers of the row operators: 8-element vectors of a row (16 bytes of bf16, 32 of fp32) and the 8-bit
+// checkpoint format.
+//
+// Format: per row, groups of 128 columns (the last one may be shorter) share one binary32 scale.  With a = max |x| of
+// the group,
+//     scale = a / 127,   code = rint(x * (127 * (1 / a))),
+// (the scale at most kMaxScale, so that 127 codes of the largest finite a do not overflow when they are read back), every
+// step one binary32 operation rounded to nearest even, so that the codes are a function of the input alone and
+// any two implementations agree on every bit.  a < 2^-100: the group is stored as zeros (1 / a would overflow on its
+// way through the subnormals).  An infinity or a NaN in the group: scale = NaN, the group reads back as NaN.
+#pragma once
+#include <cuda_bf16.h>
+#include <cstdint>
+
+namespace acx {
+namespace q8 {
+
+constexpr int kGroup = 128;            // columns that share a scale
+constexpr int kVec = 8;                // columns a thread handles at a time
+constexpr int kLanes = kGroup / kVec;  // threads of a warp that hold one group
+constexpr uint32_t kTinyBits = (127u - 100u) << 23;   // 2^-100
+constexpr uint32_t kInfBits = 0x7F800000u, kNanBits = 0x7FFFFFFFu;
+constexpr float kMaxScale = 0x1.0204060000000p+121f;            // the largest float whose 127-fold is finite
+
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&v)[8]) {
+  const uint4 u = __ldg(reinterpret_cast<const uint4*>(p));
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(w[i] << 16);
+    v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
+  const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+  v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+    w[i] = *reinterpret_cast<const uint32_t*>(&h);
+  }
+  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+  reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+  reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+
+// Largest magnitude of the group that 16 consecutive lanes hold, as bits: integer order is the order of magnitudes, with
+// infinity and then NaN on top, so nothing that is not finite gets lost.  All lanes of the warp take part.
+__device__ __forceinline__ uint32_t group_amax_bits(const float (&v)[8]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+#pragma unroll
+  for (int o = kLanes / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+  return m;
+}
+
+struct GroupScale { float scale, inv; };
+__device__ __forceinline__ GroupScale group_scale(uint32_t amax_bits) {
+  const float a = __uint_as_float(amax_bits);
+  GroupScale g;
+  if (amax_bits >= kInfBits) { g.scale = __uint_as_float(kNanBits); g.inv = 0.f; }
+  else if (amax_bits < kTinyBits) { g.scale = 0.f; g.inv = 0.f; }
+  else { g.scale = fminf(__fdiv_rn(a, 127.f), kMaxScale); g.inv = __fmul_rn(127.f, __frcp_rn(a)); }
+  return g;
+}
+
+// Eight codes as two words.  Adding 1.5 * 2^23 rounds a value of magnitude <= 2^22 to a whole number (nearest, ties to
+// even) and leaves its two's complement in the low bits of the sum's mantissa: one addition and a byte permutation
+// instead of a conversion, whose rate is a quarter.  The product and the sum are rounded separately (no fma), as the
+// format says.  A NaN product (0 * inf in a group whose scale is NaN) leaves some byte: it is read back times NaN.
+__device__ __forceinline__ uint2 encode8(const float (&v)[8], float inv) {
+  uint32_t b[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) b[i] = __float_as_uint(__fadd_rn(__fmul_rn(v[i], inv), 12582912.f));
+  uint2 c;
+  c.x = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+  c.y = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
+  return c;
+}
+
+// The values of eight codes.  A byte with its sign bit flipped is code + 128; placed into the mantissa of 2^23 it is the
+// float 2^23 + 128 + code, exactly.
+__device__ __forceinline__ void decode8(uint2 c, float scale, float (&v)[8]) {
+  const uint32_t w[2] = {c.x ^ 0x80808080u, c.y ^ 0x80808080u};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t bits = __byte_perm(w[i >> 2], 0x4B000000u, 0x7650 + (i & 3));   // bytes: 4B 00 00 code
+    v[i] = __fmul_rn(__fadd_rn(__uint_as_float(bits), -8388736.f), scale);
+  }
+}
+
+}  // namespace q8
+}  // namespace acx
