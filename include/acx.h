@@ -318,6 +318,40 @@ ACX_API acx_status acx_norm_join_bwd(const acx_rows_desc* desc, const void* dy, 
                                      const float* rstd_post, const float* rstd_pre, void* dh, void* db, float* dw_post, float* dgate,
                                      float* dw_pre, float alpha, void* ws, size_t ws_bytes, void* cuda_stream);
 
+/* Softmax cross entropy of a language model's head, logits = logit_scale * X W^T over a vocabulary, without the logits in
+ * memory.  X [tokens x d], W [vocab x d] bfloat16 (io_dtype must be ACX_BF16); d a multiple of 8, 8 <= d <= 65536;
+ * 1 <= vocab <= 2^22, any value; tokens <= 2^24, 0 is a no-op (total and dW are set to zero). */
+typedef struct acx_ce_desc {
+  uint32_t struct_size; /* sizeof(acx_ce_desc) */
+  int32_t io_dtype;     /* ACX_BF16 */
+  int64_t tokens, d, vocab;
+  float logit_scale;
+  uint32_t reserved;    /* 0 */
+} acx_ce_desc;
+
+/* Workspace of ACX_OP_CE_FWD or ACX_OP_CE_BWD; the backward's also serves the forward of the same descriptor. */
+ACX_API size_t acx_ce_workspace_bytes(const acx_ce_desc* desc, int op);
+
+/* Forward:  lse_t = log sum_v exp(logits_tv),  loss_t = lse_t - logits_ty  with y = targets[t].
+ *   targets [tokens] int64: a value outside [0, vocab) marks a token that is not trained on (loss 0, no gradient).
+ *   weight [tokens] fp32 or NULL (all one): weights of the tokens in `total` and in the gradients.
+ *   loss, lse [tokens] fp32, out;   total [2] fp32, out, or NULL: (sum of weight * loss, sum of weight) over the trained
+ *   tokens: total[0] / total[1] is the mean loss, and &total[1] the `denom` of its gradient.
+ *   The logits are fp32 sums on the tensor cores; the target's own is summed again outside them (see acx_ce.cu). */
+ACX_API acx_status acx_linear_ce_fwd(const acx_ce_desc* desc, const void* X, const void* W, const int64_t* targets, const float* weight,
+                                     float* loss, float* lse, float* total, void* ws, size_t ws_bytes, void* cuda_stream);
+
+/* Backward, of scale * (sum of weight * loss) / denom:
+ *     D = weight (exp(logits - lse) - onehot(y)),   dX = f D W,   dW = f D^T X,   f = scale * logit_scale / denom.
+ *   lse: from the forward.   denom: one fp32 number on the device, or NULL (one); f = 0 where it is not positive.
+ *   dX [tokens x d], dW [vocab x d] bfloat16, out; one of them may be NULL.
+ *   The vocabulary is taken in pieces: the logits of a piece are computed again, its D is held in bfloat16 in the workspace
+ *   until both products have used it, dX is summed over the pieces in fp32 and rounded once; what the rounding of D takes
+ *   from a target's own element is put back into dX in fp32.  Fixed summation order: reproducible bits. */
+ACX_API acx_status acx_linear_ce_bwd(const acx_ce_desc* desc, const void* X, const void* W, const int64_t* targets, const float* weight,
+                                     const float* lse, const float* denom, float scale, void* dX, void* dW, void* ws, size_t ws_bytes,
+                                     void* cuda_stream);
+
 /* Synchronises the stream and returns ACX_ERR_TIMEOUT if any kernel on this device since the last call gave up on
  * a bounded wait (its outputs are then undefined), ACX_ERR_CUDA on a CUDA error, else ACX_OK.  Clears the flag.  The
  * flag is one word per device: a kernel on any stream sets it, so the answer is about the device, not only about

@@ -31,6 +31,7 @@ EXPORTS = (
     "acx_linear_bwd_factor_builtin_scratch", "acx_reconstruct_adamw", "acx_debug_expired_wait",
     "acx_debug_force_gemm_mode", "acx_linear_fwd_v", "acx_reconstruct_v", "acx_lowrank_adamw", "acx_rsvd_factor", "acx_linear_fwd_bias", "acx_bias_grad", "acx_linear_bwd_bias",
     "acx_rows_workspace_bytes", "acx_q8_store", "acx_q8_load", "acx_swiglu_fwd", "acx_swiglu_bwd", "acx_norm_join_fwd", "acx_norm_join_bwd",
+    "acx_ce_workspace_bytes", "acx_linear_ce_fwd", "acx_linear_ce_bwd",
 )
 
 
@@ -55,6 +56,11 @@ class acx_desc(ctypes.Structure):
 
 class acx_rows_desc(ctypes.Structure):
     _fields_ = [("struct_size", ctypes.c_uint32), ("io_dtype", ctypes.c_int32), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64)]
+
+
+class acx_ce_desc(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("io_dtype", ctypes.c_int32), ("tokens", ctypes.c_int64), ("d", ctypes.c_int64),
+                ("vocab", ctypes.c_int64), ("logit_scale", ctypes.c_float), ("reserved", ctypes.c_uint32)]
 
 
 _lib = None
@@ -93,6 +99,10 @@ def lib() -> ctypes.CDLL:
         L.acx_swiglu_bwd.restype, L.acx_swiglu_bwd.argtypes = ctypes.c_int, [rp, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp]
         L.acx_norm_join_fwd.restype, L.acx_norm_join_fwd.argtypes = ctypes.c_int, [rp] + [vp] * 13 + [f32, f32, vp]
         L.acx_norm_join_bwd.restype, L.acx_norm_join_bwd.argtypes = ctypes.c_int, [rp] + [vp] * 16 + [f32, vp, sz, vp]
+        cp = ctypes.POINTER(acx_ce_desc)
+        L.acx_ce_workspace_bytes.restype, L.acx_ce_workspace_bytes.argtypes = sz, [cp, ctypes.c_int]
+        L.acx_linear_ce_fwd.restype, L.acx_linear_ce_fwd.argtypes = ctypes.c_int, [cp] + [vp] * 8 + [sz, vp]
+        L.acx_linear_ce_bwd.restype, L.acx_linear_ce_bwd.argtypes = ctypes.c_int, [cp] + [vp] * 6 + [f32, vp, vp, vp, sz, vp]
         L.acx_sketch_materialize.restype, L.acx_sketch_materialize.argtypes = ctypes.c_int, [dp, vp, vp]
         L.acx_last_device_status.restype, L.acx_last_device_status.argtypes = ctypes.c_int, [vp]
         L.acx_debug_expired_wait.restype, L.acx_debug_expired_wait.argtypes = ctypes.c_int, [ctypes.c_uint64, vp]
@@ -417,3 +427,41 @@ def acx_norm_join_bwd(desc: acx_rows_desc, dy, dh_next, w_post, gate, w_pre, Hq,
                                    _dense(rstd_pre, row, f32, "rstd_pre"), _dense(dh, shape, dt, "dh"), _dense(db, shape, dt, "db"),
                                    _dense(dw_post, vec, f32, "dw_post"), _dense(dgate, vec, f32, "dgate"), _dense(dw_pre, vec, f32, "dw_pre"),
                                    alpha, wp, wn, _stream_arg(stream)), "acx_norm_join_bwd")
+
+
+# ---- softmax cross entropy over a vocabulary ----------------------------------------------------------------------------
+def make_ce_desc(tokens: int, d: int, vocab: int, logit_scale: float = 1.0) -> acx_ce_desc:
+    return acx_ce_desc(ctypes.sizeof(acx_ce_desc), ACX_BF16, tokens, d, vocab, logit_scale, 0)
+
+
+def acx_ce_workspace_bytes(desc: acx_ce_desc, op: int) -> int:
+    return int(lib().acx_ce_workspace_bytes(ctypes.byref(desc), op))
+
+
+def alloc_ce_workspace(desc: acx_ce_desc, op: int, device="cuda") -> Optional[torch.Tensor]:
+    n = acx_ce_workspace_bytes(desc, op)
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def acx_linear_ce_fwd(desc: acx_ce_desc, X, W, targets, loss, lse, total=None, weight=None, ws=None, stream=None) -> None:
+    """Per-token cross entropy of logit_scale * X W^T at `targets` (int64; outside [0, vocab): not trained on), its log-sum-exp,
+    and total = (sum of weight * loss, sum of weight); ws: alloc_ce_workspace(desc, ACX_OP_CE_FWD)."""
+    row, f32 = (desc.tokens,), torch.float32
+    wp, wn = _ws(ws)
+    _check(lib().acx_linear_ce_fwd(desc, _dense(X, (desc.tokens, desc.d), torch.bfloat16, "X"), _dense(W, (desc.vocab, desc.d), torch.bfloat16, "W"),
+                                   _dense(targets, row, torch.int64, "targets"), _dense(weight, row, f32, "weight"),
+                                   _dense(loss, row, f32, "loss"), _dense(lse, row, f32, "lse"), _dense(total, (2,), f32, "total"), wp, wn,
+                                   _stream_arg(stream)), "acx_linear_ce_fwd")
+
+
+def acx_linear_ce_bwd(desc: acx_ce_desc, X, W, targets, lse, dX, dW, *, weight=None, denom=None, scale: float = 1.0, ws=None,
+                      stream=None) -> None:
+    """Gradients of scale * sum(weight * loss) / denom (denom: one fp32 number on the device, such as total[1:]); dX or dW may be
+    None; ws: alloc_ce_workspace(desc, ACX_OP_CE_BWD)."""
+    row, f32 = (desc.tokens,), torch.float32
+    wp, wn = _ws(ws)
+    _check(lib().acx_linear_ce_bwd(desc, _dense(X, (desc.tokens, desc.d), torch.bfloat16, "X"), _dense(W, (desc.vocab, desc.d), torch.bfloat16, "W"),
+                                   _dense(targets, row, torch.int64, "targets"), _dense(weight, row, f32, "weight"),
+                                   _dense(lse, row, f32, "lse"), _dense(denom, (1,), f32, "denom"), scale,
+                                   _dense(dX, (desc.tokens, desc.d), torch.bfloat16, "dX"), _dense(dW, (desc.vocab, desc.d), torch.bfloat16, "dW"),
+                                   wp, wn, _stream_arg(stream)), "acx_linear_ce_bwd")

@@ -1,0 +1,450 @@
+// The tcgen05 kernels of the vocabulary cross entropy: persistent, warp-specialised, on pairs of CTAs (a cluster of two
+// drives tcgen05.mma.cta_group::2 on a tile of 256 x 256).  Three kinds share the mainloop and differ in their epilogue:
+//
+//   LSE      logits tile = X W^T; every row of the tile leaves its maximum and its sum of exponentials over 128 columns
+//            (and the logit of its target, where the tile holds it): 16 bytes instead of 1 KiB of fp32 logits;
+//   DLOGITS  the same tile again, now D = w (exp(logit - lse) - onehot), rounded to bf16, for one piece of the vocabulary;
+//   GRADS    both products of a finished piece in one launch: dX += D W_piece (split over the piece when there are few
+//            tiles; fp32 sums in global memory, added by the bulk-copy engine) and dW_piece = D^T X (bf16, complete).
+//
+// What bounds them: the tensor cores, from a few hundred tokens on; with fewer the bytes of W.  Per SM a 256 x 256 pair
+// tile takes K / 16 instructions of 128 cycles; its epilogue (128 x 256 elements per CTA, eight warps, about five
+// instructions per exponential) about 2000 cycles, hidden behind the next tile's mainloop by the second accumulator.
+//
+// Roles per CTA (320 threads, one CTA per SM): warp 0 TMA producer, warp 1 UMMA issuer (of the leader) and owner of the
+// tensor memory, warps 2..9 epilogue: two per TMEM lane quarter, 128 columns each.  Six 32 KiB stages; all waits bounded.
+// Loads are plain bulk tensor copies (no cluster multicast).
+#pragma once
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include "acx_internal.h"
+#include "acx_umma.cuh"
+
+namespace acx {
+namespace ce {
+
+constexpr int kBM = 128;                   // rows of the tile per CTA (a pair: 256)
+constexpr int kTile = 256;                 // rows and columns of a pair's tile
+constexpr int kBK = 64;                    // bf16 per stage along K: one 128-byte swizzle row
+constexpr int kUmmaK = 16;
+constexpr int kStages = 6;
+constexpr int kABytes = kBM * kBK * 2, kBBytes = kBM * kBK * 2, kStageBytes = kABytes + kBBytes;
+constexpr int kChunkBytes = 64 * kBK * 2;  // MN-major operand: 64 k-rows of 128 bytes
+constexpr int kAccCols = 256, kTmemCols = 512;
+constexpr int kEpiWarp0 = 2, kEpiWarps = 8, kThreads = 32 * (kEpiWarp0 + kEpiWarps);
+constexpr int kBoxBytes = 32 * 64;         // store staging: 32 rows of 64 bytes, 64-byte swizzle; two per epilogue warp
+constexpr int kBarBytes = 1024;
+constexpr int kOutOffset = kStages * kStageBytes + kBarBytes;
+constexpr int kSmemBytes = kOutOffset + kEpiWarps * 2 * kBoxBytes + 1024;
+static_assert(kSmemBytes <= 232448, "shared memory of one CTA");
+
+enum Kind { LSE = 0, DLOGITS = 1, GRADS = 2 };
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct Params {
+  int tokens, d, vocab;
+  int units;                    // work units of this launch: CTA pair c takes c, c + pairs, ...
+  // LSE, DLOGITS: tiles (token tile, vocabulary tile); the token tiles go in groups of `group` that pass over all the
+  // vocabulary tiles together, so that a group's rows of X stay in L2 while W streams by once per group.
+  int m_tiles, n_tiles, group;
+  int v0;                       // first vocabulary column of the piece (DLOGITS, GRADS)
+  // GRADS: x_units of dX = splits x m_tiles x d_tiles, then dW: piece_tiles x d_tiles
+  int d_tiles, x_units, splits, kb_per_split, piece_kb, token_kb;
+  int acc_rows;                 // rows of one split's fp32 sums (tokens rounded up to whole tiles)
+  int first_piece;              // the sums are stored, not added
+  float c;                      // logit_scale * log2(e): exponents are taken in base 2
+  const int64_t* targets;
+  const float* lse;             // natural logarithm
+  const float* weight;          // may be null: one
+  float2* part;                 // LSE: [ceil(vocab / 128)][tokens] (maximum, sum), base 2
+  float* target_logit;          // LSE: [tokens], base 2
+  float* corr;                  // DLOGITS: [tokens] what rounding took from the target's element of D
+  const float* denom;           // GRADS: may be null; gradients are multiplied by scale / denom
+  float scale;
+  int* status;
+};
+
+struct Unit {
+  bool x;          // GRADS: a tile of dX (else of dW)
+  int m0, n0;      // first row and column of the pair's tile
+  int bn;          // columns (a multiple of 64, at most 256)
+  int kb0, kb1;    // k-blocks
+  int split;
+};
+
+template <int KIND>
+__device__ __forceinline__ Unit decode(const Params& p, int u) {
+  Unit t;
+  t.split = 0;
+  t.x = false;
+  t.bn = kTile;
+  if (KIND != GRADS) {
+    const int per_group = p.group * p.n_tiles, g = u / per_group, r = u - g * per_group;
+    const int gm = min(p.group, p.m_tiles - g * p.group);
+    t.m0 = (g * p.group + r % gm) * kTile;
+    t.n0 = (r / gm) * kTile;
+    t.kb0 = 0;
+    t.kb1 = (p.d + kBK - 1) / kBK;
+    return t;
+  }
+  int nt;
+  if (u < p.x_units) {
+    t.x = true;
+    nt = u % p.d_tiles;
+    const int r = u / p.d_tiles;
+    t.m0 = (r % p.m_tiles) * kTile;
+    t.split = r / p.m_tiles;
+    t.kb0 = t.split * p.kb_per_split;
+    t.kb1 = min(p.piece_kb, t.kb0 + p.kb_per_split);
+  } else {
+    const int v = u - p.x_units;
+    nt = v % p.d_tiles;
+    t.m0 = (v / p.d_tiles) * kTile;
+    t.kb0 = 0;
+    t.kb1 = p.token_kb;
+  }
+  t.n0 = nt * kTile;
+  t.bn = min(kTile, (p.d - t.n0 + 63) & ~63);
+  return t;
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void tma_reduce_add_2d(const CUtensorMap* map, uint32_t src, int x, int y) {
+  asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3}], [%1];"
+               ::"l"(reinterpret_cast<uint64_t>(map)), "r"(src), "r"(x), "r"(y)
+               : "memory");
+}
+
+// LSE, DLOGITS: tmap_a = X (64 x 128 boxes), tmap_b = W (64 x 128 boxes), tmap_out = D (DLOGITS).
+// GRADS: tmap_a = D as rows of tokens (64 x 128 boxes), tmap_a2 = D read MN-major (64 x 64 boxes), tmap_b = W, tmap_b2 = X
+// (both 64 x 64 boxes, MN-major), tmap_out = the fp32 sums of dX (16 x 32 boxes), tmap_out2 = dW (32 x 32 boxes).
+template <int KIND>
+__global__ void __launch_bounds__(kThreads, 1)
+    ce_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
+              const __grid_constant__ CUtensorMap tmap_a2, const __grid_constant__ CUtensorMap tmap_b2,
+              const __grid_constant__ CUtensorMap tmap_out, const __grid_constant__ CUtensorMap tmap_out2, const Params p) {
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* smem_gen = smem_raw + (smem_base - ptx::smem_u32(smem_raw));
+  const uint32_t bar_base = smem_base + kStages * kStageBytes;
+  auto full_bar = [&](int s) { return bar_base + 8u * s; };
+  auto empty_bar = [&](int s) { return bar_base + 8u * (kStages + s); };
+  auto tfull_bar = [&](int a) { return bar_base + 8u * (2 * kStages + a); };
+  auto tempty_bar = [&](int a) { return bar_base + 8u * (2 * kStages + 2 + a); };
+  constexpr int kSlot = 8 * (2 * kStages + 4);
+  volatile uint32_t* tmem_slot_gen = reinterpret_cast<volatile uint32_t*>(smem_gen + kStages * kStageBytes + kSlot);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_gen + kStages * kStageBytes + kSlot + 4);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = ptx::cluster_ctarank();
+  const int pair = int(blockIdx.x) >> 1, pairs = int(gridDim.x) >> 1;
+  auto on_leader = [&](uint32_t bar) { return ptx::map_to_rank(bar, 0u); };
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      ptx::mbar_init(full_bar(s), 1);
+      ptx::mbar_init(empty_bar(s), 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      ptx::mbar_init(tfull_bar(a), 1);
+      ptx::mbar_init(tempty_bar(a), 2 * kEpiWarps);   // the epilogue warps of both CTAs
+    }
+    *abort_flag = 0;
+    ptx::fence_barrier_init();
+    ptx::prefetch_tensormap(&tmap_a);
+    ptx::prefetch_tensormap(&tmap_b);
+    if (KIND == GRADS) {
+      ptx::prefetch_tensormap(&tmap_a2);
+      ptx::prefetch_tensormap(&tmap_b2);
+      ptx::prefetch_tensormap(&tmap_out2);
+    }
+    if (KIND != LSE) ptx::prefetch_tensormap(&tmap_out);
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc_pair(bar_base + kSlot, kTmemCols);
+    ptx::tmem_relinquish_alloc_permit_pair();
+  }
+  ptx::tcgen05_fence_before_sync();
+  ptx::cluster_sync_all();   // the peer's barriers are initialised before anything is signalled there
+  ptx::tcgen05_fence_after_sync();
+  const uint32_t tmem_base = *tmem_slot_gen;
+  auto give_up = [&]() {
+    *abort_flag = 1;
+    atomicExch(p.status, kDevTimeout);
+  };
+
+  if (warp == 0) {
+    // ------------------------------------------------------------------ TMA producer
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0, armed = 0;
+      bool ok = true;
+      for (int u = pair; ok && u < p.units; u += pairs) {
+        const Unit t = decode<KIND>(p, u);
+        const int a_row0 = t.m0 + int(rank) * kBM;
+        const int hw = t.bn >> 1, b_row0 = t.n0 + int(rank) * hw;       // this CTA's half of the B rows
+        const int b_chunks = KIND == GRADS ? (hw + 63) >> 6 : 0;
+        const uint32_t bytes = kABytes + (KIND == GRADS ? b_chunks * kChunkBytes : kBBytes);
+        for (int kb = t.kb0; kb < t.kb1; ++kb) {
+          if (!ptx::mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag)) { give_up(); ok = false; break; }
+          const uint32_t a_dst = smem_base + stage * kStageBytes, b_dst = a_dst + kABytes;
+          const uint32_t bar = on_leader(full_bar(stage));   // both CTAs' bytes are counted on the leader's barrier
+          if (rank == 0) ptx::mbar_arrive_expect_tx(full_bar(stage), 2 * bytes);
+          armed |= 1u << stage;
+          const int k0 = kb * kBK;
+          if (KIND != GRADS) {
+            ptx::tma_load_2d_pair(a_dst, &tmap_a, bar, k0, a_row0);
+            ptx::tma_load_2d_pair(b_dst, &tmap_b, bar, k0, p.v0 + b_row0);
+          } else {
+            if (t.x) {
+              ptx::tma_load_2d_pair(a_dst, &tmap_a, bar, k0, a_row0);
+            } else {
+              ptx::tma_load_2d_pair(a_dst, &tmap_a2, bar, a_row0, k0);
+              ptx::tma_load_2d_pair(a_dst + kChunkBytes, &tmap_a2, bar, a_row0 + 64, k0);
+            }
+            for (int c = 0; c < b_chunks; ++c)
+              ptx::tma_load_2d_pair(b_dst + c * kChunkBytes, t.x ? &tmap_b : &tmap_b2, bar, b_row0 + 64 * c, t.x ? p.v0 + k0 : k0);
+          }
+          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        }
+      }
+      if (!ok) {
+        // wait (bounded, one limit for all stages) for the copies still in flight before the CTA leaves
+        const uint64_t t0 = ptx::globaltimer_ns();
+        for (int s = 0; s < kStages; ++s) {
+          if (!(armed & (1u << s))) continue;
+          const uint32_t ph = (s < stage) ? phase : (phase ^ 1u);
+          while (!ptx::mbar_try_wait(full_bar(s), ph) && ptx::globaltimer_ns() - t0 < ptx::kWaitLimitNs) {}
+        }
+      } else {
+        // stay until the leader's tensor core has released every stage this CTA filled: its arrivals must not reach the
+        // memory of a CTA that left
+        for (int s = 0; s < kStages && ok; ++s) {
+          if (!(armed & (1u << s))) continue;
+          const uint32_t ph = (s < stage) ? phase : (phase ^ 1u);
+          if (!ptx::mbar_wait(empty_bar(s), ph, abort_flag)) { give_up(); ok = false; }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------ UMMA issuer (the leader's)
+    if (lane == 0 && rank == 0) {
+      int stage = 0, it = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int u = pair; ok && u < p.units; u += pairs, ++it) {
+        const Unit t = decode<KIND>(p, u);
+        const bool a_mn = KIND == GRADS && !t.x;
+        constexpr bool b_mn = KIND == GRADS;
+        const uint32_t idesc = ptx::make_idesc_bf16(kTile, t.bn, a_mn, b_mn);
+        const uint32_t a_lbo = a_mn ? kChunkBytes : 16, a_step = (a_mn ? kUmmaK * 128 : kUmmaK * 2) >> 4;
+        constexpr uint32_t b_lbo = b_mn ? kChunkBytes : 16, b_step = (b_mn ? kUmmaK * 128 : kUmmaK * 2) >> 4;
+        const int acc = it & 1;
+        const uint32_t d_tmem = tmem_base + acc * kAccCols;
+        if (!ptx::mbar_wait_cluster(tempty_bar(acc), ((it >> 1) & 1) ^ 1u, abort_flag)) { give_up(); ok = false; break; }
+        ptx::tcgen05_fence_after_sync();
+        for (int kb = t.kb0; kb < t.kb1; ++kb) {
+          if (!ptx::mbar_wait_cluster(full_bar(stage), phase, abort_flag)) { give_up(); ok = false; break; }
+          ptx::tcgen05_fence_after_sync();
+          const uint32_t a_addr = smem_base + stage * kStageBytes, b_addr = a_addr + kABytes;
+          const uint64_t da = ptx::make_smem_desc(a_addr, a_lbo, 1024), db = ptx::make_smem_desc(b_addr, b_lbo, 1024);
+#pragma unroll
+          for (int k = 0; k < kBK / kUmmaK; ++k)
+            ptx::umma_bf16_pair(d_tmem, da + uint64_t(k * a_step), db + uint64_t(k * b_step), idesc, kb > t.kb0 || k > 0);
+          ptx::umma_commit_pair(empty_bar(stage), 3);
+          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        }
+        if (ok) ptx::umma_commit_pair(tfull_bar(acc), 3);
+      }
+    }
+  } else {
+    // ------------------------------------------------------------------ epilogue
+    const int quarter = warp & 3;                       // TMEM lanes [32 * quarter, + 32) are the ones this warp may read
+    const int half = (warp - kEpiWarp0) >> 2;           // columns [128 * half, + 128) of the tile
+    uint8_t* out_gen = smem_gen + kOutOffset + (warp - kEpiWarp0) * 2 * kBoxBytes;
+    const uint32_t out_addr = smem_base + kOutOffset + (warp - kEpiWarp0) * 2 * kBoxBytes;
+    uint32_t n_stores = 0;
+    float f = 0.f;
+    if (KIND == GRADS) {
+      const float dn = p.denom ? __ldg(p.denom) : 1.f;
+      f = dn > 0.f ? p.scale / dn : 0.f;
+    }
+    // one 32-row box of 64 bytes per row, staged with the 64-byte swizzle (16-byte unit j of row l at j ^ ((l >> 1) & 3))
+    auto stage_box = [&](const uint32_t (&w)[16]) {
+      const uint32_t box = (n_stores & 1u) * kBoxBytes;
+      if (lane == 0) ptx::tma_store_wait_read<1>();   // the store that last used this box has read it
+      __syncwarp();
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<uint4*>(out_gen + box + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4)) =
+            make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+      ptx::fence_proxy_async_smem();
+      __syncwarp();
+      ++n_stores;
+      return out_addr + box;
+    };
+    auto pack = [](const uint32_t (&v)[32], uint32_t (&w)[16]) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+        w[i] = *reinterpret_cast<const uint32_t*>(&h);
+      }
+    };
+    int it = 0;
+    for (int u = pair; u < p.units; u += pairs, ++it) {
+      const Unit t = decode<KIND>(p, u);
+      const int acc = it & 1;
+      const int row0 = t.m0 + int(rank) * kBM + quarter * 32, row = row0 + lane;
+      const int col0 = t.n0 + half * 128;               // of the output; LSE, DLOGITS: of the piece
+      // what the row needs besides the accumulator, fetched before the wait for it
+      int64_t y = -1;
+      float lse2 = 0.f, w = 0.f;
+      if (KIND != GRADS && row < p.tokens) {
+        y = __ldg(p.targets + row);
+        if (y < 0 || y >= p.vocab) y = -1;              // not trained on
+        if (KIND == DLOGITS && y >= 0) {
+          lse2 = __ldg(p.lse + row) * kLog2e;
+          w = p.weight ? __ldg(p.weight + row) : 1.f;
+        }
+      }
+      const bool full_ok = ptx::mbar_wait_cluster(tfull_bar(acc), (it >> 1) & 1, abort_flag);
+      if (!__all_sync(0xFFFFFFFFu, full_ok)) { give_up(); break; }
+      ptx::tcgen05_fence_after_sync();
+      const uint32_t taddr = tmem_base + (uint32_t(quarter * 32) << 16) + acc * kAccCols + half * 128;
+      uint32_t v[32];
+      if (KIND != GRADS) {
+        const int valid = min(128, p.vocab - (p.v0 + col0));          // columns of this half that exist
+        const int tc = y >= 0 ? int(max(int64_t(-1), min(int64_t(1) << 20, y - (p.v0 + col0)))) : -1;   // the target's column here
+        if (KIND == LSE) {
+          float m = -INFINITY, s = 0.f;
+          for (int c0 = 0; c0 < valid; c0 += 32) {
+            __syncwarp();
+            ptx::tmem_ld_x32(taddr + c0, v);
+            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * p.c);
+            if (valid - c0 < 32) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (c0 + i >= valid) v[i] = __float_as_uint(-INFINITY);
+            }
+            if (__any_sync(0xFFFFFFFFu, tc >= c0 && tc < c0 + 32)) {
+              float tl = 0.f;
+#pragma unroll
+              for (int i = 0; i < 32; ++i) tl = tc == c0 + i ? __uint_as_float(v[i]) : tl;
+              if (tc >= c0 && tc < c0 + 32) p.target_logit[row] = tl;
+            }
+            float top = m;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(v[i]));
+            s *= exp2_fast(m - top);      // m = -inf at first: 0 (an all -inf row gives NaN, as the definition's difference does)
+            m = top;
+            float s1 = 0.f;
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) {
+              s += exp2_fast(__uint_as_float(v[i]) - m);
+              s1 += exp2_fast(__uint_as_float(v[i + 1]) - m);
+            }
+            s += s1;
+          }
+          if (valid > 0 && row < p.tokens) p.part[int64_t((p.v0 + col0) >> 7) * p.tokens + row] = make_float2(m, s);
+        } else {
+          for (int c0 = 0; c0 < 128; c0 += 32) {
+            __syncwarp();
+            ptx::tmem_ld_x32(taddr + c0, v);
+            ptx::tmem_ld_wait();
+            // rows that are not trained on and columns past the vocabulary are zero whatever the logit is
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(w * exp2_fast(fmaf(__uint_as_float(v[i]), p.c, -lse2)));
+            if (valid - c0 < 32) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (c0 + i >= valid) v[i] = 0u;
+            }
+            if (__any_sync(0xFFFFFFFFu, tc >= c0 && tc < c0 + 32)) {
+              float e = 0.f;
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (tc == c0 + i) {
+                  e = __uint_as_float(v[i]) - w;
+                  if (p.vocab == 1 && e == e) e = 0.f;   // one word is certain: the difference would be its rounding only
+                  v[i] = __float_as_uint(e);
+                }
+              if (tc >= c0 && tc < c0 + 32) p.corr[row] = e - __bfloat162float(__float2bfloat16_rn(e));
+            }
+            if (y < 0) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] = 0u;
+            }
+            uint32_t pk[16];
+            pack(v, pk);
+            const uint32_t src = stage_box(pk);
+            if (lane == 0) {
+              if (row0 < p.tokens) ptx::tma_store_2d(&tmap_out, src, col0 + c0, row0);
+              ptx::tma_store_commit();
+            }
+          }
+        }
+      } else {
+        const int cols = min(128, p.d - col0);          // columns of this half that exist (may be negative)
+        if (t.x) {
+          for (int c0 = 0; c0 < cols; c0 += 32) {
+            __syncwarp();
+            ptx::tmem_ld_x32(taddr + c0, v);
+            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+              if (c0 + 16 * q >= cols) break;
+              uint32_t w16[16];
+#pragma unroll
+              for (int i = 0; i < 16; ++i) w16[i] = v[16 * q + i];
+              const uint32_t src = stage_box(w16);
+              if (lane == 0) {
+                const int orow = t.split * p.acc_rows + row0;
+                if (p.first_piece) ptx::tma_store_2d(&tmap_out, src, col0 + c0 + 16 * q, orow);
+                else tma_reduce_add_2d(&tmap_out, src, col0 + c0 + 16 * q, orow);
+                ptx::tma_store_commit();
+              }
+            }
+          }
+        } else {
+          for (int c0 = 0; c0 < cols; c0 += 32) {
+            __syncwarp();
+            ptx::tmem_ld_x32(taddr + c0, v);
+            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
+            uint32_t pk[16];
+            pack(v, pk);
+            const uint32_t src = stage_box(pk);
+            if (lane == 0) {
+              if (p.v0 + row0 < p.vocab) ptx::tma_store_2d(&tmap_out2, src, col0 + c0, p.v0 + row0);
+              ptx::tma_store_commit();
+            }
+          }
+        }
+      }
+      ptx::tcgen05_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive_cluster(on_leader(tempty_bar(acc)));
+    }
+    if (KIND != LSE && lane == 0) ptx::tma_store_wait_read<0>();   // shared memory must outlive the stores' reads
+  }
+
+  ptx::tcgen05_fence_before_sync();
+  ptx::cluster_sync_all();   // neither CTA frees tensor memory or leaves while the other may still signal or read it
+  if (warp == 1) {
+    __syncwarp();
+    ptx::tcgen05_fence_after_sync();
+    ptx::tmem_dealloc_pair(tmem_base, kTmemCols);
+  }
+}
+
+}  // namespace ce
+}  // namespace acx
