@@ -274,7 +274,7 @@ ACX_API size_t acx_rows_workspace_bytes(const acx_rows_desc* desc, int op);
 
 /* 8-bit checkpoint of a matrix: codes [rows x cols] int8, dense, and one fp32 scale per row and group of ACX_Q8_GROUP
  * columns, scales [rows x ceil(cols / ACX_Q8_GROUP)].  With a = max |x| of a group:
- *     scale = a / 127,  code = rint(x * (127 * (1 / a))),  value = code * scale,
+ *     scale = a * (1 / 127),  code = rint(x * (127 * (1 / a))),  value = code * scale,
  * each step one binary32 operation (so the codes are reproducible bit for bit), the scale at most the largest float whose
  * 127-fold is finite; the value is within a / 254 of x (and a
  * few units in the last place).  Groups with a < 2^-100 are stored as zeros.  A group that holds an infinity or a NaN

@@ -1,6 +1,6 @@
 """Oracle for the row operators, numpy.  TEST INFRASTRUCTURE.
 
-8-bit checkpoint: per row, groups of 128 columns; a = max |x|, scale = a / 127, code = rint(x * (127 * (1 / a))), each step one
+8-bit checkpoint: per row, groups of 128 columns; a = max |x|, scale = a * (1 / 127), code = rint(x * (127 * (1 / a))), each step one
 binary32 operation, the scale at most MAX_SCALE (these are whole decisions of the format, so they are made in binary32 here too); everything after
 the codes is float64.  A group with a < 2^-100 is zeros; one with an infinity or a NaN reads back as NaN.
 
@@ -33,7 +33,7 @@ def q8_encode(x):
             inv = np.float32(127) * (np.float32(1) / safe)
             k = np.rint(part * inv[:, None])
             codes[:, g * GROUP:(g + 1) * GROUP] = np.where(live[:, None], k, 0).astype(np.int8)
-            scales[:, g] = np.where(bad, np.float32(np.nan), np.where(live, np.minimum(a / np.float32(127), MAX_SCALE), np.float32(0)))
+            scales[:, g] = np.where(bad, np.float32(np.nan), np.where(live, np.minimum(a * (np.float32(1) / np.float32(127)), MAX_SCALE), np.float32(0)))
     return codes, scales
 
 

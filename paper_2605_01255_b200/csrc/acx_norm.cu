@@ -49,50 +49,70 @@ struct FwdArgs {
   float eps, alpha;
 };
 
-// One row per thread block; a thread holds NV vectors of 8 columns, threadIdx.x + i * blockDim.x.
-template <typename T, int NV, bool JOIN, bool KEEP>
-__global__ void __launch_bounds__(NV == 4 ? 1024 : 512, 1) norm_join_fwd_kernel(const FwdArgs a) {
+// One row per thread block; a thread holds NV vectors of 8 columns, threadIdx.x + i * blockDim.x: 16 consecutive lanes
+// hold a group of an 8-bit checkpoint.  Bound by HBM; what it needs for that is enough loads under way, so a row is
+// spread over few threads with several vectors each (about 128 threads) and many rows are resident per SM; the weight
+// vectors are asked for before the barrier that the row's sums wait at.
+template <typename T, int NV, int MAXT, bool JOIN, bool KEEP>
+__global__ void __launch_bounds__(MAXT) norm_join_fwd_kernel(const FwdArgs a) {
   __shared__ float red[2][32];
   const int64_t row = blockIdx.x, at = row * a.cols;
   const int ng = (a.cols + kGroup - 1) / kGroup;
   const float inv_n = 1.f / float(a.cols);
-  float t[NV][8], b[JOIN ? NV : 1][8];
+  Raw<T> h[NV], b[JOIN ? NV : 1];
   auto col_of = [&](int i) { return (int(threadIdx.x) + i * int(blockDim.x)) * kVec; };
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = col_of(i);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      t[i][e] = 0.f;
-      if (JOIN) b[i][e] = 0.f;
-    }
+    h[i].zero();
+    if (JOIN) b[i].zero();
     if (c < a.cols) {
-      load8(static_cast<const T*>(a.h) + at + c, t[i]);
-      if (JOIN) load8(static_cast<const T*>(a.b) + at + c, b[i]);
+      h[i].load(static_cast<const T*>(a.h) + at + c);
+      if (JOIN) b[i].load(static_cast<const T*>(a.b) + at + c);
+    }
+  }
+  Raw<T> w1[JOIN ? NV : 1], w2[JOIN ? NV : 1];
+  if (JOIN) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = col_of(i);
+      if (c >= a.cols) continue;
+      if (a.w_post) w1[i].load(static_cast<const T*>(a.w_post) + c);
+      if (a.gate) w2[i].load(static_cast<const T*>(a.gate) + c);
     }
   }
   if (KEEP) {
-    auto keep = [&](const float (&v)[8], int c, int8_t* codes, float* scales) {
-      const GroupScale g = group_scale(group_amax_bits(v));
-      if (c < a.cols) {
-        *reinterpret_cast<uint2*>(codes + at + c) = encode8(v, g.inv);
-        if (threadIdx.x % kLanes == 0) scales[row * ng + c / kGroup] = g.scale;
-      }
+    auto keep = [&](const Raw<T>& x, uint32_t amax, int c, int8_t* codes, float* scales) {
+      const GroupScale g = group_scale(amax);
+      if (c >= a.cols) return;
+      float v[8];
+      x.get(v);
+      *reinterpret_cast<uint2*>(codes + at + c) = encode8(v, g.inv);
+      if (threadIdx.x % 16 == 0) scales[row * ng + c / kGroup] = g.scale;
     };
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      keep(t[i], col_of(i), a.Hq, a.Hs);
-      if (JOIN) keep(b[i], col_of(i), a.Bq, a.Bs);
+      uint32_t mh = h[i].amax_bits(), mb = JOIN ? b[JOIN ? i : 0].amax_bits() : 0u;
+      if (JOIN) max_pair_over<T, 16>(mh, mb);
+      else mh = max_over<16>(mh);
+      keep(h[i], mh, col_of(i), a.Hq, a.Hs);
+      if (JOIN) keep(b[JOIN ? i : 0], mb, col_of(i), a.Bq, a.Bs);
     }
   }
+  float t[NV][8];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) h[i].get(t[i]);
   if (JOIN) {
     float r_b = 1.f;
     if (a.w_post) {
       float s[1] = {0.f};
 #pragma unroll
-      for (int i = 0; i < NV; ++i)
+      for (int i = 0; i < NV; ++i) {
+        float v[8];
+        b[JOIN ? i : 0].get(v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s[0] += b[i][e] * b[i][e];
+        for (int e = 0; e < 8; ++e) s[0] += v[e] * v[e];
+      }
       block_sum(s, red[0]);
       r_b = rsqrtf(s[0] * inv_n + a.eps);
       if (KEEP && threadIdx.x == 0) a.rstd_post[row] = r_b;
@@ -101,26 +121,29 @@ __global__ void __launch_bounds__(NV == 4 ? 1024 : 512, 1) norm_join_fwd_kernel(
     for (int i = 0; i < NV; ++i) {
       const int c = col_of(i);
       if (c >= a.cols) continue;
-      float k[8];
+      float k[8], v[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) k[e] = a.alpha * r_b;
       if (a.w_post) {
-        float w[8];
-        load8(static_cast<const T*>(a.w_post) + c, w);
+        w1[JOIN ? i : 0].get(v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) k[e] *= w[e];
+        for (int e = 0; e < 8; ++e) k[e] *= v[e];
       }
       if (a.gate) {
-        float w[8];
-        load8(static_cast<const T*>(a.gate) + c, w);
+        w2[JOIN ? i : 0].get(v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) k[e] *= w[e];
+        for (int e = 0; e < 8; ++e) k[e] *= v[e];
       }
+      b[JOIN ? i : 0].get(v);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) t[i][e] += k[e] * b[i][e];
+      for (int e = 0; e < 8; ++e) t[i][e] += k[e] * v[e];
       store8(static_cast<T*>(a.h_out) + at + c, t[i]);
     }
   }
+  Raw<T> w3[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if (col_of(i) < a.cols) w3[i].load(static_cast<const T*>(a.w_pre) + col_of(i));
   float s[1] = {0.f};
 #pragma unroll
   for (int i = 0; i < NV; ++i)
@@ -134,7 +157,7 @@ __global__ void __launch_bounds__(NV == 4 ? 1024 : 512, 1) norm_join_fwd_kernel(
     const int c = col_of(i);
     if (c >= a.cols) continue;
     float w[8];
-    load8(static_cast<const T*>(a.w_pre) + c, w);
+    w3[i].get(w);
 #pragma unroll
     for (int e = 0; e < 8; ++e) w[e] *= t[i][e] * r_t;
     store8(static_cast<T*>(a.y) + at + c, w);
@@ -152,69 +175,148 @@ struct BwdArgs {
   float alpha;
 };
 
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, int bytes) {   // 8 or 16 bytes, both aligned to them
+  if (bytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+}
+
 // Persistent: a block walks the rows blockIdx.x, + gridDim.x, ... and keeps the column sums of its columns in registers.
 // Both means of a row come out of one reduction: with dt = a + f that, a = dh_next + r_t dy w_pre and f = -r_t m1,
 //     sum(k dt bhat) = sum(k a bhat) + f sum(k that bhat),
-// so a row costs one barrier instead of two.
-template <typename T, int NV, bool JOIN>
-__global__ void __launch_bounds__(NV == 4 ? 1024 : 512, 1) norm_join_bwd_kernel(const BwdArgs a) {
+// so a row costs one barrier instead of two.  The registers that the sums and the weights take leave room for few
+// threads, too few to keep HBM busy with their own loads: with DEPTH > 0 every thread copies its vectors of the next
+// DEPTH rows into shared memory asynchronously (its own slots, so no barrier guards them).
+template <typename T, int NV, int MAXT, int MINB, int DEPTH, bool JOIN>
+__global__ void __launch_bounds__(MAXT, MINB) norm_join_bwd_kernel(const BwdArgs a) {
+  extern __shared__ __align__(16) uint8_t ring[];
   __shared__ float red[2][3 * 32];
-  const int ng = (a.cols + kGroup - 1) / kGroup;
+  constexpr int kParts = sizeof(T) == 2 ? 1 : 2;          // 16-byte parts of a vector of T
+  constexpr int kSlot = 2 * 16 * kParts + (JOIN ? 16 : 8);   // dy, dh_next, codes of h and b
+  const int ng = (a.cols + kGroup - 1) / kGroup, threads = int(blockDim.x);
   const float inv_n = 1.f / float(a.cols);
-  float sum_pre[NV][8], sum_c[JOIN ? NV : 1][8];
-#pragma unroll
-  for (int i = 0; i < NV; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      sum_pre[i][e] = 0.f;
-      if (JOIN) sum_c[i][e] = 0.f;
-    }
-  auto col_of = [&](int i) { return (int(threadIdx.x) + i * int(blockDim.x)) * kVec; };
-  int turn = 0;
-  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
-    const int64_t at = row * a.cols;
-    const float r_t = __ldg(a.rstd_pre + row), r_b = (JOIN && a.w_post) ? __ldg(a.rstd_post + row) : 1.f;
-    float that[NV][8], av[NV][8], bhat[JOIN ? NV : 1][8], k[JOIN ? NV : 1][8];
-    float s[3] = {0.f, 0.f, 0.f};
+  auto col_of = [&](int i) { return (int(threadIdx.x) + i * threads) * kVec; };
+  // Shared memory: stage, vector, then dy parts | dh_next parts | codes of h | codes of b, each for all threads
+  const uint32_t ring0 = static_cast<uint32_t>(__cvta_generic_to_shared(ring));
+  auto base_of = [&](int stage, int i) { return uint32_t((stage * NV + i) * threads * kSlot); };
+  auto fetch = [&](int64_t row, int stage) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = col_of(i);
       if (c >= a.cols) continue;
-      float dy[8], w[8];
-      const uint2 hq = __ldg(reinterpret_cast<const uint2*>(a.Hq + at + c));
-      const float hs = __ldg(a.Hs + row * ng + c / kGroup);
-      load8(static_cast<const T*>(a.dy) + at + c, dy);
+      const int64_t at = row * a.cols + c;
+      const uint32_t s0 = ring0 + base_of(stage, i);
+      const uint8_t* dy = reinterpret_cast<const uint8_t*>(static_cast<const T*>(a.dy) + at);
+      const uint8_t* dn = reinterpret_cast<const uint8_t*>(static_cast<const T*>(a.dh_next) + at);
+#pragma unroll
+      for (int q = 0; q < kParts; ++q) {
+        copy_async(s0 + (q * threads + threadIdx.x) * 16, dy + 16 * q, 16);
+        if (a.dh_next) copy_async(s0 + ((kParts + q) * threads + threadIdx.x) * 16, dn + 16 * q, 16);
+      }
+      copy_async(s0 + 2 * kParts * threads * 16 + threadIdx.x * 8, a.Hq + at, 8);
+      if (JOIN) copy_async(s0 + (2 * kParts * 16 + 8) * threads + threadIdx.x * 8, a.Bq + at, 8);
+    }
+  };
+  auto vec_at = [&](uint32_t off, float (&v)[8]) {     // a vector of T in the ring
+    if (sizeof(T) == 2) {
+      Raw<__nv_bfloat16> r;
+      r.u = *reinterpret_cast<const uint4*>(ring + off + threadIdx.x * 16);
+      r.get(v);
+    } else {
+      Raw<float> r;
+      r.a = *reinterpret_cast<const float4*>(ring + off + threadIdx.x * 16);
+      r.b = *reinterpret_cast<const float4*>(ring + off + (threads + threadIdx.x) * 16);
+      r.get(v);
+    }
+  };
+
+  // what a column is multiplied with in every row
+  float k[JOIN ? NV : 1][8], wp[NV][8], sum_pre[NV][8], sum_c[JOIN ? NV : 1][8];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = col_of(i);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      sum_pre[i][e] = wp[i][e] = 0.f;
+      if (JOIN) {
+        sum_c[i][e] = 0.f;
+        k[i][e] = a.alpha;
+      }
+    }
+    if (c >= a.cols) continue;
+    load8(static_cast<const T*>(a.w_pre) + c, wp[i]);
+    float w[8];
+    if (JOIN && a.w_post) {
+      load8(static_cast<const T*>(a.w_post) + c, w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) k[i][e] *= w[e];
+    }
+    if (JOIN && a.gate) {
+      load8(static_cast<const T*>(a.gate) + c, w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) k[i][e] *= w[e];
+    }
+  }
+  const int64_t step = gridDim.x;
+#pragma unroll
+  for (int s = 0; s < DEPTH; ++s) {
+    if (blockIdx.x + s * step < a.rows) fetch(blockIdx.x + s * step, s);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  // a row's scales are asked for one row ahead
+  float hs[NV], bs[JOIN ? NV : 1], r_t = 0.f, r_b = 1.f;
+  auto scales = [&](int64_t row) {
+    if (row >= a.rows) return;
+    r_t = __ldg(a.rstd_pre + row);
+    if (JOIN && a.w_post) r_b = __ldg(a.rstd_post + row);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = col_of(i);
+      if (c >= a.cols) continue;
+      hs[i] = __ldg(a.Hs + row * ng + c / kGroup);
+      if (JOIN) bs[i] = __ldg(a.Bs + row * ng + c / kGroup);
+    }
+  };
+  scales(blockIdx.x);
+  int turn = 0, stage = 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += step, turn ^= 1) {
+    const int64_t at = row * a.cols;
+    float that[NV][8], av[NV][8], bhat[JOIN ? NV : 1][8];
+    float s[3] = {0.f, 0.f, 0.f};
+    if (DEPTH > 0) asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH > 0 ? DEPTH - 1 : 0) : "memory");
+    const float rt = r_t, rb = r_b;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = col_of(i);
+      if (c >= a.cols) continue;
+      float dy[8];
+      uint2 hq, bq;
 #pragma unroll
       for (int e = 0; e < 8; ++e) av[i][e] = 0.f;
-      if (a.dh_next) load8(static_cast<const T*>(a.dh_next) + at + c, av[i]);
-      decode8(hq, hs, that[i]);
+      if (DEPTH > 0) {
+        const uint32_t s0 = base_of(stage, i);
+        vec_at(s0, dy);
+        if (a.dh_next) vec_at(s0 + kParts * threads * 16, av[i]);
+        hq = *reinterpret_cast<const uint2*>(ring + s0 + 2 * kParts * threads * 16 + threadIdx.x * 8);
+        if (JOIN) bq = *reinterpret_cast<const uint2*>(ring + s0 + (2 * kParts * 16 + 8) * threads + threadIdx.x * 8);
+      } else {
+        load8(static_cast<const T*>(a.dy) + at + c, dy);
+        if (a.dh_next) load8(static_cast<const T*>(a.dh_next) + at + c, av[i]);
+        hq = __ldg(reinterpret_cast<const uint2*>(a.Hq + at + c));
+        if (JOIN) bq = __ldg(reinterpret_cast<const uint2*>(a.Bq + at + c));
+      }
+      decode8(hq, hs[i], that[i]);
       if (JOIN) {
-        const uint2 bq = __ldg(reinterpret_cast<const uint2*>(a.Bq + at + c));
-        const float bs = __ldg(a.Bs + row * ng + c / kGroup);
-        decode8(bq, bs * r_b, bhat[i]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) k[i][e] = a.alpha;
-        if (a.w_post) {
-          load8(static_cast<const T*>(a.w_post) + c, w);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) k[i][e] *= w[e];
-        }
-        if (a.gate) {
-          load8(static_cast<const T*>(a.gate) + c, w);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) k[i][e] *= w[e];
-        }
+        decode8(bq, bs[i] * rb, bhat[i]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) that[i][e] += k[i][e] * bhat[i][e];
       }
-      load8(static_cast<const T*>(a.w_pre) + c, w);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        that[i][e] *= r_t;
-        const float gy = dy[e] * w[e];
+        that[i][e] *= rt;
+        const float gy = dy[e] * wp[i][e];
         s[0] += gy * that[i][e];
         sum_pre[i][e] += dy[e] * that[i][e];
-        av[i][e] += r_t * gy;
+        av[i][e] += rt * gy;
         if (JOIN) {
           const float kb = k[i][e] * bhat[i][e];
           s[1] += av[i][e] * kb;
@@ -222,8 +324,14 @@ __global__ void __launch_bounds__(NV == 4 ? 1024 : 512, 1) norm_join_bwd_kernel(
         }
       }
     }
+    scales(row + step);
     block_sum(s, red[turn]);
-    const float f = -r_t * s[0] * inv_n, m2 = JOIN ? (s[1] + f * s[2]) * inv_n : 0.f;
+    if (DEPTH > 0) {   // this stage's values are in registers: its slots take the row DEPTH turns on
+      if (row + DEPTH * step < a.rows) fetch(row + DEPTH * step, stage);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      if (++stage == DEPTH) stage = 0;
+    }
+    const float f = -rt * s[0] * inv_n, m2 = JOIN ? (s[1] + f * s[2]) * inv_n : 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = col_of(i);
@@ -236,12 +344,13 @@ __global__ void __launch_bounds__(NV == 4 ? 1024 : 512, 1) norm_join_bwd_kernel(
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           sum_c[i][e] += av[i][e] * bhat[i][e];
-          db[e] = a.w_post ? r_b * (k[i][e] * av[i][e] - bhat[i][e] * m2) : k[i][e] * av[i][e];
+          db[e] = a.w_post ? rb * (k[i][e] * av[i][e] - bhat[i][e] * m2) : k[i][e] * av[i][e];
         }
         store8(static_cast<T*>(a.db) + at + c, db);
       }
     }
   }
+  if (DEPTH > 0) asm volatile("cp.async.wait_all;" ::: "memory");
   float* part = a.part + int64_t(blockIdx.x) * (JOIN ? 2 : 1) * a.cols;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -264,7 +373,13 @@ __global__ void __launch_bounds__(1024) norm_join_columns_kernel(const float* __
   const int c = int(blockIdx.x) * 32 + x;
   float s = 0.f;
   if (c < cols)
-    for (int k = y; k < blocks; k += 32) s += part[(int64_t(k) * planes + plane) * cols + c];
+    for (int k = y; k < blocks; k += 8 * 32) {   // eight loads under way, added in order
+      float v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = k + 32 * u < blocks ? __ldg(part + (int64_t(k + 32 * u) * planes + plane) * cols + c) : 0.f;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s += v[u];
+    }
   red[y][x] = s;
   __syncthreads();
   if (y != 0 || c >= cols) return;
@@ -280,22 +395,21 @@ __global__ void __launch_bounds__(1024) norm_join_columns_kernel(const float* __
   if (dgate) dgate[c] = w_post ? s * float(w_post[c]) : s;
 }
 
-// Vectors per thread and threads per block for a row of `cols` columns (at most 32768): one vector up to 4096 columns, two
-// up to 8192 (512 threads with 128 registers hold both), four beyond (1024 threads, 64 registers).
-struct Shape { int nv, threads; };
-Shape shape_of(int64_t cols) {
-  const int vecs = int(cols / kVec);
-  const int nv = vecs <= 512 ? 1 : (vecs <= 1024 ? 2 : 4);
-  return Shape{nv, ((vecs + nv - 1) / nv + 31) / 32 * 32};
-}
+int round_warp(int threads) { return (threads + 31) / 32 * 32; }
 
+template <typename T, int NV, int MAXT, bool JOIN, bool KEEP>
+void launch_fwd(const FwdArgs& a, cudaStream_t st) {
+  const int threads = round_warp((a.cols / kVec + NV - 1) / NV);
+  norm_join_fwd_kernel<T, NV, MAXT, JOIN, KEEP><<<unsigned(a.rows), threads, 0, st>>>(a);
+}
 template <typename T, bool JOIN, bool KEEP>
 void launch_fwd(const FwdArgs& a, cudaStream_t st) {
-  const Shape s = shape_of(a.cols);
-  const unsigned grid = unsigned(a.rows);
-  if (s.nv == 1) norm_join_fwd_kernel<T, 1, JOIN, KEEP><<<grid, s.threads, 0, st>>>(a);
-  else if (s.nv == 2) norm_join_fwd_kernel<T, 2, JOIN, KEEP><<<grid, s.threads, 0, st>>>(a);
-  else norm_join_fwd_kernel<T, 4, JOIN, KEEP><<<grid, s.threads, 0, st>>>(a);
+  const int vecs = a.cols / kVec;
+  if (vecs <= 128) launch_fwd<T, 1, 128, JOIN, KEEP>(a, st);
+  else if (vecs <= 256) launch_fwd<T, 2, 128, JOIN, KEEP>(a, st);
+  else if (vecs <= 384) launch_fwd<T, 3, 128, JOIN, KEEP>(a, st);
+  else if (vecs <= 1024) launch_fwd<T, 4, 256, JOIN, KEEP>(a, st);
+  else launch_fwd<T, 4, 1024, JOIN, KEEP>(a, st);
 }
 template <typename T>
 void launch_fwd(const FwdArgs& a, cudaStream_t st) {
@@ -308,27 +422,39 @@ void launch_fwd(const FwdArgs& a, cudaStream_t st) {
   }
 }
 
-// Blocks of the backward: as many as are resident (2048 threads per SM, fewer where registers bound it), so that every
-// block walks several rows and the column sums that leave the SMs stay small next to the rows.
-int bwd_blocks(int64_t rows, int64_t cols) {
-  const Shape s = shape_of(cols);
-  const int per_sm = std::max(1, (s.nv == 1 ? 1024 : 512) / s.threads);
-  return int(std::min<int64_t>(rows, int64_t(sm_count()) * per_sm));
+// The backward's shape for a row of `cols` columns (at most 32768): one vector per thread up to 3072 columns, two up to
+// 8192, four beyond; as many blocks as are resident at the registers that leaves (768, 512 or fewer threads per SM), so
+// that every block walks several rows and the column sums that leave the SMs stay small next to the rows.
+struct BwdShape { int nv, threads, per_sm; };
+BwdShape bwd_shape(int64_t cols) {
+  const int vecs = int(cols / kVec);
+  const int nv = vecs <= 384 ? 1 : (vecs <= 1024 ? 2 : 4);
+  const int threads = round_warp((vecs + nv - 1) / nv);
+  return BwdShape{nv, threads, std::max(1, std::min(16, (nv == 1 ? 768 : 512) / threads))};
 }
+int bwd_blocks(int64_t rows, int64_t cols) { return int(std::min<int64_t>(rows, int64_t(sm_count()) * bwd_shape(cols).per_sm)); }
 
-template <typename T>
-void launch_bwd(const BwdArgs& a, cudaStream_t st) {
-  const Shape s = shape_of(a.cols);
-  const int grid = bwd_blocks(a.rows, a.cols);
-  if (a.Bq) {
-    if (s.nv == 1) norm_join_bwd_kernel<T, 1, true><<<grid, s.threads, 0, st>>>(a);
-    else if (s.nv == 2) norm_join_bwd_kernel<T, 2, true><<<grid, s.threads, 0, st>>>(a);
-    else norm_join_bwd_kernel<T, 4, true><<<grid, s.threads, 0, st>>>(a);
-  } else {
-    if (s.nv == 1) norm_join_bwd_kernel<T, 1, false><<<grid, s.threads, 0, st>>>(a);
-    else if (s.nv == 2) norm_join_bwd_kernel<T, 2, false><<<grid, s.threads, 0, st>>>(a);
-    else norm_join_bwd_kernel<T, 4, false><<<grid, s.threads, 0, st>>>(a);
+template <typename T, int NV, int MAXT, int MINB, int DEPTH, bool JOIN>
+cudaError_t launch_bwd(const BwdArgs& a, int threads, cudaStream_t st) {
+  auto kernel = norm_join_bwd_kernel<T, NV, MAXT, MINB, DEPTH, JOIN>;
+  constexpr int kSlot = 2 * 8 * int(sizeof(T)) + (JOIN ? 16 : 8);
+  static DeviceOnce once;
+  if (DEPTH > 0 && once.needed()) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, DEPTH * NV * MAXT * kSlot);
+    if (e != cudaSuccess) return e;
+    once.done();
   }
+  kernel<<<bwd_blocks(a.rows, a.cols), threads, DEPTH * NV * threads * kSlot, st>>>(a);
+  return launched();
+}
+template <typename T, bool JOIN>
+cudaError_t launch_bwd(const BwdArgs& a, cudaStream_t st) {
+  const BwdShape s = bwd_shape(a.cols);
+  constexpr int kDepth = sizeof(T) == 2 ? 4 : 2;
+  if (s.nv == 1) return launch_bwd<T, 1, 384, 2, kDepth, JOIN>(a, s.threads, st);
+  if (s.nv == 2 && s.threads <= 256) return launch_bwd<T, 2, 256, 2, kDepth, JOIN>(a, s.threads, st);
+  if (s.nv == 2) return launch_bwd<T, 2, 512, 1, kDepth, JOIN>(a, s.threads, st);
+  return launch_bwd<T, 4, 1024, 1, 0, JOIN>(a, s.threads, st);
 }
 
 }  // namespace
@@ -349,9 +475,9 @@ cudaError_t norm_join_bwd(const Rows& d, const void* dy, const void* dh_next, co
                           const float* rstd_pre, void* dh, void* db, float* dw_post, float* dgate, float* dw_pre, float alpha, void* ws,
                           cudaStream_t st) {
   BwdArgs a{dy, dh_next, w_post, gate, w_pre, Hq, Bq, Hs, Bs, rstd_post, rstd_pre, dh, db, static_cast<float*>(ws), d.rows, int(d.cols), alpha};
-  if (d.bf16) launch_bwd<__nv_bfloat16>(a, st);
-  else launch_bwd<float>(a, st);
-  cudaError_t e = launched();
+  cudaError_t e;
+  if (d.bf16) e = Bq ? launch_bwd<__nv_bfloat16, true>(a, st) : launch_bwd<__nv_bfloat16, false>(a, st);
+  else e = Bq ? launch_bwd<float, true>(a, st) : launch_bwd<float, false>(a, st);
   if (e != cudaSuccess || (!dw_pre && !dw_post && !dgate)) return e;
   const int planes = Bq ? 2 : 1;
   const dim3 grid(unsigned((d.cols + 31) / 32), unsigned((dw_post || dgate) ? 2 : 1));

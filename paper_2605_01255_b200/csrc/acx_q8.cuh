@@ -3,10 +3,10 @@
 //
 // Format: per row, groups of 128 columns (the last one may be shorter) share one binary32 scale.  With a = max |x| of
 // the group,
-//     scale = a / 127,   code = rint(x * (127 * (1 / a))),
+//     scale = a * (1 / 127),   code = rint(x * (127 * (1 / a))),
 // (the scale at most kMaxScale, so that 127 codes of the largest finite a do not overflow when they are read back), every
-// step one binary32 operation rounded to nearest even, so that the codes are a function of the input alone and
-// any two implementations agree on every bit.  a < 2^-100: the group is stored as zeros (1 / a would overflow on its
+// step one binary32 operation rounded to nearest even (1 / 127 the rounded constant), so that the codes are a function of
+// the input alone and any two implementations agree on every bit.  a < 2^-100: the group is stored as zeros (1 / a would overflow on its
 // way through the subnormals).  An infinity or a NaN in the group: scale = NaN, the group reads back as NaN.
 #pragma once
 #include <cuda_bf16.h>
@@ -17,24 +17,62 @@ namespace q8 {
 
 constexpr int kGroup = 128;            // columns that share a scale
 constexpr int kVec = 8;                // columns a thread handles at a time
-constexpr int kLanes = kGroup / kVec;  // threads of a warp that hold one group
 constexpr uint32_t kTinyBits = (127u - 100u) << 23;   // 2^-100
 constexpr uint32_t kInfBits = 0x7F800000u, kNanBits = 0x7FFFFFFFu;
-constexpr float kMaxScale = 0x1.0204060000000p+121f;            // the largest float whose 127-fold is finite
+constexpr float kMaxScale = 0x1.020406p+121f;   // the largest float whose 127-fold is finite
 
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&v)[8]) {
-  const uint4 u = __ldg(reinterpret_cast<const uint4*>(p));
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+// Eight elements of a row as they are in memory: loads are issued long before the values are needed, and a bf16 vector
+// waits for that in four registers instead of eight.
+template <typename T>
+struct Raw;
+template <>
+struct Raw<__nv_bfloat16> {
+  uint4 u;
+  __device__ __forceinline__ void zero() { u = make_uint4(0u, 0u, 0u, 0u); }
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { u = __ldg(reinterpret_cast<const uint4*>(p)); }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = __uint_as_float(w[i] << 16);
-    v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
   }
-}
-__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
-  const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-  v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  // Largest magnitude, as the bits of a binary32: integer order is the order of magnitudes, with infinity and then NaN on
+  // top, so nothing that is not finite gets lost.
+  __device__ __forceinline__ uint32_t amax_bits() const {
+    const uint32_t m = 0x7FFF7FFFu;
+    const uint32_t a = __vmaxu2(__vmaxu2(u.x & m, u.y & m), __vmaxu2(u.z & m, u.w & m));
+    return max(a << 16, a & 0xFFFF0000u);
+  }
+};
+template <>
+struct Raw<float> {
+  float4 a, b;
+  __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ __forceinline__ void load(const float* p) {
+    a = __ldg(reinterpret_cast<const float4*>(p));
+    b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+  }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  }
+  __device__ __forceinline__ uint32_t amax_bits() const {
+    float v[8];
+    get(v);
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    return m;
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&v)[8]) {
+  Raw<T> r;
+  r.load(p);
+  r.get(v);
 }
 __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
   uint32_t w[4];
@@ -50,15 +88,27 @@ __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
   reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
 }
 
-// Largest magnitude of the group that 16 consecutive lanes hold, as bits: integer order is the order of magnitudes, with
-// infinity and then NaN on top, so nothing that is not finite gets lost.  All lanes of the warp take part.
-__device__ __forceinline__ uint32_t group_amax_bits(const float (&v)[8]) {
-  uint32_t m = 0;
+// Largest of a value over LANES consecutive lanes (a power of two).  All lanes of the warp take part.
+template <int LANES>
+__device__ __forceinline__ uint32_t max_over(uint32_t m) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-#pragma unroll
-  for (int o = kLanes / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+  for (int o = LANES / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
   return m;
+}
+
+// The same for two values at a time; those of bf16 elements have 16 bits and travel together.
+template <typename T, int LANES>
+__device__ __forceinline__ void max_pair_over(uint32_t& a, uint32_t& b) {
+  if (sizeof(T) == 2) {
+    uint32_t m = a | (b >> 16);
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) m = __vmaxu2(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+    a = m & 0xFFFF0000u;
+    b = m << 16;
+  } else {
+    a = max_over<LANES>(a);
+    b = max_over<LANES>(b);
+  }
 }
 
 struct GroupScale { float scale, inv; };
@@ -67,7 +117,7 @@ __device__ __forceinline__ GroupScale group_scale(uint32_t amax_bits) {
   GroupScale g;
   if (amax_bits >= kInfBits) { g.scale = __uint_as_float(kNanBits); g.inv = 0.f; }
   else if (amax_bits < kTinyBits) { g.scale = 0.f; g.inv = 0.f; }
-  else { g.scale = fminf(__fdiv_rn(a, 127.f), kMaxScale); g.inv = __fmul_rn(127.f, __frcp_rn(a)); }
+  else { g.scale = fminf(__fmul_rn(a, 1.f / 127.f), kMaxScale); g.inv = __fmul_rn(127.f, __frcp_rn(a)); }
   return g;
 }
 

@@ -3,8 +3,10 @@
 // whose backward reads G and U from their 8-bit checkpoints:
 //     dU = dH G s,   dG = dH U s (1 + G (1 - s)).
 //
-// All of them are bound by HBM: each element is read once and written once, 16 bytes per thread and access, and 16
-// consecutive lanes hold one group of 128 columns, so a group's scale costs four shuffles and no shared memory.
+// All of them are bound by HBM: each element is read once and written once, 16 bytes per thread and access.  Eight lanes
+// hold one group of 128 columns, two vectors of 8 columns each (64 columns apart, so that the eight lanes read 128
+// contiguous bytes): what a group costs once (three shuffles, its scale, where it is) is spread over 16 elements per
+// thread; with one vector per thread and sixteen lanes the forward of the gated activation was bound by instructions.
 #include <algorithm>
 
 #include "acx_internal.h"
@@ -16,80 +18,70 @@ namespace {
 using namespace q8;
 
 constexpr int kThreads = 256;
-constexpr int kGroupsPerPass = kThreads / kLanes;   // groups a thread block handles at a time
+constexpr int kLanes = 8;                           // threads that hold one group
+constexpr int kHalf = kLanes * kVec;                // columns between a thread's two vectors
+constexpr int kGroupsPerBlock = kThreads / kLanes;
 
-// Where a thread's 8 columns are.  Groups are numbered through all rows (ng per row); a block takes a contiguous run.
+// Where a thread's columns are.  Groups are numbered through all rows (ng per row); a block takes 32 in a row.
 struct Place {
-  int64_t row;
-  int col;      // first of the 8 columns
-  int64_t group;
-  bool live;    // inside the matrix (a partly filled last group has idle lanes)
+  int64_t row, group;
+  int col;
+  bool live[2];   // whether each vector is inside the matrix (a partly filled last group has idle lanes)
 };
-template <int PASSES>
-struct Places {
-  int64_t g0, row0, rows;
-  uint32_t rem0, ng;
-  int cols;
-  __device__ Places(int64_t rows_, int cols_) : rows(rows_), cols(cols_) {
-    ng = uint32_t(cols + kGroup - 1) / kGroup;
-    g0 = int64_t(blockIdx.x) * (kGroupsPerPass * PASSES);
-    row0 = g0 / ng;
-    rem0 = uint32_t(g0 - row0 * ng);
-  }
-  __device__ Place at(int pass) const {
-    const uint32_t k = uint32_t(pass) * kGroupsPerPass + (threadIdx.x / kLanes);
-    const uint32_t off = rem0 + k, dr = off / ng;
-    Place p;
-    p.row = row0 + dr;
-    p.group = g0 + k;
-    p.col = int(off - dr * ng) * kGroup + int(threadIdx.x % kLanes) * kVec;
-    p.live = p.row < rows && p.col < cols;
-    return p;
-  }
+struct Div {      // quotients by ng of numbers below ng + 32
+  uint32_t ng, inv16;   // inv16 = ceil(2^16 / ng)
 };
+__device__ __forceinline__ Place place_of(int64_t rows, int cols, Div d) {
+  const int64_t g0 = int64_t(blockIdx.x) * kGroupsPerBlock, row0 = g0 / d.ng;
+  const uint32_t k = threadIdx.x / kLanes, off = uint32_t(g0 - row0 * d.ng) + k;
+  // off < ng + 32: at most one row further where ng >= 32; else off < 64 and the 16-bit reciprocal is exact
+  const uint32_t dr = d.ng >= 32 ? (off >= d.ng ? 1u : 0u) : (off * d.inv16) >> 16;
+  Place p;
+  p.row = row0 + dr;
+  p.group = g0 + k;
+  p.col = int(off - dr * d.ng) * kGroup + int(threadIdx.x % kLanes) * kVec;
+#pragma unroll
+  for (int v = 0; v < 2; ++v) p.live[v] = p.row < rows && p.col + v * kHalf < cols;
+  return p;
+}
+__device__ __forceinline__ bool first_lane() { return threadIdx.x % kLanes == 0; }
 
-template <typename T, int PASSES>
+template <typename T>
 __global__ void __launch_bounds__(kThreads) q8_store_kernel(const T* __restrict__ X, int64_t ldx, int8_t* __restrict__ codes,
-                                                            float* __restrict__ scales, int64_t rows, int cols) {
-  const Places<PASSES> places(rows, cols);
-  float v[PASSES][8];
+                                                            float* __restrict__ scales, int64_t rows, int cols, Div d) {
+  const Place p = place_of(rows, cols, d);
+  Raw<T> x[2];
 #pragma unroll
-  for (int u = 0; u < PASSES; ++u) {   // every load is under way before the first is used
-    const Place p = places.at(u);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[u][i] = 0.f;
-    if (p.live) load8(X + p.row * ldx + p.col, v[u]);
+  for (int v = 0; v < 2; ++v) {
+    x[v].zero();
+    if (p.live[v]) x[v].load(X + p.row * ldx + p.col + v * kHalf);
   }
+  const GroupScale g = group_scale(max_over<kLanes>(max(x[0].amax_bits(), x[1].amax_bits())));
 #pragma unroll
-  for (int u = 0; u < PASSES; ++u) {
-    const Place p = places.at(u);
-    const GroupScale g = group_scale(group_amax_bits(v[u]));
-    if (!p.live) continue;
-    *reinterpret_cast<uint2*>(codes + p.row * int64_t(cols) + p.col) = encode8(v[u], g.inv);
-    if (threadIdx.x % kLanes == 0) scales[p.group] = g.scale;
+  for (int v = 0; v < 2; ++v) {
+    float f[8];
+    x[v].get(f);
+    if (p.live[v]) *reinterpret_cast<uint2*>(codes + p.row * int64_t(cols) + p.col + v * kHalf) = encode8(f, g.inv);
   }
+  if (first_lane() && p.live[0]) scales[p.group] = g.scale;
 }
 
-template <typename T, int PASSES>
+template <typename T>
 __global__ void __launch_bounds__(kThreads) q8_load_kernel(const int8_t* __restrict__ codes, const float* __restrict__ scales,
-                                                           T* __restrict__ X, int64_t ldx, int64_t rows, int cols) {
-  const Places<PASSES> places(rows, cols);
-  uint2 c[PASSES];
-  float s[PASSES];
+                                                           T* __restrict__ X, int64_t ldx, int64_t rows, int cols, Div d) {
+  const Place p = place_of(rows, cols, d);
+  uint2 c[2];
+  if (!p.live[0]) return;
+  const int64_t at = p.row * int64_t(cols) + p.col;
+  c[0] = __ldg(reinterpret_cast<const uint2*>(codes + at));
+  if (p.live[1]) c[1] = __ldg(reinterpret_cast<const uint2*>(codes + at + kHalf));
+  const float s = __ldg(scales + p.group);
 #pragma unroll
-  for (int u = 0; u < PASSES; ++u) {
-    const Place p = places.at(u);
-    if (!p.live) continue;
-    c[u] = __ldg(reinterpret_cast<const uint2*>(codes + p.row * int64_t(cols) + p.col));
-    s[u] = __ldg(scales + p.group);
-  }
-#pragma unroll
-  for (int u = 0; u < PASSES; ++u) {
-    const Place p = places.at(u);
-    if (!p.live) continue;
-    float v[8];
-    decode8(c[u], s[u], v);
-    store8(X + p.row * ldx + p.col, v);
+  for (int v = 0; v < 2; ++v) {
+    if (!p.live[v]) break;
+    float f[8];
+    decode8(c[v], s, f);
+    store8(X + p.row * ldx + p.col + v * kHalf, f);
   }
 }
 
@@ -105,128 +97,134 @@ __device__ __forceinline__ float sigmoid_of(float g, float) {
   return __fdiv_rn(g < 0.f ? e : 1.f, 1.f + e);
 }
 
-template <typename T, int PASSES, bool KEEP>
+template <typename T, bool KEEP>
 __global__ void __launch_bounds__(kThreads) swiglu_fwd_kernel(const T* __restrict__ G, int64_t ldg, const T* __restrict__ U, int64_t ldu,
                                                               T* __restrict__ H, int8_t* __restrict__ Gq, float* __restrict__ Gs,
-                                                              int8_t* __restrict__ Uq, float* __restrict__ Us, int64_t rows, int cols) {
-  const Places<PASSES> places(rows, cols);
-  float g[PASSES][8], u[PASSES][8];
+                                                              int8_t* __restrict__ Uq, float* __restrict__ Us, int64_t rows, int cols,
+                                                              Div d) {
+  const Place p = place_of(rows, cols, d);
+  Raw<T> g[2], u[2];
 #pragma unroll
-  for (int k = 0; k < PASSES; ++k) {
-    const Place p = places.at(k);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) g[k][i] = u[k][i] = 0.f;
-    if (p.live) {
-      load8(G + p.row * ldg + p.col, g[k]);
-      load8(U + p.row * ldu + p.col, u[k]);
+  for (int v = 0; v < 2; ++v) {
+    g[v].zero();
+    u[v].zero();
+    if (p.live[v]) {
+      g[v].load(G + p.row * ldg + p.col + v * kHalf);
+      u[v].load(U + p.row * ldu + p.col + v * kHalf);
     }
   }
+  GroupScale qg, qu;
+  if (KEEP) {
+    uint32_t mg = max(g[0].amax_bits(), g[1].amax_bits()), mu = max(u[0].amax_bits(), u[1].amax_bits());
+    max_pair_over<T, kLanes>(mg, mu);
+    qg = group_scale(mg);
+    qu = group_scale(mu);
+  }
+  const int64_t at = p.row * int64_t(cols) + p.col;
 #pragma unroll
-  for (int k = 0; k < PASSES; ++k) {
-    const Place p = places.at(k);
-    GroupScale qg, qu;
+  for (int v = 0; v < 2; ++v) {
+    if (!p.live[v]) break;
+    float gf[8], uf[8];
+    g[v].get(gf);
+    u[v].get(uf);
     if (KEEP) {
-      qg = group_scale(group_amax_bits(g[k]));
-      qu = group_scale(group_amax_bits(u[k]));
+      *reinterpret_cast<uint2*>(Gq + at + v * kHalf) = encode8(gf, qg.inv);
+      *reinterpret_cast<uint2*>(Uq + at + v * kHalf) = encode8(uf, qu.inv);
     }
-    if (!p.live) continue;
-    if (KEEP) {
-      *reinterpret_cast<uint2*>(Gq + p.row * int64_t(cols) + p.col) = encode8(g[k], qg.inv);
-      *reinterpret_cast<uint2*>(Uq + p.row * int64_t(cols) + p.col) = encode8(u[k], qu.inv);
-      if (threadIdx.x % kLanes == 0) {
-        Gs[p.group] = qg.scale;
-        Us[p.group] = qu.scale;
-      }
-    }
-    float h[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) h[i] = g[k][i] * sigmoid_of(g[k][i], T()) * u[k][i];
-    store8(H + p.row * int64_t(cols) + p.col, h);
+    for (int i = 0; i < 8; ++i) uf[i] *= gf[i] * sigmoid_of(gf[i], T());
+    store8(H + at + v * kHalf, uf);
+  }
+  if (KEEP && first_lane() && p.live[0]) {
+    Gs[p.group] = qg.scale;
+    Us[p.group] = qu.scale;
   }
 }
 
-template <typename T, int PASSES>
+template <typename T>
 __global__ void __launch_bounds__(kThreads) swiglu_bwd_kernel(const T* __restrict__ dH, const int8_t* __restrict__ Gq,
                                                               const float* __restrict__ Gs, const int8_t* __restrict__ Uq,
                                                               const float* __restrict__ Us, T* __restrict__ dG, int64_t lddg,
-                                                              T* __restrict__ dU, int64_t lddu, int64_t rows, int cols) {
-  const Places<PASSES> places(rows, cols);
-  uint2 cg[PASSES], cu[PASSES];
-  float sg[PASSES], su[PASSES], dh[PASSES][8];
+                                                              T* __restrict__ dU, int64_t lddu, int64_t rows, int cols, Div d) {
+  const Place p = place_of(rows, cols, d);
+  if (!p.live[0]) return;
+  uint2 cg[2], cu[2];
+  Raw<T> x[2];
+  const int64_t at = p.row * int64_t(cols) + p.col;
 #pragma unroll
-  for (int k = 0; k < PASSES; ++k) {
-    const Place p = places.at(k);
-    if (!p.live) continue;
-    const int64_t at = p.row * int64_t(cols) + p.col;
-    cg[k] = __ldg(reinterpret_cast<const uint2*>(Gq + at));
-    cu[k] = __ldg(reinterpret_cast<const uint2*>(Uq + at));
-    sg[k] = __ldg(Gs + p.group);
-    su[k] = __ldg(Us + p.group);
-    load8(dH + at, dh[k]);
+  for (int v = 0; v < 2; ++v) {
+    if (!p.live[v]) break;
+    cg[v] = __ldg(reinterpret_cast<const uint2*>(Gq + at + v * kHalf));
+    cu[v] = __ldg(reinterpret_cast<const uint2*>(Uq + at + v * kHalf));
+    x[v].load(dH + at + v * kHalf);
   }
+  const float sg = __ldg(Gs + p.group), su = __ldg(Us + p.group);
 #pragma unroll
-  for (int k = 0; k < PASSES; ++k) {
-    const Place p = places.at(k);
-    if (!p.live) continue;
-    float g[8], u[8];
-    decode8(cg[k], sg[k], g);
-    decode8(cu[k], su[k], u);
+  for (int v = 0; v < 2; ++v) {
+    if (!p.live[v]) break;
+    float g[8], u[8], dh[8];
+    decode8(cg[v], sg, g);
+    decode8(cu[v], su, u);
+    x[v].get(dh);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float s = sigmoid_of(g[i], T()), e = dh[k][i] * s;
+      const float s = sigmoid_of(g[i], T()), e = dh[i] * s;
       const float dg = e * u[i] * (1.f + g[i] * (1.f - s));
       u[i] = e * g[i];
       g[i] = dg;
     }
-    store8(dG + p.row * lddg + p.col, g);
-    store8(dU + p.row * lddu + p.col, u);
+    store8(dG + p.row * lddg + p.col + v * kHalf, g);
+    store8(dU + p.row * lddu + p.col + v * kHalf, u);
   }
 }
 
-template <int PASSES>
-unsigned grid_for(int64_t rows, int64_t cols) {
-  const int64_t groups = rows * ((cols + kGroup - 1) / kGroup), per_block = int64_t(kGroupsPerPass) * PASSES;
-  return unsigned((groups + per_block - 1) / per_block);
+struct Launch {
+  unsigned grid;
+  Div div;
+};
+Launch launch_of(const Rows& d) {
+  const int64_t ng = (d.cols + kGroup - 1) / kGroup;
+  return Launch{unsigned((d.rows * ng + kGroupsPerBlock - 1) / kGroupsPerBlock), Div{uint32_t(ng), uint32_t((65536 + ng - 1) / ng)}};
+}
+
+template <typename T>
+void launch_store(const Rows& d, const void* X, int64_t ldx, int8_t* codes, float* scales, cudaStream_t st) {
+  const Launch l = launch_of(d);
+  q8_store_kernel<T><<<l.grid, kThreads, 0, st>>>(static_cast<const T*>(X), ldx, codes, scales, d.rows, int(d.cols), l.div);
+}
+template <typename T>
+void launch_load(const Rows& d, const int8_t* codes, const float* scales, void* X, int64_t ldx, cudaStream_t st) {
+  const Launch l = launch_of(d);
+  q8_load_kernel<T><<<l.grid, kThreads, 0, st>>>(codes, scales, static_cast<T*>(X), ldx, d.rows, int(d.cols), l.div);
+}
+template <typename T, bool KEEP>
+void launch_swiglu_fwd(const Rows& d, const void* G, int64_t ldg, const void* U, int64_t ldu, void* H, int8_t* Gq, float* Gs, int8_t* Uq,
+                       float* Us, cudaStream_t st) {
+  const Launch l = launch_of(d);
+  swiglu_fwd_kernel<T, KEEP><<<l.grid, kThreads, 0, st>>>(static_cast<const T*>(G), ldg, static_cast<const T*>(U), ldu, static_cast<T*>(H),
+                                                         Gq, Gs, Uq, Us, d.rows, int(d.cols), l.div);
+}
+template <typename T>
+void launch_swiglu_bwd(const Rows& d, const void* dH, const int8_t* Gq, const float* Gs, const int8_t* Uq, const float* Us, void* dG,
+                       int64_t lddg, void* dU, int64_t lddu, cudaStream_t st) {
+  const Launch l = launch_of(d);
+  swiglu_bwd_kernel<T><<<l.grid, kThreads, 0, st>>>(static_cast<const T*>(dH), Gq, Gs, Uq, Us, static_cast<T*>(dG), lddg,
+                                                   static_cast<T*>(dU), lddu, d.rows, int(d.cols), l.div);
 }
 
 }  // namespace
 
 cudaError_t q8_store(const Rows& d, const void* X, int64_t ldx, int8_t* codes, float* scales, cudaStream_t st) {
-  constexpr int P = 2;
-  const unsigned grid = grid_for<P>(d.rows, d.cols);
-  if (d.bf16)
-    q8_store_kernel<__nv_bfloat16, P><<<grid, kThreads, 0, st>>>(static_cast<const __nv_bfloat16*>(X), ldx, codes, scales, d.rows, int(d.cols));
-  else
-    q8_store_kernel<float, P><<<grid, kThreads, 0, st>>>(static_cast<const float*>(X), ldx, codes, scales, d.rows, int(d.cols));
+  if (d.bf16) launch_store<__nv_bfloat16>(d, X, ldx, codes, scales, st);
+  else launch_store<float>(d, X, ldx, codes, scales, st);
   return launched();
 }
 
 cudaError_t q8_load(const Rows& d, const int8_t* codes, const float* scales, void* X, int64_t ldx, cudaStream_t st) {
-  constexpr int P = 2;
-  const unsigned grid = grid_for<P>(d.rows, d.cols);
-  if (d.bf16)
-    q8_load_kernel<__nv_bfloat16, P><<<grid, kThreads, 0, st>>>(codes, scales, static_cast<__nv_bfloat16*>(X), ldx, d.rows, int(d.cols));
-  else
-    q8_load_kernel<float, P><<<grid, kThreads, 0, st>>>(codes, scales, static_cast<float*>(X), ldx, d.rows, int(d.cols));
+  if (d.bf16) launch_load<__nv_bfloat16>(d, codes, scales, X, ldx, st);
+  else launch_load<float>(d, codes, scales, X, ldx, st);
   return launched();
 }
-
-namespace {
-template <typename T, bool KEEP>
-void launch_swiglu_fwd(const Rows& d, const void* G, int64_t ldg, const void* U, int64_t ldu, void* H, int8_t* Gq, float* Gs, int8_t* Uq,
-                       float* Us, cudaStream_t st) {
-  constexpr int P = 2;
-  swiglu_fwd_kernel<T, P, KEEP><<<grid_for<P>(d.rows, d.cols), kThreads, 0, st>>>(
-      static_cast<const T*>(G), ldg, static_cast<const T*>(U), ldu, static_cast<T*>(H), Gq, Gs, Uq, Us, d.rows, int(d.cols));
-}
-template <typename T>
-void launch_swiglu_bwd(const Rows& d, const void* dH, const int8_t* Gq, const float* Gs, const int8_t* Uq, const float* Us, void* dG,
-                       int64_t lddg, void* dU, int64_t lddu, cudaStream_t st) {
-  constexpr int P = 2;
-  swiglu_bwd_kernel<T, P><<<grid_for<P>(d.rows, d.cols), kThreads, 0, st>>>(static_cast<const T*>(dH), Gq, Gs, Uq, Us, static_cast<T*>(dG),
-                                                                           lddg, static_cast<T*>(dU), lddu, d.rows, int(d.cols));
-}
-}  // namespace
 
 cudaError_t swiglu_fwd(const Rows& d, const void* G, int64_t ldg, const void* U, int64_t ldu, void* H, int8_t* Gq, float* Gs, int8_t* Uq,
                        float* Us, cudaStream_t st) {
