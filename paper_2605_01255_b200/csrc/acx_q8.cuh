@@ -21,6 +21,26 @@ constexpr uint32_t kTinyBits = (127u - 100u) << 23;   // 2^-100
 constexpr uint32_t kInfBits = 0x7F800000u, kNanBits = 0x7FFFFFFFu;
 constexpr float kMaxScale = 0x1.020406p+121f;   // the largest float whose 127-fold is finite
 
+// Two binary32 operations per instruction, each rounded to nearest even on its own.
+__device__ __forceinline__ uint64_t bits2(float2 a) { return (uint64_t(__float_as_uint(a.y)) << 32) | __float_as_uint(a.x); }
+__device__ __forceinline__ float2 float2_of(uint64_t b) { return make_float2(__uint_as_float(uint32_t(b)), __uint_as_float(uint32_t(b >> 32))); }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)));
+  return float2_of(r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)));
+  return float2_of(r);
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)), "l"(bits2(c)));
+  return float2_of(r);
+}
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
 // Eight elements of a row as they are in memory: loads are issued long before the values are needed, and a bf16 vector
 // waits for that in four registers instead of eight.
 template <typename T>
@@ -30,20 +50,20 @@ struct Raw<__nv_bfloat16> {
   uint4 u;
   __device__ __forceinline__ void zero() { u = make_uint4(0u, 0u, 0u, 0u); }
   __device__ __forceinline__ void load(const __nv_bfloat16* p) { u = __ldg(reinterpret_cast<const uint4*>(p)); }
-  __device__ __forceinline__ void get(float (&v)[8]) const {
+  __device__ __forceinline__ void get(float2 (&v)[4]) const {
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = __uint_as_float(w[i] << 16);
-      v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    }
+    for (int i = 0; i < 4; ++i) v[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
   }
-  // Largest magnitude, as the bits of a binary32: integer order is the order of magnitudes, with infinity and then NaN on
-  // top, so nothing that is not finite gets lost.
+  // Largest magnitude, as the bits of a binary32; a NaN wins over everything.
   __device__ __forceinline__ uint32_t amax_bits() const {
-    const uint32_t m = 0x7FFF7FFFu;
-    const uint32_t a = __vmaxu2(__vmaxu2(u.x & m, u.y & m), __vmaxu2(u.z & m, u.w & m));
+    const uint32_t a = max16x2(max16x2(u.x & 0x7FFF7FFFu, u.y & 0x7FFF7FFFu), max16x2(u.z & 0x7FFF7FFFu, u.w & 0x7FFF7FFFu));
     return max(a << 16, a & 0xFFFF0000u);
+  }
+  // Both halves' maxima of two pairs of non-negative bf16 values (a NaN wins)
+  static __device__ __forceinline__ uint32_t max16x2(uint32_t a, uint32_t b) {
+    const __nv_bfloat162 m = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&m);
   }
 };
 template <>
@@ -54,13 +74,13 @@ struct Raw<float> {
     a = __ldg(reinterpret_cast<const float4*>(p));
     b = __ldg(reinterpret_cast<const float4*>(p) + 1);
   }
-  __device__ __forceinline__ void get(float (&v)[8]) const {
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  __device__ __forceinline__ void get(float2 (&v)[4]) const {
+    v[0] = make_float2(a.x, a.y); v[1] = make_float2(a.z, a.w);
+    v[2] = make_float2(b.x, b.y); v[3] = make_float2(b.z, b.w);
   }
+  // Integer order is the order of magnitudes, with infinity and then NaN on top.
   __device__ __forceinline__ uint32_t amax_bits() const {
-    float v[8];
-    get(v);
+    const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
     uint32_t m = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
@@ -69,23 +89,23 @@ struct Raw<float> {
 };
 
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, float (&v)[8]) {
+__device__ __forceinline__ void load8(const T* p, float2 (&v)[4]) {
   Raw<T> r;
   r.load(p);
   r.get(v);
 }
-__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float2 (&v)[4]) {
   uint32_t w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+    const __nv_bfloat162 h = __floats2bfloat162_rn(v[i].x, v[i].y);
     w[i] = *reinterpret_cast<const uint32_t*>(&h);
   }
   *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
-  reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-  reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+__device__ __forceinline__ void store8(float* p, const float2 (&v)[4]) {
+  reinterpret_cast<float4*>(p)[0] = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
+  reinterpret_cast<float4*>(p)[1] = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
 }
 
 // Largest of a value over LANES consecutive lanes (a power of two).  All lanes of the warp take part.
@@ -102,7 +122,7 @@ __device__ __forceinline__ void max_pair_over(uint32_t& a, uint32_t& b) {
   if (sizeof(T) == 2) {
     uint32_t m = a | (b >> 16);
 #pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) m = __vmaxu2(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+    for (int o = LANES / 2; o > 0; o >>= 1) m = Raw<__nv_bfloat16>::max16x2(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
     a = m & 0xFFFF0000u;
     b = m << 16;
   } else {
@@ -124,11 +144,15 @@ __device__ __forceinline__ GroupScale group_scale(uint32_t amax_bits) {
 // Eight codes as two words.  Adding 1.5 * 2^23 rounds a value of magnitude <= 2^22 to a whole number (nearest, ties to
 // even) and leaves its two's complement in the low bits of the sum's mantissa: one addition and a byte permutation
 // instead of a conversion, whose rate is a quarter.  The product and the sum are rounded separately (no fma), as the
-// format says.  A NaN product (0 * inf in a group whose scale is NaN) leaves some byte: it is read back times NaN.
-__device__ __forceinline__ uint2 encode8(const float (&v)[8], float inv) {
+// format says (the additions one at a time: the assembler fuses the two-at-a-time forms of both into one rounding).  A NaN product (0 * inf in a group whose scale is NaN) leaves some byte: it is read back times NaN.
+__device__ __forceinline__ uint2 encode8(const float2 (&v)[4], float inv) {
   uint32_t b[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) b[i] = __float_as_uint(__fadd_rn(__fmul_rn(v[i], inv), 12582912.f));
+  for (int i = 0; i < 4; ++i) {
+    const float2 q = mul2(v[i], both(inv));
+    b[2 * i] = __float_as_uint(__fadd_rn(q.x, 12582912.f));
+    b[2 * i + 1] = __float_as_uint(__fadd_rn(q.y, 12582912.f));
+  }
   uint2 c;
   c.x = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
   c.y = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
@@ -137,12 +161,13 @@ __device__ __forceinline__ uint2 encode8(const float (&v)[8], float inv) {
 
 // The values of eight codes.  A byte with its sign bit flipped is code + 128; placed into the mantissa of 2^23 it is the
 // float 2^23 + 128 + code, exactly.
-__device__ __forceinline__ void decode8(uint2 c, float scale, float (&v)[8]) {
+__device__ __forceinline__ void decode8(uint2 c, float scale, float2 (&v)[4]) {
   const uint32_t w[2] = {c.x ^ 0x80808080u, c.y ^ 0x80808080u};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t bits = __byte_perm(w[i >> 2], 0x4B000000u, 0x7650 + (i & 3));   // bytes: 4B 00 00 code
-    v[i] = __fmul_rn(__fadd_rn(__uint_as_float(bits), -8388736.f), scale);
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t lo = __byte_perm(w[i >> 1], 0x4B000000u, 0x7650 + 2 * (i & 1));   // bytes: 4B 00 00 code
+    const uint32_t hi = __byte_perm(w[i >> 1], 0x4B000000u, 0x7651 + 2 * (i & 1));
+    v[i] = mul2(add2(make_float2(__uint_as_float(lo), __uint_as_float(hi)), both(-8388736.f)), both(scale));
   }
 }
 

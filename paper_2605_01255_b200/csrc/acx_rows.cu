@@ -59,7 +59,7 @@ __global__ void __launch_bounds__(kThreads) q8_store_kernel(const T* __restrict_
   const GroupScale g = group_scale(max_over<kLanes>(max(x[0].amax_bits(), x[1].amax_bits())));
 #pragma unroll
   for (int v = 0; v < 2; ++v) {
-    float f[8];
+    float2 f[4];
     x[v].get(f);
     if (p.live[v]) *reinterpret_cast<uint2*>(codes + p.row * int64_t(cols) + p.col + v * kHalf) = encode8(f, g.inv);
   }
@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(kThreads) q8_load_kernel(const int8_t* __restr
 #pragma unroll
   for (int v = 0; v < 2; ++v) {
     if (!p.live[v]) break;
-    float f[8];
+    float2 f[4];
     decode8(c[v], s, f);
     store8(X + p.row * ldx + p.col + v * kHalf, f);
   }
@@ -96,6 +96,9 @@ __device__ __forceinline__ float sigmoid_of(float g, float) {
   const float e = expf(-fabsf(g));
   return __fdiv_rn(g < 0.f ? e : 1.f, 1.f + e);
 }
+
+template <typename T>
+__device__ __forceinline__ float2 sigmoid2(float2 g, T) { return make_float2(sigmoid_of(g.x, T()), sigmoid_of(g.y, T())); }
 
 template <typename T, bool KEEP>
 __global__ void __launch_bounds__(kThreads) swiglu_fwd_kernel(const T* __restrict__ G, int64_t ldg, const T* __restrict__ U, int64_t ldu,
@@ -124,7 +127,7 @@ __global__ void __launch_bounds__(kThreads) swiglu_fwd_kernel(const T* __restric
 #pragma unroll
   for (int v = 0; v < 2; ++v) {
     if (!p.live[v]) break;
-    float gf[8], uf[8];
+    float2 gf[4], uf[4];
     g[v].get(gf);
     u[v].get(uf);
     if (KEEP) {
@@ -132,7 +135,7 @@ __global__ void __launch_bounds__(kThreads) swiglu_fwd_kernel(const T* __restric
       *reinterpret_cast<uint2*>(Uq + at + v * kHalf) = encode8(uf, qu.inv);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) uf[i] *= gf[i] * sigmoid_of(gf[i], T());
+    for (int i = 0; i < 4; ++i) uf[i] = mul2(uf[i], mul2(gf[i], sigmoid2(gf[i], T())));
     store8(H + at + v * kHalf, uf);
   }
   if (KEEP && first_lane() && p.live[0]) {
@@ -162,19 +165,19 @@ __global__ void __launch_bounds__(kThreads) swiglu_bwd_kernel(const T* __restric
 #pragma unroll
   for (int v = 0; v < 2; ++v) {
     if (!p.live[v]) break;
-    float g[8], u[8], dh[8];
+    float2 g[4], u[4], dh[4];
     decode8(cg[v], sg, g);
     decode8(cu[v], su, u);
     x[v].get(dh);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float s = sigmoid_of(g[i], T()), e = dh[i] * s;
-      const float dg = e * u[i] * (1.f + g[i] * (1.f - s));
-      u[i] = e * g[i];
-      g[i] = dg;
+    for (int i = 0; i < 4; ++i) {
+      const float2 s = sigmoid2(g[i], T()), e = mul2(dh[i], s);
+      const float2 slope = fma2(g[i], fma2(s, both(-1.f), both(1.f)), both(1.f));   // 1 + g (1 - s)
+      u[i] = mul2(mul2(e, u[i]), slope);
+      g[i] = mul2(e, g[i]);
     }
-    store8(dG + p.row * lddg + p.col + v * kHalf, g);
-    store8(dU + p.row * lddu + p.col + v * kHalf, u);
+    store8(dG + p.row * lddg + p.col + v * kHalf, u);
+    store8(dU + p.row * lddu + p.col + v * kHalf, g);
   }
 }
 
