@@ -13,7 +13,7 @@ namespace {
 
 using ce::Params;
 
-constexpr int kTokensPerBlock = 32;
+constexpr int kTokensPerBlock = 8;
 
 __device__ __forceinline__ float dot8(uint4 a, uint4 b, float s) {
   const uint32_t x[4] = {a.x, a.y, a.z, a.w}, w[4] = {b.x, b.y, b.z, b.w};
@@ -25,85 +25,98 @@ __device__ __forceinline__ float dot8(uint4 a, uint4 b, float s) {
   return s;
 }
 
-// Joins the (maximum, sum) pairs of 32 tokens: 32 warps, a token per lane, every warp takes each 32nd pair.  The target's
-// logit is taken again as a plain fp32 product (a warp per token): the tensor core adds 16 products at a time with
-// truncation, an error of up to 2^-24 of the logit per step and of one sign, which the loss of an unlikely token would
-// show in full; its term of the sum is exchanged along with it.
-__global__ void __launch_bounds__(1024) ce_join_kernel(const float2* __restrict__ part, const float* __restrict__ target_logit,
-                                                       const __nv_bfloat16* __restrict__ X, const __nv_bfloat16* __restrict__ W,
-                                                       const int64_t* __restrict__ targets, const float* __restrict__ weight, int tokens,
-                                                       int d, int vocab, int parts, float c, float* __restrict__ loss,
-                                                       float* __restrict__ lse, float2* __restrict__ block_sums) {
-  __shared__ float2 red[32][33];
+__device__ __forceinline__ void wait_for_launch_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// (m, s) <- (m, s) joined with (m1, s1): sums of 2^(x - maximum)
+__device__ __forceinline__ void join_pair(float& m, float& s, float m1, float s1) {
+  const float top = fmaxf(m, m1);
+  // a side that holds nothing has (-inf, 0): it must not turn into a NaN; one that holds a NaN must stay one
+  const float a = (m == -INFINITY && s == 0.f) ? 0.f : s * exp2f(m - top), b = (m1 == -INFINITY && s1 == 0.f) ? 0.f : s1 * exp2f(m1 - top);
+  m = top;
+  s = a + b;
+}
+
+// Joins the (maximum, sum) pairs of 8 tokens: 32 warps; a lane has token lane & 7 and every 128th pair, eight at a time.  The
+// target's logit is taken again as a plain fp32 product (four warps per token): the tensor core adds 16 products at a time
+// with truncation, an error of up to 2^-24 of the logit per step and of one sign, which the loss of an unlikely token would
+// show in full; its term of the sum is exchanged along with it.  The last block to finish adds the blocks' sums of losses
+// and weights, in order.  Launched behind the logits' kernel before that has finished; the products need nothing of it.
+__global__ void __launch_bounds__(1024) ce_join_kernel(const float2* part, const float* target_logit, const __nv_bfloat16* __restrict__ X,
+                                                       const __nv_bfloat16* __restrict__ W, const int64_t* __restrict__ targets,
+                                                       const float* __restrict__ weight, int tokens, int d, int vocab, int parts, float c,
+                                                       float* __restrict__ loss, float* __restrict__ lse, float2* block_sums,
+                                                       uint32_t* ticket, float* __restrict__ total) {
+  __shared__ float2 red[32][9];
   __shared__ float exact[32];
+  __shared__ bool last;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t0 = int(blockIdx.x) * kTokensPerBlock;
-  const int t = t0 + lane;
-  float m = -INFINITY, s = 0.f;
-  if (t < tokens) {
-    for (int q = warp; q < parts; q += 8 * 32) {   // eight pairs in flight
-      float2 v[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = q + 32 * i < parts ? __ldg(part + int64_t(q + 32 * i) * tokens + t) : make_float2(-INFINITY, 0.f);
-      float top = m;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) top = fmaxf(top, v[i].x);
-      s *= exp2f(m - top);
-      m = top;
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (q + 32 * i < parts) s += v[i].y * exp2f(v[i].x - m);
-    }
-  }
-  red[warp][lane] = make_float2(m, s);
   {
-    const int tt = t0 + warp;
+    const int tt = t0 + (warp >> 2);
     const int64_t y = tt < tokens ? __ldg(targets + tt) : -1;
     float p = 0.f;
     if (y >= 0 && y < vocab) {
       const uint4* x = reinterpret_cast<const uint4*>(X + int64_t(tt) * d);
       const uint4* w = reinterpret_cast<const uint4*>(W + y * int64_t(d));
-      for (int i = lane; i < d / 8; i += 32) p = dot8(__ldg(x + i), __ldg(w + i), p);
+      for (int i = (warp & 3) * 32 + lane; i < d / 8; i += 128) p = dot8(__ldg(x + i), __ldg(w + i), p);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) p += __shfl_xor_sync(0xFFFFFFFFu, p, o);
-    if (lane == 0) exact[warp] = p * c;
+    if (lane == 0) exact[warp] = p;
   }
-  __syncthreads();
-  if (warp != 0) return;
-  float wl = 0.f, wt = 0.f;
+  wait_for_launch_before();
+  const int tok = lane & 7, t = t0 + tok;
+  float m = -INFINITY, s = 0.f;
   if (t < tokens) {
+    for (int q = warp * 4 + (lane >> 3); q < parts; q += 8 * 128) {   // eight pairs in flight
+      float2 v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = q + 128 * i < parts ? __ldcg(part + int64_t(q + 128 * i) * tokens + t) : make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) join_pair(m, s, v[i].x, v[i].y);
+    }
+  }
+#pragma unroll
+  for (int o = 8; o <= 16; o <<= 1) join_pair(m, s, __shfl_xor_sync(0xFFFFFFFFu, m, o), __shfl_xor_sync(0xFFFFFFFFu, s, o));
+  if (lane < 8) red[warp][lane] = make_float2(m, s);
+  __syncthreads();
+  if (warp == 0) {
     m = -INFINITY;
     s = 0.f;
-    for (int k = 0; k < 32; ++k) m = fmaxf(m, red[k][lane].x);
-    for (int k = 0; k < 32; ++k)
-      if (red[k][lane].x != -INFINITY || red[k][lane].y != 0.f) s += red[k][lane].y * exp2f(red[k][lane].x - m);
-    const int64_t y = __ldg(targets + t);
-    const bool trained = y >= 0 && y < vocab;
-    const float ty = exact[lane];
-    if (trained) s += exp2f(ty - m) - exp2f(target_logit[t] - m);
-    const float l2 = m + log2f(s);
-    constexpr float kLn2 = 0.6931471805599453f;
-    lse[t] = l2 * kLn2;
-    const float l = trained ? (l2 - ty) * kLn2 : 0.f;
-    loss[t] = l;
-    wt = trained ? (weight ? __ldg(weight + t) : 1.f) : 0.f;
-    wl = trained ? wt * l : 0.f;
-  }
-  if (!block_sums) return;
+    for (int k = lane >> 3; k < 32; k += 4) join_pair(m, s, red[k][tok].x, red[k][tok].y);
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    wl += __shfl_xor_sync(0xFFFFFFFFu, wl, o);
-    wt += __shfl_xor_sync(0xFFFFFFFFu, wt, o);
+    for (int o = 8; o <= 16; o <<= 1) join_pair(m, s, __shfl_xor_sync(0xFFFFFFFFu, m, o), __shfl_xor_sync(0xFFFFFFFFu, s, o));
+    float wl = 0.f, wt = 0.f;
+    if (lane < 8 && t < tokens) {
+      const int64_t y = __ldg(targets + t);
+      const bool trained = y >= 0 && y < vocab;
+      const float ty = ((exact[4 * tok] + exact[4 * tok + 1]) + (exact[4 * tok + 2] + exact[4 * tok + 3])) * c;
+      if (trained) s += exp2f(ty - m) - exp2f(__ldcg(target_logit + t) - m);
+      const float l2 = m + log2f(s);
+      constexpr float kLn2 = 0.6931471805599453f;
+      lse[t] = l2 * kLn2;
+      const float l = trained ? (l2 - ty) * kLn2 : 0.f;
+      loss[t] = l;
+      wt = trained ? (weight ? __ldg(weight + t) : 1.f) : 0.f;
+      wl = trained ? wt * l : 0.f;
+    }
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) {
+      wl += __shfl_xor_sync(0xFFFFFFFFu, wl, o);
+      wt += __shfl_xor_sync(0xFFFFFFFFu, wt, o);
+    }
+    if (lane == 0 && total) {
+      block_sums[blockIdx.x] = make_float2(wl, wt);
+      __threadfence();
+      last = atomicAdd(ticket, 1u) == gridDim.x - 1;
+    }
   }
-  if (lane == 0) block_sums[blockIdx.x] = make_float2(wl, wt);
-}
-
-// total = (sum of w loss, sum of w): the blocks' sums in a fixed order.
-__global__ void __launch_bounds__(1024) ce_total_kernel(const float2* __restrict__ block_sums, int n, float* __restrict__ total) {
-  __shared__ float2 red[32];
+  if (!total) return;
+  __syncthreads();
+  if (!last) return;
+  __threadfence();
   float a = 0.f, b = 0.f;
-  for (int i = threadIdx.x; i < n; i += 1024) {
-    const float2 v = block_sums[i];
+  for (int i = threadIdx.x; i < int(gridDim.x); i += 1024) {
+    const float2 v = __ldcg(block_sums + i);
     a += v.x;
     b += v.y;
   }
@@ -112,17 +125,17 @@ __global__ void __launch_bounds__(1024) ce_total_kernel(const float2* __restrict
     a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
     b += __shfl_xor_sync(0xFFFFFFFFu, b, o);
   }
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = make_float2(a, b);
+  if (lane == 0) red[warp][0] = make_float2(a, b);
   __syncthreads();
-  if (threadIdx.x >= 32) return;
-  a = red[threadIdx.x].x;
-  b = red[threadIdx.x].y;
+  if (warp != 0) return;
+  a = red[lane][0].x;
+  b = red[lane][0].y;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
     b += __shfl_xor_sync(0xFFFFFFFFu, b, o);
   }
-  if (threadIdx.x == 0) {
+  if (lane == 0) {
     total[0] = a;
     total[1] = b;
   }
@@ -130,8 +143,8 @@ __global__ void __launch_bounds__(1024) ce_total_kernel(const float2* __restrict
 
 // dX = f (sum over the splits + corr W[y]): what rounding D to bf16 took from the target's element, the largest of its row
 // and the only one whose rounding is not averaged out, comes back here in fp32.
-__global__ void __launch_bounds__(256) ce_finish_kernel(const float* __restrict__ acc, int splits, int64_t split_stride,
-                                                        const float* __restrict__ corr, const int64_t* __restrict__ targets,
+__global__ void __launch_bounds__(256) ce_finish_kernel(const float* acc, int splits, int64_t split_stride,
+                                                        const float* corr, const int64_t* __restrict__ targets,
                                                         const __nv_bfloat16* __restrict__ W, const float* __restrict__ denom, float scale,
                                                         __nv_bfloat16* __restrict__ dX, int tokens, int d, int vocab) {
   const int vecs = d / 8;
@@ -143,15 +156,24 @@ __global__ void __launch_bounds__(256) ce_finish_kernel(const float* __restrict_
   float v[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = 0.f;
-  for (int s = 0; s < splits; ++s) {
-    const float4* p = reinterpret_cast<const float4*>(acc + s * split_stride + t * d + c);
-    const float4 a = __ldg(p), b = __ldg(p + 1);
-    v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
-    v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+  wait_for_launch_before();
+  for (int s0 = 0; s0 < splits; s0 += 4) {   // four splits' loads under way, added in order
+    float4 a[4], b[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float4* p = reinterpret_cast<const float4*>(acc + (s0 + k) * split_stride + t * d + c);
+      a[k] = s0 + k < splits ? __ldcg(p) : make_float4(0.f, 0.f, 0.f, 0.f);
+      b[k] = s0 + k < splits ? __ldcg(p + 1) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[0] += a[k].x; v[1] += a[k].y; v[2] += a[k].z; v[3] += a[k].w;
+      v[4] += b[k].x; v[5] += b[k].y; v[6] += b[k].z; v[7] += b[k].w;
+    }
   }
   const int64_t y = __ldg(targets + t);
   if (y >= 0 && y < vocab) {
-    const float k = __ldg(corr + t);
+    const float k = __ldcg(corr + t);
     const uint4 w = __ldg(reinterpret_cast<const uint4*>(W + y * int64_t(d) + c));
     const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -174,9 +196,39 @@ size_t aligned(size_t bytes) { return (bytes + 1023) & ~size_t(1023); }
 
 int pair_count() { return std::max(1, sm_count() / 2); }
 
+// behind: launched with programmatic stream serialization, so that it may start before the launch before it has finished.
+template <typename... K, typename... A>
+cudaError_t launch_kernel(void (*kernel)(K...), unsigned grid, unsigned threads, size_t smem, int cluster, bool behind, cudaStream_t st,
+                          const A&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  unsigned n = 0;
+  if (cluster > 1) {
+    attr[n].id = cudaLaunchAttributeClusterDimension;
+    attr[n].val.clusterDim.x = unsigned(cluster);
+    attr[n].val.clusterDim.y = 1;
+    attr[n].val.clusterDim.z = 1;
+    ++n;
+  }
+  if (behind) {
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n].val.programmaticStreamSerializationAllowed = 1;
+    ++n;
+  }
+  cfg.attrs = attr;
+  cfg.numAttrs = n;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
+  kernel_launch_counter().fetch_add(1, std::memory_order_relaxed);
+  return e;
+}
+
 template <int KIND>
 cudaError_t launch(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& ta2, const CUtensorMap& tb2, const CUtensorMap& to,
-                   const CUtensorMap& to2, const Params& p, cudaStream_t st) {
+                   const CUtensorMap& to2, const Params& p, bool behind, cudaStream_t st) {
   auto kernel = ce::ce_kernel<KIND>;
   static DeviceOnce once;
   if (once.needed()) {
@@ -184,21 +236,8 @@ cudaError_t launch(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorM
     if (e != cudaSuccess) return e;
     once.done();
   }
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(unsigned(2 * std::min(p.units, pair_count())));
-  cfg.blockDim = dim3(ce::kThreads);
-  cfg.dynamicSmemBytes = ce::kSmemBytes;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = 2;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, ta, tb, ta2, tb2, to, to2, p);
-  kernel_launch_counter().fetch_add(1, std::memory_order_relaxed);
-  return e;
+  return launch_kernel(kernel, unsigned(2 * std::min(p.units, pair_count())), ce::kThreads, ce::kSmemBytes, 2, behind, st, ta, tb, ta2, tb2,
+                       to, to2, p);
 }
 
 // Token tiles that pass over the vocabulary together: as many as have their rows of X (d wide, bf16) in 48 MB, so that X
@@ -223,7 +262,7 @@ void common(const CeProblem& q, Params* p, const int64_t* targets, const float* 
 
 struct FwdPlan {
   int parts, blocks;
-  size_t part, target, sums, bytes;
+  size_t part, target, sums, ticket, bytes;
 };
 FwdPlan fwd_plan(const CeProblem& q) {
   FwdPlan f;
@@ -232,32 +271,53 @@ FwdPlan fwd_plan(const CeProblem& q) {
   f.part = 0;
   f.target = f.part + aligned(size_t(f.parts) * size_t(q.m) * sizeof(float2));
   f.sums = f.target + aligned(size_t(q.m) * 4);
-  f.bytes = f.sums + aligned(size_t(f.blocks) * sizeof(float2));
+  f.ticket = f.sums + aligned(size_t(f.blocks) * sizeof(float2));
+  f.bytes = f.ticket + aligned(4);
   return f;
 }
 
 // Pieces of the vocabulary: D of one piece takes at most about 128 MB, so that much of it is still in L2 when the two
-// products read it, and the pieces are of equal size.
+// products read it, and the pieces are of equal size.  Up to three pieces are under way at a time (see ce_bwd).
+constexpr int64_t kPieceBytes = int64_t(128) << 20;
+constexpr int kBuffers = 3;
 struct BwdPlan {
-  int piece_tiles, pieces, splits, kb_per_split, d_tiles, acc_rows;
-  size_t D, acc, corr, bytes;
+  int piece_tiles, pieces, buffers, splits, kb_per_split, d_tiles, d_width, acc_rows;
+  size_t D, D_stride, acc, corr, bytes;
 };
 BwdPlan bwd_plan(const CeProblem& q) {
   BwdPlan b;
-  const int n_tiles = ceil_div(q.vocab, ce::kTile), m_tiles = ceil_div(q.m, ce::kTile);
-  const int fit = int(std::max<int64_t>(1, (int64_t(128) << 20) / (q.m * ce::kTile * 2)));
+  const int n_tiles = ceil_div(q.vocab, ce::kTile), m_tiles = ceil_div(q.m, ce::kTile), pairs = pair_count();
+  const int fit = int(std::max<int64_t>(1, kPieceBytes / (q.m * ce::kTile * 2)));
   b.pieces = ceil_div(n_tiles, fit);
   b.piece_tiles = ceil_div(n_tiles, b.pieces);
   b.pieces = ceil_div(n_tiles, b.piece_tiles);
+  b.buffers = std::min(b.pieces, kBuffers);
   b.d_tiles = ceil_div(q.d, ce::kTile);
+  b.d_width = (ceil_div(q.d, b.d_tiles) + 31) & ~31;
   b.acc_rows = m_tiles * ce::kTile;
-  // dX: few tiles are split along the piece until there are about two per CTA pair (at least 8 k-blocks each)
-  const int piece_kb = b.piece_tiles * (ce::kTile / ce::kBK), units = m_tiles * b.d_tiles, want = 2 * pair_count();
-  const int splits = std::max(1, std::min({units >= want ? 1 : want / units, piece_kb / 8, 32}));
-  b.kb_per_split = ceil_div(piece_kb, splits);
+  // dX is split along the piece where that lets the longest-loaded pair of CTAs finish sooner: pair c takes the units c,
+  // c + pairs, ..., the tiles of dX first.  Every split costs its fp32 sums' way through memory (a unit's epilogue is worth
+  // about 4 k-blocks, the last kernel's reading about one per split).
+  const int piece_kb = b.piece_tiles * (ce::kTile / ce::kBK), token_kb = ceil_div(q.m, ce::kBK);
+  const int64_t x1 = int64_t(m_tiles) * b.d_tiles, w = int64_t(b.piece_tiles) * b.d_tiles;
+  double best = 1e300;
+  b.kb_per_split = piece_kb;
+  for (int s : {1, 2, 3, 4, 6, 8, 10, 12, 16, 20, 24, 32}) {
+    if (s > 1 && piece_kb / s < 8) break;
+    const int kb = ceil_div(piece_kb, s);
+    const int64_t x = x1 * ceil_div(piece_kb, kb);
+    double worst = 0;
+    for (int c = 0; c < pairs; ++c) {
+      const int64_t nx = x > c ? (x - c + pairs - 1) / pairs : 0, all = x + w > c ? (x + w - c + pairs - 1) / pairs : 0;
+      worst = std::max(worst, double(nx) * (kb + 4) + double(all - nx) * (token_kb + 4));
+    }
+    worst += s;
+    if (worst < best) { best = worst; b.kb_per_split = kb; }
+  }
   b.splits = ceil_div(piece_kb, b.kb_per_split);
   b.D = 0;
-  b.acc = b.D + aligned(size_t(q.m) * size_t(b.piece_tiles) * ce::kTile * 2);
+  b.D_stride = aligned(size_t(q.m) * size_t(b.piece_tiles) * ce::kTile * 2);
+  b.acc = b.D + size_t(b.buffers) * b.D_stride;
   b.corr = b.acc + aligned(size_t(b.splits) * size_t(b.acc_rows) * size_t(q.d) * 4);
   b.bytes = b.corr + aligned(size_t(q.m) * 4);
   return b;
@@ -278,25 +338,28 @@ cudaError_t ce_fwd(const CeProblem& q, const void* X, const void* W, const int64
   p.units = p.m_tiles * p.n_tiles;
   p.part = reinterpret_cast<float2*>(w8 + f.part);
   p.target_logit = reinterpret_cast<float*>(w8 + f.target);
+  p.ticket = reinterpret_cast<uint32_t*>(w8 + f.ticket);
   CUtensorMap ta, tb;
   if (!make_tmap_bf16(&ta, X, q.m, q.d, ce::kBK, ce::kBM) || !make_tmap_bf16(&tb, W, q.vocab, q.d, ce::kBK, ce::kBM)) return cudaErrorInvalidValue;
-  cudaError_t e = launch<ce::LSE>(ta, tb, ta, tb, ta, ta, p, st);
+  const cudaError_t e = launch<ce::LSE>(ta, tb, ta, tb, ta, ta, p, false, st);
   if (e != cudaSuccess) return e;
-  float2* sums = total ? reinterpret_cast<float2*>(w8 + f.sums) : nullptr;
-  ce_join_kernel<<<f.blocks, 1024, 0, st>>>(p.part, p.target_logit, static_cast<const __nv_bfloat16*>(X), static_cast<const __nv_bfloat16*>(W),
-                                            targets, weight, p.tokens, p.d, p.vocab, f.parts, p.c, loss, lse, sums);
-  e = launched();
-  if (e != cudaSuccess || !total) return e;
-  ce_total_kernel<<<1, 1024, 0, st>>>(sums, f.blocks, total);
-  return launched();
+  return launch_kernel(ce_join_kernel, unsigned(f.blocks), 1024, 0, 1, true, st, static_cast<const float2*>(p.part),
+                       static_cast<const float*>(p.target_logit), static_cast<const __nv_bfloat16*>(X), static_cast<const __nv_bfloat16*>(W),
+                       targets, weight, p.tokens, p.d, p.vocab, f.parts, p.c, loss, lse, reinterpret_cast<float2*>(w8 + f.sums), p.ticket, total);
 }
 
+// The launches of a backward pass, L = DLOGITS and G = GRADS of a piece:
+//     L0  L1  G0  L2  G1  L3  G2  ...  G(n-1)
+// Two launches that follow one another need nothing of each other (D has three buffers), and each may start while the one
+// before it is still at its last tiles: a launch lets the next one start only after the end of the one before itself, so
+// that whatever a launch sees running beside it is its direct neighbour.  G0 thus finds L0 finished, L3 (which writes the
+// buffer that G0 read) finds G0 finished, and G1 adds to sums that G0 has finished.  The last G follows another G, to whose
+// sums it adds, and waits for its end.
 cudaError_t ce_bwd(const CeProblem& q, const void* X, const void* W, const int64_t* targets, const float* weight, const float* lse,
                    const float* denom, float scale, void* dX, void* dW, void* ws, int* status, cudaStream_t st) {
   const BwdPlan b = bwd_plan(q);
   uint8_t* w8 = static_cast<uint8_t*>(ws);
   const int64_t piece_cols = int64_t(b.piece_tiles) * ce::kTile;
-  void* D = w8 + b.D;
   float* acc = reinterpret_cast<float*>(w8 + b.acc);
   float* corr = reinterpret_cast<float*>(w8 + b.corr);
   Params p{};
@@ -306,41 +369,53 @@ cudaError_t ce_bwd(const CeProblem& q, const void* X, const void* W, const int64
   p.denom = denom;
   p.scale = scale * q.logit_scale;
   p.acc_rows = b.acc_rows;
-  p.splits = b.splits;
   p.kb_per_split = b.kb_per_split;
   p.token_kb = ceil_div(q.m, ce::kBK);
   p.d_tiles = b.d_tiles;
-  CUtensorMap xk, wk, dst, dk, dmn, wmn, xmn, accm, dwm;
+  p.d_width = b.d_width;
+  CUtensorMap xk, wk, wmn, xmn, accm, dwm, dst[kBuffers], dk[kBuffers], dmn[kBuffers];
   if (!make_tmap_bf16(&xk, X, q.m, q.d, ce::kBK, ce::kBM) || !make_tmap_bf16(&wk, W, q.vocab, q.d, ce::kBK, ce::kBM) ||
-      !make_tmap_bf16_store_sw64(&dst, D, q.m, piece_cols) || !make_tmap_bf16(&dk, D, q.m, piece_cols, ce::kBK, ce::kBM) ||
-      !make_tmap_bf16(&dmn, D, q.m, piece_cols, 64, ce::kBK) || !make_tmap_bf16(&wmn, W, q.vocab, q.d, 64, ce::kBK) ||
-      !make_tmap_bf16(&xmn, X, q.m, q.d, 64, ce::kBK) ||
+      !make_tmap_bf16(&wmn, W, q.vocab, q.d, 64, ce::kBK) || !make_tmap_bf16(&xmn, X, q.m, q.d, 64, ce::kBK) ||
       !make_tmap_2d(&accm, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, acc, int64_t(b.splits) * b.acc_rows, q.d, 16, 32, CU_TENSOR_MAP_SWIZZLE_64B) ||
-      !make_tmap_bf16_store_sw64(&dwm, dW ? dW : D, q.vocab, q.d))
+      !make_tmap_bf16_store_sw64(&dwm, dW ? dW : X, dW ? q.vocab : q.m, q.d))
     return cudaErrorInvalidValue;
+  for (int k = 0; k < b.buffers; ++k) {
+    void* D = w8 + b.D + k * b.D_stride;
+    if (!make_tmap_bf16_store_sw64(&dst[k], D, q.m, piece_cols) || !make_tmap_bf16(&dk[k], D, q.m, piece_cols, ce::kBK, ce::kBM) ||
+        !make_tmap_bf16(&dmn[k], D, q.m, piece_cols, 64, ce::kBK))
+      return cudaErrorInvalidValue;
+  }
   const int n_tiles = ceil_div(q.vocab, ce::kTile);
-  for (int piece = 0; piece < b.pieces; ++piece) {
-    const int tiles = std::min(b.piece_tiles, n_tiles - piece * b.piece_tiles);
+  auto set_piece = [&](int piece) {
     p.v0 = piece * int(piece_cols);
+    p.n_tiles = std::min(b.piece_tiles, n_tiles - piece * b.piece_tiles);
+  };
+  auto dlogits = [&](int piece) {
+    set_piece(piece);
+    const CUtensorMap& out = dst[piece % kBuffers];
+    p.units = p.m_tiles * p.n_tiles;
+    return launch<ce::DLOGITS>(xk, wk, xk, wk, out, out, p, piece > 0, st);
+  };
+  auto grads = [&](int piece) {
+    set_piece(piece);
     p.first_piece = piece == 0;
-    p.n_tiles = tiles;
-    p.units = p.m_tiles * tiles;
-    cudaError_t e = launch<ce::DLOGITS>(xk, wk, xk, wk, dst, dst, p, st);
-    if (e != cudaSuccess) return e;
-    p.piece_kb = tiles * (ce::kTile / ce::kBK);
+    p.piece_kb = p.n_tiles * (ce::kTile / ce::kBK);
     // a last piece shorter than the others may leave the last splits without a k-block: those tiles are left out
     const int splits = std::min(b.splits, ceil_div(p.piece_kb, b.kb_per_split));
     p.x_units = dX ? splits * p.m_tiles * b.d_tiles : 0;
-    p.units = p.x_units + (dW ? tiles * b.d_tiles : 0);
-    e = launch<ce::GRADS>(dk, wmn, dmn, xmn, accm, dwm, p, st);
-    if (e != cudaSuccess) return e;
+    p.units = p.x_units + (dW ? p.n_tiles * b.d_tiles : 0);
+    return launch<ce::GRADS>(dk[piece % kBuffers], wmn, dmn[piece % kBuffers], xmn, accm, dwm, p, piece + 1 < b.pieces, st);
+  };
+  cudaError_t e = dlogits(0);
+  for (int piece = 0; piece < b.pieces && e == cudaSuccess; ++piece) {
+    if (piece + 1 < b.pieces) e = dlogits(piece + 1);
+    if (e == cudaSuccess) e = grads(piece);
   }
-  if (!dX) return cudaSuccess;
+  if (e != cudaSuccess || !dX) return e;
   const int64_t threads = q.m * (q.d / 8);
-  ce_finish_kernel<<<unsigned((threads + 255) / 256), 256, 0, st>>>(acc, b.splits, int64_t(b.acc_rows) * q.d, corr, targets,
-                                                                   static_cast<const __nv_bfloat16*>(W), denom, p.scale,
-                                                                   static_cast<__nv_bfloat16*>(dX), p.tokens, p.d, p.vocab);
-  return launched();
+  return launch_kernel(ce_finish_kernel, unsigned((threads + 255) / 256), 256, 0, 1, true, st, static_cast<const float*>(acc), b.splits,
+                       int64_t(b.acc_rows) * q.d, static_cast<const float*>(corr), targets, static_cast<const __nv_bfloat16*>(W), denom,
+                       p.scale, static_cast<__nv_bfloat16*>(dX), p.tokens, p.d, p.vocab);
 }
 
 }  // namespace acx

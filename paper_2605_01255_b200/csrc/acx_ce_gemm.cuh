@@ -50,8 +50,9 @@ struct Params {
   // vocabulary tiles together, so that a group's rows of X stay in L2 while W streams by once per group.
   int m_tiles, n_tiles, group;
   int v0;                       // first vocabulary column of the piece (DLOGITS, GRADS)
-  // GRADS: x_units of dX = splits x m_tiles x d_tiles, then dW: piece_tiles x d_tiles
-  int d_tiles, x_units, splits, kb_per_split, piece_kb, token_kb;
+  // GRADS: x_units of dX = splits x m_tiles x d_tiles (the long ones first), then dW: piece_tiles x d_tiles
+  int d_tiles, d_width;         // columns of d per tile: a multiple of 32
+  int x_units, kb_per_split, piece_kb, token_kb;
   int acc_rows;                 // rows of one split's fp32 sums (tokens rounded up to whole tiles)
   int first_piece;              // the sums are stored, not added
   float c;                      // logit_scale * log2(e): exponents are taken in base 2
@@ -60,6 +61,7 @@ struct Params {
   const float* weight;          // may be null: one
   float2* part;                 // LSE: [ceil(vocab / 128)][tokens] (maximum, sum), base 2
   float* target_logit;          // LSE: [tokens], base 2
+  uint32_t* ticket;             // LSE: set to zero for the kernel behind it
   float* corr;                  // DLOGITS: [tokens] what rounding took from the target's element of D
   const float* denom;           // GRADS: may be null; gradients are multiplied by scale / denom
   float scale;
@@ -69,7 +71,7 @@ struct Params {
 struct Unit {
   bool x;          // GRADS: a tile of dX (else of dW)
   int m0, n0;      // first row and column of the pair's tile
-  int bn;          // columns (a multiple of 64, at most 256)
+  int bn;          // columns (a multiple of 32, at most 256)
   int kb0, kb1;    // k-blocks
   int split;
 };
@@ -105,8 +107,8 @@ __device__ __forceinline__ Unit decode(const Params& p, int u) {
     t.kb0 = 0;
     t.kb1 = p.token_kb;
   }
-  t.n0 = nt * kTile;
-  t.bn = min(kTile, (p.d - t.n0 + 63) & ~63);
+  t.n0 = nt * p.d_width;
+  t.bn = min(p.d_width, (p.d - t.n0 + 31) & ~31);
   return t;
 }
 
@@ -156,6 +158,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       ptx::mbar_init(tempty_bar(a), 2 * kEpiWarps);   // the epilogue warps of both CTAs
     }
     *abort_flag = 0;
+    if (KIND == LSE && blockIdx.x == 0) *p.ticket = 0u;
     ptx::fence_barrier_init();
     ptx::prefetch_tensormap(&tmap_a);
     ptx::prefetch_tensormap(&tmap_b);
@@ -231,6 +234,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (!ptx::mbar_wait(empty_bar(s), ph, abort_flag)) { give_up(); ok = false; }
         }
       }
+      // Launches may overlap with the one before them, not with the one before that (see ce_bwd): every CTA waits for the
+      // end of the launch before this one, by now long past as a rule, before it lets the next one start.
+      asm volatile("griddepcontrol.wait;" ::: "memory");
+      asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------------ UMMA issuer (the leader's)
@@ -392,7 +399,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
       } else {
-        const int cols = min(128, p.d - col0);          // columns of this half that exist (may be negative)
+        const int cols = min(min(128, t.bn - half * 128), p.d - col0);   // columns of this half that exist (may be negative)
         if (t.x) {
           for (int c0 = 0; c0 < cols; c0 += 32) {
             __syncwarp();
