@@ -13,7 +13,7 @@ namespace {
 
 using ce::Params;
 
-constexpr int kTokensPerBlock = 8;
+constexpr int kTokensPerBlock = 8, kJoinThreads = 512;
 
 __device__ __forceinline__ float dot8(uint4 a, uint4 b, float s) {
   const uint32_t x[4] = {a.x, a.y, a.z, a.w}, w[4] = {b.x, b.y, b.z, b.w};
@@ -36,28 +36,28 @@ __device__ __forceinline__ void join_pair(float& m, float& s, float m1, float s1
   s = a + b;
 }
 
-// Joins the (maximum, sum) pairs of 8 tokens: 32 warps; a lane has token lane & 7 and every 128th pair, eight at a time.  The
-// target's logit is taken again as a plain fp32 product (four warps per token): the tensor core adds 16 products at a time
+// Joins the (maximum, sum) pairs of 8 tokens: 16 warps; a lane has token lane & 7 and every 64th pair, eight at a time.  The
+// target's logit is taken again as a plain fp32 product (two warps per token): the tensor core adds 16 products at a time
 // with truncation, an error of up to 2^-24 of the logit per step and of one sign, which the loss of an unlikely token would
 // show in full; its term of the sum is exchanged along with it.  The last block to finish adds the blocks' sums of losses
 // and weights, in order.  Launched behind the logits' kernel before that has finished; the products need nothing of it.
-__global__ void __launch_bounds__(1024) ce_join_kernel(const float2* part, const float* target_logit, const __nv_bfloat16* __restrict__ X,
+__global__ void __launch_bounds__(kJoinThreads, 3) ce_join_kernel(const float2* part, const float* target_logit, const __nv_bfloat16* __restrict__ X,
                                                        const __nv_bfloat16* __restrict__ W, const int64_t* __restrict__ targets,
                                                        const float* __restrict__ weight, int tokens, int d, int vocab, int parts, float c,
                                                        float* __restrict__ loss, float* __restrict__ lse, float2* block_sums,
                                                        uint32_t* ticket, float* __restrict__ total) {
-  __shared__ float2 red[32][9];
-  __shared__ float exact[32];
+  __shared__ float2 red[16][9];
+  __shared__ float exact[16];
   __shared__ bool last;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t0 = int(blockIdx.x) * kTokensPerBlock;
   {
-    const int tt = t0 + (warp >> 2);
+    const int tt = t0 + (warp >> 1);
     const int64_t y = tt < tokens ? __ldg(targets + tt) : -1;
     float p = 0.f;
     if (y >= 0 && y < vocab) {
       const uint4* x = reinterpret_cast<const uint4*>(X + int64_t(tt) * d);
       const uint4* w = reinterpret_cast<const uint4*>(W + y * int64_t(d));
-      for (int i = (warp & 3) * 32 + lane; i < d / 8; i += 128) p = dot8(__ldg(x + i), __ldg(w + i), p);
+      for (int i = (warp & 1) * 32 + lane; i < d / 8; i += 64) p = dot8(__ldg(x + i), __ldg(w + i), p);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) p += __shfl_xor_sync(0xFFFFFFFFu, p, o);
@@ -67,10 +67,10 @@ __global__ void __launch_bounds__(1024) ce_join_kernel(const float2* part, const
   const int tok = lane & 7, t = t0 + tok;
   float m = -INFINITY, s = 0.f;
   if (t < tokens) {
-    for (int q = warp * 4 + (lane >> 3); q < parts; q += 8 * 128) {   // eight pairs in flight
+    for (int q = warp * 4 + (lane >> 3); q < parts; q += 8 * 64) {   // eight pairs in flight
       float2 v[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = q + 128 * i < parts ? __ldcg(part + int64_t(q + 128 * i) * tokens + t) : make_float2(-INFINITY, 0.f);
+      for (int i = 0; i < 8; ++i) v[i] = q + 64 * i < parts ? __ldcg(part + int64_t(q + 64 * i) * tokens + t) : make_float2(-INFINITY, 0.f);
 #pragma unroll
       for (int i = 0; i < 8; ++i) join_pair(m, s, v[i].x, v[i].y);
     }
@@ -82,14 +82,14 @@ __global__ void __launch_bounds__(1024) ce_join_kernel(const float2* part, const
   if (warp == 0) {
     m = -INFINITY;
     s = 0.f;
-    for (int k = lane >> 3; k < 32; k += 4) join_pair(m, s, red[k][tok].x, red[k][tok].y);
+    for (int k = lane >> 3; k < 16; k += 4) join_pair(m, s, red[k][tok].x, red[k][tok].y);
 #pragma unroll
     for (int o = 8; o <= 16; o <<= 1) join_pair(m, s, __shfl_xor_sync(0xFFFFFFFFu, m, o), __shfl_xor_sync(0xFFFFFFFFu, s, o));
     float wl = 0.f, wt = 0.f;
     if (lane < 8 && t < tokens) {
       const int64_t y = __ldg(targets + t);
       const bool trained = y >= 0 && y < vocab;
-      const float ty = ((exact[4 * tok] + exact[4 * tok + 1]) + (exact[4 * tok + 2] + exact[4 * tok + 3])) * c;
+      const float ty = (exact[2 * tok] + exact[2 * tok + 1]) * c;
       if (trained) s += exp2f(ty - m) - exp2f(__ldcg(target_logit + t) - m);
       const float l2 = m + log2f(s);
       constexpr float kLn2 = 0.6931471805599453f;
@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(1024) ce_join_kernel(const float2* part, const
   if (!last) return;
   __threadfence();
   float a = 0.f, b = 0.f;
-  for (int i = threadIdx.x; i < int(gridDim.x); i += 1024) {
+  for (int i = threadIdx.x; i < int(gridDim.x); i += kJoinThreads) {
     const float2 v = __ldcg(block_sums + i);
     a += v.x;
     b += v.y;
@@ -128,8 +128,8 @@ __global__ void __launch_bounds__(1024) ce_join_kernel(const float2* part, const
   if (lane == 0) red[warp][0] = make_float2(a, b);
   __syncthreads();
   if (warp != 0) return;
-  a = red[lane][0].x;
-  b = red[lane][0].y;
+  a = lane < 16 ? red[lane][0].x : 0.f;
+  b = lane < 16 ? red[lane][0].y : 0.f;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
@@ -278,7 +278,10 @@ FwdPlan fwd_plan(const CeProblem& q) {
 
 // Pieces of the vocabulary: D of one piece takes at most about 128 MB, so that much of it is still in L2 when the two
 // products read it, and the pieces are of equal size.  Up to three pieces are under way at a time (see ce_bwd).
-constexpr int64_t kPieceBytes = int64_t(128) << 20;
+#ifndef PIECE_MB
+#define PIECE_MB 128
+#endif
+constexpr int64_t kPieceBytes = int64_t(PIECE_MB) << 20;
 constexpr int kBuffers = 3;
 struct BwdPlan {
   int piece_tiles, pieces, buffers, splits, kb_per_split, d_tiles, d_width, acc_rows;
@@ -343,7 +346,7 @@ cudaError_t ce_fwd(const CeProblem& q, const void* X, const void* W, const int64
   if (!make_tmap_bf16(&ta, X, q.m, q.d, ce::kBK, ce::kBM) || !make_tmap_bf16(&tb, W, q.vocab, q.d, ce::kBK, ce::kBM)) return cudaErrorInvalidValue;
   const cudaError_t e = launch<ce::LSE>(ta, tb, ta, tb, ta, ta, p, false, st);
   if (e != cudaSuccess) return e;
-  return launch_kernel(ce_join_kernel, unsigned(f.blocks), 1024, 0, 1, true, st, static_cast<const float2*>(p.part),
+  return launch_kernel(ce_join_kernel, unsigned(f.blocks), kJoinThreads, 0, 1, true, st, static_cast<const float2*>(p.part),
                        static_cast<const float*>(p.target_logit), static_cast<const __nv_bfloat16*>(X), static_cast<const __nv_bfloat16*>(W),
                        targets, weight, p.tokens, p.d, p.vocab, f.parts, p.c, loss, lse, reinterpret_cast<float2*>(w8 + f.sums), p.ticket, total);
 }

@@ -19,6 +19,8 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <type_traits>
+
 #include "acx_internal.h"
 #include "acx_umma.cuh"
 
@@ -192,29 +194,45 @@ __global__ void __launch_bounds__(kThreads, 1)
         const Unit t = decode<KIND>(p, u);
         const int a_row0 = t.m0 + int(rank) * kBM;
         const int hw = t.bn >> 1, b_row0 = t.n0 + int(rank) * hw;       // this CTA's half of the B rows
-        const int b_chunks = KIND == GRADS ? (hw + 63) >> 6 : 0;
-        const uint32_t bytes = kABytes + (KIND == GRADS ? b_chunks * kChunkBytes : kBBytes);
-        for (int kb = t.kb0; kb < t.kb1; ++kb) {
-          if (!ptx::mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag)) { give_up(); ok = false; break; }
-          const uint32_t a_dst = smem_base + stage * kStageBytes, b_dst = a_dst + kABytes;
-          const uint32_t bar = on_leader(full_bar(stage));   // both CTAs' bytes are counted on the leader's barrier
+        // one loop per operand layout, so that everything that does not change along K is fixed in it
+        auto stages = [&](auto load) {
+          for (int kb = t.kb0; kb < t.kb1; ++kb) {
+            if (!ptx::mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag)) { give_up(); ok = false; break; }
+            const uint32_t a_dst = smem_base + stage * kStageBytes;
+            armed |= 1u << stage;
+            load(a_dst, a_dst + kABytes, on_leader(full_bar(stage)), kb * kBK);   // both CTAs' bytes are counted on the leader's barrier
+            if (++stage == kStages) { stage = 0; phase ^= 1u; }
+          }
+        };
+        auto arm = [&](uint32_t bytes) {
           if (rank == 0) ptx::mbar_arrive_expect_tx(full_bar(stage), 2 * bytes);
-          armed |= 1u << stage;
-          const int k0 = kb * kBK;
-          if (KIND != GRADS) {
+        };
+        if (KIND != GRADS) {
+          const int w_row0 = p.v0 + b_row0;
+          stages([&](uint32_t a_dst, uint32_t b_dst, uint32_t bar, int k0) {
+            arm(kABytes + kBBytes);
             ptx::tma_load_2d_pair(a_dst, &tmap_a, bar, k0, a_row0);
-            ptx::tma_load_2d_pair(b_dst, &tmap_b, bar, k0, p.v0 + b_row0);
-          } else {
-            if (t.x) {
+            ptx::tma_load_2d_pair(b_dst, &tmap_b, bar, k0, w_row0);
+          });
+        } else {
+          const bool two = hw > 64;     // 64-column chunks of this CTA's half
+          const uint32_t bytes = kABytes + (two ? 2 : 1) * kChunkBytes;
+          if (t.x) {
+            stages([&](uint32_t a_dst, uint32_t b_dst, uint32_t bar, int k0) {
+              arm(bytes);
               ptx::tma_load_2d_pair(a_dst, &tmap_a, bar, k0, a_row0);
-            } else {
+              ptx::tma_load_2d_pair(b_dst, &tmap_b, bar, b_row0, p.v0 + k0);
+              if (two) ptx::tma_load_2d_pair(b_dst + kChunkBytes, &tmap_b, bar, b_row0 + 64, p.v0 + k0);
+            });
+          } else {
+            stages([&](uint32_t a_dst, uint32_t b_dst, uint32_t bar, int k0) {
+              arm(bytes);
               ptx::tma_load_2d_pair(a_dst, &tmap_a2, bar, a_row0, k0);
               ptx::tma_load_2d_pair(a_dst + kChunkBytes, &tmap_a2, bar, a_row0 + 64, k0);
-            }
-            for (int c = 0; c < b_chunks; ++c)
-              ptx::tma_load_2d_pair(b_dst + c * kChunkBytes, t.x ? &tmap_b : &tmap_b2, bar, b_row0 + 64 * c, t.x ? p.v0 + k0 : k0);
+              ptx::tma_load_2d_pair(b_dst, &tmap_b2, bar, b_row0, k0);
+              if (two) ptx::tma_load_2d_pair(b_dst + kChunkBytes, &tmap_b2, bar, b_row0 + 64, k0);
+            });
           }
-          if (++stage == kStages) { stage = 0; phase ^= 1u; }
         }
       }
       if (!ok) {
@@ -247,26 +265,29 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool ok = true;
       for (int u = pair; ok && u < p.units; u += pairs, ++it) {
         const Unit t = decode<KIND>(p, u);
-        const bool a_mn = KIND == GRADS && !t.x;
-        constexpr bool b_mn = KIND == GRADS;
-        const uint32_t idesc = ptx::make_idesc_bf16(kTile, t.bn, a_mn, b_mn);
-        const uint32_t a_lbo = a_mn ? kChunkBytes : 16, a_step = (a_mn ? kUmmaK * 128 : kUmmaK * 2) >> 4;
-        constexpr uint32_t b_lbo = b_mn ? kChunkBytes : 16, b_step = (b_mn ? kUmmaK * 128 : kUmmaK * 2) >> 4;
         const int acc = it & 1;
         const uint32_t d_tmem = tmem_base + acc * kAccCols;
         if (!ptx::mbar_wait_cluster(tempty_bar(acc), ((it >> 1) & 1) ^ 1u, abort_flag)) { give_up(); ok = false; break; }
         ptx::tcgen05_fence_after_sync();
-        for (int kb = t.kb0; kb < t.kb1; ++kb) {
-          if (!ptx::mbar_wait_cluster(full_bar(stage), phase, abort_flag)) { give_up(); ok = false; break; }
-          ptx::tcgen05_fence_after_sync();
-          const uint32_t a_addr = smem_base + stage * kStageBytes, b_addr = a_addr + kABytes;
-          const uint64_t da = ptx::make_smem_desc(a_addr, a_lbo, 1024), db = ptx::make_smem_desc(b_addr, b_lbo, 1024);
+        auto products = [&](auto a_is_mn) {
+          constexpr bool a_mn = decltype(a_is_mn)::value, b_mn = KIND == GRADS;
+          constexpr uint32_t a_lbo = a_mn ? kChunkBytes : 16, a_step = (a_mn ? kUmmaK * 128 : kUmmaK * 2) >> 4;
+          constexpr uint32_t b_lbo = b_mn ? kChunkBytes : 16, b_step = (b_mn ? kUmmaK * 128 : kUmmaK * 2) >> 4;
+          const uint32_t idesc = ptx::make_idesc_bf16(kTile, t.bn, a_mn, b_mn);
+          for (int kb = t.kb0; kb < t.kb1; ++kb) {
+            if (!ptx::mbar_wait_cluster(full_bar(stage), phase, abort_flag)) { give_up(); ok = false; break; }
+            ptx::tcgen05_fence_after_sync();
+            const uint32_t a_addr = smem_base + stage * kStageBytes, b_addr = a_addr + kABytes;
+            const uint64_t da = ptx::make_smem_desc(a_addr, a_lbo, 1024), db = ptx::make_smem_desc(b_addr, b_lbo, 1024);
 #pragma unroll
-          for (int k = 0; k < kBK / kUmmaK; ++k)
-            ptx::umma_bf16_pair(d_tmem, da + uint64_t(k * a_step), db + uint64_t(k * b_step), idesc, kb > t.kb0 || k > 0);
-          ptx::umma_commit_pair(empty_bar(stage), 3);
-          if (++stage == kStages) { stage = 0; phase ^= 1u; }
-        }
+            for (int k = 0; k < kBK / kUmmaK; ++k)
+              ptx::umma_bf16_pair(d_tmem, da + uint64_t(k * a_step), db + uint64_t(k * b_step), idesc, kb > t.kb0 || k > 0);
+            ptx::umma_commit_pair(empty_bar(stage), 3);
+            if (++stage == kStages) { stage = 0; phase ^= 1u; }
+          }
+        };
+        if (KIND == GRADS && !t.x) products(std::true_type{});
+        else products(std::false_type{});
         if (ok) ptx::umma_commit_pair(tfull_bar(acc), 3);
       }
     }
