@@ -359,16 +359,22 @@ def _strided(t: torch.Tensor, shape: Tuple[int, int], dtype, name: str) -> Tuple
     return t.data_ptr(), (t.stride(0) if shape[0] > 1 else shape[1])
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", None)   # without the lazy initialisation: there are CUDA tensors by now
+
+
 def _stream_arg(stream) -> int:
     if stream is not None:
         return stream.cuda_stream
-    return _raw_stream(torch.cuda.current_device()) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+    if _raw_stream is not None and _current_device is not None and torch.cuda.is_initialized():
+        return _raw_stream(_current_device())
+    return torch.cuda.current_stream().cuda_stream
 
 
 def _q8_ptrs(desc: acx_rows_desc, codes, scales, name: str) -> Tuple[Optional[int], Optional[int]]:
     rows, cols = desc.rows, desc.cols
-    return (_dense(codes, (rows, cols), torch.int8, name + " codes"),
-            _dense(scales, (rows, -(-cols // ACX_Q8_GROUP)), torch.float32, name + " scales"))
+    if codes is None and scales is None:
+        return None, None
+    return _dense(codes, (rows, cols), torch.int8, name), _dense(scales, (rows, -(-cols // ACX_Q8_GROUP)), torch.float32, name)
 
 
 def _rows_dtype(desc: acx_rows_desc):
@@ -378,13 +384,13 @@ def _rows_dtype(desc: acx_rows_desc):
 def acx_q8_store(desc: acx_rows_desc, X, codes, scales, stream=None) -> None:
     """Codes and scales of X (rows x cols; its rows may be strided)."""
     xp, ldx = _strided(X, (desc.rows, desc.cols), _rows_dtype(desc), "X")
-    _check(lib().acx_q8_store(desc, xp, ldx, *_q8_ptrs(desc, codes, scales, "X"), _stream_arg(stream)), "acx_q8_store")
+    _check(lib().acx_q8_store(desc, xp, ldx, *_q8_ptrs(desc, codes, scales, "checkpoint of X"), _stream_arg(stream)), "acx_q8_store")
 
 
 def acx_q8_load(desc: acx_rows_desc, codes, scales, X, stream=None) -> None:
     """The values of an 8-bit checkpoint into X (rows x cols; its rows may be strided)."""
     xp, ldx = _strided(X, (desc.rows, desc.cols), _rows_dtype(desc), "X")
-    _check(lib().acx_q8_load(desc, *_q8_ptrs(desc, codes, scales, "X"), xp, ldx, _stream_arg(stream)), "acx_q8_load")
+    _check(lib().acx_q8_load(desc, *_q8_ptrs(desc, codes, scales, "8-bit X"), xp, ldx, _stream_arg(stream)), "acx_q8_load")
 
 
 def acx_swiglu_fwd(desc: acx_rows_desc, G, U, H, Gq=None, Gs=None, Uq=None, Us=None, stream=None) -> None:
@@ -392,7 +398,7 @@ def acx_swiglu_fwd(desc: acx_rows_desc, G, U, H, Gq=None, Gs=None, Uq=None, Us=N
     shape, dt = (desc.rows, desc.cols), _rows_dtype(desc)
     gp, ldg = _strided(G, shape, dt, "G")
     up, ldu = _strided(U, shape, dt, "U")
-    _check(lib().acx_swiglu_fwd(desc, gp, ldg, up, ldu, _dense(H, shape, dt, "H"), *_q8_ptrs(desc, Gq, Gs, "G"), *_q8_ptrs(desc, Uq, Us, "U"),
+    _check(lib().acx_swiglu_fwd(desc, gp, ldg, up, ldu, _dense(H, shape, dt, "H"), *_q8_ptrs(desc, Gq, Gs, "checkpoint of G"), *_q8_ptrs(desc, Uq, Us, "checkpoint of U"),
                                 _stream_arg(stream)), "acx_swiglu_fwd")
 
 
@@ -401,7 +407,7 @@ def acx_swiglu_bwd(desc: acx_rows_desc, dH, Gq, Gs, Uq, Us, dG, dU, stream=None)
     shape, dt = (desc.rows, desc.cols), _rows_dtype(desc)
     gp, ldg = _strided(dG, shape, dt, "dG")
     up, ldu = _strided(dU, shape, dt, "dU")
-    _check(lib().acx_swiglu_bwd(desc, _dense(dH, shape, dt, "dH"), *_q8_ptrs(desc, Gq, Gs, "G"), *_q8_ptrs(desc, Uq, Us, "U"), gp, ldg, up, ldu,
+    _check(lib().acx_swiglu_bwd(desc, _dense(dH, shape, dt, "dH"), *_q8_ptrs(desc, Gq, Gs, "checkpoint of G"), *_q8_ptrs(desc, Uq, Us, "checkpoint of U"), gp, ldg, up, ldu,
                                 _stream_arg(stream)), "acx_swiglu_bwd")
 
 
@@ -411,7 +417,7 @@ def acx_norm_join_fwd(desc: acx_rows_desc, h, b, w_post, gate, w_pre, h_out, y, 
     shape, vec, row, dt = (desc.rows, desc.cols), (desc.cols,), (desc.rows,), _rows_dtype(desc)
     _check(lib().acx_norm_join_fwd(desc, _dense(h, shape, dt, "h"), _dense(b, shape, dt, "b"), _dense(w_post, vec, dt, "w_post"),
                                    _dense(gate, vec, dt, "gate"), _dense(w_pre, vec, dt, "w_pre"), _dense(h_out, shape, dt, "h_out"),
-                                   _dense(y, shape, dt, "y"), *_q8_ptrs(desc, Hq, Hs, "h"), *_q8_ptrs(desc, Bq, Bs, "b"),
+                                   _dense(y, shape, dt, "y"), *_q8_ptrs(desc, Hq, Hs, "checkpoint of h"), *_q8_ptrs(desc, Bq, Bs, "checkpoint of b"),
                                    _dense(rstd_post, row, torch.float32, "rstd_post"), _dense(rstd_pre, row, torch.float32, "rstd_pre"),
                                    eps, alpha, _stream_arg(stream)), "acx_norm_join_fwd")
 
@@ -422,8 +428,8 @@ def acx_norm_join_bwd(desc: acx_rows_desc, dy, dh_next, w_post, gate, w_pre, Hq,
     shape, vec, row, dt, f32 = (desc.rows, desc.cols), (desc.cols,), (desc.rows,), _rows_dtype(desc), torch.float32
     wp, wn = _ws(ws)
     _check(lib().acx_norm_join_bwd(desc, _dense(dy, shape, dt, "dy"), _dense(dh_next, shape, dt, "dh_next"), _dense(w_post, vec, dt, "w_post"),
-                                   _dense(gate, vec, dt, "gate"), _dense(w_pre, vec, dt, "w_pre"), *_q8_ptrs(desc, Hq, Hs, "h"),
-                                   *_q8_ptrs(desc, Bq, Bs, "b"), _dense(rstd_post, row, f32, "rstd_post"),
+                                   _dense(gate, vec, dt, "gate"), _dense(w_pre, vec, dt, "w_pre"), *_q8_ptrs(desc, Hq, Hs, "checkpoint of h"),
+                                   *_q8_ptrs(desc, Bq, Bs, "checkpoint of b"), _dense(rstd_post, row, f32, "rstd_post"),
                                    _dense(rstd_pre, row, f32, "rstd_pre"), _dense(dh, shape, dt, "dh"), _dense(db, shape, dt, "db"),
                                    _dense(dw_post, vec, f32, "dw_post"), _dense(dgate, vec, f32, "dgate"), _dense(dw_pre, vec, f32, "dw_pre"),
                                    alpha, wp, wn, _stream_arg(stream)), "acx_norm_join_bwd")

@@ -26,6 +26,7 @@ __device__ __forceinline__ float dot8(uint4 a, uint4 b, float s) {
 }
 
 __device__ __forceinline__ void wait_for_launch_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_launch_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // (m, s) <- (m, s) joined with (m1, s1): sums of 2^(x - maximum)
 __device__ __forceinline__ void join_pair(float& m, float& s, float m1, float s1) {
@@ -64,6 +65,7 @@ __global__ void __launch_bounds__(kJoinThreads, 3) ce_join_kernel(const float2* 
     if (lane == 0) exact[warp] = p;
   }
   wait_for_launch_before();
+  let_next_launch_start();
   const int tok = lane & 7, t = t0 + tok;
   float m = -INFINITY, s = 0.f;
   if (t < tokens) {
@@ -147,6 +149,8 @@ __global__ void __launch_bounds__(256) ce_finish_kernel(const float* acc, int sp
                                                         const float* corr, const int64_t* __restrict__ targets,
                                                         const __nv_bfloat16* __restrict__ W, const float* __restrict__ denom, float scale,
                                                         __nv_bfloat16* __restrict__ dX, int tokens, int d, int vocab) {
+  wait_for_launch_before();
+  let_next_launch_start();
   const int vecs = d / 8;
   const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
   const int64_t t = i / vecs;
@@ -156,7 +160,6 @@ __global__ void __launch_bounds__(256) ce_finish_kernel(const float* acc, int sp
   float v[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = 0.f;
-  wait_for_launch_before();
   for (int s0 = 0; s0 < splits; s0 += 4) {   // four splits' loads under way, added in order
     float4 a[4], b[4];
 #pragma unroll
@@ -196,10 +199,10 @@ size_t aligned(size_t bytes) { return (bytes + 1023) & ~size_t(1023); }
 
 int pair_count() { return std::max(1, sm_count() / 2); }
 
-// behind: launched with programmatic stream serialization, so that it may start before the launch before it has finished.
+// With programmatic stream serialization: the kernel may start before the launch before it has finished, and says itself what
+// it waits for.
 template <typename... K, typename... A>
-cudaError_t launch_kernel(void (*kernel)(K...), unsigned grid, unsigned threads, size_t smem, int cluster, bool behind, cudaStream_t st,
-                          const A&... args) {
+cudaError_t launch_kernel(void (*kernel)(K...), unsigned grid, unsigned threads, size_t smem, int cluster, cudaStream_t st, const A&... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(threads);
@@ -214,11 +217,9 @@ cudaError_t launch_kernel(void (*kernel)(K...), unsigned grid, unsigned threads,
     attr[n].val.clusterDim.z = 1;
     ++n;
   }
-  if (behind) {
-    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[n].val.programmaticStreamSerializationAllowed = 1;
-    ++n;
-  }
+  attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[n].val.programmaticStreamSerializationAllowed = 1;
+  ++n;
   cfg.attrs = attr;
   cfg.numAttrs = n;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
@@ -228,7 +229,7 @@ cudaError_t launch_kernel(void (*kernel)(K...), unsigned grid, unsigned threads,
 
 template <int KIND>
 cudaError_t launch(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& ta2, const CUtensorMap& tb2, const CUtensorMap& to,
-                   const CUtensorMap& to2, const Params& p, bool behind, cudaStream_t st) {
+                   const CUtensorMap& to2, const Params& p, cudaStream_t st) {
   auto kernel = ce::ce_kernel<KIND>;
   static DeviceOnce once;
   if (once.needed()) {
@@ -236,7 +237,7 @@ cudaError_t launch(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorM
     if (e != cudaSuccess) return e;
     once.done();
   }
-  return launch_kernel(kernel, unsigned(2 * std::min(p.units, pair_count())), ce::kThreads, ce::kSmemBytes, 2, behind, st, ta, tb, ta2, tb2,
+  return launch_kernel(kernel, unsigned(2 * std::min(p.units, pair_count())), ce::kThreads, ce::kSmemBytes, 2, st, ta, tb, ta2, tb2,
                        to, to2, p);
 }
 
@@ -258,6 +259,7 @@ void common(const CeProblem& q, Params* p, const int64_t* targets, const float* 
   p->targets = targets;
   p->weight = weight;
   p->status = status;
+  p->wait_first = 1;
 }
 
 struct FwdPlan {
@@ -344,20 +346,20 @@ cudaError_t ce_fwd(const CeProblem& q, const void* X, const void* W, const int64
   p.ticket = reinterpret_cast<uint32_t*>(w8 + f.ticket);
   CUtensorMap ta, tb;
   if (!make_tmap_bf16(&ta, X, q.m, q.d, ce::kBK, ce::kBM) || !make_tmap_bf16(&tb, W, q.vocab, q.d, ce::kBK, ce::kBM)) return cudaErrorInvalidValue;
-  const cudaError_t e = launch<ce::LSE>(ta, tb, ta, tb, ta, ta, p, false, st);
+  const cudaError_t e = launch<ce::LSE>(ta, tb, ta, tb, ta, ta, p, st);
   if (e != cudaSuccess) return e;
-  return launch_kernel(ce_join_kernel, unsigned(f.blocks), kJoinThreads, 0, 1, true, st, static_cast<const float2*>(p.part),
+  return launch_kernel(ce_join_kernel, unsigned(f.blocks), kJoinThreads, 0, 1, st, static_cast<const float2*>(p.part),
                        static_cast<const float*>(p.target_logit), static_cast<const __nv_bfloat16*>(X), static_cast<const __nv_bfloat16*>(W),
                        targets, weight, p.tokens, p.d, p.vocab, f.parts, p.c, loss, lse, reinterpret_cast<float2*>(w8 + f.sums), p.ticket, total);
 }
 
 // The launches of a backward pass, L = DLOGITS and G = GRADS of a piece:
 //     L0  L1  G0  L2  G1  L3  G2  ...  G(n-1)
-// Two launches that follow one another need nothing of each other (D has three buffers), and each may start while the one
-// before it is still at its last tiles: a launch lets the next one start only after the end of the one before itself, so
-// that whatever a launch sees running beside it is its direct neighbour.  G0 thus finds L0 finished, L3 (which writes the
-// buffer that G0 read) finds G0 finished, and G1 adds to sums that G0 has finished.  The last G follows another G, to whose
-// sums it adds, and waits for its end.
+// Two launches in the middle that follow one another need nothing of each other (D has three buffers), and each may start
+// while the one before it is still at its last tiles: a launch lets the next one start only after the end of the one before
+// itself, so that whatever a launch sees running beside it is its direct neighbour.  G0 thus finds L0 finished, L3 (which
+// writes the buffer that G0 read) finds G0 finished, and G1 adds to sums that G0 has finished.  L0 needs the forward's
+// results, and the last G follows another G, to whose sums it adds (or its own L): those two wait first.
 cudaError_t ce_bwd(const CeProblem& q, const void* X, const void* W, const int64_t* targets, const float* weight, const float* lse,
                    const float* denom, float scale, void* dX, void* dW, void* ws, int* status, cudaStream_t st) {
   const BwdPlan b = bwd_plan(q);
@@ -397,17 +399,19 @@ cudaError_t ce_bwd(const CeProblem& q, const void* X, const void* W, const int64
     set_piece(piece);
     const CUtensorMap& out = dst[piece % kBuffers];
     p.units = p.m_tiles * p.n_tiles;
-    return launch<ce::DLOGITS>(xk, wk, xk, wk, out, out, p, piece > 0, st);
+    p.wait_first = piece == 0;
+    return launch<ce::DLOGITS>(xk, wk, xk, wk, out, out, p, st);
   };
   auto grads = [&](int piece) {
     set_piece(piece);
     p.first_piece = piece == 0;
+    p.wait_first = piece + 1 == b.pieces;
     p.piece_kb = p.n_tiles * (ce::kTile / ce::kBK);
     // a last piece shorter than the others may leave the last splits without a k-block: those tiles are left out
     const int splits = std::min(b.splits, ceil_div(p.piece_kb, b.kb_per_split));
     p.x_units = dX ? splits * p.m_tiles * b.d_tiles : 0;
     p.units = p.x_units + (dW ? p.n_tiles * b.d_tiles : 0);
-    return launch<ce::GRADS>(dk[piece % kBuffers], wmn, dmn[piece % kBuffers], xmn, accm, dwm, p, piece + 1 < b.pieces, st);
+    return launch<ce::GRADS>(dk[piece % kBuffers], wmn, dmn[piece % kBuffers], xmn, accm, dwm, p, st);
   };
   cudaError_t e = dlogits(0);
   for (int piece = 0; piece < b.pieces && e == cudaSuccess; ++piece) {
@@ -416,7 +420,7 @@ cudaError_t ce_bwd(const CeProblem& q, const void* X, const void* W, const int64
   }
   if (e != cudaSuccess || !dX) return e;
   const int64_t threads = q.m * (q.d / 8);
-  return launch_kernel(ce_finish_kernel, unsigned((threads + 255) / 256), 256, 0, 1, true, st, static_cast<const float*>(acc), b.splits,
+  return launch_kernel(ce_finish_kernel, unsigned((threads + 255) / 256), 256, 0, 1, st, static_cast<const float*>(acc), b.splits,
                        int64_t(b.acc_rows) * q.d, static_cast<const float*>(corr), targets, static_cast<const __nv_bfloat16*>(W), denom,
                        p.scale, static_cast<__nv_bfloat16*>(dX), p.tokens, p.d, p.vocab);
 }

@@ -57,6 +57,7 @@ struct Params {
   int x_units, kb_per_split, piece_kb, token_kb;
   int acc_rows;                 // rows of one split's fp32 sums (tokens rounded up to whole tiles)
   int first_piece;              // the sums are stored, not added
+  int wait_first;               // this launch needs what the launch before it writes (else only what the one before that does)
   float c;                      // logit_scale * log2(e): exponents are taken in base 2
   const int64_t* targets;
   const float* lse;             // natural logarithm
@@ -160,7 +161,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       ptx::mbar_init(tempty_bar(a), 2 * kEpiWarps);   // the epilogue warps of both CTAs
     }
     *abort_flag = 0;
-    if (KIND == LSE && blockIdx.x == 0) *p.ticket = 0u;
     ptx::fence_barrier_init();
     ptx::prefetch_tensormap(&tmap_a);
     ptx::prefetch_tensormap(&tmap_b);
@@ -179,6 +179,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   ptx::cluster_sync_all();   // the peer's barriers are initialised before anything is signalled there
   ptx::tcgen05_fence_after_sync();
   const uint32_t tmem_base = *tmem_slot_gen;
+  // Every launch may start while the one before it is still running.  One that needs its results waits for its end here, with
+  // everything set up; one that does not waits at its own end (see below).  Either way a launch lets the next one start
+  // only once the launch before itself has ended: whatever runs beside a launch is its direct neighbour.
+  if (p.wait_first) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  }
+  if (KIND == LSE && blockIdx.x == 0 && threadIdx.x == 0) *p.ticket = 0u;
   auto give_up = [&]() {
     *abort_flag = 1;
     atomicExch(p.status, kDevTimeout);
@@ -252,10 +260,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (!ptx::mbar_wait(empty_bar(s), ph, abort_flag)) { give_up(); ok = false; }
         }
       }
-      // Launches may overlap with the one before them, not with the one before that (see ce_bwd): every CTA waits for the
-      // end of the launch before this one, by now long past as a rule, before it lets the next one start.
-      asm volatile("griddepcontrol.wait;" ::: "memory");
-      asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+      if (!p.wait_first) {   // the launch before this one has long ended as a rule
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+      }
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------------ UMMA issuer (the leader's)
