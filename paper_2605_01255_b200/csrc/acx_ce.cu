@@ -194,6 +194,67 @@ __global__ void __launch_bounds__(256) ce_finish_kernel(const float* acc, int sp
   *reinterpret_cast<uint4*>(dX + t * d + c) = make_uint4(o[0], o[1], o[2], o[3]);
 }
 
+// What rounding D to bf16 took from the targets' elements, for dW: row_add[t] = sum of corr X over the tokens with the same
+// target as t, in fp32 and in the order of the tokens, where t is the first of them (row_key[t] = its target; -1 for the
+// others).  A target's element is most of what its token adds to dW.  With few tokens the rounding of each would be seen in
+// full (with one to sixteen weighted tokens up to 3 times the error of rounding dW alone, more than 1.5 times in one case out
+// of four); from some 256 tokens on they average out (1.3 times), so this is done for up to kPutBackTokens tokens, where it
+// takes 4 us beside the 40 to 150 us of the step.
+constexpr int kPutBackTokens = 512;
+__global__ void __launch_bounds__(kPutBackTokens) ce_put_back_kernel(const float* corr, const int64_t* __restrict__ targets,
+                                                                     const __nv_bfloat16* __restrict__ X, int tokens, int d, int v0, int v1,
+                                                                     int* __restrict__ row_key, float* __restrict__ row_add) {
+  __shared__ int same[kPutBackTokens];
+  __shared__ float weight[kPutBackTokens];
+  __shared__ int counts[kPutBackTokens / 32];
+  const int t = int(blockIdx.x), tt = int(threadIdx.x), lane = tt & 31, warp = tt >> 5;
+  const int64_t y = __ldg(targets + t);
+  const bool here = y >= v0 && y < v1;                     // the target is in this piece of the vocabulary
+  const bool hit = here && tt < tokens && __ldg(targets + tt) == y;
+  wait_for_launch_before();
+  let_next_launch_start();
+  if (!__syncthreads_or(here) || __syncthreads_or(hit && tt < t)) {   // not here, or another token was there before
+    if (tt == 0) row_key[t] = -1;
+    return;
+  }
+  const uint32_t hits = __ballot_sync(0xFFFFFFFFu, hit);
+  if (lane == 0) counts[warp] = __popc(hits);
+  __syncthreads();
+  int at = __popc(hits & ((1u << lane) - 1u)), n = 0;
+  for (int w = 0; w < kPutBackTokens / 32; ++w) {
+    at += w < warp ? counts[w] : 0;
+    n += counts[w];
+  }
+  if (hit) {
+    same[at] = tt;
+    weight[at] = __ldcg(corr + tt);
+  }
+  __syncthreads();
+  for (int c = tt; c < d / 8; c += kPutBackTokens) {
+    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int k0 = 0; k0 < n; k0 += 4) {
+      uint4 x[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        x[k] = k0 + k < n ? __ldg(reinterpret_cast<const uint4*>(X + int64_t(same[k0 + k]) * d) + c) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float w = k0 + k < n ? weight[k0 + k] : 0.f;
+        const uint32_t h[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[2 * i] = fmaf(w, __uint_as_float(h[i] << 16), s[2 * i]);
+          s[2 * i + 1] = fmaf(w, __uint_as_float(h[i] & 0xFFFF0000u), s[2 * i + 1]);
+        }
+      }
+    }
+    float4* o = reinterpret_cast<float4*>(row_add + int64_t(t) * d + 8 * c);
+    o[0] = make_float4(s[0], s[1], s[2], s[3]);
+    o[1] = make_float4(s[4], s[5], s[6], s[7]);
+  }
+  if (tt == 0) row_key[t] = int(y);
+}
+
 int ceil_div(int64_t a, int64_t b) { return int((a + b - 1) / b); }
 size_t aligned(size_t bytes) { return (bytes + 1023) & ~size_t(1023); }
 
@@ -278,16 +339,15 @@ FwdPlan fwd_plan(const CeProblem& q) {
   return f;
 }
 
-// Pieces of the vocabulary: D of one piece takes at most about 128 MB, so that much of it is still in L2 when the two
-// products read it, and the pieces are of equal size.  Up to three pieces are under way at a time (see ce_bwd).
-#ifndef PIECE_MB
-#define PIECE_MB 128
-#endif
-constexpr int64_t kPieceBytes = int64_t(PIECE_MB) << 20;
+// Pieces of the vocabulary, of equal size: D of one takes at most about 128 MB.  Up to three are under way at a time (see
+// ce_bwd).  Backward of 8192 x 3072 x 128256 with 64 / 128 / 256 / 512 MB: 15.3 / 15.1 / 15.0 / 14.9 ms under sustained load;
+// of 4096 x 896 x 151936: 3.06 / 2.97 / 2.98 / 2.95 ms.  Larger pieces are not worth their memory.
+constexpr int64_t kPieceBytes = int64_t(128) << 20;
 constexpr int kBuffers = 3;
 struct BwdPlan {
   int piece_tiles, pieces, buffers, splits, kb_per_split, d_tiles, d_width, acc_rows;
-  size_t D, D_stride, acc, corr, bytes;
+  bool put_back;
+  size_t D, D_stride, acc, corr, row_key, row_add, bytes;
 };
 BwdPlan bwd_plan(const CeProblem& q) {
   BwdPlan b;
@@ -324,7 +384,10 @@ BwdPlan bwd_plan(const CeProblem& q) {
   b.D_stride = aligned(size_t(q.m) * size_t(b.piece_tiles) * ce::kTile * 2);
   b.acc = b.D + size_t(b.buffers) * b.D_stride;
   b.corr = b.acc + aligned(size_t(b.splits) * size_t(b.acc_rows) * size_t(q.d) * 4);
-  b.bytes = b.corr + aligned(size_t(q.m) * 4);
+  b.put_back = q.m <= kPutBackTokens;
+  b.row_key = b.corr + aligned(size_t(q.m) * 4);
+  b.row_add = b.row_key + aligned(size_t(q.m) * 4);
+  b.bytes = b.row_add + (b.put_back ? aligned(size_t(q.m) * size_t(q.d) * 4) : 0);
   return b;
 }
 
@@ -371,6 +434,13 @@ cudaError_t ce_bwd(const CeProblem& q, const void* X, const void* W, const int64
   common(q, &p, targets, weight, status);
   p.lse = lse;
   p.corr = corr;
+  const bool put_back = b.put_back && dW;
+  int* row_key = reinterpret_cast<int*>(w8 + b.row_key);
+  float* row_add = reinterpret_cast<float*>(w8 + b.row_add);
+  if (put_back) {
+    p.row_key = row_key;
+    p.row_add = row_add;
+  }
   p.denom = denom;
   p.scale = scale * q.logit_scale;
   p.acc_rows = b.acc_rows;
@@ -399,13 +469,13 @@ cudaError_t ce_bwd(const CeProblem& q, const void* X, const void* W, const int64
     set_piece(piece);
     const CUtensorMap& out = dst[piece % kBuffers];
     p.units = p.m_tiles * p.n_tiles;
-    p.wait_first = piece == 0;
+    p.wait_first = piece == 0 || put_back;
     return launch<ce::DLOGITS>(xk, wk, xk, wk, out, out, p, st);
   };
   auto grads = [&](int piece) {
     set_piece(piece);
     p.first_piece = piece == 0;
-    p.wait_first = piece + 1 == b.pieces;
+    p.wait_first = piece + 1 == b.pieces || put_back;
     p.piece_kb = p.n_tiles * (ce::kTile / ce::kBK);
     // a last piece shorter than the others may leave the last splits without a k-block: those tiles are left out
     const int splits = std::min(b.splits, ceil_div(p.piece_kb, b.kb_per_split));
@@ -413,10 +483,22 @@ cudaError_t ce_bwd(const CeProblem& q, const void* X, const void* W, const int64
     p.units = p.x_units + (dW ? p.n_tiles * b.d_tiles : 0);
     return launch<ce::GRADS>(dk[piece % kBuffers], wmn, dmn[piece % kBuffers], xmn, accm, dwm, p, st);
   };
-  cudaError_t e = dlogits(0);
-  for (int piece = 0; piece < b.pieces && e == cudaSuccess; ++piece) {
-    if (piece + 1 < b.pieces) e = dlogits(piece + 1);
-    if (e == cudaSuccess) e = grads(piece);
+  cudaError_t e = cudaSuccess;
+  if (put_back) {   // few tokens: one piece as a rule; every launch needs the one before it
+    for (int piece = 0; piece < b.pieces && e == cudaSuccess; ++piece) {
+      e = dlogits(piece);
+      if (e == cudaSuccess)
+        e = launch_kernel(ce_put_back_kernel, unsigned(q.m), kPutBackTokens, 0, 1, st, static_cast<const float*>(corr), targets,
+                          static_cast<const __nv_bfloat16*>(X), p.tokens, p.d, p.v0, std::min(p.vocab, p.v0 + p.n_tiles * ce::kTile), row_key,
+                          row_add);
+      if (e == cudaSuccess) e = grads(piece);
+    }
+  } else {
+    e = dlogits(0);
+    for (int piece = 0; piece < b.pieces && e == cudaSuccess; ++piece) {
+      if (piece + 1 < b.pieces) e = dlogits(piece + 1);
+      if (e == cudaSuccess) e = grads(piece);
+    }
   }
   if (e != cudaSuccess || !dX) return e;
   const int64_t threads = q.m * (q.d / 8);

@@ -66,6 +66,8 @@ struct Params {
   float* target_logit;          // LSE: [tokens], base 2
   uint32_t* ticket;             // LSE: set to zero for the kernel behind it
   float* corr;                  // DLOGITS: [tokens] what rounding took from the target's element of D
+  const int* row_key;           // GRADS: [tokens], may be null: the row of dW that `row_add` belongs to, -1: none
+  const float* row_add;         // GRADS: [tokens][d], added to that row before it is rounded (see ce_put_back_kernel)
   const float* denom;           // GRADS: may be null; gradients are multiplied by scale / denom
   float scale;
   int* status;
@@ -332,6 +334,19 @@ __global__ void __launch_bounds__(kThreads, 1)
         w[i] = *reinterpret_cast<const uint32_t*>(&h);
       }
     };
+    // The token whose row_add belongs to row `first_row` + lane of dW, or -1.  At most one does.
+    auto find_row_add = [&](int first_row) {
+      int mine = -1;
+#pragma unroll 4
+      for (int t0 = 0; t0 < p.tokens; t0 += 32) {
+        const int r = (t0 + lane < p.tokens ? __ldcg(p.row_key + t0 + lane) : -1) - first_row;
+        for (uint32_t hits = __ballot_sync(0xFFFFFFFFu, r >= 0 && r < 32); hits; hits &= hits - 1) {
+          const int src = __ffs(hits) - 1;
+          if (__shfl_sync(0xFFFFFFFFu, r, src) == lane) mine = t0 + src;
+        }
+      }
+      return mine;
+    };
     int it = 0;
     for (int u = pair; u < p.units; u += pairs, ++it) {
       const Unit t = decode<KIND>(p, u);
@@ -349,10 +364,16 @@ __global__ void __launch_bounds__(kThreads, 1)
           w = p.weight ? __ldg(p.weight + row) : 1.f;
         }
       }
+      const int add_token = (KIND == GRADS && !t.x && p.row_key) ? find_row_add(p.v0 + row0) : -1;
       const bool full_ok = ptx::mbar_wait_cluster(tfull_bar(acc), (it >> 1) & 1, abort_flag);
       if (!__all_sync(0xFFFFFFFFu, full_ok)) { give_up(); break; }
       ptx::tcgen05_fence_after_sync();
       const uint32_t taddr = tmem_base + (uint32_t(quarter * 32) << 16) + acc * kAccCols + half * 128;
+      auto release_accumulator = [&]() {
+        ptx::tcgen05_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive_cluster(on_leader(tempty_bar(acc)));
+      };
       uint32_t v[32];
       if (KIND != GRADS) {
         const int valid = min(128, p.vocab - (p.v0 + col0));          // columns of this half that exist
@@ -450,25 +471,50 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
         } else {
-          for (int c0 = 0; c0 < cols; c0 += 32) {
-            __syncwarp();
-            ptx::tmem_ld_x32(taddr + c0, v);
-            ptx::tmem_ld_wait();
+          // 64 columns at a time; the accumulator is free once the last of them have been read
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
-            uint32_t pk[16];
-            pack(v, pk);
-            const uint32_t src = stage_box(pk);
-            if (lane == 0) {
-              if (p.v0 + row0 < p.vocab) ptx::tma_store_2d(&tmap_out2, src, col0 + c0, p.v0 + row0);
-              ptx::tma_store_commit();
+          for (int h = 0; h < 128; h += 64) {
+            uint32_t w2[2][32];
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+              if (h + 32 * c < cols) {
+                __syncwarp();
+                ptx::tmem_ld_x32(taddr + h + 32 * c, w2[c]);
+              }
+            ptx::tmem_ld_wait();
+            if (h == 64) release_accumulator();
+            if (add_token >= 0) {
+              const float4* x = reinterpret_cast<const float4*>(p.row_add + int64_t(add_token) * p.d + col0 + h);
+#pragma unroll
+              for (int j = 0; j < 16; ++j)
+                if (h + 4 * j < cols) {
+                  const float4 q = __ldcg(x + j);
+                  uint32_t* o = &w2[j >> 3][4 * (j & 7)];
+                  o[0] = __float_as_uint(__uint_as_float(o[0]) + q.x);
+                  o[1] = __float_as_uint(__uint_as_float(o[1]) + q.y);
+                  o[2] = __float_as_uint(__uint_as_float(o[2]) + q.z);
+                  o[3] = __float_as_uint(__uint_as_float(o[3]) + q.w);
+                }
             }
+            __syncwarp();
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+              if (h + 32 * c < cols) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) w2[c][i] = __float_as_uint(__uint_as_float(w2[c][i]) * f);
+                uint32_t pk[16];
+                pack(w2[c], pk);
+                const uint32_t src = stage_box(pk);
+                if (lane == 0) {
+                  if (p.v0 + row0 < p.vocab) ptx::tma_store_2d(&tmap_out2, src, col0 + h + 32 * c, p.v0 + row0);
+                  ptx::tma_store_commit();
+                }
+              }
           }
+          continue;
         }
       }
-      ptx::tcgen05_fence_before_sync();
-      __syncwarp();
-      if (lane == 0) ptx::mbar_arrive_cluster(on_leader(tempty_bar(acc)));
+      release_accumulator();
     }
     if (KIND != LSE && lane == 0) ptx::tma_store_wait_read<0>();   // shared memory must outlive the stores' reads
   }
