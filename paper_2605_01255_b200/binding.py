@@ -354,9 +354,12 @@ def _dense(t: Optional[torch.Tensor], shape: Tuple[int, ...], dtype, name: str) 
 
 def _strided(t: torch.Tensor, shape: Tuple[int, int], dtype, name: str) -> Tuple[int, int]:
     """Address and row stride of a CUDA matrix whose rows are dense (a column slice of a wider one is fine)."""
-    if t is None or t.dtype is not dtype or t.shape != shape or not t.is_cuda or t.stride(1) != 1:
-        raise ValueError("%s must be a CUDA matrix of shape %s and dtype %s with unit column stride" % (name, tuple(shape), dtype))
-    return t.data_ptr(), (t.stride(0) if shape[0] > 1 else shape[1])
+    if t is None or t.dtype is not dtype or t.shape != shape or not t.is_cuda:
+        raise ValueError("%s must be a CUDA matrix of shape %s and dtype %s" % (name, tuple(shape), dtype))
+    rows, cols = t.stride()
+    if cols != 1:
+        raise ValueError("%s must have unit column stride (got %s)" % (name, (rows, cols)))
+    return t.data_ptr(), (rows if shape[0] > 1 else shape[1])
 
 
 _current_device = getattr(torch._C, "_cuda_getDevice", None)   # without the lazy initialisation: there are CUDA tensors by now

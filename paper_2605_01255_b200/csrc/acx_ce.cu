@@ -25,9 +25,6 @@ __device__ __forceinline__ float dot8(uint4 a, uint4 b, float s) {
   return s;
 }
 
-__device__ __forceinline__ void wait_for_launch_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void let_next_launch_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-
 // (m, s) <- (m, s) joined with (m1, s1): sums of 2^(x - maximum)
 __device__ __forceinline__ void join_pair(float& m, float& s, float m1, float s1) {
   const float top = fmaxf(m, m1);
@@ -156,7 +153,7 @@ __global__ void __launch_bounds__(256) ce_finish_kernel(const float* acc, int sp
   const int64_t t = i / vecs;
   if (t >= tokens) return;
   const int c = int(i - t * vecs) * 8;
-  const float dn = denom ? __ldg(denom) : 1.f, f = dn > 0.f ? scale / dn : 0.f;
+  const float dn = denom ? __ldcg(denom) : 1.f, f = dn > 0.f ? scale / dn : 0.f;
   float v[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = 0.f;
@@ -260,34 +257,6 @@ size_t aligned(size_t bytes) { return (bytes + 1023) & ~size_t(1023); }
 
 int pair_count() { return std::max(1, sm_count() / 2); }
 
-// With programmatic stream serialization: the kernel may start before the launch before it has finished, and says itself what
-// it waits for.
-template <typename... K, typename... A>
-cudaError_t launch_kernel(void (*kernel)(K...), unsigned grid, unsigned threads, size_t smem, int cluster, cudaStream_t st, const A&... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[2];
-  unsigned n = 0;
-  if (cluster > 1) {
-    attr[n].id = cudaLaunchAttributeClusterDimension;
-    attr[n].val.clusterDim.x = unsigned(cluster);
-    attr[n].val.clusterDim.y = 1;
-    attr[n].val.clusterDim.z = 1;
-    ++n;
-  }
-  attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[n].val.programmaticStreamSerializationAllowed = 1;
-  ++n;
-  cfg.attrs = attr;
-  cfg.numAttrs = n;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
-  kernel_launch_counter().fetch_add(1, std::memory_order_relaxed);
-  return e;
-}
-
 template <int KIND>
 cudaError_t launch(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& ta2, const CUtensorMap& tb2, const CUtensorMap& to,
                    const CUtensorMap& to2, const Params& p, cudaStream_t st) {
@@ -298,8 +267,23 @@ cudaError_t launch(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorM
     if (e != cudaSuccess) return e;
     once.done();
   }
-  return launch_kernel(kernel, unsigned(2 * std::min(p.units, pair_count())), ce::kThreads, ce::kSmemBytes, 2, st, ta, tb, ta2, tb2,
-                       to, to2, p);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(2 * std::min(p.units, pair_count())));
+  cfg.blockDim = dim3(ce::kThreads);
+  cfg.dynamicSmemBytes = ce::kSmemBytes;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // see wait_first
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, ta, tb, ta2, tb2, to, to2, p);
+  kernel_launch_counter().fetch_add(1, std::memory_order_relaxed);
+  return e;
 }
 
 // Token tiles that pass over the vocabulary together: as many as have their rows of X (d wide, bf16) in 48 MB, so that X
@@ -411,7 +395,7 @@ cudaError_t ce_fwd(const CeProblem& q, const void* X, const void* W, const int64
   if (!make_tmap_bf16(&ta, X, q.m, q.d, ce::kBK, ce::kBM) || !make_tmap_bf16(&tb, W, q.vocab, q.d, ce::kBK, ce::kBM)) return cudaErrorInvalidValue;
   const cudaError_t e = launch<ce::LSE>(ta, tb, ta, tb, ta, ta, p, st);
   if (e != cudaSuccess) return e;
-  return launch_kernel(ce_join_kernel, unsigned(f.blocks), kJoinThreads, 0, 1, st, static_cast<const float2*>(p.part),
+  return launch_lined_up(ce_join_kernel, dim3(unsigned(f.blocks)), dim3(kJoinThreads), 0, st, static_cast<const float2*>(p.part),
                        static_cast<const float*>(p.target_logit), static_cast<const __nv_bfloat16*>(X), static_cast<const __nv_bfloat16*>(W),
                        targets, weight, p.tokens, p.d, p.vocab, f.parts, p.c, loss, lse, reinterpret_cast<float2*>(w8 + f.sums), p.ticket, total);
 }
@@ -488,7 +472,7 @@ cudaError_t ce_bwd(const CeProblem& q, const void* X, const void* W, const int64
     for (int piece = 0; piece < b.pieces && e == cudaSuccess; ++piece) {
       e = dlogits(piece);
       if (e == cudaSuccess)
-        e = launch_kernel(ce_put_back_kernel, unsigned(q.m), kPutBackTokens, 0, 1, st, static_cast<const float*>(corr), targets,
+        e = launch_lined_up(ce_put_back_kernel, dim3(unsigned(q.m)), dim3(kPutBackTokens), 0, st, static_cast<const float*>(corr), targets,
                           static_cast<const __nv_bfloat16*>(X), p.tokens, p.d, p.v0, std::min(p.vocab, p.v0 + p.n_tiles * ce::kTile), row_key,
                           row_add);
       if (e == cudaSuccess) e = grads(piece);
@@ -502,7 +486,7 @@ cudaError_t ce_bwd(const CeProblem& q, const void* X, const void* W, const int64
   }
   if (e != cudaSuccess || !dX) return e;
   const int64_t threads = q.m * (q.d / 8);
-  return launch_kernel(ce_finish_kernel, unsigned((threads + 255) / 256), 256, 0, 1, st, static_cast<const float*>(acc), b.splits,
+  return launch_lined_up(ce_finish_kernel, dim3(unsigned((threads + 255) / 256)), dim3(256), 0, st, static_cast<const float*>(acc), b.splits,
                        int64_t(b.acc_rows) * q.d, static_cast<const float*>(corr), targets, static_cast<const __nv_bfloat16*>(W), denom,
                        p.scale, static_cast<__nv_bfloat16*>(dX), p.tokens, p.d, p.vocab);
 }

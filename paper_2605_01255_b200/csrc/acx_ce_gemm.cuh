@@ -310,7 +310,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t n_stores = 0;
     float f = 0.f;
     if (KIND == GRADS) {
-      const float dn = p.denom ? __ldg(p.denom) : 1.f;
+      const float dn = p.denom ? __ldcg(p.denom) : 1.f;
       f = dn > 0.f ? p.scale / dn : 0.f;
     }
     // one 32-row box of 64 bytes per row, staged with the 64-byte swizzle (16-byte unit j of row l at j ^ ((l >> 1) & 3))
@@ -357,11 +357,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       int64_t y = -1;
       float lse2 = 0.f, w = 0.f;
       if (KIND != GRADS && row < p.tokens) {
-        y = __ldg(p.targets + row);
+        y = __ldcg(p.targets + row);
         if (y < 0 || y >= p.vocab) y = -1;              // not trained on
         if (KIND == DLOGITS && y >= 0) {
-          lse2 = __ldg(p.lse + row) * kLog2e;
-          w = p.weight ? __ldg(p.weight + row) : 1.f;
+          lse2 = __ldcg(p.lse + row) * kLog2e;
+          w = p.weight ? __ldcg(p.weight + row) : 1.f;
         }
       }
       const int add_token = (KIND == GRADS && !t.x && p.row_key) ? find_row_add(p.v0 + row0) : -1;

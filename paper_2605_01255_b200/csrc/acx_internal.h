@@ -44,6 +44,29 @@ inline cudaError_t launched() {
   return cudaGetLastError();
 }
 
+// Launches with programmatic stream serialization: the kernel may start before the launch before it has finished, and waits
+// for that itself (wait_for_launch_before, first thing or as soon as it needs to).
+template <typename... K, typename... A>
+cudaError_t launch_lined_up(void (*kernel)(K...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, const A&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
+  kernel_launch_counter().fetch_add(1, std::memory_order_relaxed);
+  return e;
+}
+#ifdef __CUDACC__
+__device__ __forceinline__ void wait_for_launch_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_launch_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+#endif
+
 // One-time set-up that holds per device (a kernel's function attributes are set for the device that is current):
 // `static DeviceOnce once; if (once.needed()) { ...; once.done(); }`.  Safe to race: the set-up is idempotent.
 class DeviceOnce {

@@ -127,6 +127,8 @@ template <typename T, int NV, int MAXT, int MINB, int DEPTH, bool JOIN, bool KEE
 __global__ void __launch_bounds__(MAXT, MINB) norm_join_fwd_kernel(const FwdArgs a) {
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ float red[2][2][32];
+  wait_for_launch_before();
+  let_next_launch_start();
   using S = Slots<T, MAXT>;
   constexpr int kVecSlot = S::kBytes * (JOIN ? 2 : 1);
   const int ng = (a.cols + kGroup - 1) / kGroup, lane16 = threadIdx.x & 15;
@@ -266,7 +268,8 @@ template <typename T, int NV, int MAXT, int MINB, int DEPTH, bool JOIN, bool FUL
 __global__ void __launch_bounds__(MAXT, MINB) norm_join_bwd_kernel(const BwdArgs a) {
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ float4 red[2][32];
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the kernel that adds the columns' sums may line up
+  wait_for_launch_before();
+  let_next_launch_start();
   using S = Slots<T, MAXT>;
   constexpr int kCodes = MAXT * 8, kVecSlot = 2 * S::kBytes + (JOIN ? 2 : 1) * kCodes;   // dy, dh_next, codes of h and b
   const int ng = (a.cols + kGroup - 1) / kGroup;
@@ -311,14 +314,14 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_join_bwd_kernel(const BwdArgs
   next.r_b = 1.f;
   auto scales = [&](int64_t row) {
     if (row >= a.rows) return;
-    next.r_t = __ldg(a.rstd_pre + row);
-    if (JOIN && a.w_post) next.r_b = __ldg(a.rstd_post + row);
+    next.r_t = __ldcg(a.rstd_pre + row);
+    if (JOIN && a.w_post) next.r_b = __ldcg(a.rstd_post + row);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       if (!live(i)) continue;
       const int64_t g = row * ng + col_of(i) / kGroup;
-      next.hs[i] = __ldg(a.Hs + g);
-      if (JOIN) next.bs[JOIN ? i : 0] = __ldg(a.Bs + g);
+      next.hs[i] = __ldcg(a.Hs + g);
+      if (JOIN) next.bs[JOIN ? i : 0] = __ldcg(a.Bs + g);
     }
   };
   scales(blockIdx.x);
@@ -349,8 +352,8 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_join_bwd_kernel(const BwdArgs
         const int64_t ac = at + col_of(i);
         load8(static_cast<const T*>(a.dy) + ac, dy);
         if (a.dh_next) load8(static_cast<const T*>(a.dh_next) + ac, av[i]);
-        hq = __ldg(reinterpret_cast<const uint2*>(a.Hq + ac));
-        if (JOIN) bq = __ldg(reinterpret_cast<const uint2*>(a.Bq + ac));
+        hq = __ldcg(reinterpret_cast<const uint2*>(a.Hq + ac));
+        if (JOIN) bq = __ldcg(reinterpret_cast<const uint2*>(a.Bq + ac));
       }
       decode8(hq, now.hs[i], that[i]);
       if (JOIN) decode8(bq, now.bs[j] * rb, bhat[j]);
@@ -421,14 +424,15 @@ __global__ void __launch_bounds__(1024) norm_join_columns_kernel(const float* pa
   const int x = threadIdx.x & 31, y = threadIdx.x >> 5, plane = blockIdx.y;
   const int c = int(blockIdx.x) * 32 + x;
   float s = 0.f;
-  asm volatile("griddepcontrol.wait;" ::: "memory");   // launched behind the kernel that writes `part` before that has finished
+  wait_for_launch_before();
+  let_next_launch_start();
   if (c < cols)
-    for (int k = y; k < blocks; k += 12 * 32) {   // twelve loads under way, added in order
-      float v[12];
+    for (int k = y; k < blocks; k += 16 * 32) {   // sixteen loads under way, added in order
+      float v[16];
 #pragma unroll
-      for (int u = 0; u < 12; ++u) v[u] = k + 32 * u < blocks ? __ldcg(part + (int64_t(k + 32 * u) * planes + plane) * cols + c) : 0.f;
+      for (int u = 0; u < 16; ++u) v[u] = k + 32 * u < blocks ? __ldcg(part + (int64_t(k + 32 * u) * planes + plane) * cols + c) : 0.f;
 #pragma unroll
-      for (int u = 0; u < 12; ++u) s += v[u];
+      for (int u = 0; u < 16; ++u) s += v[u];
     }
   red[y][x] = s;
   __syncthreads();
@@ -467,8 +471,7 @@ cudaError_t launch_rows(K kernel, DeviceOnce& once, const A& a, const Shape& s, 
     if (e != cudaSuccess) return e;
     once.done();
   }
-  kernel<<<s.blocks, s.threads, smem, st>>>(a);
-  return launched();
+  return launch_lined_up(kernel, dim3(unsigned(s.blocks)), dim3(unsigned(s.threads)), size_t(smem), st, a);
 }
 template <typename T>
 constexpr int depth_of() { return sizeof(T) == 2 ? 4 : 2; }   // rows ahead: the same bytes for both types
@@ -535,24 +538,12 @@ cudaError_t norm_join_bwd(const Rows& d, const void* dy, const void* dh_next, co
   const int planes = Bq ? 2 : 1;
   const dim3 grid(unsigned((d.cols + 31) / 32), unsigned((dw_post || dgate) ? 2 : 1));
   const int blocks = bwd_shape(d.rows, d.cols).blocks;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(1024);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
   const float* part = a.part;
   if (d.bf16)
-    e = cudaLaunchKernelEx(&cfg, norm_join_columns_kernel<__nv_bfloat16>, part, blocks, a.cols, planes, alpha,
+    return launch_lined_up(norm_join_columns_kernel<__nv_bfloat16>, grid, dim3(1024), 0, st, part, blocks, a.cols, planes, alpha,
                            static_cast<const __nv_bfloat16*>(w_post), static_cast<const __nv_bfloat16*>(gate), dw_pre, dw_post, dgate);
-  else
-    e = cudaLaunchKernelEx(&cfg, norm_join_columns_kernel<float>, part, blocks, a.cols, planes, alpha, static_cast<const float*>(w_post),
-                           static_cast<const float*>(gate), dw_pre, dw_post, dgate);
-  kernel_launch_counter().fetch_add(1, std::memory_order_relaxed);
-  return e;
+  return launch_lined_up(norm_join_columns_kernel<float>, grid, dim3(1024), 0, st, part, blocks, a.cols, planes, alpha,
+                         static_cast<const float*>(w_post), static_cast<const float*>(gate), dw_pre, dw_post, dgate);
 }
 
 }  // namespace acx

@@ -41,6 +41,9 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
 }
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 
+// Loads go through L2 (ld.global.cg), not through the read-only path: a kernel that was launched while the one before it was
+// still running may not assume that memory has not changed since its own start.
+//
 // Eight elements of a row as they are in memory: loads are issued long before the values are needed, and a bf16 vector
 // waits for that in four registers instead of eight.
 template <typename T>
@@ -49,7 +52,7 @@ template <>
 struct Raw<__nv_bfloat16> {
   uint4 u;
   __device__ __forceinline__ void zero() { u = make_uint4(0u, 0u, 0u, 0u); }
-  __device__ __forceinline__ void load(const __nv_bfloat16* p) { u = __ldg(reinterpret_cast<const uint4*>(p)); }
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { u = __ldcg(reinterpret_cast<const uint4*>(p)); }
   __device__ __forceinline__ void get(float2 (&v)[4]) const {
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
@@ -71,8 +74,8 @@ struct Raw<float> {
   float4 a, b;
   __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
   __device__ __forceinline__ void load(const float* p) {
-    a = __ldg(reinterpret_cast<const float4*>(p));
-    b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+    a = __ldcg(reinterpret_cast<const float4*>(p));
+    b = __ldcg(reinterpret_cast<const float4*>(p) + 1);
   }
   __device__ __forceinline__ void get(float2 (&v)[4]) const {
     v[0] = make_float2(a.x, a.y); v[1] = make_float2(a.z, a.w);

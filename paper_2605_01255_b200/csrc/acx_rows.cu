@@ -49,6 +49,8 @@ __device__ __forceinline__ bool first_lane() { return threadIdx.x % kLanes == 0;
 template <typename T>
 __global__ void __launch_bounds__(kThreads) q8_store_kernel(const T* __restrict__ X, int64_t ldx, int8_t* __restrict__ codes,
                                                             float* __restrict__ scales, int64_t rows, int cols, Div d) {
+  wait_for_launch_before();
+  let_next_launch_start();
   const Place p = place_of(rows, cols, d);
   Raw<T> x[2];
 #pragma unroll
@@ -69,13 +71,15 @@ __global__ void __launch_bounds__(kThreads) q8_store_kernel(const T* __restrict_
 template <typename T>
 __global__ void __launch_bounds__(kThreads) q8_load_kernel(const int8_t* __restrict__ codes, const float* __restrict__ scales,
                                                            T* __restrict__ X, int64_t ldx, int64_t rows, int cols, Div d) {
+  wait_for_launch_before();
+  let_next_launch_start();
   const Place p = place_of(rows, cols, d);
   uint2 c[2];
   if (!p.live[0]) return;
   const int64_t at = p.row * int64_t(cols) + p.col;
-  c[0] = __ldg(reinterpret_cast<const uint2*>(codes + at));
-  if (p.live[1]) c[1] = __ldg(reinterpret_cast<const uint2*>(codes + at + kHalf));
-  const float s = __ldg(scales + p.group);
+  c[0] = __ldcg(reinterpret_cast<const uint2*>(codes + at));
+  if (p.live[1]) c[1] = __ldcg(reinterpret_cast<const uint2*>(codes + at + kHalf));
+  const float s = __ldcg(scales + p.group);
 #pragma unroll
   for (int v = 0; v < 2; ++v) {
     if (!p.live[v]) break;
@@ -105,6 +109,8 @@ __global__ void __launch_bounds__(kThreads) swiglu_fwd_kernel(const T* __restric
                                                               T* __restrict__ H, int8_t* __restrict__ Gq, float* __restrict__ Gs,
                                                               int8_t* __restrict__ Uq, float* __restrict__ Us, int64_t rows, int cols,
                                                               Div d) {
+  wait_for_launch_before();
+  let_next_launch_start();
   const Place p = place_of(rows, cols, d);
   Raw<T> g[2], u[2];
 #pragma unroll
@@ -149,6 +155,8 @@ __global__ void __launch_bounds__(kThreads) swiglu_bwd_kernel(const T* __restric
                                                               const float* __restrict__ Gs, const int8_t* __restrict__ Uq,
                                                               const float* __restrict__ Us, T* __restrict__ dG, int64_t lddg,
                                                               T* __restrict__ dU, int64_t lddu, int64_t rows, int cols, Div d) {
+  wait_for_launch_before();
+  let_next_launch_start();
   const Place p = place_of(rows, cols, d);
   if (!p.live[0]) return;
   uint2 cg[2], cu[2];
@@ -157,11 +165,11 @@ __global__ void __launch_bounds__(kThreads) swiglu_bwd_kernel(const T* __restric
 #pragma unroll
   for (int v = 0; v < 2; ++v) {
     if (!p.live[v]) break;
-    cg[v] = __ldg(reinterpret_cast<const uint2*>(Gq + at + v * kHalf));
-    cu[v] = __ldg(reinterpret_cast<const uint2*>(Uq + at + v * kHalf));
+    cg[v] = __ldcg(reinterpret_cast<const uint2*>(Gq + at + v * kHalf));
+    cu[v] = __ldcg(reinterpret_cast<const uint2*>(Uq + at + v * kHalf));
     x[v].load(dH + at + v * kHalf);
   }
-  const float sg = __ldg(Gs + p.group), su = __ldg(Us + p.group);
+  const float sg = __ldcg(Gs + p.group), su = __ldcg(Us + p.group);
 #pragma unroll
   for (int v = 0; v < 2; ++v) {
     if (!p.live[v]) break;
@@ -191,61 +199,53 @@ Launch launch_of(const Rows& d) {
 }
 
 template <typename T>
-void launch_store(const Rows& d, const void* X, int64_t ldx, int8_t* codes, float* scales, cudaStream_t st) {
+cudaError_t launch_store(const Rows& d, const void* X, int64_t ldx, int8_t* codes, float* scales, cudaStream_t st) {
   const Launch l = launch_of(d);
-  q8_store_kernel<T><<<l.grid, kThreads, 0, st>>>(static_cast<const T*>(X), ldx, codes, scales, d.rows, int(d.cols), l.div);
+  return launch_lined_up(q8_store_kernel<T>, dim3(l.grid), dim3(kThreads), 0, st, static_cast<const T*>(X), ldx, codes, scales, d.rows, int(d.cols), l.div);
 }
 template <typename T>
-void launch_load(const Rows& d, const int8_t* codes, const float* scales, void* X, int64_t ldx, cudaStream_t st) {
+cudaError_t launch_load(const Rows& d, const int8_t* codes, const float* scales, void* X, int64_t ldx, cudaStream_t st) {
   const Launch l = launch_of(d);
-  q8_load_kernel<T><<<l.grid, kThreads, 0, st>>>(codes, scales, static_cast<T*>(X), ldx, d.rows, int(d.cols), l.div);
+  return launch_lined_up(q8_load_kernel<T>, dim3(l.grid), dim3(kThreads), 0, st, codes, scales, static_cast<T*>(X), ldx, d.rows, int(d.cols), l.div);
 }
 template <typename T, bool KEEP>
-void launch_swiglu_fwd(const Rows& d, const void* G, int64_t ldg, const void* U, int64_t ldu, void* H, int8_t* Gq, float* Gs, int8_t* Uq,
+cudaError_t launch_swiglu_fwd(const Rows& d, const void* G, int64_t ldg, const void* U, int64_t ldu, void* H, int8_t* Gq, float* Gs, int8_t* Uq,
                        float* Us, cudaStream_t st) {
   const Launch l = launch_of(d);
-  swiglu_fwd_kernel<T, KEEP><<<l.grid, kThreads, 0, st>>>(static_cast<const T*>(G), ldg, static_cast<const T*>(U), ldu, static_cast<T*>(H),
+  return launch_lined_up(swiglu_fwd_kernel<T, KEEP>, dim3(l.grid), dim3(kThreads), 0, st, static_cast<const T*>(G), ldg, static_cast<const T*>(U), ldu, static_cast<T*>(H),
                                                          Gq, Gs, Uq, Us, d.rows, int(d.cols), l.div);
 }
 template <typename T>
-void launch_swiglu_bwd(const Rows& d, const void* dH, const int8_t* Gq, const float* Gs, const int8_t* Uq, const float* Us, void* dG,
+cudaError_t launch_swiglu_bwd(const Rows& d, const void* dH, const int8_t* Gq, const float* Gs, const int8_t* Uq, const float* Us, void* dG,
                        int64_t lddg, void* dU, int64_t lddu, cudaStream_t st) {
   const Launch l = launch_of(d);
-  swiglu_bwd_kernel<T><<<l.grid, kThreads, 0, st>>>(static_cast<const T*>(dH), Gq, Gs, Uq, Us, static_cast<T*>(dG), lddg,
+  return launch_lined_up(swiglu_bwd_kernel<T>, dim3(l.grid), dim3(kThreads), 0, st, static_cast<const T*>(dH), Gq, Gs, Uq, Us, static_cast<T*>(dG), lddg,
                                                    static_cast<T*>(dU), lddu, d.rows, int(d.cols), l.div);
 }
 
 }  // namespace
 
 cudaError_t q8_store(const Rows& d, const void* X, int64_t ldx, int8_t* codes, float* scales, cudaStream_t st) {
-  if (d.bf16) launch_store<__nv_bfloat16>(d, X, ldx, codes, scales, st);
-  else launch_store<float>(d, X, ldx, codes, scales, st);
-  return launched();
+  return d.bf16 ? launch_store<__nv_bfloat16>(d, X, ldx, codes, scales, st) : launch_store<float>(d, X, ldx, codes, scales, st);
 }
 
 cudaError_t q8_load(const Rows& d, const int8_t* codes, const float* scales, void* X, int64_t ldx, cudaStream_t st) {
-  if (d.bf16) launch_load<__nv_bfloat16>(d, codes, scales, X, ldx, st);
-  else launch_load<float>(d, codes, scales, X, ldx, st);
-  return launched();
+  return d.bf16 ? launch_load<__nv_bfloat16>(d, codes, scales, X, ldx, st) : launch_load<float>(d, codes, scales, X, ldx, st);
 }
 
 cudaError_t swiglu_fwd(const Rows& d, const void* G, int64_t ldg, const void* U, int64_t ldu, void* H, int8_t* Gq, float* Gs, int8_t* Uq,
                        float* Us, cudaStream_t st) {
-  if (d.bf16) {
-    if (Gq) launch_swiglu_fwd<__nv_bfloat16, true>(d, G, ldg, U, ldu, H, Gq, Gs, Uq, Us, st);
-    else launch_swiglu_fwd<__nv_bfloat16, false>(d, G, ldg, U, ldu, H, Gq, Gs, Uq, Us, st);
-  } else {
-    if (Gq) launch_swiglu_fwd<float, true>(d, G, ldg, U, ldu, H, Gq, Gs, Uq, Us, st);
-    else launch_swiglu_fwd<float, false>(d, G, ldg, U, ldu, H, Gq, Gs, Uq, Us, st);
-  }
-  return launched();
+  if (d.bf16)
+    return Gq ? launch_swiglu_fwd<__nv_bfloat16, true>(d, G, ldg, U, ldu, H, Gq, Gs, Uq, Us, st)
+              : launch_swiglu_fwd<__nv_bfloat16, false>(d, G, ldg, U, ldu, H, Gq, Gs, Uq, Us, st);
+  return Gq ? launch_swiglu_fwd<float, true>(d, G, ldg, U, ldu, H, Gq, Gs, Uq, Us, st)
+            : launch_swiglu_fwd<float, false>(d, G, ldg, U, ldu, H, Gq, Gs, Uq, Us, st);
 }
 
 cudaError_t swiglu_bwd(const Rows& d, const void* dH, const int8_t* Gq, const float* Gs, const int8_t* Uq, const float* Us, void* dG,
                        int64_t lddg, void* dU, int64_t lddu, cudaStream_t st) {
-  if (d.bf16) launch_swiglu_bwd<__nv_bfloat16>(d, dH, Gq, Gs, Uq, Us, dG, lddg, dU, lddu, st);
-  else launch_swiglu_bwd<float>(d, dH, Gq, Gs, Uq, Us, dG, lddg, dU, lddu, st);
-  return launched();
+  return d.bf16 ? launch_swiglu_bwd<__nv_bfloat16>(d, dH, Gq, Gs, Uq, Us, dG, lddg, dU, lddu, st)
+                : launch_swiglu_bwd<float>(d, dH, Gq, Gs, Uq, Us, dG, lddg, dU, lddu, st);
 }
 
 }  // namespace acx
