@@ -55,7 +55,17 @@ __global__ void __launch_bounds__(kJoinThreads, 3) ce_join_kernel(const float2* 
     if (y >= 0 && y < vocab) {
       const uint4* x = reinterpret_cast<const uint4*>(X + int64_t(tt) * d);
       const uint4* w = reinterpret_cast<const uint4*>(W + y * int64_t(d));
-      for (int i = (warp & 1) * 32 + lane; i < d / 8; i += 64) p = dot8(__ldg(x + i), __ldg(w + i), p);
+      for (int i0 = (warp & 1) * 32 + lane; i0 < d / 8; i0 += 4 * 64) {   // four vectors of each under way
+        uint4 a[4], b[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const bool in = i0 + 64 * k < d / 8;
+          a[k] = in ? __ldg(x + i0 + 64 * k) : make_uint4(0u, 0u, 0u, 0u);
+          b[k] = in ? __ldg(w + i0 + 64 * k) : make_uint4(0u, 0u, 0u, 0u);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) p = dot8(a[k], b[k], p);
+      }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) p += __shfl_xor_sync(0xFFFFFFFFu, p, o);
@@ -320,7 +330,8 @@ struct FwdPlan {
 };
 FwdPlan fwd_plan(const CeProblem& q) {
   FwdPlan f;
-  f.parts = ceil_div(q.vocab, 128);
+  const int tiles = ceil_div(q.vocab, ce::kTile);
+  f.parts = q.m <= ce::kTile ? 2 * std::min(tiles, pair_count()) : ceil_div(q.vocab, 128);   // see Params::part
   f.blocks = ceil_div(q.m, kTokensPerBlock);
   f.part = 0;
   f.target = f.part + aligned(size_t(f.parts) * size_t(q.m) * sizeof(float2));

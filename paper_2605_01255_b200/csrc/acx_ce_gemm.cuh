@@ -62,7 +62,8 @@ struct Params {
   const int64_t* targets;
   const float* lse;             // natural logarithm
   const float* weight;          // may be null: one
-  float2* part;                 // LSE: [ceil(vocab / 128)][tokens] (maximum, sum), base 2
+  float2* part;                 // LSE: [.][tokens] (maximum, sum) in base 2, of 128 columns each; of one token tile: of all the
+                                // columns that a pair's column half met ([2 * pairs][tokens])
   float* target_logit;          // LSE: [tokens], base 2
   uint32_t* ticket;             // LSE: set to zero for the kernel behind it
   float* corr;                  // DLOGITS: [tokens] what rounding took from the target's element of D
@@ -347,6 +348,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       return mine;
     };
+    float run_m = -INFINITY, run_s = 0.f;    // LSE
     int it = 0;
     for (int u = pair; u < p.units; u += pairs, ++it) {
       const Unit t = decode<KIND>(p, u);
@@ -379,7 +381,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int valid = min(128, p.vocab - (p.v0 + col0));          // columns of this half that exist
         const int tc = y >= 0 ? int(max(int64_t(-1), min(int64_t(1) << 20, y - (p.v0 + col0)))) : -1;   // the target's column here
         if (KIND == LSE) {
-          float m = -INFINITY, s = 0.f;
+          const bool one_tile = p.m_tiles == 1;       // every unit of this pair has the same rows
+          float m = one_tile ? run_m : -INFINITY, s = one_tile ? run_s : 0.f;
           for (int c0 = 0; c0 < valid; c0 += 32) {
             __syncwarp();
             ptx::tmem_ld_x32(taddr + c0, v);
@@ -410,7 +413,13 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             s += s1;
           }
-          if (valid > 0 && row < p.tokens) p.part[int64_t((p.v0 + col0) >> 7) * p.tokens + row] = make_float2(m, s);
+          if (one_tile) {
+            run_m = m;
+            run_s = s;
+            if (u + pairs >= p.units && row < p.tokens) p.part[int64_t(2 * pair + half) * p.tokens + row] = make_float2(m, s);
+          } else if (valid > 0 && row < p.tokens) {
+            p.part[int64_t(col0 >> 7) * p.tokens + row] = make_float2(m, s);
+          }
         } else {
           for (int c0 = 0; c0 < 128; c0 += 32) {
             __syncwarp();
