@@ -267,10 +267,10 @@ size_t aligned(size_t bytes) { return (bytes + 1023) & ~size_t(1023); }
 
 int pair_count() { return std::max(1, sm_count() / 2); }
 
-template <int KIND>
+template <int KIND, bool FEW>
 cudaError_t launch(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& ta2, const CUtensorMap& tb2, const CUtensorMap& to,
                    const CUtensorMap& to2, const Params& p, cudaStream_t st) {
-  auto kernel = ce::ce_kernel<KIND>;
+  auto kernel = ce::ce_kernel<KIND, FEW>;
   static DeviceOnce once;
   if (once.needed()) {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ce::kSmemBytes);
@@ -295,6 +295,16 @@ cudaError_t launch(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorM
   kernel_launch_counter().fetch_add(1, std::memory_order_relaxed);
   return e;
 }
+
+template <int KIND>
+cudaError_t launch(bool few, const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& ta2, const CUtensorMap& tb2,
+                   const CUtensorMap& to, const CUtensorMap& to2, const Params& p, cudaStream_t st) {
+  return few ? launch<KIND, true>(ta, tb, ta2, tb2, to, to2, p, st) : launch<KIND, false>(ta, tb, ta2, tb2, to, to2, p, st);
+}
+
+// Up to 64 tokens: the kernels with the operands exchanged (see FEW).
+bool is_few(const CeProblem& q) { return q.m <= ce::kFewTokens; }
+int few_columns(const CeProblem& q) { return int(q.m + 31) & ~31; }
 
 // Token tiles that pass over the vocabulary together: as many as have their rows of X (d wide, bf16) in 48 MB, so that X
 // stays in L2 beside the tiles of W that stream by.
@@ -322,6 +332,7 @@ void common(const CeProblem& q, Params* p, const int64_t* targets, const float* 
   p->weight = weight;
   p->status = status;
   p->wait_first = 1;
+  p->few_n = few_columns(q);
 }
 
 struct FwdPlan {
@@ -330,8 +341,7 @@ struct FwdPlan {
 };
 FwdPlan fwd_plan(const CeProblem& q) {
   FwdPlan f;
-  const int tiles = ceil_div(q.vocab, ce::kTile);
-  f.parts = q.m <= ce::kTile ? 2 * std::min(tiles, pair_count()) : ceil_div(q.vocab, 128);   // see Params::part
+  f.parts = is_few(q) ? 8 * std::min(ceil_div(q.vocab, ce::kTile), pair_count()) : ceil_div(q.vocab, 128);   // see Params::part
   f.blocks = ceil_div(q.m, kTokensPerBlock);
   f.part = 0;
   f.target = f.part + aligned(size_t(f.parts) * size_t(q.m) * sizeof(float2));
@@ -361,12 +371,12 @@ BwdPlan bwd_plan(const CeProblem& q) {
   b.buffers = std::min(b.pieces, kBuffers);
   b.d_tiles = ceil_div(q.d, ce::kTile);
   b.d_width = (ceil_div(q.d, b.d_tiles) + 31) & ~31;
-  b.acc_rows = m_tiles * ce::kTile;
+  b.acc_rows = is_few(q) ? int(q.m) : m_tiles * ce::kTile;
   // dX is split along the piece where that lets the longest-loaded pair of CTAs finish sooner: pair c takes the units c,
   // c + pairs, ..., the tiles of dX first.  Every split costs its fp32 sums' way through memory (a unit's epilogue is worth
   // about 4 k-blocks, the last kernel's reading about one per split).
   const int piece_kb = b.piece_tiles * (ce::kTile / ce::kBK), token_kb = ceil_div(q.m, ce::kBK);
-  const int64_t x1 = int64_t(m_tiles) * b.d_tiles, w = int64_t(b.piece_tiles) * b.d_tiles;
+  const int64_t x1 = is_few(q) ? ceil_div(q.d, ce::kTile) : int64_t(m_tiles) * b.d_tiles, w = int64_t(b.piece_tiles) * b.d_tiles;
   double best = 1e300;
   b.kb_per_split = piece_kb;
   for (int s : {1, 2, 3, 4, 6, 8, 10, 12, 16, 20, 24, 32}) {
@@ -405,13 +415,15 @@ cudaError_t ce_fwd(const CeProblem& q, const void* X, const void* W, const int64
   Params p{};
   common(q, &p, targets, weight, status);
   p.n_tiles = ceil_div(q.vocab, ce::kTile);
-  p.units = p.m_tiles * p.n_tiles;
+  p.units = is_few(q) ? p.n_tiles : p.m_tiles * p.n_tiles;
   p.part = reinterpret_cast<float2*>(w8 + f.part);
   p.target_logit = reinterpret_cast<float*>(w8 + f.target);
   p.ticket = reinterpret_cast<uint32_t*>(w8 + f.ticket);
   CUtensorMap ta, tb;
-  if (!make_tmap_bf16(&ta, X, q.m, q.d, ce::kBK, ce::kBM) || !make_tmap_bf16(&tb, W, q.vocab, q.d, ce::kBK, ce::kBM)) return cudaErrorInvalidValue;
-  const cudaError_t e = launch<ce::LSE>(ta, tb, ta, tb, ta, ta, p, st);
+  const bool few = is_few(q);
+  const int token_box = few ? p.few_n / 2 : ce::kBM;
+  if (!make_tmap_bf16(&ta, X, q.m, q.d, ce::kBK, token_box) || !make_tmap_bf16(&tb, W, q.vocab, q.d, ce::kBK, ce::kBM)) return cudaErrorInvalidValue;
+  const cudaError_t e = launch<ce::LSE>(few, ta, tb, ta, tb, ta, ta, p, st);
   if (e != cudaSuccess) return e;
   return launch_lined_up(ce_join_kernel, dim3(unsigned(f.blocks)), dim3(kJoinThreads), 0, st, static_cast<const float2*>(p.part),
                        static_cast<const float*>(p.target_logit), static_cast<const __nv_bfloat16*>(X), static_cast<const __nv_bfloat16*>(W),
@@ -436,6 +448,8 @@ cudaError_t ce_bwd(const CeProblem& q, const void* X, const void* W, const int64
   common(q, &p, targets, weight, status);
   p.lse = lse;
   p.corr = corr;
+  p.acc = acc;
+  p.ld_d = piece_cols;
   const bool put_back = b.put_back && dW;
   int* row_key = reinterpret_cast<int*>(w8 + b.row_key);
   float* row_add = reinterpret_cast<float*>(w8 + b.row_add);
@@ -451,14 +465,16 @@ cudaError_t ce_bwd(const CeProblem& q, const void* X, const void* W, const int64
   p.d_tiles = b.d_tiles;
   p.d_width = b.d_width;
   CUtensorMap xk, wk, wmn, xmn, accm, dwm, dst[kBuffers], dk[kBuffers], dmn[kBuffers];
-  if (!make_tmap_bf16(&xk, X, q.m, q.d, ce::kBK, ce::kBM) || !make_tmap_bf16(&wk, W, q.vocab, q.d, ce::kBK, ce::kBM) ||
+  const bool few = is_few(q);
+  const int token_box = few ? p.few_n / 2 : ce::kBM;
+  if (!make_tmap_bf16(&xk, X, q.m, q.d, ce::kBK, token_box) || !make_tmap_bf16(&wk, W, q.vocab, q.d, ce::kBK, ce::kBM) ||
       !make_tmap_bf16(&wmn, W, q.vocab, q.d, 64, ce::kBK) || !make_tmap_bf16(&xmn, X, q.m, q.d, 64, ce::kBK) ||
       !make_tmap_2d(&accm, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, acc, int64_t(b.splits) * b.acc_rows, q.d, 16, 32, CU_TENSOR_MAP_SWIZZLE_64B) ||
       !make_tmap_bf16_store_sw64(&dwm, dW ? dW : X, dW ? q.vocab : q.m, q.d))
     return cudaErrorInvalidValue;
   for (int k = 0; k < b.buffers; ++k) {
     void* D = w8 + b.D + k * b.D_stride;
-    if (!make_tmap_bf16_store_sw64(&dst[k], D, q.m, piece_cols) || !make_tmap_bf16(&dk[k], D, q.m, piece_cols, ce::kBK, ce::kBM) ||
+    if (!make_tmap_bf16_store_sw64(&dst[k], D, q.m, piece_cols) || !make_tmap_bf16(&dk[k], D, q.m, piece_cols, ce::kBK, token_box) ||
         !make_tmap_bf16(&dmn[k], D, q.m, piece_cols, 64, ce::kBK))
       return cudaErrorInvalidValue;
   }
@@ -470,20 +486,21 @@ cudaError_t ce_bwd(const CeProblem& q, const void* X, const void* W, const int64
   auto dlogits = [&](int piece) {
     set_piece(piece);
     const CUtensorMap& out = dst[piece % kBuffers];
-    p.units = p.m_tiles * p.n_tiles;
-    p.wait_first = piece == 0 || put_back;
-    return launch<ce::DLOGITS>(xk, wk, xk, wk, out, out, p, st);
+    p.units = few ? p.n_tiles : p.m_tiles * p.n_tiles;
+    p.D = reinterpret_cast<__nv_bfloat16*>(w8 + b.D + (piece % kBuffers) * b.D_stride);
+    p.wait_first = piece == 0 || put_back || few;
+    return launch<ce::DLOGITS>(few, xk, wk, xk, wk, out, out, p, st);
   };
   auto grads = [&](int piece) {
     set_piece(piece);
     p.first_piece = piece == 0;
-    p.wait_first = piece + 1 == b.pieces || put_back;
+    p.wait_first = piece + 1 == b.pieces || put_back || few;
     p.piece_kb = p.n_tiles * (ce::kTile / ce::kBK);
     // a last piece shorter than the others may leave the last splits without a k-block: those tiles are left out
     const int splits = std::min(b.splits, ceil_div(p.piece_kb, b.kb_per_split));
-    p.x_units = dX ? splits * p.m_tiles * b.d_tiles : 0;
+    p.x_units = dX ? splits * (few ? ceil_div(q.d, ce::kTile) : p.m_tiles * b.d_tiles) : 0;
     p.units = p.x_units + (dW ? p.n_tiles * b.d_tiles : 0);
-    return launch<ce::GRADS>(dk[piece % kBuffers], wmn, dmn[piece % kBuffers], xmn, accm, dwm, p, st);
+    return launch<ce::GRADS>(few, dk[piece % kBuffers], wmn, dmn[piece % kBuffers], xmn, accm, dwm, p, st);
   };
   cudaError_t e = cudaSuccess;
   if (put_back) {   // few tokens: one piece as a rule; every launch needs the one before it

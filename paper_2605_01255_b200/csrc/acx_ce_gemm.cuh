@@ -11,6 +11,12 @@
 // tile takes K / 16 instructions of 128 cycles; its epilogue (128 x 256 elements per CTA, eight warps, about five
 // instructions per exponential) about 2000 cycles, hidden behind the next tile's mainloop by the second accumulator.
 //
+// FEW: at most 64 tokens.  A tile of 256 tokens would be mostly empty rows, and the tensor core takes as long for those: with
+// 64 tokens and 2048 columns the logits of 128256 words were bound by it (119 us under sustained load, at 1.3 GHz under the
+// power limit) instead of by the 525 MB of W.  So the operands change places: W's rows (of the logits; W's columns for dX)
+// are the 256 rows of the tile and the tokens its 32 or 64 columns, a quarter of the instructions' time, and the smaller
+// stages leave room for nine.  A lane then has a word, and keeps its own maximum and sum per token over all its tiles.
+//
 // Roles per CTA (320 threads, one CTA per SM): warp 0 TMA producer, warp 1 UMMA issuer (of the leader) and owner of the
 // tensor memory, warps 2..9 epilogue: two per TMEM lane quarter, 128 columns each.  Six 32 KiB stages; all waits bounded.
 // Loads are plain bulk tensor copies (no cluster multicast).
@@ -31,14 +37,23 @@ constexpr int kBM = 128;                   // rows of the tile per CTA (a pair: 
 constexpr int kTile = 256;                 // rows and columns of a pair's tile
 constexpr int kBK = 64;                    // bf16 per stage along K: one 128-byte swizzle row
 constexpr int kUmmaK = 16;
-constexpr int kStages = 6;
-constexpr int kABytes = kBM * kBK * 2, kBBytes = kBM * kBK * 2, kStageBytes = kABytes + kBBytes;
+constexpr int kFewTokens = 64;
+constexpr int kABytes = kBM * kBK * 2, kBBytes = kBM * kBK * 2;
+constexpr int kFewBBytes = kFewTokens / 2 * kBK * 2;   // FEW: half of the tokens per CTA
+constexpr int kStagesBytes = 6 * (kABytes + kBBytes);
+// Stages: six of 32 KiB; nine of 20 KiB where the tokens are the narrow operand of every unit (dW needs the whole 32 KiB)
+template <int KIND, bool FEW>
+struct Stages {
+  static constexpr bool kNarrow = FEW && KIND != 2;
+  static constexpr int kCount = kNarrow ? 9 : 6, kBytes = kABytes + (kNarrow ? kFewBBytes : kBBytes);
+  static_assert(kCount * kBytes <= kStagesBytes, "stages");
+};
 constexpr int kChunkBytes = 64 * kBK * 2;  // MN-major operand: 64 k-rows of 128 bytes
 constexpr int kAccCols = 256, kTmemCols = 512;
 constexpr int kEpiWarp0 = 2, kEpiWarps = 8, kThreads = 32 * (kEpiWarp0 + kEpiWarps);
 constexpr int kBoxBytes = 32 * 64;         // store staging: 32 rows of 64 bytes, 64-byte swizzle; two per epilogue warp
 constexpr int kBarBytes = 1024;
-constexpr int kOutOffset = kStages * kStageBytes + kBarBytes;
+constexpr int kOutOffset = kStagesBytes + kBarBytes;
 constexpr int kSmemBytes = kOutOffset + kEpiWarps * 2 * kBoxBytes + 1024;
 static_assert(kSmemBytes <= 232448, "shared memory of one CTA");
 
@@ -57,13 +72,16 @@ struct Params {
   int x_units, kb_per_split, piece_kb, token_kb;
   int acc_rows;                 // rows of one split's fp32 sums (tokens rounded up to whole tiles)
   int first_piece;              // the sums are stored, not added
+  int few_n;                    // FEW: tokens rounded up to 32
+  __nv_bfloat16* D;             // FEW, DLOGITS: the piece's D, [tokens][ld_d]
+  int64_t ld_d;
+  float* acc;                   // FEW, GRADS: the fp32 sums of dX, [split][acc_rows][d]
   int wait_first;               // this launch needs what the launch before it writes (else only what the one before that does)
   float c;                      // logit_scale * log2(e): exponents are taken in base 2
   const int64_t* targets;
   const float* lse;             // natural logarithm
   const float* weight;          // may be null: one
-  float2* part;                 // LSE: [.][tokens] (maximum, sum) in base 2, of 128 columns each; of one token tile: of all the
-                                // columns that a pair's column half met ([2 * pairs][tokens])
+  float2* part;                 // LSE: [.][tokens] (maximum, sum) in base 2: of 128 columns each; FEW: of what 32 lanes met
   float* target_logit;          // LSE: [tokens], base 2
   uint32_t* ticket;             // LSE: set to zero for the kernel behind it
   float* corr;                  // DLOGITS: [tokens] what rounding took from the target's element of D
@@ -82,12 +100,29 @@ struct Unit {
   int split;
 };
 
-template <int KIND>
+template <int KIND, bool FEW>
 __device__ __forceinline__ Unit decode(const Params& p, int u) {
   Unit t;
   t.split = 0;
   t.x = false;
   t.bn = kTile;
+  if (FEW && (KIND != GRADS || u < p.x_units)) {   // rows: words of the piece, or columns of d
+    t.x = KIND == GRADS;
+    t.n0 = 0;
+    t.bn = p.few_n;
+    if (KIND != GRADS) {
+      t.m0 = u * kTile;
+      t.kb0 = 0;
+      t.kb1 = (p.d + kBK - 1) / kBK;
+    } else {
+      const int tiles = (p.d + kTile - 1) / kTile;
+      t.m0 = (u % tiles) * kTile;
+      t.split = u / tiles;
+      t.kb0 = t.split * p.kb_per_split;
+      t.kb1 = min(p.piece_kb, t.kb0 + p.kb_per_split);
+    }
+    return t;
+  }
   if (KIND != GRADS) {
     const int per_group = p.group * p.n_tiles, g = u / per_group, r = u - g * per_group;
     const int gm = min(p.group, p.m_tiles - g * p.group);
@@ -130,24 +165,26 @@ __device__ __forceinline__ void tma_reduce_add_2d(const CUtensorMap* map, uint32
 }
 
 // LSE, DLOGITS: tmap_a = X (64 x 128 boxes), tmap_b = W (64 x 128 boxes), tmap_out = D (DLOGITS).
+// FEW: the maps of X and of D as rows of tokens have boxes of 64 x few_n / 2.
 // GRADS: tmap_a = D as rows of tokens (64 x 128 boxes), tmap_a2 = D read MN-major (64 x 64 boxes), tmap_b = W, tmap_b2 = X
 // (both 64 x 64 boxes, MN-major), tmap_out = the fp32 sums of dX (16 x 32 boxes), tmap_out2 = dW (32 x 32 boxes).
-template <int KIND>
+template <int KIND, bool FEW>
 __global__ void __launch_bounds__(kThreads, 1)
     ce_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
               const __grid_constant__ CUtensorMap tmap_a2, const __grid_constant__ CUtensorMap tmap_b2,
               const __grid_constant__ CUtensorMap tmap_out, const __grid_constant__ CUtensorMap tmap_out2, const Params p) {
+  constexpr int kStages = Stages<KIND, FEW>::kCount, kStageBytes = Stages<KIND, FEW>::kBytes;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem_gen = smem_raw + (smem_base - ptx::smem_u32(smem_raw));
-  const uint32_t bar_base = smem_base + kStages * kStageBytes;
+  const uint32_t bar_base = smem_base + kStagesBytes;
   auto full_bar = [&](int s) { return bar_base + 8u * s; };
   auto empty_bar = [&](int s) { return bar_base + 8u * (kStages + s); };
   auto tfull_bar = [&](int a) { return bar_base + 8u * (2 * kStages + a); };
   auto tempty_bar = [&](int a) { return bar_base + 8u * (2 * kStages + 2 + a); };
   constexpr int kSlot = 8 * (2 * kStages + 4);
-  volatile uint32_t* tmem_slot_gen = reinterpret_cast<volatile uint32_t*>(smem_gen + kStages * kStageBytes + kSlot);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_gen + kStages * kStageBytes + kSlot + 4);
+  volatile uint32_t* tmem_slot_gen = reinterpret_cast<volatile uint32_t*>(smem_gen + kStagesBytes + kSlot);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_gen + kStagesBytes + kSlot + 4);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = ptx::cluster_ctarank();
@@ -202,7 +239,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t phase = 0, armed = 0;
       bool ok = true;
       for (int u = pair; ok && u < p.units; u += pairs) {
-        const Unit t = decode<KIND>(p, u);
+        const Unit t = decode<KIND, FEW>(p, u);
         const int a_row0 = t.m0 + int(rank) * kBM;
         const int hw = t.bn >> 1, b_row0 = t.n0 + int(rank) * hw;       // this CTA's half of the B rows
         // one loop per operand layout, so that everything that does not change along K is fixed in it
@@ -218,7 +255,21 @@ __global__ void __launch_bounds__(kThreads, 1)
         auto arm = [&](uint32_t bytes) {
           if (rank == 0) ptx::mbar_arrive_expect_tx(full_bar(stage), 2 * bytes);
         };
-        if (KIND != GRADS) {
+        if (FEW && KIND != GRADS) {
+          const int w_row0 = p.v0 + a_row0;
+          stages([&](uint32_t a_dst, uint32_t b_dst, uint32_t bar, int k0) {
+            arm(kABytes + hw * kBK * 2);
+            ptx::tma_load_2d_pair(a_dst, &tmap_b, bar, k0, w_row0);
+            ptx::tma_load_2d_pair(b_dst, &tmap_a, bar, k0, b_row0);
+          });
+        } else if (FEW && t.x) {
+          stages([&](uint32_t a_dst, uint32_t b_dst, uint32_t bar, int k0) {
+            arm(kABytes + hw * kBK * 2);
+            ptx::tma_load_2d_pair(a_dst, &tmap_b, bar, a_row0, p.v0 + k0);
+            ptx::tma_load_2d_pair(a_dst + kChunkBytes, &tmap_b, bar, a_row0 + 64, p.v0 + k0);
+            ptx::tma_load_2d_pair(b_dst, &tmap_a, bar, k0, b_row0);
+          });
+        } else if (KIND != GRADS) {
           const int w_row0 = p.v0 + b_row0;
           stages([&](uint32_t a_dst, uint32_t b_dst, uint32_t bar, int k0) {
             arm(kABytes + kBBytes);
@@ -275,13 +326,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t phase = 0;
       bool ok = true;
       for (int u = pair; ok && u < p.units; u += pairs, ++it) {
-        const Unit t = decode<KIND>(p, u);
+        const Unit t = decode<KIND, FEW>(p, u);
         const int acc = it & 1;
         const uint32_t d_tmem = tmem_base + acc * kAccCols;
         if (!ptx::mbar_wait_cluster(tempty_bar(acc), ((it >> 1) & 1) ^ 1u, abort_flag)) { give_up(); ok = false; break; }
         ptx::tcgen05_fence_after_sync();
-        auto products = [&](auto a_is_mn) {
-          constexpr bool a_mn = decltype(a_is_mn)::value, b_mn = KIND == GRADS;
+        auto products = [&](auto a_is_mn, auto b_is_mn) {
+          constexpr bool a_mn = decltype(a_is_mn)::value, b_mn = decltype(b_is_mn)::value;
           constexpr uint32_t a_lbo = a_mn ? kChunkBytes : 16, a_step = (a_mn ? kUmmaK * 128 : kUmmaK * 2) >> 4;
           constexpr uint32_t b_lbo = b_mn ? kChunkBytes : 16, b_step = (b_mn ? kUmmaK * 128 : kUmmaK * 2) >> 4;
           const uint32_t idesc = ptx::make_idesc_bf16(kTile, t.bn, a_mn, b_mn);
@@ -297,8 +348,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (++stage == kStages) { stage = 0; phase ^= 1u; }
           }
         };
-        if (KIND == GRADS && !t.x) products(std::true_type{});
-        else products(std::false_type{});
+        using Yes = std::true_type;
+        using No = std::false_type;
+        if (KIND != GRADS) products(No{}, No{});
+        else if (!t.x) products(Yes{}, Yes{});
+        else if (FEW) products(Yes{}, No{});
+        else products(No{}, Yes{});
         if (ok) ptx::umma_commit_pair(tfull_bar(acc), 3);
       }
     }
@@ -348,17 +403,42 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       return mine;
     };
-    float run_m = -INFINITY, run_s = 0.f;    // LSE
+    // FEW: this warp has the 32 tokens from few0 on (there may be none); a lane's own token's target, and in the staging what
+    // the tokens need (DLOGITS)
+    const int few0 = 32 * half;
+    int few_y = -1;
+    float few_m[FEW && KIND == LSE ? 32 : 1], few_s[FEW && KIND == LSE ? 32 : 1];
+    float* const few_lse2 = reinterpret_cast<float*>(out_gen);
+    float* const few_w = few_lse2 + 32;
+    if (FEW) {
+      const int tt = few0 + lane;
+      if (KIND != GRADS && tt < p.tokens) {
+        const int64_t y = __ldcg(p.targets + tt);
+        few_y = y >= 0 && y < p.vocab ? int(y) : -1;
+      }
+      if (KIND == DLOGITS) {
+        few_lse2[lane] = few_y >= 0 ? __ldcg(p.lse + tt) * kLog2e : 0.f;
+        few_w[lane] = few_y >= 0 ? (p.weight ? __ldcg(p.weight + tt) : 1.f) : 0.f;
+        __syncwarp();
+      }
+      if (KIND == LSE) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          few_m[FEW && KIND == LSE ? j : 0] = -INFINITY;
+          few_s[FEW && KIND == LSE ? j : 0] = 0.f;
+        }
+      }
+    }
     int it = 0;
     for (int u = pair; u < p.units; u += pairs, ++it) {
-      const Unit t = decode<KIND>(p, u);
+      const Unit t = decode<KIND, FEW>(p, u);
       const int acc = it & 1;
       const int row0 = t.m0 + int(rank) * kBM + quarter * 32, row = row0 + lane;
       const int col0 = t.n0 + half * 128;               // of the output; LSE, DLOGITS: of the piece
       // what the row needs besides the accumulator, fetched before the wait for it
       int64_t y = -1;
       float lse2 = 0.f, w = 0.f;
-      if (KIND != GRADS && row < p.tokens) {
+      if (!FEW && KIND != GRADS && row < p.tokens) {
         y = __ldcg(p.targets + row);
         if (y < 0 || y >= p.vocab) y = -1;              // not trained on
         if (KIND == DLOGITS && y >= 0) {
@@ -377,12 +457,64 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) ptx::mbar_arrive_cluster(on_leader(tempty_bar(acc)));
       };
       uint32_t v[32];
+      if (FEW && (KIND != GRADS || t.x)) {
+        const uint32_t few_addr = tmem_base + (uint32_t(quarter * 32) << 16) + acc * kAccCols + few0;
+        if (few0 < t.bn) {
+          __syncwarp();
+          ptx::tmem_ld_x32(few_addr, v);
+          ptx::tmem_ld_wait();
+          const bool word = KIND != GRADS && p.v0 + row < p.vocab;   // this lane's row is a word of the vocabulary
+          if (KIND == LSE) {
+            if (word) {
+#pragma unroll
+              for (int j = 0; j < 32; ++j) {
+                const int k = FEW && KIND == LSE ? j : 0;
+                const float x = __uint_as_float(v[j]) * p.c, top = fmaxf(few_m[k], x);
+                few_s[k] = few_s[k] * exp2_fast(few_m[k] - top) + exp2_fast(x - top);
+                few_m[k] = top;
+              }
+            }
+          } else if (KIND == DLOGITS) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+              const float w1 = few_w[j], e = w1 * exp2_fast(fmaf(__uint_as_float(v[j]), p.c, -few_lse2[j]));
+              if (few0 + j < p.tokens) p.D[int64_t(few0 + j) * p.ld_d + row] = __float2bfloat16_rn(word && w1 != 0.f ? e : 0.f);
+            }
+          } else if (row < p.d) {
+            float* o = p.acc + (int64_t(t.split) * p.acc_rows + few0) * p.d + row;
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (few0 + j < p.tokens) {     // one addition per element and launch: the order is that of the pieces
+                if (p.first_piece) o[int64_t(j) * p.d] = __uint_as_float(v[j]);
+                else atomicAdd(o + int64_t(j) * p.d, __uint_as_float(v[j]));
+              }
+          }
+          if (KIND != GRADS) {               // the targets among this warp's words
+            const int r = few_y < 0 ? -1 : few_y - (p.v0 + row0);
+            for (uint32_t hits = __ballot_sync(0xFFFFFFFFu, r >= 0 && r < 32); hits; hits &= hits - 1) {
+              const int j = __ffs(hits) - 1, owner = __shfl_sync(0xFFFFFFFFu, r, j), tt = few0 + j;
+              const float x = __uint_as_float(ptx::tmem_ld_x1(few_addr + j));
+              if (lane == owner && KIND == LSE) p.target_logit[tt] = x * p.c;
+              if (lane == owner && KIND == DLOGITS) {
+                const float w1 = few_w[j];
+                float e = w1 * exp2_fast(fmaf(x, p.c, -few_lse2[j])) - w1;
+                if (p.vocab == 1 && e == e) e = 0.f;   // one word is certain: the difference would be its rounding only
+                const __nv_bfloat16 b = __float2bfloat16_rn(e);
+                p.D[int64_t(tt) * p.ld_d + row] = b;
+                p.corr[tt] = e - __bfloat162float(b);
+              }
+              __syncwarp();
+            }
+          }
+        }
+        release_accumulator();
+        continue;
+      }
       if (KIND != GRADS) {
         const int valid = min(128, p.vocab - (p.v0 + col0));          // columns of this half that exist
         const int tc = y >= 0 ? int(max(int64_t(-1), min(int64_t(1) << 20, y - (p.v0 + col0)))) : -1;   // the target's column here
         if (KIND == LSE) {
-          const bool one_tile = p.m_tiles == 1;       // every unit of this pair has the same rows
-          float m = one_tile ? run_m : -INFINITY, s = one_tile ? run_s : 0.f;
+          float m = -INFINITY, s = 0.f;
           for (int c0 = 0; c0 < valid; c0 += 32) {
             __syncwarp();
             ptx::tmem_ld_x32(taddr + c0, v);
@@ -413,13 +545,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             s += s1;
           }
-          if (one_tile) {
-            run_m = m;
-            run_s = s;
-            if (u + pairs >= p.units && row < p.tokens) p.part[int64_t(2 * pair + half) * p.tokens + row] = make_float2(m, s);
-          } else if (valid > 0 && row < p.tokens) {
-            p.part[int64_t(col0 >> 7) * p.tokens + row] = make_float2(m, s);
-          }
+          if (valid > 0 && row < p.tokens) p.part[int64_t(col0 >> 7) * p.tokens + row] = make_float2(m, s);
         } else {
           for (int c0 = 0; c0 < 128; c0 += 32) {
             __syncwarp();
@@ -524,6 +650,25 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       release_accumulator();
+    }
+    if (FEW && KIND == LSE && few0 < p.few_n) {
+      // the 32 lanes' pairs of every token into one: the token's own lane keeps it
+      float m = 0.f, s = 0.f;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) {
+        const int k = FEW && KIND == LSE ? j : 0;
+        float top = few_m[k];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        float sum = few_s[k] == 0.f ? 0.f : few_s[k] * exp2_fast(few_m[k] - top);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+        if (lane == j) {
+          m = top;
+          s = sum;
+        }
+      }
+      if (few0 + lane < p.tokens) p.part[int64_t((2 * pair + int(rank)) * 4 + quarter) * p.tokens + few0 + lane] = make_float2(m, s);
     }
     if (KIND != LSE && lane == 0) ptx::tma_store_wait_read<0>();   // shared memory must outlive the stores' reads
   }

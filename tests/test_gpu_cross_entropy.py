@@ -57,10 +57,11 @@ def logit_error(X, W, scale, lse):
     return 2.0 ** -23 * (d / 16 + 8) * mag + 2.0 ** -21 * (1 + np.abs(lse))
 
 
-# a word, a partly filled tile, odd everything, several token tiles, a d of several tiles, split sums; the last two in pieces,
-# with and without what is put back into dW for few tokens
+# a word, a partly filled tile, odd everything, several token tiles, a d of several tiles, split sums; up to 64 tokens (exchanged
+# operands) and just above; the last three in pieces, with few tokens, with and without what is put back into dW
 SHAPES = [(1, 64, 1000), (7, 8, 1), (5, 72, 37), (130, 136, 257), (300, 904, 3203), (1000, 264, 20000), (257, 2056, 1111), (700, 520, 513),
-          (64, 1024, 50001), (513, 136, 777),
+          (64, 1024, 50001), (33, 264, 5000), (65, 264, 5000), (513, 136, 777),
+          (64, 8, 1100001),
           (500, 64, 140001), (4096, 72, 17001)]
 
 
