@@ -205,9 +205,10 @@ __global__ void __launch_bounds__(256) ce_finish_kernel(const float* acc, int sp
 // target as t, in fp32 and in the order of the tokens, where t is the first of them (row_key[t] = its target; -1 for the
 // others).  A target's element is most of what its token adds to dW.  With few tokens the rounding of each would be seen in
 // full (with one to sixteen weighted tokens up to 3 times the error of rounding dW alone, more than 1.5 times in one case out
-// of four); from some 256 tokens on they average out (1.3 times), so this is done for up to kPutBackTokens tokens, where it
-// takes 4 us beside the 40 to 150 us of the step.
-constexpr int kPutBackTokens = 512;
+// of four); from 256 tokens on they average out (1.3 times), so this is done for up to that many, where it takes 4 to 6 us of
+// the 35 to 150 us of a step (at 333 tokens it was 8 %).  Folding it into the products' epilogue token by token took twice as
+// long: targets are skewed, and a frequent word's tokens all meet one lane there.
+using ce::kPutBackTokens;
 __global__ void __launch_bounds__(kPutBackTokens) ce_put_back_kernel(const float* corr, const int64_t* __restrict__ targets,
                                                                      const __nv_bfloat16* __restrict__ X, int tokens, int d, int v0, int v1,
                                                                      int* __restrict__ row_key, float* __restrict__ row_add) {
@@ -269,7 +270,7 @@ int pair_count() { return std::max(1, sm_count() / 2); }
 
 template <int KIND, bool FEW>
 cudaError_t launch(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& ta2, const CUtensorMap& tb2, const CUtensorMap& to,
-                   const CUtensorMap& to2, const Params& p, cudaStream_t st) {
+                   const CUtensorMap& to2, const CUtensorMap& to3, const Params& p, cudaStream_t st) {
   auto kernel = ce::ce_kernel<KIND, FEW>;
   static DeviceOnce once;
   if (once.needed()) {
@@ -291,15 +292,15 @@ cudaError_t launch(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorM
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, ta, tb, ta2, tb2, to, to2, p);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, ta, tb, ta2, tb2, to, to2, to3, p);
   kernel_launch_counter().fetch_add(1, std::memory_order_relaxed);
   return e;
 }
 
 template <int KIND>
 cudaError_t launch(bool few, const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& ta2, const CUtensorMap& tb2,
-                   const CUtensorMap& to, const CUtensorMap& to2, const Params& p, cudaStream_t st) {
-  return few ? launch<KIND, true>(ta, tb, ta2, tb2, to, to2, p, st) : launch<KIND, false>(ta, tb, ta2, tb2, to, to2, p, st);
+                   const CUtensorMap& to, const CUtensorMap& to2, const CUtensorMap& to3, const Params& p, cudaStream_t st) {
+  return few ? launch<KIND, true>(ta, tb, ta2, tb2, to, to2, to3, p, st) : launch<KIND, false>(ta, tb, ta2, tb2, to, to2, to3, p, st);
 }
 
 // Up to 64 tokens: the kernels with the operands exchanged (see FEW).
@@ -341,7 +342,7 @@ struct FwdPlan {
 };
 FwdPlan fwd_plan(const CeProblem& q) {
   FwdPlan f;
-  f.parts = is_few(q) ? 8 * std::min(ceil_div(q.vocab, ce::kTile), pair_count()) : ceil_div(q.vocab, 128);   // see Params::part
+  f.parts = is_few(q) ? 8 * std::min(ceil_div(q.vocab, ce::kTile), pair_count()) : ceil_div(q.vocab, ce::kGroupCols);   // see Params::part
   f.blocks = ceil_div(q.m, kTokensPerBlock);
   f.part = 0;
   f.target = f.part + aligned(size_t(f.parts) * size_t(q.m) * sizeof(float2));
@@ -423,7 +424,7 @@ cudaError_t ce_fwd(const CeProblem& q, const void* X, const void* W, const int64
   const bool few = is_few(q);
   const int token_box = few ? p.few_n / 2 : ce::kBM;
   if (!make_tmap_bf16(&ta, X, q.m, q.d, ce::kBK, token_box) || !make_tmap_bf16(&tb, W, q.vocab, q.d, ce::kBK, ce::kBM)) return cudaErrorInvalidValue;
-  const cudaError_t e = launch<ce::LSE>(few, ta, tb, ta, tb, ta, ta, p, st);
+  const cudaError_t e = launch<ce::LSE>(few, ta, tb, ta, tb, ta, ta, ta, p, st);
   if (e != cudaSuccess) return e;
   return launch_lined_up(ce_join_kernel, dim3(unsigned(f.blocks)), dim3(kJoinThreads), 0, st, static_cast<const float2*>(p.part),
                        static_cast<const float*>(p.target_logit), static_cast<const __nv_bfloat16*>(X), static_cast<const __nv_bfloat16*>(W),
@@ -464,17 +465,17 @@ cudaError_t ce_bwd(const CeProblem& q, const void* X, const void* W, const int64
   p.token_kb = ceil_div(q.m, ce::kBK);
   p.d_tiles = b.d_tiles;
   p.d_width = b.d_width;
-  CUtensorMap xk, wk, wmn, xmn, accm, dwm, dst[kBuffers], dk[kBuffers], dmn[kBuffers];
+  CUtensorMap xk, wk, wmn, xmn, accm, dwm, dwn, dst[kBuffers], dk[kBuffers], dmn[kBuffers];
   const bool few = is_few(q);
   const int token_box = few ? p.few_n / 2 : ce::kBM;
   if (!make_tmap_bf16(&xk, X, q.m, q.d, ce::kBK, token_box) || !make_tmap_bf16(&wk, W, q.vocab, q.d, ce::kBK, ce::kBM) ||
       !make_tmap_bf16(&wmn, W, q.vocab, q.d, 64, ce::kBK) || !make_tmap_bf16(&xmn, X, q.m, q.d, 64, ce::kBK) ||
-      !make_tmap_2d(&accm, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, acc, int64_t(b.splits) * b.acc_rows, q.d, 16, 32, CU_TENSOR_MAP_SWIZZLE_64B) ||
-      !make_tmap_bf16_store_sw64(&dwm, dW ? dW : X, dW ? q.vocab : q.m, q.d))
+      !make_tmap_f32(&accm, acc, int64_t(b.splits) * b.acc_rows, q.d, 32, 16) || !make_tmap_bf16(&dwm, dW ? dW : X, dW ? q.vocab : q.m, q.d, 64, 16) ||
+      !make_tmap_bf16_store_sw64(&dwn, dW ? dW : X, dW ? q.vocab : q.m, q.d))
     return cudaErrorInvalidValue;
   for (int k = 0; k < b.buffers; ++k) {
     void* D = w8 + b.D + k * b.D_stride;
-    if (!make_tmap_bf16_store_sw64(&dst[k], D, q.m, piece_cols) || !make_tmap_bf16(&dk[k], D, q.m, piece_cols, ce::kBK, token_box) ||
+    if (!make_tmap_bf16(&dst[k], D, q.m, piece_cols, 64, 16) || !make_tmap_bf16(&dk[k], D, q.m, piece_cols, ce::kBK, token_box) ||
         !make_tmap_bf16(&dmn[k], D, q.m, piece_cols, 64, ce::kBK))
       return cudaErrorInvalidValue;
   }
@@ -489,7 +490,7 @@ cudaError_t ce_bwd(const CeProblem& q, const void* X, const void* W, const int64
     p.units = few ? p.n_tiles : p.m_tiles * p.n_tiles;
     p.D = reinterpret_cast<__nv_bfloat16*>(w8 + b.D + (piece % kBuffers) * b.D_stride);
     p.wait_first = piece == 0 || put_back || few;
-    return launch<ce::DLOGITS>(few, xk, wk, xk, wk, out, out, p, st);
+    return launch<ce::DLOGITS>(few, xk, wk, xk, wk, out, out, out, p, st);
   };
   auto grads = [&](int piece) {
     set_piece(piece);
@@ -500,7 +501,7 @@ cudaError_t ce_bwd(const CeProblem& q, const void* X, const void* W, const int64
     const int splits = std::min(b.splits, ceil_div(p.piece_kb, b.kb_per_split));
     p.x_units = dX ? splits * (few ? ceil_div(q.d, ce::kTile) : p.m_tiles * b.d_tiles) : 0;
     p.units = p.x_units + (dW ? p.n_tiles * b.d_tiles : 0);
-    return launch<ce::GRADS>(few, dk[piece % kBuffers], wmn, dmn[piece % kBuffers], xmn, accm, dwm, p, st);
+    return launch<ce::GRADS>(few, dk[piece % kBuffers], wmn, dmn[piece % kBuffers], xmn, accm, dwm, dwn, p, st);
   };
   cudaError_t e = cudaSuccess;
   if (put_back) {   // few tokens: one piece as a rule; every launch needs the one before it

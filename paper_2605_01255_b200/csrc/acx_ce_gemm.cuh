@@ -8,8 +8,9 @@
 //            tiles; fp32 sums in global memory, added by the bulk-copy engine) and dW_piece = D^T X (bf16, complete).
 //
 // What bounds them: the tensor cores, from a few hundred tokens on; with fewer the bytes of W.  Per SM a 256 x 256 pair
-// tile takes K / 16 instructions of 128 cycles; its epilogue (128 x 256 elements per CTA, eight warps, about five
-// instructions per exponential) about 2000 cycles, hidden behind the next tile's mainloop by the second accumulator.
+// tile takes K / 16 instructions of 128 cycles.  Its epilogue (128 x 256 elements per CTA: 2048 cycles of exponentials at
+// least) is hidden behind the next tile's mainloop by the second accumulator where d is large enough for that; sixteen
+// warps share it, because with eight the latencies of its dependent steps made it 4600 (LSE) and 8300 cycles (DLOGITS).
 //
 // FEW: at most 64 tokens.  A tile of 256 tokens would be mostly empty rows, and the tensor core takes as long for those: with
 // 64 tokens and 2048 columns the logits of 128256 words were bound by it (119 us under sustained load, at 1.3 GHz under the
@@ -17,8 +18,8 @@
 // are the 256 rows of the tile and the tokens its 32 or 64 columns, a quarter of the instructions' time, and the smaller
 // stages leave room for nine.  A lane then has a word, and keeps its own maximum and sum per token over all its tiles.
 //
-// Roles per CTA (320 threads, one CTA per SM): warp 0 TMA producer, warp 1 UMMA issuer (of the leader) and owner of the
-// tensor memory, warps 2..9 epilogue: two per TMEM lane quarter, 128 columns each.  Six 32 KiB stages; all waits bounded.
+// Roles per CTA (576 threads, one CTA per SM): warp 0 TMA producer, warp 1 UMMA issuer (of the leader) and owner of the
+// tensor memory, warps 2..17 epilogue: four per TMEM lane quarter, 64 columns each.  Six 32 KiB stages; all waits bounded.
 // Loads are plain bulk tensor copies (no cluster multicast).
 #pragma once
 #include <cuda.h>
@@ -28,6 +29,7 @@
 #include <type_traits>
 
 #include "acx_internal.h"
+#include "acx_q8.cuh"
 #include "acx_umma.cuh"
 
 namespace acx {
@@ -38,6 +40,7 @@ constexpr int kTile = 256;                 // rows and columns of a pair's tile
 constexpr int kBK = 64;                    // bf16 per stage along K: one 128-byte swizzle row
 constexpr int kUmmaK = 16;
 constexpr int kFewTokens = 64;
+constexpr int kPutBackTokens = 256;        // see ce_put_back_kernel
 constexpr int kABytes = kBM * kBK * 2, kBBytes = kBM * kBK * 2;
 constexpr int kFewBBytes = kFewTokens / 2 * kBK * 2;   // FEW: half of the tokens per CTA
 constexpr int kStagesBytes = 6 * (kABytes + kBBytes);
@@ -50,11 +53,11 @@ struct Stages {
 };
 constexpr int kChunkBytes = 64 * kBK * 2;  // MN-major operand: 64 k-rows of 128 bytes
 constexpr int kAccCols = 256, kTmemCols = 512;
-constexpr int kEpiWarp0 = 2, kEpiWarps = 8, kThreads = 32 * (kEpiWarp0 + kEpiWarps);
-constexpr int kBoxBytes = 32 * 64;         // store staging: 32 rows of 64 bytes, 64-byte swizzle; two per epilogue warp
+constexpr int kEpiWarp0 = 2, kEpiWarps = 16, kGroupCols = 64, kThreads = 32 * (kEpiWarp0 + kEpiWarps);
+constexpr int kBoxBytes = 16 * 128;        // store staging, one box per epilogue warp: 16 rows of 128 bytes, 128-byte swizzle
 constexpr int kBarBytes = 1024;
 constexpr int kOutOffset = kStagesBytes + kBarBytes;
-constexpr int kSmemBytes = kOutOffset + kEpiWarps * 2 * kBoxBytes + 1024;
+constexpr int kSmemBytes = kOutOffset + kEpiWarps * kBoxBytes + 1024;
 static_assert(kSmemBytes <= 232448, "shared memory of one CTA");
 
 enum Kind { LSE = 0, DLOGITS = 1, GRADS = 2 };
@@ -81,7 +84,7 @@ struct Params {
   const int64_t* targets;
   const float* lse;             // natural logarithm
   const float* weight;          // may be null: one
-  float2* part;                 // LSE: [.][tokens] (maximum, sum) in base 2: of 128 columns each; FEW: of what 32 lanes met
+  float2* part;                 // LSE: [.][tokens] (maximum, sum) in base 2: of 64 columns each; FEW: of what 32 lanes met
   float* target_logit;          // LSE: [tokens], base 2
   uint32_t* ticket;             // LSE: set to zero for the kernel behind it
   float* corr;                  // DLOGITS: [tokens] what rounding took from the target's element of D
@@ -167,12 +170,14 @@ __device__ __forceinline__ void tma_reduce_add_2d(const CUtensorMap* map, uint32
 // LSE, DLOGITS: tmap_a = X (64 x 128 boxes), tmap_b = W (64 x 128 boxes), tmap_out = D (DLOGITS).
 // FEW: the maps of X and of D as rows of tokens have boxes of 64 x few_n / 2.
 // GRADS: tmap_a = D as rows of tokens (64 x 128 boxes), tmap_a2 = D read MN-major (64 x 64 boxes), tmap_b = W, tmap_b2 = X
-// (both 64 x 64 boxes, MN-major), tmap_out = the fp32 sums of dX (16 x 32 boxes), tmap_out2 = dW (32 x 32 boxes).
+// (both 64 x 64 boxes, MN-major), tmap_out = the fp32 sums of dX (32 x 16 boxes), tmap_out2 = dW (64 x 16 boxes), tmap_out3 =
+// dW (32 x 32 boxes, 64-byte swizzle).
 template <int KIND, bool FEW>
 __global__ void __launch_bounds__(kThreads, 1)
     ce_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
               const __grid_constant__ CUtensorMap tmap_a2, const __grid_constant__ CUtensorMap tmap_b2,
-              const __grid_constant__ CUtensorMap tmap_out, const __grid_constant__ CUtensorMap tmap_out2, const Params p) {
+              const __grid_constant__ CUtensorMap tmap_out, const __grid_constant__ CUtensorMap tmap_out2,
+              const __grid_constant__ CUtensorMap tmap_out3, const Params p) {
   constexpr int kStages = Stages<KIND, FEW>::kCount, kStageBytes = Stages<KIND, FEW>::kBytes;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -208,6 +213,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       ptx::prefetch_tensormap(&tmap_a2);
       ptx::prefetch_tensormap(&tmap_b2);
       ptx::prefetch_tensormap(&tmap_out2);
+      ptx::prefetch_tensormap(&tmap_out3);
     }
     if (KIND != LSE) ptx::prefetch_tensormap(&tmap_out);
   }
@@ -360,59 +366,86 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else {
     // ------------------------------------------------------------------ epilogue
     const int quarter = warp & 3;                       // TMEM lanes [32 * quarter, + 32) are the ones this warp may read
-    const int half = (warp - kEpiWarp0) >> 2;           // columns [128 * half, + 128) of the tile
-    uint8_t* out_gen = smem_gen + kOutOffset + (warp - kEpiWarp0) * 2 * kBoxBytes;
-    const uint32_t out_addr = smem_base + kOutOffset + (warp - kEpiWarp0) * 2 * kBoxBytes;
-    uint32_t n_stores = 0;
+    const int group = (warp - kEpiWarp0) >> 2;          // columns [64 * group, + 64) of the tile
+    uint8_t* out_gen = smem_gen + kOutOffset + (warp - kEpiWarp0) * kBoxBytes;
+    const uint32_t out_addr = smem_base + kOutOffset + (warp - kEpiWarp0) * kBoxBytes;
     float f = 0.f;
     if (KIND == GRADS) {
       const float dn = p.denom ? __ldcg(p.denom) : 1.f;
       f = dn > 0.f ? p.scale / dn : 0.f;
     }
-    // one 32-row box of 64 bytes per row, staged with the 64-byte swizzle (16-byte unit j of row l at j ^ ((l >> 1) & 3))
-    auto stage_box = [&](const uint32_t (&w)[16]) {
-      const uint32_t box = (n_stores & 1u) * kBoxBytes;
-      if (lane == 0) ptx::tma_store_wait_read<1>();   // the store that last used this box has read it
+    // 32 rows of 32 words (64 bf16 or 32 fp32 columns), a row per lane, to (x, y) of a map whose boxes are 16 rows of 128 bytes
+    // (16-byte unit j of row l at j ^ (l & 7)).  Rows of 128 bytes leave a CTA in half the time that twice as many of 64 take.
+    auto store_rows = [&](const uint32_t (&words)[32], const CUtensorMap* map, int x, int y, bool add) {
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        if (lane == 0) ptx::tma_store_wait_read<0>();   // the store that last used the box has read it
+        __syncwarp();
+        if ((lane >> 4) == r) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            *reinterpret_cast<uint4*>(out_gen + (lane & 15) * 128 + ((j ^ (lane & 7)) << 4)) =
+                make_uint4(words[4 * j], words[4 * j + 1], words[4 * j + 2], words[4 * j + 3]);
+        }
+        ptx::fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          if (add) tma_reduce_add_2d(map, out_addr, x, y + 16 * r);
+          else ptx::tma_store_2d(map, out_addr, x, y + 16 * r);
+          ptx::tma_store_commit();
+        }
+      }
+    };
+    // 32 rows of 16 words (32 bf16 columns), boxes of 32 rows of 64 bytes (unit j of row l at j ^ ((l >> 1) & 3))
+    auto store_narrow = [&](const uint32_t (&words)[32], const CUtensorMap* map, int x, int y) {
+      if (lane == 0) ptx::tma_store_wait_read<0>();
       __syncwarp();
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<uint4*>(out_gen + box + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4)) =
-            make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+        *reinterpret_cast<uint4*>(out_gen + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4)) =
+            make_uint4(words[4 * j], words[4 * j + 1], words[4 * j + 2], words[4 * j + 3]);
       ptx::fence_proxy_async_smem();
       __syncwarp();
-      ++n_stores;
-      return out_addr + box;
-    };
-    auto pack = [](const uint32_t (&v)[32], uint32_t (&w)[16]) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
-        w[i] = *reinterpret_cast<const uint32_t*>(&h);
+      if (lane == 0) {
+        ptx::tma_store_2d(map, out_addr, x, y);
+        ptx::tma_store_commit();
       }
     };
-    // The token whose row_add belongs to row `first_row` + lane of dW, or -1.  At most one does.
+    auto pack2 = [](uint32_t lo, uint32_t hi) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(lo), __uint_as_float(hi));
+      return *reinterpret_cast<const uint32_t*>(&h);
+    };
+    // The token whose row_add belongs to row `first_row` + lane of dW, or -1.  At most one does.  The keys stay in registers.
+    constexpr int kKeys = kPutBackTokens / 32;
+    int key[KIND == GRADS ? kKeys : 1];
+    if (KIND == GRADS && p.row_key) {
+#pragma unroll
+      for (int i = 0; i < kKeys; ++i) key[KIND == GRADS ? i : 0] = 32 * i + lane < p.tokens ? __ldcg(p.row_key + 32 * i + lane) : -1;
+    }
     auto find_row_add = [&](int first_row) {
       int mine = -1;
-#pragma unroll 4
-      for (int t0 = 0; t0 < p.tokens; t0 += 32) {
-        const int r = (t0 + lane < p.tokens ? __ldcg(p.row_key + t0 + lane) : -1) - first_row;
+#pragma unroll
+      for (int i = 0; i < kKeys; ++i) {
+        if (32 * i >= p.tokens) break;
+        const int r = key[KIND == GRADS ? i : 0] - first_row;
         for (uint32_t hits = __ballot_sync(0xFFFFFFFFu, r >= 0 && r < 32); hits; hits &= hits - 1) {
           const int src = __ffs(hits) - 1;
-          if (__shfl_sync(0xFFFFFFFFu, r, src) == lane) mine = t0 + src;
+          if (__shfl_sync(0xFFFFFFFFu, r, src) == lane) mine = 32 * i + src;
         }
       }
       return mine;
     };
-    // FEW: this warp has the 32 tokens from few0 on (there may be none); a lane's own token's target, and in the staging what
+    // FEW: this warp has the 16 tokens from few0 on (there may be none); a lane's own token's target, and in the staging what
     // the tokens need (DLOGITS)
-    const int few0 = 32 * half;
+    constexpr int kFew = 16;
+    const int few0 = kFew * group;
     int few_y = -1;
-    float few_m[FEW && KIND == LSE ? 32 : 1], few_s[FEW && KIND == LSE ? 32 : 1];
+    float few_m[FEW && KIND == LSE ? kFew : 1], few_s[FEW && KIND == LSE ? kFew : 1];
     float* const few_lse2 = reinterpret_cast<float*>(out_gen);
     float* const few_w = few_lse2 + 32;
     if (FEW) {
       const int tt = few0 + lane;
-      if (KIND != GRADS && tt < p.tokens) {
+      if (KIND != GRADS && lane < kFew && tt < p.tokens) {
         const int64_t y = __ldcg(p.targets + tt);
         few_y = y >= 0 && y < p.vocab ? int(y) : -1;
       }
@@ -423,51 +456,64 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (KIND == LSE) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
+        for (int j = 0; j < kFew; ++j) {
           few_m[FEW && KIND == LSE ? j : 0] = -INFINITY;
           few_s[FEW && KIND == LSE ? j : 0] = 0.f;
         }
       }
     }
-    int it = 0;
-    for (int u = pair; u < p.units; u += pairs, ++it) {
-      const Unit t = decode<KIND, FEW>(p, u);
-      const int acc = it & 1;
-      const int row0 = t.m0 + int(rank) * kBM + quarter * 32, row = row0 + lane;
-      const int col0 = t.n0 + half * 128;               // of the output; LSE, DLOGITS: of the piece
-      // what the row needs besides the accumulator, fetched before the wait for it
-      int64_t y = -1;
-      float lse2 = 0.f, w = 0.f;
-      if (!FEW && KIND != GRADS && row < p.tokens) {
-        y = __ldcg(p.targets + row);
-        if (y < 0 || y >= p.vocab) y = -1;              // not trained on
-        if (KIND == DLOGITS && y >= 0) {
-          lse2 = __ldcg(p.lse + row) * kLog2e;
-          w = p.weight ? __ldcg(p.weight + row) : 1.f;
+    // What a lane's row needs besides the accumulator, asked for one tile ahead (from L2 it takes longer than a small tile)
+    struct RowNeeds {
+      int2 y;          // the target, as it is in memory
+      float lse, weight;
+    };
+    auto needs_of = [&](int m0) {
+      RowNeeds n{make_int2(-1, -1), 0.f, 1.f};
+      const int r = m0 + int(rank) * kBM + quarter * 32 + lane;
+      if (!FEW && KIND != GRADS && r < p.tokens) {
+        n.y = __ldcg(reinterpret_cast<const int2*>(p.targets) + r);
+        if (KIND == DLOGITS) {
+          n.lse = __ldcg(p.lse + r);
+          if (p.weight) n.weight = __ldcg(p.weight + r);
         }
       }
+      return n;
+    };
+    int it = 0;
+    Unit ahead = decode<KIND, FEW>(p, min(pair, p.units - 1));
+    RowNeeds needs = needs_of(ahead.m0);
+    for (int u = pair; u < p.units; u += pairs, ++it) {
+      const Unit t = ahead;
+      ahead = decode<KIND, FEW>(p, min(u + pairs, p.units - 1));
+      const int acc = it & 1;
+      const int row0 = t.m0 + int(rank) * kBM + quarter * 32, row = row0 + lane;
+      const int col0 = t.n0 + group * kGroupCols;               // of the output; LSE, DLOGITS: of the piece
+      // a target outside [0, vocab): not trained on
+      const int y = needs.y.y == 0 && uint32_t(needs.y.x) < uint32_t(p.vocab) ? needs.y.x : -1;
+      const float lse2 = needs.lse * kLog2e, weight = y >= 0 ? needs.weight : 0.f;
+      needs = needs_of(ahead.m0);
       const int add_token = (KIND == GRADS && !t.x && p.row_key) ? find_row_add(p.v0 + row0) : -1;
       const bool full_ok = ptx::mbar_wait_cluster(tfull_bar(acc), (it >> 1) & 1, abort_flag);
       if (!__all_sync(0xFFFFFFFFu, full_ok)) { give_up(); break; }
       ptx::tcgen05_fence_after_sync();
-      const uint32_t taddr = tmem_base + (uint32_t(quarter * 32) << 16) + acc * kAccCols + half * 128;
+      const uint32_t taddr = tmem_base + (uint32_t(quarter * 32) << 16) + acc * kAccCols + group * kGroupCols;
       auto release_accumulator = [&]() {
         ptx::tcgen05_fence_before_sync();
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive_cluster(on_leader(tempty_bar(acc)));
+        if (lane == 0) ptx::mbar_arrive_remote(on_leader(tempty_bar(acc)));
       };
-      uint32_t v[32];
       if (FEW && (KIND != GRADS || t.x)) {
+        uint32_t v[kFew];
         const uint32_t few_addr = tmem_base + (uint32_t(quarter * 32) << 16) + acc * kAccCols + few0;
         if (few0 < t.bn) {
           __syncwarp();
-          ptx::tmem_ld_x32(few_addr, v);
+          ptx::tmem_ld_x16(few_addr, v);
           ptx::tmem_ld_wait();
           const bool word = KIND != GRADS && p.v0 + row < p.vocab;   // this lane's row is a word of the vocabulary
           if (KIND == LSE) {
             if (word) {
 #pragma unroll
-              for (int j = 0; j < 32; ++j) {
+              for (int j = 0; j < kFew; ++j) {
                 const int k = FEW && KIND == LSE ? j : 0;
                 const float x = __uint_as_float(v[j]) * p.c, top = fmaxf(few_m[k], x);
                 few_s[k] = few_s[k] * exp2_fast(few_m[k] - top) + exp2_fast(x - top);
@@ -476,14 +522,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           } else if (KIND == DLOGITS) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
+            for (int j = 0; j < kFew; ++j) {
               const float w1 = few_w[j], e = w1 * exp2_fast(fmaf(__uint_as_float(v[j]), p.c, -few_lse2[j]));
               if (few0 + j < p.tokens) p.D[int64_t(few0 + j) * p.ld_d + row] = __float2bfloat16_rn(word && w1 != 0.f ? e : 0.f);
             }
           } else if (row < p.d) {
             float* o = p.acc + (int64_t(t.split) * p.acc_rows + few0) * p.d + row;
 #pragma unroll
-            for (int j = 0; j < 32; ++j)
+            for (int j = 0; j < kFew; ++j)
               if (few0 + j < p.tokens) {     // one addition per element and launch: the order is that of the pieces
                 if (p.first_piece) o[int64_t(j) * p.d] = __uint_as_float(v[j]);
                 else atomicAdd(o + int64_t(j) * p.d, __uint_as_float(v[j]));
@@ -510,152 +556,156 @@ __global__ void __launch_bounds__(kThreads, 1)
         release_accumulator();
         continue;
       }
+      // Columns [32 c, + 32) of the row out of tensor memory; `last`: the accumulator is free for the tile after next.
+      auto drain = [&](int c, uint32_t (&v)[32], bool last) {
+        __syncwarp();
+        ptx::tmem_ld_x32(taddr + 32 * c, v);
+        ptx::tmem_ld_wait();
+        if (last) release_accumulator();
+      };
       if (KIND != GRADS) {
-        const int valid = min(128, p.vocab - (p.v0 + col0));          // columns of this half that exist
-        const int tc = y >= 0 ? int(max(int64_t(-1), min(int64_t(1) << 20, y - (p.v0 + col0)))) : -1;   // the target's column here
-        if (KIND == LSE) {
-          float m = -INFINITY, s = 0.f;
-          for (int c0 = 0; c0 < valid; c0 += 32) {
-            __syncwarp();
-            ptx::tmem_ld_x32(taddr + c0, v);
-            ptx::tmem_ld_wait();
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * p.c);
-            if (valid - c0 < 32) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (c0 + i >= valid) v[i] = __float_as_uint(-INFINITY);
-            }
-            if (__any_sync(0xFFFFFFFFu, tc >= c0 && tc < c0 + 32)) {
-              float tl = 0.f;
-#pragma unroll
-              for (int i = 0; i < 32; ++i) tl = tc == c0 + i ? __uint_as_float(v[i]) : tl;
-              if (tc >= c0 && tc < c0 + 32) p.target_logit[row] = tl;
-            }
-            float top = m;
-#pragma unroll
-            for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(v[i]));
-            s *= exp2_fast(m - top);      // m = -inf at first: 0 (an all -inf row gives NaN, as the definition's difference does)
-            m = top;
-            float s1 = 0.f;
-#pragma unroll
-            for (int i = 0; i < 32; i += 2) {
-              s += exp2_fast(__uint_as_float(v[i]) - m);
-              s1 += exp2_fast(__uint_as_float(v[i + 1]) - m);
-            }
-            s += s1;
-          }
-          if (valid > 0 && row < p.tokens) p.part[int64_t(col0 >> 7) * p.tokens + row] = make_float2(m, s);
-        } else {
-          for (int c0 = 0; c0 < 128; c0 += 32) {
-            __syncwarp();
-            ptx::tmem_ld_x32(taddr + c0, v);
-            ptx::tmem_ld_wait();
-            // rows that are not trained on and columns past the vocabulary are zero whatever the logit is
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(w * exp2_fast(fmaf(__uint_as_float(v[i]), p.c, -lse2)));
-            if (valid - c0 < 32) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (c0 + i >= valid) v[i] = 0u;
-            }
-            if (__any_sync(0xFFFFFFFFu, tc >= c0 && tc < c0 + 32)) {
-              float e = 0.f;
-#pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (tc == c0 + i) {
-                  e = __uint_as_float(v[i]) - w;
-                  if (p.vocab == 1 && e == e) e = 0.f;   // one word is certain: the difference would be its rounding only
-                  v[i] = __float_as_uint(e);
-                }
-              if (tc >= c0 && tc < c0 + 32) p.corr[row] = e - __bfloat162float(__float2bfloat16_rn(e));
-            }
-            if (y < 0) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] = 0u;
-            }
-            uint32_t pk[16];
-            pack(v, pk);
-            const uint32_t src = stage_box(pk);
-            if (lane == 0) {
-              if (row0 < p.tokens) ptx::tma_store_2d(&tmap_out, src, col0 + c0, row0);
-              ptx::tma_store_commit();
-            }
-          }
-        }
-      } else {
-        const int cols = min(min(128, t.bn - half * 128), p.d - col0);   // columns of this half that exist (may be negative)
-        if (t.x) {
-          for (int c0 = 0; c0 < cols; c0 += 32) {
-            __syncwarp();
-            ptx::tmem_ld_x32(taddr + c0, v);
-            ptx::tmem_ld_wait();
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-              if (c0 + 16 * q >= cols) break;
-              uint32_t w16[16];
-#pragma unroll
-              for (int i = 0; i < 16; ++i) w16[i] = v[16 * q + i];
-              const uint32_t src = stage_box(w16);
-              if (lane == 0) {
-                const int orow = t.split * p.acc_rows + row0;
-                if (p.first_piece) ptx::tma_store_2d(&tmap_out, src, col0 + c0 + 16 * q, orow);
-                else tma_reduce_add_2d(&tmap_out, src, col0 + c0 + 16 * q, orow);
-                ptx::tma_store_commit();
-              }
-            }
-          }
-        } else {
-          // 64 columns at a time; the accumulator is free once the last of them have been read
-#pragma unroll
-          for (int h = 0; h < 128; h += 64) {
-            uint32_t w2[2][32];
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-              if (h + 32 * c < cols) {
-                __syncwarp();
-                ptx::tmem_ld_x32(taddr + h + 32 * c, w2[c]);
-              }
-            ptx::tmem_ld_wait();
-            if (h == 64) release_accumulator();
-            if (add_token >= 0) {
-              const float4* x = reinterpret_cast<const float4*>(p.row_add + int64_t(add_token) * p.d + col0 + h);
-#pragma unroll
-              for (int j = 0; j < 16; ++j)
-                if (h + 4 * j < cols) {
-                  const float4 q = __ldcg(x + j);
-                  uint32_t* o = &w2[j >> 3][4 * (j & 7)];
-                  o[0] = __float_as_uint(__uint_as_float(o[0]) + q.x);
-                  o[1] = __float_as_uint(__uint_as_float(o[1]) + q.y);
-                  o[2] = __float_as_uint(__uint_as_float(o[2]) + q.z);
-                  o[3] = __float_as_uint(__uint_as_float(o[3]) + q.w);
-                }
-            }
-            __syncwarp();
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-              if (h + 32 * c < cols) {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) w2[c][i] = __float_as_uint(__uint_as_float(w2[c][i]) * f);
-                uint32_t pk[16];
-                pack(w2[c], pk);
-                const uint32_t src = stage_box(pk);
-                if (lane == 0) {
-                  if (p.v0 + row0 < p.vocab) ptx::tma_store_2d(&tmap_out2, src, col0 + h + 32 * c, p.v0 + row0);
-                  ptx::tma_store_commit();
-                }
-              }
-          }
+        const int valid = min(kGroupCols, p.vocab - (p.v0 + col0));   // columns of this warp that exist (may be negative)
+        const int tc = y >= 0 ? y - (p.v0 + col0) : -1;               // the target's column here, if in [0, 64)
+        const bool target_here = __any_sync(0xFFFFFFFFu, tc >= 0 && tc < kGroupCols);
+        if (row0 >= p.tokens || (KIND == LSE && valid <= 0)) {
+          release_accumulator();
           continue;
         }
+        if (KIND == LSE) {
+          uint32_t w[2][32];
+          __syncwarp();
+          ptx::tmem_ld_x32(taddr, w[0]);
+          if (valid > 32) ptx::tmem_ld_x32(taddr + 32, w[1]);
+          ptx::tmem_ld_wait();
+          release_accumulator();
+          // exponents are w c - max(w c); with a negative c, or columns that do not exist, the products are made first
+          float c1 = p.c;
+          if (c1 < 0.f || valid < kGroupCols) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+              for (int i = 0; i < 32; ++i) w[c][i] = __float_as_uint(32 * c + i < valid ? __uint_as_float(w[c][i]) * c1 : -INFINITY);
+            c1 = 1.f;
+          }
+          if (target_here) {
+            float tl = 0.f;
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+              for (int i = 0; i < 32; ++i) tl = tc == 32 * c + i ? __uint_as_float(w[c][i]) : tl;
+            if (tc >= 0 && tc < kGroupCols) p.target_logit[row] = tl * c1;
+          }
+          float top[4];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            top[c] = __uint_as_float(w[c >> 1][16 * (c & 1)]);
+#pragma unroll
+            for (int i = 1; i < 16; ++i) top[c] = fmaxf(top[c], __uint_as_float(w[c >> 1][16 * (c & 1) + i]));
+          }
+          const float m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c1;
+          float2 sum[4];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            sum[c] = q8::both(0.f);
+#pragma unroll
+            for (int i = 16 * (c & 1); i < 16 * (c & 1) + 16; i += 2) {   // (an all -inf row gives NaN, as the definition's difference does)
+              const float2 x = q8::fma2(make_float2(__uint_as_float(w[c >> 1][i]), __uint_as_float(w[c >> 1][i + 1])), q8::both(c1), q8::both(-m));
+              sum[c] = q8::add2(sum[c], make_float2(exp2_fast(x.x), exp2_fast(x.y)));
+            }
+          }
+          sum[0] = q8::add2(q8::add2(sum[0], sum[1]), q8::add2(sum[2], sum[3]));
+          if (row < p.tokens) p.part[int64_t(col0 / kGroupCols) * p.tokens + row] = make_float2(m, sum[0].x + sum[0].y);
+        } else {
+          uint32_t pk[32];
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {            // (32 columns at a time: 96 registers do not hold 64 and the packed ones)
+            uint32_t v[32];
+            drain(c, v, c == 1);
+            uint32_t target_bits = 0u;             // the target's element, taken on its own
+            if (target_here) {
+              float l = 0.f;
+#pragma unroll
+              for (int i = 0; i < 32; ++i) l = tc == 32 * c + i ? __uint_as_float(v[i]) : l;
+              if (tc >= 32 * c && tc < 32 * c + 32) {
+                float e = weight * exp2_fast(fmaf(l, p.c, -lse2)) - weight;
+                if (p.vocab == 1 && e == e) e = 0.f;   // one word is certain: the difference would be its rounding only
+                target_bits = pack2(__float_as_uint(e), 0u);
+                p.corr[row] = e - __uint_as_float(target_bits << 16);
+              }
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float2 x = q8::fma2(make_float2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), q8::both(p.c), q8::both(-lse2));
+              const float2 e = q8::mul2(make_float2(exp2_fast(x.x), exp2_fast(x.y)), q8::both(weight));
+              pk[16 * c + i] = pack2(__float_as_uint(e.x), __float_as_uint(e.y));
+            }
+            if (target_here) {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                uint32_t& q = pk[16 * c + i];
+                if (tc == 32 * c + 2 * i) q = (q & 0xFFFF0000u) | target_bits;
+                if (tc == 32 * c + 2 * i + 1) q = (q & 0xFFFFu) | (target_bits << 16);
+              }
+            }
+          }
+          // columns past the vocabulary and rows that are not trained on are zero whatever the logit is
+          if (valid < kGroupCols) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) pk[i] = 2 * i + 1 < valid ? pk[i] : (2 * i < valid ? pk[i] & 0xFFFFu : 0u);
+          }
+          if (y < 0) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) pk[i] = 0u;
+          }
+          store_rows(pk, &tmap_out, col0, row0, false);
+        }
+        continue;
       }
-      release_accumulator();
+      const int cols = min(min(kGroupCols, t.bn - group * kGroupCols), p.d - col0);   // columns that exist (may be negative)
+      const bool rows_exist = t.x ? row0 < p.tokens : p.v0 + row0 < p.vocab;
+      if (cols <= 0 || !rows_exist) {
+        release_accumulator();
+        continue;
+      }
+      uint32_t pk[32];
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        if (32 * c >= cols) break;
+        uint32_t v[32];
+        drain(c, v, c == 1 || cols <= 32);
+        if (t.x) {
+          store_rows(v, &tmap_out, col0 + 32 * c, t.split * p.acc_rows + row0, !p.first_piece);
+          continue;
+        }
+        if (add_token >= 0) {
+          const float4* x = reinterpret_cast<const float4*>(p.row_add + int64_t(add_token) * p.d + col0 + 32 * c);
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (32 * c + 4 * j < cols) {
+              const float4 q = __ldcg(x + j);
+              v[4 * j] = __float_as_uint(__uint_as_float(v[4 * j]) + q.x);
+              v[4 * j + 1] = __float_as_uint(__uint_as_float(v[4 * j + 1]) + q.y);
+              v[4 * j + 2] = __float_as_uint(__uint_as_float(v[4 * j + 2]) + q.z);
+              v[4 * j + 3] = __float_as_uint(__uint_as_float(v[4 * j + 3]) + q.w);
+            }
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float2 e = q8::mul2(make_float2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), q8::both(f));
+          pk[16 * c + i] = pack2(__float_as_uint(e.x), __float_as_uint(e.y));
+        }
+      }
+      if (t.x) continue;
+      // columns that end after 32 inside d belong to two tiles: the store must not reach into the next one
+      if (cols > 32) store_rows(pk, &tmap_out2, col0, p.v0 + row0, false);
+      else store_narrow(pk, &tmap_out3, col0, p.v0 + row0);
     }
     if (FEW && KIND == LSE && few0 < p.few_n) {
       // the 32 lanes' pairs of every token into one: the token's own lane keeps it
       float m = 0.f, s = 0.f;
 #pragma unroll
-      for (int j = 0; j < 32; ++j) {
+      for (int j = 0; j < kFew; ++j) {
         const int k = FEW && KIND == LSE ? j : 0;
         float top = few_m[k];
 #pragma unroll
@@ -668,7 +718,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           s = sum;
         }
       }
-      if (few0 + lane < p.tokens) p.part[int64_t((2 * pair + int(rank)) * 4 + quarter) * p.tokens + few0 + lane] = make_float2(m, s);
+      if (lane < kFew && few0 + lane < p.tokens) p.part[int64_t((2 * pair + int(rank)) * 4 + quarter) * p.tokens + few0 + lane] = make_float2(m, s);
     }
     if (KIND != LSE && lane == 0) ptx::tma_store_wait_read<0>();   // shared memory must outlive the stores' reads
   }
