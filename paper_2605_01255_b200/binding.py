@@ -1,6 +1,7 @@
 """ctypes binding to libacx.so: same names as the C ABI (include/acx.h), argument marshalling only.
 
-torch supplies device memory and streams; every arithmetic step runs in the library's kernels.  If
+torch supplies device memory and streams; every arithmetic step runs in the library's kernels.  The row operators and the
+cross entropy check and convert their arguments in a compiled module (csrc/host_calls.cpp), the linears here.  If
 the library has not been built the import of a symbol raises: there is no fallback of any kind.
 """
 from __future__ import annotations
@@ -342,100 +343,58 @@ def q8_empty(rows: int, cols: int, device="cuda") -> Tuple[torch.Tensor, torch.T
             torch.empty(rows, -(-cols // ACX_Q8_GROUP), dtype=torch.float32, device=device))
 
 
-def _dense(t: Optional[torch.Tensor], shape: Tuple[int, ...], dtype, name: str) -> Optional[int]:
-    """Address of a dense CUDA tensor, checked like _ptr."""
-    if t is None:
-        return None
-    if t.dtype is not dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous CUDA tensor of shape %s and dtype %s (got %s %s on %s)"
-                         % (name, tuple(shape), dtype, tuple(t.shape), t.dtype, t.device))
-    return t.data_ptr()
+_host = None
 
 
-def _strided(t: torch.Tensor, shape: Tuple[int, int], dtype, name: str) -> Tuple[int, int]:
-    """Address and row stride of a CUDA matrix whose rows are dense (a column slice of a wider one is fine)."""
-    if t is None or t.dtype is not dtype or t.shape != shape or not t.is_cuda:
-        raise ValueError("%s must be a CUDA matrix of shape %s and dtype %s" % (name, tuple(shape), dtype))
-    rows, cols = t.stride()
-    if cols != 1:
-        raise ValueError("%s must have unit column stride (got %s)" % (name, (rows, cols)))
-    return t.data_ptr(), (rows if shape[0] > 1 else shape[1])
-
-
-_current_device = getattr(torch._C, "_cuda_getDevice", None)   # without the lazy initialisation: there are CUDA tensors by now
-
-
-def _stream_arg(stream) -> int:
-    if stream is not None:
-        return stream.cuda_stream
-    if _raw_stream is not None and _current_device is not None and torch.cuda.is_initialized():
-        return _raw_stream(_current_device())
-    return torch.cuda.current_stream().cuda_stream
-
-
-def _q8_ptrs(desc: acx_rows_desc, codes, scales, name: str) -> Tuple[Optional[int], Optional[int]]:
-    rows, cols = desc.rows, desc.cols
-    if codes is None and scales is None:
-        return None, None
-    return _dense(codes, (rows, cols), torch.int8, name), _dense(scales, (rows, -(-cols // ACX_Q8_GROUP)), torch.float32, name)
-
-
-def _rows_dtype(desc: acx_rows_desc):
-    return torch.bfloat16 if desc.io_dtype == ACX_BF16 else torch.float32
+def _calls():
+    """The compiled argument checks of the operators below (csrc/host_calls.cpp), bound to the library's entry points: a small call
+    costs its launch and little more.  Raises if the module has not been built."""
+    global _host
+    if _host is None:
+        L = lib()
+        try:
+            from . import _acx_host
+        except ImportError as e:
+            raise RuntimeError("_acx_host.so is not built for this torch; run `python -m paper_2605_01255_b200.build`") from e
+        _acx_host.bind(tuple(ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in (
+            "acx_q8_store", "acx_q8_load", "acx_swiglu_fwd", "acx_swiglu_bwd", "acx_norm_join_fwd", "acx_norm_join_bwd",
+            "acx_linear_ce_fwd", "acx_linear_ce_bwd")))
+        _host = _acx_host
+    return _host
 
 
 def acx_q8_store(desc: acx_rows_desc, X, codes, scales, stream=None) -> None:
     """Codes and scales of X (rows x cols; its rows may be strided)."""
-    xp, ldx = _strided(X, (desc.rows, desc.cols), _rows_dtype(desc), "X")
-    _check(lib().acx_q8_store(desc, xp, ldx, *_q8_ptrs(desc, codes, scales, "checkpoint of X"), _stream_arg(stream)), "acx_q8_store")
+    _check((_host or _calls()).q8_store(desc, X, codes, scales, stream), "acx_q8_store")
 
 
 def acx_q8_load(desc: acx_rows_desc, codes, scales, X, stream=None) -> None:
     """The values of an 8-bit checkpoint into X (rows x cols; its rows may be strided)."""
-    xp, ldx = _strided(X, (desc.rows, desc.cols), _rows_dtype(desc), "X")
-    _check(lib().acx_q8_load(desc, *_q8_ptrs(desc, codes, scales, "8-bit X"), xp, ldx, _stream_arg(stream)), "acx_q8_load")
+    _check((_host or _calls()).q8_load(desc, codes, scales, X, stream), "acx_q8_load")
 
 
 def acx_swiglu_fwd(desc: acx_rows_desc, G, U, H, Gq=None, Gs=None, Uq=None, Us=None, stream=None) -> None:
     """H = silu(G) * U; with Gq, Gs, Uq, Us also the 8-bit checkpoints of G and U."""
-    shape, dt = (desc.rows, desc.cols), _rows_dtype(desc)
-    gp, ldg = _strided(G, shape, dt, "G")
-    up, ldu = _strided(U, shape, dt, "U")
-    _check(lib().acx_swiglu_fwd(desc, gp, ldg, up, ldu, _dense(H, shape, dt, "H"), *_q8_ptrs(desc, Gq, Gs, "checkpoint of G"), *_q8_ptrs(desc, Uq, Us, "checkpoint of U"),
-                                _stream_arg(stream)), "acx_swiglu_fwd")
+    _check((_host or _calls()).swiglu_fwd(desc, G, U, H, Gq, Gs, Uq, Us, stream), "acx_swiglu_fwd")
 
 
 def acx_swiglu_bwd(desc: acx_rows_desc, dH, Gq, Gs, Uq, Us, dG, dU, stream=None) -> None:
     """dG, dU of H = silu(G) * U at the checkpointed G and U."""
-    shape, dt = (desc.rows, desc.cols), _rows_dtype(desc)
-    gp, ldg = _strided(dG, shape, dt, "dG")
-    up, ldu = _strided(dU, shape, dt, "dU")
-    _check(lib().acx_swiglu_bwd(desc, _dense(dH, shape, dt, "dH"), *_q8_ptrs(desc, Gq, Gs, "checkpoint of G"), *_q8_ptrs(desc, Uq, Us, "checkpoint of U"), gp, ldg, up, ldu,
-                                _stream_arg(stream)), "acx_swiglu_bwd")
+    _check((_host or _calls()).swiglu_bwd(desc, dH, Gq, Gs, Uq, Us, dG, dU, stream), "acx_swiglu_bwd")
 
 
 def acx_norm_join_fwd(desc: acx_rows_desc, h, b, w_post, gate, w_pre, h_out, y, Hq=None, Hs=None, Bq=None, Bs=None, rstd_post=None,
                       rstd_pre=None, *, eps: float = 1e-5, alpha: float = 1.0, stream=None) -> None:
     """h_out = h + alpha * gate * RMSNorm(b) * w_post and y = RMSNorm(h_out) * w_pre; b, w_post, gate may be None (see acx.h)."""
-    shape, vec, row, dt = (desc.rows, desc.cols), (desc.cols,), (desc.rows,), _rows_dtype(desc)
-    _check(lib().acx_norm_join_fwd(desc, _dense(h, shape, dt, "h"), _dense(b, shape, dt, "b"), _dense(w_post, vec, dt, "w_post"),
-                                   _dense(gate, vec, dt, "gate"), _dense(w_pre, vec, dt, "w_pre"), _dense(h_out, shape, dt, "h_out"),
-                                   _dense(y, shape, dt, "y"), *_q8_ptrs(desc, Hq, Hs, "checkpoint of h"), *_q8_ptrs(desc, Bq, Bs, "checkpoint of b"),
-                                   _dense(rstd_post, row, torch.float32, "rstd_post"), _dense(rstd_pre, row, torch.float32, "rstd_pre"),
-                                   eps, alpha, _stream_arg(stream)), "acx_norm_join_fwd")
+    _check((_host or _calls()).norm_join_fwd(desc, h, b, w_post, gate, w_pre, h_out, y, Hq, Hs, Bq, Bs, rstd_post, rstd_pre, eps, alpha,
+                                             stream), "acx_norm_join_fwd")
 
 
 def acx_norm_join_bwd(desc: acx_rows_desc, dy, dh_next, w_post, gate, w_pre, Hq, Hs, Bq, Bs, rstd_post, rstd_pre, dh, db, dw_post, dgate,
                       dw_pre, *, alpha: float = 1.0, ws=None, stream=None) -> None:
     """Gradients of acx_norm_join_fwd at its checkpoints; ws: alloc_rows_workspace(desc, ACX_OP_NORM_BWD)."""
-    shape, vec, row, dt, f32 = (desc.rows, desc.cols), (desc.cols,), (desc.rows,), _rows_dtype(desc), torch.float32
-    wp, wn = _ws(ws)
-    _check(lib().acx_norm_join_bwd(desc, _dense(dy, shape, dt, "dy"), _dense(dh_next, shape, dt, "dh_next"), _dense(w_post, vec, dt, "w_post"),
-                                   _dense(gate, vec, dt, "gate"), _dense(w_pre, vec, dt, "w_pre"), *_q8_ptrs(desc, Hq, Hs, "checkpoint of h"),
-                                   *_q8_ptrs(desc, Bq, Bs, "checkpoint of b"), _dense(rstd_post, row, f32, "rstd_post"),
-                                   _dense(rstd_pre, row, f32, "rstd_pre"), _dense(dh, shape, dt, "dh"), _dense(db, shape, dt, "db"),
-                                   _dense(dw_post, vec, f32, "dw_post"), _dense(dgate, vec, f32, "dgate"), _dense(dw_pre, vec, f32, "dw_pre"),
-                                   alpha, wp, wn, _stream_arg(stream)), "acx_norm_join_bwd")
+    _check((_host or _calls()).norm_join_bwd(desc, dy, dh_next, w_post, gate, w_pre, Hq, Hs, Bq, Bs, rstd_post, rstd_pre, dh, db, dw_post,
+                                             dgate, dw_pre, alpha, ws, stream), "acx_norm_join_bwd")
 
 
 # ---- softmax cross entropy over a vocabulary ----------------------------------------------------------------------------
@@ -455,22 +414,11 @@ def alloc_ce_workspace(desc: acx_ce_desc, op: int, device="cuda") -> Optional[to
 def acx_linear_ce_fwd(desc: acx_ce_desc, X, W, targets, loss, lse, total=None, weight=None, ws=None, stream=None) -> None:
     """Per-token cross entropy of logit_scale * X W^T at `targets` (int64; outside [0, vocab): not trained on), its log-sum-exp,
     and total = (sum of weight * loss, sum of weight); ws: alloc_ce_workspace(desc, ACX_OP_CE_FWD)."""
-    row, f32 = (desc.tokens,), torch.float32
-    wp, wn = _ws(ws)
-    _check(lib().acx_linear_ce_fwd(desc, _dense(X, (desc.tokens, desc.d), torch.bfloat16, "X"), _dense(W, (desc.vocab, desc.d), torch.bfloat16, "W"),
-                                   _dense(targets, row, torch.int64, "targets"), _dense(weight, row, f32, "weight"),
-                                   _dense(loss, row, f32, "loss"), _dense(lse, row, f32, "lse"), _dense(total, (2,), f32, "total"), wp, wn,
-                                   _stream_arg(stream)), "acx_linear_ce_fwd")
+    _check((_host or _calls()).linear_ce_fwd(desc, X, W, targets, weight, loss, lse, total, ws, stream), "acx_linear_ce_fwd")
 
 
 def acx_linear_ce_bwd(desc: acx_ce_desc, X, W, targets, lse, dX, dW, *, weight=None, denom=None, scale: float = 1.0, ws=None,
                       stream=None) -> None:
     """Gradients of scale * sum(weight * loss) / denom (denom: one fp32 number on the device, such as total[1:]); dX or dW may be
     None; ws: alloc_ce_workspace(desc, ACX_OP_CE_BWD)."""
-    row, f32 = (desc.tokens,), torch.float32
-    wp, wn = _ws(ws)
-    _check(lib().acx_linear_ce_bwd(desc, _dense(X, (desc.tokens, desc.d), torch.bfloat16, "X"), _dense(W, (desc.vocab, desc.d), torch.bfloat16, "W"),
-                                   _dense(targets, row, torch.int64, "targets"), _dense(weight, row, f32, "weight"),
-                                   _dense(lse, row, f32, "lse"), _dense(denom, (1,), f32, "denom"), scale,
-                                   _dense(dX, (desc.tokens, desc.d), torch.bfloat16, "dX"), _dense(dW, (desc.vocab, desc.d), torch.bfloat16, "dW"),
-                                   wp, wn, _stream_arg(stream)), "acx_linear_ce_bwd")
+    _check((_host or _calls()).linear_ce_bwd(desc, X, W, targets, weight, lse, denom, scale, dX, dW, ws, stream), "acx_linear_ce_bwd")

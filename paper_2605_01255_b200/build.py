@@ -1,4 +1,4 @@
-"""Builds libacx.so (sm_100a) in-tree with nvcc.  `python -m paper_2605_01255_b200.build [--force]`."""
+"""Builds libacx.so (sm_100a) in-tree with nvcc, and the Python side's argument checks with g++.  `python -m paper_2605_01255_b200.build [--force]`."""
 from __future__ import annotations
 
 import concurrent.futures
@@ -6,11 +6,14 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "libacx.so")
+HOST_SRC = os.path.join(CSRC, "host_calls.cpp")
+HOST_PATH = os.path.join(HERE, "_acx_host.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -42,8 +45,24 @@ def _stale(target: str, deps) -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def _host_job(force: bool):
+    """The command that builds the host module against the installed torch, or None where it is up to date."""
+    import torch
+
+    if not force and not _stale(HOST_PATH, [HOST_SRC, _headers()[-1], torch.version.__file__]):
+        return None
+    home = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(_nvcc()))
+    # g++ of the path, as nvcc takes it: torch and this module have to share one libstdc++
+    return [shutil.which("g++") or os.environ.get("CXX") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+            "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+            *("-I" + d for d in (sysconfig.get_paths()["include"], os.path.join(home, "include"),
+                                 os.path.join(home, "include", "torch", "csrc", "api", "include"), os.path.join(cuda, "include"))),
+            HOST_SRC, "-o", HOST_PATH, "-L" + os.path.join(home, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+
+
 def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
-    """Compile every .cu under csrc/ and link libacx.so next to this file.  Returns the library path."""
+    """Compile every .cu under csrc/, link libacx.so next to this file and build the host module.  Returns the library path."""
     nvcc = _nvcc()
     os.makedirs(OBJ_DIR, exist_ok=True)
     headers = _headers()
@@ -54,18 +73,19 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
         objs.append(obj)
         if force or _stale(obj, [src] + headers):
             jobs.append([nvcc, *NVCC_FLAGS, *extra_flags, "-c", src, "-o", obj])
+    host = _host_job(force)
 
     def run(cmd):
         if verbose:
             print(" ".join(cmd), flush=True)
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
-            raise RuntimeError("nvcc failed:\n%s\n%s\n%s" % (" ".join(cmd), r.stdout, r.stderr))
+            raise RuntimeError("build failed:\n%s\n%s\n%s" % (" ".join(cmd), r.stdout, r.stderr))
         if verbose and (r.stdout or r.stderr):
             print(r.stdout, r.stderr, flush=True)
 
-    with concurrent.futures.ThreadPoolExecutor(max_workers=max(1, min(8, len(jobs)))) as ex:
-        list(ex.map(run, jobs))
+    with concurrent.futures.ThreadPoolExecutor(max_workers=max(1, min(8, len(jobs) + 1))) as ex:
+        list(ex.map(run, jobs + ([host] if host else [])))
     if jobs or force or _stale(LIB_PATH, objs):
         run([nvcc, "-shared", "-o", LIB_PATH, *objs])
     return LIB_PATH
