@@ -368,3 +368,42 @@ def test_rows_on_two_streams_and_in_a_graph():
     torch.cuda.synchronize()
     for o in outs + [graphed]:
         assert torch.equal(o["H"], ref["H"]) and torch.equal(o["dGU"], ref["dGU"])
+
+
+@pytest.mark.parametrize("rows,cols", [(3, 8), (37, 264), (9, 2056), (5, 3000)])
+def test_fp32_matrices_that_start_between_two_32_byte_boundaries(rows, cols):
+    """The same bits wherever the matrices start: 16-byte alignment is all that is asked for, 32 bytes take the wide accesses."""
+    n, vec, one = rows * cols, (cols,), torch.float32
+
+    def at(offset, *shape):     # a dense fp32 matrix `offset` elements behind a 32-byte boundary, with a guard behind it
+        flat = torch.full((offset + int(np.prod(shape)) + 8,), NAN, dtype=one, device="cuda")
+        assert flat.data_ptr() % 32 == 0
+        return flat, flat[offset:offset + int(np.prod(shape))].view(shape)
+
+    d = B.make_rows_desc(rows, cols, "f32")
+    src = [to_device(act(rows, cols, 11 + k, "f32"), "f32") for k in range(4)]
+    w = [to_device(1 + I.gaussian((1, cols), 20 + k, 0.2), "f32")[0] for k in range(3)]
+    ws = B.alloc_rows_workspace(d, B.ACX_OP_NORM_BWD)
+    results = []
+    for offset in (0, 4):
+        ins = []
+        for t in src + w:
+            v = at(offset, *t.shape)[1]
+            v.copy_(t)
+            ins.append(v)
+        x, b, dy, dn, w_post, gate, w_pre = ins
+        flats, outs = zip(*[at(offset, rows, cols) for _ in range(8)])
+        H, dG, dU, h_out, y, dh, db, back = outs
+        q = [q8_new(rows, cols) for _ in range(4)]
+        r = [new(rows, dt=one) for _ in range(2)]
+        g = [new(*vec, dt=one) for _ in range(3)]
+        B.acx_swiglu_fwd(d, x, b, H, *q[0], *q[1])
+        B.acx_swiglu_bwd(d, dy, *q[0], *q[1], dG, dU)
+        B.acx_norm_join_fwd(d, x, b, w_post, gate, w_pre, h_out, y, *q[2], *q[3], *r, alpha=0.5)
+        B.acx_norm_join_bwd(d, dy, dn, w_post, gate, w_pre, *q[2], *q[3], *r, dh, db, *g, alpha=0.5, ws=ws)
+        B.acx_q8_load(d, *q[2], back)
+        for flat in flats:
+            assert torch.isnan(flat[:offset]).all() and torch.isnan(flat[offset + n:]).all()
+        results.append([t.clone() for t in (*outs, *g, *r, *(t for pair in q for t in pair))])
+    for a, c in zip(*results):
+        assert torch.equal(a, c) and not torch.isnan(a.float()).any()
