@@ -8,6 +8,7 @@
 //     dh = dt,   db = r_b (k dt - bhat m2),         m2 = mean(k dt bhat)
 //     dw_pre = sum_t dy that,   dw_post = alpha gate c,   dgate = alpha w_post c,   c = sum_t dt bhat.
 #include <algorithm>
+#include <climits>
 
 #include "acx_internal.h"
 #include "acx_q8.cuh"
@@ -66,26 +67,49 @@ __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_
 template <int N>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// A thread's slots in shared memory for vectors on their way: MAXT slots of 16 bytes per part of a vector of T (one part of
-// bf16, two of fp32), so that a warp's accesses are contiguous.  A thread only ever touches its own.
+// Slots in shared memory for the vectors of a block's threads on their way.  `src` is where the thread's own vector is, `left`
+// how many columns of the row there are from it on.
+//
+// bf16: MAXT slots of 16 bytes; a thread only ever touches its own.
+// fp32: a vector is two pieces of 16 bytes.  The lanes of a warp copy its pieces in the order they have in memory, which is
+// also theirs in the slots (each lane its own two: 32 passes of the load unit per copy instruction instead of 16: forward and
+// backward of 8192 x 2048 took 66 and 72 us, 57 and 58 this way).
+// So a warp's lanes have to meet between the end of the copies and the reads, and before the next copies.  Four lanes of
+// eight read the second halves first: eight consecutive lanes then cover all banks.
 template <typename T, int MAXT>
-struct Slots {
-  static constexpr int kParts = int(sizeof(T)) / 2;
-  static constexpr int kBytes = kParts * MAXT * 16;
-  static __device__ __forceinline__ void fetch(uint32_t smem, const T* src) {
-#pragma unroll
-    for (int q = 0; q < kParts; ++q)
-      copy_async(smem + q * MAXT * 16 + threadIdx.x * 16, reinterpret_cast<const uint8_t*>(src) + 16 * q, 16);
+struct Slots;
+template <int MAXT>
+struct Slots<__nv_bfloat16, MAXT> {
+  static constexpr int kBytes = MAXT * 16;
+  static __device__ __forceinline__ void meet() {}
+  static __device__ __forceinline__ void fetch(uint32_t smem, const __nv_bfloat16* src, int left) {
+    if (left > 0) copy_async(smem + threadIdx.x * 16, src, 16);
   }
-  static __device__ __forceinline__ Raw<__nv_bfloat16> take(const uint8_t* smem, __nv_bfloat16) {
+  static __device__ __forceinline__ Raw<__nv_bfloat16> take(const uint8_t* smem) {
     Raw<__nv_bfloat16> r;
     r.u = *reinterpret_cast<const uint4*>(smem + threadIdx.x * 16);
     return r;
   }
-  static __device__ __forceinline__ Raw<float> take(const uint8_t* smem, float) {
+};
+template <int MAXT>
+struct Slots<float, MAXT> {
+  static constexpr int kBytes = MAXT * 32;
+  static __device__ __forceinline__ void meet() { __syncwarp(); }
+  static __device__ __forceinline__ void fetch(uint32_t smem, const float* src, int left) {
+    const int lane = int(threadIdx.x & 31);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int ahead = 128 * q - 4 * lane;   // this lane's piece, in columns from its own vector
+      if (ahead < left) copy_async(smem + (threadIdx.x & ~31u) * 32 + q * 512 + lane * 16, src + ahead, 16);
+    }
+  }
+  static __device__ __forceinline__ Raw<float> take(const uint8_t* smem) {
+    const bool swap = threadIdx.x & 4;
+    const uint8_t* o = smem + threadIdx.x * 32;
+    const float4 x = *reinterpret_cast<const float4*>(o + (swap ? 16 : 0)), y = *reinterpret_cast<const float4*>(o + (swap ? 0 : 16));
     Raw<float> r;
-    r.a = *reinterpret_cast<const float4*>(smem + threadIdx.x * 16);
-    r.b = *reinterpret_cast<const float4*>(smem + MAXT * 16 + threadIdx.x * 16);
+    r.a = swap ? y : x;
+    r.b = swap ? x : y;
     return r;
   }
 };
@@ -139,11 +163,11 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_join_fwd_kernel(const FwdArgs
   auto fetch = [&](int64_t row, int stage) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      if (!live(i)) continue;
       const int64_t at = row * a.cols + col_of(i);
+      const int left = FULL ? INT_MAX : a.cols - col_of(i);
       const uint32_t o = ring0 + (stage * NV + i) * kVecSlot;
-      S::fetch(o, static_cast<const T*>(a.h) + at);
-      if (JOIN) S::fetch(o + S::kBytes, static_cast<const T*>(a.b) + at);
+      S::fetch(o, static_cast<const T*>(a.h) + at, left);
+      if (JOIN) S::fetch(o + S::kBytes, static_cast<const T*>(a.b) + at, left);
     }
   };
   const int64_t step = gridDim.x;
@@ -164,6 +188,7 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_join_fwd_kernel(const FwdArgs
     const int64_t at = row * a.cols;
     Raw<T> h[NV], b[JOIN ? NV : 1];
     copies_wait<(DEPTH > 0 ? DEPTH - 1 : 0)>();
+    S::meet();
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       h[i].zero();
@@ -171,8 +196,8 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_join_fwd_kernel(const FwdArgs
       if (!live(i)) continue;
       if (DEPTH > 0) {
         const uint8_t* o = ring + (stage * NV + i) * kVecSlot;
-        h[i] = S::take(o, T());
-        if (JOIN) b[JOIN ? i : 0] = S::take(o + S::kBytes, T());
+        h[i] = S::take(o);
+        if (JOIN) b[JOIN ? i : 0] = S::take(o + S::kBytes);
       } else {
         h[i].load(static_cast<const T*>(a.h) + at + col_of(i));
         if (JOIN) b[JOIN ? i : 0].load(static_cast<const T*>(a.b) + at + col_of(i));
@@ -232,6 +257,7 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_join_fwd_kernel(const FwdArgs
       for (int e = 0; e < 4; ++e) s = fma2(t[i][e], t[i][e], s);
     const float r_t = rsqrtf(block_sum(s.x + s.y, red[turn][1]) * inv_n + a.eps);
     if (DEPTH > 0) {   // this stage's values are in registers: its slots take the row DEPTH turns on
+      S::meet();
       if (row + DEPTH * step < a.rows) fetch(row + DEPTH * step, stage);
       copies_commit();
       if (++stage == DEPTH) stage = 0;
@@ -280,11 +306,12 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_join_bwd_kernel(const BwdArgs
   auto fetch = [&](int64_t row, int stage) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      if (!live(i)) continue;
       const int64_t at = row * a.cols + col_of(i);
+      const int left = FULL ? INT_MAX : a.cols - col_of(i);
       const uint32_t o = ring0 + (stage * NV + i) * kVecSlot;
-      S::fetch(o, static_cast<const T*>(a.dy) + at);
-      if (a.dh_next) S::fetch(o + S::kBytes, static_cast<const T*>(a.dh_next) + at);
+      S::fetch(o, static_cast<const T*>(a.dy) + at, left);
+      if (a.dh_next) S::fetch(o + S::kBytes, static_cast<const T*>(a.dh_next) + at, left);
+      if (!live(i)) continue;
       copy_async(o + 2 * S::kBytes + threadIdx.x * 8, a.Hq + at, 8);
       if (JOIN) copy_async(o + 2 * S::kBytes + kCodes + threadIdx.x * 8, a.Bq + at, 8);
     }
@@ -332,6 +359,7 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_join_bwd_kernel(const BwdArgs
     float2 that[NV][4], av[NV][4], bhat[JOIN ? NV : 1][4];
     float2 s0 = both(0.f), s1 = both(0.f), s2 = both(0.f);
     copies_wait<(DEPTH > 0 ? DEPTH - 1 : 0)>();
+    S::meet();
     const RowScales now = next;
     const float rt = now.r_t, rb = now.r_b;
 #pragma unroll
@@ -344,8 +372,8 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_join_bwd_kernel(const BwdArgs
       for (int e = 0; e < 4; ++e) av[i][e] = both(0.f);
       if (DEPTH > 0) {
         const uint8_t* o = ring + (stage * NV + i) * kVecSlot;
-        S::take(o, T()).get(dy);
-        if (a.dh_next) S::take(o + S::kBytes, T()).get(av[i]);
+        S::take(o).get(dy);
+        if (a.dh_next) S::take(o + S::kBytes).get(av[i]);
         hq = *reinterpret_cast<const uint2*>(o + 2 * S::kBytes + threadIdx.x * 8);
         if (JOIN) bq = *reinterpret_cast<const uint2*>(o + 2 * S::kBytes + kCodes + threadIdx.x * 8);
       } else {
@@ -378,6 +406,7 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_join_bwd_kernel(const BwdArgs
     scales(row + step);
     const float3 sums = block_sum3(s0.x + s0.y, s1.x + s1.y, s2.x + s2.y, red[turn]);
     if (DEPTH > 0) {   // this stage's values are in registers: its slots take the row DEPTH turns on
+      S::meet();
       if (row + DEPTH * step < a.rows) fetch(row + DEPTH * step, stage);
       copies_commit();
       if (++stage == DEPTH) stage = 0;
