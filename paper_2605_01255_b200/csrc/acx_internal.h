@@ -45,22 +45,28 @@ inline cudaError_t launched() {
 }
 
 // Launches with programmatic stream serialization: the kernel may start before the launch before it has finished, and waits
-// for that itself (wait_for_launch_before, first thing or as soon as it needs to).
+// for that itself (wait_for_launch_before, first thing or as soon as it needs to).  In clusters of `cluster` blocks along x.
 template <typename... K, typename... A>
-cudaError_t launch_lined_up(void (*kernel)(K...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, const A&... args) {
+cudaError_t launch_lined_up_in_clusters(unsigned cluster, void (*kernel)(K...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, const A&... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = block;
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim = {cluster, 1, 1};
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
   kernel_launch_counter().fetch_add(1, std::memory_order_relaxed);
   return e;
+}
+template <typename... K, typename... A>
+cudaError_t launch_lined_up(void (*kernel)(K...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, const A&... args) {
+  return launch_lined_up_in_clusters(1, kernel, grid, block, smem, st, args...);
 }
 #ifdef __CUDACC__
 __device__ __forceinline__ void wait_for_launch_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }

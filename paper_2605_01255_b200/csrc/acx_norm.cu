@@ -8,11 +8,13 @@
 //     dh = dt,   db = r_b (k dt - bhat m2),         m2 = mean(k dt bhat)
 //     dw_pre = sum_t dy that,   dw_post = alpha gate c,   dgate = alpha w_post c,   c = sum_t dt bhat.
 #include <algorithm>
+#include <atomic>
 #include <climits>
 
 #include "acx_internal.h"
 #include "acx_q8.cuh"
 #include "acx_tmap.h"
+#include "acx_umma.cuh"
 
 namespace acx {
 namespace {
@@ -58,6 +60,52 @@ __device__ __forceinline__ float block_sum(float s, float* red) {
   }
   return s;
 }
+
+// Wide rows: a row is shared by the blocks of a cluster, each with its own columns.  A block sends its sums to all of them and
+// adds what it gets in the order of the ranks.  Stores that count on the receiver's barrier order nothing else: a cluster
+// barrier would first wait for all that the block has written to global memory (2000 x 16384 forward: 129 us
+// with one, 87 this way).
+// SUMS per row, each with slots for two rows in turn, since a peer may be one row ahead.
+template <int SUMS>
+struct Peers {
+  float4 slot[2][SUMS][8];
+  uint64_t bar[2][SUMS];
+  int gave_up;
+
+  __device__ __forceinline__ void start() {
+    if (threadIdx.x == 0) {
+      for (int k = 0; k < 2 * SUMS; ++k) ptx::mbar_init(ptx::smem_u32(&bar[0][0] + k), 1);
+      gave_up = 0;
+      ptx::fence_barrier_init();
+    }
+    ptx::cluster_sync_all();
+  }
+  // Ends when no block of the cluster sends any more.
+  __device__ __forceinline__ void end() { ptx::cluster_sync_all(); }
+  __device__ __forceinline__ float3 sum(float3 s, int turn, int which, uint32_t parity, uint32_t ranks, int* status) {
+    const uint32_t mine = ptx::smem_u32(&bar[turn][which]);
+    if (threadIdx.x == 0) ptx::mbar_arrive_expect_tx(mine, ranks * 16);
+    if (threadIdx.x < ranks)
+      asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(
+                       ptx::map_to_rank(ptx::smem_u32(&slot[turn][which][ptx::cluster_ctarank()]), threadIdx.x)),
+                   "f"(s.x), "f"(s.y), "f"(s.z), "f"(0.f), "r"(ptx::map_to_rank(mine, threadIdx.x))
+                   : "memory");
+    if (!ptx::mbar_wait_cluster(mine, parity, &gave_up)) {
+      *static_cast<volatile int*>(&gave_up) = 1;
+      atomicExch(status, kDevTimeout);
+    }
+    float3 r = make_float3(0.f, 0.f, 0.f);
+    for (uint32_t k = 0; k < ranks; ++k) {
+      const float4 q = slot[turn][which][k];
+      r.x += q.x;
+      r.y += q.y;
+      r.z += q.z;
+    }
+    return r;
+  }
+};
+template <>
+struct Peers<0> {};
 
 __device__ __forceinline__ void copy_async(uint32_t dst, const void* src, int bytes) {   // 8 or 16 bytes, both aligned to them
   if (bytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -137,20 +185,23 @@ struct FwdArgs {
   void *h_out, *y;
   int8_t *Hq, *Bq;
   float *Hs, *Bs, *rstd_post, *rstd_pre;
-  int64_t rows;
+  unsigned rows;   // below 2^31: numbers of rows, also some steps past the last, fit 32 bits
   int cols;
   float eps, alpha;
+  int cluster;   // blocks that share a row (1 unless WIDE)
+  int* status;
 };
 
 // Persistent: a block walks the rows blockIdx.x, + gridDim.x, ...; a thread holds NV vectors of 8 columns, threadIdx.x +
 // i * blockDim.x (16 consecutive lanes hold a group of an 8-bit checkpoint), and keeps their weights in registers as
 // binary32.  (One block per row, the weights read and unpacked again for each, was bound by instructions: 431 per vector
-// and 131 us at 16384 x 3072.)  With DEPTH > 0 a thread copies its vectors of the next DEPTH rows into shared memory
+// and 131 us at 16384 x 3072.)  The vectors of the next DEPTH rows are copied into shared memory
 // asynchronously, into its own slots, so no barrier guards them.  FULL: every vector of every thread is inside the row.
-template <typename T, int NV, int MAXT, int MINB, int DEPTH, bool JOIN, bool KEEP, bool FULL>
+template <typename T, int NV, int MAXT, int MINB, int DEPTH, bool JOIN, bool KEEP, bool FULL, bool WIDE>
 __global__ void __launch_bounds__(MAXT, MINB) norm_join_fwd_kernel(const FwdArgs a) {
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ float red[2][2][32];
+  __shared__ Peers<WIDE ? 2 : 0> peers;
   wait_for_launch_before();
   let_next_launch_start();
   using S = Slots<T, MAXT>;
@@ -158,22 +209,24 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_join_fwd_kernel(const FwdArgs
   const int ng = (a.cols + kGroup - 1) / kGroup, lane16 = threadIdx.x & 15;
   const float inv_n = 1.f / float(a.cols);
   const uint32_t ring0 = static_cast<uint32_t>(__cvta_generic_to_shared(ring));
-  auto col_of = [&](int i) { return (int(threadIdx.x) + i * int(blockDim.x)) * kVec; };
+  const int rank = WIDE ? int(blockIdx.x) % a.cluster : 0, first = rank * NV * int(blockDim.x);   // of this block's vectors
+  const unsigned row0 = WIDE ? blockIdx.x / unsigned(a.cluster) : blockIdx.x;
+  auto col_of = [&](int i) { return (first + int(threadIdx.x) + i * int(blockDim.x)) * kVec; };
   auto live = [&](int i) { return FULL || col_of(i) < a.cols; };
-  auto fetch = [&](int64_t row, int stage) {
+  auto fetch = [&](unsigned row, int stage) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int64_t at = row * a.cols + col_of(i);
+      const int64_t at = int64_t(row) * a.cols + col_of(i);
       const int left = FULL ? INT_MAX : a.cols - col_of(i);
       const uint32_t o = ring0 + (stage * NV + i) * kVecSlot;
       S::fetch(o, static_cast<const T*>(a.h) + at, left);
       if (JOIN) S::fetch(o + S::kBytes, static_cast<const T*>(a.b) + at, left);
     }
   };
-  const int64_t step = gridDim.x;
+  const unsigned step = WIDE ? gridDim.x / unsigned(a.cluster) : gridDim.x;
 #pragma unroll
   for (int s = 0; s < DEPTH; ++s) {
-    if (blockIdx.x + s * step < a.rows) fetch(blockIdx.x + s * step, s);
+    if (row0 + s * step < a.rows) fetch(row0 + s * step, s);
     copies_commit();
   }
   float2 k[JOIN ? NV : 1][4], wp[NV][4];
@@ -184,24 +237,21 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_join_fwd_kernel(const FwdArgs
     load8(static_cast<const T*>(a.w_pre) + col_of(i), wp[i]);
   }
   int turn = 0, stage = 0;
-  for (int64_t row = blockIdx.x; row < a.rows; row += step, turn ^= 1) {
-    const int64_t at = row * a.cols;
+  uint32_t parity = 0;   // of the barriers of this turn
+  if constexpr (WIDE) peers.start();
+  for (unsigned row = row0; row < a.rows; row += step, parity ^= turn, turn ^= 1) {
+    const int64_t at = int64_t(row) * a.cols;
     Raw<T> h[NV], b[JOIN ? NV : 1];
-    copies_wait<(DEPTH > 0 ? DEPTH - 1 : 0)>();
+    copies_wait<DEPTH - 1>();
     S::meet();
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       h[i].zero();
       if (JOIN) b[JOIN ? i : 0].zero();
       if (!live(i)) continue;
-      if (DEPTH > 0) {
-        const uint8_t* o = ring + (stage * NV + i) * kVecSlot;
-        h[i] = S::take(o);
-        if (JOIN) b[JOIN ? i : 0] = S::take(o + S::kBytes);
-      } else {
-        h[i].load(static_cast<const T*>(a.h) + at + col_of(i));
-        if (JOIN) b[JOIN ? i : 0].load(static_cast<const T*>(a.b) + at + col_of(i));
-      }
+      const uint8_t* o = ring + (stage * NV + i) * kVecSlot;
+      h[i] = S::take(o);
+      if (JOIN) b[JOIN ? i : 0] = S::take(o + S::kBytes);
     }
     float2 t[NV][4], bf[JOIN ? NV : 1][4];
 #pragma unroll
@@ -225,7 +275,7 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_join_fwd_kernel(const FwdArgs
         const float inv_b = JOIN ? __shfl_sync(0xFFFFFFFFu, g.inv, threadIdx.x | 1) : 0.f;
         const int c = col_of(i);
         if (lane16 < (JOIN ? 2 : 1) && (FULL || c - lane16 * kVec < a.cols))   // the group exists, whether or not this lane's vector does
-          (JOIN && lane16 == 1 ? a.Bs : a.Hs)[row * ng + c / kGroup] = g.scale;
+          (JOIN && lane16 == 1 ? a.Bs : a.Hs)[int64_t(row) * ng + c / kGroup] = g.scale;
         if (!live(i)) continue;
         *reinterpret_cast<uint2*>(a.Hq + at + c) = encode8(t[i], inv_h);
         if (JOIN) *reinterpret_cast<uint2*>(a.Bq + at + c) = encode8(bf[JOIN ? i : 0], inv_b);
@@ -239,8 +289,10 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_join_fwd_kernel(const FwdArgs
         for (int i = 0; i < NV; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) s = fma2(bf[JOIN ? i : 0][e], bf[JOIN ? i : 0][e], s);
-        r_b = rsqrtf(block_sum(s.x + s.y, red[turn][0]) * inv_n + a.eps);
-        if (KEEP && threadIdx.x == 0) a.rstd_post[row] = r_b;
+        float sum = block_sum(s.x + s.y, red[turn][0]);
+        if constexpr (WIDE) sum = peers.sum(make_float3(sum, 0.f, 0.f), turn, 0, parity, a.cluster, a.status).x;
+        r_b = rsqrtf(sum * inv_n + a.eps);
+        if (KEEP && threadIdx.x == 0 && rank == 0) a.rstd_post[row] = r_b;
       }
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
@@ -255,14 +307,15 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_join_fwd_kernel(const FwdArgs
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) s = fma2(t[i][e], t[i][e], s);
-    const float r_t = rsqrtf(block_sum(s.x + s.y, red[turn][1]) * inv_n + a.eps);
-    if (DEPTH > 0) {   // this stage's values are in registers: its slots take the row DEPTH turns on
-      S::meet();
-      if (row + DEPTH * step < a.rows) fetch(row + DEPTH * step, stage);
-      copies_commit();
-      if (++stage == DEPTH) stage = 0;
-    }
-    if (KEEP && threadIdx.x == 0) a.rstd_pre[row] = r_t;
+    float sum = block_sum(s.x + s.y, red[turn][1]);
+    if constexpr (WIDE) sum = peers.sum(make_float3(sum, 0.f, 0.f), turn, 1, parity, a.cluster, a.status).x;
+    const float r_t = rsqrtf(sum * inv_n + a.eps);
+    // this stage's values are in registers: its slots take the row DEPTH turns on
+    S::meet();
+    if (row + DEPTH * step < a.rows) fetch(row + DEPTH * step, stage);
+    copies_commit();
+    if (++stage == DEPTH) stage = 0;
+    if (KEEP && threadIdx.x == 0 && rank == 0) a.rstd_pre[row] = r_t;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       if (!live(i)) continue;
@@ -272,6 +325,7 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_join_fwd_kernel(const FwdArgs
       store8(static_cast<T*>(a.y) + at + col_of(i), y);
     }
   }
+  if constexpr (WIDE) peers.end();
 }
 
 struct BwdArgs {
@@ -280,9 +334,11 @@ struct BwdArgs {
   const float *Hs, *Bs, *rstd_post, *rstd_pre;
   void *dh, *db;
   float* part;   // [gridDim.x][JOIN ? 2 : 1][cols]: this block's column sums of dy that and of dt bhat
-  int64_t rows;
+  unsigned rows;   // below 2^31: numbers of rows, also some steps past the last, fit 32 bits
   int cols;
   float alpha;
+  int cluster;   // blocks that share a row (1 unless WIDE)
+  int* status;
 };
 
 // Persistent like the forward; the column sums of a block's rows stay in registers.  Both means of a row come out of one
@@ -290,10 +346,11 @@ struct BwdArgs {
 //     sum(k dt bhat) = sum(k a bhat) + f sum(k that bhat),
 // so a row costs one barrier instead of two.  The registers that the sums and the weights take leave room for few threads,
 // too few to keep HBM busy with their own loads: hence the copies ahead (DEPTH rows; without them 193 us at 16384 x 3072).
-template <typename T, int NV, int MAXT, int MINB, int DEPTH, bool JOIN, bool FULL>
+template <typename T, int NV, int MAXT, int MINB, int DEPTH, bool JOIN, bool FULL, bool WIDE>
 __global__ void __launch_bounds__(MAXT, MINB) norm_join_bwd_kernel(const BwdArgs a) {
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ float4 red[2][32];
+  __shared__ Peers<WIDE ? 1 : 0> peers;
   wait_for_launch_before();
   let_next_launch_start();
   using S = Slots<T, MAXT>;
@@ -301,12 +358,14 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_join_bwd_kernel(const BwdArgs
   const int ng = (a.cols + kGroup - 1) / kGroup;
   const float inv_n = 1.f / float(a.cols);
   const uint32_t ring0 = static_cast<uint32_t>(__cvta_generic_to_shared(ring));
-  auto col_of = [&](int i) { return (int(threadIdx.x) + i * int(blockDim.x)) * kVec; };
+  const int rank = WIDE ? int(blockIdx.x) % a.cluster : 0, first = rank * NV * int(blockDim.x);   // of this block's vectors
+  const unsigned row0 = WIDE ? blockIdx.x / unsigned(a.cluster) : blockIdx.x;
+  auto col_of = [&](int i) { return (first + int(threadIdx.x) + i * int(blockDim.x)) * kVec; };
   auto live = [&](int i) { return FULL || col_of(i) < a.cols; };
-  auto fetch = [&](int64_t row, int stage) {
+  auto fetch = [&](unsigned row, int stage) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int64_t at = row * a.cols + col_of(i);
+      const int64_t at = int64_t(row) * a.cols + col_of(i);
       const int left = FULL ? INT_MAX : a.cols - col_of(i);
       const uint32_t o = ring0 + (stage * NV + i) * kVecSlot;
       S::fetch(o, static_cast<const T*>(a.dy) + at, left);
@@ -316,10 +375,10 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_join_bwd_kernel(const BwdArgs
       if (JOIN) copy_async(o + 2 * S::kBytes + kCodes + threadIdx.x * 8, a.Bq + at, 8);
     }
   };
-  const int64_t step = gridDim.x;
+  const unsigned step = WIDE ? gridDim.x / unsigned(a.cluster) : gridDim.x;
 #pragma unroll
   for (int s = 0; s < DEPTH; ++s) {
-    if (blockIdx.x + s * step < a.rows) fetch(blockIdx.x + s * step, s);
+    if (row0 + s * step < a.rows) fetch(row0 + s * step, s);
     copies_commit();
   }
   float2 k[JOIN ? NV : 1][4], wp[NV][4], sum_pre[NV][4], sum_c[JOIN ? NV : 1][4];
@@ -340,25 +399,27 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_join_bwd_kernel(const BwdArgs
     float hs[NV], bs[JOIN ? NV : 1], r_t, r_b;
   } next = {};
   next.r_b = 1.f;
-  auto scales = [&](int64_t row) {
+  auto scales = [&](unsigned row) {
     if (row >= a.rows) return;
     next.r_t = __ldcg(a.rstd_pre + row);
     if (JOIN && a.w_post) next.r_b = __ldcg(a.rstd_post + row);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       if (!live(i)) continue;
-      const int64_t g = row * ng + col_of(i) / kGroup;
+      const int64_t g = int64_t(row) * ng + col_of(i) / kGroup;
       next.hs[i] = __ldcg(a.Hs + g);
       if (JOIN) next.bs[JOIN ? i : 0] = __ldcg(a.Bs + g);
     }
   };
-  scales(blockIdx.x);
+  scales(row0);
   int turn = 0, stage = 0;
-  for (int64_t row = blockIdx.x; row < a.rows; row += step, turn ^= 1) {
-    const int64_t at = row * a.cols;
+  uint32_t parity = 0;   // of the barriers of this turn
+  if constexpr (WIDE) peers.start();
+  for (unsigned row = row0; row < a.rows; row += step, parity ^= turn, turn ^= 1) {
+    const int64_t at = int64_t(row) * a.cols;
     float2 that[NV][4], av[NV][4], bhat[JOIN ? NV : 1][4];
     float2 s0 = both(0.f), s1 = both(0.f), s2 = both(0.f);
-    copies_wait<(DEPTH > 0 ? DEPTH - 1 : 0)>();
+    copies_wait<DEPTH - 1>();
     S::meet();
     const RowScales now = next;
     const float rt = now.r_t, rb = now.r_b;
@@ -370,19 +431,11 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_join_bwd_kernel(const BwdArgs
       uint2 hq, bq;
 #pragma unroll
       for (int e = 0; e < 4; ++e) av[i][e] = both(0.f);
-      if (DEPTH > 0) {
-        const uint8_t* o = ring + (stage * NV + i) * kVecSlot;
-        S::take(o).get(dy);
-        if (a.dh_next) S::take(o + S::kBytes).get(av[i]);
-        hq = *reinterpret_cast<const uint2*>(o + 2 * S::kBytes + threadIdx.x * 8);
-        if (JOIN) bq = *reinterpret_cast<const uint2*>(o + 2 * S::kBytes + kCodes + threadIdx.x * 8);
-      } else {
-        const int64_t ac = at + col_of(i);
-        load8(static_cast<const T*>(a.dy) + ac, dy);
-        if (a.dh_next) load8(static_cast<const T*>(a.dh_next) + ac, av[i]);
-        hq = __ldcg(reinterpret_cast<const uint2*>(a.Hq + ac));
-        if (JOIN) bq = __ldcg(reinterpret_cast<const uint2*>(a.Bq + ac));
-      }
+      const uint8_t* o = ring + (stage * NV + i) * kVecSlot;
+      S::take(o).get(dy);
+      if (a.dh_next) S::take(o + S::kBytes).get(av[i]);
+      hq = *reinterpret_cast<const uint2*>(o + 2 * S::kBytes + threadIdx.x * 8);
+      if (JOIN) bq = *reinterpret_cast<const uint2*>(o + 2 * S::kBytes + kCodes + threadIdx.x * 8);
       decode8(hq, now.hs[i], that[i]);
       if (JOIN) decode8(bq, now.bs[j] * rb, bhat[j]);
 #pragma unroll
@@ -404,13 +457,13 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_join_bwd_kernel(const BwdArgs
       }
     }
     scales(row + step);
-    const float3 sums = block_sum3(s0.x + s0.y, s1.x + s1.y, s2.x + s2.y, red[turn]);
-    if (DEPTH > 0) {   // this stage's values are in registers: its slots take the row DEPTH turns on
-      S::meet();
-      if (row + DEPTH * step < a.rows) fetch(row + DEPTH * step, stage);
-      copies_commit();
-      if (++stage == DEPTH) stage = 0;
-    }
+    float3 sums = block_sum3(s0.x + s0.y, s1.x + s1.y, s2.x + s2.y, red[turn]);
+    if constexpr (WIDE) sums = peers.sum(sums, turn, 0, parity, a.cluster, a.status);
+    // this stage's values are in registers: its slots take the row DEPTH turns on
+    S::meet();
+    if (row + DEPTH * step < a.rows) fetch(row + DEPTH * step, stage);
+    copies_commit();
+    if (++stage == DEPTH) stage = 0;
     const float f = -rt * sums.x * inv_n, m2 = JOIN ? (sums.y + f * sums.z) * inv_n : 0.f;
     // db = r_b (k dt - bhat m2); without w_post r_b is 1 and nothing is taken off
     const float r1 = a.w_post ? rb : 1.f, r2 = a.w_post ? -rb * m2 : 0.f;
@@ -434,7 +487,8 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_join_bwd_kernel(const BwdArgs
       }
     }
   }
-  float* part = a.part + int64_t(blockIdx.x) * (JOIN ? 2 : 1) * a.cols;
+  if constexpr (WIDE) peers.end();
+  float* part = a.part + int64_t(row0) * (JOIN ? 2 : 1) * a.cols;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     if (!live(i)) continue;
@@ -443,24 +497,24 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_join_bwd_kernel(const BwdArgs
   }
 }
 
-// Adds the blocks' column sums in a fixed order: 32 columns by 32 strips of blocks per thread block, strips then added in
+// Adds the blocks' column sums in a fixed order: 32 columns by STRIPS strips of blocks per thread block, strips then added in
 // order; turns c into the gradients of w_post and of the gate.
-template <typename T>
-__global__ void __launch_bounds__(1024) norm_join_columns_kernel(const float* part, int blocks, int cols, int planes, float alpha,
+template <typename T, int STRIPS>
+__global__ void __launch_bounds__(32 * STRIPS) norm_join_columns_kernel(const float* part, int blocks, int cols, int planes, float alpha,
                                                                  const T* __restrict__ w_post, const T* __restrict__ gate,
                                                                  float* __restrict__ dw_pre, float* __restrict__ dw_post,
                                                                  float* __restrict__ dgate) {
-  __shared__ float red[32][33];
+  __shared__ float red[STRIPS][33];
   const int x = threadIdx.x & 31, y = threadIdx.x >> 5, plane = blockIdx.y;
   const int c = int(blockIdx.x) * 32 + x;
   float s = 0.f;
   wait_for_launch_before();
   let_next_launch_start();
   if (c < cols)
-    for (int k = y; k < blocks; k += 16 * 32) {   // sixteen loads under way, added in order
+    for (int k = y; k < blocks; k += 16 * STRIPS) {   // sixteen loads under way, added in order
       float v[16];
 #pragma unroll
-      for (int u = 0; u < 16; ++u) v[u] = k + 32 * u < blocks ? __ldcg(part + (int64_t(k + 32 * u) * planes + plane) * cols + c) : 0.f;
+      for (int u = 0; u < 16; ++u) v[u] = k + STRIPS * u < blocks ? __ldcg(part + (int64_t(k + STRIPS * u) * planes + plane) * cols + c) : 0.f;
 #pragma unroll
       for (int u = 0; u < 16; ++u) s += v[u];
     }
@@ -469,7 +523,7 @@ __global__ void __launch_bounds__(1024) norm_join_columns_kernel(const float* pa
   if (y != 0 || c >= cols) return;
   s = 0.f;
 #pragma unroll
-  for (int k = 0; k < 32; ++k) s += red[k][x];
+  for (int k = 0; k < STRIPS; ++k) s += red[k][x];
   if (plane == 0) {
     if (dw_pre) dw_pre[c] = s;
     return;
@@ -481,46 +535,89 @@ __global__ void __launch_bounds__(1024) norm_join_columns_kernel(const float* pa
 
 int round_warp(int threads) { return (threads + 31) / 32 * 32; }
 
-// Vectors per thread, threads per block and blocks per SM for a row of `cols` columns (at most 32768).  `one`, `two`: up to
-// how many threads one and two vectors are taken; `per_sm`: threads per SM at the registers the kernel is bounded to.
-struct Shape { int nv, threads, blocks; };
-Shape shape_of(int64_t rows, int64_t cols, int one, int two, int per_sm_1, int per_sm_2) {
-  const int vecs = int(cols / kVec);
-  const int nv = vecs <= one ? 1 : (vecs <= 2 * two ? 2 : 4), threads = round_warp((vecs + nv - 1) / nv);
-  const int per_sm = std::max(1, std::min(16, (nv == 1 ? per_sm_1 : (nv == 2 ? per_sm_2 : 1024)) / threads));
-  return Shape{nv, threads, int(std::min<int64_t>(rows, int64_t(sm_count()) * per_sm))};
+// Vectors per thread, threads per block, blocks that share a row, and rows under way.
+struct Shape { int nv, threads, cluster, blocks; };
+constexpr int kOneVec = 384;     // threads of a block with one vector each, at most
+constexpr int kTwoVecs = 512;    // with two: alone on its SM above 256
+// `per_sm`: threads per SM at the registers that the kernels with one and with two vectors are bounded to.
+struct PerSm { int one, two; };
+Shape shape_of(int64_t rows, int vecs, int nv, int cluster, PerSm p) {
+  const int threads = round_warp((vecs + nv * cluster - 1) / (nv * cluster));
+  const int per_sm = std::max(1, std::min(16, (nv == 1 ? p.one : p.two) / threads));
+  return Shape{nv, threads, cluster, int(std::min<int64_t>(rows, int64_t(sm_count()) * per_sm / cluster))};
 }
-Shape fwd_shape(int64_t rows, int64_t cols) { return shape_of(rows, cols, 384, 512, 1152, 512); }
-Shape bwd_shape(int64_t rows, int64_t cols) { return shape_of(rows, cols, 384, 512, 768, 512); }
+// Forward: rows of more than 8192 columns are shared by three to eight blocks of 256 threads with two vectors each.  (One block,
+// four vectors of 1024 threads: its values spilled, 2000 x 16384 took 142 us, shared by four 87.  Narrower rows are faster
+// alone: 8192 x 8192 110 us, shared by four 182.)
+Shape fwd_shape(int64_t rows, int64_t cols) {
+  const int vecs = int(cols / kVec);
+  return shape_of(rows, vecs, vecs <= kOneVec ? 1 : 2, vecs <= 2 * kTwoVecs ? 1 : (vecs + 511) / 512, PerSm{1152, 512});
+}
+// Backward: the sums take more registers, so rows are shared as soon as one vector per thread does for two blocks (8192 x 6144:
+// 152 us, 164 in one block with two vectors) and, from 8192 columns on, for four or eight (4096 x 12288: 164 us, 250 with two
+// vectors in three blocks, 512 with four in one; 2000 x 16384: 117, 376 in one).  Between the two one block of two vectors
+// per thread is faster (8192 x 8192: 181 us, 221 shared by four).
+Shape bwd_shape(int64_t rows, int64_t cols) {
+  const int vecs = int(cols / kVec);
+  int cluster = 1;
+  if ((vecs > kTwoVecs && vecs <= 2 * kOneVec) || vecs > 2 * kTwoVecs)
+    while (cluster < 8 && cluster * kOneVec < vecs) cluster *= 2;
+  return shape_of(rows, vecs, vecs <= cluster * kOneVec ? 1 : 2, cluster, PerSm{768, 512});
+}
 bool is_full(const Shape& s, int64_t cols) { return cols == int64_t(s.nv) * s.threads * kVec; }
 
+// How many clusters of a size and of blocks of so many warps run at once, asked once for each (0: not yet): the last clusters of a persistent grid that does
+// not fit would start when the others end and double the time.
+using ClusterLimit = std::atomic<int>[9][kOneVec / 32 + 1];
+
+// s.blocks: at most as many rows under way as run at once.
 template <typename K, typename A>
-cudaError_t launch_rows(K kernel, DeviceOnce& once, const A& a, const Shape& s, int smem, cudaStream_t st) {
-  if (smem > 0 && once.needed()) {
+cudaError_t launch_rows(K kernel, DeviceOnce& once, ClusterLimit& limit, const A& a, Shape& s, int smem, cudaStream_t st) {
+  if (once.needed()) {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     once.done();
   }
-  return launch_lined_up(kernel, dim3(unsigned(s.blocks)), dim3(unsigned(s.threads)), size_t(smem), st, a);
+  if (s.cluster > 1) {
+    std::atomic<int>& known = limit[s.cluster][s.threads / 32];
+    int n = known.load(std::memory_order_relaxed);
+    if (n == 0) {
+      cudaLaunchConfig_t cfg = {};
+      cudaLaunchAttribute attr[1];
+      cfg.gridDim = dim3(unsigned(s.cluster));
+      cfg.blockDim = dim3(unsigned(s.threads));
+      cfg.dynamicSmemBytes = size_t(smem);
+      attr[0].id = cudaLaunchAttributeClusterDimension;
+      attr[0].val.clusterDim = {unsigned(s.cluster), 1, 1};
+      cfg.attrs = attr;
+      cfg.numAttrs = 1;
+      const cudaError_t e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
+      if (e != cudaSuccess) return e;
+      known.store(n = std::max(n, 1), std::memory_order_relaxed);
+    }
+    s.blocks = std::min(s.blocks, n);
+  }
+  return launch_lined_up_in_clusters(unsigned(s.cluster), kernel, dim3(unsigned(s.blocks * s.cluster)), dim3(unsigned(s.threads)), size_t(smem), st, a);
 }
 template <typename T>
 constexpr int depth_of() { return sizeof(T) == 2 ? 4 : 2; }   // rows ahead in the forward: the same bytes for both types
 
-template <typename T, int NV, int MAXT, int MINB, int DEPTH, bool JOIN, bool KEEP, bool FULL>
-cudaError_t launch_fwd(const FwdArgs& a, const Shape& s, cudaStream_t st) {
+template <typename T, int NV, int MAXT, int MINB, int DEPTH, bool JOIN, bool KEEP, bool FULL, bool WIDE = false>
+cudaError_t launch_fwd(const FwdArgs& a, Shape s, cudaStream_t st) {
   static DeviceOnce once;
-  return launch_rows(norm_join_fwd_kernel<T, NV, MAXT, MINB, DEPTH, JOIN, KEEP, FULL>, once, a, s,
+  static ClusterLimit limit;
+  return launch_rows(norm_join_fwd_kernel<T, NV, MAXT, MINB, DEPTH, JOIN, KEEP, FULL, WIDE>, once, limit, a, s,
                      DEPTH * NV * MAXT * 8 * int(sizeof(T)) * (JOIN ? 2 : 1), st);
 }
 template <typename T, bool JOIN, bool KEEP>
 cudaError_t launch_fwd(const FwdArgs& a, cudaStream_t st) {
   const Shape s = fwd_shape(a.rows, a.cols);
   constexpr int D = depth_of<T>();
+  if (s.cluster > 1) return launch_fwd<T, 2, 256, 2, D, JOIN, KEEP, false, true>(a, s, st);
   if (s.nv == 1 && s.threads <= 128) return launch_fwd<T, 1, 128, 9, D, JOIN, KEEP, false>(a, s, st);
   if (s.nv == 1) return is_full(s, a.cols) ? launch_fwd<T, 1, 384, 3, D, JOIN, KEEP, true>(a, s, st) : launch_fwd<T, 1, 384, 3, D, JOIN, KEEP, false>(a, s, st);
   if (s.nv == 2 && s.threads <= 256) return launch_fwd<T, 2, 256, 2, D, JOIN, KEEP, false>(a, s, st);
-  if (s.nv == 2) return launch_fwd<T, 2, 512, 1, D, JOIN, KEEP, false>(a, s, st);
-  return launch_fwd<T, 4, 1024, 1, 0, JOIN, KEEP, false>(a, s, st);
+  return launch_fwd<T, 2, 512, 1, D, JOIN, KEEP, false>(a, s, st);
 }
 template <typename T>
 cudaError_t launch_fwd(const FwdArgs& a, cudaStream_t st) {
@@ -528,21 +625,22 @@ cudaError_t launch_fwd(const FwdArgs& a, cudaStream_t st) {
   return a.Hq ? launch_fwd<T, false, true>(a, st) : launch_fwd<T, false, false>(a, st);
 }
 
-template <typename T, int NV, int MAXT, int MINB, int DEPTH, bool JOIN, bool FULL>
-cudaError_t launch_bwd(const BwdArgs& a, const Shape& s, cudaStream_t st) {
+template <typename T, int NV, int MAXT, int MINB, int DEPTH, bool JOIN, bool FULL, bool WIDE = false>
+cudaError_t launch_bwd(const BwdArgs& a, Shape& s, cudaStream_t st) {
   static DeviceOnce once;
-  return launch_rows(norm_join_bwd_kernel<T, NV, MAXT, MINB, DEPTH, JOIN, FULL>, once, a, s,
+  static ClusterLimit limit;
+  return launch_rows(norm_join_bwd_kernel<T, NV, MAXT, MINB, DEPTH, JOIN, FULL, WIDE>, once, limit, a, s,
                      DEPTH * NV * MAXT * (2 * 8 * int(sizeof(T)) + (JOIN ? 16 : 8)), st);
 }
 template <typename T, bool JOIN>
-cudaError_t launch_bwd(const BwdArgs& a, cudaStream_t st) {
-  const Shape s = bwd_shape(a.rows, a.cols);
+cudaError_t launch_bwd(const BwdArgs& a, Shape& s, cudaStream_t st) {
   constexpr int D = 2;   // rows ahead; 3, 4 and 6 are 1 to 3 % slower (bf16, 16384 x 3072)
+  if (s.cluster > 1 && s.nv == 1) return launch_bwd<T, 1, kOneVec, 2, D, JOIN, false, true>(a, s, st);
+  if (s.cluster > 1) return launch_bwd<T, 2, 256, 2, D, JOIN, false, true>(a, s, st);
   if (s.nv == 1 && s.threads <= 128) return launch_bwd<T, 1, 128, 6, D, JOIN, false>(a, s, st);
   if (s.nv == 1) return is_full(s, a.cols) ? launch_bwd<T, 1, 384, 2, D, JOIN, true>(a, s, st) : launch_bwd<T, 1, 384, 2, D, JOIN, false>(a, s, st);
   if (s.nv == 2 && s.threads <= 256) return launch_bwd<T, 2, 256, 2, D, JOIN, false>(a, s, st);
-  if (s.nv == 2) return launch_bwd<T, 2, 512, 1, D, JOIN, false>(a, s, st);
-  return launch_bwd<T, 4, 1024, 1, 0, JOIN, false>(a, s, st);
+  return launch_bwd<T, 2, 512, 1, D, JOIN, false>(a, s, st);
 }
 
 }  // namespace
@@ -550,7 +648,8 @@ cudaError_t launch_bwd(const BwdArgs& a, cudaStream_t st) {
 cudaError_t norm_join_fwd(const Rows& d, const void* h, const void* b, const void* w_post, const void* gate, const void* w_pre, void* h_out,
                           void* y, int8_t* Hq, float* Hs, int8_t* Bq, float* Bs, float* rstd_post, float* rstd_pre, float eps, float alpha,
                           cudaStream_t st) {
-  FwdArgs a{h, b, w_post, gate, w_pre, h_out, y, Hq, Bq, Hs, Bs, rstd_post, rstd_pre, d.rows, int(d.cols), eps, alpha};
+  FwdArgs a{h, b, w_post, gate, w_pre, h_out, y, Hq, Bq, Hs, Bs, rstd_post, rstd_pre, unsigned(d.rows), int(d.cols), eps, alpha, fwd_shape(d.rows, d.cols).cluster, nullptr};
+  if (a.cluster > 1 && !(a.status = device_status_ptr())) return cudaErrorMemoryAllocation;
   return d.bf16 ? launch_fwd<__nv_bfloat16>(a, st) : launch_fwd<float>(a, st);
 }
 
@@ -560,20 +659,26 @@ cudaError_t norm_join_bwd(const Rows& d, const void* dy, const void* dh_next, co
                           const int8_t* Hq, const float* Hs, const int8_t* Bq, const float* Bs, const float* rstd_post,
                           const float* rstd_pre, void* dh, void* db, float* dw_post, float* dgate, float* dw_pre, float alpha, void* ws,
                           cudaStream_t st) {
-  BwdArgs a{dy, dh_next, w_post, gate, w_pre, Hq, Bq, Hs, Bs, rstd_post, rstd_pre, dh, db, static_cast<float*>(ws), d.rows, int(d.cols), alpha};
+  Shape s = bwd_shape(d.rows, d.cols);
+  BwdArgs a{dy, dh_next, w_post, gate, w_pre, Hq, Bq, Hs, Bs, rstd_post, rstd_pre, dh, db, static_cast<float*>(ws), unsigned(d.rows), int(d.cols), alpha, s.cluster, nullptr};
+  if (s.cluster > 1 && !(a.status = device_status_ptr())) return cudaErrorMemoryAllocation;
   cudaError_t e;
-  if (d.bf16) e = Bq ? launch_bwd<__nv_bfloat16, true>(a, st) : launch_bwd<__nv_bfloat16, false>(a, st);
-  else e = Bq ? launch_bwd<float, true>(a, st) : launch_bwd<float, false>(a, st);
+  if (d.bf16) e = Bq ? launch_bwd<__nv_bfloat16, true>(a, s, st) : launch_bwd<__nv_bfloat16, false>(a, s, st);
+  else e = Bq ? launch_bwd<float, true>(a, s, st) : launch_bwd<float, false>(a, s, st);
   if (e != cudaSuccess || (!dw_pre && !dw_post && !dgate)) return e;
   const int planes = Bq ? 2 : 1;
   const dim3 grid(unsigned((d.cols + 31) / 32), unsigned((dw_post || dgate) ? 2 : 1));
-  const int blocks = bwd_shape(d.rows, d.cols).blocks;
+  const int blocks = s.blocks;
   const float* part = a.part;
+  // wide rows: few sums for each of many columns, and more thread blocks of 32 strips than run at once
+  const bool many = int64_t(grid.x) * grid.y > 2 * sm_count();
   if (d.bf16)
-    return launch_lined_up(norm_join_columns_kernel<__nv_bfloat16>, grid, dim3(1024), 0, st, part, blocks, a.cols, planes, alpha,
-                           static_cast<const __nv_bfloat16*>(w_post), static_cast<const __nv_bfloat16*>(gate), dw_pre, dw_post, dgate);
-  return launch_lined_up(norm_join_columns_kernel<float>, grid, dim3(1024), 0, st, part, blocks, a.cols, planes, alpha,
-                         static_cast<const float*>(w_post), static_cast<const float*>(gate), dw_pre, dw_post, dgate);
+    return launch_lined_up(many ? norm_join_columns_kernel<__nv_bfloat16, 8> : norm_join_columns_kernel<__nv_bfloat16, 32>, grid,
+                           dim3(many ? 256 : 1024), 0, st, part, blocks, a.cols, planes, alpha, static_cast<const __nv_bfloat16*>(w_post),
+                           static_cast<const __nv_bfloat16*>(gate), dw_pre, dw_post, dgate);
+  return launch_lined_up(many ? norm_join_columns_kernel<float, 8> : norm_join_columns_kernel<float, 32>, grid, dim3(many ? 256 : 1024), 0,
+                         st, part, blocks, a.cols, planes, alpha, static_cast<const float*>(w_post), static_cast<const float*>(gate), dw_pre,
+                         dw_post, dgate);
 }
 
 }  // namespace acx

@@ -167,6 +167,7 @@ def test_swiglu_gradient_against_differences():
 VARIANTS = [(False, False, False), (True, False, False), (True, True, False), (True, False, True), (True, True, True)]
 # below a warp, one vector per thread, two, four; ragged last vectors and groups; more rows than resident blocks
 NORM_SHAPES = [(1, 8), (5, 264), (1500, 896), (2500, 1000), (67, 4096), (41, 4872), (11, 8200), (3, 32768)]
+WIDE_SHAPES = [(650, 5640), (700, 12296), (301, 16384), (90, 28672)]    # rows shared by several blocks, more of them than run at once
 
 
 def _norm_inputs(rows, cols, dtype, join, post, gate, exact=False):
@@ -192,7 +193,7 @@ def _norm_fwd(desc, dv, dtype, alpha, keep=True, eps=1e-5):
     return o, k
 
 
-@pytest.mark.parametrize("rows,cols", NORM_SHAPES)
+@pytest.mark.parametrize("rows,cols", NORM_SHAPES + WIDE_SHAPES)
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("join,post,gate", VARIANTS)
 def test_norm_join(rows, cols, dtype, join, post, gate):
