@@ -1,8 +1,8 @@
 // The tcgen05 kernels of the vocabulary cross entropy: persistent, warp-specialised, on pairs of CTAs (a cluster of two
 // drives tcgen05.mma.cta_group::2 on a tile of 256 x 256).  Three kinds share the mainloop and differ in their epilogue:
 //
-//   LSE      logits tile = X W^T; every row of the tile leaves its maximum and its sum of exponentials over 128 columns
-//            (and the logit of its target, where the tile holds it): 16 bytes instead of 1 KiB of fp32 logits;
+//   LSE      logits tile = X W^T; every row of the tile leaves its maximum and its sum of exponentials over 64 columns
+//            (and the logit of its target, where the tile holds it): 32 bytes instead of 1 KiB of fp32 logits;
 //   DLOGITS  the same tile again, now D = w (exp(logit - lse) - onehot), rounded to bf16, for one piece of the vocabulary;
 //   GRADS    both products of a finished piece in one launch: dX += D W_piece (split over the piece when there are few
 //            tiles; fp32 sums in global memory, added by the bulk-copy engine) and dW_piece = D^T X (bf16, complete).
@@ -10,7 +10,8 @@
 // What bounds them: the tensor cores, from a few hundred tokens on; with fewer the bytes of W.  Per SM a 256 x 256 pair
 // tile takes K / 16 instructions of 128 cycles.  Its epilogue (128 x 256 elements per CTA: 2048 cycles of exponentials at
 // least) is hidden behind the next tile's mainloop by the second accumulator where d is large enough for that; sixteen
-// warps share it, because with eight the latencies of its dependent steps made it 4600 (LSE) and 8300 cycles (DLOGITS).
+// warps share it: with eight the latencies of its dependent steps bound tiles of small d (LSE of 4096 x 128 x 65536: 172 us,
+// 117 with sixteen and the accumulator handed back as soon as it is read).
 //
 // FEW: at most 64 tokens.  A tile of 256 tokens would be mostly empty rows, and the tensor core takes as long for those: with
 // 64 tokens and 2048 columns the logits of 128256 words were bound by it (119 us under sustained load, at 1.3 GHz under the
