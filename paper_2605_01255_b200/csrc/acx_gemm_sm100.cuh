@@ -118,6 +118,7 @@ struct Params {
                                 // (the bias gradient: A is G_out read MN-major, so a column of A^T is a row of D)
   int64_t c_split_stride;       // elements between split partials
   int* status;                  // device status word (kDevTimeout on give-up)
+  int ends_after;               // this grid started beside the one before it and needs nothing of it: it ends after it all the same
 };
 
 struct Tile {
@@ -334,8 +335,9 @@ __global__ void __launch_bounds__(Cfg<MT, BROWS, PAIR>::threads(SKETCH == SKETCH
   ptx::tcgen05_fence_after_sync();
   const uint32_t tmem_base = *tmem_slot_gen;
   // A grid launched behind this one with programmatic stream serialization may take the SMs that this grid's CTAs
-  // leave as they finish (the gradient factor of the same call behind dX: it needs nothing that dX writes).
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  // leave as they finish (the gradient factor of the same call behind dX: it needs nothing that dX writes).  Not behind a
+  // grid that itself started early: see the producer's end.
+  if (!p.ends_after) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   auto give_up = [&]() {
     *abort_flag = 1;
@@ -424,6 +426,13 @@ __global__ void __launch_bounds__(Cfg<MT, BROWS, PAIR>::threads(SKETCH == SKETCH
           const uint32_t ph = (s < stage) ? phase : (phase ^ 1u);   // parity of the last phase filled on stage s
           if (!ptx::mbar_wait(empty_bar(s), ph, abort_flag)) { give_up(); ok = false; }
         }
+      }
+      // The launch behind this one may be lined up too; it then waits for this grid and for no other.  So this grid must
+      // not end, nor let that one start, before the grid that it overtook has ended.  A grid ends with its last block: that
+      // one waits, and the others leave their SMs to whatever is left of either grid.
+      if (p.ends_after && blockIdx.x == gridDim.x - 1) {
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
       }
     }
   } else if (warp == 1) {

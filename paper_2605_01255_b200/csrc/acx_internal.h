@@ -46,6 +46,10 @@ inline cudaError_t launched() {
 
 // Launches with programmatic stream serialization: the kernel may start before the launch before it has finished, and waits
 // for that itself (wait_for_launch_before, first thing or as soon as it needs to).  In clusters of `cluster` blocks along x.
+//
+// That wait covers the launch before and no other.  So every kernel of the library that is launched this way ends only after
+// the launch before it has ended, whether or not it needs anything of it (what it waits for is then all that was launched
+// before); and one that needs nothing of it lets the next launch start only then, too.
 template <typename... K, typename... A>
 cudaError_t launch_lined_up_in_clusters(unsigned cluster, void (*kernel)(K...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, const A&... args) {
   cudaLaunchConfig_t cfg = {};

@@ -529,8 +529,9 @@ cudaError_t sm100_dx(const Problem& q, const void* G, const void* W, void* dX, i
 }
 
 // after_dx: the grid launched just before on this stream is the dX kernel of the same call.  The factor reads nothing
-// that dX writes, so it is launched with programmatic stream serialization and never waits for it: its thread blocks
-// take over the SMs as the dX kernel's last round of tiles leaves them idle.
+// that dX writes, so it is launched with programmatic stream serialization and starts without waiting for it: its thread
+// blocks take over the SMs as the dX kernel's last round of tiles leaves them idle.  It ends after dX, though: a launch that
+// is lined up behind the factor (launch_lined_up) waits for the factor alone, and reads dX.
 cudaError_t sm100_factor(const Problem& q, const void* G, const void* XS, float* A, void* ws, int* status, cudaStream_t st,
                          bool allow_cluster, float* db_part, int* db_splits, bool after_dx) {
   const FactorPlan f = allow_cluster ? factor_plan_public(q) : factor_plan(q);
@@ -543,6 +544,7 @@ cudaError_t sm100_factor(const Problem& q, const void* G, const void* XS, float*
   p.n_tiles = 1;
   p.splits = f.splits; p.kb_per_split = f.kb_per_split;
   p.ldc = q.r; p.status = status;
+  p.ends_after = after_dx;
   p.c_split_stride = q.d_out * int64_t(q.r);
   p.C = (f.splits > 1 && !f.cluster) ? ws : static_cast<void*>(A);
   CUtensorMap ta, tb;
