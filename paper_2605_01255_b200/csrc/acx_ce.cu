@@ -11,6 +11,7 @@
 namespace acx {
 namespace {
 
+using ce::kLowest;
 using ce::Params;
 
 constexpr int kTokensPerBlock = 8, kJoinThreads = 512;
@@ -25,13 +26,11 @@ __device__ __forceinline__ float dot8(uint4 a, uint4 b, float s) {
   return s;
 }
 
-// (m, s) <- (m, s) joined with (m1, s1): sums of 2^(x - maximum)
+// (m, s) <- (m, s) joined with (m1, s1): sums of 2^(x - maximum); one that holds nothing is (kLowest, 0)
 __device__ __forceinline__ void join_pair(float& m, float& s, float m1, float s1) {
   const float top = fmaxf(m, m1);
-  // a side that holds nothing has (-inf, 0): it must not turn into a NaN; one that holds a NaN must stay one
-  const float a = (m == -INFINITY && s == 0.f) ? 0.f : s * exp2f(m - top), b = (m1 == -INFINITY && s1 == 0.f) ? 0.f : s1 * exp2f(m1 - top);
+  s = s * exp2f(m - top) + s1 * exp2f(m1 - top);
   m = top;
-  s = a + b;
 }
 
 // Joins the (maximum, sum) pairs of 8 tokens: 16 warps; a lane has token lane & 7 and every 64th pair, eight at a time.  The
@@ -74,12 +73,12 @@ __global__ void __launch_bounds__(kJoinThreads, 3) ce_join_kernel(const float2* 
   wait_for_launch_before();
   let_next_launch_start();
   const int tok = lane & 7, t = t0 + tok;
-  float m = -INFINITY, s = 0.f;
+  float m = kLowest, s = 0.f;
   if (t < tokens) {
     for (int q = warp * 4 + (lane >> 3); q < parts; q += 8 * 64) {   // eight pairs in flight
       float2 v[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = q + 64 * i < parts ? __ldcg(part + int64_t(q + 64 * i) * tokens + t) : make_float2(-INFINITY, 0.f);
+      for (int i = 0; i < 8; ++i) v[i] = q + 64 * i < parts ? __ldcg(part + int64_t(q + 64 * i) * tokens + t) : make_float2(kLowest, 0.f);
 #pragma unroll
       for (int i = 0; i < 8; ++i) join_pair(m, s, v[i].x, v[i].y);
     }
@@ -89,7 +88,7 @@ __global__ void __launch_bounds__(kJoinThreads, 3) ce_join_kernel(const float2* 
   if (lane < 8) red[warp][lane] = make_float2(m, s);
   __syncthreads();
   if (warp == 0) {
-    m = -INFINITY;
+    m = kLowest;
     s = 0.f;
     for (int k = lane >> 3; k < 16; k += 4) join_pair(m, s, red[k][tok].x, red[k][tok].y);
 #pragma unroll
@@ -100,7 +99,7 @@ __global__ void __launch_bounds__(kJoinThreads, 3) ce_join_kernel(const float2* 
       const bool trained = y >= 0 && y < vocab;
       const float ty = (exact[2 * tok] + exact[2 * tok + 1]) * c;
       if (trained) s += exp2f(ty - m) - exp2f(__ldcg(target_logit + t) - m);
-      const float l2 = m + log2f(s);
+      const float l2 = s > 0.f ? m + log2f(s) : NAN;   // no word is possible, or a NaN
       constexpr float kLn2 = 0.6931471805599453f;
       lse[t] = l2 * kLn2;
       const float l = trained ? (l2 - ty) * kLn2 : 0.f;

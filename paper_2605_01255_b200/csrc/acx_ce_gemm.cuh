@@ -63,6 +63,9 @@ static_assert(kSmemBytes <= 232448, "shared memory of one CTA");
 
 enum Kind { LSE = 0, DLOGITS = 1, GRADS = 2 };
 constexpr float kLog2e = 1.4426950408889634f;
+// The maximum of logits of which none is more than minus infinity, with a sum of zero: a finite number, so that no difference
+// of two maxima is one of infinities (which would turn a sum that holds nothing into a NaN).
+constexpr float kLowest = -0x1.fffffep127f;
 
 struct Params {
   int tokens, d, vocab;
@@ -458,7 +461,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (KIND == LSE) {
 #pragma unroll
         for (int j = 0; j < kFew; ++j) {
-          few_m[FEW && KIND == LSE ? j : 0] = -INFINITY;
+          few_m[FEW && KIND == LSE ? j : 0] = kLowest;
           few_s[FEW && KIND == LSE ? j : 0] = 0.f;
         }
       }
@@ -603,13 +606,13 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int i = 1; i < 16; ++i) top[c] = fmaxf(top[c], __uint_as_float(w[c >> 1][16 * (c & 1) + i]));
           }
-          const float m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c1;
+          const float m = fmaxf(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c1, kLowest);
           float2 sum[4];
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             sum[c] = q8::both(0.f);
 #pragma unroll
-            for (int i = 16 * (c & 1); i < 16 * (c & 1) + 16; i += 2) {   // (an all -inf row gives NaN, as the definition's difference does)
+            for (int i = 16 * (c & 1); i < 16 * (c & 1) + 16; i += 2) {
               const float2 x = q8::fma2(make_float2(__uint_as_float(w[c >> 1][i]), __uint_as_float(w[c >> 1][i + 1])), q8::both(c1), q8::both(-m));
               sum[c] = q8::add2(sum[c], make_float2(exp2_fast(x.x), exp2_fast(x.y)));
             }
@@ -711,7 +714,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         float top = few_m[k];
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-        float sum = few_s[k] == 0.f ? 0.f : few_s[k] * exp2_fast(few_m[k] - top);
+        float sum = few_s[k] * exp2_fast(few_m[k] - top);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
         if (lane == j) {

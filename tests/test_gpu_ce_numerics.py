@@ -1,0 +1,85 @@
+"""Accuracy of the vocabulary cross entropy where little is left of a difference: logits of minus infinity, tokens that are almost
+certain, the systematic part of the tensor core's error, the roundings of D, weights of zero."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import cross_entropy as C
+from paper_2605_01255_b200 import binding as B
+from paper_2605_01255_b200 import inputs as I
+
+from _harness import to_device, to_host
+
+pytestmark = pytest.mark.gpu
+NAN = float("nan")
+
+
+def run(X, W, y, weight=None, logit_scale=1.0, backward=True, scale=1.0):
+    """Outputs of a forward and a backward call, by name; numpy float64."""
+    (t, d), v = X.shape, W.shape[0]
+    desc = B.make_ce_desc(t, d, v, logit_scale)
+    Xd, Wd, yd = to_device(X, "bf16"), to_device(W, "bf16"), torch.from_numpy(np.asarray(y, np.int64)).cuda()
+    wd = None if weight is None else to_device(np.asarray(weight, np.float32), "f32")
+    o = {"loss": torch.full((t,), NAN, device="cuda"), "lse": torch.full((t,), NAN, device="cuda"), "total": torch.full((2,), NAN, device="cuda")}
+    ws = B.alloc_ce_workspace(desc, B.ACX_OP_CE_BWD)
+    ws.fill_(255)                  # NaN everywhere
+    B.acx_linear_ce_fwd(desc, Xd, Wd, yd, o["loss"], o["lse"], o["total"], wd, ws)
+    if backward:
+        o["dX"], o["dW"] = torch.full_like(Xd, NAN), torch.full_like(Wd, NAN)
+        B.acx_linear_ce_bwd(desc, Xd, Wd, yd, o["lse"], o["dX"], o["dW"], weight=wd, scale=scale, ws=ws)
+    assert B.acx_last_device_status() == B.ACX_OK
+    return {k: to_host(a) for k, a in o.items()}
+
+
+# up to 64 tokens the words are the rows of a tile, above that the tokens
+TOKENS = [7, 64, 65, 300]
+
+
+@pytest.mark.parametrize("t", TOKENS)
+@pytest.mark.parametrize("d,v", [(64, 700), (72, 65)])
+def test_logits_of_minus_infinity(t, d, v):
+    """Words whose products overflow to minus infinity count for nothing, whether they fill 64 columns, a lane's first word, the
+    last words or all but one."""
+    g = np.random.Generator(np.random.Philox(t + v))
+    for some in range(3):
+        gone = np.zeros(v, bool)
+        if some == 0:
+            gone[:min(v - 1, 128)] = True
+            gone[-37:] = True
+            gone[v // 2] = False
+        elif some == 1:
+            gone[g.random(v) < 0.5] = True
+            gone[3] = False
+        else:
+            gone[:] = True
+            gone[v - 1] = False
+        X, W = I.gaussian((t, d), 1, 1.0, "bf16"), I.gaussian((v, d), 2, d ** -0.5, "bf16")
+        X[:, 0] = 2.0 ** 120
+        W[:, 0] = np.where(gone, -2.0 ** 20, 0.0)
+        left = np.nonzero(~gone)[0]
+        y = left[g.integers(0, len(left), t)]
+        y[1] = -1
+        o = run(X, W, y)
+        loss, lse, total = C.ce_fwd(X, W, y)
+        e = 2.0 ** -23 * (d / 16 + 8) * (np.abs(X[:, 1:]).astype(np.float64) @ np.abs(W[left, 1:]).astype(np.float64).T).max(1)
+        e += 2.0 ** -21 * (1 + np.abs(lse))
+        assert np.all(np.abs(o["lse"] - lse) <= e) and np.all(np.abs(o["loss"] - loss) <= 2 * e)
+        assert abs(o["total"][0] - total[0]) <= np.sum(2 * e) + 2.0 ** -20 * np.sum(loss)
+        assert not o["dW"][gone].any()
+        if len(left) == 1:             # (one word is certain: its gradients are a rounding error's)
+            continue
+        dX, dW = C.ce_bwd(X, W, y)
+        D = np.abs(C.ce_dlogits(X, W, y))
+        per_d = 2.0 ** -8 * D + 4 * e[:, None] * np.minimum(D + 1, D * 4 + 1e-30)
+        for got, want, mag in ((o["dX"], dX, (per_d + 2.0 ** -23 * (v / 16 + 40) * D) @ np.abs(W.astype(np.float64))),
+                               (o["dW"], dW, (per_d + 2.0 ** -23 * (t / 16 + 40) * D).T @ np.abs(X.astype(np.float64)))):
+            assert np.all(np.abs(got - want) <= 1.05 * mag + 2.0 ** -8 * np.abs(want) + 1e-37)
+    # a target that is impossible: an infinite loss; its element of D is -1, everything else is what it was
+    y2 = y.copy()
+    y2[0] = np.nonzero(gone)[0][0]
+    q = run(X, W, y2)
+    assert q["loss"][0] == np.inf and q["total"][0] == np.inf and np.array_equal(q["lse"][1:], o["lse"][1:])
+    assert np.array_equal(q["dX"][1:], o["dX"][1:]) and np.isfinite(q["dX"][0, 1:]).all()
+    # and no possible word at all: nothing to be said
+    W[:, 0] = -2.0 ** 20
+    assert np.isnan(run(X, W, y, backward=False)["lse"]).all()
