@@ -337,7 +337,8 @@ ACX_API size_t acx_ce_workspace_bytes(const acx_ce_desc* desc, int op);
  *   weight [tokens] fp32 or NULL (all one): weights of the tokens in `total` and in the gradients.
  *   loss, lse [tokens] fp32, out;   total [2] fp32, out, or NULL: (sum of weight * loss, sum of weight) over the trained
  *   tokens: total[0] / total[1] is the mean loss, and &total[1] the `denom` of its gradient.
- *   The logits are fp32 sums on the tensor cores; the target's own is summed again outside them (see acx_ce.cu). */
+ *   The logits are fp32 sums on the tensor cores; the target's own is summed again outside them.  The loss is computed as
+ *   log(1 + sum over the other words / the target's), not as a difference: that of an almost certain token keeps its digits. */
 ACX_API acx_status acx_linear_ce_fwd(const acx_ce_desc* desc, const void* X, const void* W, const int64_t* targets, const float* weight,
                                      float* loss, float* lse, float* total, void* ws, size_t ws_bytes, void* cuda_stream);
 

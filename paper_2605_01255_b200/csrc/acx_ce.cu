@@ -34,11 +34,14 @@ __device__ __forceinline__ void join_pair(float& m, float& s, float m1, float s1
 }
 
 // Joins the (maximum, sum) pairs of 8 tokens: 16 warps; a lane has token lane & 7 and every 64th pair, eight at a time.  The
-// target's logit is taken again as a plain fp32 product (two warps per token): the tensor core adds 16 products at a time
-// with truncation, an error of up to 2^-24 of the logit per step and of one sign, which the loss of an unlikely token would
-// show in full; its term of the sum is exchanged along with it.  The last block to finish adds the blocks' sums of losses
-// and weights, in order.  Launched behind the logits' kernel before that has finished; the products need nothing of it.
-__global__ void __launch_bounds__(kJoinThreads, 3) ce_join_kernel(const float2* part, const float* target_logit, const __nv_bfloat16* __restrict__ X,
+// pairs are of all words but the target.  Its logit is taken as a plain fp32 product here (two warps per token): the tensor
+// core adds 16 products at a time with truncation, an error of up to 2^-24 of the logit per step and of one sign, which the
+// loss of an unlikely token would show in full.  With x = log(sum over the others) - target's logit,
+//     loss = log(1 + e^x) = max(x, 0) + log(1 + e^-|x|),   lse = the larger of the two + log(1 + e^-|x|),
+// so that the loss of a likely token keeps its digits: it is about e^x, and a difference of lse and the target's logit would
+// have the rounding of those in it.  The last block to finish adds the blocks' sums of losses and weights, in order.
+// Launched behind the logits' kernel before that has finished; the products need nothing of it.
+__global__ void __launch_bounds__(kJoinThreads, 3) ce_join_kernel(const float2* part, const __nv_bfloat16* __restrict__ X,
                                                        const __nv_bfloat16* __restrict__ W, const int64_t* __restrict__ targets,
                                                        const float* __restrict__ weight, int tokens, int d, int vocab, int parts, float c,
                                                        float* __restrict__ loss, float* __restrict__ lse, float2* block_sums,
@@ -97,12 +100,12 @@ __global__ void __launch_bounds__(kJoinThreads, 3) ce_join_kernel(const float2* 
     if (lane < 8 && t < tokens) {
       const int64_t y = __ldg(targets + t);
       const bool trained = y >= 0 && y < vocab;
-      const float ty = (exact[2 * tok] + exact[2 * tok + 1]) * c;
-      if (trained) s += exp2f(ty - m) - exp2f(__ldcg(target_logit + t) - m);
-      const float l2 = s > 0.f ? m + log2f(s) : NAN;   // no word is possible, or a NaN
+      const float others = m + log2f(s), ty = trained ? (exact[2 * tok] + exact[2 * tok + 1]) * c : -INFINITY;
+      // (no word possible at all: infinity minus infinity, NaN)
+      const float x = others - ty, beside = log1pf(exp2f(-fabsf(x)));
       constexpr float kLn2 = 0.6931471805599453f;
-      lse[t] = l2 * kLn2;
-      const float l = trained ? (l2 - ty) * kLn2 : 0.f;
+      lse[t] = fmaf(x > 0.f ? others : ty, kLn2, beside);
+      const float l = trained ? fmaf(fmaxf(x, 0.f), kLn2, beside) : 0.f;
       loss[t] = l;
       wt = trained ? (weight ? __ldg(weight + t) : 1.f) : 0.f;
       wl = trained ? wt * l : 0.f;
@@ -337,15 +340,14 @@ void common(const CeProblem& q, Params* p, const int64_t* targets, const float* 
 
 struct FwdPlan {
   int parts, blocks;
-  size_t part, target, sums, ticket, bytes;
+  size_t part, sums, ticket, bytes;
 };
 FwdPlan fwd_plan(const CeProblem& q) {
   FwdPlan f;
   f.parts = is_few(q) ? 8 * std::min(ceil_div(q.vocab, ce::kTile), pair_count()) : ceil_div(q.vocab, ce::kGroupCols);   // see Params::part
   f.blocks = ceil_div(q.m, kTokensPerBlock);
   f.part = 0;
-  f.target = f.part + aligned(size_t(f.parts) * size_t(q.m) * sizeof(float2));
-  f.sums = f.target + aligned(size_t(q.m) * 4);
+  f.sums = f.part + aligned(size_t(f.parts) * size_t(q.m) * sizeof(float2));
   f.ticket = f.sums + aligned(size_t(f.blocks) * sizeof(float2));
   f.bytes = f.ticket + aligned(4);
   return f;
@@ -417,7 +419,6 @@ cudaError_t ce_fwd(const CeProblem& q, const void* X, const void* W, const int64
   p.n_tiles = ceil_div(q.vocab, ce::kTile);
   p.units = is_few(q) ? p.n_tiles : p.m_tiles * p.n_tiles;
   p.part = reinterpret_cast<float2*>(w8 + f.part);
-  p.target_logit = reinterpret_cast<float*>(w8 + f.target);
   p.ticket = reinterpret_cast<uint32_t*>(w8 + f.ticket);
   CUtensorMap ta, tb;
   const bool few = is_few(q);
@@ -426,7 +427,7 @@ cudaError_t ce_fwd(const CeProblem& q, const void* X, const void* W, const int64
   const cudaError_t e = launch<ce::LSE>(few, ta, tb, ta, tb, ta, ta, ta, p, st);
   if (e != cudaSuccess) return e;
   return launch_lined_up(ce_join_kernel, dim3(unsigned(f.blocks)), dim3(kJoinThreads), 0, st, static_cast<const float2*>(p.part),
-                       static_cast<const float*>(p.target_logit), static_cast<const __nv_bfloat16*>(X), static_cast<const __nv_bfloat16*>(W),
+                       static_cast<const __nv_bfloat16*>(X), static_cast<const __nv_bfloat16*>(W),
                        targets, weight, p.tokens, p.d, p.vocab, f.parts, q.logit_scale * ce::kLog2e, loss, lse, reinterpret_cast<float2*>(w8 + f.sums), p.ticket, total);
 }
 

@@ -1,8 +1,8 @@
 // The tcgen05 kernels of the vocabulary cross entropy: persistent, warp-specialised, on pairs of CTAs (a cluster of two
 // drives tcgen05.mma.cta_group::2 on a tile of 256 x 256).  Three kinds share the mainloop and differ in their epilogue:
 //
-//   LSE      logits tile = X W^T; every row of the tile leaves its maximum and its sum of exponentials over 64 columns
-//            (and the logit of its target, where the tile holds it): 32 bytes instead of 1 KiB of fp32 logits;
+//   LSE      logits tile = X W^T; every row of the tile leaves its maximum and its sum of exponentials over 64 columns,
+//            its target's left out: 32 bytes instead of 1 KiB of fp32 logits;
 //   DLOGITS  the same tile again, now D = w (exp(logit - lse) - onehot), rounded to bf16, for one piece of the vocabulary;
 //   GRADS    both products of a finished piece in one launch: dX += D W_piece (split over the piece when there are few
 //            tiles; fp32 sums in global memory, added by the bulk-copy engine) and dW_piece = D^T X (bf16, complete).
@@ -88,8 +88,8 @@ struct Params {
   const int64_t* targets;
   const float* lse;             // natural logarithm
   const float* weight;          // may be null: one
-  float2* part;                 // LSE: [.][tokens] (maximum, sum) in base 2: of 64 columns each; FEW: of what 32 lanes met
-  float* target_logit;          // LSE: [tokens], base 2
+  float2* part;                 // LSE: [.][tokens] (maximum, sum) in base 2 of all words but the target: of 64 columns each;
+                                // FEW: of what 32 lanes met
   uint32_t* ticket;             // LSE: set to zero for the kernel behind it
   float* corr;                  // DLOGITS: [tokens] what rounding took from the target's element of D
   const int* row_key;           // GRADS: [tokens], may be null: the row of dW that `row_add` belongs to, -1: none
@@ -514,12 +514,20 @@ __global__ void __launch_bounds__(kThreads, 1)
           ptx::tmem_ld_x16(few_addr, v);
           ptx::tmem_ld_wait();
           const bool word = KIND != GRADS && p.v0 + row < p.vocab;   // this lane's row is a word of the vocabulary
+          // the targets among this warp's words: of tokens `hits`, each a word `r` of it
+          const int r = few_y < 0 ? -1 : few_y - (p.v0 + row0);
+          const uint32_t hits = KIND != GRADS ? __ballot_sync(0xFFFFFFFFu, r >= 0 && r < 32) : 0u;
           if (KIND == LSE) {
+            uint32_t mine = 0u;                // tokens whose target is this lane's word
+            for (uint32_t h = hits; h; h &= h - 1) {
+              const int j = __ffs(h) - 1;
+              if (__shfl_sync(0xFFFFFFFFu, r, j) == lane) mine |= 1u << j;
+            }
             if (word) {
 #pragma unroll
               for (int j = 0; j < kFew; ++j) {
                 const int k = FEW && KIND == LSE ? j : 0;
-                const float x = __uint_as_float(v[j]) * p.c, top = fmaxf(few_m[k], x);
+                const float x = (mine >> j) & 1u ? -INFINITY : __uint_as_float(v[j]) * p.c, top = fmaxf(few_m[k], x);
                 few_s[k] = few_s[k] * exp2_fast(few_m[k] - top) + exp2_fast(x - top);
                 few_m[k] = top;
               }
@@ -539,13 +547,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                 else atomicAdd(o + int64_t(j) * p.d, __uint_as_float(v[j]));
               }
           }
-          if (KIND != GRADS) {               // the targets among this warp's words
-            const int r = few_y < 0 ? -1 : few_y - (p.v0 + row0);
-            for (uint32_t hits = __ballot_sync(0xFFFFFFFFu, r >= 0 && r < 32); hits; hits &= hits - 1) {
-              const int j = __ffs(hits) - 1, owner = __shfl_sync(0xFFFFFFFFu, r, j), tt = few0 + j;
+          if (KIND == DLOGITS) {
+            for (uint32_t h = hits; h; h &= h - 1) {
+              const int j = __ffs(h) - 1, owner = __shfl_sync(0xFFFFFFFFu, r, j), tt = few0 + j;
               const float x = __uint_as_float(ptx::tmem_ld_x1(few_addr + j));
-              if (lane == owner && KIND == LSE) p.target_logit[tt] = x * p.c;
-              if (lane == owner && KIND == DLOGITS) {
+              if (lane == owner) {
                 const float w1 = few_w[j];
                 float e = w1 * exp2_fast(fmaf(x, p.c, -few_lse2[j])) - w1;
                 if (p.vocab == 1 && e == e) e = 0.f;   // one word is certain: the difference would be its rounding only
@@ -582,22 +588,15 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (valid > 32) ptx::tmem_ld_x32(taddr + 32, w[1]);
           ptx::tmem_ld_wait();
           release_accumulator();
-          // exponents are w c - max(w c); with a negative c, or columns that do not exist, the products are made first
+          // exponents are w c - max(w c); where c is negative, or columns do not exist or are a target, the products are made first
           float c1 = p.c;
-          if (c1 < 0.f || valid < kGroupCols) {
+          if (c1 < 0.f || valid < kGroupCols || target_here) {
 #pragma unroll
             for (int c = 0; c < 2; ++c)
 #pragma unroll
-              for (int i = 0; i < 32; ++i) w[c][i] = __float_as_uint(32 * c + i < valid ? __uint_as_float(w[c][i]) * c1 : -INFINITY);
+              for (int i = 0; i < 32; ++i)
+                w[c][i] = __float_as_uint(32 * c + i < valid && 32 * c + i != tc ? __uint_as_float(w[c][i]) * c1 : -INFINITY);
             c1 = 1.f;
-          }
-          if (target_here) {
-            float tl = 0.f;
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-              for (int i = 0; i < 32; ++i) tl = tc == 32 * c + i ? __uint_as_float(w[c][i]) : tl;
-            if (tc >= 0 && tc < kGroupCols) p.target_logit[row] = tl * c1;
           }
           float top[4];
 #pragma unroll

@@ -83,3 +83,38 @@ def test_logits_of_minus_infinity(t, d, v):
     # and no possible word at all: nothing to be said
     W[:, 0] = -2.0 ** 20
     assert np.isnan(run(X, W, y, backward=False)["lse"]).all()
+
+
+def _certain(t, v, d, shift, seed):
+    """Tokens whose target's logit stands 8 to 26 above `shift`, the other words' around it."""
+    g = np.random.Generator(np.random.Philox(seed))
+    W = I.gaussian((v, d), seed + 1, d ** -0.5, "bf16")
+    W[:, 0] = 1.0
+    y = g.integers(0, v, t)
+    rest = W[:, 1:].astype(np.float64)
+    X = np.zeros((t, d))
+    X[:, 0] = shift
+    X[:, 1:] = 0.3 * I.gaussian((t, d - 1), seed + 2) + np.linspace(8, 26, t)[:, None] * rest[y] / (rest[y] ** 2).sum(1, keepdims=True)
+    return I.round_to_dtype(X.astype(np.float32), "bf16"), W, y
+
+
+@pytest.mark.parametrize("t", [40, 300])
+@pytest.mark.parametrize("shift", [0.0, 24.0])
+@pytest.mark.parametrize("v", [1, 2, 1000])
+def test_loss_of_almost_certain_tokens(t, shift, v):
+    """The loss is known relative to itself: log(1 + sum over the others / the target's), not a difference of two logits."""
+    d = 64
+    X, W, y = _certain(t, v, d, shift, 11 + v)
+    loss, lse, _ = C.ce_fwd(X, W, y)
+    L = C.logits(X, W)
+    with np.errstate(divide="ignore"):
+        others = np.exp(L - L[np.arange(t), y][:, None])
+        others[np.arange(t), y] = 0
+        loss = np.log1p(others.sum(1))               # (the oracle's difference in 64 bits has 1e-15 of the logits left)
+    o = run(X, W, y, backward=False)
+    # a logit's error, and the roundings of the two logarithms' difference and of the result
+    e = 2.0 ** -23 * (d / 16 + 8) * (np.abs(X).astype(np.float64) @ np.abs(W).astype(np.float64).T).max(1) + 2.0 ** -21
+    assert np.all(np.abs(o["loss"] - loss) <= 2 * e * loss)
+    assert np.all(o["loss"] >= 0) and np.all(np.abs(o["lse"] - lse) <= e + 2.0 ** -22 * np.abs(lse))
+    if v == 1000:
+        assert loss.min() < 2e-6 and loss.max() > 0.1     # what the inputs are meant to cover
