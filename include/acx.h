@@ -344,7 +344,10 @@ ACX_API acx_status acx_linear_ce_fwd(const acx_ce_desc* desc, const void* X, con
 
 /* Backward, of scale * (sum of weight * loss) / denom:
  *     D = weight (exp(logits - lse) - onehot(y)),   dX = f D W,   dW = f D^T X,   f = scale * logit_scale / denom.
- *   lse: from the forward.   denom: one fp32 number on the device, or NULL (one); f = 0 where it is not positive.
+ *   lse: from the forward.   acx_linear_ce_bwd_loss: loss: from the forward too (or NULL, as without it).  A target's own element of
+ *   D is then weight (exp(-loss) - 1) to its last digits.  From lse alone it is known to about 2^-23 (1 + |lse|): enough for
+ *   tokens that are not yet certain; of 1 - p below that nothing is left.
+ *   denom: one fp32 number on the device, or NULL (one); f = 0 where it is not positive.
  *   dX [tokens x d], dW [vocab x d] bfloat16, out; one of them may be NULL.
  *   The vocabulary is taken in pieces: the logits of a piece are computed again, its D is held in bfloat16 in the workspace
  *   until both products have used it, dX is summed over the pieces in fp32 and rounded once; what the rounding of D takes
@@ -353,6 +356,9 @@ ACX_API acx_status acx_linear_ce_fwd(const acx_ce_desc* desc, const void* X, con
 ACX_API acx_status acx_linear_ce_bwd(const acx_ce_desc* desc, const void* X, const void* W, const int64_t* targets, const float* weight,
                                      const float* lse, const float* denom, float scale, void* dX, void* dW, void* ws, size_t ws_bytes,
                                      void* cuda_stream);
+ACX_API acx_status acx_linear_ce_bwd_loss(const acx_ce_desc* desc, const void* X, const void* W, const int64_t* targets, const float* weight,
+                                          const float* lse, const float* loss, const float* denom, float scale, void* dX, void* dW, void* ws,
+                                          size_t ws_bytes, void* cuda_stream);
 
 /* Synchronises the stream and returns ACX_ERR_TIMEOUT if any kernel on this device since the last call gave up on
  * a bounded wait (its outputs are then undefined), ACX_ERR_CUDA on a CUDA error, else ACX_OK.  Clears the flag.  The

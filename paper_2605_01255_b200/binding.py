@@ -32,7 +32,7 @@ EXPORTS = (
     "acx_linear_bwd_factor_builtin_scratch", "acx_reconstruct_adamw", "acx_debug_expired_wait",
     "acx_debug_force_gemm_mode", "acx_linear_fwd_v", "acx_reconstruct_v", "acx_lowrank_adamw", "acx_rsvd_factor", "acx_linear_fwd_bias", "acx_bias_grad", "acx_linear_bwd_bias",
     "acx_rows_workspace_bytes", "acx_q8_store", "acx_q8_load", "acx_swiglu_fwd", "acx_swiglu_bwd", "acx_norm_join_fwd", "acx_norm_join_bwd",
-    "acx_ce_workspace_bytes", "acx_linear_ce_fwd", "acx_linear_ce_bwd",
+    "acx_ce_workspace_bytes", "acx_linear_ce_fwd", "acx_linear_ce_bwd", "acx_linear_ce_bwd_loss",
 )
 
 
@@ -104,6 +104,7 @@ def lib() -> ctypes.CDLL:
         L.acx_ce_workspace_bytes.restype, L.acx_ce_workspace_bytes.argtypes = sz, [cp, ctypes.c_int]
         L.acx_linear_ce_fwd.restype, L.acx_linear_ce_fwd.argtypes = ctypes.c_int, [cp] + [vp] * 8 + [sz, vp]
         L.acx_linear_ce_bwd.restype, L.acx_linear_ce_bwd.argtypes = ctypes.c_int, [cp] + [vp] * 6 + [f32, vp, vp, vp, sz, vp]
+        L.acx_linear_ce_bwd_loss.restype, L.acx_linear_ce_bwd_loss.argtypes = ctypes.c_int, [cp] + [vp] * 7 + [f32, vp, vp, vp, sz, vp]
         L.acx_sketch_materialize.restype, L.acx_sketch_materialize.argtypes = ctypes.c_int, [dp, vp, vp]
         L.acx_last_device_status.restype, L.acx_last_device_status.argtypes = ctypes.c_int, [vp]
         L.acx_debug_expired_wait.restype, L.acx_debug_expired_wait.argtypes = ctypes.c_int, [ctypes.c_uint64, vp]
@@ -358,7 +359,7 @@ def _calls():
             raise RuntimeError("_acx_host.so is not built for this torch; run `python -m paper_2605_01255_b200.build`") from e
         _acx_host.bind(tuple(ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in (
             "acx_q8_store", "acx_q8_load", "acx_swiglu_fwd", "acx_swiglu_bwd", "acx_norm_join_fwd", "acx_norm_join_bwd",
-            "acx_linear_ce_fwd", "acx_linear_ce_bwd")))
+            "acx_linear_ce_fwd", "acx_linear_ce_bwd_loss")))
         _host = _acx_host
     return _host
 
@@ -417,8 +418,9 @@ def acx_linear_ce_fwd(desc: acx_ce_desc, X, W, targets, loss, lse, total=None, w
     _check((_host or _calls()).linear_ce_fwd(desc, X, W, targets, weight, loss, lse, total, ws, stream), "acx_linear_ce_fwd")
 
 
-def acx_linear_ce_bwd(desc: acx_ce_desc, X, W, targets, lse, dX, dW, *, weight=None, denom=None, scale: float = 1.0, ws=None,
+def acx_linear_ce_bwd(desc: acx_ce_desc, X, W, targets, lse, dX, dW, *, loss=None, weight=None, denom=None, scale: float = 1.0, ws=None,
                       stream=None) -> None:
     """Gradients of scale * sum(weight * loss) / denom (denom: one fp32 number on the device, such as total[1:]); dX or dW may be
-    None; ws: alloc_ce_workspace(desc, ACX_OP_CE_BWD)."""
-    _check((_host or _calls()).linear_ce_bwd(desc, X, W, targets, weight, lse, denom, scale, dX, dW, ws, stream), "acx_linear_ce_bwd")
+    None; loss: the forward's, so that the gradients of almost certain tokens keep their digits (see acx.h); ws:
+    alloc_ce_workspace(desc, ACX_OP_CE_BWD)."""
+    _check((_host or _calls()).linear_ce_bwd(desc, X, W, targets, weight, lse, loss, denom, scale, dX, dW, ws, stream), "acx_linear_ce_bwd")

@@ -11,6 +11,7 @@
 namespace acx {
 namespace {
 
+using ce::kLn2;
 using ce::kLowest;
 using ce::Params;
 
@@ -103,7 +104,6 @@ __global__ void __launch_bounds__(kJoinThreads, 3) ce_join_kernel(const float2* 
       const float others = m + log2f(s), ty = trained ? (exact[2 * tok] + exact[2 * tok + 1]) * c : -INFINITY;
       // (no word possible at all: infinity minus infinity, NaN)
       const float x = others - ty, beside = log1pf(exp2f(-fabsf(x)));
-      constexpr float kLn2 = 0.6931471805599453f;
       lse[t] = fmaf(x > 0.f ? others : ty, kLn2, beside);
       const float l = trained ? fmaf(fmaxf(x, 0.f), kLn2, beside) : 0.f;
       loss[t] = l;
@@ -439,7 +439,7 @@ cudaError_t ce_fwd(const CeProblem& q, const void* X, const void* W, const int64
 // writes the buffer that G0 read) finds G0 finished, and G1 adds to sums that G0 has finished.  L0 needs the forward's
 // results, and the last G follows another G, to whose sums it adds (or its own L): those two wait first.
 cudaError_t ce_bwd(const CeProblem& q, const void* X, const void* W, const int64_t* targets, const float* weight, const float* lse,
-                   const float* denom, float scale, void* dX, void* dW, void* ws, int* status, cudaStream_t st) {
+                   const float* loss, const float* denom, float scale, void* dX, void* dW, void* ws, int* status, cudaStream_t st) {
   const BwdPlan b = bwd_plan(q);
   uint8_t* w8 = static_cast<uint8_t*>(ws);
   const int64_t piece_cols = int64_t(b.piece_tiles) * ce::kTile;
@@ -448,6 +448,7 @@ cudaError_t ce_bwd(const CeProblem& q, const void* X, const void* W, const int64
   Params p{};
   common(q, &p, targets, weight, status);
   p.lse = lse;
+  p.loss = loss;
   p.corr = corr;
   p.acc = acc;
   p.ld_d = piece_cols;

@@ -61,6 +61,12 @@ acx_status acx_linear_ce_fwd(const acx_ce_desc* desc, const void* X, const void*
 acx_status acx_linear_ce_bwd(const acx_ce_desc* desc, const void* X, const void* W, const int64_t* targets, const float* weight,
                              const float* lse, const float* denom, float scale, void* dX, void* dW, void* ws, size_t ws_bytes,
                              void* cuda_stream) {
+  return acx_linear_ce_bwd_loss(desc, X, W, targets, weight, lse, nullptr, denom, scale, dX, dW, ws, ws_bytes, cuda_stream);
+}
+
+acx_status acx_linear_ce_bwd_loss(const acx_ce_desc* desc, const void* X, const void* W, const int64_t* targets, const float* weight,
+                                  const float* lse, const float* loss, const float* denom, float scale, void* dX, void* dW, void* ws,
+                                  size_t ws_bytes, void* cuda_stream) {
   CeProblem p;
   const acx_status s = validate_ce(desc, &p);
   if (s != ACX_OK) return s;
@@ -71,11 +77,11 @@ acx_status acx_linear_ce_bwd(const acx_ce_desc* desc, const void* X, const void*
     return dW ? from_cuda(cudaMemsetAsync(dW, 0, size_t(p.vocab) * size_t(p.d) * 2, st)) : ACX_OK;
   }
   if (any_null(X, W, targets, lse) || (!dX && !dW)) return ACX_ERR_INVALID_ARG;
-  if (any_misaligned(X, W, targets, weight, lse, dX, dW, ws) || (reinterpret_cast<uintptr_t>(denom) & 3u)) return ACX_ERR_ALIGNMENT;
+  if (any_misaligned(X, W, targets, weight, lse, loss, dX, dW, ws) || (reinterpret_cast<uintptr_t>(denom) & 3u)) return ACX_ERR_ALIGNMENT;
   if (!ws || ws_bytes < ce_bwd_workspace_bytes(p)) return ACX_ERR_WORKSPACE;
   int* status = device_status_ptr();
   if (!status) return ACX_ERR_CUDA;
-  return from_cuda(ce_bwd(p, X, W, targets, weight, lse, denom, scale, dX, dW, ws, status, st));
+  return from_cuda(ce_bwd(p, X, W, targets, weight, lse, loss, denom, scale, dX, dW, ws, status, st));
 }
 
 }  // extern "C"

@@ -62,7 +62,7 @@ constexpr int kSmemBytes = kOutOffset + kEpiWarps * kBoxBytes + 1024;
 static_assert(kSmemBytes <= 232448, "shared memory of one CTA");
 
 enum Kind { LSE = 0, DLOGITS = 1, GRADS = 2 };
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // The maximum of logits of which none is more than minus infinity, with a sum of zero: a finite number, so that no difference
 // of two maxima is one of infinities (which would turn a sum that holds nothing into a NaN).
 constexpr float kLowest = -0x1.fffffep127f;
@@ -87,6 +87,7 @@ struct Params {
   float c;                      // logit_scale * log2(e): exponents are taken in base 2
   const int64_t* targets;
   const float* lse;             // natural logarithm
+  const float* loss;            // DLOGITS: may be null; minus the logarithm of the target's probability
   const float* weight;          // may be null: one
   float2* part;                 // LSE: [.][tokens] (maximum, sum) in base 2 of all words but the target: of 64 columns each;
                                 // FEW: of what 32 lanes met
@@ -173,6 +174,9 @@ __device__ __forceinline__ void tma_reduce_add_2d(const CUtensorMap* map, uint32
 
 // LSE, DLOGITS: tmap_a = X (64 x 128 boxes), tmap_b = W (64 x 128 boxes), tmap_out = D (DLOGITS).
 // FEW: the maps of X and of D as rows of tokens have boxes of 64 x few_n / 2.
+// DLOGITS, the target's element: w (p - 1) = w expm1(log p), with log p = -loss where the losses are given.  Without them log p is the
+// difference of the logit and the rounded log-sum-exp, good to about 2^-23 of those: nothing of 1 - p is left of it where
+// that is smaller.
 // GRADS: tmap_a = D as rows of tokens (64 x 128 boxes), tmap_a2 = D read MN-major (64 x 64 boxes), tmap_b = W, tmap_b2 = X
 // (both 64 x 64 boxes, MN-major), tmap_out = the fp32 sums of dX (32 x 16 boxes), tmap_out2 = dW (64 x 16 boxes), tmap_out3 =
 // dW (32 x 32 boxes, 64-byte swizzle).
@@ -447,6 +451,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     float few_m[FEW && KIND == LSE ? kFew : 1], few_s[FEW && KIND == LSE ? kFew : 1];
     float* const few_lse2 = reinterpret_cast<float*>(out_gen);
     float* const few_w = few_lse2 + 32;
+    float* const few_loss = few_lse2 + 64;
     if (FEW) {
       const int tt = few0 + lane;
       if (KIND != GRADS && lane < kFew && tt < p.tokens) {
@@ -456,6 +461,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (KIND == DLOGITS) {
         few_lse2[lane] = few_y >= 0 ? __ldcg(p.lse + tt) * kLog2e : 0.f;
         few_w[lane] = few_y >= 0 ? (p.weight ? __ldcg(p.weight + tt) : 1.f) : 0.f;
+        few_loss[lane] = few_y >= 0 && p.loss ? __ldcg(p.loss + tt) : 0.f;
         __syncwarp();
       }
       if (KIND == LSE) {
@@ -469,16 +475,22 @@ __global__ void __launch_bounds__(kThreads, 1)
     // What a lane's row needs besides the accumulator, asked for one tile ahead (from L2 it takes longer than a small tile)
     struct RowNeeds {
       int2 y;          // the target, as it is in memory
-      float lse, weight;
+      float lse, weight, loss;
+    };
+    // e: the target's element of D, from log p = -loss or (without losses) from the logit's exponent x less the log-sum-exp in base 2
+    auto target_element = [&](float w, float loss, float x) {
+      const float e = w * expm1f(p.loss ? -loss : x * kLn2);
+      return !p.loss && p.vocab == 1 && e == e ? 0.f : e;   // one word is certain: the difference would be its rounding only
     };
     auto needs_of = [&](int m0) {
-      RowNeeds n{make_int2(-1, -1), 0.f, 1.f};
+      RowNeeds n{make_int2(-1, -1), 0.f, 1.f, 0.f};
       const int r = m0 + int(rank) * kBM + quarter * 32 + lane;
       if (!FEW && KIND != GRADS && r < p.tokens) {
         n.y = __ldcg(reinterpret_cast<const int2*>(p.targets) + r);
         if (KIND == DLOGITS) {
           n.lse = __ldcg(p.lse + r);
           if (p.weight) n.weight = __ldcg(p.weight + r);
+          if (p.loss) n.loss = __ldcg(p.loss + r);
         }
       }
       return n;
@@ -494,7 +506,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int col0 = t.n0 + group * kGroupCols;               // of the output; LSE, DLOGITS: of the piece
       // a target outside [0, vocab): not trained on
       const int y = needs.y.y == 0 && uint32_t(needs.y.x) < uint32_t(p.vocab) ? needs.y.x : -1;
-      const float lse2 = needs.lse * kLog2e, weight = y >= 0 ? needs.weight : 0.f;
+      const float lse2 = needs.lse * kLog2e, weight = y >= 0 ? needs.weight : 0.f, loss = needs.loss;
       needs = needs_of(ahead.m0);
       const int add_token = (KIND == GRADS && !t.x && p.row_key) ? find_row_add(p.v0 + row0) : -1;
       const bool full_ok = ptx::mbar_wait_cluster(tfull_bar(acc), (it >> 1) & 1, abort_flag);
@@ -552,9 +564,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               const int j = __ffs(h) - 1, owner = __shfl_sync(0xFFFFFFFFu, r, j), tt = few0 + j;
               const float x = __uint_as_float(ptx::tmem_ld_x1(few_addr + j));
               if (lane == owner) {
-                const float w1 = few_w[j];
-                float e = w1 * exp2_fast(fmaf(x, p.c, -few_lse2[j])) - w1;
-                if (p.vocab == 1 && e == e) e = 0.f;   // one word is certain: the difference would be its rounding only
+                const float e = target_element(few_w[j], few_loss[j], fmaf(x, p.c, -few_lse2[j]));
                 const __nv_bfloat16 b = __float2bfloat16_rn(e);
                 p.D[int64_t(tt) * p.ld_d + row] = b;
                 p.corr[tt] = e - __bfloat162float(b);
@@ -630,8 +640,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
               for (int i = 0; i < 32; ++i) l = tc == 32 * c + i ? __uint_as_float(v[i]) : l;
               if (tc >= 32 * c && tc < 32 * c + 32) {
-                float e = weight * exp2_fast(fmaf(l, p.c, -lse2)) - weight;
-                if (p.vocab == 1 && e == e) e = 0.f;   // one word is certain: the difference would be its rounding only
+                const float e = target_element(weight, loss, fmaf(l, p.c, -lse2));
                 target_bits = pack2(__float_as_uint(e), 0u);
                 p.corr[row] = e - __uint_as_float(target_bits << 16);
               }

@@ -162,7 +162,7 @@ cudaError_t ce_fwd(const CeProblem& p, const void* X, const void* W, const int64
                    float* total, void* ws, int* status, cudaStream_t st);
 size_t ce_bwd_workspace_bytes(const CeProblem& p);
 cudaError_t ce_bwd(const CeProblem& p, const void* X, const void* W, const int64_t* targets, const float* weight, const float* lse,
-                   const float* denom, float scale, void* dX, void* dW, void* ws, int* status, cudaStream_t st);
+                   const float* loss, const float* denom, float scale, void* dX, void* dW, void* ws, int* status, cudaStream_t st);
 
 // Test/debug: overrides the tile-shape cost models of the forward and dX (0 = off, 1..4 = a GEMM mode).
 void sm100_force_gemm_mode(int mode);

@@ -26,7 +26,7 @@ struct Entries {
   decltype(&acx_norm_join_fwd) norm_join_fwd;
   decltype(&acx_norm_join_bwd) norm_join_bwd;
   decltype(&acx_linear_ce_fwd) linear_ce_fwd;
-  decltype(&acx_linear_ce_bwd) linear_ce_bwd;
+  decltype(&acx_linear_ce_bwd_loss) linear_ce_bwd;
 } entries;
 constexpr int kEntries = sizeof(Entries) / sizeof(void*);
 
@@ -268,12 +268,13 @@ acx_status linear_ce_bwd(PyObject* const* a) {
   const int64_t* const targets = dense<int64_t>(a[3], "targets", c.row, at::kLong);
   const float* const weight = c.row_f32(a[4], "weight");
   const float* const lse = c.row_f32(a[5], "lse");
-  const float* const denom = dense<float>(a[6], "denom", one, at::kFloat);
-  const float scale = number(a[7]);
-  void *const dX = dense(a[8], "dX", c.x, at::kBFloat16), *const dW = dense(a[9], "dW", c.w, at::kBFloat16);
-  const Workspace ws(a[10]);
-  void* const st = stream(a[11]);
-  return without_gil([&] { return entries.linear_ce_bwd(&c.d, X, W, targets, weight, lse, denom, scale, dX, dW, ws.p, ws.bytes, st); });
+  const float* const loss = c.row_f32(a[6], "loss");
+  const float* const denom = dense<float>(a[7], "denom", one, at::kFloat);
+  const float scale = number(a[8]);
+  void *const dX = dense(a[9], "dX", c.x, at::kBFloat16), *const dW = dense(a[10], "dW", c.w, at::kBFloat16);
+  const Workspace ws(a[11]);
+  void* const st = stream(a[12]);
+  return without_gil([&] { return entries.linear_ce_bwd(&c.d, X, W, targets, weight, lse, loss, denom, scale, dX, dW, ws.p, ws.bytes, st); });
 }
 
 // Python entry of an operator of COUNT arguments: its acx_status as an int.
@@ -318,7 +319,7 @@ PyObject* bind(PyObject*, PyObject* addresses) {
 PyMethodDef methods[] = {
     {"bind", bind, METH_O, nullptr},
     ACX_ENTRY(q8_store, 5),       ACX_ENTRY(q8_load, 5),        ACX_ENTRY(swiglu_fwd, 9),     ACX_ENTRY(swiglu_bwd, 9),
-    ACX_ENTRY(norm_join_fwd, 17), ACX_ENTRY(norm_join_bwd, 20), ACX_ENTRY(linear_ce_fwd, 10), ACX_ENTRY(linear_ce_bwd, 12),
+    ACX_ENTRY(norm_join_fwd, 17), ACX_ENTRY(norm_join_bwd, 20), ACX_ENTRY(linear_ce_fwd, 10), ACX_ENTRY(linear_ce_bwd, 13),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_acx_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -116,8 +116,8 @@ class MlpLm:
         """Gradient of the mean loss with respect to h0; with lr > 0 every linear takes its AdamW step as soon as its factor is
         known (after the last use of its weights in this pass)."""
         s, n = self.s, self.s.inter
-        B.acx_linear_ce_bwd(self.ce, self.y, self.head, self.targets, self.lse, self.dy, self.grads["head"][0], weight=self.weight,
-                            denom=self.total[1:], ws=self.ws_ce)
+        B.acx_linear_ce_bwd(self.ce, self.y, self.head, self.targets, self.lse, self.dy, self.grads["head"][0], loss=self.loss,
+                            weight=self.weight, denom=self.total[1:], ws=self.ws_ce)
         dh = None
         for l in range(s.layers - 1, -1, -1):
             out = self.dh[l % 2]

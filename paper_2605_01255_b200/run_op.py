@@ -65,7 +65,7 @@ def _linear_ce(m, d_in, d_out, tdt):
 
     def run():
         B.acx_linear_ce_fwd(d, X, W, y, loss, lse, total, ws=ws)
-        B.acx_linear_ce_bwd(d, X, W, y, lse, dX, dW, denom=total[1:], ws=ws)
+        B.acx_linear_ce_bwd(d, X, W, y, lse, dX, dW, loss=loss, denom=total[1:], ws=ws)
     return run
 
 

@@ -14,7 +14,7 @@ pytestmark = pytest.mark.gpu
 NAN = float("nan")
 
 
-def run(X, W, y, weight=None, logit_scale=1.0, backward=True, scale=1.0):
+def run(X, W, y, weight=None, logit_scale=1.0, backward=True, scale=1.0, with_loss=True):
     """Outputs of a forward and a backward call, by name; numpy float64."""
     (t, d), v = X.shape, W.shape[0]
     desc = B.make_ce_desc(t, d, v, logit_scale)
@@ -26,7 +26,8 @@ def run(X, W, y, weight=None, logit_scale=1.0, backward=True, scale=1.0):
     B.acx_linear_ce_fwd(desc, Xd, Wd, yd, o["loss"], o["lse"], o["total"], wd, ws)
     if backward:
         o["dX"], o["dW"] = torch.full_like(Xd, NAN), torch.full_like(Wd, NAN)
-        B.acx_linear_ce_bwd(desc, Xd, Wd, yd, o["lse"], o["dX"], o["dW"], weight=wd, scale=scale, ws=ws)
+        B.acx_linear_ce_bwd(desc, Xd, Wd, yd, o["lse"], o["dX"], o["dW"], loss=o["loss"] if with_loss else None, weight=wd, scale=scale,
+                            ws=ws)
     assert B.acx_last_device_status() == B.ACX_OK
     return {k: to_host(a) for k, a in o.items()}
 
@@ -66,8 +67,6 @@ def test_logits_of_minus_infinity(t, d, v):
         assert np.all(np.abs(o["lse"] - lse) <= e) and np.all(np.abs(o["loss"] - loss) <= 2 * e)
         assert abs(o["total"][0] - total[0]) <= np.sum(2 * e) + 2.0 ** -20 * np.sum(loss)
         assert not o["dW"][gone].any()
-        if len(left) == 1:             # (one word is certain: its gradients are a rounding error's)
-            continue
         dX, dW = C.ce_bwd(X, W, y)
         D = np.abs(C.ce_dlogits(X, W, y))
         per_d = 2.0 ** -8 * D + 4 * e[:, None] * np.minimum(D + 1, D * 4 + 1e-30)
@@ -118,3 +117,47 @@ def test_loss_of_almost_certain_tokens(t, shift, v):
     assert np.all(o["loss"] >= 0) and np.all(np.abs(o["lse"] - lse) <= e + 2.0 ** -22 * np.abs(lse))
     if v == 1000:
         assert loss.min() < 2e-6 and loss.max() > 0.1     # what the inputs are meant to cover
+
+
+@pytest.mark.parametrize("t", [40, 300])
+@pytest.mark.parametrize("shift", [0.0, 24.0])
+@pytest.mark.parametrize("v", [1, 2, 1000])
+def test_gradients_of_almost_certain_tokens(t, shift, v):
+    """With the forward's losses a token's gradient is right relative to 1 - p, however small that is."""
+    d = 64
+    X, W, y = _certain(t, v, d, shift, 31 + v)
+    w = (0.5 + np.random.Generator(np.random.Philox(5)).random(t)).astype(np.float32)
+    at = np.arange(t)
+    L = C.logits(X, W)
+    D = np.exp(L - L.max(1, keepdims=True))
+    D /= D.sum(1, keepdims=True)
+    D[at, y] = 0.0
+    rest = D.sum(1)
+    D[at, y] = -rest                                  # p - 1 without the difference
+    D *= w[:, None]
+    o = run(X, W, y, w, scale=2.0)
+    e = 2.0 ** -23 * (d / 16 + 8) * (np.abs(X).astype(np.float64) @ np.abs(W).astype(np.float64).T).max(1) + 2.0 ** -20
+    e += 2.0 ** -22 * np.abs(C.ce_fwd(X, W, y)[1])   # the log-sum-exp is a 32-bit number
+    A = np.abs(D)
+    # bf16 elements of D (half a unit: 2^-8 of it; the target's is made good in fp32), their exponents, sums on the tensor core
+    rel = np.full_like(A, 2.0 ** -8)
+    rel_x = rel.copy()
+    rel_x[at, y] = 0.0
+    for name, want, mag in (("dX", 2 * (D @ W.astype(np.float64)), 2 * ((A * (rel_x + 2 * e[:, None] + 2.0 ** -23 * (v / 16 + 40))) @ np.abs(W.astype(np.float64)))),
+                            ("dW", 2 * (D.T @ X.astype(np.float64)), 2 * ((A * (rel + 2 * e[:, None] + 2.0 ** -23 * (t / 16 + 40))).T @ np.abs(X.astype(np.float64))))):
+        assert np.all(np.abs(o[name] - want) <= mag + 2.0 ** -8 * np.abs(want) + 1e-37), name
+    if v == 1:
+        assert not o["dX"].any() and not o["dW"].any()
+
+
+def test_losses_of_another_type_or_shape_are_refused():
+    X, W, y = _certain(9, 40, 64, 0.0, 3)
+    d, Xd, Wd, yd = B.make_ce_desc(9, 64, 40), to_device(X, "bf16"), to_device(W, "bf16"), torch.from_numpy(y).cuda()
+    lse, ws = torch.zeros(9, device="cuda"), B.alloc_ce_workspace(B.make_ce_desc(9, 64, 40), B.ACX_OP_CE_BWD)
+    launches = B.acx_kernel_launches()
+    for bad in (lse.double(), lse[:8].clone(), lse.cpu(), torch.zeros(18, device="cuda")[::2]):
+        with pytest.raises(ValueError, match="loss must be"):
+            B.acx_linear_ce_bwd(d, Xd, Wd, yd, lse, torch.empty_like(Xd), torch.empty_like(Wd), loss=bad, ws=ws)
+    with pytest.raises(B.AcxError) as err:
+        B.acx_linear_ce_bwd(d, Xd, Wd, yd, lse, torch.empty_like(Xd), torch.empty_like(Wd), loss=torch.zeros(16, device="cuda")[1:10], ws=ws)
+    assert err.value.status == B.ACX_ERR_ALIGNMENT and B.acx_kernel_launches() == launches
