@@ -448,6 +448,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     constexpr int kFew = 16;
     const int few0 = kFew * group;
     int few_y = -1;
+    uint32_t few_trained = 0u;               // which of the tokens are trained on
     float few_m[FEW && KIND == LSE ? kFew : 1], few_s[FEW && KIND == LSE ? kFew : 1];
     float* const few_lse2 = reinterpret_cast<float*>(out_gen);
     float* const few_w = few_lse2 + 32;
@@ -458,6 +459,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int64_t y = __ldcg(p.targets + tt);
         few_y = y >= 0 && y < p.vocab ? int(y) : -1;
       }
+      few_trained = __ballot_sync(0xFFFFFFFFu, few_y >= 0);
       if (KIND == DLOGITS) {
         few_lse2[lane] = few_y >= 0 ? __ldcg(p.lse + tt) * kLog2e : 0.f;
         few_w[lane] = few_y >= 0 ? (p.weight ? __ldcg(p.weight + tt) : 1.f) : 0.f;
@@ -547,8 +549,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           } else if (KIND == DLOGITS) {
 #pragma unroll
             for (int j = 0; j < kFew; ++j) {
-              const float w1 = few_w[j], e = w1 * exp2_fast(fmaf(__uint_as_float(v[j]), p.c, -few_lse2[j]));
-              if (few0 + j < p.tokens) p.D[int64_t(few0 + j) * p.ld_d + row] = __float2bfloat16_rn(word && w1 != 0.f ? e : 0.f);
+              const float e = few_w[j] * exp2_fast(fmaf(__uint_as_float(v[j]), p.c, -few_lse2[j]));
+              if (few0 + j < p.tokens) p.D[int64_t(few0 + j) * p.ld_d + row] = __float2bfloat16_rn(word && (few_trained >> j & 1u) ? e : 0.f);
             }
           } else if (row < p.d) {
             float* o = p.acc + (int64_t(t.split) * p.acc_rows + few0) * p.d + row;

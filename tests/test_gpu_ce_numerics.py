@@ -161,3 +161,21 @@ def test_losses_of_another_type_or_shape_are_refused():
     with pytest.raises(B.AcxError) as err:
         B.acx_linear_ce_bwd(d, Xd, Wd, yd, lse, torch.empty_like(Xd), torch.empty_like(Wd), loss=torch.zeros(16, device="cuda")[1:10], ws=ws)
     assert err.value.status == B.ACX_ERR_ALIGNMENT and B.acx_kernel_launches() == launches
+
+
+@pytest.mark.parametrize("t", TOKENS)
+def test_a_weight_of_zero_does_not_hide_a_nan(t):
+    """A token that is trained on with weight zero adds 0 * softmax: nothing, or the NaN that its row holds, however many tokens
+    there are."""
+    X, W, y = _certain(t, 300, 64, 0.0, 7)
+    w = np.ones(t, np.float32)
+    w[3] = 0.0
+    o = run(X, W, y, w)
+    assert not o["dX"][3].any() and np.isfinite(o["dW"]).all() and o["dX"][2].any()
+    X[3, 5] = np.nan
+    n = run(X, W, y, w)
+    assert np.isnan(n["loss"][3]) and np.isnan(n["dX"][3]).all() and np.isnan(n["dW"]).all()
+    assert np.array_equal(n["dX"][4:], o["dX"][4:])
+    y[3] = -100                     # not trained on: its D is zero (and zero times the NaN of X in D^T X)
+    n = run(X, W, y, w)
+    assert n["loss"][3] == 0 and not n["dX"][3].any() and np.isfinite(np.delete(n["dW"], 5, 1)).all()
