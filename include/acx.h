@@ -351,8 +351,8 @@ ACX_API acx_status acx_linear_ce_fwd(const acx_ce_desc* desc, const void* X, con
  *   dX [tokens x d], dW [vocab x d] bfloat16, out; one of them may be NULL.
  *   The vocabulary is taken in pieces: the logits of a piece are computed again, its D is held in bfloat16 in the workspace
  *   until both products have used it, dX is summed over the pieces in fp32 and rounded once; what the rounding of D takes
- *   from a target's own element is put back in fp32, into dX and, for up to 256 tokens (with more the roundings average
- *   out), into dW.  Fixed summation order: reproducible bits. */
+ *   from a target's own element is put back in fp32, into dX and, for up to 512 tokens, into dW (beyond,
+ *   dW's error is about 1.3 times that of rounding it once).  Fixed summation order: reproducible bits. */
 ACX_API acx_status acx_linear_ce_bwd(const acx_ce_desc* desc, const void* X, const void* W, const int64_t* targets, const float* weight,
                                      const float* lse, const float* denom, float scale, void* dX, void* dW, void* ws, size_t ws_bytes,
                                      void* cuda_stream);

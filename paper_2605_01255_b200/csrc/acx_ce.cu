@@ -207,8 +207,9 @@ __global__ void __launch_bounds__(256) ce_finish_kernel(const float* acc, int sp
 // target as t, in fp32 and in the order of the tokens, where t is the first of them (row_key[t] = its target; -1 for the
 // others).  A target's element is most of what its token adds to dW.  With few tokens the rounding of each would be seen in
 // full (with one to sixteen weighted tokens up to 3 times the error of rounding dW alone, more than 1.5 times in one case out
-// of four); from 256 tokens on they average out (1.3 times), so this is done for up to that many, where it takes 4 to 6 us of
-// the 35 to 150 us of a step (at 333 tokens it was 8 %).  Folding it into the products' epilogue token by token took twice as
+// of four, 1.25 to 1.3 times at 257 to 512 tokens, where it is 1.0 times with this).  Done for up to 512 tokens; it takes 4 to
+// 6 us of the 35 to 150 us of a step, and 14 us of the backward at 333 x 904 x 32003, whose products wait for it (101 -> 115
+// us).  Folding it into the products' epilogue token by token took twice as
 // long: targets are skewed, and a frequent word's tokens all meet one lane there.
 using ce::kPutBackTokens;
 __global__ void __launch_bounds__(kPutBackTokens) ce_put_back_kernel(const float* corr, const int64_t* __restrict__ targets,
@@ -505,7 +506,7 @@ cudaError_t ce_bwd(const CeProblem& q, const void* X, const void* W, const int64
     return launch<ce::GRADS>(few, dk[piece % kBuffers], wmn, dmn[piece % kBuffers], xmn, accm, dwm, dwn, p, st);
   };
   cudaError_t e = cudaSuccess;
-  if (put_back) {   // few tokens: one piece as a rule; every launch needs the one before it
+  if (put_back) {   // up to 512 tokens: one piece as a rule; every launch needs the one before it
     for (int piece = 0; piece < b.pieces && e == cudaSuccess; ++piece) {
       e = dlogits(piece);
       if (e == cudaSuccess)

@@ -41,7 +41,7 @@ constexpr int kTile = 256;                 // rows and columns of a pair's tile
 constexpr int kBK = 64;                    // bf16 per stage along K: one 128-byte swizzle row
 constexpr int kUmmaK = 16;
 constexpr int kFewTokens = 64;
-constexpr int kPutBackTokens = 256;        // see ce_put_back_kernel
+constexpr int kPutBackTokens = 512;        // see ce_put_back_kernel
 constexpr int kABytes = kBM * kBK * 2, kBBytes = kBM * kBK * 2;
 constexpr int kFewBBytes = kFewTokens / 2 * kBK * 2;   // FEW: half of the tokens per CTA
 constexpr int kStagesBytes = 6 * (kABytes + kBBytes);
@@ -423,22 +423,27 @@ __global__ void __launch_bounds__(kThreads, 1)
       const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(lo), __uint_as_float(hi));
       return *reinterpret_cast<const uint32_t*>(&h);
     };
-    // The token whose row_add belongs to row `first_row` + lane of dW, or -1.  At most one does.  The keys stay in registers.
-    constexpr int kKeys = kPutBackTokens / 32;
+    // The token whose row_add belongs to row `first_row` + lane of dW, or -1.  At most one does.  The keys of up to 64 tokens
+    // stay in registers (read for every tile: step of 64 x 2048 x 128256 311 -> 324 us); more are read again for every tile,
+    // while its products are on their way (eight in registers: 256 x 2048 x 65536 266 us, 229 without; sixteen spill).
+    constexpr int kKeys = FEW ? kFewTokens / 32 : 8;
     int key[KIND == GRADS ? kKeys : 1];
-    if (KIND == GRADS && p.row_key) {
+    auto read_keys = [&](int t0) {
 #pragma unroll
-      for (int i = 0; i < kKeys; ++i) key[KIND == GRADS ? i : 0] = 32 * i + lane < p.tokens ? __ldcg(p.row_key + 32 * i + lane) : -1;
-    }
+      for (int i = 0; i < kKeys; ++i) key[KIND == GRADS ? i : 0] = t0 + 32 * i + lane < p.tokens ? __ldcg(p.row_key + t0 + 32 * i + lane) : -1;
+    };
+    if (FEW && KIND == GRADS && p.row_key) read_keys(0);
     auto find_row_add = [&](int first_row) {
       int mine = -1;
+      for (int t0 = 0; t0 < p.tokens; t0 += 32 * kKeys) {
+        if (!FEW) read_keys(t0);
 #pragma unroll
-      for (int i = 0; i < kKeys; ++i) {
-        if (32 * i >= p.tokens) break;
-        const int r = key[KIND == GRADS ? i : 0] - first_row;
-        for (uint32_t hits = __ballot_sync(0xFFFFFFFFu, r >= 0 && r < 32); hits; hits &= hits - 1) {
-          const int src = __ffs(hits) - 1;
-          if (__shfl_sync(0xFFFFFFFFu, r, src) == lane) mine = 32 * i + src;
+        for (int i = 0; i < kKeys; ++i) {
+          const int r = key[KIND == GRADS ? i : 0] - first_row;
+          for (uint32_t hits = __ballot_sync(0xFFFFFFFFu, r >= 0 && r < 32); hits; hits &= hits - 1) {
+            const int src = __ffs(hits) - 1;
+            if (__shfl_sync(0xFFFFFFFFu, r, src) == lane) mine = t0 + 32 * i + src;
+          }
         }
       }
       return mine;

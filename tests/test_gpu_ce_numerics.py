@@ -179,3 +179,20 @@ def test_a_weight_of_zero_does_not_hide_a_nan(t):
     y[3] = -100                     # not trained on: its D is zero (and zero times the NaN of X in D^T X)
     n = run(X, W, y, w)
     assert n["loss"][3] == 0 and not n["dX"][3].any() and np.isfinite(np.delete(n["dW"], 5, 1)).all()
+
+
+@pytest.mark.parametrize("t", [1, 16, 100, 256, 257, 333, 512])
+def test_error_of_dw_is_that_of_one_rounding(t):
+    """Up to 512 tokens dW does not show that D is held in bfloat16: what rounding takes from the targets' elements, the large
+    ones, is put back.  The other elements' roundings remain; both are random, so their squares add up."""
+    d, v = 264, 3203
+    g = np.random.Generator(np.random.Philox(t))
+    X, W = I.gaussian((t, d), 1, 1.0, "bf16"), I.gaussian((v, d), 2, d ** -0.5, "bf16")
+    y = (g.random(t) ** 3 * v).astype(np.int64)
+    w = (g.random(t) * 2).astype(np.float32)
+    o = run(X, W, y, w)
+    want = C.ce_bwd(X, W, y, w)[1]
+    one = np.linalg.norm(I.round_to_dtype(want.astype(np.float32), "bf16") - want)
+    mag = (C.ce_dlogits(X, W, y, w) ** 2) * (X.astype(np.float64) ** 2).sum(1, keepdims=True)
+    target = mag[np.arange(t), y].sum()
+    assert np.linalg.norm(o["dW"] - want) <= 1.05 * one * np.sqrt(1 + (mag.sum() - target) / target)
