@@ -337,7 +337,9 @@ ACX_API size_t acx_ce_workspace_bytes(const acx_ce_desc* desc, int op);
  *   weight [tokens] fp32 or NULL (all one): weights of the tokens in `total` and in the gradients.
  *   loss, lse [tokens] fp32, out;   total [2] fp32, out, or NULL: (sum of weight * loss, sum of weight) over the trained
  *   tokens: total[0] / total[1] is the mean loss, and &total[1] the `denom` of its gradient.
- *   The logits are fp32 sums on the tensor cores; the target's own is summed again outside them.  The loss is computed as
+ *   The logits are fp32 sums on the tensor cores, whose additions truncate; logit_scale is raised by 0.135 * 2^-23 per 16 columns of
+ *   d, what that takes from dense rows on average (4e-6 of a logit at d = 4096; where the sums are exact it is that much too
+ *   large).  The target's own logit is summed again outside them, to nearest and with logit_scale as it is.  The loss is computed as
  *   log(1 + sum over the other words / the target's), not as a difference: that of an almost certain token keeps its digits. */
 ACX_API acx_status acx_linear_ce_fwd(const acx_ce_desc* desc, const void* X, const void* W, const int64_t* targets, const float* weight,
                                      float* loss, float* lse, float* total, void* ws, size_t ws_bytes, void* cuda_stream);

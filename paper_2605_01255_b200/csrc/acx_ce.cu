@@ -320,9 +320,12 @@ int token_group(int64_t d, int m_tiles) {
 
 // The tensor core adds 16 products at a time to the running sum and truncates: every sum comes out too small by a share of
 // its size.  While a logit builds up over d / 16 steps its running sum is on average half of it, so that the logit ends short
-// by d / 16 * kTruncation of itself (measured on d = 256 ... 4096, flat and peaked: 0.128 to 0.144 * 2^-23 a step).  All
-// logits of a row being short alike, the log-sum-exp would be off by that share of the mean logit, 2.5e-6 at d = 4096; with
-// the logits' scale raised by it, 3e-7 is left.
+// by d / 16 * kTruncation of itself.  All logits of a row being short alike, the log-sum-exp would be off by that share of the
+// mean logit, 2.5e-6 at d = 4096; with the logits' scale raised by it, 3e-7 is left.  How short, in 2^-23 of the logit per
+// step (2048 rows): rows of N(0, 1) 0.10 to 0.135 from d = 256 to 65536, the same with 12 or 40 times the word's own row added
+// 0.14 to 0.19, with one column in 64 eight times as large 0.145 to 0.16.  Rows that lose less get too much: half of the columns
+// zero 0.08, 5 % of them not zero 0.02 to 0.04, sums that are exact 0.  Their logits are then long by up to kTruncation per
+// step, less than what dense ones would be short by without it.
 constexpr double kTruncation = 0.135 / (1 << 23);
 
 void common(const CeProblem& q, Params* p, const int64_t* targets, const float* weight, int* status) {

@@ -196,3 +196,53 @@ def test_error_of_dw_is_that_of_one_rounding(t):
     mag = (C.ce_dlogits(X, W, y, w) ** 2) * (X.astype(np.float64) ** 2).sum(1, keepdims=True)
     target = mag[np.arange(t), y].sum()
     assert np.linalg.norm(o["dW"] - want) <= 1.05 * one * np.sqrt(1 + (mag.sum() - target) / target)
+
+
+def _raw_logits(X, W):
+    """The logits of one word as the tensor core and the logits' scale give them: the log-sum-exp of tokens that are not trained on
+    over a vocabulary of that word."""
+    t, d = X.shape
+    desc = B.make_ce_desc(t, d, 1)
+    loss, lse = torch.empty(t, device="cuda"), torch.empty(t, device="cuda")
+    B.acx_linear_ce_fwd(desc, X, W, torch.full((t,), -100, device="cuda"), loss, lse, None, None, B.alloc_ce_workspace(desc, B.ACX_OP_CE_FWD))
+    return lse.double()
+
+
+@pytest.mark.parametrize("d", [256, 1024, 4096, 16384])
+@pytest.mark.parametrize("kind", ["flat", "peaked", "outliers"])
+@pytest.mark.parametrize("t", [64, 2048])
+def test_dense_logits_have_no_systematic_error(d, kind, t):
+    """What the tensor core's truncation takes from dense rows, some 0.135 * 2^-23 of a logit per 16 columns, is put back: at most half of
+    it is left on average.  (Without the correction, or with its sign turned, the whole or twice of it would be.)"""
+    g = torch.Generator(device="cuda").manual_seed(d)
+    short, size = 0.0, 0.0
+    for _ in range(2048 // t):
+        W = torch.randn(1, d, generator=g, device="cuda") * d ** -0.5
+        X = torch.randn(t, d, generator=g, device="cuda")
+        if kind == "outliers":
+            X[:, ::64] *= 8
+        if kind != "flat":
+            X += 12 * W / W.square().sum()
+        X, W = X.bfloat16(), W.bfloat16()
+        want = (X.double() @ W.double().T)[:, 0]
+        short += float(((want - _raw_logits(X, W)) * want.sign()).sum())
+        size += float(want.abs().sum())
+    assert abs(short / size) <= 0.07 * 2.0 ** -23 * d / 16 + 2.0 ** -25      # (and the roundings to and from base 2)
+
+
+@pytest.mark.parametrize("d", [1024, 4096, 16384])
+@pytest.mark.parametrize("t", [48, 100])
+def test_exact_sums(d, t):
+    """Rows of +-1 lose nothing on the tensor core: there the correction is what the logits are off by, and no more; the target's own
+    logit, summed apart, is exact."""
+    g = np.random.Generator(np.random.Philox(d))
+    v = 500
+    X, W = (2.0 * g.integers(0, 2, s).astype(np.float32) - 1 for s in ((t, d), (v, d)))
+    W *= 2.0 ** -np.round(np.log2(d ** 0.5 / 16))       # logits of size 16
+    y = g.integers(0, v, t)
+    o = run(X, W, y, backward=False)
+    loss, lse, _ = C.ce_fwd(X, W, y)
+    L = C.logits(X, W)
+    rounding = 2.0 ** -22 * (1 + np.abs(L).max(1))
+    assert np.all(np.abs(o["lse"] - lse) <= 0.14 * 2.0 ** -23 * d / 16 * np.abs(L).max(1) + rounding)
+    assert np.all(np.abs(o["lse"] - o["loss"] - L[np.arange(t), y]) <= 2 * rounding)
