@@ -55,55 +55,94 @@ bool fits(const at::Tensor& t, at::IntArrayRef shape, at::ScalarType type) {
   return t.is_cuda() && t.layout() == at::kStrided && t.scalar_type() == type && t.sizes() == shape;
 }
 
-template <typename P = void>
-P* dense(PyObject* o, const char* name, at::IntArrayRef shape, at::ScalarType type) {
-  const at::Tensor* t = tensor(o, name);
-  if (!t) return nullptr;
-  if (!fits(*t, shape, type) || !t->is_contiguous()) refuse(o, name, "contiguous CUDA tensor", shape, type);
-  return static_cast<P*>(t->data_ptr());
-}
-
 struct Matrix {
   void* p;
   int64_t ld;
 };
-
-// A matrix whose rows are dense: a column slice of a wider one is fine.
-Matrix strided(PyObject* o, const char* name, at::IntArrayRef shape, at::ScalarType type) {
-  const at::Tensor* t = tensor(o, name);
-  if (!t) {
-    PyErr_Format(PyExc_ValueError, "%s must be a CUDA matrix (got None)", name);
-    throw PythonError();
-  }
-  if (!fits(*t, shape, type) || t->stride(1) != 1) refuse(o, name, "CUDA matrix with unit column stride", shape, type);
-  return Matrix{t->data_ptr(), shape[0] > 1 ? t->stride(0) : shape[1]};
-}
-
 struct Workspace {
-  void* p = nullptr;
-  size_t bytes = 0;
-  explicit Workspace(PyObject* o) {
+  void* p;
+  size_t bytes;
+};
+
+// What the arguments of one call have in common: the device of its tensors, which has to be the current one (the library
+// launches there) and the stream's.
+class Call {
+ public:
+  template <typename P = void>
+  P* dense(PyObject* o, const char* name, at::IntArrayRef shape, at::ScalarType type) {
+    const at::Tensor* t = tensor(o, name);
+    if (!t) return nullptr;
+    if (!fits(*t, shape, type) || !t->is_contiguous()) refuse(o, name, "contiguous CUDA tensor", shape, type);
+    same_device(*t, name);
+    return static_cast<P*>(t->data_ptr());
+  }
+
+  // A matrix whose rows are dense: a column slice of a wider one is fine.
+  Matrix strided(PyObject* o, const char* name, at::IntArrayRef shape, at::ScalarType type) {
+    const at::Tensor* t = tensor(o, name);
+    if (!t) {
+      PyErr_Format(PyExc_ValueError, "%s must be a CUDA matrix (got None)", name);
+      throw PythonError();
+    }
+    if (!fits(*t, shape, type) || t->stride(1) != 1) refuse(o, name, "CUDA matrix with unit column stride", shape, type);
+    same_device(*t, name);
+    return Matrix{t->data_ptr(), shape[0] > 1 ? t->stride(0) : shape[1]};
+  }
+
+  Workspace workspace(PyObject* o) {
     const at::Tensor* t = tensor(o, "workspace");
-    if (!t) return;
+    if (!t) return Workspace{nullptr, 0};
     if (!t->is_cuda() || !t->is_contiguous()) {
       PyErr_SetString(PyExc_ValueError, "workspace must be a contiguous CUDA tensor");
       throw PythonError();
     }
-    p = t->data_ptr();
-    bytes = t->nbytes();
+    same_device(*t, "workspace");
+    return Workspace{t->data_ptr(), t->nbytes()};
+  }
+
+  // None: torch's current stream of the current device.  Taken last, when the tensors' device is known.
+  void* stream(PyObject* o) const {
+    if (o == Py_None) {
+      const c10::cuda::CUDAStream s = c10::cuda::getCurrentCUDAStream();
+      current_is(s.device_index());
+      return s.stream();
+    }
+    PyObject* h = PyObject_GetAttrString(o, "cuda_stream");
+    if (!h) throw PythonError();
+    void* p = PyLong_AsVoidPtr(h);
+    Py_DECREF(h);
+    if (!p && PyErr_Occurred()) throw PythonError();
+    if (PyObject* d = PyObject_GetAttrString(o, "device_index")) {
+      const long index = PyLong_AsLong(d);
+      Py_DECREF(d);
+      if (index == -1 && PyErr_Occurred()) throw PythonError();
+      if (device_ >= 0 && index != device_) {
+        PyErr_Format(PyExc_ValueError, "the stream is on cuda:%ld, the tensors on cuda:%d", index, device_);
+        throw PythonError();
+      }
+    } else {
+      PyErr_Clear();   // a handle without a device
+    }
+    current_is(c10::cuda::current_device());
+    return p;
+  }
+
+ private:
+  int device_ = -1;
+
+  void same_device(const at::Tensor& t, const char* name) {
+    const int index = t.device().index();
+    if (device_ < 0) device_ = index;
+    if (index == device_) return;
+    PyErr_Format(PyExc_ValueError, "%s is on cuda:%d, the tensors before it on cuda:%d", name, index, device_);
+    throw PythonError();
+  }
+  void current_is(int device) const {
+    if (device_ < 0 || device == device_) return;
+    PyErr_Format(PyExc_ValueError, "the tensors are on cuda:%d, the current device is cuda:%d", device_, device);
+    throw PythonError();
   }
 };
-
-// None: torch's current stream of the current device.
-void* stream(PyObject* o) {
-  if (o == Py_None) return c10::cuda::getCurrentCUDAStream().stream();
-  PyObject* h = PyObject_GetAttrString(o, "cuda_stream");
-  if (!h) throw PythonError();
-  void* p = PyLong_AsVoidPtr(h);
-  Py_DECREF(h);
-  if (!p && PyErr_Occurred()) throw PythonError();
-  return p;
-}
 
 float number(PyObject* o) {
   const double v = PyFloat_AsDouble(o);
@@ -129,7 +168,7 @@ D descriptor(PyObject* o) {
 
 at::ScalarType io_type(const acx_rows_desc& d) { return d.io_dtype == ACX_BF16 ? at::kBFloat16 : at::kFloat; }
 
-struct RowArgs {
+struct RowArgs : Call {
   acx_rows_desc d;
   at::ScalarType io;
   std::array<int64_t, 2> shape, groups;
@@ -140,16 +179,16 @@ struct RowArgs {
     row = {d.rows};
     vec = {d.cols};
   }
-  int8_t* codes(PyObject* o, const char* name) const { return dense<int8_t>(o, name, shape, at::kChar); }
-  float* scales(PyObject* o, const char* name) const { return dense<float>(o, name, groups, at::kFloat); }
-  void* matrix(PyObject* o, const char* name) const { return dense(o, name, shape, io); }
-  void* vector(PyObject* o, const char* name) const { return dense(o, name, vec, io); }
-  float* row_f32(PyObject* o, const char* name) const { return dense<float>(o, name, row, at::kFloat); }
-  float* vec_f32(PyObject* o, const char* name) const { return dense<float>(o, name, vec, at::kFloat); }
-  Matrix rows_of(PyObject* o, const char* name) const { return strided(o, name, shape, io); }
+  int8_t* codes(PyObject* o, const char* name) { return dense<int8_t>(o, name, shape, at::kChar); }
+  float* scales(PyObject* o, const char* name) { return dense<float>(o, name, groups, at::kFloat); }
+  void* matrix(PyObject* o, const char* name) { return dense(o, name, shape, io); }
+  void* vector(PyObject* o, const char* name) { return dense(o, name, vec, io); }
+  float* row_f32(PyObject* o, const char* name) { return dense<float>(o, name, row, at::kFloat); }
+  float* vec_f32(PyObject* o, const char* name) { return dense<float>(o, name, vec, at::kFloat); }
+  Matrix rows_of(PyObject* o, const char* name) { return strided(o, name, shape, io); }
 };
 
-struct CeArgs {
+struct CeArgs : Call {
   acx_ce_desc d;
   std::array<int64_t, 2> x, w;
   std::array<int64_t, 1> row;
@@ -158,7 +197,7 @@ struct CeArgs {
     w = {d.vocab, d.d};
     row = {d.tokens};
   }
-  float* row_f32(PyObject* o, const char* name) const { return dense<float>(o, name, row, at::kFloat); }
+  float* row_f32(PyObject* o, const char* name) { return dense<float>(o, name, row, at::kFloat); }
 };
 
 template <typename F>
@@ -170,49 +209,49 @@ acx_status without_gil(F&& f) {
 }
 
 acx_status q8_store(PyObject* const* a) {
-  const RowArgs r(a[0]);
+  RowArgs r(a[0]);
   const Matrix X = r.rows_of(a[1], "X");
   int8_t* const q = r.codes(a[2], "codes of X");
   float* const s = r.scales(a[3], "scales of X");
-  void* const st = stream(a[4]);
+  void* const st = r.stream(a[4]);
   return without_gil([&] { return entries.q8_store(&r.d, X.p, X.ld, q, s, st); });
 }
 
 acx_status q8_load(PyObject* const* a) {
-  const RowArgs r(a[0]);
+  RowArgs r(a[0]);
   const int8_t* const q = r.codes(a[1], "codes of X");
   const float* const s = r.scales(a[2], "scales of X");
   const Matrix X = r.rows_of(a[3], "X");
-  void* const st = stream(a[4]);
+  void* const st = r.stream(a[4]);
   return without_gil([&] { return entries.q8_load(&r.d, q, s, X.p, X.ld, st); });
 }
 
 acx_status swiglu_fwd(PyObject* const* a) {
-  const RowArgs r(a[0]);
+  RowArgs r(a[0]);
   const Matrix G = r.rows_of(a[1], "G"), U = r.rows_of(a[2], "U");
   void* const H = r.matrix(a[3], "H");
   int8_t* const Gq = r.codes(a[4], "Gq");
   float* const Gs = r.scales(a[5], "Gs");
   int8_t* const Uq = r.codes(a[6], "Uq");
   float* const Us = r.scales(a[7], "Us");
-  void* const st = stream(a[8]);
+  void* const st = r.stream(a[8]);
   return without_gil([&] { return entries.swiglu_fwd(&r.d, G.p, G.ld, U.p, U.ld, H, Gq, Gs, Uq, Us, st); });
 }
 
 acx_status swiglu_bwd(PyObject* const* a) {
-  const RowArgs r(a[0]);
+  RowArgs r(a[0]);
   const void* const dH = r.matrix(a[1], "dH");
   const int8_t* const Gq = r.codes(a[2], "Gq");
   const float* const Gs = r.scales(a[3], "Gs");
   const int8_t* const Uq = r.codes(a[4], "Uq");
   const float* const Us = r.scales(a[5], "Us");
   const Matrix dG = r.rows_of(a[6], "dG"), dU = r.rows_of(a[7], "dU");
-  void* const st = stream(a[8]);
+  void* const st = r.stream(a[8]);
   return without_gil([&] { return entries.swiglu_bwd(&r.d, dH, Gq, Gs, Uq, Us, dG.p, dG.ld, dU.p, dU.ld, st); });
 }
 
 acx_status norm_join_fwd(PyObject* const* a) {
-  const RowArgs r(a[0]);
+  RowArgs r(a[0]);
   const void *const h = r.matrix(a[1], "h"), *const b = r.matrix(a[2], "b");
   const void *const w_post = r.vector(a[3], "w_post"), *const gate = r.vector(a[4], "gate"), *const w_pre = r.vector(a[5], "w_pre");
   void *const h_out = r.matrix(a[6], "h_out"), *const y = r.matrix(a[7], "y");
@@ -222,14 +261,14 @@ acx_status norm_join_fwd(PyObject* const* a) {
   float* const Bs = r.scales(a[11], "Bs");
   float *const rstd_post = r.row_f32(a[12], "rstd_post"), *const rstd_pre = r.row_f32(a[13], "rstd_pre");
   const float eps = number(a[14]), alpha = number(a[15]);
-  void* const st = stream(a[16]);
+  void* const st = r.stream(a[16]);
   return without_gil([&] {
     return entries.norm_join_fwd(&r.d, h, b, w_post, gate, w_pre, h_out, y, Hq, Hs, Bq, Bs, rstd_post, rstd_pre, eps, alpha, st);
   });
 }
 
 acx_status norm_join_bwd(PyObject* const* a) {
-  const RowArgs r(a[0]);
+  RowArgs r(a[0]);
   const void *const dy = r.matrix(a[1], "dy"), *const dh_next = r.matrix(a[2], "dh_next");
   const void *const w_post = r.vector(a[3], "w_post"), *const gate = r.vector(a[4], "gate"), *const w_pre = r.vector(a[5], "w_pre");
   const int8_t* const Hq = r.codes(a[6], "Hq");
@@ -240,8 +279,8 @@ acx_status norm_join_bwd(PyObject* const* a) {
   void *const dh = r.matrix(a[12], "dh"), *const db = r.matrix(a[13], "db");
   float *const dw_post = r.vec_f32(a[14], "dw_post"), *const dgate = r.vec_f32(a[15], "dgate"), *const dw_pre = r.vec_f32(a[16], "dw_pre");
   const float alpha = number(a[17]);
-  const Workspace ws(a[18]);
-  void* const st = stream(a[19]);
+  const Workspace ws = r.workspace(a[18]);
+  void* const st = r.stream(a[19]);
   return without_gil([&] {
     return entries.norm_join_bwd(&r.d, dy, dh_next, w_post, gate, w_pre, Hq, Hs, Bq, Bs, rstd_post, rstd_pre, dh, db, dw_post, dgate, dw_pre,
                                  alpha, ws.p, ws.bytes, st);
@@ -249,31 +288,31 @@ acx_status norm_join_bwd(PyObject* const* a) {
 }
 
 acx_status linear_ce_fwd(PyObject* const* a) {
-  const CeArgs c(a[0]);
+  CeArgs c(a[0]);
   const std::array<int64_t, 1> two{2};
-  const void *const X = dense(a[1], "X", c.x, at::kBFloat16), *const W = dense(a[2], "W", c.w, at::kBFloat16);
-  const int64_t* const targets = dense<int64_t>(a[3], "targets", c.row, at::kLong);
+  const void *const X = c.dense(a[1], "X", c.x, at::kBFloat16), *const W = c.dense(a[2], "W", c.w, at::kBFloat16);
+  const int64_t* const targets = c.dense<int64_t>(a[3], "targets", c.row, at::kLong);
   const float* const weight = c.row_f32(a[4], "weight");
   float *const loss = c.row_f32(a[5], "loss"), *const lse = c.row_f32(a[6], "lse");
-  float* const total = dense<float>(a[7], "total", two, at::kFloat);
-  const Workspace ws(a[8]);
-  void* const st = stream(a[9]);
+  float* const total = c.dense<float>(a[7], "total", two, at::kFloat);
+  const Workspace ws = c.workspace(a[8]);
+  void* const st = c.stream(a[9]);
   return without_gil([&] { return entries.linear_ce_fwd(&c.d, X, W, targets, weight, loss, lse, total, ws.p, ws.bytes, st); });
 }
 
 acx_status linear_ce_bwd(PyObject* const* a) {
-  const CeArgs c(a[0]);
+  CeArgs c(a[0]);
   const std::array<int64_t, 1> one{1};
-  const void *const X = dense(a[1], "X", c.x, at::kBFloat16), *const W = dense(a[2], "W", c.w, at::kBFloat16);
-  const int64_t* const targets = dense<int64_t>(a[3], "targets", c.row, at::kLong);
+  const void *const X = c.dense(a[1], "X", c.x, at::kBFloat16), *const W = c.dense(a[2], "W", c.w, at::kBFloat16);
+  const int64_t* const targets = c.dense<int64_t>(a[3], "targets", c.row, at::kLong);
   const float* const weight = c.row_f32(a[4], "weight");
   const float* const lse = c.row_f32(a[5], "lse");
   const float* const loss = c.row_f32(a[6], "loss");
-  const float* const denom = dense<float>(a[7], "denom", one, at::kFloat);
+  const float* const denom = c.dense<float>(a[7], "denom", one, at::kFloat);
   const float scale = number(a[8]);
-  void *const dX = dense(a[9], "dX", c.x, at::kBFloat16), *const dW = dense(a[10], "dW", c.w, at::kBFloat16);
-  const Workspace ws(a[11]);
-  void* const st = stream(a[12]);
+  void *const dX = c.dense(a[9], "dX", c.x, at::kBFloat16), *const dW = c.dense(a[10], "dW", c.w, at::kBFloat16);
+  const Workspace ws = c.workspace(a[11]);
+  void* const st = c.stream(a[12]);
   return without_gil([&] { return entries.linear_ce_bwd(&c.d, X, W, targets, weight, lse, loss, denom, scale, dX, dW, ws.p, ws.bytes, st); });
 }
 
