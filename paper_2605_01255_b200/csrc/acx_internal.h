@@ -6,6 +6,7 @@
 #include <cstdint>
 
 #include "../../include/acx.h"
+#include "acx_device.h"
 #include "acx_sketch.cuh"
 
 namespace acx {
@@ -76,21 +77,6 @@ cudaError_t launch_lined_up(void (*kernel)(K...), dim3 grid, dim3 block, size_t 
 __device__ __forceinline__ void wait_for_launch_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void let_next_launch_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 #endif
-
-// One-time set-up that holds per device (a kernel's function attributes are set for the device that is current):
-// `static DeviceOnce once; if (once.needed()) { ...; once.done(); }`.  Safe to race: the set-up is idempotent.
-class DeviceOnce {
-  std::atomic<unsigned long long> mask_{0};
-  static unsigned long long bit() {
-    int dev = 0;
-    cudaGetDevice(&dev);
-    return 1ull << (unsigned(dev) & 63u);
-  }
-
- public:
-  bool needed() const { return (mask_.load(std::memory_order_acquire) & bit()) == 0; }
-  void done() { mask_.fetch_or(bit(), std::memory_order_release); }
-};
 
 // Checks a caller's descriptor and derives the launch problem from it (defined with the C ABI).
 acx_status validate(const acx_desc* d, Problem* out);

@@ -567,9 +567,10 @@ Shape bwd_shape(int64_t rows, int64_t cols) {
 }
 bool is_full(const Shape& s, int64_t cols) { return cols == int64_t(s.nv) * s.threads * kVec; }
 
-// How many clusters of a size and of blocks of so many warps run at once, asked once for each (0: not yet): the last clusters of a persistent grid that does
-// not fit would start when the others end and double the time.
-using ClusterLimit = std::atomic<int>[9][kOneVec / 32 + 1];
+// How many clusters of a size and of blocks of so many warps run at once on a device, asked once for each: the last clusters of
+// a persistent grid that does not fit would start when the others end and double the time.
+constexpr int kMaxWarps = kOneVec / 32;
+using ClusterLimit = DeviceNumbers<9 * (kMaxWarps + 1)>;
 
 // s.blocks: at most as many rows under way as run at once.
 template <typename K, typename A>
@@ -580,8 +581,9 @@ cudaError_t launch_rows(K kernel, DeviceOnce& once, ClusterLimit& limit, const A
     once.done();
   }
   if (s.cluster > 1) {
-    std::atomic<int>& known = limit[s.cluster][s.threads / 32];
-    int n = known.load(std::memory_order_relaxed);
+    std::atomic<int>* known = limit.here();
+    if (known) known += s.cluster * (kMaxWarps + 1) + s.threads / 32;
+    int n = known ? known->load(std::memory_order_relaxed) : 0;
     if (n == 0) {
       cudaLaunchConfig_t cfg = {};
       cudaLaunchAttribute attr[1];
@@ -594,7 +596,8 @@ cudaError_t launch_rows(K kernel, DeviceOnce& once, ClusterLimit& limit, const A
       cfg.numAttrs = 1;
       const cudaError_t e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
       if (e != cudaSuccess) return e;
-      known.store(n = std::max(n, 1), std::memory_order_relaxed);
+      n = std::max(n, 1);
+      if (known) known->store(n, std::memory_order_relaxed);
     }
     s.blocks = std::min(s.blocks, n);
   }
