@@ -6,7 +6,9 @@
 //     scale = a * (1 / 127),   code = rint(x * (127 * (1 / a))),
 // (the scale at most kMaxScale, so that 127 codes of the largest finite a do not overflow when they are read back), every
 // step one binary32 operation rounded to nearest even (1 / 127 the rounded constant), so that the codes are a function of
-// the input alone and any two implementations agree on every bit.  a < 2^-100: the group is stored as zeros (1 / a would overflow on its
+// the input alone and any two implementations agree on every bit.  (They are products with rounded reciprocals, as torch takes
+// x / 127.0 and 127.0 / x on the GPU too; quotients differ in the last bit of one scale in twenty, and in the code of a value
+// half way between two.)  a < 2^-100: the group is stored as zeros (1 / a would overflow on its
 // way through the subnormals).  An infinity or a NaN in the group: scale = NaN, the group reads back as NaN.
 #pragma once
 #include <cuda_bf16.h>
