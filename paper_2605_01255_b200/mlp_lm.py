@@ -90,7 +90,8 @@ class MlpLm:
         size = lambda ts: sum(t.numel() * t.element_size() for t in ts)  # noqa: E731
         s = self.s
         kept = size(t for group in (self.q_h, self.q_b, self.q_g, self.q_u) for q in group for t in q)
-        kept += size(self.rstd_pre) + size(self.rstd_post) + size(t for x in self.xs for t in x.values()) + size([self.lse])
+        kept += size(self.rstd_pre) + size(self.rstd_post) + size(t for x in self.xs for t in x.values())
+        kept += size([self.y, self.lse, self.loss, self.total])      # what the head's backward reads: its input is kept as it is
         # h, b, the norms' outputs (the linears' inputs), G, U and H of every layer; the logits are not counted on either side
         plain = 2 * s.tokens * (s.layers * (3 * s.d + 3 * s.inter) + 2 * s.d)
         return {"kept": kept, "bf16": plain, "logits_bf16": 2 * s.tokens * s.vocab}
