@@ -1,4 +1,6 @@
-"""Builds libacx.so (sm_100a) in-tree with nvcc, and the Python side's argument checks with g++.  `python -m paper_2605_01255_b200.build [--force]`."""
+"""Builds libacx.so (sm_100a) in-tree with nvcc, and the Python side's argument checks with g++ against the installed torch.
+`python -m paper_2605_01255_b200.build [--force] [--library-only]`; the library alone, all that users of the C ABI need, is
+built without torch's and Python's headers."""
 from __future__ import annotations
 
 import concurrent.futures
@@ -61,8 +63,9 @@ def _host_job(force: bool):
             HOST_SRC, "-o", HOST_PATH, "-L" + os.path.join(home, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
 
 
-def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
-    """Compile every .cu under csrc/, link libacx.so next to this file and build the host module.  Returns the library path."""
+def build(force: bool = False, verbose: bool = False, extra_flags=(), library_only: bool = False) -> str:
+    """Compile every .cu under csrc/, link libacx.so next to this file and build the host module.  Returns the library path.  A host
+    module that cannot be built is an error that is raised once the library is in place."""
     nvcc = _nvcc()
     os.makedirs(OBJ_DIR, exist_ok=True)
     headers = _headers()
@@ -73,8 +76,6 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
         objs.append(obj)
         if force or _stale(obj, [src] + headers):
             jobs.append([nvcc, *NVCC_FLAGS, *extra_flags, "-c", src, "-o", obj])
-    host = _host_job(force)
-
     def run(cmd):
         if verbose:
             print(" ".join(cmd), flush=True)
@@ -84,13 +85,21 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
         if verbose and (r.stdout or r.stderr):
             print(r.stdout, r.stderr, flush=True)
 
+    def run_host():
+        job = _host_job(force)
+        if job:
+            run(job)
+
     with concurrent.futures.ThreadPoolExecutor(max_workers=max(1, min(8, len(jobs) + 1))) as ex:
-        list(ex.map(run, jobs + ([host] if host else [])))
+        host = None if library_only else ex.submit(run_host)
+        list(ex.map(run, jobs))
     if jobs or force or _stale(LIB_PATH, objs):
         run([nvcc, "-shared", "-o", LIB_PATH, *objs])
+    if host and host.exception():
+        raise RuntimeError("%s is built; the argument checks of the Python binding (%s) are not" % (LIB_PATH, HOST_PATH)) from host.exception()
     return LIB_PATH
 
 
 if __name__ == "__main__":
     extra = ["-Xptxas", "-v"] if "--ptxas" in sys.argv else []
-    print(build(force="--force" in sys.argv, verbose=True, extra_flags=extra))
+    print(build(force="--force" in sys.argv, verbose=True, extra_flags=extra, library_only="--library-only" in sys.argv))
