@@ -1,18 +1,11 @@
 // C ABI of the row operators (8-bit checkpoints, gated activation, residual join): argument checks and dispatch.
 #include <cmath>
 
+#include "acx_checks.h"
 #include "acx_internal.h"
 
 namespace acx {
 namespace {
-
-bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
-template <typename... P>
-bool any_misaligned(const P*... p) { return (misaligned(p) || ...); }
-template <typename... P>
-bool any_null(const P*... p) { return ((p == nullptr) || ...); }
-
-acx_status from_cuda(cudaError_t e) { return e == cudaSuccess ? ACX_OK : ACX_ERR_CUDA; }
 
 acx_status validate_rows(const acx_rows_desc* d, Rows* out) {
   if (!d || d->struct_size != sizeof(acx_rows_desc)) return ACX_ERR_INVALID_ARG;
