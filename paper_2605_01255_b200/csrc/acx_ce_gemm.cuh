@@ -424,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       return *reinterpret_cast<const uint32_t*>(&h);
     };
     // The token whose row_add belongs to row `first_row` + lane of dW, or -1.  At most one does.  The keys of up to 64 tokens
-    // stay in registers (read for every tile: step of 64 x 2048 x 128256 311 -> 324 us); more are read again for every tile,
+    // stay in registers (read for every tile: backward of 64 x 2048 x 128256 311 -> 324 us); more are read again for every tile,
     // while its products are on their way (eight in registers: 256 x 2048 x 65536 266 us, 229 without; sixteen spill).
     constexpr int kKeys = FEW ? kFewTokens / 32 : 8;
     int key[KIND == GRADS ? kKeys : 1];
