@@ -336,7 +336,7 @@ __global__ void __launch_bounds__(Cfg<MT, BROWS, PAIR>::threads(SKETCH == SKETCH
   const uint32_t tmem_base = *tmem_slot_gen;
   // A grid launched behind this one with programmatic stream serialization may take the SMs that this grid's CTAs
   // leave as they finish (the gradient factor of the same call behind dX: it needs nothing that dX writes).  Not behind a
-  // grid that itself started early: see the producer's end.
+  // grid that itself started early: see the end.
   if (!p.ends_after) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   auto give_up = [&]() {
@@ -426,13 +426,6 @@ __global__ void __launch_bounds__(Cfg<MT, BROWS, PAIR>::threads(SKETCH == SKETCH
           const uint32_t ph = (s < stage) ? phase : (phase ^ 1u);   // parity of the last phase filled on stage s
           if (!ptx::mbar_wait(empty_bar(s), ph, abort_flag)) { give_up(); ok = false; }
         }
-      }
-      // The launch behind this one may be lined up too; it then waits for this grid and for no other.  So this grid must
-      // not end, nor let that one start, before the grid that it overtook has ended.  A grid ends with its last block: that
-      // one waits, and the others leave their SMs to whatever is left of either grid.
-      if (p.ends_after && blockIdx.x == gridDim.x - 1) {
-        asm volatile("griddepcontrol.wait;" ::: "memory");
-        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
       }
     }
   } else if (warp == 1) {
@@ -812,6 +805,13 @@ __global__ void __launch_bounds__(Cfg<MT, BROWS, PAIR>::threads(SKETCH == SKETCH
     ptx::tcgen05_fence_after_sync();
     if (PAIR) ptx::tmem_dealloc_pair(tmem_base, kTmemCols);
     else ptx::tmem_dealloc(tmem_base, kTmemCols);
+  }
+  // The launch behind this one may be lined up too; it then waits for this grid and for no other.  So this grid must not end,
+  // nor let that one start, before the grid that it overtook has ended.  A grid ends with its last block: that one waits,
+  // with all its work done, and the others leave their SMs to whatever is left of either grid.
+  if (p.ends_after && blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   }
 }
 
