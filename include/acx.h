@@ -77,7 +77,12 @@ typedef enum acx_op {
   ACX_OP_BWD_BIAS = 6,
   ACX_OP_NORM_BWD = 7, /* for acx_rows_workspace_bytes */
   ACX_OP_CE_FWD = 8,   /* for acx_ce_workspace_bytes */
-  ACX_OP_CE_BWD = 9
+  ACX_OP_CE_BWD = 9,
+  ACX_OP_ATTN_PLAN = 10, /* for acx_attn_workspace_bytes */
+  ACX_OP_ATTN_BWD = 11,
+  ACX_OP_EMBED_BWD = 12, /* for acx_embed_workspace_bytes */
+  ACX_OP_GRAD_PLAN = 13, /* for acx_grad_workspace_bytes */
+  ACX_OP_GRAD_CLIP = 14
 } acx_op;
 
 /* Problem descriptor: plain data, filled by the caller, read-only for the library. */
@@ -361,6 +366,108 @@ ACX_API acx_status acx_linear_ce_bwd(const acx_ce_desc* desc, const void* X, con
 ACX_API acx_status acx_linear_ce_bwd_loss(const acx_ce_desc* desc, const void* X, const void* W, const int64_t* targets, const float* weight,
                                           const float* lse, const float* loss, const float* denom, float scale, void* dX, void* dW, void* ws,
                                           size_t ws_bytes, void* cuda_stream);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * What a language model's training step has around its linears: the lookup in front, attention in between, the clipping of the
+ * gradients before the optimizer.
+ * --------------------------------------------------------------------------------------------------------------- */
+
+/* Softmax attention of packed documents.  Token t's heads are rows of matrices [tokens][heads][head_dim] (bfloat16; the heads of a
+ * token lie one behind the other, from token to token there are ld elements: a multiple of 8, at least heads * head_dim; so q, k
+ * and v may be column slices of one product's output).  Query head h reads key head h / (heads / kv_heads).  With
+ *     s = scale * q_i k_j,   z = cap(s) - slopes[h] |i - j|,   cap(s) = softcap * tanh(s / softcap), or s where softcap is 0,
+ * o_i = sum of p_ij v_j, p the softmax of z over the keys that i sees: those of its own document and, where causal, only the keys
+ * j <= i and those of the document's prefix.
+ *   head_dim a multiple of 8, 8 <= head_dim <= 128;  heads a multiple of kv_heads, at most 4096;  tokens <= 2^24 (0 is a no-op);
+ *   docs >= 1;  scale > 0;  (tokens / 128 + docs) * heads <= 2^30. */
+typedef struct acx_attn_desc {
+  uint32_t struct_size; /* sizeof(acx_attn_desc) */
+  int32_t io_dtype;     /* ACX_BF16 */
+  int64_t tokens, docs;
+  int32_t heads, kv_heads, head_dim;
+  int32_t causal;       /* 0 or 1 */
+  float scale, softcap;
+} acx_attn_desc;
+
+/* Bytes of the plan (ACX_OP_ATTN_PLAN) and of the backward's scratch (ACX_OP_ATTN_BWD). */
+ACX_API size_t acx_attn_workspace_bytes(const acx_attn_desc* desc, int op);
+
+/* Lays a batch's documents out as work for the kernels; one plan serves every layer's calls with the same tokens, docs and causal.
+ *   offsets [docs + 1] int32, device: document i has the tokens [offsets[i], offsets[i+1]); they must not decrease.  Tokens before
+ *      the first and behind the last document (padding) belong to none: their o, dq, dk and dv are zero, their lse minus infinity, and
+ *      nothing of their q, k, v, dO reaches another token, whatever it is.  Documents without a token are fine.
+ *   prefix [docs] int32, device, or NULL (none): the first prefix[i] tokens of document i are seen by all of its tokens; causal only.
+ *   plan: device memory of acx_attn_workspace_bytes(desc, ACX_OP_ATTN_PLAN) bytes, out. */
+ACX_API acx_status acx_attn_plan(const acx_attn_desc* desc, const int32_t* offsets, const int32_t* prefix, void* plan, size_t plan_bytes,
+                                 void* cuda_stream);
+
+/*   Q [tokens][heads][head_dim], K, V [tokens][kv_heads][head_dim] in;  slopes [heads] fp32 or NULL: no bias;
+ *   O [tokens][heads][head_dim] out;  lse [heads][tokens] fp32, out, or NULL: log of the sum of exp(z), for the backward.
+ * Scores and sums are fp32; the probabilities enter the second product rounded to bfloat16, as dS = p (dP - delta) does in the
+ * backward; every output is rounded once. */
+ACX_API acx_status acx_attn_fwd(const acx_attn_desc* desc, const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv,
+                                const float* slopes, const void* plan, size_t plan_bytes, void* O, int64_t ldo, float* lse, void* cuda_stream);
+
+/* Gradients of the forward at Q, K, V (the same plan, slopes and descriptor; O and lse as it left them).
+ *   dO [tokens][heads][head_dim] in;  dQ, dK, dV out, shaped as Q, K, V;  ws/ws_bytes: ACX_OP_ATTN_BWD.
+ * Fixed summation order, no atomics: reproducible bits. */
+ACX_API acx_status acx_attn_bwd(const acx_attn_desc* desc, const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv,
+                                const float* slopes, const void* plan, size_t plan_bytes, const void* O, int64_t ldo, const void* dO, int64_t lddo,
+                                const float* lse, void* dQ, int64_t lddq, void* dK, int64_t lddk, void* dV, int64_t lddv, void* ws, size_t ws_bytes,
+                                void* cuda_stream);
+
+/* Embedding table: E [vocab x d] io_dtype.  d a multiple of 8, 8 <= d <= 65536;  1 <= vocab <= 2^22;  tokens <= 2^28. */
+typedef struct acx_embed_desc {
+  uint32_t struct_size; /* sizeof(acx_embed_desc) */
+  int32_t io_dtype;     /* acx_dtype of E, Y and dY */
+  int32_t grad_dtype;   /* acx_dtype of dE */
+  float scale;
+  int64_t tokens, d, vocab;
+} acx_embed_desc;
+
+/* Workspace of ACX_OP_EMBED_BWD. */
+ACX_API size_t acx_embed_workspace_bytes(const acx_embed_desc* desc, int op);
+
+/*   acx_embed_fwd:  Y_t = scale * E[ids[t]].   ids [tokens] int64, device: a value outside [0, vocab) gives a row of zeros;
+ *      Y [tokens x d] io_dtype, out.
+ *   acx_embed_bwd:  dE = beta * dE + scale * (for every word, the sum of dY over the tokens that have it).
+ *      dY [tokens x d] io_dtype, in;  dE [vocab x d] grad_dtype, in/out: with beta = 0 it is not read, with beta = 1 (the head's gradient
+ *      of a shared table, or micro-batches) only the rows of words that occur are touched.  Sums in fp32, each row rounded once;
+ *      fixed summation order: reproducible bits.  tokens == 0: dE = beta * dE. */
+ACX_API acx_status acx_embed_fwd(const acx_embed_desc* desc, const int64_t* ids, const void* E, void* Y, void* cuda_stream);
+ACX_API acx_status acx_embed_bwd(const acx_embed_desc* desc, const int64_t* ids, const void* dY, void* dE, float beta, void* ws, size_t ws_bytes,
+                                 void* cuda_stream);
+
+/* One gradient of a list: n elements at src (device, 16-byte aligned, any n >= 0), clipped into dst (which may be src; else neither
+ * may overlap another). */
+typedef struct acx_grad {
+  const void* src;
+  void* dst;
+  int64_t n;
+  float weight;         /* >= 0: multiplies its sum of squares in the squared norm.  1 for a gradient; d_in / r for a factor A, whose
+                           ||A S^T||^2 is that many times ||A||^2 on average over the sketches (E[S^T S] = (d_in / r) I) */
+  int32_t src_dtype, dst_dtype;
+  int32_t reserved;
+} acx_grad;
+typedef struct acx_grad_desc {
+  uint32_t struct_size; /* sizeof(acx_grad_desc) */
+  uint32_t reserved;    /* 0 */
+  int64_t tensors, chunks;
+} acx_grad_desc;
+
+/* Checks a list (host memory) and fills its descriptor. */
+ACX_API acx_status acx_grad_describe(const acx_grad* list, int64_t count, acx_grad_desc* desc);
+/* Bytes of the plan (ACX_OP_GRAD_PLAN) and of the clipping's scratch (ACX_OP_GRAD_CLIP). */
+ACX_API size_t acx_grad_workspace_bytes(const acx_grad_desc* desc, int op);
+/* Writes the list to device memory, for any number of calls: gradients keep their buffers from step to step.  The list itself is
+ * not needed after the call. */
+ACX_API acx_status acx_grad_plan(const acx_grad_desc* desc, const acx_grad* list, void* plan, size_t plan_bytes, void* cuda_stream);
+/* norm = sqrt(sum of weight * sum of x^2),  f = max_norm / norm where norm > max_norm, else 1;  dst = f * src for every tensor.
+ *   max_norm > 0 (infinity: only the norm, and a copy where dst is not src);  total [2] fp32, out: norm and f.
+ *   A norm that is not finite (an infinity or a NaN among the gradients) leaves f = 1: the caller sees it in total[0] and may leave the
+ *   step out.  Sums in 64 bits, fixed order: reproducible bits. */
+ACX_API acx_status acx_grad_clip(const acx_grad_desc* desc, const void* plan, size_t plan_bytes, float max_norm, float* total, void* ws,
+                                 size_t ws_bytes, void* cuda_stream);
 
 /* Synchronises the stream and returns ACX_ERR_TIMEOUT if any kernel on this device since the last call gave up on
  * a bounded wait (its outputs are then undefined), ACX_ERR_CUDA on a CUDA error, else ACX_OK.  Clears the flag.  The

@@ -1,14 +1,15 @@
 """ctypes binding to libacx.so: same names as the C ABI (include/acx.h), argument marshalling only.
 
-torch supplies device memory and streams; every arithmetic step runs in the library's kernels.  The row operators and the
-cross entropy check and convert their arguments in a compiled module (csrc/host_calls.cpp), the linears here.  If
+torch supplies device memory and streams; every arithmetic step runs in the library's kernels.  The row operators, the
+cross entropy, attention, the embedding table and gradient clipping check and convert their arguments in a compiled module
+(csrc/host_calls.cpp), the linears here.  If
 the library has not been built the import of a symbol raises: there is no fallback of any kind.
 """
 from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Tuple
+from typing import Optional, Sequence, Tuple
 
 import torch
 
@@ -24,6 +25,7 @@ ACX_F32, ACX_BF16 = 0, 1
 ACX_OP_FWD, ACX_OP_BWD, ACX_OP_RECONSTRUCT, ACX_OP_BWD_BUILTIN_SCRATCH, ACX_OP_RSVD, ACX_OP_BIAS_GRAD = 0, 1, 2, 3, 4, 5
 ACX_OP_BWD_BIAS = 6
 ACX_OP_NORM_BWD, ACX_OP_CE_FWD, ACX_OP_CE_BWD = 7, 8, 9
+ACX_OP_ATTN_PLAN, ACX_OP_ATTN_BWD, ACX_OP_EMBED_BWD, ACX_OP_GRAD_PLAN, ACX_OP_GRAD_CLIP = 10, 11, 12, 13, 14
 ACX_Q8_GROUP = 128
 
 EXPORTS = (
@@ -33,6 +35,9 @@ EXPORTS = (
     "acx_debug_force_gemm_mode", "acx_linear_fwd_v", "acx_reconstruct_v", "acx_lowrank_adamw", "acx_rsvd_factor", "acx_linear_fwd_bias", "acx_bias_grad", "acx_linear_bwd_bias",
     "acx_rows_workspace_bytes", "acx_q8_store", "acx_q8_load", "acx_swiglu_fwd", "acx_swiglu_bwd", "acx_norm_join_fwd", "acx_norm_join_bwd",
     "acx_ce_workspace_bytes", "acx_linear_ce_fwd", "acx_linear_ce_bwd", "acx_linear_ce_bwd_loss",
+    "acx_attn_workspace_bytes", "acx_attn_plan", "acx_attn_fwd", "acx_attn_bwd",
+    "acx_embed_workspace_bytes", "acx_embed_fwd", "acx_embed_bwd",
+    "acx_grad_describe", "acx_grad_workspace_bytes", "acx_grad_plan", "acx_grad_clip",
 )
 
 
@@ -62,6 +67,26 @@ class acx_rows_desc(ctypes.Structure):
 class acx_ce_desc(ctypes.Structure):
     _fields_ = [("struct_size", ctypes.c_uint32), ("io_dtype", ctypes.c_int32), ("tokens", ctypes.c_int64), ("d", ctypes.c_int64),
                 ("vocab", ctypes.c_int64), ("logit_scale", ctypes.c_float), ("reserved", ctypes.c_uint32)]
+
+
+class acx_attn_desc(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("io_dtype", ctypes.c_int32), ("tokens", ctypes.c_int64), ("docs", ctypes.c_int64),
+                ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("causal", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("softcap", ctypes.c_float)]
+
+
+class acx_embed_desc(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("io_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("tokens", ctypes.c_int64), ("d", ctypes.c_int64), ("vocab", ctypes.c_int64)]
+
+
+class acx_grad(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("n", ctypes.c_int64), ("weight", ctypes.c_float),
+                ("src_dtype", ctypes.c_int32), ("dst_dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class acx_grad_desc(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("reserved", ctypes.c_uint32), ("tensors", ctypes.c_int64), ("chunks", ctypes.c_int64)]
 
 
 _lib = None
@@ -105,6 +130,19 @@ def lib() -> ctypes.CDLL:
         L.acx_linear_ce_fwd.restype, L.acx_linear_ce_fwd.argtypes = ctypes.c_int, [cp] + [vp] * 8 + [sz, vp]
         L.acx_linear_ce_bwd.restype, L.acx_linear_ce_bwd.argtypes = ctypes.c_int, [cp] + [vp] * 6 + [f32, vp, vp, vp, sz, vp]
         L.acx_linear_ce_bwd_loss.restype, L.acx_linear_ce_bwd_loss.argtypes = ctypes.c_int, [cp] + [vp] * 7 + [f32, vp, vp, vp, sz, vp]
+        ap, ep, gp, gl = (ctypes.POINTER(t) for t in (acx_attn_desc, acx_embed_desc, acx_grad_desc, acx_grad))
+        L.acx_attn_workspace_bytes.restype, L.acx_attn_workspace_bytes.argtypes = sz, [ap, ctypes.c_int]
+        L.acx_attn_plan.restype, L.acx_attn_plan.argtypes = ctypes.c_int, [ap, vp, vp, vp, sz, vp]
+        L.acx_attn_fwd.restype, L.acx_attn_fwd.argtypes = ctypes.c_int, [ap] + [vp, i64] * 3 + [vp, vp, sz, vp, i64, vp, vp]
+        L.acx_attn_bwd.restype = ctypes.c_int
+        L.acx_attn_bwd.argtypes = [ap] + [vp, i64] * 3 + [vp, vp, sz] + [vp, i64] * 2 + [vp] + [vp, i64] * 3 + [vp, sz, vp]
+        L.acx_embed_workspace_bytes.restype, L.acx_embed_workspace_bytes.argtypes = sz, [ep, ctypes.c_int]
+        L.acx_embed_fwd.restype, L.acx_embed_fwd.argtypes = ctypes.c_int, [ep] + [vp] * 4
+        L.acx_embed_bwd.restype, L.acx_embed_bwd.argtypes = ctypes.c_int, [ep, vp, vp, vp, f32, vp, sz, vp]
+        L.acx_grad_describe.restype, L.acx_grad_describe.argtypes = ctypes.c_int, [gl, i64, gp]
+        L.acx_grad_workspace_bytes.restype, L.acx_grad_workspace_bytes.argtypes = sz, [gp, ctypes.c_int]
+        L.acx_grad_plan.restype, L.acx_grad_plan.argtypes = ctypes.c_int, [gp, gl, vp, sz, vp]
+        L.acx_grad_clip.restype, L.acx_grad_clip.argtypes = ctypes.c_int, [gp, vp, sz, f32, vp, vp, sz, vp]
         L.acx_sketch_materialize.restype, L.acx_sketch_materialize.argtypes = ctypes.c_int, [dp, vp, vp]
         L.acx_last_device_status.restype, L.acx_last_device_status.argtypes = ctypes.c_int, [vp]
         L.acx_debug_expired_wait.restype, L.acx_debug_expired_wait.argtypes = ctypes.c_int, [ctypes.c_uint64, vp]
@@ -359,7 +397,8 @@ def _calls():
             raise RuntimeError("_acx_host.so is not built for this torch; run `python -m paper_2605_01255_b200.build`") from e
         _acx_host.bind(tuple(ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in (
             "acx_q8_store", "acx_q8_load", "acx_swiglu_fwd", "acx_swiglu_bwd", "acx_norm_join_fwd", "acx_norm_join_bwd",
-            "acx_linear_ce_fwd", "acx_linear_ce_bwd_loss")))
+            "acx_linear_ce_fwd", "acx_linear_ce_bwd_loss", "acx_attn_plan", "acx_attn_fwd", "acx_attn_bwd", "acx_embed_fwd", "acx_embed_bwd",
+            "acx_grad_clip")))
         _host = _acx_host
     return _host
 
@@ -424,3 +463,110 @@ def acx_linear_ce_bwd(desc: acx_ce_desc, X, W, targets, lse, dX, dW, *, loss=Non
     None; loss: the forward's, so that the gradients of almost certain tokens keep their digits (see acx.h); ws:
     alloc_ce_workspace(desc, ACX_OP_CE_BWD)."""
     _check((_host or _calls()).linear_ce_bwd(desc, X, W, targets, weight, lse, loss, denom, scale, dX, dW, ws, stream), "acx_linear_ce_bwd")
+
+
+# ---- softmax attention over packed documents ------------------------------------------------------------------------------
+def make_attn_desc(tokens: int, heads: int, kv_heads: int, head_dim: int, docs: int = 1, *, causal: bool = True, scale: Optional[float] = None,
+                   softcap: float = 0.0) -> acx_attn_desc:
+    """scale: None for head_dim ** -0.5; softcap: 0 for none."""
+    return acx_attn_desc(ctypes.sizeof(acx_attn_desc), ACX_BF16, tokens, docs, heads, kv_heads, head_dim, int(causal),
+                         head_dim ** -0.5 if scale is None else scale, softcap)
+
+
+def acx_attn_workspace_bytes(desc: acx_attn_desc, op: int) -> int:
+    return int(lib().acx_attn_workspace_bytes(ctypes.byref(desc), op))
+
+
+def alloc_attn_workspace(desc: acx_attn_desc, op: int, device="cuda") -> Optional[torch.Tensor]:
+    """ACX_OP_ATTN_PLAN: room for a batch's plan; ACX_OP_ATTN_BWD: the backward's scratch."""
+    n = acx_attn_workspace_bytes(desc, op)
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def acx_attn_plan(desc: acx_attn_desc, offsets, plan, prefix=None, stream=None) -> None:
+    """Lays out a batch's documents (offsets: int32, docs + 1; prefix: int32, docs) for the calls below; one plan for all layers."""
+    _check((_host or _calls()).attn_plan(desc, offsets, prefix, plan, stream), "acx_attn_plan")
+
+
+def acx_attn_fwd(desc: acx_attn_desc, Q, K, V, plan, O, lse=None, *, slopes=None, stream=None) -> None:
+    """O = softmax(cap(scale Q K^T) - slopes |i - j|) V within the documents; Q, O (tokens, heads, head_dim), K, V (tokens, kv_heads,
+    head_dim), each possibly a column slice of a wider matrix; lse (heads, tokens) for the backward."""
+    _check((_host or _calls()).attn_fwd(desc, Q, K, V, slopes, plan, O, lse, stream), "acx_attn_fwd")
+
+
+def acx_attn_bwd(desc: acx_attn_desc, Q, K, V, plan, O, dO, lse, dQ, dK, dV, *, slopes=None, ws=None, stream=None) -> None:
+    """Gradients of acx_attn_fwd; O and lse: the forward's; ws: alloc_attn_workspace(desc, ACX_OP_ATTN_BWD)."""
+    _check((_host or _calls()).attn_bwd(desc, Q, K, V, slopes, plan, O, dO, lse, dQ, dK, dV, ws, stream), "acx_attn_bwd")
+
+
+# ---- embedding table ------------------------------------------------------------------------------------------------------
+def make_embed_desc(tokens: int, d: int, vocab: int, dtype, grad_dtype=None, *, scale: float = 1.0) -> acx_embed_desc:
+    """dtype of the table and its rows, grad_dtype of the table's gradient (None: the same)."""
+    codes = {torch.float32: ACX_F32, torch.bfloat16: ACX_BF16, "f32": ACX_F32, "bf16": ACX_BF16}
+    return acx_embed_desc(ctypes.sizeof(acx_embed_desc), codes[dtype], codes[dtype if grad_dtype is None else grad_dtype], scale, tokens, d, vocab)
+
+
+def acx_embed_workspace_bytes(desc: acx_embed_desc, op: int) -> int:
+    return int(lib().acx_embed_workspace_bytes(ctypes.byref(desc), op))
+
+
+def alloc_embed_workspace(desc: acx_embed_desc, op: int, device="cuda") -> Optional[torch.Tensor]:
+    n = acx_embed_workspace_bytes(desc, op)
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def acx_embed_fwd(desc: acx_embed_desc, ids, E, Y, stream=None) -> None:
+    """Y = scale * E[ids]; ids int64, a row of zeros for those outside the vocabulary."""
+    _check((_host or _calls()).embed_fwd(desc, ids, E, Y, stream), "acx_embed_fwd")
+
+
+def acx_embed_bwd(desc: acx_embed_desc, ids, dY, dE, *, beta: float = 0.0, ws=None, stream=None) -> None:
+    """dE = beta * dE + scale * (for every word the sum of its tokens' dY); ws: alloc_embed_workspace(desc, ACX_OP_EMBED_BWD)."""
+    _check((_host or _calls()).embed_bwd(desc, ids, dY, dE, beta, ws, stream), "acx_embed_bwd")
+
+
+# ---- norm of many gradients, clipping -------------------------------------------------------------------------------------
+class GradList:
+    """Gradients that are clipped together: they keep their buffers from step to step (and this object keeps the buffers)."""
+
+    def __init__(self, desc: acx_grad_desc, plan: torch.Tensor, tensors):
+        self.desc, self.plan, self._tensors = desc, plan, tensors
+
+
+def make_grad_list(tensors: Sequence[torch.Tensor], weights: Optional[Sequence[float]] = None, out: Optional[Sequence[torch.Tensor]] = None,
+                   stream=None) -> GradList:
+    """Contiguous fp32 or bf16 gradients of one device, their weights in the squared norm (None: 1) and where they go clipped (None: in
+    place).  The list is written to the device here, once, and waited for."""
+    tensors, out = list(tensors), list(tensors if out is None else out)
+    weights = [1.0] * len(tensors) if weights is None else list(weights)
+    if not tensors or not len(tensors) == len(out) == len(weights):
+        raise ValueError("as many weights and outputs as gradients, and one gradient at least")
+    codes = {torch.float32: ACX_F32, torch.bfloat16: ACX_BF16}
+    dev = tensors[0].device
+    items = (acx_grad * len(tensors))()
+    for i, (x, y, w) in enumerate(zip(tensors, out, weights)):
+        for name, t in (("gradient", x), ("output", y)):
+            if not t.is_cuda or t.layout is not torch.strided or not t.is_contiguous() or t.dtype not in codes or t.device != dev:
+                raise ValueError("%s %d must be a contiguous fp32 or bf16 tensor on %s (got %s on %s)" % (name, i, dev, t.dtype, t.device))
+        if x.shape != y.shape:
+            raise ValueError("output %d must have the shape %s (got %s)" % (i, tuple(x.shape), tuple(y.shape)))
+        items[i] = acx_grad(x.data_ptr(), y.data_ptr(), x.numel(), w, codes[x.dtype], codes[y.dtype], 0)
+    desc = acx_grad_desc()
+    _check(lib().acx_grad_describe(items, len(tensors), ctypes.byref(desc)), "acx_grad_describe")
+    if dev.index != torch.cuda.current_device():
+        raise ValueError("the gradients are on %s, the current device is cuda:%d" % (dev, torch.cuda.current_device()))
+    plan = torch.empty(int(lib().acx_grad_workspace_bytes(ctypes.byref(desc), ACX_OP_GRAD_PLAN)), dtype=torch.uint8, device=dev)
+    _check(lib().acx_grad_plan(ctypes.byref(desc), items, ctypes.c_void_p(plan.data_ptr()), plan.numel(), _stream(stream)), "acx_grad_plan")
+    (stream or torch.cuda.current_stream()).synchronize()
+    return GradList(desc, plan, (tensors, out))
+
+
+def alloc_grad_workspace(grads: GradList) -> torch.Tensor:
+    n = int(lib().acx_grad_workspace_bytes(ctypes.byref(grads.desc), ACX_OP_GRAD_CLIP))
+    return torch.empty(n, dtype=torch.uint8, device=grads.plan.device)
+
+
+def acx_grad_clip(grads: GradList, max_norm: float, total, *, ws=None, stream=None) -> None:
+    """Scales the list's gradients by f = min(1, max_norm / norm), norm = sqrt(sum of weight * sum of squares); total (fp32, 2): norm and
+    f.  max_norm = inf: the norm alone.  A norm that is not finite leaves them as they are.  ws: alloc_grad_workspace(grads)."""
+    _check((_host or _calls()).grad_clip(grads.desc, grads.plan, max_norm, total, ws, stream), "acx_grad_clip")

@@ -1,0 +1,239 @@
+// Softmax attention over packed documents: what its kernels share.
+//
+// For query i and key j of one document, with 2-based exponents throughout,
+//     x_ij = log2(e) (cap(scale q_i k_j) - slope |i - j|),   cap(s) = c tanh(s / c) or s,
+//     p_ij = 2^(x_ij - lse_i),   o_i = sum_j p_ij v_j        over the keys that i sees.
+// Which those are is an interval for every query: from its document's start to its end (not causal), or to the larger of its own
+// position and the prefix's end.  Tiles never reach over a document's border: the tiles of queries and of keys start
+// at the document's own start (a bulk tensor copy may start at any token), so a tile is masked at most along the diagonal, at the
+// prefix's end and behind the document's last token, and nothing of a neighbouring document or of padding is multiplied: rows
+// behind the last token are overwritten with zeros in shared memory before a product sums over them.
+//
+// The plan, one kernel per batch, lists the tiles of every document with the longest first; work item u of a launch is tile
+// u / heads for head u % heads, so that the heads that share a key head run beside one another.
+#pragma once
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <type_traits>
+
+#include "acx_internal.h"
+#include "acx_q8.cuh"
+#include "acx_umma.cuh"
+
+namespace acx {
+namespace attn {
+
+constexpr int kRows = 128;          // rows of one tile: lanes of tensor memory
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct Item {
+  int row0;        // first token of the tile
+  int start, end;  // the document's tokens
+  int prefix;      // end of the part that all of the document's tokens see (start: none)
+};
+// The plan in device memory: this, then the lists.
+struct PlanHeader {
+  int wide;          // items of 256 queries (forward)
+  int tiles;         // items of 128 tokens (backward, both lists)
+  int head_end;      // tokens [0, head_end) and [tail_begin, tokens) belong to no document
+  int tail_begin;
+};
+constexpr size_t kPlanListOffset = 256;
+struct PlanLayout {
+  int64_t wide_cap, tile_cap;
+  size_t wide, queries, keys, cum, bytes;   // byte offsets of the lists; cum: running tile counts of the documents
+};
+__host__ __device__ inline PlanLayout plan_layout(int64_t tokens, int64_t docs) {
+  const int64_t d = docs < tokens ? docs : tokens;   // documents that hold a token
+  PlanLayout p;
+  p.wide_cap = tokens / 256 + d + 1;
+  p.tile_cap = tokens / 128 + d + 1;
+  p.wide = kPlanListOffset;
+  p.queries = p.wide + size_t(p.wide_cap) * sizeof(Item);
+  p.keys = p.queries + size_t(p.tile_cap) * sizeof(Item);
+  p.cum = p.keys + size_t(p.tile_cap) * sizeof(Item);
+  p.bytes = p.cum + size_t(docs + 1) * 8;
+  return p;
+}
+
+struct Params {
+  int tokens, heads, kv_heads, group;
+  int d;                     // columns of a head
+  int causal;
+  const PlanHeader* plan;
+  const Item* items;         // the list that this launch works through
+  const float* slopes;       // [heads], BIAS only
+  float scale;
+  float c;                   // scale log2(e): x = c s without a cap
+  float cap_in;              // scale / cap: the tanh's argument per unit of s
+  float cap_out;             // cap log2(e)
+  float* lse;                // [heads][tokens], natural logarithm
+  int* status;
+  // forward
+  __nv_bfloat16* O;
+  int64_t ldo;
+  // backward
+  const float* delta;        // [heads][tokens]
+  __nv_bfloat16 *dQ, *dK, *dV;
+  int64_t lddq, lddk, lddv;
+  float *dk_part, *dv_part;  // [part][tokens][kv_heads][d], or null: one part, written to dK and dV
+  int parts, heads_per_part;
+};
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float rcp_fast(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// tanh: 1 - 2 / (1 + e^2u) keeps about 2^-23 absolutely, which is too little near zero once a large cap multiplies it; there
+// the odd series (its first left-out term is below 2^-25 of the value at the border).
+__device__ __forceinline__ float tanh_of(float u) {
+  const float r = 1.f - 2.f * rcp_fast(1.f + exp2_fast(u * (2.f * kLog2e)));
+  const float q = u * u;
+  const float t = fmaf(q, fmaf(q, fmaf(q, fmaf(q, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
+  return fabsf(u) < 0.2f ? u * t : r;
+}
+
+// x of a raw score s; `far` = query position - key position.  For CAP, *slope = d x / d s in units of c.
+template <bool CAP, bool BIAS>
+__device__ __forceinline__ float exponent(const Params& p, float s, float far, float slope2, float* slope = nullptr) {
+  float x;
+  if (CAP) {
+    const float t = tanh_of(s * p.cap_in);
+    x = t * p.cap_out;
+    if (slope) *slope = fmaf(-t, t, 1.f);
+  } else {
+    x = s * p.c;
+  }
+  if (BIAS) x = fmaf(-slope2, fabsf(far), x);
+  return x;
+}
+
+// A wait of a whole warp, which it leaves together: what follows (tensor memory loads and stores) has to be executed by converged
+// warps, and lanes that find a barrier complete at different polls are not.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  return __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar, parity, abort_flag));
+}
+
+// Waits for the tensor memory loads issued so far and hands their registers over behind the wait: as far as the compiler can see
+// an inline load has delivered at once, and what uses its registers need not stay behind a wait that does not name them.
+__device__ __forceinline__ void hand_over(uint32_t (&v)[32]) {
+  asm volatile("" : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]),
+               "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]), "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]),
+               "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]),
+               "+r"(v[30]), "+r"(v[31])::"memory");
+}
+__device__ __forceinline__ void hand_over(uint32_t (&v)[16]) {
+  asm volatile("" : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]),
+               "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])::"memory");
+}
+template <typename... V>
+__device__ __forceinline__ void tmem_loaded(V&... v) {
+  ptx::tmem_ld_wait();
+  (hand_over(v), ...);
+}
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// 32 columns of a row from registers, times f, as bf16; `left` columns (a multiple of 8) are inside the head.  Two stores of 32 bytes
+// where the row's address allows them.
+__device__ __forceinline__ void store_bf16(__nv_bfloat16* at, const uint32_t (&v)[32], float f, int left) {
+  uint32_t w[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) w[i] = pack2(__uint_as_float(v[2 * i]) * f, __uint_as_float(v[2 * i + 1]) * f);
+  if (left >= 32 && (reinterpret_cast<uintptr_t>(at) & 31) == 0) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(at + 16 * i), "r"(w[8 * i]), "r"(w[8 * i + 1]), "r"(w[8 * i + 2]),
+                   "r"(w[8 * i + 3]), "r"(w[8 * i + 4]), "r"(w[8 * i + 5]), "r"(w[8 * i + 6]), "r"(w[8 * i + 7])
+                   : "memory");
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (8 * i < left) *reinterpret_cast<uint4*>(at + 8 * i) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+}
+__device__ __forceinline__ void store_f32(float* at, const uint32_t (&v)[32], float f, int left) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (8 * i < left) {
+      float2 q[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) q[k] = make_float2(__uint_as_float(v[8 * i + 2 * k]) * f, __uint_as_float(v[8 * i + 2 * k + 1]) * f);
+      q8::store8(at + 8 * i, q);
+    }
+}
+
+// Rows that belong to no document: zeros (all threads of the grid; row r of `heads` heads of d columns, stride ld).
+__device__ __forceinline__ void zero_rows_outside(const Params& p, __nv_bfloat16* out, int64_t ld, int heads, float* row_value, float value) {
+  const int head_end = p.plan->head_end, tail = p.plan->tail_begin;
+  const int64_t outside = int64_t(head_end) + (p.tokens - tail);
+  const int per_row = heads * (p.d / 8);
+  for (int64_t k = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; k < outside * per_row; k += int64_t(gridDim.x) * blockDim.x) {
+    const int64_t r = k / per_row;
+    const int64_t row = r < head_end ? r : tail + (r - head_end);
+    *reinterpret_cast<uint4*>(out + row * ld + (k - r * per_row) * 8) = make_uint4(0u, 0u, 0u, 0u);
+  }
+  if (!row_value) return;
+  for (int64_t k = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; k < outside * heads; k += int64_t(gridDim.x) * blockDim.x) {
+    const int64_t h = k / outside, r = k - h * outside;
+    row_value[h * p.tokens + (r < head_end ? r : tail + (r - head_end))] = value;
+  }
+}
+
+// A tile of 128 rows in shared memory: chunks of 64 columns, rows of 128 bytes with the 128-byte swizzle.
+template <int HD>
+struct Tile {
+  static constexpr int kChunks = HD / 64, kChunkBytes = kRows * 128, kBytes = kChunks * kChunkBytes;
+  // One thread: the rows from `row` on of one head.
+  static __device__ __forceinline__ void load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int head, int row) {
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) ptx::tma_load_3d(dst + c * kChunkBytes, map, bar, 64 * c, head, row);
+  }
+  // One thread: zeros into rows [first, last), at most 15, visible to the tensor core.
+  static __device__ __forceinline__ void zero_rows(uint8_t* tile, int first, int last) {
+    for (int c = 0; c < kChunks; ++c)
+#pragma unroll 8
+      for (int i = first * 128; i < last * 128; i += 16)   // the swizzle stays within a row
+        *reinterpret_cast<uint4*>(tile + c * kChunkBytes + i) = make_uint4(0u, 0u, 0u, 0u);
+    ptx::fence_proxy_async_smem();
+  }
+};
+
+// Products of 128-row tiles, issued by one thread.  D (128 x 128) = A B^T over the head's columns, both tiles K-major.
+template <int HD>
+__device__ __forceinline__ void scores_mma(uint32_t tmem_d, uint32_t a, uint32_t b, int d16) {
+  const uint32_t idesc = ptx::make_idesc_bf16(kRows, kRows, false, false);
+  const uint64_t da = ptx::make_smem_desc(a, 16, 1024), db = ptx::make_smem_desc(b, 16, 1024);
+#pragma unroll
+  for (int k = 0; k < HD / 16; ++k) {
+    const uint64_t at = uint64_t((k >> 2) * (Tile<HD>::kChunkBytes >> 4) + (k & 3) * 2);
+    if (k < d16) ptx::umma_bf16(tmem_d, da + at, db + at, idesc, k > 0);
+  }
+}
+// D (128 x 16 d16) (+)= A B with A (128 x 16 steps, bf16) in tensor memory and B the first 16 * steps rows of a tile.  The columns of
+// A from 64 on start at tmem_a2.
+template <int HD>
+__device__ __forceinline__ void rows_mma(uint32_t tmem_d, uint32_t tmem_a, uint32_t tmem_a2, uint32_t b, int steps, int d16, bool add) {
+  const uint32_t idesc = ptx::make_idesc_bf16(kRows, 16 * d16, false, true);
+  const uint64_t db = ptx::make_smem_desc(b, Tile<HD>::kChunkBytes, 1024);
+#pragma unroll
+  for (int k = 0; k < kRows / 16; ++k)
+    if (k < steps) ptx::umma_bf16_tmem_a(tmem_d, (k < 4 ? tmem_a : tmem_a2 - 32) + 8 * k, db + uint64_t(k * (16 * 128 >> 4)), idesc, add || k > 0);
+}
+
+Params common_params(const AttnProblem& q, const void* plan, const float* slopes, float* lse, int* status);
+
+}  // namespace attn
+}  // namespace acx

@@ -1,0 +1,517 @@
+// Attention: the plan and the forward kernel.
+//
+// Forward, one work item: 256 queries of one head (two halves of 128) against the keys they see, tile by tile from the last one
+// to the first (so that the masked tiles, and with a distance bias the largest scores, come first).  S = Q K^T of a half lies
+// in 128 columns of tensor memory, one query per lane; a warpgroup takes the rows' maxima, writes P = 2^(x - m) over S as bf16
+// and the tensor core multiplies P from there with V.  The two halves take turns: while one's exponentials are taken the
+// products of the other run.
+//
+// The sums O are rescaled only where a row's maximum has grown by more than 2^8 since its reference m was taken (P then is at
+// most 2^8, bf16 and fp32 hold that without loss of digits), which after the first tiles hardly ever happens; the row sums are
+// taken from the unrounded fp32 exponentials.
+//
+// What bounds it: per tile of 128 x 128 and d = 128 the tensor core needs 2 x 512 cycles and the 16384 exponentials 1024 cycles of
+// the special function units: both at once.
+//
+// Roles (384 threads, one CTA per SM, persistent): warp 0 copies, warp 1 products and tensor memory, warps 4..7 and 8..11
+// the rows of the two halves.
+#include <algorithm>
+
+#include "acx_attn.cuh"
+#include "acx_tmap.h"
+
+namespace acx {
+namespace attn {
+namespace {
+
+// ------------------------------------------------------------------------------------------------------------------- plan
+constexpr int kPlanThreads = 1024, kBins = 1024;
+
+__device__ __forceinline__ int block_scan(int v, int* warp_sums, int* total) {   // exclusive, over the block
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int x = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+    if (lane >= o) x += y;
+  }
+  __syncthreads();
+  if (lane == 31) warp_sums[warp] = x;
+  __syncthreads();
+  if (warp == 0) {
+    int s = warp_sums[lane];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xFFFFFFFFu, s, o);
+      if (lane >= o) s += y;
+    }
+    warp_sums[lane] = s;
+  }
+  __syncthreads();
+  *total = warp_sums[31];
+  return x - v + (warp ? warp_sums[warp - 1] : 0);
+}
+
+// One block.  Offsets that decrease or lie outside [0, tokens] are brought into it, lists never grow beyond their room:
+// whatever the offsets hold, items name only tokens that exist.
+__global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int* __restrict__ offsets, const int* __restrict__ prefix, int docs, int tokens,
+                                                            int causal, uint8_t* __restrict__ plan) {
+  __shared__ int warp_sums[32];
+  __shared__ int bins[kBins];
+  wait_for_launch_before();
+  let_next_launch_start();
+  const PlanLayout at = plan_layout(tokens, docs);
+  PlanHeader* header = reinterpret_cast<PlanHeader*>(plan);
+  int* cum_wide = reinterpret_cast<int*>(plan + at.cum);
+  int* cum_tile = cum_wide + docs + 1;
+  auto clamped = [&](int i) { return min(max(__ldcg(offsets + i), 0), tokens); };
+  int wide = 0, tiles = 0;
+  for (int base = 0; base < docs; base += kPlanThreads) {
+    const int i = base + int(threadIdx.x);
+    const int n = i < docs ? max(clamped(i + 1) - clamped(i), 0) : 0;
+    int total;
+    const int w = block_scan((n + 255) / 256, warp_sums, &total) + wide;
+    wide = min(wide + total, int(at.wide_cap));
+    const int t = block_scan((n + 127) / 128, warp_sums, &total) + tiles;
+    tiles = min(tiles + total, int(at.tile_cap));
+    if (i < docs) {
+      cum_wide[i] = min(w, int(at.wide_cap));
+      cum_tile[i] = min(t, int(at.tile_cap));
+    }
+  }
+  if (threadIdx.x == 0) {
+    cum_wide[docs] = wide;
+    cum_tile[docs] = tiles;
+    header->wide = wide;
+    header->tiles = tiles;
+    const int first = docs > 0 ? clamped(0) : tokens;
+    header->head_end = first;
+    header->tail_begin = docs > 0 ? max(clamped(docs), first) : tokens;
+  }
+  __syncthreads();
+  const int most = (tokens + 127) / 128 + 1;
+  for (int list = 0; list < 3; ++list) {
+    const int* cum = list == 0 ? cum_wide : cum_tile;
+    const int count = list == 0 ? wide : tiles, rows = list == 0 ? 256 : 128;
+    Item* out = reinterpret_cast<Item*>(plan + (list == 0 ? at.wide : list == 1 ? at.queries : at.keys));
+    auto item = [&](int k, int* bin) {
+      int lo = 0, hi = docs;   // the last document whose first tile is at or before k
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (cum[mid] <= k) lo = mid; else hi = mid;
+      }
+      Item t;
+      t.start = clamped(lo);
+      t.end = max(clamped(lo + 1), t.start);
+      t.prefix = causal && prefix ? t.start + min(max(__ldcg(prefix + lo), 0), t.end - t.start) : t.start;
+      t.row0 = t.start + (k - cum[lo]) * rows;
+      int work;   // tiles on the other side
+      if (list < 2) work = (causal ? max(min(t.row0 + rows, t.end), t.prefix) : t.end) - t.start;
+      else work = t.end - (causal && t.row0 >= t.prefix ? t.row0 : t.start);
+      *bin = kBins - 1 - int(int64_t(min((work + 127) / 128, most)) * (kBins - 1) / most);
+      return t;
+    };
+    bins[threadIdx.x] = 0;
+    __syncthreads();
+    for (int k = threadIdx.x; k < count; k += kPlanThreads) {
+      int b;
+      item(k, &b);
+      atomicAdd(&bins[b], 1);
+    }
+    __syncthreads();
+    int total;
+    const int first = block_scan(bins[threadIdx.x], warp_sums, &total);
+    bins[threadIdx.x] = first;
+    __syncthreads();
+    for (int k = threadIdx.x; k < count; k += kPlanThreads) {
+      int b;
+      const Item t = item(k, &b);
+      out[atomicAdd(&bins[b], 1)] = t;   // the order within a bin does not matter: an item's results are its own
+    }
+    __syncthreads();
+  }
+}
+static_assert(kBins == kPlanThreads, "one bin per thread");
+
+// ---------------------------------------------------------------------------------------------------------------- forward
+constexpr int kFwdThreads = 384;
+template <int HD>
+struct FwdSmem {
+  static constexpr int kStages = HD == 128 ? 4 : 8;
+  static constexpr int kQ = 2 * Tile<HD>::kBytes, kBars = kQ + kStages * Tile<HD>::kBytes;
+  static constexpr int kBytes = kBars + 512 + 1024;   // 1024: the tiles' alignment
+};
+
+template <int HD, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(kFwdThreads, 1)
+    attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                    const __grid_constant__ CUtensorMap map_v, const Params p) {
+  using T = Tile<HD>;
+  constexpr int kStages = FwdSmem<HD>::kStages;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* gen = smem_raw + (base - ptx::smem_u32(smem_raw));
+  const uint32_t bars = base + FwdSmem<HD>::kBars;
+  auto full = [&](int s) { return bars + 8u * s; };
+  auto empty = [&](int s) { return bars + 8u * (kStages + s); };
+  const uint32_t misc = bars + 16u * kStages;
+  const uint32_t q_full = misc, q_empty = misc + 8, done = misc + 16;
+  auto s_full = [&](int h) { return misc + 24 + 8u * h; };
+  auto p_full = [&](int h) { return misc + 40 + 8u * h; };
+  auto o_full = [&](int h) { return misc + 56 + 8u * h; };
+  auto o_free = [&](int h) { return misc + 72 + 8u * h; };
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + FwdSmem<HD>::kBars + 16 * kStages + 88);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + FwdSmem<HD>::kBars + 16 * kStages + 92);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      ptx::mbar_init(full(s), 1);
+      ptx::mbar_init(empty(s), 1);
+    }
+    ptx::mbar_init(q_full, 1);
+    ptx::mbar_init(q_empty, 1);
+    ptx::mbar_init(done, 1);
+    for (int h = 0; h < 2; ++h) {
+      ptx::mbar_init(s_full(h), 1);
+      ptx::mbar_init(p_full(h), 4);
+      ptx::mbar_init(o_full(h), 1);
+      ptx::mbar_init(o_free(h), 4);
+    }
+    *abort_flag = 0;
+    ptx::fence_barrier_init();   // no prefetch of the tensor maps: a block without work would leave with it in flight
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc(misc + 88, 512);
+    ptx::tmem_relinquish_alloc_permit();
+  }
+  ptx::tcgen05_fence_before_sync();
+  __syncthreads();
+  ptx::tcgen05_fence_after_sync();
+  const uint32_t tmem = *tmem_slot;
+  auto tmem_s = [&](int h) { return tmem + 128u * h; };
+  auto tmem_o = [&](int h) { return tmem + 256u + HD * h; };
+  wait_for_launch_before();
+  let_next_launch_start();
+  const int units = __ldcg(&p.plan->wide) * p.heads;
+  auto give_up = [&]() {
+    *abort_flag = 1;
+    atomicExch(p.status, kDevTimeout);
+  };
+  auto fetch = [&](int u) {
+    const int4 v = __ldcg(reinterpret_cast<const int4*>(p.items) + u / p.heads);
+    return Item{v.x, v.y, v.z, v.w};
+  };
+  // key tiles that a half of the queries sees
+  auto key_tiles = [&](const Item& t, int half) {
+    const int r = t.row0 + kRows * half;
+    if (r >= t.end) return 0;
+    return ((p.causal ? max(min(r + kRows, t.end), t.prefix) : t.end) - t.start + kRows - 1) / kRows;
+  };
+
+  if (warp == 0) {
+    // ---------------------------------------------------------------------------------------------------- copies
+    if (lane == 0) {
+      int stage = 0, it = 0;
+      uint32_t phase = 0, armed = 0;
+      bool ok = true;
+      auto push = [&](const CUtensorMap* map, int head, int row) {
+        if (!ptx::mbar_wait(empty(stage), phase ^ 1u, abort_flag)) { give_up(); ok = false; return; }
+        armed |= 1u << stage;
+        ptx::mbar_arrive_expect_tx(full(stage), T::kBytes);
+        T::load(base + FwdSmem<HD>::kQ + stage * T::kBytes, map, full(stage), head, row);
+        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+      };
+      for (int u = blockIdx.x; ok && u < units; u += gridDim.x, ++it) {
+        const Item t = fetch(u);
+        const int h = u % p.heads, g = h / p.group;
+        const int n1 = key_tiles(t, 1), n = max(key_tiles(t, 0), n1);
+        if (!ptx::mbar_wait(q_empty, (it & 1) ^ 1u, abort_flag)) { give_up(); ok = false; break; }
+        ptx::mbar_arrive_expect_tx(q_full, (n1 ? 2 : 1) * T::kBytes);
+        T::load(base, &map_q, q_full, h, t.row0);
+        if (n1) T::load(base + T::kBytes, &map_q, q_full, h, t.row0 + kRows);
+        for (int j = n - 1; ok && j >= 0; --j) {
+          push(&map_k, g, t.start + j * kRows);
+          if (ok) push(&map_v, g, t.start + j * kRows);
+        }
+      }
+      if (!ok) {   // copies in flight must land before the CTA leaves (one limit for all)
+        const uint64_t t0 = ptx::globaltimer_ns();
+        for (int s = 0; s < kStages; ++s) {
+          if (!(armed & (1u << s))) continue;
+          const uint32_t ph = s < stage ? phase : phase ^ 1u;
+          while (!ptx::mbar_try_wait(full(s), ph) && ptx::globaltimer_ns() - t0 < ptx::kWaitLimitNs) {}
+        }
+        if (it > 0 || armed)
+          while (!ptx::mbar_try_wait(q_full, it & 1) && ptx::globaltimer_ns() - t0 < ptx::kWaitLimitNs / 4) {}
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    // ---------------------------------------------------------------------------------------------------- products
+    if (lane == 0) {
+      int stage = 0, it = 0, turns[2] = {0, 0}, outs[2] = {0, 0};
+      uint32_t phase = 0;
+      bool ok = true;
+      const int d16 = (p.d + 15) / 16;
+      auto wait = [&](uint32_t bar, uint32_t parity) {
+        if (ok && !ptx::mbar_wait(bar, parity, abort_flag)) { give_up(); ok = false; }
+        return ok;
+      };
+      struct Slot { int stage; uint32_t phase; };
+      auto next = [&]() {
+        const Slot s{stage, phase};
+        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        return s;
+      };
+      auto addr = [&](Slot s) { return base + FwdSmem<HD>::kQ + s.stage * T::kBytes; };
+      for (int u = blockIdx.x; ok && u < units; u += gridDim.x, ++it) {
+        const Item t = fetch(u);
+        const int nt[2] = {key_tiles(t, 0), key_tiles(t, 1)}, n = max(nt[0], nt[1]);
+        auto scores = [&](int h, Slot k) {
+          scores_mma<HD>(tmem_s(h), base + h * T::kBytes, addr(k), d16);
+          ptx::umma_commit(s_full(h));
+        };
+        wait(q_full, it & 1);
+        Slot k = next(), v;
+        if (!wait(full(k.stage), k.phase)) break;
+        ptx::tcgen05_fence_after_sync();
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          if (nt[h] == n) scores(h, k);
+        ptx::umma_commit(empty(k.stage));
+        if (n == 1) ptx::umma_commit(q_empty);
+        for (int j = n - 1; ok && j >= 0; --j) {
+          v = next();
+          if (!wait(full(v.stage), v.phase)) break;
+          const int left = t.end - (t.start + j * kRows);   // keys of this tile inside the document
+          const int steps = min(kRows, left + 15) / 16;
+          if (left < 16 * steps) T::zero_rows(gen + (addr(v) - base), left, 16 * steps);
+          if (j > 0) {
+            k = next();
+            if (!wait(full(k.stage), k.phase)) break;
+          }
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (j < nt[h]) {
+              if (j == nt[h] - 1 && !wait(o_free(h), (outs[h] & 1) ^ 1u)) break;
+              if (!wait(p_full(h), turns[h] & 1)) break;
+              ++turns[h];
+              ptx::tcgen05_fence_after_sync();
+              rows_mma<HD>(tmem_o(h), tmem_s(h), tmem_s(h) + 32, addr(v), steps, d16, j < nt[h] - 1);
+              if (j == 0) {
+                ptx::umma_commit(o_full(h));
+                ++outs[h];
+              }
+            }
+            if (j > 0 && j <= nt[h]) scores(h, k);
+          }
+          ptx::umma_commit(empty(v.stage));
+          if (j > 0) ptx::umma_commit(empty(k.stage));
+          if (j == 1) ptx::umma_commit(q_empty);
+        }
+      }
+      // everything that was issued has to be done before the tensor memory is given back
+      if (it > 0 || !ok) {
+        ptx::umma_commit(done);
+        const uint64_t t0 = ptx::globaltimer_ns();
+        while (!ptx::mbar_try_wait(done, 0) && ptx::globaltimer_ns() - t0 < ptx::kWaitLimitNs) {}
+      }
+    }
+    __syncwarp();
+  } else if (warp >= 4) {
+    // ---------------------------------------------------------------------------------------------------- rows
+    const int half = (warp - 4) >> 2, quarter = warp & 3;
+    const uint32_t lanes = uint32_t(32 * quarter) << 16;
+    const uint32_t s_at = tmem_s(half) + lanes, o_at = tmem_o(half) + lanes;
+    int turns = 0, outs = 0;
+    bool ok = true;
+    for (int u = blockIdx.x; ok && u < units; u += gridDim.x) {
+      const Item t = fetch(u);
+      const int n = key_tiles(t, half), head = u % p.heads;
+      if (n == 0) continue;
+      const int r0 = t.row0 + kRows * half, row = r0 + 32 * quarter + lane;
+      const int sees = p.causal ? min(max(row + 1, t.prefix), t.end) : t.end;       // this row: keys [start, sees)
+      const int all_see = p.causal ? min(max(r0 + 1, t.prefix), t.end) : t.end;     // every row of the half
+      const float slope2 = BIAS ? __ldg(p.slopes + head) * kLog2e : 0.f;
+      float m = 0.f, l = 0.f;
+      for (int j = n - 1; j >= 0; --j) {
+        if (!warp_wait(s_full(half), turns & 1, abort_flag)) { give_up(); ok = false; break; }
+        ++turns;
+        ptx::tcgen05_fence_after_sync();
+        const int k0 = t.start + j * kRows;
+        const bool masked = k0 + kRows > all_see;
+        const int limit = sees - k0;
+        constexpr bool kRaw = !CAP && !BIAS;   // raw scores: the scale is left to the exponent's fma
+        const float scale = kRaw ? p.c : 1.f;
+        // 32 columns at a time, twice: first for the maximum (other than raw scores go back as exponents), then for the
+        // probabilities.  All 128 in registers at once do not fit beside the rest.
+        float mx = __int_as_float(0xFF800000);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t s[32];
+          ptx::tmem_ld_x32(s_at + 32 * c, s);
+          tmem_loaded(s);
+          if (!kRaw) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              s[i] = __float_as_uint(exponent<CAP, BIAS>(p, __uint_as_float(s[i]), float(row - k0) - float(32 * c + i), slope2));
+          }
+          if (masked) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (32 * c + i >= limit) s[i] = 0xFF800000u;   // minus infinity
+          }
+          if (!kRaw) ptx::tmem_st_x32(s_at + 32 * c, s);
+          float top[2] = {__uint_as_float(s[0]), __uint_as_float(s[1])};
+#pragma unroll
+          for (int i = 2; i < 32; ++i) top[i & 1] = fmaxf(top[i & 1], __uint_as_float(s[i]));
+          mx = fmaxf(mx, fmaxf(top[0], top[1]));
+        }
+        if (!kRaw) ptx::tmem_st_wait();
+        mx *= scale;
+        if (j == n - 1) {
+          m = mx;
+        } else if (__any_sync(0xFFFFFFFFu, mx > m + 8.f)) {
+          // the products up to the tile before are done: this tile's scores were issued behind them
+          const float m_new = fmaxf(m, mx), f = exp2_fast(m - m_new);
+          m = m_new;
+          l *= f;
+#pragma unroll
+          for (int c = 0; c < HD / 16; ++c) {
+            uint32_t o[16];
+            ptx::tmem_ld_x16(o_at + 16 * c, o);
+            tmem_loaded(o);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+            ptx::tmem_st_x16(o_at + 16 * c, o);
+          }
+        }
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t s[32], w[16];
+          ptx::tmem_ld_x32(s_at + 32 * c, s);
+          tmem_loaded(s);
+          if (kRaw && masked) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (32 * c + i >= limit) s[i] = 0xFF800000u;
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float a = exp2_fast(fmaf(__uint_as_float(s[2 * i]), scale, -m)), b = exp2_fast(fmaf(__uint_as_float(s[2 * i + 1]), scale, -m));
+            sum[(2 * i) & 3] += a;
+            sum[(2 * i + 1) & 3] += b;
+            w[i] = pack2(a, b);
+          }
+          ptx::tmem_st_x16(s_at + 16 * c, w);   // over columns that have been read
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        ptx::tmem_st_wait();
+        ptx::tcgen05_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(p_full(half));
+        __syncwarp();
+      }
+      if (!ok) break;
+      if (!warp_wait(o_full(half), outs & 1, abort_flag)) { give_up(); break; }
+      ++outs;
+      ptx::tcgen05_fence_after_sync();
+      const float f = 1.f / l;
+      __nv_bfloat16* at = p.O + int64_t(row) * p.ldo + int64_t(head) * p.d;
+#pragma unroll
+      for (int c = 0; c < HD / 32; ++c) {
+        if (32 * c >= p.d) break;
+        uint32_t o[32];
+        ptx::tmem_ld_x32(o_at + 32 * c, o);
+        tmem_loaded(o);
+        if (32 * (c + 1) >= p.d) {   // all read
+          ptx::tcgen05_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(o_free(half));
+          __syncwarp();
+        }
+        if (row < t.end) store_bf16(at + 32 * c, o, f, p.d - 32 * c);
+        __syncwarp();
+      }
+      if (p.lse && row < t.end) p.lse[int64_t(head) * p.tokens + row] = (m + log2f(l)) * kLn2;
+    }
+  }
+  zero_rows_outside(p, p.O, p.ldo, p.heads, p.lse, __int_as_float(0xFF800000));
+  __syncwarp();
+  ptx::tcgen05_fence_before_sync();
+  __syncthreads();
+  if (warp == 1) {
+    __syncwarp();
+    ptx::tcgen05_fence_after_sync();
+    ptx::tmem_dealloc(tmem, 512);
+  }
+}
+
+template <int HD, bool CAP, bool BIAS>
+cudaError_t launch_fwd(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, unsigned grid, cudaStream_t st) {
+  static DeviceOnce once;
+  if (once.needed()) {
+    const cudaError_t e = cudaFuncSetAttribute(attn_fwd_kernel<HD, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, FwdSmem<HD>::kBytes);
+    if (e != cudaSuccess) return e;
+    once.done();
+  }
+  return launch_lined_up(attn_fwd_kernel<HD, CAP, BIAS>, dim3(grid), dim3(kFwdThreads), FwdSmem<HD>::kBytes, st, q, k, v, p);
+}
+template <int HD>
+cudaError_t launch_fwd(bool cap, bool bias, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, unsigned grid,
+                       cudaStream_t st) {
+  if (cap) return bias ? launch_fwd<HD, true, true>(q, k, v, p, grid, st) : launch_fwd<HD, true, false>(q, k, v, p, grid, st);
+  return bias ? launch_fwd<HD, false, true>(q, k, v, p, grid, st) : launch_fwd<HD, false, false>(q, k, v, p, grid, st);
+}
+
+}  // namespace
+
+Params common_params(const AttnProblem& q, const void* plan, const float* slopes, float* lse, int* status) {
+  Params p{};
+  p.tokens = int(q.tokens);
+  p.heads = q.heads;
+  p.kv_heads = q.kv_heads;
+  p.group = q.heads / q.kv_heads;
+  p.d = q.d;
+  p.causal = q.causal;
+  p.plan = static_cast<const PlanHeader*>(plan);
+  p.slopes = slopes;
+  p.scale = q.scale;
+  p.c = q.scale * kLog2e;
+  p.cap_in = q.softcap > 0.f ? q.scale / q.softcap : 0.f;
+  p.cap_out = q.softcap * kLog2e;
+  p.lse = lse;
+  p.status = status;
+  return p;
+}
+
+}  // namespace attn
+
+using namespace attn;
+
+size_t attn_plan_bytes(const AttnProblem& q) { return plan_layout(q.tokens, q.docs).bytes; }
+
+cudaError_t attn_plan(const AttnProblem& q, const int* offsets, const int* prefix, void* plan, cudaStream_t st) {
+  return launch_lined_up(plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, offsets, prefix, int(q.docs), int(q.tokens), q.causal,
+                         static_cast<uint8_t*>(plan));
+}
+
+cudaError_t attn_fwd(const AttnProblem& q, const AttnMatrix& Q, const AttnMatrix& K, const AttnMatrix& V, const float* slopes, const void* plan,
+                     const AttnMatrix& O, float* lse, int* status, cudaStream_t st) {
+  Params p = common_params(q, plan, slopes, lse, status);
+  const PlanLayout at = plan_layout(q.tokens, q.docs);
+  p.items = reinterpret_cast<const Item*>(static_cast<const uint8_t*>(plan) + at.wide);
+  p.O = static_cast<__nv_bfloat16*>(O.p);
+  p.ldo = O.ld;
+  CUtensorMap mq, mk, mv;
+  if (!make_tmap_heads(&mq, Q.p, q.tokens, q.heads, q.d, Q.ld, kRows) || !make_tmap_heads(&mk, K.p, q.tokens, q.kv_heads, q.d, K.ld, kRows) ||
+      !make_tmap_heads(&mv, V.p, q.tokens, q.kv_heads, q.d, V.ld, kRows))
+    return cudaErrorInvalidValue;
+  const unsigned grid = unsigned(std::min<int64_t>(at.wide_cap * q.heads, sm_count()));
+  const bool cap = q.softcap > 0.f, bias = slopes != nullptr;
+  return q.d <= 64 ? launch_fwd<64>(cap, bias, mq, mk, mv, p, grid, st) : launch_fwd<128>(cap, bias, mq, mk, mv, p, grid, st);
+}
+
+}  // namespace acx

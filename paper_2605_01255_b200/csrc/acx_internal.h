@@ -31,6 +31,30 @@ struct CeProblem {
   float logit_scale;
 };
 
+// A validated acx_attn_desc.
+struct AttnProblem {
+  int64_t tokens, docs;
+  int heads, kv_heads, d, causal;
+  float scale, softcap;
+};
+struct AttnMatrix {   // [tokens][heads][d] with ld elements from one token to the next
+  void* p;
+  int64_t ld;
+};
+
+// A validated acx_embed_desc.
+struct EmbedProblem {
+  int64_t tokens, d, vocab;
+  bool bf16, grad_bf16;
+  float scale;
+};
+
+// A validated acx_grad_desc.
+struct GradProblem {
+  int64_t tensors, chunks;
+};
+constexpr int64_t kGradChunk = 8192;   // elements of a tensor that a block scales at a time
+
 // Device-side status word values (written by kernels whose bounded waits expire).
 constexpr int kDevOk = 0;
 constexpr int kDevTimeout = 1;
@@ -149,6 +173,27 @@ cudaError_t ce_fwd(const CeProblem& p, const void* X, const void* W, const int64
 size_t ce_bwd_workspace_bytes(const CeProblem& p);
 cudaError_t ce_bwd(const CeProblem& p, const void* X, const void* W, const int64_t* targets, const float* weight, const float* lse,
                    const float* loss, const float* denom, float scale, void* dX, void* dW, void* ws, int* status, cudaStream_t st);
+
+// ---- softmax attention over packed documents (bf16) -----------------------------------------------
+size_t attn_plan_bytes(const AttnProblem& q);
+cudaError_t attn_plan(const AttnProblem& q, const int* offsets, const int* prefix, void* plan, cudaStream_t st);
+cudaError_t attn_fwd(const AttnProblem& q, const AttnMatrix& Q, const AttnMatrix& K, const AttnMatrix& V, const float* slopes, const void* plan,
+                     const AttnMatrix& O, float* lse, int* status, cudaStream_t st);
+size_t attn_bwd_workspace_bytes(const AttnProblem& q);
+cudaError_t attn_bwd(const AttnProblem& q, const AttnMatrix& Q, const AttnMatrix& K, const AttnMatrix& V, const float* slopes, const void* plan,
+                     const AttnMatrix& O, const AttnMatrix& dO, const float* lse, const AttnMatrix& dQ, const AttnMatrix& dK, const AttnMatrix& dV,
+                     void* ws, int* status, cudaStream_t st);
+
+// ---- embedding table (bf16 or fp32) ----------------------------------------------------------------
+cudaError_t embed_fwd(const EmbedProblem& q, const int64_t* ids, const void* E, void* Y, cudaStream_t st);
+size_t embed_bwd_workspace_bytes(const EmbedProblem& q);   // tokens > 0
+cudaError_t embed_bwd(const EmbedProblem& q, const int64_t* ids, const void* dY, void* dE, float beta, void* ws, cudaStream_t st);
+
+// ---- norm of many gradients, clipping --------------------------------------------------------------
+size_t grad_plan_bytes(const GradProblem& q);
+size_t grad_clip_workspace_bytes(const GradProblem& q);
+cudaError_t grad_plan(const GradProblem& q, const acx_grad* list, void* plan, cudaStream_t st);
+cudaError_t grad_clip(const GradProblem& q, const void* plan, float max_norm, float* total, void* ws, cudaStream_t st);
 
 // Test/debug: overrides the tile-shape cost models of the forward and dX (0 = off, 1..4 = a GEMM mode).
 void sm100_force_gemm_mode(int mode);

@@ -55,6 +55,19 @@ inline bool make_tmap_f32(CUtensorMap* map, const void* base, int64_t rows, int6
   return make_tmap_2d(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, base, rows, cols, box_cols, box_rows);
 }
 
+// [tokens][heads][d] bf16 with `ld` elements from one token to the next; boxes of 64 columns of one head x box_rows tokens,
+// 128-byte swizzle.  Columns from d on read as zero.
+inline bool make_tmap_heads(CUtensorMap* map, const void* base, int64_t tokens, int64_t heads, int64_t d, int64_t ld, int box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[3] = {cuuint64_t(d), cuuint64_t(heads), cuuint64_t(tokens)};
+  const cuuint64_t strides[2] = {cuuint64_t(d) * 2, cuuint64_t(ld) * 2};
+  const cuuint32_t box[3] = {64, 1, cuuint32_t(box_rows)};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 inline int sm_count() {
   static int n = 0;
   if (n == 0) {

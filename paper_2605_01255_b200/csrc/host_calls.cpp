@@ -1,4 +1,5 @@
-// Argument checks and marshalling of the row operators and the vocabulary cross entropy for Python: torch tensors in, one C
+// Argument checks and marshalling of the row operators, the vocabulary cross entropy, attention, the embedding table and gradient
+// clipping for Python: torch tensors in, one C
 // call of libacx out.  The small calls (decoding, short batches) are bound by the host: checked in Python and called through
 // ctypes the norm join of 16 x 896 with seven tensors took 8.2 us (0.41 us per tensor checked, 1.4 us to convert the
 // arguments), through this file 3.3 us, launch included; the gated activation of 8 x 4864 5.7 and 2.6 us.  The library
@@ -27,6 +28,12 @@ struct Entries {
   decltype(&acx_norm_join_bwd) norm_join_bwd;
   decltype(&acx_linear_ce_fwd) linear_ce_fwd;
   decltype(&acx_linear_ce_bwd_loss) linear_ce_bwd;
+  decltype(&acx_attn_plan) attn_plan;
+  decltype(&acx_attn_fwd) attn_fwd;
+  decltype(&acx_attn_bwd) attn_bwd;
+  decltype(&acx_embed_fwd) embed_fwd;
+  decltype(&acx_embed_bwd) embed_bwd;
+  decltype(&acx_grad_clip) grad_clip;
 } entries;
 constexpr int kEntries = sizeof(Entries) / sizeof(void*);
 
@@ -89,14 +96,27 @@ class Call {
     return Matrix{t->data_ptr(), shape[0] > 1 ? t->stride(0) : shape[1]};
   }
 
-  Workspace workspace(PyObject* o) {
-    const at::Tensor* t = tensor(o, "workspace");
-    if (!t) return Workspace{nullptr, 0};
-    if (!t->is_cuda() || !t->is_contiguous()) {
-      PyErr_SetString(PyExc_ValueError, "workspace must be a contiguous CUDA tensor");
+  // [tokens][heads][columns] whose heads lie one behind the other: a column slice of a wider matrix of tokens is fine.
+  Matrix heads(PyObject* o, const char* name, at::IntArrayRef shape, at::ScalarType type) {
+    const at::Tensor* t = tensor(o, name);
+    if (!t) {
+      PyErr_Format(PyExc_ValueError, "%s must be a CUDA tensor (got None)", name);
       throw PythonError();
     }
-    same_device(*t, "workspace");
+    if (!fits(*t, shape, type) || t->stride(2) != 1 || (shape[1] > 1 && t->stride(1) != shape[2]))
+      refuse(o, name, "CUDA tensor with dense heads", shape, type);
+    same_device(*t, name);
+    return Matrix{t->data_ptr(), shape[0] > 1 ? t->stride(0) : shape[1] * shape[2]};
+  }
+
+  Workspace workspace(PyObject* o, const char* name = "workspace") {
+    const at::Tensor* t = tensor(o, name);
+    if (!t) return Workspace{nullptr, 0};
+    if (!t->is_cuda() || !t->is_contiguous()) {
+      PyErr_Format(PyExc_ValueError, "%s must be a contiguous CUDA tensor", name);
+      throw PythonError();
+    }
+    same_device(*t, name);
     return Workspace{t->data_ptr(), t->nbytes()};
   }
 
@@ -198,6 +218,34 @@ struct CeArgs : Call {
     row = {d.tokens};
   }
   float* row_f32(PyObject* o, const char* name) { return dense<float>(o, name, row, at::kFloat); }
+};
+
+struct AttnArgs : Call {
+  acx_attn_desc d;
+  std::array<int64_t, 3> q, kv;
+  std::array<int64_t, 2> row;
+  std::array<int64_t, 1> per_head;
+  explicit AttnArgs(PyObject* o) : d(descriptor<acx_attn_desc>(o)) {
+    q = {d.tokens, d.heads, d.head_dim};
+    kv = {d.tokens, d.kv_heads, d.head_dim};
+    row = {d.heads, d.tokens};
+    per_head = {d.heads};
+  }
+  Matrix queries(PyObject* o, const char* name) { return heads(o, name, q, at::kBFloat16); }
+  Matrix keys(PyObject* o, const char* name) { return heads(o, name, kv, at::kBFloat16); }
+};
+
+struct EmbedArgs : Call {
+  acx_embed_desc d;
+  std::array<int64_t, 2> rows, table;
+  std::array<int64_t, 1> row;
+  explicit EmbedArgs(PyObject* o) : d(descriptor<acx_embed_desc>(o)) {
+    rows = {d.tokens, d.d};
+    table = {d.vocab, d.d};
+    row = {d.tokens};
+  }
+  static at::ScalarType type(int32_t t) { return t == ACX_BF16 ? at::kBFloat16 : at::kFloat; }
+  const int64_t* ids(PyObject* o) { return dense<int64_t>(o, "ids", row, at::kLong); }
 };
 
 template <typename F>
@@ -316,6 +364,75 @@ acx_status linear_ce_bwd(PyObject* const* a) {
   return without_gil([&] { return entries.linear_ce_bwd(&c.d, X, W, targets, weight, lse, loss, denom, scale, dX, dW, ws.p, ws.bytes, st); });
 }
 
+acx_status attn_plan(PyObject* const* a) {
+  AttnArgs c(a[0]);
+  const std::array<int64_t, 1> ends{c.d.docs + 1}, docs{c.d.docs};
+  const int32_t* const offsets = c.dense<int32_t>(a[1], "offsets", ends, at::kInt);
+  const int32_t* const prefix = c.dense<int32_t>(a[2], "prefix", docs, at::kInt);
+  const Workspace plan = c.workspace(a[3], "plan");
+  void* const st = c.stream(a[4]);
+  return without_gil([&] { return entries.attn_plan(&c.d, offsets, prefix, plan.p, plan.bytes, st); });
+}
+
+acx_status attn_fwd(PyObject* const* a) {
+  AttnArgs c(a[0]);
+  const Matrix Q = c.queries(a[1], "Q"), K = c.keys(a[2], "K"), V = c.keys(a[3], "V");
+  const float* const slopes = c.dense<float>(a[4], "slopes", c.per_head, at::kFloat);
+  const Workspace plan = c.workspace(a[5], "plan");
+  const Matrix O = c.queries(a[6], "O");
+  float* const lse = c.dense<float>(a[7], "lse", c.row, at::kFloat);
+  void* const st = c.stream(a[8]);
+  return without_gil([&] { return entries.attn_fwd(&c.d, Q.p, Q.ld, K.p, K.ld, V.p, V.ld, slopes, plan.p, plan.bytes, O.p, O.ld, lse, st); });
+}
+
+acx_status attn_bwd(PyObject* const* a) {
+  AttnArgs c(a[0]);
+  const Matrix Q = c.queries(a[1], "Q"), K = c.keys(a[2], "K"), V = c.keys(a[3], "V");
+  const float* const slopes = c.dense<float>(a[4], "slopes", c.per_head, at::kFloat);
+  const Workspace plan = c.workspace(a[5], "plan");
+  const Matrix O = c.queries(a[6], "O"), dO = c.queries(a[7], "dO");
+  const float* const lse = c.dense<float>(a[8], "lse", c.row, at::kFloat);
+  const Matrix dQ = c.queries(a[9], "dQ"), dK = c.keys(a[10], "dK"), dV = c.keys(a[11], "dV");
+  const Workspace ws = c.workspace(a[12]);
+  void* const st = c.stream(a[13]);
+  return without_gil([&] {
+    return entries.attn_bwd(&c.d, Q.p, Q.ld, K.p, K.ld, V.p, V.ld, slopes, plan.p, plan.bytes, O.p, O.ld, dO.p, dO.ld, lse, dQ.p, dQ.ld, dK.p,
+                            dK.ld, dV.p, dV.ld, ws.p, ws.bytes, st);
+  });
+}
+
+acx_status embed_fwd(PyObject* const* a) {
+  EmbedArgs c(a[0]);
+  const int64_t* const ids = c.ids(a[1]);
+  const void* const E = c.dense(a[2], "E", c.table, c.type(c.d.io_dtype));
+  void* const Y = c.dense(a[3], "Y", c.rows, c.type(c.d.io_dtype));
+  void* const st = c.stream(a[4]);
+  return without_gil([&] { return entries.embed_fwd(&c.d, ids, E, Y, st); });
+}
+
+acx_status embed_bwd(PyObject* const* a) {
+  EmbedArgs c(a[0]);
+  const int64_t* const ids = c.ids(a[1]);
+  const void* const dY = c.dense(a[2], "dY", c.rows, c.type(c.d.io_dtype));
+  void* const dE = c.dense(a[3], "dE", c.table, c.type(c.d.grad_dtype));
+  const float beta = number(a[4]);
+  const Workspace ws = c.workspace(a[5]);
+  void* const st = c.stream(a[6]);
+  return without_gil([&] { return entries.embed_bwd(&c.d, ids, dY, dE, beta, ws.p, ws.bytes, st); });
+}
+
+acx_status grad_clip(PyObject* const* a) {
+  Call c;
+  const acx_grad_desc d = descriptor<acx_grad_desc>(a[0]);
+  const std::array<int64_t, 1> two{2};
+  const Workspace plan = c.workspace(a[1], "plan");
+  const float max_norm = number(a[2]);
+  float* const total = c.dense<float>(a[3], "total", two, at::kFloat);
+  const Workspace ws = c.workspace(a[4]);
+  void* const st = c.stream(a[5]);
+  return without_gil([&] { return entries.grad_clip(&d, plan.p, plan.bytes, max_norm, total, ws.p, ws.bytes, st); });
+}
+
 // Python entry of an operator of COUNT arguments: its acx_status as an int.
 template <acx_status (*OP)(PyObject* const*), int COUNT>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t count) {
@@ -359,6 +476,8 @@ PyMethodDef methods[] = {
     {"bind", bind, METH_O, nullptr},
     ACX_ENTRY(q8_store, 5),       ACX_ENTRY(q8_load, 5),        ACX_ENTRY(swiglu_fwd, 9),     ACX_ENTRY(swiglu_bwd, 9),
     ACX_ENTRY(norm_join_fwd, 17), ACX_ENTRY(norm_join_bwd, 20), ACX_ENTRY(linear_ce_fwd, 10), ACX_ENTRY(linear_ce_bwd, 13),
+    ACX_ENTRY(attn_plan, 5),      ACX_ENTRY(attn_fwd, 9),       ACX_ENTRY(attn_bwd, 14),      ACX_ENTRY(embed_fwd, 5),
+    ACX_ENTRY(embed_bwd, 7),      ACX_ENTRY(grad_clip, 6),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_acx_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
