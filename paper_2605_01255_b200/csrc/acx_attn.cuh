@@ -71,11 +71,10 @@ struct Params {
   float cap_out;             // cap log2(e)
   float* lse;                // [heads][tokens], natural logarithm
   int* status;
-  // forward
   __nv_bfloat16* O;
   int64_t ldo;
   // backward
-  const float* delta;        // [heads][tokens]
+  float* delta;              // [heads][tokens], made exact by the launch for the queries
   __nv_bfloat16 *dQ, *dK, *dV;
   int64_t lddq, lddk, lddv;
   float *dk_part, *dv_part;  // [part][tokens][kv_heads][d], or null: one part, written to dK and dV
@@ -141,27 +140,39 @@ __device__ __forceinline__ void tmem_loaded(V&... v) {
   (hand_over(v), ...);
 }
 
+__device__ __forceinline__ Item fetch_item(const Item* items, int k) {
+  const int4 v = __ldcg(reinterpret_cast<const int4*>(items) + k);
+  return Item{v.x, v.y, v.z, v.w};
+}
+// The same by a whole warp, as values that are known to be the same in all lanes.
+__device__ __forceinline__ Item fetch_item_warp(const Item* items, int k) {
+  const Item t = fetch_item(items, k);
+  return Item{__shfl_sync(0xFFFFFFFFu, t.row0, 0), __shfl_sync(0xFFFFFFFFu, t.start, 0), __shfl_sync(0xFFFFFFFFu, t.end, 0),
+              __shfl_sync(0xFFFFFFFFu, t.prefix, 0)};
+}
+
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// 32 columns of a row from registers, times f, as bf16; `left` columns (a multiple of 8) are inside the head.  Two stores of 32 bytes
-// where the row's address allows them.
-__device__ __forceinline__ void store_bf16(__nv_bfloat16* at, const uint32_t (&v)[32], float f, int left) {
-  uint32_t w[16];
+// COLS columns (16 or 32) of a row from registers, times f, as bf16; `left` columns (a multiple of 8) are inside the head.  Stores
+// of 32 bytes where the row's address allows them.
+template <int COLS>
+__device__ __forceinline__ void store_bf16(__nv_bfloat16* at, const uint32_t (&v)[COLS], float f, int left) {
+  uint32_t w[COLS / 2];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) w[i] = pack2(__uint_as_float(v[2 * i]) * f, __uint_as_float(v[2 * i + 1]) * f);
-  if (left >= 32 && (reinterpret_cast<uintptr_t>(at) & 31) == 0) {
+  for (int i = 0; i < COLS / 2; ++i) w[i] = pack2(__uint_as_float(v[2 * i]) * f, __uint_as_float(v[2 * i + 1]) * f);
+  if (left >= COLS && (reinterpret_cast<uintptr_t>(at) & 31) == 0) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < COLS / 16; ++i)
       asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(at + 16 * i), "r"(w[8 * i]), "r"(w[8 * i + 1]), "r"(w[8 * i + 2]),
                    "r"(w[8 * i + 3]), "r"(w[8 * i + 4]), "r"(w[8 * i + 5]), "r"(w[8 * i + 6]), "r"(w[8 * i + 7])
                    : "memory");
     return;
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < COLS / 8; ++i)
     if (8 * i < left) *reinterpret_cast<uint4*>(at + 8 * i) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
 }
 __device__ __forceinline__ void store_f32(float* at, const uint32_t (&v)[32], float f, int left) {
@@ -201,36 +212,57 @@ struct Tile {
 #pragma unroll
     for (int c = 0; c < kChunks; ++c) ptx::tma_load_3d(dst + c * kChunkBytes, map, bar, 64 * c, head, row);
   }
-  // One thread: zeros into rows [first, last), at most 15, visible to the tensor core.
+  // A whole warp: zeros into rows [first, last), visible to the tensor core.
   static __device__ __forceinline__ void zero_rows(uint8_t* tile, int first, int last) {
+    const int n = (last - first) * 8;   // 16-byte units; the swizzle stays within a row
     for (int c = 0; c < kChunks; ++c)
-#pragma unroll 8
-      for (int i = first * 128; i < last * 128; i += 16)   // the swizzle stays within a row
-        *reinterpret_cast<uint4*>(tile + c * kChunkBytes + i) = make_uint4(0u, 0u, 0u, 0u);
+      for (int i = threadIdx.x & 31; i < n; i += 32)
+        *reinterpret_cast<uint4*>(tile + c * kChunkBytes + first * 128 + i * 16) = make_uint4(0u, 0u, 0u, 0u);
     ptx::fence_proxy_async_smem();
+    __syncwarp();
   }
 };
 
-// Products of 128-row tiles, issued by one thread.  D (128 x 128) = A B^T over the head's columns, both tiles K-major.
+// Products of 128-row tiles; a whole warp.  Unrolled without regard to where the operands live, the descriptors of all steps of all
+// products of a kernel are live at once, more than there are uniform registers, and products were seen to run with another
+// step's operand: each block of four steps takes its own from one base instead.
+//
+// D (128 x 128) = A B^T over the head's columns, both tiles K-major.
 template <int HD>
 __device__ __forceinline__ void scores_mma(uint32_t tmem_d, uint32_t a, uint32_t b, int d16) {
   const uint32_t idesc = ptx::make_idesc_bf16(kRows, kRows, false, false);
   const uint64_t da = ptx::make_smem_desc(a, 16, 1024), db = ptx::make_smem_desc(b, 16, 1024);
+  const uint32_t hi = uint32_t(da >> 32);
 #pragma unroll
-  for (int k = 0; k < HD / 16; ++k) {
-    const uint64_t at = uint64_t((k >> 2) * (Tile<HD>::kChunkBytes >> 4) + (k & 3) * 2);
-    if (k < d16) ptx::umma_bf16(tmem_d, da + at, db + at, idesc, k > 0);
+  for (int c = 0; c < HD / 64; ++c) {
+    const uint32_t al = uint32_t(da) + c * (Tile<HD>::kChunkBytes >> 4), bl = uint32_t(db) + c * (Tile<HD>::kChunkBytes >> 4);
+    const int steps = d16 - 4 * c;
+    if (steps >= 4) {
+      ptx::umma_steps<4>(tmem_d, al, bl, hi, idesc, c > 0);
+    } else {
+#pragma unroll 1
+      for (int k = 0; k < steps; ++k) ptx::umma_steps<1>(tmem_d, al + 2 * k, bl + 2 * k, hi, idesc, c > 0 || k > 0);
+    }
   }
 }
-// D (128 x 16 d16) (+)= A B with A (128 x 16 steps, bf16) in tensor memory and B the first 16 * steps rows of a tile.  The columns of
-// A from 64 on start at tmem_a2.
-template <int HD>
-__device__ __forceinline__ void rows_mma(uint32_t tmem_d, uint32_t tmem_a, uint32_t tmem_a2, uint32_t b, int steps, int d16, bool add) {
+// D (128 x 16 d16) (+)= A B with A (128 x 16 steps, bf16) in tensor memory and B the first 16 * steps rows of a tile.  Every 32
+// columns of A start 16 + GAP columns of tensor memory apart, 16 in use.
+template <int HD, int GAP>
+__device__ __forceinline__ void rows_mma(uint32_t tmem_d, uint32_t tmem_a, uint32_t b, int steps, int d16, bool add) {
   const uint32_t idesc = ptx::make_idesc_bf16(kRows, 16 * d16, false, true);
   const uint64_t db = ptx::make_smem_desc(b, Tile<HD>::kChunkBytes, 1024);
+  const uint32_t lo = uint32_t(db), hi = uint32_t(db >> 32);
 #pragma unroll
-  for (int k = 0; k < kRows / 16; ++k)
-    if (k < steps) ptx::umma_bf16_tmem_a(tmem_d, (k < 4 ? tmem_a : tmem_a2 - 32) + 8 * k, db + uint64_t(k * (16 * 128 >> 4)), idesc, add || k > 0);
+  for (int c = 0; c < 2; ++c) {
+    const uint32_t at = tmem_a + c * (32 + 2 * GAP), bl = lo + c * 512;
+    if (steps >= 4 * c + 4) {
+      ptx::umma_steps_tmem_a<4, 8 + GAP>(tmem_d, at, bl, hi, idesc, add || c > 0);
+    } else {
+#pragma unroll 1
+      for (int k = 0; k < steps - 4 * c; ++k)
+        ptx::umma_steps_tmem_a<1, 0>(tmem_d, at + 8 * k + (k >= 2 ? GAP : 0), bl + 128 * k, hi, idesc, add || c > 0 || k > 0);
+    }
+  }
 }
 
 Params common_params(const AttnProblem& q, const void* plan, const float* slopes, float* lse, int* status);

@@ -1,22 +1,28 @@
 // Attention: the backward kernels.
 //
-// With dO and the forward's lse, and delta_i = sum over the columns of dO_i O_i,
+// With dO and the forward's lse, and delta_i = sum over the keys of p_ij dP_ij (which is dO_i O_i),
 //     P = 2^(x - lse),   dP = dO V^T,   dS = P (dP - delta) dx/ds,
 //     dQ = scale dS K,   dK = scale dS^T Q,   dV = P^T dO.
-// Two kernels, each with sums that no other work item adds to, so that no atomics are needed and results are reproducible bit for
-// bit: one per tile of queries (three products: S, dP, dQ), one per tile of keys and key head (four: S^T, dP^T, dV, dK), which
-// goes through the query heads of the group and the queries that see the tile.  The price is that S and dP are computed twice: seven
-// products instead of five.
+// Two launches of one kernel, each with sums that no other work item adds to, so that no atomics are needed and results are
+// reproducible bit for bit.  Rows of the tile: queries (dQ) or keys (dK, dV).  Either has two tiles that stay (Q, dO or K, V) and goes
+// through pairs of others (K, V of the keys that the queries see; Q, dO of the queries that see the keys, head by head of the group):
+//     S = R0 T0^T,   dP = R1 T1^T,   first += P T,   second += dS T0.
+// For keys `first` is dV (T = dO) and `second` dK.  For queries `second` is dQ, and `first` = P K corrects it: O rounded to bf16
+// gives delta to within that rounding only, and an error e of delta is one of -e P K in dQ, which was as large as the rounding of dS and dQ
+// together (errors of dQ 0.0029 relative to its size, 0.0024 with it).  So dS is taken with the delta that O gives, r_i = sum of
+// p (dP - delta) summed in fp32 beside it, and dQ = scale (second - r first); delta + r is what the launch for the keys uses.
+// The price of two launches is that S and dP are computed twice: eight products instead of five.
 //
-// Queries (dQ): S is double buffered, dP and dQ are not: 4 x 128 columns of tensor memory.  Lane = query; eight warps take 64
-// keys each of their 32 rows.  dS is written over dP as bf16 and multiplied with K from there.
-// Keys (dK, dV): S^T, dP^T, dV, dK fill the tensor memory.  Lane = key, columns = queries.  While the exponentials of a tile are
-// taken the tensor core runs dK of the tile before and dP^T, while dS is formed dV and the next S^T.
+// S, dP, first and second fill the tensor memory (4 x 128 columns).  While the exponentials of a tile are taken the tensor core runs
+// `second` of the tile before and dP, while dS is formed `first` and the next S.  Sixteen warps share a tile, 32 rows x 32 columns
+// each: eight with 64 columns were bound by the latencies of their dependent steps (dK, dV of 8192 x 24 x 8 x 128 1104 us).
 //
 // A query that sees one key only has p = 1 and no gradient through its scores: exactly zero, not the difference of two roundings.
 //
 // Where a batch has few key tiles for the SMs a group's query heads are dealt to several work items, whose fp32 sums a last kernel adds
 // in a fixed order.
+#include <cuda_fp16.h>
+
 #include <algorithm>
 
 #include "acx_attn.cuh"
@@ -26,9 +32,9 @@ namespace acx {
 namespace attn {
 namespace {
 
-constexpr int kThreads = 384;
-constexpr int kRowWarps = 8;
-constexpr int kPanel = 64;        // columns of a tile that one warp takes
+constexpr int kRowWarp0 = 4, kRowWarps = 16, kThreads = 32 * (kRowWarp0 + kRowWarps);
+constexpr int kPanel = 32;        // columns of a tile that one warp takes
+constexpr int kPanels = kRows / kPanel;
 
 // ------------------------------------------------------------------------------------------------------------------ delta
 // delta[head][token] = sum of dO O over the head's columns.  Sixteen lanes per row.
@@ -71,85 +77,127 @@ struct Ring {   // stages of a tile each
   }
 };
 
-__device__ __forceinline__ Item fetch_item(const Params& p, int k) {
-  const int4 v = __ldcg(reinterpret_cast<const int4*>(p.items) + k);
-  return Item{v.x, v.y, v.z, v.w};
-}
+__device__ __forceinline__ void load_columns(uint32_t at, uint32_t (&v)[32]) { ptx::tmem_ld_x32(at, v); }
+__device__ __forceinline__ void load_columns(uint32_t at, uint32_t (&v)[16]) { ptx::tmem_ld_x16(at, v); }
 
-// ---------------------------------------------------------------------------------------------------------------- queries
-template <int HD>
-struct QuerySmem {
-  static constexpr int kK = HD == 128 ? 3 : 4, kV = HD == 128 ? 2 : 4;   // stages
-  static constexpr int kTiles = 2 + kK + kV, kBars = kTiles * Tile<HD>::kBytes, kBytes = kBars + 512 + 1024;
+// KEYS: rows are keys
+template <int HD, bool KEYS>
+struct Smem {
+  static constexpr int kT0 = KEYS ? 2 : 3, kT1 = 2;                    // stages
+  static constexpr int kVec = (2 + kT0 + kT1) * Tile<HD>::kBytes;
+  static constexpr int kVecStages = KEYS ? 4 : 0, kVecBytes = 2 * kRows * 4;   // KEYS: lse and delta of a tile of queries
+  static constexpr int kPartBytes = kPanels / 2 * kRows * 4;
+  static constexpr int kExchange = kVec + kVecStages * kVecBytes;              // else: partial sums of the rows
+  static constexpr int kBars = kExchange + (KEYS ? 0 : kPartBytes), kBytes = kBars + 256 + 1024;
   static_assert(kBytes <= 232448, "shared memory of one CTA");
 };
 
-template <int HD, bool CAP, bool BIAS>
+// What one work item goes through.
+struct Unit {
+  Item t;
+  int head, heads;       // query heads: the first, how many
+  int kv_head, part;
+  int other0, tiles;     // first token and number of the tiles on the other side
+};
+
+template <int HD, bool KEYS, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(kThreads, 1)
-    attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                   const __grid_constant__ CUtensorMap map_do, const Params p) {
+    attn_bwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                    const __grid_constant__ CUtensorMap map_do, const Params p) {
   using T = Tile<HD>;
-  using M = QuerySmem<HD>;
+  using M = Smem<HD, KEYS>;
   extern __shared__ uint8_t smem_raw[];
-  const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;   // tiles start on their swizzle's boundary
   uint8_t* gen = smem_raw + (base - ptx::smem_u32(smem_raw));
-  const uint32_t q_tile = base, do_tile = base + T::kBytes, k_tiles = base + 2 * T::kBytes, v_tiles = k_tiles + M::kK * T::kBytes;
+  const uint32_t r0_tile = base, r1_tile = base + T::kBytes, t0_tiles = base + 2 * T::kBytes, t1_tiles = t0_tiles + M::kT0 * T::kBytes;
   const uint32_t bars = base + M::kBars;
-  auto k_full = [&](int s) { return bars + 8u * s; };
-  auto k_empty = [&](int s) { return bars + 32 + 8u * s; };
-  auto v_full = [&](int s) { return bars + 64 + 8u * s; };
-  auto v_empty = [&](int s) { return bars + 96 + 8u * s; };
-  const uint32_t q_full = bars + 128, q_empty = bars + 136, dp_full = bars + 160, ds_full = bars + 168, out_full = bars + 176, out_free = bars + 184,
-                 done = bars + 192;
-  auto s_full = [&](int b) { return bars + 144 + 8u * b; };
-  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + M::kBars + 200);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + M::kBars + 204);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  auto t0_full = [&](int s) { return bars + 8u * s; };
+  auto t0_empty = [&](int s) { return bars + 24 + 8u * s; };
+  auto t1_full = [&](int s) { return bars + 48 + 8u * s; };
+  auto t1_empty = [&](int s) { return bars + 64 + 8u * s; };
+  auto vec_full = [&](int s) { return bars + 80 + 8u * s; };
+  auto vec_empty = [&](int s) { return bars + 112 + 8u * s; };
+  const uint32_t r_full = bars + 144, r_empty = bars + 152, s_full = bars + 160, p_full = bars + 168, dp_full = bars + 176, ds_full = bars + 184,
+                 out_full = bars + 192, out_free = bars + 200, done = bars + 208, parts_full = bars + 216, parts_free = bars + 224;
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + M::kBars + 232);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + M::kBars + 236);
+  volatile int* no_abort = abort_flag + 1;   // for the one wait that has to run its time even so
+  const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // the warp's number, known to be the same in all lanes
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < 4; ++s) {
-      ptx::mbar_init(k_full(s), 1);
-      ptx::mbar_init(k_empty(s), 1);
-      ptx::mbar_init(v_full(s), 1);
-      ptx::mbar_init(v_empty(s), 1);
+    for (int s = 0; s < M::kT0; ++s) {
+      ptx::mbar_init(t0_full(s), 1);
+      ptx::mbar_init(t0_empty(s), 1);
     }
-    ptx::mbar_init(q_full, 1);
-    ptx::mbar_init(q_empty, 1);
-    ptx::mbar_init(s_full(0), 1);
-    ptx::mbar_init(s_full(1), 1);
+    for (int s = 0; s < M::kT1; ++s) {
+      ptx::mbar_init(t1_full(s), 1);
+      ptx::mbar_init(t1_empty(s), 1);
+    }
+    for (int s = 0; s < M::kVecStages; ++s) {
+      ptx::mbar_init(vec_full(s), 1);
+      ptx::mbar_init(vec_empty(s), kRowWarps);
+    }
+    ptx::mbar_init(r_full, 1);
+    ptx::mbar_init(r_empty, 1);
+    ptx::mbar_init(s_full, 1);
+    ptx::mbar_init(p_full, kRowWarps);
     ptx::mbar_init(dp_full, 1);
     ptx::mbar_init(ds_full, kRowWarps);
     ptx::mbar_init(out_full, 1);
     ptx::mbar_init(out_free, kRowWarps);
     ptx::mbar_init(done, 1);
+    *no_abort = 0;
+    ptx::mbar_init(parts_full, kRowWarps);
+    ptx::mbar_init(parts_free, kRowWarps);
     *abort_flag = 0;
-    ptx::fence_barrier_init();   // no prefetch of the tensor maps: a block without work would leave with it in flight
+    ptx::fence_barrier_init();
   }
+  // A warp comes to the barrier as a whole: halves of it would count as two, and let the others read the address before it is there
+  __syncwarp();
   if (warp == 1) {
-    ptx::tmem_alloc(bars + 200, 512);
+    ptx::tmem_alloc(bars + 232, 512);
     ptx::tmem_relinquish_alloc_permit();
+    __syncwarp();
   }
   ptx::tcgen05_fence_before_sync();
   __syncthreads();
   ptx::tcgen05_fence_after_sync();
   const uint32_t tmem = *tmem_slot;
-  auto tmem_s = [&](int b) { return tmem + 128u * b; };
-  const uint32_t tmem_dp = tmem + 256, tmem_dq = tmem + 384;
+  const uint32_t tmem_s = tmem, tmem_dp = tmem + 128, tmem_first = tmem + 256, tmem_second = tmem + 384;
   wait_for_launch_before();
   let_next_launch_start();
-  const int units = __ldcg(&p.plan->tiles) * p.heads;
+  const int per_tile = KEYS ? p.kv_heads * p.parts : p.heads;
+  const int units = __ldcg(&p.plan->tiles) * per_tile;
   auto give_up = [&]() {
     *abort_flag = 1;
     atomicExch(p.status, kDevTimeout);
   };
-  auto key_tiles = [&](const Item& t) {
-    return ((p.causal ? max(min(t.row0 + kRows, t.end), t.prefix) : t.end) - t.start + kRows - 1) / kRows;
+  auto decode = [&](int u, const Item& t) {
+    Unit w;
+    w.t = t;
+    const int r = u % per_tile;
+    if (KEYS) {
+      w.kv_head = r / p.parts;
+      w.part = r % p.parts;
+      w.head = w.kv_head * p.group + w.part * p.heads_per_part;
+      w.heads = min(p.heads_per_part, p.group - w.part * p.heads_per_part);
+      w.other0 = p.causal && w.t.row0 >= w.t.prefix ? w.t.row0 : w.t.start;
+      w.tiles = (w.t.end - w.other0 + kRows - 1) / kRows;
+    } else {
+      w.head = r;
+      w.heads = 1;
+      w.kv_head = r / p.group;
+      w.part = 0;
+      w.other0 = w.t.start;
+      w.tiles = ((p.causal ? max(min(w.t.row0 + kRows, w.t.end), w.t.prefix) : w.t.end) - w.t.start + kRows - 1) / kRows;
+    }
+    return w;
   };
 
   if (warp == 0) {
     // ---------------------------------------------------------------------------------------------------- copies
     if (lane == 0) {
-      Ring rk(M::kK), rv(M::kV);
+      Ring r0(M::kT0), r1(M::kT1);
       int it = 0;
       bool ok = true;
       auto push = [&](Ring& r, uint32_t full, uint32_t empty, uint32_t tiles, const CUtensorMap* map, int head, int row) {
@@ -159,16 +207,17 @@ __global__ void __launch_bounds__(kThreads, 1)
         T::load(tiles + s.stage * T::kBytes, map, full + 8u * s.stage, head, row);
       };
       for (int u = blockIdx.x; ok && u < units; u += gridDim.x, ++it) {
-        const Item t = fetch_item(p, u / p.heads);
-        const int h = u % p.heads, g = h / p.group, n = key_tiles(t);
-        if (!ptx::mbar_wait(q_empty, (it & 1) ^ 1u, abort_flag)) { give_up(); ok = false; break; }
-        ptx::mbar_arrive_expect_tx(q_full, 2 * T::kBytes);
-        T::load(q_tile, &map_q, q_full, h, t.row0);
-        T::load(do_tile, &map_do, q_full, h, t.row0);
-        for (int j = 0; ok && j < n; ++j) {
-          push(rk, k_full(0), k_empty(0), k_tiles, &map_k, g, t.start + j * kRows);
-          if (ok) push(rv, v_full(0), v_empty(0), v_tiles, &map_v, g, t.start + j * kRows);
-        }
+        const Unit w = decode(u, fetch_item(p.items, u / per_tile));
+        if (!ptx::mbar_wait(r_empty, (it & 1) ^ 1u, abort_flag)) { give_up(); ok = false; break; }
+        ptx::mbar_arrive_expect_tx(r_full, 2 * T::kBytes);
+        T::load(r0_tile, KEYS ? &map_k : &map_q, r_full, KEYS ? w.kv_head : w.head, w.t.row0);
+        T::load(r1_tile, KEYS ? &map_v : &map_do, r_full, KEYS ? w.kv_head : w.head, w.t.row0);
+        for (int h = w.head; ok && h < w.head + w.heads; ++h)
+          for (int i = 0; ok && i < w.tiles; ++i) {
+            const int other = KEYS ? h : w.kv_head, row = w.other0 + i * kRows;
+            push(r0, t0_full(0), t0_empty(0), t0_tiles, KEYS ? &map_q : &map_k, other, row);
+            if (ok) push(r1, t1_full(0), t1_empty(0), t1_tiles, KEYS ? &map_do : &map_v, other, row);
+          }
       }
       if (!ok) {   // copies in flight land before the CTA leaves: one limit, well above a copy's time
         const uint64_t t0 = ptx::globaltimer_ns();
@@ -178,523 +227,318 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncwarp();
   } else if (warp == 1) {
     // ---------------------------------------------------------------------------------------------------- products
-    if (lane == 0) {
-      Ring rk(M::kK), rv(M::kV);
-      int it = 0, turns = 0;
-      bool ok = true;
-      const int d16 = (p.d + 15) / 16;
-      auto wait = [&](uint32_t bar, uint32_t parity) {
-        if (ok && !ptx::mbar_wait(bar, parity, abort_flag)) { give_up(); ok = false; }
-        return ok;
-      };
-      for (int u = blockIdx.x; ok && u < units; u += gridDim.x, ++it) {
-        const Item t = fetch_item(p, u / p.heads);
-        const int n = key_tiles(t);
-        // K of tile j is here: rows behind the document's end become zeros (dS K sums over them)
-        auto ready = [&](Ring::Slot k, int j) {
-          if (!wait(k_full(k.stage), k.phase)) return false;
-          const int left = t.end - (t.start + j * kRows);
-          if (left < kRows && left % 16) T::zero_rows(gen + (k_tiles - base) + k.stage * T::kBytes, left, (left + 15) & ~15);
-          ptx::tcgen05_fence_after_sync();
-          return true;
-        };
-        auto scores = [&](Ring::Slot k, int turn) {
-          scores_mma<HD>(tmem_s(turn & 1), q_tile, k_tiles + k.stage * T::kBytes, d16);
-          ptx::umma_commit(s_full(turn & 1));
-        };
-        auto dprobs = [&](Ring::Slot v) {
-          scores_mma<HD>(tmem_dp, do_tile, v_tiles + v.stage * T::kBytes, d16);
-          ptx::umma_commit(dp_full);
-          ptx::umma_commit(v_empty(v.stage));
-        };
-        wait(q_full, it & 1);
-        Ring::Slot k = rk.next(), k_next = k, v = rv.next();
-        if (!ready(k, 0)) break;
-        scores(k, turns);
-        if (!wait(v_full(v.stage), v.phase)) break;
-        ptx::tcgen05_fence_after_sync();
-        dprobs(v);
-        for (int j = 0; ok && j < n; ++j, ++turns) {
-          if (j + 1 < n) {
-            k_next = rk.next();
-            if (!ready(k_next, j + 1)) break;
-            scores(k_next, turns + 1);   // its buffer was read before the dS of the tile before
-          }
-          if (j == 0 && !wait(out_free, (it & 1) ^ 1u)) break;
-          if (!wait(ds_full, turns & 1)) break;
-          ptx::tcgen05_fence_after_sync();
-          const int steps = min(kRows, t.end - (t.start + j * kRows) + 15) / 16;
-          rows_mma<HD>(tmem_dq, tmem_dp, tmem_dp + kPanel, k_tiles + k.stage * T::kBytes, steps, d16, j > 0);
-          ptx::umma_commit(k_empty(k.stage));
-          if (j == n - 1) {
-            ptx::umma_commit(out_full);
-            ptx::umma_commit(q_empty);
-          }
-          if (j + 1 < n) {
-            v = rv.next();
-            if (!wait(v_full(v.stage), v.phase)) break;
-            ptx::tcgen05_fence_after_sync();
-            dprobs(v);
-          }
-          k = k_next;
-        }
-      }
-      if (it > 0 || !ok) {
-        ptx::umma_commit(done);
-        const uint64_t t0 = ptx::globaltimer_ns();
-        while (!ptx::mbar_try_wait(done, 0) && ptx::globaltimer_ns() - t0 < ptx::kWaitLimitNs) {}
-      }
-    }
-    __syncwarp();
-  } else if (warp >= 4) {
-    // ---------------------------------------------------------------------------------------------------- rows
-    const int panel = (warp - 4) >> 2, quarter = warp & 3;
-    const uint32_t lanes = uint32_t(32 * quarter) << 16, col0 = kPanel * panel;
-    int turns = 0, it = 0;
+    Ring r0(M::kT0), r1(M::kT1);
+    int it = 0, turns = 0;
     bool ok = true;
+    const int d16 = (p.d + 15) / 16;
+    auto wait = [&](uint32_t bar, uint32_t parity) {
+      if (ok && !warp_wait(bar, parity, abort_flag)) { give_up(); ok = false; }
+      return ok;
+    };
     for (int u = blockIdx.x; ok && u < units; u += gridDim.x, ++it) {
-      const Item t = fetch_item(p, u / p.heads);
-      const int n = key_tiles(t), head = u % p.heads;
-      const int row = t.row0 + 32 * quarter + lane;
-      const int sees = p.causal ? min(max(row + 1, t.prefix), t.end) : t.end;
-      const int all_see = p.causal ? min(max(t.row0 + 1, t.prefix), t.end) : t.end;
-      const float slope2 = BIAS ? __ldg(p.slopes + head) * kLog2e : 0.f;
-      const bool live = row < t.end;
-      const int64_t at = int64_t(head) * p.tokens + row;
-      const float lse2 = live ? __ldcg(p.lse + at) * kLog2e : 0.f, delta = live ? __ldcg(p.delta + at) : 0.f;
-      const float one = sees - t.start > 1 ? 1.f : 0.f;
-      for (int j = 0; j < n; ++j, ++turns) {
-        if (!warp_wait(s_full(turns & 1), (turns >> 1) & 1, abort_flag)) { give_up(); ok = false; break; }
+      const Unit w = decode(u, fetch_item_warp(p.items, u / per_tile));
+      const int n = w.heads * w.tiles;
+      auto left_of = [&](int i) { return w.t.end - (w.other0 + (i % w.tiles) * kRows); };   // tokens from this tile's start to the end
+      // a tile is here; if products sum over its rows, those behind the document's end become zeros up to a whole step
+      auto ready = [&](uint32_t full, Ring::Slot s, uint32_t tiles, int i, bool summed) {
+        if (!wait(full + 8u * s.stage, s.phase)) return false;
+        const int left = left_of(i);
+        if (summed && left < kRows && left % 16)
+          T::zero_rows(gen + (tiles - base) + s.stage * T::kBytes, left, (left + 15) & ~15);
         ptx::tcgen05_fence_after_sync();
-        uint32_t s[2][32];
-#pragma unroll
-        for (int c = 0; c < 2; ++c) ptx::tmem_ld_x32(tmem_s(turns & 1) + lanes + col0 + 32 * c, s[c]);
-        tmem_loaded(s[0], s[1]);
-        const int k0 = t.start + j * kRows + int(col0);
-        const bool masked = k0 + kPanel > all_see;
-        const int limit = sees - k0;
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            float slope = 1.f;
-            float x;
-            if (!CAP && !BIAS) x = fmaf(__uint_as_float(s[c][i]), p.c, -lse2);
-            else x = exponent<CAP, BIAS>(p, __uint_as_float(s[c][i]), float(row - k0) - float(32 * c + i), slope2, &slope) - lse2;
-            float w = exp2_fast(x);
-            if (CAP) w *= slope;
-            s[c][i] = __float_as_uint(w);
-          }
-        if (masked) {
-#pragma unroll
-          for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int i = 0; i < 32; ++i) s[c][i] = 32 * c + i < limit ? __float_as_uint(__uint_as_float(s[c][i]) * one) : 0u;
-        }
-        if (!warp_wait(dp_full, turns & 1, abort_flag)) { give_up(); ok = false; break; }
+        return true;
+      };
+      auto scores = [&](Ring::Slot a) {
+        scores_mma<HD>(tmem_s, r0_tile, t0_tiles + a.stage * T::kBytes, d16);
+        ptx::umma_commit_elected(s_full);
+      };
+      auto dprobs = [&](Ring::Slot b, bool last) {
+        scores_mma<HD>(tmem_dp, r1_tile, t1_tiles + b.stage * T::kBytes, d16);
+        ptx::umma_commit_elected(dp_full);
+        if (!KEYS) ptx::umma_commit_elected(t1_empty(b.stage));
+        if (last) ptx::umma_commit_elected(r_empty);
+      };
+      wait(r_full, it & 1);
+      Ring::Slot a = r0.next(), b = r1.next(), a_next = a, b_next = b;
+      if (!ready(t0_full(0), a, t0_tiles, 0, true)) break;
+      scores(a);
+      if (!ready(t1_full(0), b, t1_tiles, 0, KEYS)) break;
+      dprobs(b, n == 1);
+      for (int i = 0; ok && i < n; ++i, ++turns) {
+        const int steps = min(kRows, left_of(i) + 15) / 16;
+        if (i == 0 && !wait(out_free, (it & 1) ^ 1u)) break;
+        if (!wait(p_full, turns & 1)) break;
         ptx::tcgen05_fence_after_sync();
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          uint32_t g[32], w[16];
-          ptx::tmem_ld_x32(tmem_dp + lanes + col0 + 32 * c, g);
-          tmem_loaded(g);
-          // a masked key's dP may be anything (rows of another document): selected away, not multiplied
-          if (masked) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) g[i] = 32 * c + i < limit ? g[i] : __float_as_uint(delta);
-          }
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            w[i] = pack2(__uint_as_float(s[c][2 * i]) * (__uint_as_float(g[2 * i]) - delta),
-                         __uint_as_float(s[c][2 * i + 1]) * (__uint_as_float(g[2 * i + 1]) - delta));
-          ptx::tmem_st_x16(tmem_dp + lanes + col0 + 16 * c, w);
+        rows_mma<HD, 16>(tmem_first, tmem_s, KEYS ? t1_tiles + b.stage * T::kBytes : t0_tiles + a.stage * T::kBytes, steps, d16, i > 0);
+        if (KEYS) ptx::umma_commit_elected(t1_empty(b.stage));
+        if (i + 1 < n) {
+          a_next = r0.next();
+          if (!ready(t0_full(0), a_next, t0_tiles, i + 1, true)) break;
+          scores(a_next);
         }
-        ptx::tmem_st_wait();
-        ptx::tcgen05_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(ds_full);
-        __syncwarp();
-      }
-      if (!ok) break;
-      if (!warp_wait(out_full, it & 1, abort_flag)) { give_up(); break; }
-      ptx::tcgen05_fence_after_sync();
-      // the panel's half of the head's columns
-      __nv_bfloat16* out = p.dQ + int64_t(row) * p.lddq + int64_t(head) * p.d;
-      uint32_t o[HD / 64][32];
-#pragma unroll
-      for (int c = 0; c < HD / 64; ++c) ptx::tmem_ld_x32(tmem_dq + lanes + HD / 2 * panel + 32 * c, o[c]);
-      ptx::tmem_ld_wait();
-#pragma unroll
-      for (int c = 0; c < HD / 64; ++c) hand_over(o[c]);
-      ptx::tcgen05_fence_before_sync();
-      __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(out_free);
-      __syncwarp();
-#pragma unroll
-      for (int c = 0; c < HD / 64; ++c) {
-        const int at_col = HD / 2 * panel + 32 * c;
-        if (live && at_col < p.d) store_bf16(out + at_col, o[c], p.scale, p.d - at_col);
-      }
-    }
-  }
-  zero_rows_outside(p, p.dQ, p.lddq, p.heads, nullptr, 0.f);
-  __syncwarp();
-  ptx::tcgen05_fence_before_sync();
-  __syncthreads();
-  if (warp == 1) {
-    __syncwarp();
-    ptx::tcgen05_fence_after_sync();
-    ptx::tmem_dealloc(tmem, 512);
-  }
-}
-
-// ------------------------------------------------------------------------------------------------------------------- keys
-template <int HD>
-struct KeySmem {
-  static constexpr int kStages = 2;   // of Q and of dO each
-  static constexpr int kTiles = 2 + 2 * kStages, kVec = kTiles * Tile<HD>::kBytes;
-  static constexpr int kVecStages = 4, kVecBytes = 2 * kRows * 4;     // lse and delta of a tile of queries
-  static constexpr int kBars = kVec + kVecStages * kVecBytes, kBytes = kBars + 512 + 1024;
-  static_assert(kBytes <= 232448, "shared memory of one CTA");
-};
-
-template <int HD, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(kThreads, 1)
-    attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                    const __grid_constant__ CUtensorMap map_do, const Params p) {
-  using T = Tile<HD>;
-  using M = KeySmem<HD>;
-  extern __shared__ uint8_t smem_raw[];
-  const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
-  uint8_t* gen = smem_raw + (base - ptx::smem_u32(smem_raw));
-  const uint32_t k_tile = base, v_tile = base + T::kBytes, q_tiles = base + 2 * T::kBytes, do_tiles = q_tiles + M::kStages * T::kBytes;
-  const uint32_t bars = base + M::kBars;
-  auto q_full = [&](int s) { return bars + 8u * s; };
-  auto q_empty = [&](int s) { return bars + 16 + 8u * s; };
-  auto do_full = [&](int s) { return bars + 32 + 8u * s; };
-  auto do_empty = [&](int s) { return bars + 48 + 8u * s; };
-  auto vec_full = [&](int s) { return bars + 64 + 8u * s; };
-  auto vec_empty = [&](int s) { return bars + 96 + 8u * s; };
-  const uint32_t kv_full = bars + 128, kv_empty = bars + 136, s_full = bars + 144, p_full = bars + 152, dp_full = bars + 160, ds_full = bars + 168,
-                 out_full = bars + 176, out_free = bars + 184, done = bars + 192;
-  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + M::kBars + 200);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + M::kBars + 204);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-
-  if (threadIdx.x == 0) {
-    for (int s = 0; s < M::kStages; ++s) {
-      ptx::mbar_init(q_full(s), 1);
-      ptx::mbar_init(q_empty(s), 1);
-      ptx::mbar_init(do_full(s), 1);
-      ptx::mbar_init(do_empty(s), 1);
-    }
-    for (int s = 0; s < M::kVecStages; ++s) {
-      ptx::mbar_init(vec_full(s), 1);
-      ptx::mbar_init(vec_empty(s), kRowWarps);
-    }
-    ptx::mbar_init(kv_full, 1);
-    ptx::mbar_init(kv_empty, 1);
-    ptx::mbar_init(s_full, 1);
-    ptx::mbar_init(p_full, kRowWarps);
-    ptx::mbar_init(dp_full, 1);
-    ptx::mbar_init(ds_full, kRowWarps);
-    ptx::mbar_init(out_full, 1);
-    ptx::mbar_init(out_free, kRowWarps);
-    ptx::mbar_init(done, 1);
-    *abort_flag = 0;
-    ptx::fence_barrier_init();   // no prefetch of the tensor maps: a block without work would leave with it in flight
-  }
-  if (warp == 1) {
-    ptx::tmem_alloc(bars + 200, 512);
-    ptx::tmem_relinquish_alloc_permit();
-  }
-  ptx::tcgen05_fence_before_sync();
-  __syncthreads();
-  ptx::tcgen05_fence_after_sync();
-  const uint32_t tmem = *tmem_slot;
-  const uint32_t tmem_s = tmem, tmem_dp = tmem + 128, tmem_dv = tmem + 256, tmem_dk = tmem + 384;
-  wait_for_launch_before();
-  let_next_launch_start();
-  const int per_tile = p.kv_heads * p.parts;
-  const int units = __ldcg(&p.plan->tiles) * per_tile;
-  auto give_up = [&]() {
-    *abort_flag = 1;
-    atomicExch(p.status, kDevTimeout);
-  };
-  struct Unit {
-    Item t;
-    int kv_head, part, first_head, heads, q0, tiles;   // query heads, first query, tiles of queries
-  };
-  auto decode = [&](int u) {
-    Unit w;
-    w.t = fetch_item(p, u / per_tile);
-    const int r = u % per_tile;
-    w.kv_head = r / p.parts;
-    w.part = r % p.parts;
-    w.first_head = w.kv_head * p.group + w.part * p.heads_per_part;
-    w.heads = min(p.heads_per_part, p.group - w.part * p.heads_per_part);
-    w.q0 = p.causal && w.t.row0 >= w.t.prefix ? w.t.row0 : w.t.start;
-    w.tiles = (w.t.end - w.q0 + kRows - 1) / kRows;
-    return w;
-  };
-
-  if (warp == 0) {
-    // ---------------------------------------------------------------------------------------------------- copies
-    if (lane == 0) {
-      Ring rq(M::kStages), rd(M::kStages);
-      int it = 0;
-      bool ok = true;
-      auto push = [&](Ring& r, uint32_t full, uint32_t empty, uint32_t tiles, const CUtensorMap* map, int head, int row) {
-        const Ring::Slot s = r.next();
-        if (!ptx::mbar_wait(empty + 8u * s.stage, s.phase ^ 1u, abort_flag)) { give_up(); ok = false; return; }
-        ptx::mbar_arrive_expect_tx(full + 8u * s.stage, T::kBytes);
-        T::load(tiles + s.stage * T::kBytes, map, full + 8u * s.stage, head, row);
-      };
-      for (int u = blockIdx.x; ok && u < units; u += gridDim.x, ++it) {
-        const Unit w = decode(u);
-        if (!ptx::mbar_wait(kv_empty, (it & 1) ^ 1u, abort_flag)) { give_up(); ok = false; break; }
-        ptx::mbar_arrive_expect_tx(kv_full, 2 * T::kBytes);
-        T::load(k_tile, &map_k, kv_full, w.kv_head, w.t.row0);
-        T::load(v_tile, &map_v, kv_full, w.kv_head, w.t.row0);
-        for (int h = w.first_head; ok && h < w.first_head + w.heads; ++h)
-          for (int i = 0; ok && i < w.tiles; ++i) {
-            push(rq, q_full(0), q_empty(0), q_tiles, &map_q, h, w.q0 + i * kRows);
-            if (ok) push(rd, do_full(0), do_empty(0), do_tiles, &map_do, h, w.q0 + i * kRows);
-          }
-      }
-      if (!ok) {
-        const uint64_t t0 = ptx::globaltimer_ns();
-        while (ptx::globaltimer_ns() - t0 < 10000000ull) {}
-      }
-    }
-    __syncwarp();
-  } else if (warp == 1) {
-    // ---------------------------------------------------------------------------------------------------- products
-    if (lane == 0) {
-      Ring rq(M::kStages), rd(M::kStages);
-      int it = 0, turns = 0;
-      bool ok = true;
-      const int d16 = (p.d + 15) / 16;
-      auto wait = [&](uint32_t bar, uint32_t parity) {
-        if (ok && !ptx::mbar_wait(bar, parity, abort_flag)) { give_up(); ok = false; }
-        return ok;
-      };
-      for (int u = blockIdx.x; ok && u < units; u += gridDim.x, ++it) {
-        const Unit w = decode(u);
-        const int n = w.heads * w.tiles;
-        auto rows_of = [&](int i) { return w.t.end - (w.q0 + (i % w.tiles) * kRows); };   // queries from this tile's start to the end
-        // a tile of Q or dO is here: rows behind the document's end become zeros
-        auto ready = [&](uint32_t full, Ring::Slot s, uint32_t tiles, int i) {
-          if (!wait(full + 8u * s.stage, s.phase)) return false;
-          const int left = rows_of(i);
-          if (left < kRows && left % 16) T::zero_rows(gen + (tiles - base) + s.stage * T::kBytes, left, (left + 15) & ~15);
-          ptx::tcgen05_fence_after_sync();
-          return true;
-        };
-        auto scores = [&](Ring::Slot q) {
-          scores_mma<HD>(tmem_s, k_tile, q_tiles + q.stage * T::kBytes, d16);
-          ptx::umma_commit(s_full);
-        };
-        auto dprobs = [&](Ring::Slot d, bool last) {
-          scores_mma<HD>(tmem_dp, v_tile, do_tiles + d.stage * T::kBytes, d16);
-          ptx::umma_commit(dp_full);
-          if (last) ptx::umma_commit(kv_empty);
-        };
-        wait(kv_full, it & 1);
-        Ring::Slot q = rq.next(), d = rd.next(), q_next = q, d_next = d;
-        if (!ready(q_full(0), q, q_tiles, 0)) break;
-        scores(q);
-        if (!ready(do_full(0), d, do_tiles, 0)) break;
-        dprobs(d, n == 1);
-        for (int i = 0; ok && i < n; ++i, ++turns) {
-          const int steps = min(kRows, rows_of(i) + 15) / 16;
-          if (i == 0 && !wait(out_free, (it & 1) ^ 1u)) break;
-          if (!wait(p_full, turns & 1)) break;
-          ptx::tcgen05_fence_after_sync();
-          rows_mma<HD>(tmem_dv, tmem_s, tmem_s + kPanel, do_tiles + d.stage * T::kBytes, steps, d16, i > 0);
-          ptx::umma_commit(do_empty(d.stage));
-          if (i + 1 < n) {
-            q_next = rq.next();
-            if (!ready(q_full(0), q_next, q_tiles, i + 1)) break;
-            scores(q_next);
-          }
-          if (!wait(ds_full, turns & 1)) break;
-          ptx::tcgen05_fence_after_sync();
-          rows_mma<HD>(tmem_dk, tmem_dp, tmem_dp + kPanel, q_tiles + q.stage * T::kBytes, steps, d16, i > 0);
-          ptx::umma_commit(q_empty(q.stage));
-          if (i == n - 1) ptx::umma_commit(out_full);
-          if (i + 1 < n) {
-            d_next = rd.next();
-            if (!ready(do_full(0), d_next, do_tiles, i + 1)) break;
-            dprobs(d_next, i + 2 == n);
-          }
-          q = q_next;
-          d = d_next;
+        if (!wait(ds_full, turns & 1)) break;
+        ptx::tcgen05_fence_after_sync();
+        rows_mma<HD, 16>(tmem_second, tmem_dp, t0_tiles + a.stage * T::kBytes, steps, d16, i > 0);
+        ptx::umma_commit_elected(t0_empty(a.stage));
+        if (i == n - 1) ptx::umma_commit_elected(out_full);
+        if (i + 1 < n) {
+          b_next = r1.next();
+          if (!ready(t1_full(0), b_next, t1_tiles, i + 1, KEYS)) break;
+          dprobs(b_next, i + 2 == n);
         }
+        a = a_next;
+        b = b_next;
       }
-      if (it > 0 || !ok) {
-        ptx::umma_commit(done);
-        const uint64_t t0 = ptx::globaltimer_ns();
-        while (!ptx::mbar_try_wait(done, 0) && ptx::globaltimer_ns() - t0 < ptx::kWaitLimitNs) {}
-      }
+    }
+    if (it > 0 || !ok) {   // everything that was issued has to be done before the tensor memory is given back
+      ptx::umma_commit_elected(done);
+      warp_wait(done, 0, no_abort);
     }
     __syncwarp();
   } else if (warp == 2) {
-    // ---------------------------------------------------------------------------------------------------- lse and delta
-    Ring rv(M::kVecStages);
-    bool ok = true;
-    for (int u = blockIdx.x; ok && u < units; u += gridDim.x) {
-      const Unit w = decode(u);
-      for (int h = w.first_head; ok && h < w.first_head + w.heads; ++h)
-        for (int i = 0; ok && i < w.tiles; ++i) {
-          const Ring::Slot s = rv.next();
-          float a[4], b[4];
+    // ---------------------------------------------------------------------------------------------------- lse and delta of queries
+    if (KEYS) {
+      Ring rv(M::kVecStages);
+      bool ok = true;
+      for (int u = blockIdx.x; ok && u < units; u += gridDim.x) {
+        const Unit w = decode(u, fetch_item_warp(p.items, u / per_tile));
+        for (int h = w.head; ok && h < w.head + w.heads; ++h)
+          for (int i = 0; ok && i < w.tiles; ++i) {
+            const Ring::Slot s = rv.next();
+            float a[4], b[4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int row = w.q0 + i * kRows + 32 * k + lane;
-            const int64_t at = int64_t(h) * p.tokens + row;
-            a[k] = row < w.t.end ? __ldcg(p.lse + at) * kLog2e : 0.f;   // behind the document's end: masked
-            b[k] = row < w.t.end ? __ldcg(p.delta + at) : 0.f;
-          }
-          if (!warp_wait(vec_empty(s.stage), s.phase ^ 1u, abort_flag)) { give_up(); ok = false; break; }
-          float* v = reinterpret_cast<float*>(gen + M::kVec + s.stage * M::kVecBytes);
+            for (int k = 0; k < 4; ++k) {
+              const int row = w.other0 + i * kRows + 32 * k + lane;
+              const int64_t at = int64_t(h) * p.tokens + row;
+              a[k] = row < w.t.end ? __ldcg(p.lse + at) * kLog2e : 0.f;   // behind the document's end: masked
+              b[k] = row < w.t.end ? __ldcg(p.delta + at) : 0.f;
+            }
+            if (!warp_wait(vec_empty(s.stage), s.phase ^ 1u, abort_flag)) { give_up(); ok = false; break; }
+            float* v = reinterpret_cast<float*>(gen + M::kVec + s.stage * M::kVecBytes);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            v[32 * k + lane] = a[k];
-            v[kRows + 32 * k + lane] = b[k];
+            for (int k = 0; k < 4; ++k) {
+              v[32 * k + lane] = a[k];
+              v[kRows + 32 * k + lane] = b[k];
+            }
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(vec_full(s.stage));
+            __syncwarp();
           }
-          __syncwarp();
-          if (lane == 0) ptx::mbar_arrive(vec_full(s.stage));
-          __syncwarp();
-        }
+      }
     }
-  } else if (warp >= 4) {
+  } else if (warp >= kRowWarp0) {
     // ---------------------------------------------------------------------------------------------------- rows
-    const int panel = (warp - 4) >> 2, quarter = warp & 3;
+    const int panel = (warp - kRowWarp0) >> 2, quarter = warp & 3, r = 32 * quarter + lane;
     const uint32_t lanes = uint32_t(32 * quarter) << 16, col0 = kPanel * panel;
+    const uint32_t s_at = tmem_s + lanes + col0, dp_at = tmem_dp + lanes + col0;
     int turns = 0, it = 0;
-    Ring rv(M::kVecStages);
+    Ring rv(KEYS ? M::kVecStages : 1);
     bool ok = true;
     for (int u = blockIdx.x; ok && u < units; u += gridDim.x, ++it) {
-      const Unit w = decode(u);
-      const int key = w.t.row0 + 32 * quarter + lane;
-      // this key is seen by the queries from here on, and by none before; from `all_from` on every key of the tile is
-      const int from = p.causal && key >= w.t.prefix ? key : w.t.start;
-      const int all_from = p.causal && min(w.t.row0 + kRows, w.t.end) > w.t.prefix ? min(w.t.row0 + kRows, w.t.end) - 1 : w.t.start;
-      // the document's first query sees one key only
-      const bool lonely = w.t.end - w.t.start == 1 || (p.causal && w.t.prefix <= w.t.start + 1);
-      for (int h = w.first_head; ok && h < w.first_head + w.heads; ++h) {
+      const Unit w = decode(u, fetch_item_warp(p.items, u / per_tile));
+      const int row = w.t.row0 + r;              // the token of this lane
+      const bool live = row < w.t.end;
+      // the columns that this row's mask leaves in a tile are [first, last) once the tile's first token is taken off; every row of
+      // the tile keeps those in [all_first, all_last)
+      int first, last, all_first, all_last;
+      if (KEYS) {
+        first = p.causal && row >= w.t.prefix ? row : w.t.start;
+        all_first = p.causal && min(w.t.row0 + kRows, w.t.end) > w.t.prefix ? min(w.t.row0 + kRows, w.t.end) - 1 : w.t.start;
+        last = all_last = w.t.end;
+      } else {
+        first = all_first = w.t.start;
+        last = p.causal ? min(max(row + 1, w.t.prefix), w.t.end) : w.t.end;
+        all_last = p.causal ? min(max(w.t.row0 + 1, w.t.prefix), w.t.end) : w.t.end;
+      }
+      // KEYS: the document's first query sees one key only; else: this row does
+      const bool lonely = KEYS ? w.t.end - w.t.start == 1 || (p.causal && w.t.prefix <= w.t.start + 1) : last - w.t.start == 1;
+      float lse2 = 0.f, delta = 0.f, rest = 0.f;
+      if (!KEYS) {
+        const int64_t at = int64_t(w.head) * p.tokens + row;
+        lse2 = live ? __ldcg(p.lse + at) * kLog2e : 0.f;
+        delta = live ? __ldcg(p.delta + at) : 0.f;
+      }
+      for (int h = w.head; ok && h < w.head + w.heads; ++h) {
         const float slope2 = BIAS ? __ldg(p.slopes + h) * kLog2e : 0.f;
         for (int i = 0; i < w.tiles; ++i, ++turns) {
           const Ring::Slot vs = rv.next();
           const float* vec = reinterpret_cast<const float*>(gen + M::kVec + vs.stage * M::kVecBytes) + col0;
-          const int c0 = w.q0 + i * kRows + int(col0);     // the query of column 0
-          if (!warp_wait(vec_full(vs.stage), vs.phase, abort_flag) || !warp_wait(s_full, turns & 1, abort_flag)) {
+          const int c0 = w.other0 + i * kRows + int(col0);     // the token of column 0
+          if ((KEYS && !warp_wait(vec_full(vs.stage), vs.phase, abort_flag)) || !warp_wait(s_full, turns & 1, abort_flag)) {
             give_up();
             ok = false;
             break;
           }
           ptx::tcgen05_fence_after_sync();
-          uint32_t s[2][32];
-#pragma unroll
-          for (int c = 0; c < 2; ++c) ptx::tmem_ld_x32(tmem_s + lanes + col0 + 32 * c, s[c]);
-          tmem_loaded(s[0], s[1]);
-          const bool masked = c0 < all_from || c0 + kPanel > w.t.end;
-          const int first = from - c0, last = w.t.end - c0;
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
+          uint32_t s[32];
+          ptx::tmem_ld_x32(s_at, s);
+          tmem_loaded(s);
+          const bool masked = c0 < all_first || c0 + kPanel > all_last;
+          const int lo = first - c0, hi = last - c0;
+          // dx/ds of the cap, as fp16: 2^-12 of it is little beside the rounding of dS
+          __half2 slopes[CAP ? 16 : 1];
+          {
             uint32_t pk[16];
 #pragma unroll
             for (int i4 = 0; i4 < 8; ++i4) {
-              const float4 l4 = *reinterpret_cast<const float4*>(vec + 32 * c + 4 * i4);
-              const float l[4] = {l4.x, l4.y, l4.z, l4.w};
-              float e[4];
+              float l[4] = {lse2, lse2, lse2, lse2};
+              if (KEYS) {
+                const float4 v = *reinterpret_cast<const float4*>(vec + 4 * i4);
+                l[0] = v.x; l[1] = v.y; l[2] = v.z; l[3] = v.w;
+              }
+              float e[4], slope[4] = {1.f, 1.f, 1.f, 1.f};
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
                 const int col = 4 * i4 + k;
-                float slope = 1.f, x;
-                if (!CAP && !BIAS) x = fmaf(__uint_as_float(s[c][col]), p.c, -l[k]);
-                else x = exponent<CAP, BIAS>(p, __uint_as_float(s[c][col]), float(c0 - key) + float(32 * c + col), slope2, &slope) - l[k];
+                float x;
+                if (!CAP && !BIAS) x = fmaf(__uint_as_float(s[col]), p.c, -l[k]);
+                else x = exponent<CAP, BIAS>(p, __uint_as_float(s[col]), float(c0 - row) + float(col), slope2, &slope[k]) - l[k];
                 e[k] = exp2_fast(x);
-                if (masked) e[k] = 32 * c + col < first || 32 * c + col >= last ? 0.f : e[k];
-                s[c][col] = __float_as_uint(CAP ? e[k] * slope : e[k]);
+                if (masked) e[k] = col >= lo && col < hi ? e[k] : 0.f;
+                s[col] = __float_as_uint(e[k]);
+                if (CAP && !KEYS) e[k] *= slope[k];   // what an error of delta is multiplied with
+              }
+              if (CAP) {
+                slopes[CAP ? 2 * i4 : 0] = __floats2half2_rn(slope[0], slope[1]);
+                slopes[CAP ? 2 * i4 + 1 : 0] = __floats2half2_rn(slope[2], slope[3]);
               }
               pk[2 * i4] = pack2(e[0], e[1]);
               pk[2 * i4 + 1] = pack2(e[2], e[3]);
             }
-            ptx::tmem_st_x16(tmem_s + lanes + col0 + 16 * c, pk);
+            ptx::tmem_st_x16(s_at, pk);
           }
           ptx::tmem_st_wait();
           ptx::tcgen05_fence_before_sync();
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive(p_full);
           __syncwarp();
-          if (lonely && c0 == w.t.start) s[0][0] = 0u;
+          if (KEYS) {
+            if (lonely && c0 == w.t.start) s[0] = 0u;
+          } else if (lonely) {
+#pragma unroll
+            for (int k = 0; k < 32; ++k) s[k] = 0u;
+          }
           if (!warp_wait(dp_full, turns & 1, abort_flag)) { give_up(); ok = false; break; }
           ptx::tcgen05_fence_after_sync();
+          uint32_t pk[16];
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            uint32_t g[32], pk[16];
-            ptx::tmem_ld_x32(tmem_dp + lanes + col0 + 32 * c, g);
+            uint32_t g[16];
+            ptx::tmem_ld_x16(dp_at + 16 * c, g);
             tmem_loaded(g);
-            if (masked) {   // queries of another document: their dP may be anything
+            if (masked) {   // tokens of another document: their dP may be anything
 #pragma unroll
-              for (int i = 0; i < 32; ++i) g[i] = 32 * c + i < last ? g[i] : 0u;
+              for (int k = 0; k < 16; ++k) g[k] = 16 * c + k >= lo && 16 * c + k < hi ? g[k] : __float_as_uint(delta);
             }
 #pragma unroll
-            for (int i4 = 0; i4 < 8; ++i4) {
-              const float4 d4 = *reinterpret_cast<const float4*>(vec + kRows + 32 * c + 4 * i4);
-              const float dl[4] = {d4.x, d4.y, d4.z, d4.w};
+            for (int i4 = 0; i4 < 4; ++i4) {
+              float dl[4] = {delta, delta, delta, delta};
+              if (KEYS) {
+                const float4 v = *reinterpret_cast<const float4*>(vec + kRows + 16 * c + 4 * i4);
+                dl[0] = v.x; dl[1] = v.y; dl[2] = v.z; dl[3] = v.w;
+              }
               float e[4];
 #pragma unroll
-              for (int k = 0; k < 4; ++k) e[k] = __uint_as_float(s[c][4 * i4 + k]) * (__uint_as_float(g[4 * i4 + k]) - dl[k]);
-              pk[2 * i4] = pack2(e[0], e[1]);
-              pk[2 * i4 + 1] = pack2(e[2], e[3]);
+              for (int k = 0; k < 4; ++k) {
+                e[k] = __uint_as_float(s[16 * c + 4 * i4 + k]) * (__uint_as_float(g[4 * i4 + k]) - dl[k]);
+                if (!KEYS) rest += e[k];
+              }
+              if (CAP) {
+                const float2 f0 = __half22float2(slopes[CAP ? 8 * c + 2 * i4 : 0]), f1 = __half22float2(slopes[CAP ? 8 * c + 2 * i4 + 1 : 0]);
+                e[0] *= f0.x; e[1] *= f0.y; e[2] *= f1.x; e[3] *= f1.y;
+              }
+              pk[8 * c + 2 * i4] = pack2(e[0], e[1]);
+              pk[8 * c + 2 * i4 + 1] = pack2(e[2], e[3]);
             }
-            ptx::tmem_st_x16(tmem_dp + lanes + col0 + 16 * c, pk);
           }
+          ptx::tmem_st_x16(dp_at, pk);
           ptx::tmem_st_wait();
           ptx::tcgen05_fence_before_sync();
           __syncwarp();
           if (lane == 0) {
             ptx::mbar_arrive(ds_full);
-            ptx::mbar_arrive(vec_empty(vs.stage));
+            if (KEYS) ptx::mbar_arrive(vec_empty(vs.stage));
           }
           __syncwarp();
         }
       }
       if (!ok) break;
+      if (!KEYS) {
+        // r of the row: the panels' parts, [0] + [2] and [1] + [3] first (room for two)
+        float* part = reinterpret_cast<float*>(gen + M::kExchange);
+        if (!warp_wait(parts_free, (it & 1) ^ 1u, abort_flag)) { give_up(); break; }   // those of the item before have been read
+        if (panel < 2) part[panel * kRows + r] = rest;
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(parts_full);
+        __syncwarp();
+        if (!warp_wait(parts_full, 0u, abort_flag)) { give_up(); break; }
+        if (panel >= 2) part[(panel - 2) * kRows + r] += rest;
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(parts_full);
+        __syncwarp();
+        if (!warp_wait(parts_full, 1u, abort_flag)) { give_up(); break; }
+        rest = part[r] + part[kRows + r];
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(parts_free);
+        __syncwarp();
+        if (panel == 0 && live) p.delta[int64_t(w.head) * p.tokens + row] = delta + rest;
+        __syncwarp();
+      }
       if (!warp_wait(out_full, it & 1, abort_flag)) { give_up(); break; }
       ptx::tcgen05_fence_after_sync();
-      const bool live = key < w.t.end;
-      // panel 0 stores dV, panel 1 dK
-      const uint32_t from_col = (panel ? tmem_dk : tmem_dv) + lanes;
-      const float f = panel ? p.scale : 1.f;
-      float* part = panel ? p.dk_part : p.dv_part;
-      if (part) part += ((int64_t(w.part) * p.tokens + key) * p.kv_heads + w.kv_head) * p.d;
-      __nv_bfloat16* out = panel ? p.dK + int64_t(key) * p.lddk : p.dV + int64_t(key) * p.lddv;
-      out += int64_t(w.kv_head) * p.d;
+      if (KEYS) {
+        // panels 0 and 1 store dV's halves, 2 and 3 dK's
+        const bool dk = panel >= 2;
+        const int half = (panel & 1) * (HD / 2);
+        const float f = dk ? p.scale : 1.f;
+        float* part = dk ? p.dk_part : p.dv_part;
+        if (part) part += ((int64_t(w.part) * p.tokens + row) * p.kv_heads + w.kv_head) * p.d;
+        __nv_bfloat16* out = (dk ? p.dK + int64_t(row) * p.lddk : p.dV + int64_t(row) * p.lddv) + int64_t(w.kv_head) * p.d;
 #pragma unroll
-      for (int c = 0; c < HD / 32; ++c) {
-        uint32_t o[32];
-        ptx::tmem_ld_x32(from_col + 32 * c, o);
-        tmem_loaded(o);
-        if (c == HD / 32 - 1) {
-          ptx::tcgen05_fence_before_sync();
-          __syncwarp();
-          if (lane == 0) ptx::mbar_arrive(out_free);
+        for (int c = 0; c < HD / 64; ++c) {
+          const int col = half + 32 * c;
+          uint32_t o[32];
+          ptx::tmem_ld_x32((dk ? tmem_second : tmem_first) + lanes + col, o);
+          tmem_loaded(o);
+          if (c == HD / 64 - 1) {
+            ptx::tcgen05_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(out_free);
+            __syncwarp();
+          }
+          if (live && col < p.d) {
+            if (part) store_f32(part + col, o, f, p.d - col);
+            else store_bf16(out + col, o, f, p.d - col);
+          }
           __syncwarp();
         }
-        if (live && 32 * c < p.d) {
-          if (part) store_f32(part + 32 * c, o, f, p.d - 32 * c);
-          else store_bf16(out + 32 * c, o, f, p.d - 32 * c);
-        }
+      } else {
+        // a panel stores a quarter of dQ's columns
+        const int quarter_cols = HD / 4, col = panel * quarter_cols;
+        uint32_t a[quarter_cols], b[quarter_cols];
+        load_columns(tmem_second + lanes + col, a);
+        load_columns(tmem_first + lanes + col, b);
+        ptx::tmem_ld_wait();
+        hand_over(a);
+        hand_over(b);
+        ptx::tcgen05_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(out_free);
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < quarter_cols; ++k) a[k] = __float_as_uint(fmaf(-rest, __uint_as_float(b[k]), __uint_as_float(a[k])));
+        if (live && col < p.d) store_bf16(p.dQ + int64_t(row) * p.lddq + int64_t(w.head) * p.d + col, a, p.scale, p.d - col);
         __syncwarp();
       }
     }
   }
-  zero_rows_outside(p, p.dK, p.lddk, p.kv_heads, nullptr, 0.f);
-  zero_rows_outside(p, p.dV, p.lddv, p.kv_heads, nullptr, 0.f);
+  __syncwarp();
+  if (KEYS) {
+    zero_rows_outside(p, p.dK, p.lddk, p.kv_heads, nullptr, 0.f);
+    zero_rows_outside(p, p.dV, p.lddv, p.kv_heads, nullptr, 0.f);
+  } else {
+    zero_rows_outside(p, p.dQ, p.lddq, p.heads, nullptr, 0.f);
+  }
   __syncwarp();
   ptx::tcgen05_fence_before_sync();
   __syncthreads();
@@ -741,8 +585,8 @@ cudaError_t launch(DeviceOnce& once, K kernel, int smem, const Maps& m, const Pa
 template <int HD, bool CAP, bool BIAS>
 cudaError_t launch_both(const Maps& m, const Params& pq, unsigned grid_q, const Params& pk, unsigned grid_k, cudaStream_t st) {
   static DeviceOnce once_q, once_k;
-  const cudaError_t e = launch(once_q, attn_dq_kernel<HD, CAP, BIAS>, QuerySmem<HD>::kBytes, m, pq, grid_q, st);
-  return e != cudaSuccess ? e : launch(once_k, attn_dkv_kernel<HD, CAP, BIAS>, KeySmem<HD>::kBytes, m, pk, grid_k, st);
+  const cudaError_t e = launch(once_q, attn_bwd_kernel<HD, false, CAP, BIAS>, Smem<HD, false>::kBytes, m, pq, grid_q, st);
+  return e != cudaSuccess ? e : launch(once_k, attn_bwd_kernel<HD, true, CAP, BIAS>, Smem<HD, true>::kBytes, m, pk, grid_k, st);
 }
 template <int HD>
 cudaError_t launch_both(bool cap, bool bias, const Maps& m, const Params& pq, unsigned grid_q, const Params& pk, unsigned grid_k, cudaStream_t st) {

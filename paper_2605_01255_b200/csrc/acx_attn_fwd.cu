@@ -162,7 +162,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
   auto o_free = [&](int h) { return misc + 72 + 8u * h; };
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + FwdSmem<HD>::kBars + 16 * kStages + 88);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + FwdSmem<HD>::kBars + 16 * kStages + 92);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  volatile int* no_abort = abort_flag + 1;   // for the one wait that has to run its time even so
+  const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // the warp's number, known to be the same in all lanes
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -172,6 +173,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
     ptx::mbar_init(q_full, 1);
     ptx::mbar_init(q_empty, 1);
     ptx::mbar_init(done, 1);
+    *no_abort = 0;
     for (int h = 0; h < 2; ++h) {
       ptx::mbar_init(s_full(h), 1);
       ptx::mbar_init(p_full(h), 4);
@@ -181,9 +183,12 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
     *abort_flag = 0;
     ptx::fence_barrier_init();   // no prefetch of the tensor maps: a block without work would leave with it in flight
   }
+  // A warp comes to the barrier as a whole: halves of it would count as two, and let the others read the address before it is there
+  __syncwarp();
   if (warp == 1) {
     ptx::tmem_alloc(misc + 88, 512);
     ptx::tmem_relinquish_alloc_permit();
+    __syncwarp();
   }
   ptx::tcgen05_fence_before_sync();
   __syncthreads();
@@ -197,10 +202,6 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
   auto give_up = [&]() {
     *abort_flag = 1;
     atomicExch(p.status, kDevTimeout);
-  };
-  auto fetch = [&](int u) {
-    const int4 v = __ldcg(reinterpret_cast<const int4*>(p.items) + u / p.heads);
-    return Item{v.x, v.y, v.z, v.w};
   };
   // key tiles that a half of the queries sees
   auto key_tiles = [&](const Item& t, int half) {
@@ -223,7 +224,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
         if (++stage == kStages) { stage = 0; phase ^= 1u; }
       };
       for (int u = blockIdx.x; ok && u < units; u += gridDim.x, ++it) {
-        const Item t = fetch(u);
+        const Item t = fetch_item(p.items, u / p.heads);
         const int h = u % p.heads, g = h / p.group;
         const int n1 = key_tiles(t, 1), n = max(key_tiles(t, 0), n1);
         if (!ptx::mbar_wait(q_empty, (it & 1) ^ 1u, abort_flag)) { give_up(); ok = false; break; }
@@ -249,74 +250,71 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
     __syncwarp();
   } else if (warp == 1) {
     // ---------------------------------------------------------------------------------------------------- products
-    if (lane == 0) {
-      int stage = 0, it = 0, turns[2] = {0, 0}, outs[2] = {0, 0};
-      uint32_t phase = 0;
-      bool ok = true;
-      const int d16 = (p.d + 15) / 16;
-      auto wait = [&](uint32_t bar, uint32_t parity) {
-        if (ok && !ptx::mbar_wait(bar, parity, abort_flag)) { give_up(); ok = false; }
-        return ok;
+    int stage = 0, it = 0, turns[2] = {0, 0}, outs[2] = {0, 0};
+    uint32_t phase = 0;
+    bool ok = true;
+    const int d16 = (p.d + 15) / 16;
+    auto wait = [&](uint32_t bar, uint32_t parity) {
+      if (ok && !warp_wait(bar, parity, abort_flag)) { give_up(); ok = false; }
+      return ok;
+    };
+    struct Slot { int stage; uint32_t phase; };
+    auto next = [&]() {
+      const Slot s{stage, phase};
+      if (++stage == kStages) { stage = 0; phase ^= 1u; }
+      return s;
+    };
+    auto addr = [&](Slot s) { return base + FwdSmem<HD>::kQ + s.stage * T::kBytes; };
+    for (int u = blockIdx.x; ok && u < units; u += gridDim.x, ++it) {
+      const Item t = fetch_item_warp(p.items, u / p.heads);
+      const int nt[2] = {key_tiles(t, 0), key_tiles(t, 1)}, n = max(nt[0], nt[1]);
+      auto scores = [&](int h, Slot k) {
+        scores_mma<HD>(tmem_s(h), base + h * T::kBytes, addr(k), d16);
+        ptx::umma_commit_elected(s_full(h));
       };
-      struct Slot { int stage; uint32_t phase; };
-      auto next = [&]() {
-        const Slot s{stage, phase};
-        if (++stage == kStages) { stage = 0; phase ^= 1u; }
-        return s;
-      };
-      auto addr = [&](Slot s) { return base + FwdSmem<HD>::kQ + s.stage * T::kBytes; };
-      for (int u = blockIdx.x; ok && u < units; u += gridDim.x, ++it) {
-        const Item t = fetch(u);
-        const int nt[2] = {key_tiles(t, 0), key_tiles(t, 1)}, n = max(nt[0], nt[1]);
-        auto scores = [&](int h, Slot k) {
-          scores_mma<HD>(tmem_s(h), base + h * T::kBytes, addr(k), d16);
-          ptx::umma_commit(s_full(h));
-        };
-        wait(q_full, it & 1);
-        Slot k = next(), v;
-        if (!wait(full(k.stage), k.phase)) break;
-        ptx::tcgen05_fence_after_sync();
+      wait(q_full, it & 1);
+      Slot k = next(), v;
+      if (!wait(full(k.stage), k.phase)) break;
+      ptx::tcgen05_fence_after_sync();
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-          if (nt[h] == n) scores(h, k);
-        ptx::umma_commit(empty(k.stage));
-        if (n == 1) ptx::umma_commit(q_empty);
-        for (int j = n - 1; ok && j >= 0; --j) {
-          v = next();
-          if (!wait(full(v.stage), v.phase)) break;
-          const int left = t.end - (t.start + j * kRows);   // keys of this tile inside the document
-          const int steps = min(kRows, left + 15) / 16;
-          if (left < 16 * steps) T::zero_rows(gen + (addr(v) - base), left, 16 * steps);
-          if (j > 0) {
-            k = next();
-            if (!wait(full(k.stage), k.phase)) break;
-          }
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            if (j < nt[h]) {
-              if (j == nt[h] - 1 && !wait(o_free(h), (outs[h] & 1) ^ 1u)) break;
-              if (!wait(p_full(h), turns[h] & 1)) break;
-              ++turns[h];
-              ptx::tcgen05_fence_after_sync();
-              rows_mma<HD>(tmem_o(h), tmem_s(h), tmem_s(h) + 32, addr(v), steps, d16, j < nt[h] - 1);
-              if (j == 0) {
-                ptx::umma_commit(o_full(h));
-                ++outs[h];
-              }
-            }
-            if (j > 0 && j <= nt[h]) scores(h, k);
-          }
-          ptx::umma_commit(empty(v.stage));
-          if (j > 0) ptx::umma_commit(empty(k.stage));
-          if (j == 1) ptx::umma_commit(q_empty);
+      for (int h = 0; h < 2; ++h)
+        if (nt[h] == n) scores(h, k);
+      ptx::umma_commit_elected(empty(k.stage));
+      if (n == 1) ptx::umma_commit_elected(q_empty);
+      for (int j = n - 1; ok && j >= 0; --j) {
+        v = next();
+        if (!wait(full(v.stage), v.phase)) break;
+        const int left = t.end - (t.start + j * kRows);   // keys of this tile inside the document
+        const int steps = min(kRows, left + 15) / 16;
+        if (left < 16 * steps) T::zero_rows(gen + (addr(v) - base), left, 16 * steps);
+        if (j > 0) {
+          k = next();
+          if (!wait(full(k.stage), k.phase)) break;
         }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (j < nt[h]) {
+            if (j == nt[h] - 1 && !wait(o_free(h), (outs[h] & 1) ^ 1u)) break;
+            if (!wait(p_full(h), turns[h] & 1)) break;
+            ++turns[h];
+            ptx::tcgen05_fence_after_sync();
+            rows_mma<HD, 0>(tmem_o(h), tmem_s(h), addr(v), steps, d16, j < nt[h] - 1);
+            if (j == 0) {
+              ptx::umma_commit_elected(o_full(h));
+              ++outs[h];
+            }
+          }
+          if (j > 0 && j <= nt[h]) scores(h, k);
+        }
+        ptx::umma_commit_elected(empty(v.stage));
+        if (j > 0) ptx::umma_commit_elected(empty(k.stage));
+        if (j == 1) ptx::umma_commit_elected(q_empty);
       }
-      // everything that was issued has to be done before the tensor memory is given back
-      if (it > 0 || !ok) {
-        ptx::umma_commit(done);
-        const uint64_t t0 = ptx::globaltimer_ns();
-        while (!ptx::mbar_try_wait(done, 0) && ptx::globaltimer_ns() - t0 < ptx::kWaitLimitNs) {}
-      }
+    }
+    // everything that was issued has to be done before the tensor memory is given back
+    if (it > 0 || !ok) {
+      ptx::umma_commit_elected(done);
+      warp_wait(done, 0, no_abort);
     }
     __syncwarp();
   } else if (warp >= 4) {
@@ -327,7 +325,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
     int turns = 0, outs = 0;
     bool ok = true;
     for (int u = blockIdx.x; ok && u < units; u += gridDim.x) {
-      const Item t = fetch(u);
+      const Item t = fetch_item_warp(p.items, u / p.heads);
       const int n = key_tiles(t, half), head = u % p.heads;
       if (n == 0) continue;
       const int r0 = t.row0 + kRows * half, row = r0 + 32 * quarter + lane;

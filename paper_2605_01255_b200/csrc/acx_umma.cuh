@@ -205,13 +205,70 @@ __device__ __forceinline__ void umma_bf16(uint32_t tmem_d, uint64_t desc_a, uint
       ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(uint32_t(accumulate))
       : "memory");
 }
-// The same with A in tensor memory: lane = row, each 32-bit column two consecutive bf16 along K.
-__device__ __forceinline__ void umma_bf16_tmem_a(uint32_t tmem_d, uint32_t tmem_a, uint64_t desc_b, uint32_t idesc, bool accumulate) {
+// Several steps of a product from one block of instructions, executed by a whole warp of which one elected thread issues.  The operands
+// of a product of 128 x 128 x 16 (64 cycles) have to be there before it: with a thread issuing alone, each instruction's descriptors
+// went from its registers to the warp's uniform ones (150 to 180 cycles an instruction, and the attention kernels were bound by it);
+// here all lanes hold the same values, and a step is two additions.
+//   lo, hi: halves of make_smem_desc's value.  A and B advance by two units of 16 bytes per step (K-major, inside 64 columns).
+template <int STEPS>
+__device__ __forceinline__ void umma_steps(uint32_t tmem_d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, bool accumulate) {
+  static_assert(STEPS == 1 || STEPS == 4, "a step or four");
+  if (STEPS == 1)
+    asm volatile(
+        "{\n\t.reg .pred lead, acc;\n\t.reg .b64 a, b;\n\t"
+        "elect.sync _|lead, 0xFFFFFFFF;\n\tsetp.ne.b32 acc, %5, 0;\n\t"
+        "mov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\t"
+        "@lead tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, acc;\n\t}"
+        ::"r"(tmem_d), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(uint32_t(accumulate))
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred lead, acc;\n\t.reg .b64 a, b;\n\t.reg .b32 al, bl;\n\t"
+        "elect.sync _|lead, 0xFFFFFFFF;\n\tsetp.ne.b32 acc, %5, 0;\n\t"
+        "mov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\t"
+        "@lead tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, acc;\n\t"
+        "setp.eq.u32 acc, 0, 0;\n\t"
+        "add.u32 al, %1, 2;\n\tadd.u32 bl, %2, 2;\n\tmov.b64 a, {al, %3};\n\tmov.b64 b, {bl, %3};\n\t"
+        "@lead tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, acc;\n\t"
+        "add.u32 al, %1, 4;\n\tadd.u32 bl, %2, 4;\n\tmov.b64 a, {al, %3};\n\tmov.b64 b, {bl, %3};\n\t"
+        "@lead tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, acc;\n\t"
+        "add.u32 al, %1, 6;\n\tadd.u32 bl, %2, 6;\n\tmov.b64 a, {al, %3};\n\tmov.b64 b, {bl, %3};\n\t"
+        "@lead tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, acc;\n\t}"
+        ::"r"(tmem_d), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(uint32_t(accumulate))
+        : "memory");
+}
+// The same with A in tensor memory (lane = row, each 32-bit column two consecutive bf16 along K), eight columns per step, A's third step GAP columns behind the second; B (MN-major, 128 bytes wide
+// rows) advances by 16 rows.
+template <int STEPS, int GAP>
+__device__ __forceinline__ void umma_steps_tmem_a(uint32_t tmem_d, uint32_t tmem_a, uint32_t b_lo, uint32_t hi, uint32_t idesc, bool accumulate) {
+  static_assert(STEPS == 1 || STEPS == 4, "a step or four");
+  if (STEPS == 1)
+    asm volatile(
+        "{\n\t.reg .pred lead, acc;\n\t.reg .b64 b;\n\t"
+        "elect.sync _|lead, 0xFFFFFFFF;\n\tsetp.ne.b32 acc, %5, 0;\n\tmov.b64 b, {%2, %3};\n\t"
+        "@lead tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, acc;\n\t}"
+        ::"r"(tmem_d), "r"(tmem_a), "r"(b_lo), "r"(hi), "r"(idesc), "r"(uint32_t(accumulate))
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred lead, acc;\n\t.reg .b64 b;\n\t.reg .b32 at, bl;\n\t"
+        "elect.sync _|lead, 0xFFFFFFFF;\n\tsetp.ne.b32 acc, %5, 0;\n\tmov.b64 b, {%2, %3};\n\t"
+        "@lead tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, acc;\n\t"
+        "setp.eq.u32 acc, 0, 0;\n\t"
+        "add.u32 at, %1, 8;\n\tadd.u32 bl, %2, 128;\n\tmov.b64 b, {bl, %3};\n\t"
+        "@lead tcgen05.mma.cta_group::1.kind::f16 [%0], [at], b, %4, acc;\n\t"
+        "add.u32 at, %1, %6;\n\tadd.u32 bl, %2, 256;\n\tmov.b64 b, {bl, %3};\n\t"
+        "@lead tcgen05.mma.cta_group::1.kind::f16 [%0], [at], b, %4, acc;\n\t"
+        "add.u32 at, %1, %7;\n\tadd.u32 bl, %2, 384;\n\tmov.b64 b, {bl, %3};\n\t"
+        "@lead tcgen05.mma.cta_group::1.kind::f16 [%0], [at], b, %4, acc;\n\t}"
+        ::"r"(tmem_d), "r"(tmem_a), "r"(b_lo), "r"(hi), "r"(idesc), "r"(uint32_t(accumulate)), "n"(8 + GAP), "n"(16 + GAP)
+        : "memory");
+}
+// umma_commit by the thread that the calls above elect.
+__device__ __forceinline__ void umma_commit_elected(uint32_t bar) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-      ::"r"(tmem_d), "r"(tmem_a), "l"(desc_b), "r"(idesc), "r"(uint32_t(accumulate))
+      "{\n\t.reg .pred lead;\n\telect.sync _|lead, 0xFFFFFFFF;\n\t"
+      "@lead tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar)
       : "memory");
 }
 // The mbarrier gets one arrival once every previously issued MMA of this thread has completed.
