@@ -92,21 +92,24 @@ __device__ __forceinline__ float rcp_fast(float x) {
   return y;
 }
 
-// tanh: 1 - 2 / (1 + e^2u) keeps about 2^-23 absolutely, which is too little near zero once a large cap multiplies it; there
-// the odd series (its first left-out term is below 2^-25 of the value at the border).
+// tanh.  1 - 2 / (1 + e^2u) keeps about 2^-23 absolutely, which is too little near zero once a large cap multiplies it; up to 0.75
+// an odd polynomial, fitted to tanh(u) / u (relative error 1.4e-9 before rounding), takes over.  SMALL: all arguments are below that.
+template <bool SMALL>
 __device__ __forceinline__ float tanh_of(float u) {
-  const float r = 1.f - 2.f * rcp_fast(1.f + exp2_fast(u * (2.f * kLog2e)));
   const float q = u * u;
-  const float t = fmaf(q, fmaf(q, fmaf(q, fmaf(q, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
-  return fabsf(u) < 0.2f ? u * t : r;
+  float t = fmaf(q, fmaf(q, fmaf(q, fmaf(q, fmaf(q, 1.7277066e-3f, -7.6394570e-3f), 2.1438753e-2f), -5.3887937e-2f), 0.13332610f), -0.33333308f);
+  t = fmaf(u * q, t, u);
+  if (SMALL) return t;
+  const float r = 1.f - 2.f * rcp_fast(1.f + exp2_fast(u * (2.f * kLog2e)));
+  return fabsf(u) < 0.75f ? t : r;
 }
 
 // x of a raw score s; `far` = query position - key position.  For CAP, *slope = d x / d s in units of c.
-template <bool CAP, bool BIAS>
+template <bool CAP, bool BIAS, bool SMALL>
 __device__ __forceinline__ float exponent(const Params& p, float s, float far, float slope2, float* slope = nullptr) {
   float x;
   if (CAP) {
-    const float t = tanh_of(s * p.cap_in);
+    const float t = tanh_of<SMALL>(s * p.cap_in);
     x = t * p.cap_out;
     if (slope) *slope = fmaf(-t, t, 1.f);
   } else {
@@ -114,6 +117,14 @@ __device__ __forceinline__ float exponent(const Params& p, float s, float far, f
   }
   if (BIAS) x = fmaf(-slope2, fabsf(far), x);
   return x;
+}
+// Whether the tanh's polynomial alone does for a warp's scores.
+template <int N>
+__device__ __forceinline__ bool small_scores(const Params& p, const uint32_t (&s)[N]) {
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) top = fmaxf(top, fabsf(__uint_as_float(s[i])));
+  return __all_sync(0xFFFFFFFFu, top * p.cap_in < 0.75f);
 }
 
 // A wait of a whole warp, which it leaves together: what follows (tensor memory loads and stores) has to be executed by converged
@@ -138,6 +149,14 @@ template <typename... V>
 __device__ __forceinline__ void tmem_loaded(V&... v) {
   ptx::tmem_ld_wait();
   (hand_over(v), ...);
+}
+
+// The unit of work that this block takes in round `it`: the longest come first, and rounds go through the blocks there and back
+// again, so that no block gets the longer ones of every round (the keys' launch of 8192 x 24 x 8 x 128: a block's tiles at most 432 of 337
+// on average without, 354 with it).
+__device__ __forceinline__ int unit_of(int it) {
+  const int g = int(gridDim.x), b = int(blockIdx.x);
+  return it * g + ((it & 1) ? g - 1 - b : b);
 }
 
 __device__ __forceinline__ Item fetch_item(const Item* items, int k) {
@@ -238,10 +257,10 @@ __device__ __forceinline__ void scores_mma(uint32_t tmem_d, uint32_t a, uint32_t
     const uint32_t al = uint32_t(da) + c * (Tile<HD>::kChunkBytes >> 4), bl = uint32_t(db) + c * (Tile<HD>::kChunkBytes >> 4);
     const int steps = d16 - 4 * c;
     if (steps >= 4) {
-      ptx::umma_steps<4>(tmem_d, al, bl, hi, idesc, c > 0);
+      ptx::umma_steps<4, 2>(tmem_d, al, bl, hi, idesc, c > 0);
     } else {
 #pragma unroll 1
-      for (int k = 0; k < steps; ++k) ptx::umma_steps<1>(tmem_d, al + 2 * k, bl + 2 * k, hi, idesc, c > 0 || k > 0);
+      for (int k = 0; k < steps; ++k) ptx::umma_steps<1, 0>(tmem_d, al + 2 * k, bl + 2 * k, hi, idesc, c > 0 || k > 0);
     }
   }
 }
@@ -261,6 +280,23 @@ __device__ __forceinline__ void rows_mma(uint32_t tmem_d, uint32_t tmem_a, uint3
 #pragma unroll 1
       for (int k = 0; k < steps - 4 * c; ++k)
         ptx::umma_steps_tmem_a<1, 0>(tmem_d, at + 8 * k + (k >= 2 ? GAP : 0), bl + 128 * k, hi, idesc, add || c > 0 || k > 0);
+    }
+  }
+}
+
+// The same with A in shared memory: two K-major chunks of 64 columns.
+template <int HD>
+__device__ __forceinline__ void smem_rows_mma(uint32_t tmem_d, uint32_t a, uint32_t b, int steps, int d16, bool add) {
+  const uint32_t idesc = ptx::make_idesc_bf16(kRows, 16 * d16, false, true);
+  const uint64_t da = ptx::make_smem_desc(a, 16, 1024), db = ptx::make_smem_desc(b, Tile<HD>::kChunkBytes, 1024);
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const uint32_t al = uint32_t(da) + c * (kRows * 128 >> 4), bl = uint32_t(db) + c * 512;
+    if (steps >= 4 * c + 4) {
+      ptx::umma_steps<4, 128>(tmem_d, al, bl, uint32_t(da >> 32), idesc, add || c > 0);
+    } else {
+#pragma unroll 1
+      for (int k = 0; k < steps - 4 * c; ++k) ptx::umma_steps<1, 0>(tmem_d, al + 2 * k, bl + 128 * k, uint32_t(da >> 32), idesc, add || c > 0 || k > 0);
     }
   }
 }

@@ -13,9 +13,9 @@
 // p (dP - delta) summed in fp32 beside it, and dQ = scale (second - r first); delta + r is what the launch for the keys uses.
 // The price of two launches is that S and dP are computed twice: eight products instead of five.
 //
-// S, dP, first and second fill the tensor memory (4 x 128 columns).  While the exponentials of a tile are taken the tensor core runs
-// `second` of the tile before and dP, while dS is formed `first` and the next S.  Sixteen warps share a tile, 32 rows x 32 columns
-// each: eight with 64 columns were bound by the latencies of their dependent steps (dK, dV of 8192 x 24 x 8 x 128 1104 us).
+// S, dP, first and second fill the tensor memory (4 x 128 columns); dS goes over dP as bf16 and is multiplied from there, P goes to shared
+// memory, so that the next S can be taken as soon as this one has been read: the rows' warps never wait for it (with P over S they
+// waited 1600 of 3900 cycles a tile).  Sixteen warps share a tile, 32 rows x 32 columns each.
 //
 // A query that sees one key only has p = 1 and no gradient through its scores: exactly zero, not the difference of two roundings.
 //
@@ -83,12 +83,15 @@ __device__ __forceinline__ void load_columns(uint32_t at, uint32_t (&v)[16]) { p
 // KEYS: rows are keys
 template <int HD, bool KEYS>
 struct Smem {
-  static constexpr int kT0 = KEYS ? 2 : 3, kT1 = 2;                    // stages
-  static constexpr int kVec = (2 + kT0 + kT1) * Tile<HD>::kBytes;
-  static constexpr int kVecStages = KEYS ? 4 : 0, kVecBytes = 2 * kRows * 4;   // KEYS: lse and delta of a tile of queries
+  // Stages.  T0 is read by S, a tile ahead, and by `second` at the end (and by `first` for queries); T1 by dP alone for queries, and by
+  // `first` for keys.  At d = 128 six tiles fit beside P.
+  static constexpr int kT0 = KEYS && HD == 128 ? 2 : 3, kT1 = !KEYS && HD == 128 ? 1 : 2;
+  static constexpr int kP = (2 + kT0 + kT1) * Tile<HD>::kBytes, kPBytes = kRows * kRows * 2;
+  static constexpr int kVec = kP + kPBytes;
+  static constexpr int kVecStages = KEYS ? 2 : 0, kVecBytes = 2 * kRows * 4;   // KEYS: lse and delta of a tile of queries
   static constexpr int kPartBytes = kPanels / 2 * kRows * 4;
   static constexpr int kExchange = kVec + kVecStages * kVecBytes;              // else: partial sums of the rows
-  static constexpr int kBars = kExchange + (KEYS ? 0 : kPartBytes), kBytes = kBars + 256 + 1024;
+  static constexpr int kBars = kExchange + (KEYS ? 0 : kPartBytes), kBytes = kBars + 256;
   static_assert(kBytes <= 232448, "shared memory of one CTA");
 };
 
@@ -106,23 +109,29 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const __grid_constant__ CUtensorMap map_do, const Params p) {
   using T = Tile<HD>;
   using M = Smem<HD, KEYS>;
-  extern __shared__ uint8_t smem_raw[];
-  const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;   // tiles start on their swizzle's boundary
-  uint8_t* gen = smem_raw + (base - ptx::smem_u32(smem_raw));
-  const uint32_t r0_tile = base, r1_tile = base + T::kBytes, t0_tiles = base + 2 * T::kBytes, t1_tiles = t0_tiles + M::kT0 * T::kBytes;
+  extern __shared__ __align__(1024) uint8_t gen[];   // tiles start on their swizzle's boundary
+  const uint32_t base = ptx::smem_u32(gen);
+  const uint32_t r0_tile = base, r1_tile = base + T::kBytes, t0_tiles = base + 2 * T::kBytes, t1_tiles = t0_tiles + M::kT0 * T::kBytes,
+                 p_tile = base + M::kP;
   const uint32_t bars = base + M::kBars;
   auto t0_full = [&](int s) { return bars + 8u * s; };
   auto t0_empty = [&](int s) { return bars + 24 + 8u * s; };
   auto t1_full = [&](int s) { return bars + 48 + 8u * s; };
   auto t1_empty = [&](int s) { return bars + 64 + 8u * s; };
   auto vec_full = [&](int s) { return bars + 80 + 8u * s; };
-  auto vec_empty = [&](int s) { return bars + 112 + 8u * s; };
-  const uint32_t r_full = bars + 144, r_empty = bars + 152, s_full = bars + 160, p_full = bars + 168, dp_full = bars + 176, ds_full = bars + 184,
-                 out_full = bars + 192, out_free = bars + 200, done = bars + 208, parts_full = bars + 216, parts_free = bars + 224;
-  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + M::kBars + 232);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + M::kBars + 236);
+  auto vec_empty = [&](int s) { return bars + 96 + 8u * s; };
+  const uint32_t r_full = bars + 112, r_empty = bars + 120, s_full = bars + 128, s_free = bars + 136, p_full = bars + 144, p_free = bars + 152,
+                 dp_full = bars + 160, ds_full = bars + 168, out_full = bars + 176, out_free = bars + 184, parts_full = bars + 192,
+                 parts_free = bars + 200, done = bars + 208;
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + M::kBars + 216);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + M::kBars + 220);
   volatile int* no_abort = abort_flag + 1;   // for the one wait that has to run its time even so
   const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // the warp's number, known to be the same in all lanes
+
+  if (base & 1023u) {   // not a place for tiles: nothing is done, and said so
+    if (threadIdx.x == 0) atomicExch(p.status, kDevTimeout);
+    return;
+  }
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < M::kT0; ++s) {
@@ -140,7 +149,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     ptx::mbar_init(r_full, 1);
     ptx::mbar_init(r_empty, 1);
     ptx::mbar_init(s_full, 1);
+    ptx::mbar_init(s_free, kRowWarps);
     ptx::mbar_init(p_full, kRowWarps);
+    ptx::mbar_init(p_free, 1);
     ptx::mbar_init(dp_full, 1);
     ptx::mbar_init(ds_full, kRowWarps);
     ptx::mbar_init(out_full, 1);
@@ -155,7 +166,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   // A warp comes to the barrier as a whole: halves of it would count as two, and let the others read the address before it is there
   __syncwarp();
   if (warp == 1) {
-    ptx::tmem_alloc(bars + 232, 512);
+    ptx::tmem_alloc(bars + 216, 512);
     ptx::tmem_relinquish_alloc_permit();
     __syncwarp();
   }
@@ -206,7 +217,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         ptx::mbar_arrive_expect_tx(full + 8u * s.stage, T::kBytes);
         T::load(tiles + s.stage * T::kBytes, map, full + 8u * s.stage, head, row);
       };
-      for (int u = blockIdx.x; ok && u < units; u += gridDim.x, ++it) {
+      for (int u; ok && (u = unit_of(it)) < units; ++it) {
         const Unit w = decode(u, fetch_item(p.items, u / per_tile));
         if (!ptx::mbar_wait(r_empty, (it & 1) ^ 1u, abort_flag)) { give_up(); ok = false; break; }
         ptx::mbar_arrive_expect_tx(r_full, 2 * T::kBytes);
@@ -235,7 +246,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (ok && !warp_wait(bar, parity, abort_flag)) { give_up(); ok = false; }
       return ok;
     };
-    for (int u = blockIdx.x; ok && u < units; u += gridDim.x, ++it) {
+    for (int u; ok && (u = unit_of(it)) < units; ++it) {
       const Unit w = decode(u, fetch_item_warp(p.items, u / per_tile));
       const int n = w.heads * w.tiles;
       auto left_of = [&](int i) { return w.t.end - (w.other0 + (i % w.tiles) * kRows); };   // tokens from this tile's start to the end
@@ -266,16 +277,19 @@ __global__ void __launch_bounds__(kThreads, 1)
       dprobs(b, n == 1);
       for (int i = 0; ok && i < n; ++i, ++turns) {
         const int steps = min(kRows, left_of(i) + 15) / 16;
+        if (i + 1 < n) {   // the next scores as soon as these have been read
+          a_next = r0.next();
+          if (!ready(t0_full(0), a_next, t0_tiles, i + 1, true)) break;
+          if (!wait(s_free, turns & 1)) break;
+          ptx::tcgen05_fence_after_sync();
+          scores(a_next);
+        }
         if (i == 0 && !wait(out_free, (it & 1) ^ 1u)) break;
         if (!wait(p_full, turns & 1)) break;
         ptx::tcgen05_fence_after_sync();
-        rows_mma<HD, 16>(tmem_first, tmem_s, KEYS ? t1_tiles + b.stage * T::kBytes : t0_tiles + a.stage * T::kBytes, steps, d16, i > 0);
+        smem_rows_mma<HD>(tmem_first, p_tile, KEYS ? t1_tiles + b.stage * T::kBytes : t0_tiles + a.stage * T::kBytes, steps, d16, i > 0);
+        ptx::umma_commit_elected(p_free);
         if (KEYS) ptx::umma_commit_elected(t1_empty(b.stage));
-        if (i + 1 < n) {
-          a_next = r0.next();
-          if (!ready(t0_full(0), a_next, t0_tiles, i + 1, true)) break;
-          scores(a_next);
-        }
         if (!wait(ds_full, turns & 1)) break;
         ptx::tcgen05_fence_after_sync();
         rows_mma<HD, 16>(tmem_second, tmem_dp, t0_tiles + a.stage * T::kBytes, steps, d16, i > 0);
@@ -285,6 +299,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           b_next = r1.next();
           if (!ready(t1_full(0), b_next, t1_tiles, i + 1, KEYS)) break;
           dprobs(b_next, i + 2 == n);
+        } else if (!wait(s_free, turns & 1)) {   // (no scores follow in this item: the phase is taken all the same)
+          break;
         }
         a = a_next;
         b = b_next;
@@ -300,7 +316,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (KEYS) {
       Ring rv(M::kVecStages);
       bool ok = true;
-      for (int u = blockIdx.x; ok && u < units; u += gridDim.x) {
+      int it = 0;
+      for (int u; ok && (u = unit_of(it)) < units; ++it) {
         const Unit w = decode(u, fetch_item_warp(p.items, u / per_tile));
         for (int h = w.head; ok && h < w.head + w.heads; ++h)
           for (int i = 0; ok && i < w.tiles; ++i) {
@@ -331,10 +348,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int panel = (warp - kRowWarp0) >> 2, quarter = warp & 3, r = 32 * quarter + lane;
     const uint32_t lanes = uint32_t(32 * quarter) << 16, col0 = kPanel * panel;
     const uint32_t s_at = tmem_s + lanes + col0, dp_at = tmem_dp + lanes + col0;
+    uint8_t* const p_row = gen + M::kP + (panel >> 1) * (kRows * 128) + r * 128;
     int turns = 0, it = 0;
     Ring rv(KEYS ? M::kVecStages : 1);
     bool ok = true;
-    for (int u = blockIdx.x; ok && u < units; u += gridDim.x, ++it) {
+    for (int u; ok && (u = unit_of(it)) < units; ++it) {
       const Unit w = decode(u, fetch_item_warp(p.items, u / per_tile));
       const int row = w.t.row0 + r;              // the token of this lane
       const bool live = row < w.t.end;
@@ -352,7 +370,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       // KEYS: the document's first query sees one key only; else: this row does
       const bool lonely = KEYS ? w.t.end - w.t.start == 1 || (p.causal && w.t.prefix <= w.t.start + 1) : last - w.t.start == 1;
-      float lse2 = 0.f, delta = 0.f, rest = 0.f;
+      float lse2 = 0.f, delta = 0.f;
+      float2 rest2 = make_float2(0.f, 0.f);
       if (!KEYS) {
         const int64_t at = int64_t(w.head) * p.tokens + row;
         lse2 = live ? __ldcg(p.lse + at) * kLog2e : 0.f;
@@ -373,12 +392,17 @@ __global__ void __launch_bounds__(kThreads, 1)
           uint32_t s[32];
           ptx::tmem_ld_x32(s_at, s);
           tmem_loaded(s);
+          ptx::tcgen05_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(s_free);
+          __syncwarp();
           const bool masked = c0 < all_first || c0 + kPanel > all_last;
           const int lo = first - c0, hi = last - c0;
           // dx/ds of the cap, as fp16: 2^-12 of it is little beside the rounding of dS
           __half2 slopes[CAP ? 16 : 1];
-          {
-            uint32_t pk[16];
+          uint32_t pk[16];
+          auto probabilities = [&](auto with_mask, auto is_small) {
+            constexpr bool kMask = decltype(with_mask)::value, kSmall = decltype(is_small)::value;
 #pragma unroll
             for (int i4 = 0; i4 < 8; ++i4) {
               float l[4] = {lse2, lse2, lse2, lse2};
@@ -387,14 +411,17 @@ __global__ void __launch_bounds__(kThreads, 1)
                 l[0] = v.x; l[1] = v.y; l[2] = v.z; l[3] = v.w;
               }
               float e[4], slope[4] = {1.f, 1.f, 1.f, 1.f};
+              auto score = [&](int k) { return make_float2(__uint_as_float(s[4 * i4 + k]), __uint_as_float(s[4 * i4 + k + 1])); };
+              const float2 x01 = q8::fma2(score(0), q8::both(p.c), make_float2(-l[0], -l[1])),
+                           x23 = q8::fma2(score(2), q8::both(p.c), make_float2(-l[2], -l[3]));
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
                 const int col = 4 * i4 + k;
                 float x;
-                if (!CAP && !BIAS) x = fmaf(__uint_as_float(s[col]), p.c, -l[k]);
-                else x = exponent<CAP, BIAS>(p, __uint_as_float(s[col]), float(c0 - row) + float(col), slope2, &slope[k]) - l[k];
+                if (!CAP && !BIAS) x = k & 1 ? (k == 1 ? x01.y : x23.y) : (k == 0 ? x01.x : x23.x);
+                else x = exponent<CAP, BIAS, kSmall>(p, __uint_as_float(s[col]), float(c0 - row) + float(col), slope2, &slope[k]) - l[k];
                 e[k] = exp2_fast(x);
-                if (masked) e[k] = col >= lo && col < hi ? e[k] : 0.f;
+                if (kMask) e[k] = col >= lo && col < hi ? e[k] : 0.f;
                 s[col] = __float_as_uint(e[k]);
                 if (CAP && !KEYS) e[k] *= slope[k];   // what an error of delta is multiplied with
               }
@@ -405,51 +432,51 @@ __global__ void __launch_bounds__(kThreads, 1)
               pk[2 * i4] = pack2(e[0], e[1]);
               pk[2 * i4 + 1] = pack2(e[2], e[3]);
             }
-            ptx::tmem_st_x16(s_at, pk);
-          }
-          ptx::tmem_st_wait();
-          ptx::tcgen05_fence_before_sync();
+            if (kMask && KEYS && lonely && c0 == w.t.start) s[0] = 0u;
+            if (kMask && !KEYS && lonely) {
+#pragma unroll
+              for (int k = 0; k < 32; ++k) s[k] = 0u;
+            }
+          };
+          if (masked) probabilities(std::true_type{}, std::false_type{});
+          else if (CAP && small_scores(p, s)) probabilities(std::false_type{}, std::true_type{});
+          else probabilities(std::false_type{}, std::false_type{});
+          // P to shared memory: this row's 64 bytes of the panel's 64-column chunk
+          if (!warp_wait(p_free, (turns & 1) ^ 1u, abort_flag)) { give_up(); ok = false; break; }
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<uint4*>(p_row + ((((panel & 1) * 4 + q) ^ (r & 7)) << 4)) = make_uint4(pk[4 * q], pk[4 * q + 1], pk[4 * q + 2], pk[4 * q + 3]);
+          ptx::fence_proxy_async_smem();
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive(p_full);
           __syncwarp();
-          if (KEYS) {
-            if (lonely && c0 == w.t.start) s[0] = 0u;
-          } else if (lonely) {
-#pragma unroll
-            for (int k = 0; k < 32; ++k) s[k] = 0u;
-          }
           if (!warp_wait(dp_full, turns & 1, abort_flag)) { give_up(); ok = false; break; }
           ptx::tcgen05_fence_after_sync();
-          uint32_t pk[16];
+          uint32_t g[32];
+          ptx::tmem_ld_x32(dp_at, g);
+          tmem_loaded(g);
+          if (masked) {   // tokens of another document: their dP may be anything
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            uint32_t g[16];
-            ptx::tmem_ld_x16(dp_at + 16 * c, g);
-            tmem_loaded(g);
-            if (masked) {   // tokens of another document: their dP may be anything
+            for (int k = 0; k < 32; ++k) g[k] = k >= lo && k < hi ? g[k] : __float_as_uint(delta);
+          }
 #pragma unroll
-              for (int k = 0; k < 16; ++k) g[k] = 16 * c + k >= lo && 16 * c + k < hi ? g[k] : __float_as_uint(delta);
+          for (int i4 = 0; i4 < 8; ++i4) {
+            float2 d0 = q8::both(-delta), d1 = d0;
+            if (KEYS) {
+              const float4 v = *reinterpret_cast<const float4*>(vec + kRows + 4 * i4);
+              d0 = make_float2(-v.x, -v.y);
+              d1 = make_float2(-v.z, -v.w);
             }
-#pragma unroll
-            for (int i4 = 0; i4 < 4; ++i4) {
-              float dl[4] = {delta, delta, delta, delta};
-              if (KEYS) {
-                const float4 v = *reinterpret_cast<const float4*>(vec + kRows + 16 * c + 4 * i4);
-                dl[0] = v.x; dl[1] = v.y; dl[2] = v.z; dl[3] = v.w;
-              }
-              float e[4];
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                e[k] = __uint_as_float(s[16 * c + 4 * i4 + k]) * (__uint_as_float(g[4 * i4 + k]) - dl[k]);
-                if (!KEYS) rest += e[k];
-              }
-              if (CAP) {
-                const float2 f0 = __half22float2(slopes[CAP ? 8 * c + 2 * i4 : 0]), f1 = __half22float2(slopes[CAP ? 8 * c + 2 * i4 + 1 : 0]);
-                e[0] *= f0.x; e[1] *= f0.y; e[2] *= f1.x; e[3] *= f1.y;
-              }
-              pk[8 * c + 2 * i4] = pack2(e[0], e[1]);
-              pk[8 * c + 2 * i4 + 1] = pack2(e[2], e[3]);
+            auto pair = [&](int k) { return make_float2(__uint_as_float(g[k]), __uint_as_float(g[k + 1])); };
+            auto prob = [&](int k) { return make_float2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])); };
+            float2 e0 = q8::mul2(prob(4 * i4), q8::add2(pair(4 * i4), d0)), e1 = q8::mul2(prob(4 * i4 + 2), q8::add2(pair(4 * i4 + 2), d1));
+            if (!KEYS) rest2 = q8::add2(rest2, q8::add2(e0, e1));
+            if (CAP) {
+              e0 = q8::mul2(e0, __half22float2(slopes[CAP ? 2 * i4 : 0]));
+              e1 = q8::mul2(e1, __half22float2(slopes[CAP ? 2 * i4 + 1 : 0]));
             }
+            pk[2 * i4] = pack2(e0.x, e0.y);
+            pk[2 * i4 + 1] = pack2(e1.x, e1.y);
           }
           ptx::tmem_st_x16(dp_at, pk);
           ptx::tmem_st_wait();
@@ -465,6 +492,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!ok) break;
       if (!KEYS) {
         // r of the row: the panels' parts, [0] + [2] and [1] + [3] first (room for two)
+        float rest = rest2.x + rest2.y;
         float* part = reinterpret_cast<float*>(gen + M::kExchange);
         if (!warp_wait(parts_free, (it & 1) ^ 1u, abort_flag)) { give_up(); break; }   // those of the item before have been read
         if (panel < 2) part[panel * kRows + r] = rest;
@@ -483,6 +511,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         if (panel == 0 && live) p.delta[int64_t(w.head) * p.tokens + row] = delta + rest;
         __syncwarp();
+        rest2.x = rest;
       }
       if (!warp_wait(out_full, it & 1, abort_flag)) { give_up(); break; }
       ptx::tcgen05_fence_after_sync();
@@ -526,7 +555,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) ptx::mbar_arrive(out_free);
         __syncwarp();
 #pragma unroll
-        for (int k = 0; k < quarter_cols; ++k) a[k] = __float_as_uint(fmaf(-rest, __uint_as_float(b[k]), __uint_as_float(a[k])));
+        for (int k = 0; k < quarter_cols; ++k) a[k] = __float_as_uint(fmaf(-rest2.x, __uint_as_float(b[k]), __uint_as_float(a[k])));
         if (live && col < p.d) store_bf16(p.dQ + int64_t(row) * p.lddq + int64_t(w.head) * p.d + col, a, p.scale, p.d - col);
         __syncwarp();
       }

@@ -2,9 +2,10 @@
 //
 // Forward, one work item: 256 queries of one head (two halves of 128) against the keys they see, tile by tile from the last one
 // to the first (so that the masked tiles, and with a distance bias the largest scores, come first).  S = Q K^T of a half lies
-// in 128 columns of tensor memory, one query per lane; a warpgroup takes the rows' maxima, writes P = 2^(x - m) over S as bf16
-// and the tensor core multiplies P from there with V.  The two halves take turns: while one's exponentials are taken the
-// products of the other run.
+// in 128 columns of tensor memory, one query per lane; a warpgroup reads its rows whole into registers, takes their maxima, and
+// writes P = 2^(x - m) to shared memory as bf16, from where the tensor core multiplies it with V.  The next S is taken as soon as this
+// one is in registers, so the warpgroups never wait for scores: with P written over S they did, for as long as they
+// worked.
 //
 // The sums O are rescaled only where a row's maximum has grown by more than 2^8 since its reference m was taken (P then is at
 // most 2^8, bf16 and fp32 hold that without loss of digits), which after the first tiles hardly ever happens; the row sums are
@@ -14,7 +15,8 @@
 // the special function units: both at once.
 //
 // Roles (384 threads, one CTA per SM, persistent): warp 0 copies, warp 1 products and tensor memory, warps 4..7 and 8..11
-// the rows of the two halves.
+// the rows of the two halves, with 208 registers a thread (the first warpgroup's threads keep 88: 128 x 88 + 256 x 208 is what
+// the launch has).
 #include <algorithm>
 
 #include "acx_attn.cuh"
@@ -137,9 +139,11 @@ static_assert(kBins == kPlanThreads, "one bin per thread");
 constexpr int kFwdThreads = 384;
 template <int HD>
 struct FwdSmem {
-  static constexpr int kStages = HD == 128 ? 4 : 8;
-  static constexpr int kQ = 2 * Tile<HD>::kBytes, kBars = kQ + kStages * Tile<HD>::kBytes;
-  static constexpr int kBytes = kBars + 512 + 1024;   // 1024: the tiles' alignment
+  static constexpr int kStages = HD == 128 ? 3 : 6;
+  static constexpr int kP = 2 * Tile<HD>::kBytes, kPBytes = kRows * kRows * 2;      // behind the two halves of Q
+  static constexpr int kTiles = kP + 2 * kPBytes, kBars = kTiles + kStages * Tile<HD>::kBytes;
+  static constexpr int kBytes = kBars + 256;
+  static_assert(kBytes <= 232448, "shared memory of one CTA");
 };
 
 template <int HD, bool CAP, bool BIAS>
@@ -148,20 +152,22 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
                     const __grid_constant__ CUtensorMap map_v, const Params p) {
   using T = Tile<HD>;
   constexpr int kStages = FwdSmem<HD>::kStages;
-  extern __shared__ uint8_t smem_raw[];
-  const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
-  uint8_t* gen = smem_raw + (base - ptx::smem_u32(smem_raw));
+  extern __shared__ __align__(1024) uint8_t gen[];   // tiles start on their swizzle's boundary
+  const uint32_t base = ptx::smem_u32(gen);
   const uint32_t bars = base + FwdSmem<HD>::kBars;
   auto full = [&](int s) { return bars + 8u * s; };
   auto empty = [&](int s) { return bars + 8u * (kStages + s); };
   const uint32_t misc = bars + 16u * kStages;
   const uint32_t q_full = misc, q_empty = misc + 8, done = misc + 16;
   auto s_full = [&](int h) { return misc + 24 + 8u * h; };
-  auto p_full = [&](int h) { return misc + 40 + 8u * h; };
-  auto o_full = [&](int h) { return misc + 56 + 8u * h; };
-  auto o_free = [&](int h) { return misc + 72 + 8u * h; };
-  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + FwdSmem<HD>::kBars + 16 * kStages + 88);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + FwdSmem<HD>::kBars + 16 * kStages + 92);
+  auto s_free = [&](int h) { return misc + 40 + 8u * h; };
+  auto p_full = [&](int h) { return misc + 56 + 8u * h; };
+  auto p_free = [&](int h) { return misc + 72 + 8u * h; };
+  auto o_full = [&](int h) { return misc + 88 + 8u * h; };
+  auto o_free = [&](int h) { return misc + 104 + 8u * h; };
+  constexpr int kSlot = FwdSmem<HD>::kBars + 16 * kStages + 120;
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + kSlot);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + kSlot + 4);
   volatile int* no_abort = abort_flag + 1;   // for the one wait that has to run its time even so
   const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // the warp's number, known to be the same in all lanes
 
@@ -176,7 +182,9 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
     *no_abort = 0;
     for (int h = 0; h < 2; ++h) {
       ptx::mbar_init(s_full(h), 1);
+      ptx::mbar_init(s_free(h), 4);
       ptx::mbar_init(p_full(h), 4);
+      ptx::mbar_init(p_free(h), 1);
       ptx::mbar_init(o_full(h), 1);
       ptx::mbar_init(o_free(h), 4);
     }
@@ -186,7 +194,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
   // A warp comes to the barrier as a whole: halves of it would count as two, and let the others read the address before it is there
   __syncwarp();
   if (warp == 1) {
-    ptx::tmem_alloc(misc + 88, 512);
+    ptx::tmem_alloc(base + kSlot, 512);
     ptx::tmem_relinquish_alloc_permit();
     __syncwarp();
   }
@@ -210,20 +218,20 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
     return ((p.causal ? max(min(r + kRows, t.end), t.prefix) : t.end) - t.start + kRows - 1) / kRows;
   };
 
+  if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
   if (warp == 0) {
     // ---------------------------------------------------------------------------------------------------- copies
     if (lane == 0) {
       int stage = 0, it = 0;
-      uint32_t phase = 0, armed = 0;
+      uint32_t phase = 0;
       bool ok = true;
       auto push = [&](const CUtensorMap* map, int head, int row) {
         if (!ptx::mbar_wait(empty(stage), phase ^ 1u, abort_flag)) { give_up(); ok = false; return; }
-        armed |= 1u << stage;
         ptx::mbar_arrive_expect_tx(full(stage), T::kBytes);
-        T::load(base + FwdSmem<HD>::kQ + stage * T::kBytes, map, full(stage), head, row);
+        T::load(base + FwdSmem<HD>::kTiles + stage * T::kBytes, map, full(stage), head, row);
         if (++stage == kStages) { stage = 0; phase ^= 1u; }
       };
-      for (int u = blockIdx.x; ok && u < units; u += gridDim.x, ++it) {
+      for (int u; ok && (u = unit_of(it)) < units; ++it) {
         const Item t = fetch_item(p.items, u / p.heads);
         const int h = u % p.heads, g = h / p.group;
         const int n1 = key_tiles(t, 1), n = max(key_tiles(t, 0), n1);
@@ -231,26 +239,22 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
         ptx::mbar_arrive_expect_tx(q_full, (n1 ? 2 : 1) * T::kBytes);
         T::load(base, &map_q, q_full, h, t.row0);
         if (n1) T::load(base + T::kBytes, &map_q, q_full, h, t.row0 + kRows);
+        // in the order of their use: a tile's keys one turn ahead of its values
+        push(&map_k, g, t.start + (n - 1) * kRows);
         for (int j = n - 1; ok && j >= 0; --j) {
-          push(&map_k, g, t.start + j * kRows);
+          if (j > 0) push(&map_k, g, t.start + (j - 1) * kRows);
           if (ok) push(&map_v, g, t.start + j * kRows);
         }
       }
-      if (!ok) {   // copies in flight must land before the CTA leaves (one limit for all)
+      if (!ok) {   // copies in flight land before the CTA leaves: one limit, well above a copy's time
         const uint64_t t0 = ptx::globaltimer_ns();
-        for (int s = 0; s < kStages; ++s) {
-          if (!(armed & (1u << s))) continue;
-          const uint32_t ph = s < stage ? phase : phase ^ 1u;
-          while (!ptx::mbar_try_wait(full(s), ph) && ptx::globaltimer_ns() - t0 < ptx::kWaitLimitNs) {}
-        }
-        if (it > 0 || armed)
-          while (!ptx::mbar_try_wait(q_full, it & 1) && ptx::globaltimer_ns() - t0 < ptx::kWaitLimitNs / 4) {}
+        while (ptx::globaltimer_ns() - t0 < 10000000ull) {}
       }
     }
     __syncwarp();
   } else if (warp == 1) {
     // ---------------------------------------------------------------------------------------------------- products
-    int stage = 0, it = 0, turns[2] = {0, 0}, outs[2] = {0, 0};
+    int stage = 0, it = 0, reads[2] = {0, 0}, turns[2] = {0, 0}, outs[2] = {0, 0};
     uint32_t phase = 0;
     bool ok = true;
     const int d16 = (p.d + 15) / 16;
@@ -264,51 +268,50 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
       if (++stage == kStages) { stage = 0; phase ^= 1u; }
       return s;
     };
-    auto addr = [&](Slot s) { return base + FwdSmem<HD>::kQ + s.stage * T::kBytes; };
-    for (int u = blockIdx.x; ok && u < units; u += gridDim.x, ++it) {
+    auto addr = [&](Slot s) { return base + FwdSmem<HD>::kTiles + s.stage * T::kBytes; };
+    for (int u; ok && (u = unit_of(it)) < units; ++it) {
       const Item t = fetch_item_warp(p.items, u / p.heads);
       const int nt[2] = {key_tiles(t, 0), key_tiles(t, 1)}, n = max(nt[0], nt[1]);
-      auto scores = [&](int h, Slot k) {
-        scores_mma<HD>(tmem_s(h), base + h * T::kBytes, addr(k), d16);
-        ptx::umma_commit_elected(s_full(h));
-      };
-      wait(q_full, it & 1);
-      Slot k = next(), v;
-      if (!wait(full(k.stage), k.phase)) break;
-      ptx::tcgen05_fence_after_sync();
+      // scores of key tile j for the halves that see it, each once its scores before have been read
+      auto scores = [&](int j) {
+        const Slot k = next();
+        if (!wait(full(k.stage), k.phase)) return;
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-        if (nt[h] == n) scores(h, k);
-      ptx::umma_commit_elected(empty(k.stage));
-      if (n == 1) ptx::umma_commit_elected(q_empty);
+        for (int h = 0; h < 2; ++h) {
+          if (j >= nt[h]) continue;
+          if (!wait(s_free(h), (reads[h] & 1) ^ 1u)) return;
+          ++reads[h];
+          ptx::tcgen05_fence_after_sync();
+          scores_mma<HD>(tmem_s(h), base + h * T::kBytes, addr(k), d16);
+          ptx::umma_commit_elected(s_full(h));
+        }
+        ptx::umma_commit_elected(empty(k.stage));
+        if (j == 0) ptx::umma_commit_elected(q_empty);
+      };
+      if (!wait(q_full, it & 1)) break;
+      scores(n - 1);
       for (int j = n - 1; ok && j >= 0; --j) {
-        v = next();
+        if (j > 0) scores(j - 1);
+        const Slot v = next();
         if (!wait(full(v.stage), v.phase)) break;
         const int left = t.end - (t.start + j * kRows);   // keys of this tile inside the document
         const int steps = min(kRows, left + 15) / 16;
         if (left < 16 * steps) T::zero_rows(gen + (addr(v) - base), left, 16 * steps);
-        if (j > 0) {
-          k = next();
-          if (!wait(full(k.stage), k.phase)) break;
-        }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          if (j < nt[h]) {
-            if (j == nt[h] - 1 && !wait(o_free(h), (outs[h] & 1) ^ 1u)) break;
-            if (!wait(p_full(h), turns[h] & 1)) break;
-            ++turns[h];
-            ptx::tcgen05_fence_after_sync();
-            rows_mma<HD, 0>(tmem_o(h), tmem_s(h), addr(v), steps, d16, j < nt[h] - 1);
-            if (j == 0) {
-              ptx::umma_commit_elected(o_full(h));
-              ++outs[h];
-            }
+          if (j >= nt[h]) continue;
+          if (j == nt[h] - 1 && !wait(o_free(h), (outs[h] & 1) ^ 1u)) break;
+          if (!wait(p_full(h), turns[h] & 1)) break;
+          ++turns[h];
+          ptx::tcgen05_fence_after_sync();
+          smem_rows_mma<HD>(tmem_o(h), base + FwdSmem<HD>::kP + h * FwdSmem<HD>::kPBytes, addr(v), steps, d16, j < nt[h] - 1);
+          ptx::umma_commit_elected(p_free(h));
+          if (j == 0) {
+            ptx::umma_commit_elected(o_full(h));
+            ++outs[h];
           }
-          if (j > 0 && j <= nt[h]) scores(h, k);
         }
         ptx::umma_commit_elected(empty(v.stage));
-        if (j > 0) ptx::umma_commit_elected(empty(k.stage));
-        if (j == 1) ptx::umma_commit_elected(q_empty);
       }
     }
     // everything that was issued has to be done before the tensor memory is given back
@@ -319,63 +322,93 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
     __syncwarp();
   } else if (warp >= 4) {
     // ---------------------------------------------------------------------------------------------------- rows
-    const int half = (warp - 4) >> 2, quarter = warp & 3;
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    const int half = (warp - 4) >> 2, quarter = warp & 3, r = 32 * quarter + lane;
     const uint32_t lanes = uint32_t(32 * quarter) << 16;
     const uint32_t s_at = tmem_s(half) + lanes, o_at = tmem_o(half) + lanes;
-    int turns = 0, outs = 0;
+    uint8_t* const p_row = gen + FwdSmem<HD>::kP + half * FwdSmem<HD>::kPBytes + r * 128;
+    int turns = 0, outs = 0, it = 0;
     bool ok = true;
-    for (int u = blockIdx.x; ok && u < units; u += gridDim.x) {
+    for (int u; ok && (u = unit_of(it)) < units; ++it) {
       const Item t = fetch_item_warp(p.items, u / p.heads);
       const int n = key_tiles(t, half), head = u % p.heads;
       if (n == 0) continue;
-      const int r0 = t.row0 + kRows * half, row = r0 + 32 * quarter + lane;
+      const int r0 = t.row0 + kRows * half, row = r0 + r;
       const int sees = p.causal ? min(max(row + 1, t.prefix), t.end) : t.end;       // this row: keys [start, sees)
       const int all_see = p.causal ? min(max(r0 + 1, t.prefix), t.end) : t.end;     // every row of the half
       const float slope2 = BIAS ? __ldg(p.slopes + head) * kLog2e : 0.f;
       float m = 0.f, l = 0.f;
-      for (int j = n - 1; j >= 0; --j) {
+      for (int j = n - 1; j >= 0; --j, ++turns) {
         if (!warp_wait(s_full(half), turns & 1, abort_flag)) { give_up(); ok = false; break; }
-        ++turns;
         ptx::tcgen05_fence_after_sync();
+        uint32_t s[4][32];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) ptx::tmem_ld_x32(s_at + 32 * c, s[c]);
+        tmem_loaded(s[0], s[1], s[2], s[3]);
+        ptx::tcgen05_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(s_free(half));
+        __syncwarp();
         const int k0 = t.start + j * kRows;
-        const bool masked = k0 + kRows > all_see;
-        const int limit = sees - k0;
         constexpr bool kRaw = !CAP && !BIAS;   // raw scores: the scale is left to the exponent's fma
         const float scale = kRaw ? p.c : 1.f;
-        // 32 columns at a time, twice: first for the maximum (other than raw scores go back as exponents), then for the
-        // probabilities.  All 128 in registers at once do not fit beside the rest.
-        float mx = __int_as_float(0xFF800000);
+        if (CAP) {
+          auto capped = [&](auto is_small) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                s[c][i] = __float_as_uint(exponent<CAP, BIAS, decltype(is_small)::value>(p, __uint_as_float(s[c][i]),
+                                                                                          float(row - k0) - float(32 * c + i), slope2));
+          };
+          if (small_scores(p, s[0]) && small_scores(p, s[1]) && small_scores(p, s[2]) && small_scores(p, s[3])) capped(std::true_type{});
+          else capped(std::false_type{});
+        } else if (BIAS) {
+          // where every key is before every query the distance needs no magnitude: x = c s + slope column - slope (row - k0)
+          const float2 c2 = q8::both(p.c), slopes = q8::both(slope2), from = q8::both(-slope2 * float(row - k0));
+          const bool before = k0 + kRows <= r0;
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) {
+              float2 x = make_float2(__uint_as_float(s[c][i]), __uint_as_float(s[c][i + 1]));
+              const float2 col = make_float2(float(32 * c + i), float(32 * c + i + 1));
+              if (before) {
+                x = q8::fma2(x, c2, q8::fma2(slopes, col, from));
+              } else {
+                const float d = float(row - k0);
+                x = q8::fma2(x, c2, make_float2(-slope2 * fabsf(d - col.x), -slope2 * fabsf(d - col.y)));
+              }
+              s[c][i] = __float_as_uint(x.x);
+              s[c][i + 1] = __float_as_uint(x.y);
+            }
+        }
+        if (k0 + kRows > all_see) {
+          const int limit = sees - k0;
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (32 * c + i >= limit) s[c][i] = 0xFF800000u;   // minus infinity
+        }
+        float top[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          uint32_t s[32];
-          ptx::tmem_ld_x32(s_at + 32 * c, s);
-          tmem_loaded(s);
-          if (!kRaw) {
+          top[c] = __uint_as_float(s[c][0]);
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-              s[i] = __float_as_uint(exponent<CAP, BIAS>(p, __uint_as_float(s[i]), float(row - k0) - float(32 * c + i), slope2));
-          }
-          if (masked) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (32 * c + i >= limit) s[i] = 0xFF800000u;   // minus infinity
-          }
-          if (!kRaw) ptx::tmem_st_x32(s_at + 32 * c, s);
-          float top[2] = {__uint_as_float(s[0]), __uint_as_float(s[1])};
-#pragma unroll
-          for (int i = 2; i < 32; ++i) top[i & 1] = fmaxf(top[i & 1], __uint_as_float(s[i]));
-          mx = fmaxf(mx, fmaxf(top[0], top[1]));
+          for (int i = 1; i < 32; ++i) top[c] = fmaxf(top[c], __uint_as_float(s[c][i]));
         }
-        if (!kRaw) ptx::tmem_st_wait();
-        mx *= scale;
+        const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * scale;
+        // the products with the P before are done: P's place is free, and the sums may be rescaled
+        if (!warp_wait(p_free(half), (turns & 1) ^ 1u, abort_flag)) { give_up(); ok = false; break; }
         if (j == n - 1) {
           m = mx;
         } else if (__any_sync(0xFFFFFFFFu, mx > m + 8.f)) {
-          // the products up to the tile before are done: this tile's scores were issued behind them
+          ptx::tcgen05_fence_after_sync();
           const float m_new = fmaxf(m, mx), f = exp2_fast(m - m_new);
           m = m_new;
           l *= f;
-#pragma unroll
+#pragma unroll 1
           for (int c = 0; c < HD / 16; ++c) {
             uint32_t o[16];
             ptx::tmem_ld_x16(o_at + 16 * c, o);
@@ -384,30 +417,29 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
             for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
             ptx::tmem_st_x16(o_at + 16 * c, o);
           }
+          ptx::tmem_st_wait();
+          ptx::tcgen05_fence_before_sync();
         }
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        const float2 scale2 = q8::both(scale), m2 = q8::both(-m);
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          uint32_t s[32], w[16];
-          ptx::tmem_ld_x32(s_at + 32 * c, s);
-          tmem_loaded(s);
-          if (kRaw && masked) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (32 * c + i >= limit) s[i] = 0xFF800000u;
-          }
+          for (int q = 0; q < 4; ++q) {   // eight columns: 16 bytes
+            uint32_t w[4];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const float a = exp2_fast(fmaf(__uint_as_float(s[2 * i]), scale, -m)), b = exp2_fast(fmaf(__uint_as_float(s[2 * i + 1]), scale, -m));
-            sum[(2 * i) & 3] += a;
-            sum[(2 * i + 1) & 3] += b;
-            w[i] = pack2(a, b);
+            for (int i = 0; i < 4; ++i) {
+              const int k = 8 * q + 2 * i;
+              const float2 x = q8::fma2(make_float2(__uint_as_float(s[c][k]), __uint_as_float(s[c][k + 1])), scale2, m2);
+              const float2 e = make_float2(exp2_fast(x.x), exp2_fast(x.y));
+              sum[i & 1] = q8::add2(sum[i & 1], e);
+              w[i] = pack2(e.x, e.y);
+            }
+            *reinterpret_cast<uint4*>(p_row + (c >> 1) * (kRows * 128) + ((((c & 1) * 4 + q) ^ (r & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
           }
-          ptx::tmem_st_x16(s_at + 16 * c, w);   // over columns that have been read
         }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        ptx::tmem_st_wait();
-        ptx::tcgen05_fence_before_sync();
+        l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+        ptx::fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(p_full(half));
         __syncwarp();
@@ -418,7 +450,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
       ptx::tcgen05_fence_after_sync();
       const float f = 1.f / l;
       __nv_bfloat16* at = p.O + int64_t(row) * p.ldo + int64_t(head) * p.d;
-#pragma unroll
+#pragma unroll 1
       for (int c = 0; c < HD / 32; ++c) {
         if (32 * c >= p.d) break;
         uint32_t o[32];
@@ -434,8 +466,10 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
         __syncwarp();
       }
       if (p.lse && row < t.end) p.lse[int64_t(head) * p.tokens + row] = (m + log2f(l)) * kLn2;
+      __syncwarp();
     }
   }
+  __syncwarp();
   zero_rows_outside(p, p.O, p.ldo, p.heads, p.lse, __int_as_float(0xFF800000));
   __syncwarp();
   ptx::tcgen05_fence_before_sync();

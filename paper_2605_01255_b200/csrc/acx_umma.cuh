@@ -209,8 +209,9 @@ __device__ __forceinline__ void umma_bf16(uint32_t tmem_d, uint64_t desc_a, uint
 // of a product of 128 x 128 x 16 (64 cycles) have to be there before it: with a thread issuing alone, each instruction's descriptors
 // went from its registers to the warp's uniform ones (150 to 180 cycles an instruction, and the attention kernels were bound by it);
 // here all lanes hold the same values, and a step is two additions.
-//   lo, hi: halves of make_smem_desc's value.  A and B advance by two units of 16 bytes per step (K-major, inside 64 columns).
-template <int STEPS>
+//   lo, hi: halves of make_smem_desc's value.  A advances by two units of 16 bytes per step (K-major, inside 64 columns), B by B_STEP
+//   (2 as A; 128 MN-major: 16 rows of 128 bytes).
+template <int STEPS, int B_STEP>
 __device__ __forceinline__ void umma_steps(uint32_t tmem_d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, bool accumulate) {
   static_assert(STEPS == 1 || STEPS == 4, "a step or four");
   if (STEPS == 1)
@@ -228,13 +229,13 @@ __device__ __forceinline__ void umma_steps(uint32_t tmem_d, uint32_t a_lo, uint3
         "mov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\t"
         "@lead tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, acc;\n\t"
         "setp.eq.u32 acc, 0, 0;\n\t"
-        "add.u32 al, %1, 2;\n\tadd.u32 bl, %2, 2;\n\tmov.b64 a, {al, %3};\n\tmov.b64 b, {bl, %3};\n\t"
+        "add.u32 al, %1, 2;\n\tadd.u32 bl, %2, %6;\n\tmov.b64 a, {al, %3};\n\tmov.b64 b, {bl, %3};\n\t"
         "@lead tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, acc;\n\t"
-        "add.u32 al, %1, 4;\n\tadd.u32 bl, %2, 4;\n\tmov.b64 a, {al, %3};\n\tmov.b64 b, {bl, %3};\n\t"
+        "add.u32 al, %1, 4;\n\tadd.u32 bl, %2, %7;\n\tmov.b64 a, {al, %3};\n\tmov.b64 b, {bl, %3};\n\t"
         "@lead tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, acc;\n\t"
-        "add.u32 al, %1, 6;\n\tadd.u32 bl, %2, 6;\n\tmov.b64 a, {al, %3};\n\tmov.b64 b, {bl, %3};\n\t"
+        "add.u32 al, %1, 6;\n\tadd.u32 bl, %2, %8;\n\tmov.b64 a, {al, %3};\n\tmov.b64 b, {bl, %3};\n\t"
         "@lead tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, acc;\n\t}"
-        ::"r"(tmem_d), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(uint32_t(accumulate))
+        ::"r"(tmem_d), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(uint32_t(accumulate)), "n"(B_STEP), "n"(2 * B_STEP), "n"(3 * B_STEP)
         : "memory");
 }
 // The same with A in tensor memory (lane = row, each 32-bit column two consecutive bf16 along K), eight columns per step, A's third step GAP columns behind the second; B (MN-major, 128 bytes wide
