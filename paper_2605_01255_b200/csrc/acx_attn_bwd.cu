@@ -414,13 +414,23 @@ __global__ void __launch_bounds__(kThreads, 1)
               auto score = [&](int k) { return make_float2(__uint_as_float(s[4 * i4 + k]), __uint_as_float(s[4 * i4 + k + 1])); };
               const float2 x01 = q8::fma2(score(0), q8::both(p.c), make_float2(-l[0], -l[1])),
                            x23 = q8::fma2(score(2), q8::both(p.c), make_float2(-l[2], -l[3]));
+              float2 x[2] = {x01, x23};
+              if (CAP || BIAS) {
+                auto at = [&](int k) {
+                  const int col = 4 * i4 + k;
+                  return exponent<CAP, BIAS, kSmall>(p, __uint_as_float(s[col]), float(c0 - row) + float(col), slope2, &slope[k]) - l[k];
+                };
+                x[0] = make_float2(at(0), at(1));
+                x[1] = make_float2(at(2), at(3));
+              }
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                e[2 * k] = exp2_fast(x[k].x);
+                e[2 * k + 1] = exp2_fast(x[k].y);
+              }
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
                 const int col = 4 * i4 + k;
-                float x;
-                if (!CAP && !BIAS) x = k & 1 ? (k == 1 ? x01.y : x23.y) : (k == 0 ? x01.x : x23.x);
-                else x = exponent<CAP, BIAS, kSmall>(p, __uint_as_float(s[col]), float(c0 - row) + float(col), slope2, &slope[k]) - l[k];
-                e[k] = exp2_fast(x);
                 if (kMask) e[k] = col >= lo && col < hi ? e[k] : 0.f;
                 s[col] = __float_as_uint(e[k]);
                 if (CAP && !KEYS) e[k] *= slope[k];   // what an error of delta is multiplied with

@@ -364,24 +364,27 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
           if (small_scores(p, s[0]) && small_scores(p, s[1]) && small_scores(p, s[2]) && small_scores(p, s[3])) capped(std::true_type{});
           else capped(std::false_type{});
         } else if (BIAS) {
-          // where every key is before every query the distance needs no magnitude: x = c s + slope column - slope (row - k0)
-          const float2 c2 = q8::both(p.c), slopes = q8::both(slope2), from = q8::both(-slope2 * float(row - k0));
-          const bool before = k0 + kRows <= r0;
+          const float2 c2 = q8::both(p.c);
+          const float d = float(row - k0);
+          if (k0 + kRows <= r0) {
+            // every key is before every query, the distance needs no magnitude: x = c s + slope column - slope (row - k0)
+            const float2 slopes = q8::both(slope2), from = q8::both(-slope2 * d);
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
+            for (int c = 0; c < 4; ++c)
 #pragma unroll
-            for (int i = 0; i < 32; i += 2) {
-              float2 x = make_float2(__uint_as_float(s[c][i]), __uint_as_float(s[c][i + 1]));
-              const float2 col = make_float2(float(32 * c + i), float(32 * c + i + 1));
-              if (before) {
-                x = q8::fma2(x, c2, q8::fma2(slopes, col, from));
-              } else {
-                const float d = float(row - k0);
-                x = q8::fma2(x, c2, make_float2(-slope2 * fabsf(d - col.x), -slope2 * fabsf(d - col.y)));
+              for (int i = 0; i < 32; i += 2) {
+                const float2 x = q8::fma2(make_float2(__uint_as_float(s[c][i]), __uint_as_float(s[c][i + 1])), c2,
+                                          q8::fma2(slopes, make_float2(float(32 * c + i), float(32 * c + i + 1)), from));
+                s[c][i] = __float_as_uint(x.x);
+                s[c][i + 1] = __float_as_uint(x.y);
               }
-              s[c][i] = __float_as_uint(x.x);
-              s[c][i + 1] = __float_as_uint(x.y);
-            }
+          } else {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                s[c][i] = __float_as_uint(fmaf(__uint_as_float(s[c][i]), p.c, -slope2 * fabsf(d - float(32 * c + i))));
+          }
         }
         if (k0 + kRows > all_see) {
           const int limit = sees - k0;
@@ -394,18 +397,18 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
         float top[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          top[c] = __uint_as_float(s[c][0]);
+          top[c] = max_nan(__uint_as_float(s[c][0]), __uint_as_float(s[c][1]));
 #pragma unroll
-          for (int i = 1; i < 32; ++i) top[c] = fmaxf(top[c], __uint_as_float(s[c][i]));
+          for (int i = 2; i < 32; i += 2) top[c] = max_nan(top[c], __uint_as_float(s[c][i]), __uint_as_float(s[c][i + 1]));
         }
-        const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * scale;
+        const float mx = max_nan(max_nan(top[0], top[1], top[2]), top[3]) * scale;
         // the products with the P before are done: P's place is free, and the sums may be rescaled
         if (!warp_wait(p_free(half), (turns & 1) ^ 1u, abort_flag)) { give_up(); ok = false; break; }
         if (j == n - 1) {
           m = mx;
-        } else if (__any_sync(0xFFFFFFFFu, mx > m + 8.f)) {
+        } else if (__any_sync(0xFFFFFFFFu, !(mx <= m + 8.f))) {   // (or not a number, which then the row's sums become)
           ptx::tcgen05_fence_after_sync();
-          const float m_new = fmaxf(m, mx), f = exp2_fast(m - m_new);
+          const float m_new = max_nan(m, mx), f = exp2_fast(m - m_new);
           m = m_new;
           l *= f;
 #pragma unroll 1
