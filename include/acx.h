@@ -438,8 +438,8 @@ ACX_API acx_status acx_embed_fwd(const acx_embed_desc* desc, const int64_t* ids,
 ACX_API acx_status acx_embed_bwd(const acx_embed_desc* desc, const int64_t* ids, const void* dY, void* dE, float beta, void* ws, size_t ws_bytes,
                                  void* cuda_stream);
 
-/* One gradient of a list: n elements at src (device, 16-byte aligned, any n >= 0), clipped into dst (which may be src; else neither
- * may overlap another). */
+/* One gradient of a list: n elements at src (device, 16-byte aligned, any n >= 0), clipped into dst.  dst may be src (of the same
+ * type); otherwise what is written may overlap nothing else in the list (ACX_ERR_INVALID_ARG: the order of the tensors is open). */
 typedef struct acx_grad {
   const void* src;
   void* dst;

@@ -43,7 +43,7 @@ struct PlanHeader {
 constexpr size_t kPlanListOffset = 256;
 struct PlanLayout {
   int64_t wide_cap, tile_cap;
-  size_t wide, queries, keys, cum, bytes;   // byte offsets of the lists; cum: running tile counts of the documents
+  size_t wide, queries, keys, cum, bytes;   // byte offsets of the lists; cum: the documents' running tile counts, for each list its own
 };
 __host__ __device__ inline PlanLayout plan_layout(int64_t tokens, int64_t docs) {
   const int64_t d = docs < tokens ? docs : tokens;   // documents that hold a token
@@ -54,7 +54,7 @@ __host__ __device__ inline PlanLayout plan_layout(int64_t tokens, int64_t docs) 
   p.queries = p.wide + size_t(p.wide_cap) * sizeof(Item);
   p.keys = p.queries + size_t(p.tile_cap) * sizeof(Item);
   p.cum = p.keys + size_t(p.tile_cap) * sizeof(Item);
-  p.bytes = p.cum + size_t(docs + 1) * 8;
+  p.bytes = p.cum + size_t(docs + 1) * 12;
   return p;
 }
 

@@ -20,50 +20,49 @@ namespace {
 
 constexpr int kThreads = 256, kVec = 8;
 constexpr int kChunk = int(kGradChunk);                 // elements of a tensor that a block takes at a time
-constexpr int kUnroll = 4;
-static_assert(kChunk % (kThreads * kVec * kUnroll) == 0, "whole rounds");
 constexpr int kBlocksPerSm = 4;
 constexpr int kMaxParts = 148 * kBlocksPerSm;           // blocks of the first launch at most
 
-// The plan in device memory: the tensors, then for every chunk its tensor and its number in it.
-struct Tensor {
+// The plan in device memory: one record per chunk.
+struct Chunk {
   const void* src;
   void* dst;
-  int64_t n;
+  int32_t n;
   float weight;
-  int16_t src_bf16, dst_bf16;
+  int32_t src_bf16, dst_bf16;
 };
-static_assert(sizeof(Tensor) == 32, "the plan's records");
-struct Chunk { uint32_t tensor, number; };
-size_t chunks_offset(int64_t tensors) { return (size_t(tensors) * sizeof(Tensor) + 255) & ~size_t(255); }
+static_assert(sizeof(Chunk) == 32, "two loads");
 
 // Tensors arrive as kernel parameters, so that nothing of the caller's memory is read after the call.
 constexpr int kBatch = 64;
-struct Batch {
-  Tensor t[kBatch];
-  int64_t first_chunk[kBatch];
-  int count;
-  int64_t first_tensor;
+struct Tensor {
+  const void* src;
+  void* dst;
+  int64_t n, first_chunk;
+  float weight;
+  int16_t src_bf16, dst_bf16;
 };
-__global__ void __launch_bounds__(kThreads) plan_kernel(const __grid_constant__ Batch b, Tensor* tensors, Chunk* chunks) {
+struct Batch { Tensor t[kBatch]; };
+__global__ void __launch_bounds__(kThreads) plan_kernel(const __grid_constant__ Batch b, Chunk* chunks) {
   wait_for_launch_before();
   let_next_launch_start();
-  const int i = blockIdx.x;
-  if (threadIdx.x == 0 && blockIdx.y == 0) tensors[b.first_tensor + i] = b.t[i];
-  const int64_t n = (b.t[i].n + kChunk - 1) / kChunk;
+  const Tensor& t = b.t[blockIdx.x];
+  const int64_t n = (t.n + kChunk - 1) / kChunk;
   for (int64_t k = int64_t(blockIdx.y) * kThreads + threadIdx.x; k < n; k += int64_t(gridDim.y) * kThreads)
-    chunks[b.first_chunk[i] + k] = Chunk{uint32_t(b.first_tensor + i), uint32_t(k)};
+    chunks[t.first_chunk + k] = Chunk{static_cast<const uint8_t*>(t.src) + k * (kChunk * (t.src_bf16 ? 2 : 4)),
+                                      static_cast<uint8_t*>(t.dst) + k * (kChunk * (t.dst_bf16 ? 2 : 4)),
+                                      int32_t(t.n - k * kChunk < kChunk ? t.n - k * kChunk : kChunk), t.weight, t.src_bf16, t.dst_bf16};
 }
 
-__device__ __forceinline__ Tensor fetch_tensor(const Tensor* t) {
-  union { int4 v[2]; Tensor t; } u;
-  u.v[0] = __ldcg(reinterpret_cast<const int4*>(t));
-  u.v[1] = __ldcg(reinterpret_cast<const int4*>(t) + 1);
-  return u.t;
-}
-__device__ __forceinline__ Chunk fetch_chunk(const Chunk* c) {
-  const uint2 v = __ldcg(reinterpret_cast<const uint2*>(c));
-  return Chunk{v.x, v.y};
+// Chunk i, or nothing to do if it is none
+__device__ __forceinline__ Chunk fetch_chunk(const Chunk* chunks, int64_t i, int64_t count) {
+  union { int4 v[2]; Chunk c; } u;
+  u.c.n = 0;
+  if (i >= 0 && i < count) {
+    u.v[0] = __ldcg(reinterpret_cast<const int4*>(chunks + i));
+    u.v[1] = __ldcg(reinterpret_cast<const int4*>(chunks + i) + 1);
+  }
+  return u.c;
 }
 
 template <typename T>
@@ -86,16 +85,22 @@ __device__ __forceinline__ double squares(const float2 (&v)[4]) {
   return d;
 }
 
+// Vectors of eight that a thread asks for before it uses the first: 128 bytes of either type.
+template <typename T>
+constexpr int kUnroll = 16 / int(sizeof(T));
+
 template <typename T>
 __device__ __forceinline__ double chunk_squares(const T* x, int n) {
+  constexpr int kUnroll = clip::kUnroll<T>;
   double sum = 0.;
   const int whole = n / kVec;
-  for (int i = threadIdx.x; i < whole; i += kThreads * kUnroll) {
+  const T* p = x + threadIdx.x * kVec;
+  for (int left = whole - int(threadIdx.x); left > 0; left -= kThreads * kUnroll, p += kThreads * kUnroll * kVec) {
     q8::Raw<T> r[kUnroll];
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k) {
       r[k].zero();
-      if (i + k * kThreads < whole) r[k].load(x + int64_t(i + k * kThreads) * kVec);
+      if (k * kThreads < left) r[k].load(p + k * kThreads * kVec);
     }
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k) {
@@ -125,18 +130,17 @@ __device__ __forceinline__ double block_sum(double x, double* warps) {
   return s;
 }
 
-__global__ void __launch_bounds__(kThreads) norm_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks, int64_t count,
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm) norm_kernel(const Chunk* __restrict__ chunks, int64_t count,
                                                         double* __restrict__ parts) {
   __shared__ double warps[kThreads / 32];
   wait_for_launch_before();
   let_next_launch_start();
   double sum = 0.;
+  Chunk next = fetch_chunk(chunks, blockIdx.x, count);
   for (int64_t c = blockIdx.x; c < count; c += gridDim.x) {
-    const Chunk k = fetch_chunk(chunks + c);
-    const Tensor t = fetch_tensor(tensors + k.tensor);
-    const int64_t at = int64_t(k.number) * kChunk;
-    const int n = int(min(int64_t(kChunk), t.n - at));
-    const double s = t.src_bf16 ? chunk_squares(static_cast<const __nv_bfloat16*>(t.src) + at, n) : chunk_squares(static_cast<const float*>(t.src) + at, n);
+    const Chunk t = next;
+    next = fetch_chunk(chunks, c + gridDim.x, count);
+    const double s = t.src_bf16 ? chunk_squares(static_cast<const __nv_bfloat16*>(t.src), t.n) : chunk_squares(static_cast<const float*>(t.src), t.n);
     sum += double(t.weight) * s;
   }
   sum = block_sum(sum, warps);
@@ -145,27 +149,32 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const Tensor* __restrict
 
 template <typename S, typename D>
 __device__ __forceinline__ void chunk_scale(const S* x, D* y, int n, float f) {
+  constexpr int kUnroll = clip::kUnroll<S>;
   const int whole = n / kVec;
-  for (int i = threadIdx.x; i < whole; i += kThreads * kUnroll) {
+  const S* p = x + threadIdx.x * kVec;
+  D* to = y + threadIdx.x * kVec;
+  constexpr int kRound = kThreads * kUnroll;
+  for (int left = whole - int(threadIdx.x); left > 0; left -= kRound, p += kRound * kVec, to += kRound * kVec) {
     q8::Raw<S> r[kUnroll];
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k)
-      if (i + k * kThreads < whole) r[k].load(x + int64_t(i + k * kThreads) * kVec);
+    for (int k = 0; k < kUnroll; ++k) {
+      r[k].zero();   // also what keeps the vectors of one chunk from living on to the next: the kernel spilled
+      if (k * kThreads < left) r[k].load(p + k * kThreads * kVec);
+    }
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k) {
-      if (i + k * kThreads >= whole) break;
       float2 v[4];
       r[k].get(v);
 #pragma unroll
       for (int q = 0; q < 4; ++q) v[q] = q8::mul2(v[q], q8::both(f));
-      q8::store8(y + int64_t(i + k * kThreads) * kVec, v);
+      if (k * kThreads < left) q8::store8(to + k * kThreads * kVec, v);
     }
   }
   const int i = whole * kVec + int(threadIdx.x);
   if (i < n) y[i] = D(element(x + i) * f);
 }
 
-__global__ void __launch_bounds__(kThreads) scale_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks, int64_t count,
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm) scale_kernel(const Chunk* __restrict__ chunks, int64_t count,
                                                          const double* __restrict__ parts, int part_count, float max_norm, float* __restrict__ total) {
   __shared__ double warps[kThreads / 32];
   wait_for_launch_before();
@@ -179,20 +188,19 @@ __global__ void __launch_bounds__(kThreads) scale_kernel(const Tensor* __restric
     total[0] = float(norm);
     total[1] = f;
   }
-  for (int64_t c = count - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
-    const Chunk k = fetch_chunk(chunks + c);
-    const Tensor t = fetch_tensor(tensors + k.tensor);
+  Chunk next = fetch_chunk(chunks, count - 1 - int64_t(blockIdx.x), count);
+  for (int64_t c = count - 1 - int64_t(blockIdx.x); c >= 0; c -= gridDim.x) {
+    const Chunk t = next;
+    next = fetch_chunk(chunks, c - gridDim.x, count);
     if (f == 1.f && t.src == t.dst) continue;
-    const int64_t at = int64_t(k.number) * kChunk;
-    const int n = int(min(int64_t(kChunk), t.n - at));
     if (t.src_bf16) {
-      const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(t.src) + at;
-      if (t.dst_bf16) chunk_scale(x, static_cast<__nv_bfloat16*>(t.dst) + at, n, f);
-      else chunk_scale(x, static_cast<float*>(t.dst) + at, n, f);
+      const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(t.src);
+      if (t.dst_bf16) chunk_scale(x, static_cast<__nv_bfloat16*>(t.dst), t.n, f);
+      else chunk_scale(x, static_cast<float*>(t.dst), t.n, f);
     } else {
-      const float* x = static_cast<const float*>(t.src) + at;
-      if (t.dst_bf16) chunk_scale(x, static_cast<__nv_bfloat16*>(t.dst) + at, n, f);
-      else chunk_scale(x, static_cast<float*>(t.dst) + at, n, f);
+      const float* x = static_cast<const float*>(t.src);
+      if (t.dst_bf16) chunk_scale(x, static_cast<__nv_bfloat16*>(t.dst), t.n, f);
+      else chunk_scale(x, static_cast<float*>(t.dst), t.n, f);
     }
   }
 }
@@ -204,41 +212,37 @@ unsigned blocks_for(int64_t chunks) { return unsigned(std::max<int64_t>(1, std::
 
 using namespace clip;
 
-size_t grad_plan_bytes(const GradProblem& q) { return chunks_offset(q.tensors) + size_t(q.chunks) * sizeof(Chunk); }
+size_t grad_plan_bytes(const GradProblem& q) { return size_t(std::max<int64_t>(q.chunks, 1)) * sizeof(Chunk); }
 size_t grad_clip_workspace_bytes(const GradProblem&) { return kMaxParts * sizeof(double); }
 
 cudaError_t grad_plan(const GradProblem& q, const acx_grad* list, void* plan, cudaStream_t st) {
-  Tensor* tensors = static_cast<Tensor*>(plan);
-  Chunk* chunks = reinterpret_cast<Chunk*>(static_cast<uint8_t*>(plan) + chunks_offset(q.tensors));
+  Chunk* chunks = static_cast<Chunk*>(plan);
   int64_t chunk = 0;
   for (int64_t i0 = 0; i0 < q.tensors; i0 += kBatch) {
     Batch b{};
-    b.first_tensor = i0;
-    b.count = int(std::min<int64_t>(kBatch, q.tensors - i0));
+    const int count = int(std::min<int64_t>(kBatch, q.tensors - i0));
     int64_t most = 1;
-    for (int i = 0; i < b.count; ++i) {
+    for (int i = 0; i < count; ++i) {
       const acx_grad& g = list[i0 + i];
-      b.t[i] = Tensor{g.src, g.dst, g.n, g.weight, int16_t(g.src_dtype == ACX_BF16), int16_t(g.dst_dtype == ACX_BF16)};
-      b.first_chunk[i] = chunk;
+      b.t[i] = Tensor{g.src, g.dst, g.n, chunk, g.weight, int16_t(g.src_dtype == ACX_BF16), int16_t(g.dst_dtype == ACX_BF16)};
       const int64_t n = (g.n + kChunk - 1) / kChunk;
       chunk += n;
       most = std::max(most, n);
     }
     const unsigned y = unsigned(std::min<int64_t>(64, (most + kThreads - 1) / kThreads));
-    const cudaError_t e = launch_lined_up(plan_kernel, dim3(unsigned(b.count), y), dim3(kThreads), 0, st, b, tensors, chunks);
+    const cudaError_t e = launch_lined_up(plan_kernel, dim3(unsigned(count), y), dim3(kThreads), 0, st, b, chunks);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
 }
 
 cudaError_t grad_clip(const GradProblem& q, const void* plan, float max_norm, float* total, void* ws, cudaStream_t st) {
-  const Tensor* tensors = static_cast<const Tensor*>(plan);
-  const Chunk* chunks = reinterpret_cast<const Chunk*>(static_cast<const uint8_t*>(plan) + chunks_offset(q.tensors));
+  const Chunk* chunks = static_cast<const Chunk*>(plan);
   double* parts = static_cast<double*>(ws);
   const unsigned blocks = blocks_for(q.chunks);
-  const cudaError_t e = launch_lined_up(norm_kernel, dim3(blocks), dim3(kThreads), 0, st, tensors, chunks, q.chunks, parts);
+  const cudaError_t e = launch_lined_up(norm_kernel, dim3(blocks), dim3(kThreads), 0, st, chunks, q.chunks, parts);
   if (e != cudaSuccess) return e;
-  return launch_lined_up(scale_kernel, dim3(blocks), dim3(kThreads), 0, st, tensors, chunks, q.chunks, static_cast<const double*>(parts), int(blocks),
+  return launch_lined_up(scale_kernel, dim3(blocks), dim3(kThreads), 0, st, chunks, q.chunks, static_cast<const double*>(parts), int(blocks),
                          max_norm, total);
 }
 

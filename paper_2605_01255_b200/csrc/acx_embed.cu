@@ -3,11 +3,12 @@
 // An id outside the vocabulary stands for no word: a row of zeros, no gradient.
 //
 // Both are bound by HBM.  The gradient's bytes are dY read once and the table written once (with beta = 1 the rows of the words that
-// occur only).  Its sums are taken over the tokens sorted by word: a stable radix sort with up to nine bits per pass (a kernel of
-// histograms and one that scatters), then runs of 32 sorted tokens per block.  A word whose tokens lie in one run is finished
-// there; what runs over a border leaves an fp32 row, and those rows, still sorted, are summed the same way level by level.  Every
-// sum has a fixed order: reproducible bits, and a word that fills an eighth of the batch costs no more than others.  Rows of words that
-// do not occur are written by blocks of their own in the launch of the first level, beside its latency-bound gathers.
+// occur only).  Its sums are taken over the tokens sorted by word: a stable radix sort with up to nine bits per pass (histograms
+// of the first digits by a launch of their own, of the others by the pass before), then runs of 32 sorted tokens per block.  A
+// word whose tokens lie in one run is finished there; what runs over a border leaves an fp32 row, and those rows, still sorted,
+// are summed the same way, 64 at a time, by the block that finishes the last of the runs they come from, level by level in the same
+// launch.  Every sum has a fixed order, whichever block takes it: reproducible bits, and a word that fills an eighth of the batch
+// costs no more than others.  Rows of words that do not occur are written by blocks of their own beside the latency-bound gathers.
 #include <algorithm>
 
 #include "acx_internal.h"
@@ -21,6 +22,7 @@ using q8::load8;
 using q8::store8;
 
 constexpr int kThreads = 256;
+constexpr uint32_t kNone = 0xFFFFFFFFu;
 
 // ----------------------------------------------------------------------------------------------------------------- lookup
 constexpr int kLookRows = 4;   // rows per thread, all asked for before the first is stored
@@ -55,18 +57,21 @@ __global__ void __launch_bounds__(kThreads) lookup_kernel(const int64_t* __restr
 }
 
 // ------------------------------------------------------------------------------------------------------------------- sort
-constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kRounds = 8;
-constexpr int kSortItems = kSortThreads * kRounds;   // per block; a warp has 32 * kRounds of them in a row
+constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 constexpr int kMaxDigit = 9, kMaxBins = 1 << kMaxDigit;
+// Items per thread, ROUNDS: one as long as that gives every SM a block at most (a pass is all latency then: two blocks of eight rounds
+// took 12 us for 16384 tokens), else eight, so that the table of every block's counts, which each block reads whole, stays small.
+constexpr int kFewBlocks = 148, kManyRounds = 8;
 
 struct SortPass {
   const int64_t* ids;        // first pass: keys from the ids, values 0, 1, 2, ...
   const uint2* in;           // later passes: (key, token)
   uint2* out;
   uint32_t* table;           // [block][bins]
+  uint32_t* next_table;      // the next pass's, zeros; null in the last pass
   int64_t n;
   uint32_t vocab;            // the key of every id outside the vocabulary
-  int shift, bins, blocks;
+  int shift, digit, blocks;
   uint32_t* present;         // last pass: one bit per word that occurs
 };
 __device__ __forceinline__ uint2 sort_item(const SortPass& s, int64_t i) {
@@ -74,63 +79,68 @@ __device__ __forceinline__ uint2 sort_item(const SortPass& s, int64_t i) {
   const int64_t id = __ldcg(reinterpret_cast<const long long*>(s.ids) + i);
   return make_uint2(id >= 0 && id < int64_t(s.vocab) ? uint32_t(id) : s.vocab, uint32_t(i));
 }
+// A warp has 32 * ROUNDS items in a row.
+template <int ROUNDS>
 __device__ __forceinline__ int64_t sort_at(int round) {
-  return int64_t(blockIdx.x) * kSortItems + (threadIdx.x >> 5) * (32 * kRounds) + 32 * round + (threadIdx.x & 31);
+  return int64_t(blockIdx.x) * (kSortThreads * ROUNDS) + (threadIdx.x >> 5) * (32 * ROUNDS) + 32 * round + (threadIdx.x & 31);
 }
 
-__global__ void __launch_bounds__(kSortThreads) histogram_kernel(const SortPass s, uint32_t* clear, int clear_words) {
+template <int ROUNDS>
+__global__ void __launch_bounds__(kSortThreads) histogram_kernel(const SortPass s, uint32_t* clear, int64_t clear_words) {
   __shared__ uint32_t count[kMaxBins];
-  for (int b = threadIdx.x; b < s.bins; b += kSortThreads) count[b] = 0;
+  const int bins = 1 << s.digit;
+  for (int b = threadIdx.x; b < bins; b += kSortThreads) count[b] = 0;
   wait_for_launch_before();
   let_next_launch_start();
-  for (int i = blockIdx.x * kSortThreads + threadIdx.x; i < clear_words; i += gridDim.x * kSortThreads) clear[i] = 0u;
+  for (int64_t i = int64_t(blockIdx.x) * kSortThreads + threadIdx.x; i < clear_words; i += int64_t(gridDim.x) * kSortThreads) clear[i] = 0u;
+  if (int(blockIdx.x) >= s.blocks) return;
   __syncthreads();
 #pragma unroll
-  for (int r = 0; r < kRounds; ++r) {
-    const int64_t i = sort_at(r);
-    const uint32_t digit = i < s.n ? (sort_item(s, i).x >> s.shift) & (s.bins - 1) : kMaxBins;
+  for (int r = 0; r < ROUNDS; ++r) {
+    const int64_t i = sort_at<ROUNDS>(r);
+    const uint32_t digit = i < s.n ? (sort_item(s, i).x >> s.shift) & (bins - 1) : kMaxBins;
     const uint32_t same = __match_any_sync(0xFFFFFFFFu, digit);
     if (digit < kMaxBins && __ffs(same) - 1 == int(threadIdx.x & 31)) atomicAdd(&count[digit], __popc(same));
   }
   __syncthreads();
-  for (int b = threadIdx.x; b < s.bins; b += kSortThreads) s.table[int64_t(blockIdx.x) * s.bins + b] = count[b];
+  for (int b = threadIdx.x; b < bins; b += kSortThreads) s.table[int64_t(blockIdx.x) * bins + b] = count[b];
 }
 
 // Where every digit of this block's warps goes: the items of smaller digits, those of the blocks before, of the warps before.
+template <int ROUNDS>
 __global__ void __launch_bounds__(kSortThreads) scatter_kernel(const SortPass s) {
   extern __shared__ uint32_t place[];   // [warp][bins]
   __shared__ uint32_t warp_sums[kSortWarps];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int b = threadIdx.x; b < kSortWarps * s.bins; b += kSortThreads) place[b] = 0u;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, bins = 1 << s.digit;
+  for (int b = threadIdx.x; b < kSortWarps * bins; b += kSortThreads) place[b] = 0u;
   wait_for_launch_before();
   let_next_launch_start();
   __syncthreads();
-  uint2 item[kRounds];
-  uint32_t same[kRounds];
+  uint2 item[ROUNDS];
+  uint32_t same[ROUNDS];
 #pragma unroll
-  for (int r = 0; r < kRounds; ++r) {
-    const int64_t i = sort_at(r);
+  for (int r = 0; r < ROUNDS; ++r) {
+    const int64_t i = sort_at<ROUNDS>(r);
     item[r] = i < s.n ? sort_item(s, i) : make_uint2(0u, 0xFFFFFFFFu);   // no token has that number
   }
-  auto digit_of = [&](uint2 x) { return x.y == 0xFFFFFFFFu ? uint32_t(kMaxBins) : (x.x >> s.shift) & (s.bins - 1); };
-#pragma unroll
-  for (int r = 0; r < kRounds; ++r) {
-    const uint32_t digit = digit_of(item[r]);
-    same[r] = __match_any_sync(0xFFFFFFFFu, digit);
-    if (digit < kMaxBins && __ffs(same[r]) - 1 == lane) place[warp * s.bins + digit] += __popc(same[r]);
-    __syncwarp();
-  }
-  __syncthreads();
   // thread b (bins <= kSortThreads): all items of digit b, and those of the blocks before this one
   const int b = threadIdx.x;
   uint32_t all = 0, before = 0;
-  if (b < s.bins) {
-#pragma unroll 8
+  if (b < bins) {
+#pragma unroll 16
     for (int k = 0; k < s.blocks; ++k) {
-      const uint32_t c = __ldcg(s.table + int64_t(k) * s.bins + b);
+      const uint32_t c = __ldcg(s.table + int64_t(k) * bins + b);
       all += c;
       if (k < int(blockIdx.x)) before += c;
     }
+  }
+  auto digit_of = [&](uint2 x) { return x.y == 0xFFFFFFFFu ? uint32_t(kMaxBins) : (x.x >> s.shift) & (bins - 1); };
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
+    const uint32_t digit = digit_of(item[r]);
+    same[r] = __match_any_sync(0xFFFFFFFFu, digit);
+    if (digit < kMaxBins && __ffs(same[r]) - 1 == lane) place[warp * bins + digit] += __popc(same[r]);
+    __syncwarp();
   }
   uint32_t x = all;
 #pragma unroll
@@ -150,125 +160,78 @@ __global__ void __launch_bounds__(kSortThreads) scatter_kernel(const SortPass s)
     warp_sums[lane] = w;
   }
   __syncthreads();
-  if (b < s.bins) {
+  if (b < bins) {
     uint32_t at = x - all + (warp ? warp_sums[warp - 1] : 0u) + before;
-    for (int w = 0; w < kSortWarps; ++w) {
-      const uint32_t c = place[w * s.bins + b];
-      place[w * s.bins + b] = at;
-      at += c;
+#pragma unroll
+    for (int w0 = 0; w0 < kSortWarps; w0 += 8) {
+      uint32_t c[8];
+#pragma unroll
+      for (int w = 0; w < 8; ++w) c[w] = place[(w0 + w) * bins + b];
+#pragma unroll
+      for (int w = 0; w < 8; ++w) {
+        place[(w0 + w) * bins + b] = at;
+        at += c[w];
+      }
     }
   }
   __syncthreads();
 #pragma unroll
-  for (int r = 0; r < kRounds; ++r) {
+  for (int r = 0; r < ROUNDS; ++r) {
     const uint32_t digit = digit_of(item[r]);
     const bool live = digit < kMaxBins, leader = __ffs(same[r]) - 1 == lane;
-    const uint32_t at = live ? place[warp * s.bins + digit] : 0u;
+    const uint32_t first = live ? place[warp * bins + digit] : 0u;
     __syncwarp();
+    const uint32_t at = first + __popc(same[r] & ((1u << lane) - 1u));
     if (live) {
-      s.out[at + __popc(same[r] & ((1u << lane) - 1u))] = item[r];
-      if (leader) place[warp * s.bins + digit] = at + __popc(same[r]);
+      s.out[at] = item[r];
+      if (leader) place[warp * bins + digit] = first + __popc(same[r]);
     }
     __syncwarp();
+    if (s.next_table) {   // counts, whose order does not matter
+      const uint32_t cell = live ? at / (kSortThreads * ROUNDS) * bins + ((item[r].x >> (s.shift + s.digit)) & (bins - 1)) : kNone;
+      const uint32_t peers = __match_any_sync(0xFFFFFFFFu, cell);
+      if (live && __ffs(peers) - 1 == lane) atomicAdd(s.next_table + cell, __popc(peers));
+    }
     if (s.present && live && item[r].x < s.vocab) atomicOr(s.present + (item[r].x >> 5), 1u << (item[r].x & 31u));
   }
 }
 
 // ------------------------------------------------------------------------------------------------------------------- sums
-constexpr int kRun = 32;            // sorted tokens, or rows of the level below, per block
+constexpr int kRun = 32;            // sorted tokens per block
+constexpr int kJoin = 32;           // blocks of a level whose rows are summed together in the next
 constexpr int kSumThreads = 128;
 constexpr int kFillRows = 16;       // rows of the table per block that looks after absent words
+constexpr int kMaxLevels = 8;       // 32^8 tokens and more
 
-// What a level sums: rows of `src` named by `order`, sorted by word.  It leaves two rows per block: what its first word has there, if that
-// word began before, and what its last word has there, if that goes on behind (a word that does both is in the first).
-struct Level {
-  const uint2* order;        // first level: (word, token); later ones: null
-  const uint32_t* words;     // later levels: the word of each row below, or kNone
-  int64_t n;                 // rows
-  float* part;               // [block][2][d]
-  uint32_t* part_word;       // [block][2]
-  uint32_t vocab;
+// Block i of a level leaves up to two rows of sums: of its first word, if that began before the block, and of its last, if that
+// goes on behind.  A word that does both is in the first row.  With them the words: word[2 i] or kNone, word[2 i + 1] or kNone,
+// or kGoesOn there if the first row's word goes on behind.
+constexpr uint32_t kGoesOn = 0xFFFFFFFEu;
+struct Levels {
+  int count;                 // levels; the last has one block, which leaves nothing
+  int blocks[kMaxLevels];
+  float* part[kMaxLevels];          // [block][2][d]
+  uint32_t* word[kMaxLevels];       // [column block][block][2]
+  uint32_t* arrived[kMaxLevels];    // [column block][block / kJoin], zeros at the start
 };
-constexpr uint32_t kNone = 0xFFFFFFFFu;
 
-template <typename S, typename G>
-__global__ void __launch_bounds__(kSumThreads) sum_kernel(const Level l, const S* __restrict__ src, G* __restrict__ dE, int d, float scale, float beta,
-                                                          int run_blocks, const uint32_t* __restrict__ present, int64_t vocab_rows) {
-  __shared__ uint32_t word[kRun + 2];   // with a neighbour on either side
-  __shared__ uint32_t token[kRun];
-  wait_for_launch_before();
-  let_next_launch_start();
-  const int col = (blockIdx.y * kSumThreads + threadIdx.x) * 8;
-  if (int(blockIdx.x) >= run_blocks) {
-    // words that do not occur
-    const int64_t row0 = int64_t(int(blockIdx.x) - run_blocks) * kFillRows;
-    const uint32_t bits = __ldcg(present + (row0 >> 5)) >> (row0 & 31);
-    if (col >= d) return;
-#pragma unroll 4
-    for (int r = 0; r < kFillRows; ++r) {
-      if (row0 + r >= vocab_rows || ((bits >> r) & 1u)) continue;
-      G* at = dE + (row0 + r) * d + col;
-      float2 v[4] = {};
-      if (beta != 0.f) {
-        load8(at, v);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = q8::mul2(v[k], q8::both(beta));
-      }
-      store8(at, v);
-    }
-    return;
-  }
-  const int64_t i0 = int64_t(blockIdx.x) * kRun;
-  const int count = int(min(int64_t(kRun), l.n - i0));
-  const bool top = l.part == nullptr;     // the last level: one block, nothing on either side
-  for (int k = threadIdx.x; k < kRun + 2; k += kSumThreads) {
-    const int64_t i = i0 + k - 1;
-    uint32_t w = kNone;
-    if (i >= 0 && i < l.n) {
-      if (l.order) {
-        const uint2 o = __ldcg(l.order + i);
-        w = o.x < l.vocab ? o.x : kNone;
-        if (k >= 1 && k <= kRun) token[k - 1] = o.y;
-      } else {
-        w = __ldcg(l.words + i);
-        if (k >= 1 && k <= kRun) token[k - 1] = uint32_t(i);
-      }
-    }
-    word[k] = w;
-  }
-  __syncthreads();
-  // Rows below without a word are holes; a run's neighbours are the words next to it that are none.  In the first level there are
-  // holes at the end only; in later ones a hole beside the border may hide the neighbour, so the search goes on from there.
-  uint32_t prev = word[0], next = word[count + 1];
-  if (!l.order) {
-    for (int64_t i = i0 - 2; prev == kNone && i >= 0 && i >= i0 - 4; --i) prev = __ldcg(l.words + i);
-    for (int64_t i = i0 + count + 1; next == kNone && i < l.n && i <= i0 + count + 3; ++i) next = __ldcg(l.words + i);
-  }
-  uint32_t first = kNone, last = kNone;
-  for (int k = 0; k < count; ++k) {
-    const uint32_t w = word[k + 1];
-    if (w != kNone) {
-      if (first == kNone) first = w;
-      last = w;
-    }
-  }
-  const bool from_before = first != kNone && first == prev, goes_on = last != kNone && last == next;
-  if (!top && blockIdx.y == 0 && threadIdx.x < 2)
-    l.part_word[2 * int64_t(blockIdx.x) + threadIdx.x] =
-        threadIdx.x == 0 ? (from_before ? first : kNone) : (goes_on && !(from_before && last == first) ? last : kNone);
-  if (col >= d) return;
-  float2 sum[4] = {};
-  uint32_t current = kNone;
-  auto flush = [&]() {
+template <typename G>
+struct Sink {
+  G* dE;
+  float* part;               // this block's two rows, null: the last level
+  int d, col;
+  float scale, beta;
+  uint32_t first, last;      // words whose sums go there (kNone: none)
+  float2 sum[4];
+  uint32_t current;
+
+  __device__ __forceinline__ void flush() {
     if (current == kNone) return;
-    float2 v[4];
-    const bool head = from_before && current == first, tail = goes_on && current == last;
-    if (!top && (head || tail)) {
-      store8(l.part + (2 * int64_t(blockIdx.x) + (head ? 0 : 1)) * d + col, sum);
+    if (current == first || current == last) {
+      store8(part + (current == first ? 0 : d) + col, sum);
     } else {
       G* at = dE + int64_t(current) * d + col;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = make_float2(0.f, 0.f);
+      float2 v[4] = {};
       if (beta != 0.f) {
         load8(at, v);
 #pragma unroll
@@ -280,31 +243,160 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const Level l, const S
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) sum[k] = make_float2(0.f, 0.f);
-  };
-  constexpr int kAhead = 8;
+  }
+};
+__device__ __forceinline__ void staged(const uint4* p, __nv_bfloat16, float2 (&v)[4]) {
+  q8::Raw<__nv_bfloat16> r;
+  r.u = *p;
+  r.get(v);
+}
+__device__ __forceinline__ void staged(const uint4* p, float, float2 (&v)[4]) {
+  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + kSumThreads);
+  v[0] = make_float2(a.x, a.y); v[1] = make_float2(a.z, a.w);
+  v[2] = make_float2(b.x, b.y); v[3] = make_float2(b.z, b.w);
+}
+// Rows src[row[k]], k < count, with words that are sorted; those with kNone or kGoesOn are not there.  A thread copies its eight columns
+// of many rows into its own places of shared memory before it adds the first: one trip to memory for a run of 32 rows in bf16, two in
+// fp32, and a loop that is short (with eight rows at a time in registers, unrolled, the kernel spilled and the code of the sums'
+// ends was 18 times there: 69 us for 5003 x 1000 fp32 with 32003 words).
+constexpr int kStage = 64 << 10;   // bytes of a block: three blocks per SM
+template <typename S, typename G>
+__device__ __forceinline__ void sum_rows(Sink<G>& sink, const S* src, const uint32_t* word, const uint32_t* row, int count, uint8_t* stage) {
+  constexpr int kPieces = int(sizeof(S)) / 2, kAhead = kStage / (kSumThreads * 16 * kPieces);
+  uint4* const mine = reinterpret_cast<uint4*>(stage) + threadIdx.x;
+  const uint32_t at = uint32_t(__cvta_generic_to_shared(mine));
+  sink.current = kNone;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) sink.sum[k] = make_float2(0.f, 0.f);
   for (int k0 = 0; k0 < count; k0 += kAhead) {
-    q8::Raw<S> x[kAhead];
+    const int rows = min(kAhead, count - k0);
+    for (int k = 0; k < rows; ++k) {
+      if (word[k0 + k] >= kGoesOn) continue;
+      const uint8_t* from = reinterpret_cast<const uint8_t*>(src + int64_t(row[k0 + k]) * sink.d + sink.col);
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      x[k].zero();
-      if (k0 + k < count && word[k0 + k + 1] != kNone) x[k].load(src + int64_t(token[k0 + k]) * d + col);
+      for (int h = 0; h < kPieces; ++h)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + (k * kPieces + h) * (kSumThreads * 16)), "l"(from + 16 * h) : "memory");
     }
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      if (k0 + k >= count) break;
-      const uint32_t w = word[k0 + k + 1];
-      if (w == kNone) continue;
-      if (w != current) {
-        flush();
-        current = w;
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    for (int k = 0; k < rows; ++k) {
+      const uint32_t w = word[k0 + k];
+      if (w >= kGoesOn) continue;
+      if (w != sink.current) {
+        sink.flush();
+        sink.current = w;
       }
       float2 v[4];
-      x[k].get(v);
+      staged(mine + k * kPieces * kSumThreads, S(), v);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) sum[q] = q8::add2(sum[q], v[q]);
+      for (int q = 0; q < 4; ++q) sink.sum[q] = q8::add2(sink.sum[q], v[q]);
     }
   }
-  flush();
+  sink.flush();
+}
+
+template <typename S, typename G>
+__global__ void __launch_bounds__(kSumThreads) sum_kernel(const Levels levels, const uint2* __restrict__ order, int64_t tokens, uint32_t vocab,
+                                                          const S* __restrict__ src, G* __restrict__ dE, int d, float scale, float beta,
+                                                          const uint32_t* __restrict__ present) {
+  extern __shared__ __align__(16) uint8_t stage[];
+  __shared__ uint32_t word[2 * kJoin + 2];
+  __shared__ uint32_t row[2 * kJoin];
+  __shared__ bool finished;
+  static_assert(kRun <= 2 * kJoin && 2 * kJoin <= kSumThreads, "one thread per row");
+  wait_for_launch_before();
+  let_next_launch_start();
+  Sink<G> sink;
+  sink.col = (blockIdx.y * kSumThreads + threadIdx.x) * 8;
+  sink.d = d;
+  const int run_blocks = levels.blocks[0];
+  if (int(blockIdx.x) >= run_blocks) {
+    // words that do not occur
+    const int64_t row0 = int64_t(int(blockIdx.x) - run_blocks) * kFillRows;
+    const uint32_t bits = __ldcg(present + (row0 >> 5)) >> (row0 & 31);
+    if (sink.col >= d) return;
+#pragma unroll 4
+    for (int r = 0; r < kFillRows; ++r) {
+      if (row0 + r >= int64_t(vocab) || ((bits >> r) & 1u)) continue;
+      G* at = dE + (row0 + r) * d + sink.col;
+      float2 v[4] = {};
+      if (beta != 0.f) {
+        load8(at, v);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = q8::mul2(v[k], q8::both(beta));
+      }
+      store8(at, v);
+    }
+    return;
+  }
+  sink.dE = dE;
+  sink.scale = scale;
+  sink.beta = beta;
+  const int64_t i0 = int64_t(blockIdx.x) * kRun;
+  int count = int(min(int64_t(kRun), tokens - i0));
+  // the words of the run, with a neighbour on either side: word[-1] is word[2 kJoin + 1] here
+  for (int k = threadIdx.x; k < count + 2; k += kSumThreads) {
+    const int64_t i = i0 + k - 1;
+    uint32_t w = kNone;
+    if (i >= 0 && i < tokens) {
+      const uint2 o = __ldcg(order + i);
+      w = o.x < vocab ? o.x : kNone;
+      if (k >= 1 && k <= count) row[k - 1] = o.y;
+    }
+    word[k == 0 ? 2 * kJoin + 1 : k - 1] = w;
+  }
+  __syncthreads();
+  int live = count;   // ids outside the vocabulary are last
+  while (live > 0 && word[live - 1] == kNone) --live;
+  bool from_before = live > 0 && word[0] == word[2 * kJoin + 1], goes_on = live == count && word[count - 1] == word[count];
+  uint32_t first = live > 0 ? word[0] : kNone, last = live > 0 ? word[live - 1] : kNone;
+  int block = blockIdx.x;
+  for (int level = 0;; ++level) {
+    const bool top = level + 1 == levels.count;
+    const int64_t pair = 2 * int64_t(block);
+    uint32_t* const left = levels.word[level] + 2 * int64_t(blockIdx.y) * levels.blocks[level];
+    sink.part = top ? nullptr : levels.part[level] + pair * d;
+    sink.first = !top && from_before ? first : kNone;
+    sink.last = !top && goes_on ? last : kNone;
+    if (sink.col < d) {
+      if (level == 0) sum_rows(sink, src, word, row, count, stage);
+      else sum_rows(sink, static_cast<const float*>(levels.part[level - 1]), word, row, count, stage);
+    }
+    if (top) return;
+    if (threadIdx.x == 0) {
+      left[pair] = sink.first;
+      left[pair + 1] = sink.last == kNone ? kNone : sink.last == sink.first ? kGoesOn : sink.last;
+    }
+    // the block that is the last of its group to come here sums the group's rows
+    __threadfence();
+    __syncthreads();
+    const int group = block / kJoin, members = min(kJoin, levels.blocks[level] - group * kJoin);
+    if (threadIdx.x == 0)
+      finished = atomicAdd(levels.arrived[level] + int64_t(blockIdx.y) * levels.blocks[level + 1] + group, 1u) == uint32_t(members - 1);
+    __syncthreads();
+    if (!finished) return;
+    __threadfence();
+    block = group;
+    count = 2 * members;
+    if (int(threadIdx.x) < count) {
+      const int64_t i = int64_t(group) * (2 * kJoin) + threadIdx.x;
+      word[threadIdx.x] = __ldcg(left + i);
+      row[threadIdx.x] = uint32_t(i);
+    }
+    __syncthreads();
+    // The first row that is there: one of a word from before is the group's first block's, as the block before its own would have
+    // left a row too.  The last one likewise.
+    int f = 0, l = count - 1;
+    while (f < count && word[f] >= kGoesOn) ++f;
+    while (l >= 0 && word[l] >= kGoesOn) --l;
+    first = last = kNone;
+    from_before = goes_on = false;
+    if (l >= 0) {
+      first = word[f];
+      last = word[l];
+      from_before = (f & 1) == 0;
+      goes_on = (l & 1) == 1 || word[l + 1] == kGoesOn;
+    }
+  }
 }
 
 // A whole table times beta: a batch without tokens.
@@ -325,52 +417,98 @@ size_t aligned(size_t n) { return (n + 255) & ~size_t(255); }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 struct Plan {
-  int passes, digit, blocks;
-  size_t items[2], table, present, part[2], part_word[2], bytes;
+  int passes, digit, rounds, blocks, columns, levels;
+  int64_t level_blocks[kMaxLevels];
+  size_t items[2], table, part[kMaxLevels], word[kMaxLevels];
+  size_t clear, present, next_table, arrived[kMaxLevels], clear_end;   // zeros for the first launch to write
+  size_t bytes;
 };
 Plan plan_of(const EmbedProblem& q) {
-  Plan p;
+  Plan p{};
   int bits = 1;
   while ((int64_t(1) << bits) <= q.vocab) ++bits;   // keys 0 .. vocab
   p.passes = (bits + kMaxDigit - 1) / kMaxDigit;
   p.digit = (bits + p.passes - 1) / p.passes;
-  p.blocks = int(ceil_div(q.tokens, kSortItems));
+  p.rounds = q.tokens <= int64_t(kFewBlocks) * kSortThreads ? 1 : kManyRounds;
+  p.blocks = int(ceil_div(q.tokens, kSortThreads * p.rounds));
+  p.columns = int(ceil_div(q.d, kSumThreads * 8));
+  p.levels = 1;
+  p.level_blocks[0] = ceil_div(q.tokens, kRun);
+  while (p.level_blocks[p.levels - 1] > 1) {
+    p.level_blocks[p.levels] = ceil_div(p.level_blocks[p.levels - 1], kJoin);
+    ++p.levels;
+  }
   size_t at = 0;
   auto take = [&](size_t n) { const size_t here = at; at += aligned(n); return here; };
   for (size_t& i : p.items) i = take(size_t(q.tokens) * 8);
-  p.table = take(size_t(p.blocks) * (size_t(1) << p.digit) * 4);
-  p.present = take(size_t(q.vocab / 32 + 2) * 4);
-  int64_t n = ceil_div(q.tokens, kRun);   // blocks of the level that leaves these rows
-  for (int k = 0; k < 2; ++k) {
-    p.part[k] = take(size_t(n) * 2 * size_t(q.d) * 4);
-    p.part_word[k] = take(size_t(n) * 2 * 4);
-    n = ceil_div(2 * n, kRun);
+  p.table = take(size_t(p.blocks) << (p.digit + 2));
+  for (int k = 0; k + 1 < p.levels; ++k) {
+    p.part[k] = take(size_t(p.level_blocks[k]) * 2 * size_t(q.d) * 4);
+    p.word[k] = take(size_t(p.level_blocks[k]) * 2 * size_t(p.columns) * 4);
   }
+  p.clear = at;
+  p.present = take(size_t(q.vocab / 32 + 2) * 4);
+  p.next_table = take((size_t(p.blocks) << (p.digit + 2)) * size_t(p.passes - 1));
+  for (int k = 0; k + 1 < p.levels; ++k) p.arrived[k] = take(size_t(p.level_blocks[k + 1]) * size_t(p.columns) * 4);
+  p.clear_end = at;
   p.bytes = at;
   return p;
 }
 
 template <typename S, typename G>
-cudaError_t sums(const EmbedProblem& q, const Plan& p, const uint2* order, const S* dY, G* dE, float beta, uint8_t* ws, cudaStream_t st) {
-  const unsigned cols = unsigned(ceil_div(q.d, kSumThreads * 8));
-  const uint32_t* present = reinterpret_cast<const uint32_t*>(ws + p.present);
+cudaError_t sums(const EmbedProblem& q, const Plan& p, const uint2* order, const void* dY, void* dE, float beta, uint8_t* ws, cudaStream_t st) {
+  static DeviceOnce once;
+  if (once.needed()) {
+    const cudaError_t e = cudaFuncSetAttribute(sum_kernel<S, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStage);
+    if (e != cudaSuccess) return e;
+    once.done();
+  }
+  Levels l{};
+  l.count = p.levels;
+  for (int k = 0; k < p.levels; ++k) {
+    l.blocks[k] = int(p.level_blocks[k]);
+    if (k + 1 == p.levels) break;
+    l.part[k] = reinterpret_cast<float*>(ws + p.part[k]);
+    l.word[k] = reinterpret_cast<uint32_t*>(ws + p.word[k]);
+    l.arrived[k] = reinterpret_cast<uint32_t*>(ws + p.arrived[k]);
+  }
   const int64_t fill = beta == 1.f ? 0 : ceil_div(q.vocab, kFillRows);
-  int64_t blocks = ceil_div(q.tokens, kRun);
-  Level l{order, nullptr, q.tokens, nullptr, nullptr, uint32_t(q.vocab)};
-  auto leave = [&](int level) {
-    l.part = blocks > 1 ? reinterpret_cast<float*>(ws + p.part[level & 1]) : nullptr;
-    l.part_word = reinterpret_cast<uint32_t*>(ws + p.part_word[level & 1]);
-  };
-  leave(0);
-  cudaError_t e = launch_lined_up(sum_kernel<S, G>, dim3(unsigned(blocks + fill), cols), dim3(kSumThreads), 0, st, l, dY, dE, int(q.d), q.scale, beta,
-                                  int(blocks), present, q.vocab);
-  for (int level = 1; e == cudaSuccess && blocks > 1; ++level) {
-    const float* src = l.part;
-    l = Level{nullptr, l.part_word, 2 * blocks, nullptr, nullptr, uint32_t(q.vocab)};
-    blocks = ceil_div(l.n, kRun);
-    leave(level);
-    e = launch_lined_up(sum_kernel<float, G>, dim3(unsigned(blocks), cols), dim3(kSumThreads), 0, st, l, src, dE, int(q.d), q.scale, beta, int(blocks),
-                        present, q.vocab);
+  return launch_lined_up(sum_kernel<S, G>, dim3(unsigned(p.level_blocks[0] + fill), unsigned(p.columns)), dim3(kSumThreads), kStage, st, l, order, q.tokens,
+                         uint32_t(q.vocab), static_cast<const S*>(dY), static_cast<G*>(dE), int(q.d), q.scale, beta,
+                         reinterpret_cast<const uint32_t*>(ws + p.present));
+}
+
+template <int ROUNDS>
+cudaError_t sort(const EmbedProblem& q, const Plan& p, const int64_t* ids, uint8_t* ws, const uint2** order, cudaStream_t st) {
+  static DeviceOnce once;
+  if (once.needed()) {
+    const cudaError_t e = cudaFuncSetAttribute(scatter_kernel<ROUNDS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortWarps * kMaxBins * 4);
+    if (e != cudaSuccess) return e;
+    once.done();
+  }
+  uint2* items[2] = {reinterpret_cast<uint2*>(ws + p.items[0]), reinterpret_cast<uint2*>(ws + p.items[1])};
+  SortPass s{};
+  s.ids = ids;
+  s.out = items[0];
+  s.table = reinterpret_cast<uint32_t*>(ws + p.table);
+  s.n = q.tokens;
+  s.vocab = uint32_t(q.vocab);
+  s.digit = p.digit;
+  s.blocks = p.blocks;
+  const int64_t clear_words = int64_t(p.clear_end - p.clear) / 4;
+  const unsigned grid = unsigned(std::max<int64_t>(p.blocks, std::min<int64_t>(kFewBlocks, clear_words / (4 * kSortThreads))));
+  cudaError_t e = launch_lined_up(histogram_kernel<ROUNDS>, dim3(grid), dim3(kSortThreads), 0, st, s, reinterpret_cast<uint32_t*>(ws + p.clear), clear_words);
+  for (int k = 0; k < p.passes && e == cudaSuccess; ++k) {
+    uint32_t* const next = reinterpret_cast<uint32_t*>(ws + p.next_table) + (size_t(p.blocks) << p.digit) * size_t(k);
+    s.next_table = k + 1 < p.passes ? next : nullptr;
+    s.present = k + 1 == p.passes ? reinterpret_cast<uint32_t*>(ws + p.present) : nullptr;
+    e = launch_lined_up(scatter_kernel<ROUNDS>, dim3(unsigned(p.blocks)), dim3(kSortThreads), size_t(kSortWarps) << (p.digit + 2), st, s);
+    *order = s.out;
+    s.ids = nullptr;
+    s.in = s.out;
+    s.out = items[(k & 1) ^ 1];
+    s.table = next;
+    s.shift += p.digit;
   }
   return e;
 }
@@ -405,39 +543,12 @@ cudaError_t embed_bwd(const EmbedProblem& q, const int64_t* ids, const void* dY,
   }
   const Plan p = plan_of(q);
   uint8_t* w8 = static_cast<uint8_t*>(ws);
-  uint2* items[2] = {reinterpret_cast<uint2*>(w8 + p.items[0]), reinterpret_cast<uint2*>(w8 + p.items[1])};
-  uint32_t* present = reinterpret_cast<uint32_t*>(w8 + p.present);
-  SortPass s{};
-  s.table = reinterpret_cast<uint32_t*>(w8 + p.table);
-  s.n = q.tokens;
-  s.vocab = uint32_t(q.vocab);
-  s.bins = 1 << p.digit;
-  s.blocks = p.blocks;
-  const int smem = kSortWarps * s.bins * 4;
-  static DeviceOnce once;
-  if (once.needed()) {
-    const cudaError_t e = cudaFuncSetAttribute(scatter_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortWarps * kMaxBins * 4);
-    if (e != cudaSuccess) return e;
-    once.done();
-  }
-  for (int k = 0; k < p.passes; ++k) {
-    s.ids = k == 0 ? ids : nullptr;
-    s.in = items[(k & 1) ^ 1];
-    s.out = items[k & 1];
-    s.shift = k * p.digit;
-    s.present = k + 1 == p.passes ? present : nullptr;
-    cudaError_t e = launch_lined_up(histogram_kernel, dim3(unsigned(p.blocks)), dim3(kSortThreads), 0, st, s, present,
-                                    k == 0 ? int(q.vocab / 32 + 2) : 0);
-    if (e == cudaSuccess) e = launch_lined_up(scatter_kernel, dim3(unsigned(p.blocks)), dim3(kSortThreads), size_t(smem), st, s);
-    if (e != cudaSuccess) return e;
-  }
-  const uint2* order = items[(p.passes - 1) & 1];
-  if (q.bf16) {
-    const __nv_bfloat16* g = static_cast<const __nv_bfloat16*>(dY);
-    return q.grad_bf16 ? sums(q, p, order, g, static_cast<__nv_bfloat16*>(dE), beta, w8, st) : sums(q, p, order, g, static_cast<float*>(dE), beta, w8, st);
-  }
-  const float* g = static_cast<const float*>(dY);
-  return q.grad_bf16 ? sums(q, p, order, g, static_cast<__nv_bfloat16*>(dE), beta, w8, st) : sums(q, p, order, g, static_cast<float*>(dE), beta, w8, st);
+  const uint2* order = nullptr;
+  const cudaError_t e = p.rounds == 1 ? sort<1>(q, p, ids, w8, &order, st) : sort<kManyRounds>(q, p, ids, w8, &order, st);
+  if (e != cudaSuccess) return e;
+  if (q.bf16)
+    return q.grad_bf16 ? sums<__nv_bfloat16, __nv_bfloat16>(q, p, order, dY, dE, beta, w8, st) : sums<__nv_bfloat16, float>(q, p, order, dY, dE, beta, w8, st);
+  return q.grad_bf16 ? sums<float, __nv_bfloat16>(q, p, order, dY, dE, beta, w8, st) : sums<float, float>(q, p, order, dY, dE, beta, w8, st);
 }
 
 }  // namespace acx

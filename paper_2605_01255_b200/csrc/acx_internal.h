@@ -53,7 +53,7 @@ struct EmbedProblem {
 struct GradProblem {
   int64_t tensors, chunks;
 };
-constexpr int64_t kGradChunk = 8192;   // elements of a tensor that a block scales at a time
+constexpr int64_t kGradChunk = 16384;   // elements of a tensor that a block scales at a time
 
 // Device-side status word values (written by kernels whose bounded waits expire).
 constexpr int kDevOk = 0;

@@ -1,5 +1,8 @@
 // C ABI of attention, the embedding table and gradient clipping: argument checks and dispatch.
+#include <algorithm>
 #include <cmath>
+#include <exception>
+#include <vector>
 
 #include "acx_checks.h"
 #include "acx_internal.h"
@@ -45,6 +48,29 @@ acx_status validate_embed(const acx_embed_desc* d, EmbedProblem* out) {
   out->grad_bf16 = d->grad_dtype == ACX_BF16;
   out->scale = d->scale;
   return ACX_OK;
+}
+
+// Whether a tensor that is written shares memory with another one, or with its own source other than in place: blocks work on the
+// tensors in any order.
+bool outputs_overlap(const acx_grad* list, int64_t count) {
+  struct Range { uintptr_t begin, end; bool written; };
+  std::vector<Range> ranges;
+  ranges.reserve(size_t(2 * count));
+  for (int64_t i = 0; i < count; ++i) {
+    const acx_grad& g = list[i];
+    if (g.n == 0) continue;
+    const uintptr_t src = reinterpret_cast<uintptr_t>(g.src), dst = reinterpret_cast<uintptr_t>(g.dst);
+    ranges.push_back(Range{dst, dst + uintptr_t(g.n) * (g.dst_dtype == ACX_BF16 ? 2 : 4), true});
+    if (src != dst) ranges.push_back(Range{src, src + uintptr_t(g.n) * (g.src_dtype == ACX_BF16 ? 2 : 4), false});
+  }
+  std::sort(ranges.begin(), ranges.end(), [](const Range& a, const Range& b) { return a.begin < b.begin; });
+  uintptr_t written_to = 0, read_to = 0;   // ends of the ranges so far
+  for (const Range& r : ranges) {
+    if (r.begin < written_to || (r.written && r.begin < read_to)) return true;
+    uintptr_t& to = r.written ? written_to : read_to;
+    to = std::max(to, r.end);
+  }
+  return false;
 }
 
 acx_status validate_grad(const acx_grad_desc* d, GradProblem* out) {
@@ -165,6 +191,11 @@ acx_status acx_grad_describe(const acx_grad* list, int64_t count, acx_grad_desc*
     chunks += (g.n + kGradChunk - 1) / kGradChunk;
   }
   if (chunks > (int64_t(1) << 31)) return ACX_ERR_UNSUPPORTED_SHAPE;
+  try {
+    if (outputs_overlap(list, count)) return ACX_ERR_INVALID_ARG;
+  } catch (const std::exception&) {   // no memory on the host for the ranges
+    return ACX_ERR_CUDA;
+  }
   desc->struct_size = sizeof(acx_grad_desc);
   desc->reserved = 0;
   desc->tensors = count;
