@@ -397,19 +397,24 @@ ACX_API size_t acx_attn_workspace_bytes(const acx_attn_desc* desc, int op);
  *      the first and behind the last document (padding) belong to none: their o, dq, dk and dv are zero, their lse minus infinity, and
  *      nothing of their q, k, v, dO reaches another token, whatever it is.  Documents without a token are fine.
  *   prefix [docs] int32, device, or NULL (none): the first prefix[i] tokens of document i are seen by all of its tokens; causal only.
- *   plan: device memory of acx_attn_workspace_bytes(desc, ACX_OP_ATTN_PLAN) bytes, out. */
+ *   plan: device memory of acx_attn_workspace_bytes(desc, ACX_OP_ATTN_PLAN) bytes, out.  A call that is given another plan than one
+ *      with its tokens, docs and causal writes nothing; acx_last_device_status then returns ACX_ERR_INVALID_ARG. */
 ACX_API acx_status acx_attn_plan(const acx_attn_desc* desc, const int32_t* offsets, const int32_t* prefix, void* plan, size_t plan_bytes,
                                  void* cuda_stream);
 
 /*   Q [tokens][heads][head_dim], K, V [tokens][kv_heads][head_dim] in;  slopes [heads] fp32 or NULL: no bias;
  *   O [tokens][heads][head_dim] out;  lse [heads][tokens] fp32, out, or NULL: log of the sum of exp(z), for the backward.
+ * Scores that the mask takes out may be anything.  Values of a document's own tokens have to be finite, though: a weight of zero
+ * times a NaN or an infinity is a NaN, for any query within 127 tokens before such a one.
  * Scores and sums are fp32; the probabilities enter the second product rounded to bfloat16, as dS = p (dP - delta) does in the
  * backward; every output is rounded once. */
 ACX_API acx_status acx_attn_fwd(const acx_attn_desc* desc, const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv,
                                 const float* slopes, const void* plan, size_t plan_bytes, void* O, int64_t ldo, float* lse, void* cuda_stream);
 
 /* Gradients of the forward at Q, K, V (the same plan, slopes and descriptor; O and lse as it left them).
- *   dO [tokens][heads][head_dim] in;  dQ, dK, dV out, shaped as Q, K, V;  ws/ws_bytes: ACX_OP_ATTN_BWD.
+ *   dO [tokens][heads][head_dim] in;  dQ, dK, dV out, shaped as Q, K, V, none of them in the place of an input;  ws/ws_bytes:
+ *   ACX_OP_ATTN_BWD.
+ * The probabilities are taken from lse again, to 2^-22 |lse| relative: scores far beyond some 10^4 have no gradients of use.
  * Fixed summation order, no atomics: reproducible bits. */
 ACX_API acx_status acx_attn_bwd(const acx_attn_desc* desc, const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv,
                                 const float* slopes, const void* plan, size_t plan_bytes, const void* O, int64_t ldo, const void* dO, int64_t lddo,
@@ -470,7 +475,8 @@ ACX_API acx_status acx_grad_clip(const acx_grad_desc* desc, const void* plan, si
                                  size_t ws_bytes, void* cuda_stream);
 
 /* Synchronises the stream and returns ACX_ERR_TIMEOUT if any kernel on this device since the last call gave up on
- * a bounded wait (its outputs are then undefined), ACX_ERR_CUDA on a CUDA error, else ACX_OK.  Clears the flag.  The
+ * a bounded wait (its outputs are then undefined), ACX_ERR_INVALID_ARG if one found a plan of another batch's sizes,
+ * ACX_ERR_CUDA on a CUDA error, else ACX_OK.  Clears the flag.  The
  * flag is one word per device: a kernel on any stream sets it, so the answer is about the device, not only about
  * `cuda_stream` (which is the stream that is synchronised first). */
 ACX_API acx_status acx_last_device_status(void* cuda_stream);

@@ -338,7 +338,7 @@ acx_status acx_last_device_status(void* cuda_stream) {
   if (v != kDevOk) {
     const int zero = 0;
     if (cudaMemcpyToSymbol(g_device_status, &zero, sizeof(int)) != cudaSuccess) return ACX_ERR_CUDA;
-    return ACX_ERR_TIMEOUT;
+    return v == kDevBadInput ? ACX_ERR_INVALID_ARG : ACX_ERR_TIMEOUT;
   }
   return ACX_OK;
 }

@@ -39,7 +39,9 @@ struct PlanHeader {
   int tiles;         // items of 128 tokens (backward, both lists)
   int head_end;      // tokens [0, head_end) and [tail_begin, tokens) belong to no document
   int tail_begin;
+  int tokens, docs, causal, unused;   // what it was made for
 };
+static_assert(sizeof(PlanHeader) == 32, "two loads");
 constexpr size_t kPlanListOffset = 256;
 struct PlanLayout {
   int64_t wide_cap, tile_cap;
@@ -59,7 +61,7 @@ __host__ __device__ inline PlanLayout plan_layout(int64_t tokens, int64_t docs) 
 }
 
 struct Params {
-  int tokens, heads, kv_heads, group;
+  int tokens, docs, heads, kv_heads, group;
   int d;                     // columns of a head
   int causal;
   const PlanHeader* plan;
@@ -214,6 +216,15 @@ __device__ __forceinline__ void store_f32(float* at, const uint32_t (&v)[32], fl
       for (int k = 0; k < 4; ++k) q[k] = make_float2(__uint_as_float(v[8 * i + 2 * k]) * f, __uint_as_float(v[8 * i + 2 * k + 1]) * f);
       q8::store8(at + 8 * i, q);
     }
+}
+
+// Whether the plan is one for this descriptor: any other (never written, of another batch's sizes) would name tokens that are not
+// there.  If not, nothing is done, and the device's status word says so.
+__device__ __forceinline__ bool plan_fits(const Params& p) {
+  const int4 made = __ldcg(reinterpret_cast<const int4*>(p.plan) + 1);
+  const bool fits = made.x == p.tokens && made.y == p.docs && made.z == p.causal;
+  if (!fits && blockIdx.x == 0 && threadIdx.x == 0) atomicExch(p.status, kDevBadInput);
+  return fits;
 }
 
 // Rows that belong to no document: zeros (all threads of the grid; row r of `heads` heads of d columns, stride ld).

@@ -178,7 +178,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   wait_for_launch_before();
   let_next_launch_start();
   const int per_tile = KEYS ? p.kv_heads * p.parts : p.heads;
-  const int units = __ldcg(&p.plan->tiles) * per_tile;
+  const bool fits = plan_fits(p);
+  const int units = fits ? __ldcg(&p.plan->tiles) * per_tile : 0;
   auto give_up = [&]() {
     *abort_flag = 1;
     atomicExch(p.status, kDevTimeout);
@@ -572,7 +573,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   }
   __syncwarp();
-  if (KEYS) {
+  if (!fits) {
+    // nothing
+  } else if (KEYS) {
     zero_rows_outside(p, p.dK, p.lddk, p.kv_heads, nullptr, 0.f);
     zero_rows_outside(p, p.dV, p.lddv, p.kv_heads, nullptr, 0.f);
   } else {
@@ -592,6 +595,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 __global__ void __launch_bounds__(256) attn_join_kernel(const Params p) {
   wait_for_launch_before();
   let_next_launch_start();
+  if (!plan_fits(p)) return;
   const int head_end = __ldcg(&p.plan->head_end), tail = __ldcg(&p.plan->tail_begin);
   const int per_row = p.kv_heads * (p.d / 8);
   const int64_t n = int64_t(p.tokens) * per_row, k = int64_t(blockIdx.x) * blockDim.x + threadIdx.x;

@@ -94,6 +94,10 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int* __restric
     PlanHeader* header = reinterpret_cast<PlanHeader*>(plan);
     if (list == 0) {
       header->wide = count;
+      header->tokens = tokens;
+      header->docs = docs;
+      header->causal = causal;
+      header->unused = 0;
       const int first = docs > 0 ? clamped(0) : tokens;
       header->head_end = first;
       header->tail_begin = docs > 0 ? max(clamped(docs), first) : tokens;
@@ -224,7 +228,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
   auto tmem_o = [&](int h) { return tmem + 256u + HD * h; };
   wait_for_launch_before();
   let_next_launch_start();
-  const int units = __ldcg(&p.plan->wide) * p.heads;
+  const bool fits = plan_fits(p);
+  const int units = fits ? __ldcg(&p.plan->wide) * p.heads : 0;
   auto give_up = [&]() {
     *abort_flag = 1;
     atomicExch(p.status, kDevTimeout);
@@ -369,7 +374,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
         __syncwarp();
         const int k0 = t.start + j * kRows;
         constexpr bool kRaw = !CAP && !BIAS;   // raw scores: the scale is left to the exponent's fma
-        const float scale = kRaw ? p.c : 1.f;
+        float scale = kRaw ? p.c : 1.f;
         if (CAP) {
           auto capped = [&](auto is_small) {
 #pragma unroll
@@ -420,13 +425,33 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
           for (int i = 2; i < 32; i += 2) top[c] = max_nan(top[c], __uint_as_float(s[c][i]), __uint_as_float(s[c][i + 1]));
         }
         const float mx = max_nan(max_nan(top[0], top[1], top[2]), top[3]) * scale;
+        // The fma takes a rounded maximum from an exact product: off by 2^-24 |mx|, which is 2^-12 at 2^12 and anything for scores of
+        // a mask's size.  Rows beyond round the products too.
+        if (kRaw) {
+          const bool large = fabsf(mx) > 4096.f;
+          if (__any_sync(0xFFFFFFFFu, large)) {
+            const float2 f = q8::both(large ? p.c : 1.f);
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+              for (int i = 0; i < 32; i += 2) {
+                const float2 x = q8::mul2(make_float2(__uint_as_float(s[c][i]), __uint_as_float(s[c][i + 1])), f);
+                s[c][i] = __float_as_uint(x.x);
+                s[c][i + 1] = __float_as_uint(x.y);
+              }
+            if (large) scale = 1.f;
+          }
+        }
         // the products with the P before are done: P's place is free, and the sums may be rescaled
         if (!warp_wait(p_free(half), (turns & 1) ^ 1u, abort_flag)) { give_up(); ok = false; break; }
+        // (a score that is not a number: the row's sums become that.  A row's reference is its own affair, the warp only goes along:
+        // rows behind the document's end, of another document, change nothing of the others' roundings.)
+        const bool above = row < t.end && !(mx <= m + 8.f);
         if (j == n - 1) {
           m = mx;
-        } else if (__any_sync(0xFFFFFFFFu, !(mx <= m + 8.f))) {   // (or not a number, which then the row's sums become)
+        } else if (__any_sync(0xFFFFFFFFu, above)) {
           ptx::tcgen05_fence_after_sync();
-          const float m_new = max_nan(m, mx), f = exp2_fast(m - m_new);
+          const float m_new = above ? max_nan(m, mx) : m, f = above ? exp2_fast(m - m_new) : 1.f;
           m = m_new;
           l *= f;
 #pragma unroll 1
@@ -491,7 +516,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
     }
   }
   __syncwarp();
-  zero_rows_outside(p, p.O, p.ldo, p.heads, p.lse, __int_as_float(0xFF800000));
+  if (fits) zero_rows_outside(p, p.O, p.ldo, p.heads, p.lse, __int_as_float(0xFF800000));
   __syncwarp();
   ptx::tcgen05_fence_before_sync();
   __syncthreads();
@@ -524,6 +549,7 @@ cudaError_t launch_fwd(bool cap, bool bias, const CUtensorMap& q, const CUtensor
 Params common_params(const AttnProblem& q, const void* plan, const float* slopes, float* lse, int* status) {
   Params p{};
   p.tokens = int(q.tokens);
+  p.docs = int(q.docs);
   p.heads = q.heads;
   p.kv_heads = q.kv_heads;
   p.group = q.heads / q.kv_heads;

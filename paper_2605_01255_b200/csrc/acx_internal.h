@@ -58,6 +58,7 @@ constexpr int64_t kGradChunk = 16384;   // elements of a tensor that a block sca
 // Device-side status word values (written by kernels whose bounded waits expire).
 constexpr int kDevOk = 0;
 constexpr int kDevTimeout = 1;
+constexpr int kDevBadInput = 2;   // device memory that a call was given does not hold what it has to
 
 // Counts every kernel launch the library makes (reported by acx_kernel_launches()).
 inline std::atomic<unsigned long long>& kernel_launch_counter() {

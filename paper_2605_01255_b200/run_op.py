@@ -1,11 +1,13 @@
 """Run one call of the library a few times on random inputs: the command to profile a single kernel.
 
-    python -m paper_2605_01255_b200.run_op {fwd,fwd_nows,fwd_plain,fwd_v,dx,factor,reconstruct,reconstruct_v,adamw,lowrank_adamw,rsvd,factor_bias,q8,swiglu,norm_join,linear_ce} tokens,d_in,d_out,r [launches] [f32|bf16]
+    python -m paper_2605_01255_b200.run_op {fwd,fwd_nows,fwd_plain,fwd_v,dx,factor,reconstruct,reconstruct_v,adamw,lowrank_adamw,rsvd,factor_bias,q8,swiglu,norm_join,linear_ce,attention,embed,grad_clip} tokens,d_in,d_out,r [launches] [f32|bf16]
 
 `fwd_nows` is the forward without a workspace (the sketch generated inside the GEMM), `fwd_plain` the forward of a linear
 whose input's factor another linear stores (XS = NULL); `dx` and `factor` are acx_linear_bwd with the other output left out.
 `q8` (store, then load) and `norm_join` work on tokens x d_in, `swiglu` on tokens x d_out, `linear_ce` takes d = d_in and a
-vocabulary of d_out (any number); those four run forward and backward and do not read r.  Prints "ok" after checking the
+vocabulary of d_out (any number); those four run forward and backward and do not read r.  `attention` has d_in / r query heads of r
+columns, a quarter of them (or one) for keys and values, in documents of 1 to 1023 tokens; `embed` looks tokens x d_in up in d_out
+words, and both run forward and backward; `grad_clip` takes the factors [d_out x r] of 24 linears.  Prints "ok" after checking the
 device status word.  Inputs come from torch.randn on the device (values do not matter for a profile).
 """
 from __future__ import annotations
@@ -17,7 +19,7 @@ import torch
 from . import binding as B
 
 
-def _q8(m, d_in, d_out, tdt):
+def _q8(m, d_in, d_out, r, tdt):
     d, X, q = B.make_rows_desc(m, d_in, tdt), torch.randn(m, d_in, device="cuda").to(tdt), B.q8_empty(m, d_in)
     Y = torch.empty_like(X)
 
@@ -27,7 +29,7 @@ def _q8(m, d_in, d_out, tdt):
     return run
 
 
-def _swiglu(m, d_in, d_out, tdt):
+def _swiglu(m, d_in, d_out, r, tdt):
     d = B.make_rows_desc(m, d_out, tdt)
     G, U, dH = (torch.randn(m, d_out, device="cuda").to(tdt) for _ in range(3))
     H, dG, dU = (torch.empty_like(G) for _ in range(3))
@@ -39,7 +41,7 @@ def _swiglu(m, d_in, d_out, tdt):
     return run
 
 
-def _norm_join(m, d_in, d_out, tdt):
+def _norm_join(m, d_in, d_out, r, tdt):
     d = B.make_rows_desc(m, d_in, tdt)
     h, b, dy, dn = (torch.randn(m, d_in, device="cuda").to(tdt) for _ in range(4))
     w = torch.ones(d_in, device="cuda").to(tdt)
@@ -55,7 +57,7 @@ def _norm_join(m, d_in, d_out, tdt):
     return run
 
 
-def _linear_ce(m, d_in, d_out, tdt):
+def _linear_ce(m, d_in, d_out, r, tdt):
     d = B.make_ce_desc(m, d_in, d_out)
     X, W = torch.randn(m, d_in, device="cuda").bfloat16(), (torch.randn(d_out, d_in, device="cuda") * d_in ** -0.5).bfloat16()
     y = torch.randint(0, d_out, (m,), device="cuda")
@@ -69,7 +71,46 @@ def _linear_ce(m, d_in, d_out, tdt):
     return run
 
 
-BETWEEN = {"q8": _q8, "swiglu": _swiglu, "norm_join": _norm_join, "linear_ce": _linear_ce}
+def _attention(m, d_in, d_out, r, tdt):
+    heads = d_in // r
+    kv = heads // 4 if heads % 4 == 0 else 1
+    cuts, i = [0], 0
+    while cuts[-1] < m:
+        cuts.append(min(m, cuts[-1] + 1 + i * 389 % 1023))
+        i += 1
+    d = B.make_attn_desc(m, heads, kv, r, len(cuts) - 1)
+    offsets, plan = torch.tensor(cuts, dtype=torch.int32, device="cuda"), B.alloc_attn_workspace(d, B.ACX_OP_ATTN_PLAN)
+    Q, K, V, dO = (torch.randn(m, h, r, device="cuda").bfloat16() for h in (heads, kv, kv, heads))
+    O, dQ, dK, dV = (torch.empty_like(t) for t in (Q, Q, K, V))
+    lse, ws = torch.empty(heads, m, device="cuda"), B.alloc_attn_workspace(d, B.ACX_OP_ATTN_BWD)
+
+    def run():
+        B.acx_attn_plan(d, offsets, plan)
+        B.acx_attn_fwd(d, Q, K, V, plan, O, lse)
+        B.acx_attn_bwd(d, Q, K, V, plan, O, dO, lse, dQ, dK, dV, ws=ws)
+    return run
+
+
+def _embed(m, d_in, d_out, r, tdt):
+    d = B.make_embed_desc(m, d_in, d_out, tdt, torch.float32)
+    E, ids, dY = torch.randn(d_out, d_in, device="cuda").to(tdt), torch.randint(0, d_out, (m,), device="cuda"), torch.randn(m, d_in, device="cuda").to(tdt)
+    Y, dE, ws = torch.empty_like(dY), torch.empty(d_out, d_in, device="cuda"), B.alloc_embed_workspace(d, B.ACX_OP_EMBED_BWD)
+
+    def run():
+        B.acx_embed_fwd(d, ids, E, Y)
+        B.acx_embed_bwd(d, ids, dY, dE, ws=ws)
+    return run
+
+
+def _grad_clip(m, d_in, d_out, r, tdt):
+    factors = [torch.randn(d_out, r, device="cuda") for _ in range(24)]
+    grads = B.make_grad_list(factors, [d_in / r] * len(factors))
+    total, ws = torch.empty(2, device="cuda"), B.alloc_grad_workspace(grads)
+    return lambda: B.acx_grad_clip(grads, 1.0, total, ws=ws)
+
+
+BETWEEN = {"q8": _q8, "swiglu": _swiglu, "norm_join": _norm_join, "linear_ce": _linear_ce, "attention": _attention, "embed": _embed,
+           "grad_clip": _grad_clip}
 
 
 def finish(run=None, launches: int = 0) -> int:
@@ -94,7 +135,7 @@ def main(argv) -> int:
     tdt = torch.bfloat16 if dtype == "bf16" else torch.float32
     dev = "cuda"
     if op in BETWEEN:
-        return finish(BETWEEN[op](m, d_in, d_out, tdt), launches)
+        return finish(BETWEEN[op](m, d_in, d_out, r, tdt), launches)
     d = B.make_desc(m, d_in, d_out, r, 0, dtype)
     X = torch.randn(m, d_in, device=dev).to(tdt)
     W = (torch.randn(d_out, d_in, device=dev) * 0.02).to(tdt)
