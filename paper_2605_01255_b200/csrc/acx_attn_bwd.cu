@@ -9,8 +9,10 @@
 //     S = R0 T0^T,   dP = R1 T1^T,   first += P T,   second += dS T0.
 // For keys `first` is dV (T = dO) and `second` dK.  For queries `second` is dQ, and `first` = P K corrects it: O rounded to bf16
 // gives delta to within that rounding only, and an error e of delta is one of -e P K in dQ, which was as large as the rounding of dS and dQ
-// together (errors of dQ 0.0029 relative to its size, 0.0024 with it).  So dS is taken with the delta that O gives, r_i = sum of
-// p (dP - delta) summed in fp32 beside it, and dQ = scale (second - r first); delta + r is what the launch for the keys uses.
+// together (errors of dQ 0.0029 relative to its size without it).  So dS is taken with the delta that O gives, r_i = sum of
+// p (dP - delta) summed in fp32 beside it, delta + r is what the launch for the keys uses, and dQ = scale (second - r' first) with
+// the sum r' of the dS as they were rounded: exact ones sum to zero, so r' is e and what the roundings leave of the keys' mean (errors
+// of dQ 0.00245 with r, 0.0023 with r', where the keys have a mean; the rounding of dS and of dQ themselves make 0.0023).
 // The price of two launches is that S and dP are computed twice: eight products instead of five.
 //
 // S, dP, first and second fill the tensor memory (4 x 128 columns); dS goes over dP as bf16 and is multiplied from there, P goes to shared
@@ -18,6 +20,10 @@
 // waited 1600 of 3900 cycles a tile).  Sixteen warps share a tile, 32 rows x 32 columns each.
 //
 // A query that sees one key only has p = 1 and no gradient through its scores: exactly zero, not the difference of two roundings.
+//
+// Of a few tokens (kFewTokens) dS goes into dK as two bf16 parts, the rounded one and what is left: nothing averages out between so few
+// queries, and a launch of that size is all latency.  Errors of dK 0.0023 to 0.0025 -> 0.0017, its own rounding; the backward of 256 tokens
+// x 14 heads x 64 20.2 -> 20.5 us, 512 x 8 x 64 23.7 -> 24.7, but 2048 x 6 x 128 80 -> 85 and 8192 x 24 x 128 1323 -> 1434.
 //
 // Where a batch has few key tiles for the SMs a group's query heads are dealt to several work items, whose fp32 sums a last kernel adds
 // in a fixed order.
@@ -35,6 +41,7 @@ namespace {
 constexpr int kRowWarp0 = 4, kRowWarps = 16, kThreads = 32 * (kRowWarp0 + kRowWarps);
 constexpr int kPanel = 32;        // columns of a tile that one warp takes
 constexpr int kPanels = kRows / kPanel;
+constexpr int kFewTokens = 512;
 
 // ------------------------------------------------------------------------------------------------------------------ delta
 // delta[head][token] = sum of dO O over the head's columns.  Sixteen lanes per row.
@@ -89,7 +96,7 @@ struct Smem {
   static constexpr int kP = (2 + kT0 + kT1) * Tile<HD>::kBytes, kPBytes = kRows * kRows * 2;
   static constexpr int kVec = kP + kPBytes;
   static constexpr int kVecStages = KEYS ? 2 : 0, kVecBytes = 2 * kRows * 4;   // KEYS: lse and delta of a tile of queries
-  static constexpr int kPartBytes = kPanels / 2 * kRows * 4;
+  static constexpr int kPartBytes = kPanels / 2 * kRows * 8;
   static constexpr int kExchange = kVec + kVecStages * kVecBytes;              // else: partial sums of the rows
   static constexpr int kBars = kExchange + (KEYS ? 0 : kPartBytes), kBytes = kBars + 256;
   static_assert(kBytes <= 232448, "shared memory of one CTA");
@@ -294,6 +301,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!wait(ds_full, turns & 1)) break;
         ptx::tcgen05_fence_after_sync();
         rows_mma<HD, 16>(tmem_second, tmem_dp, t0_tiles + a.stage * T::kBytes, steps, d16, i > 0);
+        if (KEYS && p.two_parts) rows_mma<HD, 16>(tmem_second, tmem_dp + 16, t0_tiles + a.stage * T::kBytes, steps, d16, true);
         ptx::umma_commit_elected(t0_empty(a.stage));
         if (i == n - 1) ptx::umma_commit_elected(out_full);
         if (i + 1 < n) {
@@ -372,7 +380,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       // KEYS: the document's first query sees one key only; else: this row does
       const bool lonely = KEYS ? w.t.end - w.t.start == 1 || (p.causal && w.t.prefix <= w.t.start + 1) : last - w.t.start == 1;
       float lse2 = 0.f, delta = 0.f;
-      float2 rest2 = make_float2(0.f, 0.f);
+      float2 rest2 = make_float2(0.f, 0.f), kept2 = rest2;   // sums of p (dP - delta), and of what dS's rounding makes of them
       if (!KEYS) {
         const int64_t at = int64_t(w.head) * p.tokens + row;
         lse2 = live ? __ldcg(p.lse + at) * kLog2e : 0.f;
@@ -401,7 +409,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int lo = first - c0, hi = last - c0;
           // dx/ds of the cap, as fp16: 2^-12 of it is little beside the rounding of dS
           __half2 slopes[CAP ? 16 : 1];
-          uint32_t pk[16];
+          uint32_t pk[16], low[16];
           auto probabilities = [&](auto with_mask, auto is_small) {
             constexpr bool kMask = decltype(with_mask)::value, kSmall = decltype(is_small)::value;
 #pragma unroll
@@ -433,6 +441,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               for (int k = 0; k < 4; ++k) {
                 const int col = 4 * i4 + k;
                 if (kMask) e[k] = col >= lo && col < hi ? e[k] : 0.f;
+                if (CAP && kMask) slope[k] = col >= lo && col < hi ? slope[k] : 0.f;   // that of another document's tokens may be no number
                 s[col] = __float_as_uint(e[k]);
                 if (CAP && !KEYS) e[k] *= slope[k];   // what an error of delta is multiplied with
               }
@@ -488,8 +497,20 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             pk[2 * i4] = pack2(e0.x, e0.y);
             pk[2 * i4 + 1] = pack2(e1.x, e1.y);
+            if (KEYS && p.two_parts) {
+              const float2 l0 = q8::add2(e0, neg2(unpack2(pk[2 * i4]))), l1 = q8::add2(e1, neg2(unpack2(pk[2 * i4 + 1])));
+              low[2 * i4] = pack2(l0.x, l0.y);
+              low[2 * i4 + 1] = pack2(l1.x, l1.y);
+            }
+            if (!KEYS) {
+              const float2 r0 = unpack2(pk[2 * i4]), r1 = unpack2(pk[2 * i4 + 1]);
+              // with a cap, whose slopes are in e by now, the roundings alone
+              if (CAP) kept2 = q8::add2(kept2, q8::add2(q8::add2(r0, neg2(e0)), q8::add2(r1, neg2(e1))));
+              else kept2 = q8::add2(kept2, q8::add2(r0, r1));
+            }
           }
           ptx::tmem_st_x16(dp_at, pk);
+          if (KEYS && p.two_parts) ptx::tmem_st_x16(dp_at + 16, low);
           ptx::tmem_st_wait();
           ptx::tcgen05_fence_before_sync();
           __syncwarp();
@@ -503,26 +524,27 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!ok) break;
       if (!KEYS) {
         // r of the row: the panels' parts, [0] + [2] and [1] + [3] first (room for two)
-        float rest = rest2.x + rest2.y;
-        float* part = reinterpret_cast<float*>(gen + M::kExchange);
+        float2 rest = make_float2(rest2.x + rest2.y, kept2.x + kept2.y);
+        if (CAP) rest.y += rest.x;
+        float2* part = reinterpret_cast<float2*>(gen + M::kExchange);
         if (!warp_wait(parts_free, (it & 1) ^ 1u, abort_flag)) { give_up(); break; }   // those of the item before have been read
         if (panel < 2) part[panel * kRows + r] = rest;
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(parts_full);
         __syncwarp();
         if (!warp_wait(parts_full, 0u, abort_flag)) { give_up(); break; }
-        if (panel >= 2) part[(panel - 2) * kRows + r] += rest;
+        if (panel >= 2) part[(panel - 2) * kRows + r] = q8::add2(part[(panel - 2) * kRows + r], rest);
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(parts_full);
         __syncwarp();
         if (!warp_wait(parts_full, 1u, abort_flag)) { give_up(); break; }
-        rest = part[r] + part[kRows + r];
+        rest = q8::add2(part[r], part[kRows + r]);
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(parts_free);
         __syncwarp();
-        if (panel == 0 && live) p.delta[int64_t(w.head) * p.tokens + row] = delta + rest;
+        if (panel == 0 && live) p.delta[int64_t(w.head) * p.tokens + row] = delta + rest.x;
         __syncwarp();
-        rest2.x = rest;
+        rest2.x = rest.y;
       }
       if (!warp_wait(out_full, it & 1, abort_flag)) { give_up(); break; }
       ptx::tcgen05_fence_after_sync();
@@ -697,6 +719,7 @@ cudaError_t attn_bwd(const AttnProblem& q, const AttnMatrix& Q, const AttnMatrix
   pk.items = reinterpret_cast<const Item*>(plan8 + at.keys);
   const unsigned grid_q = unsigned(std::min<int64_t>(at.tile_cap * q.heads, sm_count()));
   const unsigned grid_k = unsigned(std::min<int64_t>(at.tile_cap * q.kv_heads * kp.parts, sm_count()));
+  pk.two_parts = q.tokens <= kFewTokens;
   const bool cap = q.softcap > 0.f, bias = slopes != nullptr;
   e = q.d <= 64 ? launch_both<64>(cap, bias, m, p, grid_q, pk, grid_k, st) : launch_both<128>(cap, bias, m, p, grid_q, pk, grid_k, st);
   if (e != cudaSuccess || kp.parts == 1) return e;
