@@ -409,7 +409,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int lo = first - c0, hi = last - c0;
           // dx/ds of the cap, as fp16: 2^-12 of it is little beside the rounding of dS
           __half2 slopes[CAP ? 16 : 1];
-          uint32_t pk[16], low[16];
+          uint32_t pk[16];
           auto probabilities = [&](auto with_mask, auto is_small) {
             constexpr bool kMask = decltype(with_mask)::value, kSmall = decltype(is_small)::value;
 #pragma unroll
@@ -497,10 +497,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             pk[2 * i4] = pack2(e0.x, e0.y);
             pk[2 * i4 + 1] = pack2(e1.x, e1.y);
-            if (KEYS && p.two_parts) {
-              const float2 l0 = q8::add2(e0, neg2(unpack2(pk[2 * i4]))), l1 = q8::add2(e1, neg2(unpack2(pk[2 * i4 + 1])));
-              low[2 * i4] = pack2(l0.x, l0.y);
-              low[2 * i4 + 1] = pack2(l1.x, l1.y);
+            if (KEYS) {
+              s[4 * i4] = __float_as_uint(e0.x);
+              s[4 * i4 + 1] = __float_as_uint(e0.y);
+              s[4 * i4 + 2] = __float_as_uint(e1.x);
+              s[4 * i4 + 3] = __float_as_uint(e1.y);
             }
             if (!KEYS) {
               const float2 r0 = unpack2(pk[2 * i4]), r1 = unpack2(pk[2 * i4 + 1]);
@@ -510,7 +511,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
           ptx::tmem_st_x16(dp_at, pk);
-          if (KEYS && p.two_parts) ptx::tmem_st_x16(dp_at + 16, low);
+          if (KEYS && p.two_parts) {   // what the rounding left
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float2 l = q8::add2(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), neg2(unpack2(pk[i])));
+              pk[i] = pack2(l.x, l.y);
+            }
+            ptx::tmem_st_x16(dp_at + 16, pk);
+          }
           ptx::tmem_st_wait();
           ptx::tcgen05_fence_before_sync();
           __syncwarp();
