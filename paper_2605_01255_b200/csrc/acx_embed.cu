@@ -79,6 +79,18 @@ __device__ __forceinline__ uint2 sort_item(const SortPass& s, int64_t i) {
   const int64_t id = __ldcg(reinterpret_cast<const long long*>(s.ids) + i);
   return make_uint2(id >= 0 && id < int64_t(s.vocab) ? uint32_t(id) : s.vocab, uint32_t(i));
 }
+// The lanes of `among` whose v has this lane's lowest bits: a vote per bit (the instruction that matches whole words takes a turn for
+// every word that differs: 22 us for a sort of 5003 tokens, MEASURED with votes).
+__device__ __forceinline__ uint32_t lanes_with(uint32_t v, int bits, uint32_t among) {
+#pragma unroll
+  for (int b = 0; b < kMaxDigit; ++b) {
+    if (b >= bits) break;
+    const bool mine = (v >> b) & 1u;
+    const uint32_t set = __ballot_sync(0xFFFFFFFFu, mine);
+    among &= mine ? set : ~set;
+  }
+  return among;
+}
 // A warp has 32 * ROUNDS items in a row.
 template <int ROUNDS>
 __device__ __forceinline__ int64_t sort_at(int round) {
@@ -98,50 +110,18 @@ __global__ void __launch_bounds__(kSortThreads) histogram_kernel(const SortPass 
 #pragma unroll
   for (int r = 0; r < ROUNDS; ++r) {
     const int64_t i = sort_at<ROUNDS>(r);
-    const uint32_t digit = i < s.n ? (sort_item(s, i).x >> s.shift) & (bins - 1) : kMaxBins;
-    const uint32_t same = __match_any_sync(0xFFFFFFFFu, digit);
-    if (digit < kMaxBins && __ffs(same) - 1 == int(threadIdx.x & 31)) atomicAdd(&count[digit], __popc(same));
+    const bool live = i < s.n;
+    const uint32_t digit = live ? (sort_item(s, i).x >> s.shift) & (bins - 1) : 0u;
+    const uint32_t same = lanes_with(digit, s.digit, __ballot_sync(0xFFFFFFFFu, live));
+    if (live && __ffs(same) - 1 == int(threadIdx.x & 31)) atomicAdd(&count[digit], __popc(same));
   }
   __syncthreads();
   for (int b = threadIdx.x; b < bins; b += kSortThreads) s.table[int64_t(blockIdx.x) * bins + b] = count[b];
 }
 
-// Where every digit of this block's warps goes: the items of smaller digits, those of the blocks before, of the warps before.
-template <int ROUNDS>
-__global__ void __launch_bounds__(kSortThreads) scatter_kernel(const SortPass s) {
-  extern __shared__ uint32_t place[];   // [warp][bins]
-  __shared__ uint32_t warp_sums[kSortWarps];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, bins = 1 << s.digit;
-  for (int b = threadIdx.x; b < kSortWarps * bins; b += kSortThreads) place[b] = 0u;
-  wait_for_launch_before();
-  let_next_launch_start();
-  __syncthreads();
-  uint2 item[ROUNDS];
-  uint32_t same[ROUNDS];
-#pragma unroll
-  for (int r = 0; r < ROUNDS; ++r) {
-    const int64_t i = sort_at<ROUNDS>(r);
-    item[r] = i < s.n ? sort_item(s, i) : make_uint2(0u, 0xFFFFFFFFu);   // no token has that number
-  }
-  // thread b (bins <= kSortThreads): all items of digit b, and those of the blocks before this one
-  const int b = threadIdx.x;
-  uint32_t all = 0, before = 0;
-  if (b < bins) {
-#pragma unroll 16
-    for (int k = 0; k < s.blocks; ++k) {
-      const uint32_t c = __ldcg(s.table + int64_t(k) * bins + b);
-      all += c;
-      if (k < int(blockIdx.x)) before += c;
-    }
-  }
-  auto digit_of = [&](uint2 x) { return x.y == 0xFFFFFFFFu ? uint32_t(kMaxBins) : (x.x >> s.shift) & (bins - 1); };
-#pragma unroll
-  for (int r = 0; r < ROUNDS; ++r) {
-    const uint32_t digit = digit_of(item[r]);
-    same[r] = __match_any_sync(0xFFFFFFFFu, digit);
-    if (digit < kMaxBins && __ffs(same[r]) - 1 == lane) place[warp * bins + digit] += __popc(same[r]);
-    __syncwarp();
-  }
+// Adds up `all` over the threads before this one (of all threads of the block; warp_sums: a word per warp).
+__device__ __forceinline__ uint32_t sum_before(uint32_t all, uint32_t* warp_sums) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint32_t x = all;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -160,25 +140,131 @@ __global__ void __launch_bounds__(kSortThreads) scatter_kernel(const SortPass s)
     warp_sums[lane] = w;
   }
   __syncthreads();
-  if (b < bins) {
-    uint32_t at = x - all + (warp ? warp_sums[warp - 1] : 0u) + before;
+  return x - all + (warp ? warp_sums[warp - 1] : 0u);
+}
+// The warps' counts of digit b become their places, from `at` on.
+__device__ __forceinline__ void places_of(uint32_t* place, int bins, int b, uint32_t at) {
 #pragma unroll
-    for (int w0 = 0; w0 < kSortWarps; w0 += 8) {
-      uint32_t c[8];
+  for (int w0 = 0; w0 < kSortWarps; w0 += 8) {
+    uint32_t c[8];
 #pragma unroll
-      for (int w = 0; w < 8; ++w) c[w] = place[(w0 + w) * bins + b];
+    for (int w = 0; w < 8; ++w) c[w] = place[(w0 + w) * bins + b];
 #pragma unroll
-      for (int w = 0; w < 8; ++w) {
-        place[(w0 + w) * bins + b] = at;
-        at += c[w];
-      }
+    for (int w = 0; w < 8; ++w) {
+      place[(w0 + w) * bins + b] = at;
+      at += c[w];
     }
   }
+}
+
+// The whole sort of a few tokens in one block, which keeps the items between the passes.
+constexpr int kOneBlockRounds = 8, kOneBlockTokens = kSortThreads * kOneBlockRounds;
+__global__ void __launch_bounds__(kSortThreads) small_sort_kernel(const SortPass s, int passes, uint32_t* clear, int64_t clear_words) {
+  extern __shared__ uint32_t place[];   // [warp][bins], then the items
+  __shared__ uint32_t warp_sums[kSortWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, bins = 1 << s.digit, n = int(s.n), rounds = (n + kSortThreads - 1) / kSortThreads;
+  uint2* const held = reinterpret_cast<uint2*>(place + kSortWarps * bins);
+  wait_for_launch_before();
+  let_next_launch_start();
+  uint2 item[kOneBlockRounds];
+  uint32_t same[kOneBlockRounds];
+  auto at_of = [&](int r) { return warp * (32 * rounds) + 32 * r + lane; };
+#pragma unroll
+  for (int r = 0; r < kOneBlockRounds; ++r)
+    item[r] = r < rounds && at_of(r) < n ? sort_item(s, at_of(r)) : make_uint2(0u, kNone);   // no token has that number
+  for (int64_t i = threadIdx.x; i < clear_words; i += kSortThreads) clear[i] = 0u;
+  for (int pass = 0; pass < passes; ++pass) {
+    const int shift = pass * s.digit;
+    const bool end = pass + 1 == passes;
+    auto digit_of = [&](uint2 x) { return (x.x >> shift) & (bins - 1); };
+    for (int b = threadIdx.x; b < kSortWarps * bins; b += kSortThreads) place[b] = 0u;
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kOneBlockRounds; ++r) {
+      if (r >= rounds) break;
+      const uint32_t digit = digit_of(item[r]);
+      const bool live = item[r].y != kNone;
+      same[r] = lanes_with(digit, s.digit, __ballot_sync(0xFFFFFFFFu, live));
+      if (live && __ffs(same[r]) - 1 == lane) place[warp * bins + digit] += __popc(same[r]);
+      __syncwarp();
+    }
+    __syncthreads();
+    const int b = threadIdx.x;
+    uint32_t all = 0;
+    if (b < bins) {
+#pragma unroll 8
+      for (int w = 0; w < kSortWarps; ++w) all += place[w * bins + b];
+    }
+    const uint32_t at0 = sum_before(all, warp_sums);
+    if (b < bins) places_of(place, bins, b, at0);
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kOneBlockRounds; ++r) {
+      if (r >= rounds) break;
+      const uint32_t digit = digit_of(item[r]);
+      const bool live = item[r].y != kNone, leader = __ffs(same[r]) - 1 == lane;
+      const uint32_t first = live ? place[warp * bins + digit] : 0u;
+      __syncwarp();
+      if (live) {
+        const uint32_t at = first + __popc(same[r] & ((1u << lane) - 1u));
+        (end ? s.out : held)[at] = item[r];
+        if (leader) place[warp * bins + digit] = first + __popc(same[r]);
+        if (end && item[r].x < s.vocab) atomicOr(s.present + (item[r].x >> 5), 1u << (item[r].x & 31u));
+      }
+      __syncwarp();
+    }
+    if (end) return;
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kOneBlockRounds; ++r)
+      if (r < rounds && at_of(r) < n) item[r] = held[at_of(r)];
+  }
+}
+
+// Where every digit of this block's warps goes: the items of smaller digits, those of the blocks before, of the warps before.
+template <int ROUNDS>
+__global__ void __launch_bounds__(kSortThreads) scatter_kernel(const SortPass s) {
+  extern __shared__ uint32_t place[];   // [warp][bins]
+  __shared__ uint32_t warp_sums[kSortWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, bins = 1 << s.digit;
+  for (int b = threadIdx.x; b < kSortWarps * bins; b += kSortThreads) place[b] = 0u;
+  wait_for_launch_before();
+  let_next_launch_start();
+  __syncthreads();
+  uint2 item[ROUNDS];
+  uint32_t same[ROUNDS];
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
+    const int64_t i = sort_at<ROUNDS>(r);
+    item[r] = i < s.n ? sort_item(s, i) : make_uint2(0u, kNone);   // no token has that number
+  }
+  // thread b (bins <= kSortThreads): all items of digit b, and those of the blocks before this one
+  const int b = threadIdx.x;
+  uint32_t all = 0, before = 0;
+  if (b < bins) {
+#pragma unroll 16
+    for (int k = 0; k < s.blocks; ++k) {
+      const uint32_t c = __ldcg(s.table + int64_t(k) * bins + b);
+      all += c;
+      if (k < int(blockIdx.x)) before += c;
+    }
+  }
+  auto digit_of = [&](uint2 x) { return (x.x >> s.shift) & (bins - 1); };
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
+    const uint32_t digit = digit_of(item[r]);
+    const bool live = item[r].y != kNone;
+    same[r] = lanes_with(digit, s.digit, __ballot_sync(0xFFFFFFFFu, live));
+    if (live && __ffs(same[r]) - 1 == lane) place[warp * bins + digit] += __popc(same[r]);
+    __syncwarp();
+  }
+  const uint32_t smaller = sum_before(all, warp_sums);
+  if (b < bins) places_of(place, bins, b, smaller + before);
   __syncthreads();
 #pragma unroll
   for (int r = 0; r < ROUNDS; ++r) {
     const uint32_t digit = digit_of(item[r]);
-    const bool live = digit < kMaxBins, leader = __ffs(same[r]) - 1 == lane;
+    const bool live = item[r].y != kNone, leader = __ffs(same[r]) - 1 == lane;
     const uint32_t first = live ? place[warp * bins + digit] : 0u;
     __syncwarp();
     const uint32_t at = first + __popc(same[r] & ((1u << lane) - 1u));
@@ -187,10 +273,11 @@ __global__ void __launch_bounds__(kSortThreads) scatter_kernel(const SortPass s)
       if (leader) place[warp * bins + digit] = first + __popc(same[r]);
     }
     __syncwarp();
-    if (s.next_table) {   // counts, whose order does not matter
-      const uint32_t cell = live ? at / (kSortThreads * ROUNDS) * bins + ((item[r].x >> (s.shift + s.digit)) & (bins - 1)) : kNone;
-      const uint32_t peers = __match_any_sync(0xFFFFFFFFu, cell);
-      if (live && __ffs(peers) - 1 == lane) atomicAdd(s.next_table + cell, __popc(peers));
+    if (s.next_table) {   // counts, whose order does not matter; lanes of one digit go to neighbouring places, of two blocks at most
+      const uint32_t block = at / (kSortThreads * ROUNDS), digit2 = (item[r].x >> (s.shift + s.digit)) & (bins - 1);
+      const uint32_t odd = __ballot_sync(0xFFFFFFFFu, block & 1u);
+      const uint32_t peers = lanes_with(digit2, s.digit, same[r] & (block & 1u ? odd : ~odd));
+      if (live && __ffs(peers) - 1 == lane) atomicAdd(s.next_table + block * bins + digit2, __popc(peers));
     }
     if (s.present && live && item[r].x < s.vocab) atomicOr(s.present + (item[r].x >> 5), 1u << (item[r].x & 31u));
   }
@@ -255,8 +342,7 @@ __device__ __forceinline__ void staged(const uint4* p, float, float2 (&v)[4]) {
   v[0] = make_float2(a.x, a.y); v[1] = make_float2(a.z, a.w);
   v[2] = make_float2(b.x, b.y); v[3] = make_float2(b.z, b.w);
 }
-// Rows src[row[k]], k < count, with words that are sorted; those with kNone or kGoesOn are not there.  A thread copies its eight columns
-// of many rows into its own places of shared memory before it adds the first: one trip to memory for a run of 32 rows in bf16, two in
+// Rows src[row[k]], k < count, with words that are sorted.  A thread copies its eight columns of many rows into its own places of shared memory before it adds the first: one trip to memory for a run of 32 rows in bf16, two in
 // fp32, and a loop that is short (with eight rows at a time in registers, unrolled, the kernel spilled and the code of the sums'
 // ends was 18 times there: 69 us for 5003 x 1000 fp32 with 32003 words).
 constexpr int kStage = 64 << 10;   // bytes of a block: three blocks per SM
@@ -270,25 +356,27 @@ __device__ __forceinline__ void sum_rows(Sink<G>& sink, const S* src, const uint
   for (int k = 0; k < 4; ++k) sink.sum[k] = make_float2(0.f, 0.f);
   for (int k0 = 0; k0 < count; k0 += kAhead) {
     const int rows = min(kAhead, count - k0);
+#pragma unroll 4
     for (int k = 0; k < rows; ++k) {
-      if (word[k0 + k] >= kGoesOn) continue;
       const uint8_t* from = reinterpret_cast<const uint8_t*>(src + int64_t(row[k0 + k]) * sink.d + sink.col);
 #pragma unroll
       for (int h = 0; h < kPieces; ++h)
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + (k * kPieces + h) * (kSumThreads * 16)), "l"(from + 16 * h) : "memory");
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
+    uint32_t w = word[k0];
+    float2 v[4];
+    staged(mine, S(), v);
     for (int k = 0; k < rows; ++k) {
-      const uint32_t w = word[k0 + k];
-      if (w >= kGoesOn) continue;
       if (w != sink.current) {
         sink.flush();
         sink.current = w;
       }
-      float2 v[4];
-      staged(mine + k * kPieces * kSumThreads, S(), v);
 #pragma unroll
       for (int q = 0; q < 4; ++q) sink.sum[q] = q8::add2(sink.sum[q], v[q]);
+      const int next = min(k + 1, rows - 1);
+      w = word[k0 + next];
+      staged(mine + next * kPieces * kSumThreads, S(), v);
     }
   }
   sink.flush();
@@ -299,10 +387,12 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const Levels levels, c
                                                           const S* __restrict__ src, G* __restrict__ dE, int d, float scale, float beta,
                                                           const uint32_t* __restrict__ present) {
   extern __shared__ __align__(16) uint8_t stage[];
-  __shared__ uint32_t word[2 * kJoin + 2];
+  __shared__ uint32_t word[2 * kJoin];
   __shared__ uint32_t row[2 * kJoin];
+  __shared__ uint32_t beside[2];
+  __shared__ uint64_t there[2];   // bits: rows of a level that are there, and slots that say kGoesOn
   __shared__ bool finished;
-  static_assert(kRun <= 2 * kJoin && 2 * kJoin <= kSumThreads, "one thread per row");
+  static_assert(kRun <= 2 * kJoin && kJoin == 32 && 2 * kJoin + 2 <= kSumThreads, "one thread per row, two warps");
   wait_for_launch_before();
   let_next_launch_start();
   Sink<G> sink;
@@ -333,22 +423,21 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const Levels levels, c
   sink.beta = beta;
   const int64_t i0 = int64_t(blockIdx.x) * kRun;
   int count = int(min(int64_t(kRun), tokens - i0));
-  // the words of the run, with a neighbour on either side: word[-1] is word[2 kJoin + 1] here
-  for (int k = threadIdx.x; k < count + 2; k += kSumThreads) {
-    const int64_t i = i0 + k - 1;
-    uint32_t w = kNone;
-    if (i >= 0 && i < tokens) {
-      const uint2 o = __ldcg(order + i);
-      w = o.x < vocab ? o.x : kNone;
-      if (k >= 1 && k <= count) row[k - 1] = o.y;
-    }
-    word[k == 0 ? 2 * kJoin + 1 : k - 1] = w;
+  // the words of the run, and by two threads more those on either side
+  const int t = threadIdx.x;
+  const int64_t i = i0 + (t < count ? t : t == 2 * kJoin ? -1 : count);
+  uint32_t w = kNone;
+  if ((t < count || t == 2 * kJoin || t == 2 * kJoin + 1) && i >= 0 && i < tokens) {
+    const uint2 o = __ldcg(order + i);
+    w = o.x < vocab ? o.x : kNone;
+    if (t < count) row[t] = o.y;
   }
-  __syncthreads();
-  int live = count;   // ids outside the vocabulary are last
-  while (live > 0 && word[live - 1] == kNone) --live;
-  bool from_before = live > 0 && word[0] == word[2 * kJoin + 1], goes_on = live == count && word[count - 1] == word[count];
+  if (t < count) word[t] = w;
+  if (t == 2 * kJoin || t == 2 * kJoin + 1) beside[t - 2 * kJoin] = w;
+  const int live = __syncthreads_count(t < count && w != kNone);   // ids outside the vocabulary are last
+  bool from_before = live > 0 && word[0] == beside[0], goes_on = live > 0 && live == count && word[live - 1] == beside[1];
   uint32_t first = live > 0 ? word[0] : kNone, last = live > 0 ? word[live - 1] : kNone;
+  count = live;
   int block = blockIdx.x;
   for (int level = 0;; ++level) {
     const bool top = level + 1 == levels.count;
@@ -376,25 +465,34 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const Levels levels, c
     if (!finished) return;
     __threadfence();
     block = group;
-    count = 2 * members;
-    if (int(threadIdx.x) < count) {
-      const int64_t i = int64_t(group) * (2 * kJoin) + threadIdx.x;
-      word[threadIdx.x] = __ldcg(left + i);
-      row[threadIdx.x] = uint32_t(i);
+    uint32_t mark = kNone;
+    if (t < 2 * members) mark = __ldcg(left + int64_t(group) * (2 * kJoin) + t);
+    if (t < 2 * kJoin) {
+      const uint32_t a = __ballot_sync(0xFFFFFFFFu, mark < kGoesOn), b = __ballot_sync(0xFFFFFFFFu, mark == kGoesOn);
+      if ((t & 31) == 0) {
+        reinterpret_cast<uint32_t*>(&there[0])[t >> 5] = a;
+        reinterpret_cast<uint32_t*>(&there[1])[t >> 5] = b;
+      }
+    }
+    __syncthreads();
+    const uint64_t rows = there[0];
+    if (mark < kGoesOn) {
+      const int at = __popcll(rows & ((uint64_t(1) << t) - 1u));
+      word[at] = mark;
+      row[at] = uint32_t(group * (2 * kJoin) + t);
     }
     __syncthreads();
     // The first row that is there: one of a word from before is the group's first block's, as the block before its own would have
     // left a row too.  The last one likewise.
-    int f = 0, l = count - 1;
-    while (f < count && word[f] >= kGoesOn) ++f;
-    while (l >= 0 && word[l] >= kGoesOn) --l;
+    count = __popcll(rows);
     first = last = kNone;
     from_before = goes_on = false;
-    if (l >= 0) {
-      first = word[f];
-      last = word[l];
-      from_before = (f & 1) == 0;
-      goes_on = (l & 1) == 1 || word[l + 1] == kGoesOn;
+    if (count > 0) {
+      const int l = 63 - __clzll(rows);
+      first = word[0];
+      last = word[count - 1];
+      from_before = ((__ffsll(rows) - 1) & 1) == 0;
+      goes_on = (l & 1) == 1 || ((there[1] >> (l + 1)) & 1u);
     }
   }
 }
@@ -478,6 +576,26 @@ cudaError_t sums(const EmbedProblem& q, const Plan& p, const uint2* order, const
                          reinterpret_cast<const uint32_t*>(ws + p.present));
 }
 
+cudaError_t small_sort(const EmbedProblem& q, const Plan& p, const int64_t* ids, uint8_t* ws, const uint2** order, cudaStream_t st) {
+  constexpr int kMost = kSortWarps * kMaxBins * 4 + kOneBlockTokens * 8;
+  static DeviceOnce once;
+  if (once.needed()) {
+    const cudaError_t e = cudaFuncSetAttribute(small_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+    if (e != cudaSuccess) return e;
+    once.done();
+  }
+  SortPass s{};
+  s.ids = ids;
+  s.out = reinterpret_cast<uint2*>(ws + p.items[0]);
+  s.n = q.tokens;
+  s.vocab = uint32_t(q.vocab);
+  s.digit = p.digit;
+  s.present = reinterpret_cast<uint32_t*>(ws + p.present);
+  *order = s.out;
+  return launch_lined_up(small_sort_kernel, dim3(1), dim3(kSortThreads), (size_t(kSortWarps) << (p.digit + 2)) + size_t(q.tokens) * 8, st, s, p.passes,
+                         reinterpret_cast<uint32_t*>(ws + p.clear), int64_t(p.clear_end - p.clear) / 4);
+}
+
 template <int ROUNDS>
 cudaError_t sort(const EmbedProblem& q, const Plan& p, const int64_t* ids, uint8_t* ws, const uint2** order, cudaStream_t st) {
   static DeviceOnce once;
@@ -544,7 +662,7 @@ cudaError_t embed_bwd(const EmbedProblem& q, const int64_t* ids, const void* dY,
   const Plan p = plan_of(q);
   uint8_t* w8 = static_cast<uint8_t*>(ws);
   const uint2* order = nullptr;
-  const cudaError_t e = p.rounds == 1 ? sort<1>(q, p, ids, w8, &order, st) : sort<kManyRounds>(q, p, ids, w8, &order, st);
+  const cudaError_t e = q.tokens <= kOneBlockTokens ? small_sort(q, p, ids, w8, &order, st) : p.rounds == 1 ? sort<1>(q, p, ids, w8, &order, st) : sort<kManyRounds>(q, p, ids, w8, &order, st);
   if (e != cudaSuccess) return e;
   if (q.bf16)
     return q.grad_bf16 ? sums<__nv_bfloat16, __nv_bfloat16>(q, p, order, dY, dE, beta, w8, st) : sums<__nv_bfloat16, float>(q, p, order, dY, dE, beta, w8, st);
