@@ -159,6 +159,9 @@ static_assert(kBins == kPlanThreads, "one bin per thread");
 
 // ---------------------------------------------------------------------------------------------------------------- forward
 constexpr int kFwdThreads = 384;
+// Work items have 256 queries, whose halves take turns with the products; where that leaves SMs without an item they have 128, and one
+// half of the rows' warps has nothing to do (2048 tokens x 16 heads x 64, 128 items of 256: 30.2 us, 24.1 in items of 128; 3001 x 6 x
+// 72 with a cap 52.9 and 48.6; but 4096 x 14 x 64, 224 items: 54 and 70).
 template <int HD>
 struct FwdSmem {
   static constexpr int kStages = HD == 128 ? 3 : 6;
@@ -229,7 +232,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
   wait_for_launch_before();
   let_next_launch_start();
   const bool fits = plan_fits(p);
-  const int units = fits ? __ldcg(&p.plan->wide) * p.heads : 0;
+  const int units = fits ? __ldcg(p.halves == 2 ? &p.plan->wide : &p.plan->tiles) * p.heads : 0;
   auto give_up = [&]() {
     *abort_flag = 1;
     atomicExch(p.status, kDevTimeout);
@@ -237,7 +240,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
   // key tiles that a half of the queries sees
   auto key_tiles = [&](const Item& t, int half) {
     const int r = t.row0 + kRows * half;
-    if (r >= t.end) return 0;
+    if (half >= p.halves || r >= t.end) return 0;
     return ((p.causal ? max(min(r + kRows, t.end), t.prefix) : t.end) - t.start + kRows - 1) / kRows;
   };
 
@@ -581,14 +584,15 @@ cudaError_t attn_fwd(const AttnProblem& q, const AttnMatrix& Q, const AttnMatrix
                      const AttnMatrix& O, float* lse, int* status, cudaStream_t st) {
   Params p = common_params(q, plan, slopes, lse, status);
   const PlanLayout at = plan_layout(q.tokens, q.docs);
-  p.items = reinterpret_cast<const Item*>(static_cast<const uint8_t*>(plan) + at.wide);
+  p.halves = q.tokens / (2 * kRows) * q.heads > sm_count() ? 2 : 1;
+  p.items = reinterpret_cast<const Item*>(static_cast<const uint8_t*>(plan) + (p.halves == 2 ? at.wide : at.queries));
   p.O = static_cast<__nv_bfloat16*>(O.p);
   p.ldo = O.ld;
   CUtensorMap mq, mk, mv;
   if (!make_tmap_heads(&mq, Q.p, q.tokens, q.heads, q.d, Q.ld, kRows) || !make_tmap_heads(&mk, K.p, q.tokens, q.kv_heads, q.d, K.ld, kRows) ||
       !make_tmap_heads(&mv, V.p, q.tokens, q.kv_heads, q.d, V.ld, kRows))
     return cudaErrorInvalidValue;
-  const unsigned grid = unsigned(std::min<int64_t>(at.wide_cap * q.heads, sm_count()));
+  const unsigned grid = unsigned(std::min<int64_t>((p.halves == 2 ? at.wide_cap : at.tile_cap) * q.heads, sm_count()));
   const bool cap = q.softcap > 0.f, bias = slopes != nullptr;
   return q.d <= 64 ? launch_fwd<64>(cap, bias, mq, mk, mv, p, grid, st) : launch_fwd<128>(cap, bias, mq, mk, mv, p, grid, st);
 }
