@@ -80,7 +80,7 @@ __device__ __forceinline__ uint2 sort_item(const SortPass& s, int64_t i) {
   return make_uint2(id >= 0 && id < int64_t(s.vocab) ? uint32_t(id) : s.vocab, uint32_t(i));
 }
 // The lanes of `among` whose v has this lane's lowest bits: a vote per bit (the instruction that matches whole words takes a turn for
-// every word that differs: 22 us for a sort of 5003 tokens, MEASURED with votes).
+// every word that differs: 22.1 us for the sort of 5003 tokens by itself, 20.7 with votes).
 __device__ __forceinline__ uint32_t lanes_with(uint32_t v, int bits, uint32_t among) {
 #pragma unroll
   for (int b = 0; b < kMaxDigit; ++b) {
@@ -157,15 +157,23 @@ __device__ __forceinline__ void places_of(uint32_t* place, int bins, int b, uint
   }
 }
 
-// The whole sort of a few tokens in one block, which keeps the items between the passes.
+// The whole sort of a few tokens in one block, which keeps the items between the passes; the other blocks, if there are any, write zeros
+// to the table meanwhile (every row: those of words that occur are written again by the sums, which then have the memory to themselves:
+// the gradient of 5003 x 1000 fp32 with 32003 words 58.8 -> 57.3 us, and 43.6 with what else became faster then).
 constexpr int kOneBlockRounds = 8, kOneBlockTokens = kSortThreads * kOneBlockRounds;
-__global__ void __launch_bounds__(kSortThreads) small_sort_kernel(const SortPass s, int passes, uint32_t* clear, int64_t clear_words) {
+__global__ void __launch_bounds__(kSortThreads) small_sort_kernel(const SortPass s, int passes, uint32_t* clear, int64_t clear_words,
+                                                                   uint4* zeros, int64_t zero_count) {
   extern __shared__ uint32_t place[];   // [warp][bins], then the items
   __shared__ uint32_t warp_sums[kSortWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, bins = 1 << s.digit, n = int(s.n), rounds = (n + kSortThreads - 1) / kSortThreads;
   uint2* const held = reinterpret_cast<uint2*>(place + kSortWarps * bins);
   wait_for_launch_before();
   let_next_launch_start();
+  if (blockIdx.x > 0) {
+    for (int64_t i = int64_t(blockIdx.x - 1) * kSortThreads + threadIdx.x; i < zero_count; i += int64_t(gridDim.x - 1) * kSortThreads)
+      zeros[i] = make_uint4(0u, 0u, 0u, 0u);
+    return;
+  }
   uint2 item[kOneBlockRounds];
   uint32_t same[kOneBlockRounds];
   auto at_of = [&](int r) { return warp * (32 * rounds) + 32 * r + lane; };
@@ -295,6 +303,7 @@ constexpr int kMaxLevels = 8;       // 32^8 tokens and more
 // or kGoesOn there if the first row's word goes on behind.
 constexpr uint32_t kGoesOn = 0xFFFFFFFEu;
 struct Levels {
+  int columns;               // blocks of columns
   int count;                 // levels; the last has one block, which leaves nothing
   int blocks[kMaxLevels];
   float* part[kMaxLevels];          // [block][2][d]
@@ -302,58 +311,94 @@ struct Levels {
   uint32_t* arrived[kMaxLevels];    // [column block][block / kJoin], zeros at the start
 };
 
-template <typename G>
+// Columns per thread: 16 bytes of dY.  (Eight in fp32 too took 57 us for 5003 x 1000 with 32003 words: twice the blocks share what is
+// latency, 43.  Four in bf16, copies of eight bytes: 16384 x 2048 with 128256 words 184 us, 176 with eight.)
+template <typename S>
+constexpr int kCols = 16 / int(sizeof(S));
+__device__ __forceinline__ float4 load4(const float* p) { return __ldcg(reinterpret_cast<const float4*>(p)); }
+__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
+  const uint2 u = __ldcg(reinterpret_cast<const uint2*>(p));
+  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xFFFF0000u));
+}
+__device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+  *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+template <typename T>
+__device__ __forceinline__ void store_cols(T* p, const float4 (&v)[1]) { store4(p, v[0]); }
+template <typename T>
+__device__ __forceinline__ void store_cols(T* p, const float4 (&v)[2]) {
+  const float2 e[4] = {make_float2(v[0].x, v[0].y), make_float2(v[0].z, v[0].w), make_float2(v[1].x, v[1].y), make_float2(v[1].z, v[1].w)};
+  store8(p, e);
+}
+
+template <typename G, int FOURS>
 struct Sink {
   G* dE;
   float* part;               // this block's two rows, null: the last level
   int d, col;
   float scale, beta;
   uint32_t first, last;      // words whose sums go there (kNone: none)
-  float2 sum[4];
+  float4 sum[FOURS];
   uint32_t current;
 
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int q = 0; q < FOURS; ++q) sum[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  __device__ __forceinline__ void add(const float4 (&v)[FOURS]) {
+#pragma unroll
+    for (int q = 0; q < FOURS; ++q) sum[q] = make_float4(sum[q].x + v[q].x, sum[q].y + v[q].y, sum[q].z + v[q].z, sum[q].w + v[q].w);
+  }
   __device__ __forceinline__ void flush() {
     if (current == kNone) return;
     if (current == first || current == last) {
-      store8(part + (current == first ? 0 : d) + col, sum);
+      store_cols(part + (current == first ? 0 : d) + col, sum);
     } else {
       G* at = dE + int64_t(current) * d + col;
-      float2 v[4] = {};
-      if (beta != 0.f) {
-        load8(at, v);
+      float4 v[FOURS];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = q8::mul2(v[k], q8::both(beta));
+      for (int q = 0; q < FOURS; ++q) {
+        v[q] = beta != 0.f ? load4(at + 4 * q) : make_float4(0.f, 0.f, 0.f, 0.f);
+        v[q] = make_float4(fmaf(sum[q].x, scale, v[q].x * beta), fmaf(sum[q].y, scale, v[q].y * beta), fmaf(sum[q].z, scale, v[q].z * beta),
+                           fmaf(sum[q].w, scale, v[q].w * beta));
       }
-#pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = q8::fma2(sum[k], q8::both(scale), v[k]);
-      store8(at, v);
+      store_cols(at, v);
     }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) sum[k] = make_float2(0.f, 0.f);
+    clear();
   }
 };
-__device__ __forceinline__ void staged(const uint4* p, __nv_bfloat16, float2 (&v)[4]) {
-  q8::Raw<__nv_bfloat16> r;
-  r.u = *p;
-  r.get(v);
+
+// A thread's columns of a row in pieces of 16 bytes, on their way through its own places of shared memory
+template <int FOURS>
+__device__ __forceinline__ void unpack(const uint4 (&u)[1], const __nv_bfloat16*, float4 (&v)[FOURS]) {
+  v[0] = make_float4(__uint_as_float(u[0].x << 16), __uint_as_float(u[0].x & 0xFFFF0000u), __uint_as_float(u[0].y << 16), __uint_as_float(u[0].y & 0xFFFF0000u));
+  v[1] = make_float4(__uint_as_float(u[0].z << 16), __uint_as_float(u[0].z & 0xFFFF0000u), __uint_as_float(u[0].w << 16), __uint_as_float(u[0].w & 0xFFFF0000u));
 }
-__device__ __forceinline__ void staged(const uint4* p, float, float2 (&v)[4]) {
-  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + kSumThreads);
-  v[0] = make_float2(a.x, a.y); v[1] = make_float2(a.z, a.w);
-  v[2] = make_float2(b.x, b.y); v[3] = make_float2(b.z, b.w);
+template <int FOURS>
+__device__ __forceinline__ void unpack(const uint4 (&u)[FOURS], const float*, float4 (&v)[FOURS]) {
+#pragma unroll
+  for (int q = 0; q < FOURS; ++q) v[q] = make_float4(__uint_as_float(u[q].x), __uint_as_float(u[q].y), __uint_as_float(u[q].z), __uint_as_float(u[q].w));
 }
-// Rows src[row[k]], k < count, with words that are sorted.  A thread copies its eight columns of many rows into its own places of shared memory before it adds the first: one trip to memory for a run of 32 rows in bf16, two in
-// fp32, and a loop that is short (with eight rows at a time in registers, unrolled, the kernel spilled and the code of the sums'
-// ends was 18 times there: 69 us for 5003 x 1000 fp32 with 32003 words).
-constexpr int kStage = 64 << 10;   // bytes of a block: three blocks per SM
-template <typename S, typename G>
-__device__ __forceinline__ void sum_rows(Sink<G>& sink, const S* src, const uint32_t* word, const uint32_t* row, int count, uint8_t* stage) {
-  constexpr int kPieces = int(sizeof(S)) / 2, kAhead = kStage / (kSumThreads * 16 * kPieces);
+
+// Rows src[row[k]], k < count, with words that are sorted.  A thread copies its columns of many rows into its own places of shared
+// memory before it adds the first: one trip to memory for a run, and a loop that is short (with eight rows at a time in registers,
+// unrolled, the kernel spilled and the code of the sums' ends was 18 times there: 69 us for 5003 x 1000 fp32).
+constexpr int kStage = 32 * kSumThreads * 16;
+template <typename S, typename G, int FOURS>
+__device__ __forceinline__ void sum_rows(Sink<G, FOURS>& sink, const S* src, const uint32_t* word, const uint32_t* row, int count, uint8_t* stage) {
+  constexpr int kPieces = FOURS * 4 * int(sizeof(S)) / 16, kAhead = kStage / (kSumThreads * 16 * kPieces);
   uint4* const mine = reinterpret_cast<uint4*>(stage) + threadIdx.x;
   const uint32_t at = uint32_t(__cvta_generic_to_shared(mine));
-  sink.current = kNone;
+  auto staged = [&](int k, float4 (&v)[FOURS]) {
+    uint4 u[kPieces];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) sink.sum[k] = make_float2(0.f, 0.f);
+    for (int h = 0; h < kPieces; ++h) u[h] = mine[(k * kPieces + h) * kSumThreads];
+    unpack(u, src, v);
+  };
+  sink.current = kNone;
+  sink.clear();
   for (int k0 = 0; k0 < count; k0 += kAhead) {
     const int rows = min(kAhead, count - k0);
 #pragma unroll 4
@@ -365,18 +410,17 @@ __device__ __forceinline__ void sum_rows(Sink<G>& sink, const S* src, const uint
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     uint32_t w = word[k0];
-    float2 v[4];
-    staged(mine, S(), v);
+    float4 v[FOURS];
+    staged(0, v);
     for (int k = 0; k < rows; ++k) {
       if (w != sink.current) {
         sink.flush();
         sink.current = w;
       }
-#pragma unroll
-      for (int q = 0; q < 4; ++q) sink.sum[q] = q8::add2(sink.sum[q], v[q]);
+      sink.add(v);
       const int next = min(k + 1, rows - 1);
       w = word[k0 + next];
-      staged(mine + next * kPieces * kSumThreads, S(), v);
+      staged(next, v);
     }
   }
   sink.flush();
@@ -395,33 +439,35 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const Levels levels, c
   static_assert(kRun <= 2 * kJoin && kJoin == 32 && 2 * kJoin + 2 <= kSumThreads, "one thread per row, two warps");
   wait_for_launch_before();
   let_next_launch_start();
-  Sink<G> sink;
-  sink.col = (blockIdx.y * kSumThreads + threadIdx.x) * 8;
-  sink.d = d;
-  const int run_blocks = levels.blocks[0];
-  if (int(blockIdx.x) >= run_blocks) {
-    // words that do not occur
-    const int64_t row0 = int64_t(int(blockIdx.x) - run_blocks) * kFillRows;
+  const int run_blocks = levels.blocks[0], columns = levels.columns;   // (run, block of columns), run by run, then those of absent words
+  if (int64_t(blockIdx.x) >= int64_t(run_blocks) * columns) {
+    const int64_t row0 = (int64_t(blockIdx.x) - int64_t(run_blocks) * columns) * kFillRows;
     const uint32_t bits = __ldcg(present + (row0 >> 5)) >> (row0 & 31);
-    if (sink.col >= d) return;
+    for (int col = threadIdx.x * 8; col < d; col += kSumThreads * 8) {
 #pragma unroll 4
-    for (int r = 0; r < kFillRows; ++r) {
-      if (row0 + r >= int64_t(vocab) || ((bits >> r) & 1u)) continue;
-      G* at = dE + (row0 + r) * d + sink.col;
-      float2 v[4] = {};
-      if (beta != 0.f) {
-        load8(at, v);
+      for (int r = 0; r < kFillRows; ++r) {
+        if (row0 + r >= int64_t(vocab) || ((bits >> r) & 1u)) continue;
+        G* at = dE + (row0 + r) * d + col;
+        float2 v[4] = {};
+        if (beta != 0.f) {
+          load8(at, v);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = q8::mul2(v[k], q8::both(beta));
+          for (int k = 0; k < 4; ++k) v[k] = q8::mul2(v[k], q8::both(beta));
+        }
+        store8(at, v);
       }
-      store8(at, v);
     }
     return;
   }
+  int block = int(blockIdx.x) / columns;
+  const int column = int(blockIdx.x) % columns;
+  Sink<G, kCols<S> / 4> sink;
+  sink.col = (column * kSumThreads + int(threadIdx.x)) * kCols<S>;
+  sink.d = d;
   sink.dE = dE;
   sink.scale = scale;
   sink.beta = beta;
-  const int64_t i0 = int64_t(blockIdx.x) * kRun;
+  const int64_t i0 = int64_t(block) * kRun;
   int count = int(min(int64_t(kRun), tokens - i0));
   // the words of the run, and by two threads more those on either side
   const int t = threadIdx.x;
@@ -438,11 +484,10 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const Levels levels, c
   bool from_before = live > 0 && word[0] == beside[0], goes_on = live > 0 && live == count && word[live - 1] == beside[1];
   uint32_t first = live > 0 ? word[0] : kNone, last = live > 0 ? word[live - 1] : kNone;
   count = live;
-  int block = blockIdx.x;
   for (int level = 0;; ++level) {
     const bool top = level + 1 == levels.count;
     const int64_t pair = 2 * int64_t(block);
-    uint32_t* const left = levels.word[level] + 2 * int64_t(blockIdx.y) * levels.blocks[level];
+    uint32_t* const left = levels.word[level] + 2 * int64_t(column) * levels.blocks[level];
     sink.part = top ? nullptr : levels.part[level] + pair * d;
     sink.first = !top && from_before ? first : kNone;
     sink.last = !top && goes_on ? last : kNone;
@@ -460,7 +505,7 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const Levels levels, c
     __syncthreads();
     const int group = block / kJoin, members = min(kJoin, levels.blocks[level] - group * kJoin);
     if (threadIdx.x == 0)
-      finished = atomicAdd(levels.arrived[level] + int64_t(blockIdx.y) * levels.blocks[level + 1] + group, 1u) == uint32_t(members - 1);
+      finished = atomicAdd(levels.arrived[level] + int64_t(column) * levels.blocks[level + 1] + group, 1u) == uint32_t(members - 1);
     __syncthreads();
     if (!finished) return;
     __threadfence();
@@ -529,7 +574,7 @@ Plan plan_of(const EmbedProblem& q) {
   p.digit = (bits + p.passes - 1) / p.passes;
   p.rounds = q.tokens <= int64_t(kFewBlocks) * kSortThreads ? 1 : kManyRounds;
   p.blocks = int(ceil_div(q.tokens, kSortThreads * p.rounds));
-  p.columns = int(ceil_div(q.d, kSumThreads * 8));
+  p.columns = int(ceil_div(q.d, kSumThreads * (q.bf16 ? kCols<__nv_bfloat16> : kCols<float>)));
   p.levels = 1;
   p.level_blocks[0] = ceil_div(q.tokens, kRun);
   while (p.level_blocks[p.levels - 1] > 1) {
@@ -554,7 +599,7 @@ Plan plan_of(const EmbedProblem& q) {
 }
 
 template <typename S, typename G>
-cudaError_t sums(const EmbedProblem& q, const Plan& p, const uint2* order, const void* dY, void* dE, float beta, uint8_t* ws, cudaStream_t st) {
+cudaError_t sums(const EmbedProblem& q, const Plan& p, const uint2* order, const void* dY, void* dE, float beta, bool filled, uint8_t* ws, cudaStream_t st) {
   static DeviceOnce once;
   if (once.needed()) {
     const cudaError_t e = cudaFuncSetAttribute(sum_kernel<S, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStage);
@@ -563,6 +608,7 @@ cudaError_t sums(const EmbedProblem& q, const Plan& p, const uint2* order, const
   }
   Levels l{};
   l.count = p.levels;
+  l.columns = p.columns;
   for (int k = 0; k < p.levels; ++k) {
     l.blocks[k] = int(p.level_blocks[k]);
     if (k + 1 == p.levels) break;
@@ -570,13 +616,14 @@ cudaError_t sums(const EmbedProblem& q, const Plan& p, const uint2* order, const
     l.word[k] = reinterpret_cast<uint32_t*>(ws + p.word[k]);
     l.arrived[k] = reinterpret_cast<uint32_t*>(ws + p.arrived[k]);
   }
-  const int64_t fill = beta == 1.f ? 0 : ceil_div(q.vocab, kFillRows);
-  return launch_lined_up(sum_kernel<S, G>, dim3(unsigned(p.level_blocks[0] + fill), unsigned(p.columns)), dim3(kSumThreads), kStage, st, l, order, q.tokens,
+  const int64_t fill = beta == 1.f || filled ? 0 : ceil_div(q.vocab, kFillRows);
+  return launch_lined_up(sum_kernel<S, G>, dim3(unsigned(p.level_blocks[0] * p.columns + fill)), dim3(kSumThreads), kStage, st, l, order, q.tokens,
                          uint32_t(q.vocab), static_cast<const S*>(dY), static_cast<G*>(dE), int(q.d), q.scale, beta,
                          reinterpret_cast<const uint32_t*>(ws + p.present));
 }
 
-cudaError_t small_sort(const EmbedProblem& q, const Plan& p, const int64_t* ids, uint8_t* ws, const uint2** order, cudaStream_t st) {
+// zeros: the table, or null if its rows are not to be written here.
+cudaError_t small_sort(const EmbedProblem& q, const Plan& p, const int64_t* ids, uint8_t* ws, void* zeros, const uint2** order, cudaStream_t st) {
   constexpr int kMost = kSortWarps * kMaxBins * 4 + kOneBlockTokens * 8;
   static DeviceOnce once;
   if (once.needed()) {
@@ -592,8 +639,10 @@ cudaError_t small_sort(const EmbedProblem& q, const Plan& p, const int64_t* ids,
   s.digit = p.digit;
   s.present = reinterpret_cast<uint32_t*>(ws + p.present);
   *order = s.out;
-  return launch_lined_up(small_sort_kernel, dim3(1), dim3(kSortThreads), (size_t(kSortWarps) << (p.digit + 2)) + size_t(q.tokens) * 8, st, s, p.passes,
-                         reinterpret_cast<uint32_t*>(ws + p.clear), int64_t(p.clear_end - p.clear) / 4);
+  const int64_t zero_count = zeros ? q.vocab * q.d * (q.grad_bf16 ? 2 : 4) / 16 : 0;
+  const unsigned grid = unsigned(1 + std::min<int64_t>(ceil_div(zero_count, 8 * kSortThreads), 2 * kFewBlocks - 1));
+  return launch_lined_up(small_sort_kernel, dim3(grid), dim3(kSortThreads), (size_t(kSortWarps) << (p.digit + 2)) + size_t(q.tokens) * 8, st, s, p.passes,
+                         reinterpret_cast<uint32_t*>(ws + p.clear), int64_t(p.clear_end - p.clear) / 4, static_cast<uint4*>(zeros), zero_count);
 }
 
 template <int ROUNDS>
@@ -662,11 +711,12 @@ cudaError_t embed_bwd(const EmbedProblem& q, const int64_t* ids, const void* dY,
   const Plan p = plan_of(q);
   uint8_t* w8 = static_cast<uint8_t*>(ws);
   const uint2* order = nullptr;
-  const cudaError_t e = q.tokens <= kOneBlockTokens ? small_sort(q, p, ids, w8, &order, st) : p.rounds == 1 ? sort<1>(q, p, ids, w8, &order, st) : sort<kManyRounds>(q, p, ids, w8, &order, st);
+  const bool filled = q.tokens <= kOneBlockTokens && beta == 0.f;
+  const cudaError_t e = q.tokens <= kOneBlockTokens ? small_sort(q, p, ids, w8, filled ? dE : nullptr, &order, st) : p.rounds == 1 ? sort<1>(q, p, ids, w8, &order, st) : sort<kManyRounds>(q, p, ids, w8, &order, st);
   if (e != cudaSuccess) return e;
   if (q.bf16)
-    return q.grad_bf16 ? sums<__nv_bfloat16, __nv_bfloat16>(q, p, order, dY, dE, beta, w8, st) : sums<__nv_bfloat16, float>(q, p, order, dY, dE, beta, w8, st);
-  return q.grad_bf16 ? sums<float, __nv_bfloat16>(q, p, order, dY, dE, beta, w8, st) : sums<float, float>(q, p, order, dY, dE, beta, w8, st);
+    return q.grad_bf16 ? sums<__nv_bfloat16, __nv_bfloat16>(q, p, order, dY, dE, beta, filled, w8, st) : sums<__nv_bfloat16, float>(q, p, order, dY, dE, beta, filled, w8, st);
+  return q.grad_bf16 ? sums<float, __nv_bfloat16>(q, p, order, dY, dE, beta, filled, w8, st) : sums<float, float>(q, p, order, dY, dE, beta, filled, w8, st);
 }
 
 }  // namespace acx
