@@ -71,7 +71,6 @@ struct Params {
   float c;                   // scale log2(e): x = c s without a cap
   float cap_in;              // scale / cap: the tanh's argument per unit of s
   float cap_out;             // cap log2(e)
-  int halves;                // forward: halves of 128 queries in an item, 2 (from the list of wide ones) or 1
   float* lse;                // [heads][tokens], natural logarithm
   int* status;
   __nv_bfloat16* O;

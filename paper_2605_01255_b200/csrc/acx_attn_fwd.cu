@@ -171,7 +171,7 @@ struct FwdSmem {
   static_assert(kBytes <= 232448, "shared memory of one CTA");
 };
 
-template <int HD, bool CAP, bool BIAS>
+template <int HD, bool CAP, bool BIAS, int HALVES>
 __global__ void __launch_bounds__(kFwdThreads, 1)
     attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                     const __grid_constant__ CUtensorMap map_v, const Params p) {
@@ -232,7 +232,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
   wait_for_launch_before();
   let_next_launch_start();
   const bool fits = plan_fits(p);
-  const int units = fits ? __ldcg(p.halves == 2 ? &p.plan->wide : &p.plan->tiles) * p.heads : 0;
+  const int units = fits ? __ldcg(HALVES == 2 ? &p.plan->wide : &p.plan->tiles) * p.heads : 0;
   auto give_up = [&]() {
     *abort_flag = 1;
     atomicExch(p.status, kDevTimeout);
@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
   // key tiles that a half of the queries sees
   auto key_tiles = [&](const Item& t, int half) {
     const int r = t.row0 + kRows * half;
-    if (half >= p.halves || r >= t.end) return 0;
+    if (r >= t.end) return 0;
     return ((p.causal ? max(min(r + kRows, t.end), t.prefix) : t.end) - t.start + kRows - 1) / kRows;
   };
 
@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
       for (int u; ok && (u = unit_of(it)) < units; ++it) {
         const Item t = fetch_item(p.items, u / p.heads);
         const int h = u % p.heads, g = h / p.group;
-        const int n1 = key_tiles(t, 1), n = max(key_tiles(t, 0), n1);
+        const int n1 = HALVES == 2 ? key_tiles(t, 1) : 0, n = max(key_tiles(t, 0), n1);
         if (!ptx::mbar_wait(q_empty, (it & 1) ^ 1u, abort_flag)) { give_up(); ok = false; break; }
         ptx::mbar_arrive_expect_tx(q_full, (n1 ? 2 : 1) * T::kBytes);
         T::load(base, &map_q, q_full, h, t.row0);
@@ -297,7 +297,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
     auto addr = [&](Slot s) { return base + FwdSmem<HD>::kTiles + s.stage * T::kBytes; };
     for (int u; ok && (u = unit_of(it)) < units; ++it) {
       const Item t = fetch_item_warp(p.items, u / p.heads);
-      const int nt[2] = {key_tiles(t, 0), key_tiles(t, 1)}, n = max(nt[0], nt[1]);
+      const int nt[2] = {key_tiles(t, 0), HALVES == 2 ? key_tiles(t, 1) : 0}, n = max(nt[0], nt[1]);
       // scores of key tile j for the halves that see it, each once its scores before have been read
       auto scores = [&](int j) {
         const Slot k = next();
@@ -354,7 +354,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
     const uint32_t s_at = tmem_s(half) + lanes, o_at = tmem_o(half) + lanes;
     uint8_t* const p_row = gen + FwdSmem<HD>::kP + half * FwdSmem<HD>::kPBytes + r * 128;
     int turns = 0, outs = 0, it = 0;
-    bool ok = true;
+    bool ok = half < HALVES;
     for (int u; ok && (u = unit_of(it)) < units; ++it) {
       const Item t = fetch_item_warp(p.items, u / p.heads);
       const int n = key_tiles(t, half), head = u % p.heads;
@@ -530,21 +530,27 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
   }
 }
 
-template <int HD, bool CAP, bool BIAS>
+template <int HD, bool CAP, bool BIAS, int HALVES>
 cudaError_t launch_fwd(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, unsigned grid, cudaStream_t st) {
   static DeviceOnce once;
+  const auto kernel = attn_fwd_kernel<HD, CAP, BIAS, HALVES>;
   if (once.needed()) {
-    const cudaError_t e = cudaFuncSetAttribute(attn_fwd_kernel<HD, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, FwdSmem<HD>::kBytes);
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, FwdSmem<HD>::kBytes);
     if (e != cudaSuccess) return e;
     once.done();
   }
-  return launch_lined_up(attn_fwd_kernel<HD, CAP, BIAS>, dim3(grid), dim3(kFwdThreads), FwdSmem<HD>::kBytes, st, q, k, v, p);
+  return launch_lined_up(kernel, dim3(grid), dim3(kFwdThreads), FwdSmem<HD>::kBytes, st, q, k, v, p);
 }
-template <int HD>
+template <int HD, int HALVES>
 cudaError_t launch_fwd(bool cap, bool bias, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, unsigned grid,
                        cudaStream_t st) {
-  if (cap) return bias ? launch_fwd<HD, true, true>(q, k, v, p, grid, st) : launch_fwd<HD, true, false>(q, k, v, p, grid, st);
-  return bias ? launch_fwd<HD, false, true>(q, k, v, p, grid, st) : launch_fwd<HD, false, false>(q, k, v, p, grid, st);
+  if (cap) return bias ? launch_fwd<HD, true, true, HALVES>(q, k, v, p, grid, st) : launch_fwd<HD, true, false, HALVES>(q, k, v, p, grid, st);
+  return bias ? launch_fwd<HD, false, true, HALVES>(q, k, v, p, grid, st) : launch_fwd<HD, false, false, HALVES>(q, k, v, p, grid, st);
+}
+template <int HD>
+cudaError_t launch_fwd(int halves, bool cap, bool bias, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p,
+                       unsigned grid, cudaStream_t st) {
+  return halves == 2 ? launch_fwd<HD, 2>(cap, bias, q, k, v, p, grid, st) : launch_fwd<HD, 1>(cap, bias, q, k, v, p, grid, st);
 }
 
 }  // namespace
@@ -584,17 +590,17 @@ cudaError_t attn_fwd(const AttnProblem& q, const AttnMatrix& Q, const AttnMatrix
                      const AttnMatrix& O, float* lse, int* status, cudaStream_t st) {
   Params p = common_params(q, plan, slopes, lse, status);
   const PlanLayout at = plan_layout(q.tokens, q.docs);
-  p.halves = q.tokens / (2 * kRows) * q.heads > sm_count() ? 2 : 1;
-  p.items = reinterpret_cast<const Item*>(static_cast<const uint8_t*>(plan) + (p.halves == 2 ? at.wide : at.queries));
+  const int halves = q.tokens / (2 * kRows) * q.heads > sm_count() ? 2 : 1;
+  p.items = reinterpret_cast<const Item*>(static_cast<const uint8_t*>(plan) + (halves == 2 ? at.wide : at.queries));
   p.O = static_cast<__nv_bfloat16*>(O.p);
   p.ldo = O.ld;
   CUtensorMap mq, mk, mv;
   if (!make_tmap_heads(&mq, Q.p, q.tokens, q.heads, q.d, Q.ld, kRows) || !make_tmap_heads(&mk, K.p, q.tokens, q.kv_heads, q.d, K.ld, kRows) ||
       !make_tmap_heads(&mv, V.p, q.tokens, q.kv_heads, q.d, V.ld, kRows))
     return cudaErrorInvalidValue;
-  const unsigned grid = unsigned(std::min<int64_t>((p.halves == 2 ? at.wide_cap : at.tile_cap) * q.heads, sm_count()));
+  const unsigned grid = unsigned(std::min<int64_t>((halves == 2 ? at.wide_cap : at.tile_cap) * q.heads, sm_count()));
   const bool cap = q.softcap > 0.f, bias = slopes != nullptr;
-  return q.d <= 64 ? launch_fwd<64>(cap, bias, mq, mk, mv, p, grid, st) : launch_fwd<128>(cap, bias, mq, mk, mv, p, grid, st);
+  return q.d <= 64 ? launch_fwd<64>(halves, cap, bias, mq, mk, mv, p, grid, st) : launch_fwd<128>(halves, cap, bias, mq, mk, mv, p, grid, st);
 }
 
 }  // namespace acx
