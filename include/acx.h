@@ -468,7 +468,8 @@ ACX_API size_t acx_grad_workspace_bytes(const acx_grad_desc* desc, int op);
  * not needed after the call. */
 ACX_API acx_status acx_grad_plan(const acx_grad_desc* desc, const acx_grad* list, void* plan, size_t plan_bytes, void* cuda_stream);
 /* norm = sqrt(sum of weight * sum of x^2),  f = max_norm / norm where norm > max_norm, else 1;  dst = f * src for every tensor.
- *   max_norm > 0 (infinity: only the norm, and a copy where dst is not src);  total [2] fp32, out: norm and f.
+ *   max_norm > 0 (infinity: only the norm, and a copy where dst is not src);  total [2] fp32, out: norm and f (a norm beyond fp32's
+ *   range reads as infinity there, with the f < 1 that it has in 64 bits).
  *   A norm that is not finite (an infinity or a NaN among the gradients) leaves f = 1: the caller sees it in total[0] and may leave the
  *   step out.  Sums in 64 bits, fixed order: reproducible bits. */
 ACX_API acx_status acx_grad_clip(const acx_grad_desc* desc, const void* plan, size_t plan_bytes, float max_norm, float* total, void* ws,

@@ -116,6 +116,14 @@ CASES = {
     "own scale": dict(lengths=[300], heads=2, kv_heads=1, d=64, scale=0.02),
     "sharp scores": dict(lengths=[400], heads=2, kv_heads=1, d=64, size=5.0),
     "flat scores": dict(lengths=[900], heads=2, kv_heads=1, d=64, size=0.05),
+    # enough heads for work items of 256 queries, and for a key tile's heads to be dealt in twos
+    "many heads": dict(lengths=[700, 1000, 257], heads=28, kv_heads=4, d=64, before=11),
+    "many heads 128": dict(lengths=[513, 900], heads=40, kv_heads=8, d=128, behind=5),
+    "many heads, all": dict(lengths=[650, 700], heads=32, kv_heads=32, d=40, causal=False),
+    "many heads, everything": dict(lengths=[900, 640, 1], prefix=[400, 0, 1], cap=15.0, alibi=True, heads=27, kv_heads=9, d=72, before=2, behind=3),
+    "many heads, distance": dict(lengths=[1100, 300], alibi=True, heads=32, kv_heads=8, d=64),
+    "many heads, cap": dict(lengths=[1100, 300], cap=5.0, heads=32, kv_heads=8, d=64),
+    "heads in twos": dict(lengths=[256] * 12 + [200] * 5 + [131], heads=28, kv_heads=4, d=16),
 }
 
 

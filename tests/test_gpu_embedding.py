@@ -36,6 +36,11 @@ CASES = [
     (8193, 64, 2, "bf16", "f32", 1.0, "random"),
     (40000, 16, 70000, "f32", "f32", 1.0, "skewed"),
     (70001, 8, 9, "f32", "f32", 1.0, "runs"),
+    # behind the sizes at which the sort changes: one block up to 8192, one item per thread up to 148 blocks, then eight
+    (16384, 520, 130000, "bf16", "f32", 1.0, "skewed"),
+    (151_552, 8, 600, "bf16", "bf16", 1.0, "skewed"),
+    (151_553, 8, 600, "f32", "f32", 1.0, "random"),
+    (300_001, 16, 300_000, "bf16", "f32", 1.0, "skewed"),
 ]
 
 
@@ -218,6 +223,11 @@ def test_a_norm_that_is_not_finite_leaves_the_gradients(bad):
     B.acx_grad_clip(lst, 0.1, total, ws=B.alloc_grad_workspace(lst))
     assert not math.isfinite(total[0]) and float(total[1]) == 1.0
     assert all(torch.equal(a.cpu().view(torch.uint8), b.view(torch.uint8)) for a, b in zip(dev, grads))
+
+
+def test_a_list_without_elements():
+    total = check_clip([torch.zeros(0), torch.zeros(0, dtype=torch.bfloat16)], 1.0)
+    assert total.tolist() == [0.0, 1.0]
 
 
 def test_clip_again_and_same_bits():
