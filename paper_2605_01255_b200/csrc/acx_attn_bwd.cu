@@ -13,7 +13,9 @@
 // p (dP - delta) summed in fp32 beside it, delta + r is what the launch for the keys uses, and dQ = scale (second - r' first) with
 // the sum r' of the dS as they were rounded: exact ones sum to zero, so r' is e and what the roundings leave of the keys' mean (errors
 // of dQ 0.00245 with r, 0.0023 with r', where the keys have a mean; the rounding of dS and of dQ themselves make 0.0023).
-// The price of two launches is that S and dP are computed twice: eight products instead of five.
+// The price of two launches is that S and dP are computed twice: eight products instead of five.  Measured: 8192 tokens x 24 heads (8
+// of keys) x 128, causal, 609 us for the queries and 709 for the keys, 1.25 PFLOP/s over the eight, 75 % of the rate of a large product (tensor
+// pipe 70 and 56 % busy); 2650 and 3180 cycles per tile of 128 x 128 where the products alone need 2048, the rest is rows' work in between.
 //
 // S, dP, first and second fill the tensor memory (4 x 128 columns); dS goes over dP as bf16 and is multiplied from there, P goes to shared
 // memory, so that the next S can be taken as soon as this one has been read: the rows' warps never wait for it (with P over S they
@@ -635,7 +637,8 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const Params p) {
   const bool v = blockIdx.y != 0;
   const float* part = (v ? p.dv_part : p.dk_part) + row * (int64_t(p.kv_heads) * p.d) + col;
   float2 sum[4] = {};
-  for (int i = 0; i < p.parts; ++i) {
+#pragma unroll 4
+  for (int i = 0; i < p.parts; ++i) {   // several on their way at a time
     float2 x[4];
     q8::load8(part + int64_t(i) * p.tokens * p.kv_heads * p.d, x);
 #pragma unroll

@@ -238,8 +238,8 @@ __device__ __forceinline__ void umma_steps(uint32_t tmem_d, uint32_t a_lo, uint3
         ::"r"(tmem_d), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(uint32_t(accumulate)), "n"(B_STEP), "n"(2 * B_STEP), "n"(3 * B_STEP)
         : "memory");
 }
-// The same with A in tensor memory (lane = row, each 32-bit column two consecutive bf16 along K), eight columns per step, A's third step GAP columns behind the second; B (MN-major, 128 bytes wide
-// rows) advances by 16 rows.
+// The same with A in tensor memory (lane = row, each 32-bit column two consecutive bf16 along K): eight columns per step, the third
+// step GAP columns further; B (MN-major, rows of 128 bytes) advances by 16 rows.
 template <int STEPS, int GAP>
 __device__ __forceinline__ void umma_steps_tmem_a(uint32_t tmem_d, uint32_t tmem_a, uint32_t b_lo, uint32_t hi, uint32_t idesc, bool accumulate) {
   static_assert(STEPS == 1 || STEPS == 4, "a step or four");
@@ -328,22 +328,12 @@ __device__ __forceinline__ uint32_t tmem_ld_x1(uint32_t taddr) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n\ttcgen05.wait::ld.sync.aligned;" : "=r"(v) : "r"(taddr) : "memory");
   return v;
 }
-// 32 lanes x 16 or 32 consecutive 32-bit columns, to tensor memory: thread t of the warp writes lane (base lane + t).
+// 32 lanes x 16 consecutive 32-bit columns, to tensor memory: thread t of the warp writes lane (base lane + t).
 __device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t (&v)[16]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
       ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]),
         "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
-      : "memory");
-}
-__device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t (&v)[32]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
-      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
-      ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]),
-        "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]),
-        "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]),
-        "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
       : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
