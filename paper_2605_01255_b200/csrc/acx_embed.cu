@@ -75,7 +75,7 @@ struct SortPass {
   int64_t n;
   uint32_t vocab;            // the key of every id outside the vocabulary
   int shift, digit, blocks;
-  uint32_t* present;         // last pass: one bit per word that occurs
+  uint32_t* present;         // last pass: one bit per word that occurs; null where nobody asks
 };
 __device__ __forceinline__ uint2 sort_item(const SortPass& s, int64_t i) {
   if (!s.ids) return __ldcg(s.in + i);
@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(kSortThreads) small_sort_kernel(const SortPass
         const uint32_t at = first + __popc(same[r] & ((1u << lane) - 1u));
         (end ? s.out : held)[at] = item[r];
         if (leader) place[warp * bins + digit] = first + __popc(same[r]);
-        if (end && item[r].x < s.vocab) atomicOr(s.present + (item[r].x >> 5), 1u << (item[r].x & 31u));
+        if (end && s.present && item[r].x < s.vocab) atomicOr(s.present + (item[r].x >> 5), 1u << (item[r].x & 31u));
       }
       __syncwarp();
     }
@@ -602,7 +602,7 @@ Plan plan_of(const EmbedProblem& q) {
 }
 
 template <typename S, typename G>
-cudaError_t sums(const EmbedProblem& q, const Plan& p, const uint2* order, const void* dY, void* dE, float beta, bool filled, uint8_t* ws, cudaStream_t st) {
+cudaError_t sums(const EmbedProblem& q, const Plan& p, const uint2* order, const void* dY, void* dE, float beta, bool absent, uint8_t* ws, cudaStream_t st) {
   static DeviceOnce once;
   if (once.needed()) {
     const cudaError_t e = cudaFuncSetAttribute(sum_kernel<S, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStage);
@@ -619,14 +619,15 @@ cudaError_t sums(const EmbedProblem& q, const Plan& p, const uint2* order, const
     l.word[k] = reinterpret_cast<uint32_t*>(ws + p.word[k]);
     l.arrived[k] = reinterpret_cast<uint32_t*>(ws + p.arrived[k]);
   }
-  const int64_t fill = beta == 1.f || filled ? 0 : ceil_div(q.vocab, kFillRows);
+  const int64_t fill = absent ? ceil_div(q.vocab, kFillRows) : 0;
   return launch_lined_up(sum_kernel<S, G>, dim3(unsigned(p.level_blocks[0] * p.columns + fill)), dim3(kSumThreads), kStage, st, l, order, q.tokens,
                          uint32_t(q.vocab), static_cast<const S*>(dY), static_cast<G*>(dE), int(q.d), q.scale, beta,
                          reinterpret_cast<const uint32_t*>(ws + p.present));
 }
 
-// zeros: the table, or null if its rows are not to be written here.
-cudaError_t small_sort(const EmbedProblem& q, const Plan& p, const int64_t* ids, uint8_t* ws, void* zeros, const uint2** order, cudaStream_t st) {
+// zeros: the table, or null if its rows are not to be written here.  absent: whether the sums have to know absent words.
+cudaError_t small_sort(const EmbedProblem& q, const Plan& p, const int64_t* ids, uint8_t* ws, void* zeros, bool absent, const uint2** order,
+                       cudaStream_t st) {
   constexpr int kMost = kSortWarps * kMaxBins * 4 + kOneBlockTokens * 8;
   static DeviceOnce once;
   if (once.needed()) {
@@ -640,7 +641,7 @@ cudaError_t small_sort(const EmbedProblem& q, const Plan& p, const int64_t* ids,
   s.n = q.tokens;
   s.vocab = uint32_t(q.vocab);
   s.digit = p.digit;
-  s.present = reinterpret_cast<uint32_t*>(ws + p.present);
+  s.present = absent ? reinterpret_cast<uint32_t*>(ws + p.present) : nullptr;
   *order = s.out;
   const int64_t zero_count = zeros ? q.vocab * q.d * (q.grad_bf16 ? 2 : 4) / 16 : 0;
   const unsigned grid = unsigned(1 + std::min<int64_t>(ceil_div(zero_count, 8 * kSortThreads), 2 * kFewBlocks - 1));
@@ -649,7 +650,7 @@ cudaError_t small_sort(const EmbedProblem& q, const Plan& p, const int64_t* ids,
 }
 
 template <int ROUNDS>
-cudaError_t sort(const EmbedProblem& q, const Plan& p, const int64_t* ids, uint8_t* ws, const uint2** order, cudaStream_t st) {
+cudaError_t sort(const EmbedProblem& q, const Plan& p, const int64_t* ids, uint8_t* ws, bool absent, const uint2** order, cudaStream_t st) {
   static DeviceOnce once;
   if (once.needed()) {
     const cudaError_t e = cudaFuncSetAttribute(scatter_kernel<ROUNDS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortWarps * kMaxBins * 4);
@@ -671,7 +672,7 @@ cudaError_t sort(const EmbedProblem& q, const Plan& p, const int64_t* ids, uint8
   for (int k = 0; k < p.passes && e == cudaSuccess; ++k) {
     uint32_t* const next = reinterpret_cast<uint32_t*>(ws + p.next_table) + (size_t(p.blocks) << p.digit) * size_t(k);
     s.next_table = k + 1 < p.passes ? next : nullptr;
-    s.present = k + 1 == p.passes ? reinterpret_cast<uint32_t*>(ws + p.present) : nullptr;
+    s.present = absent && k + 1 == p.passes ? reinterpret_cast<uint32_t*>(ws + p.present) : nullptr;
     e = launch_lined_up(scatter_kernel<ROUNDS>, dim3(unsigned(p.blocks)), dim3(kSortThreads), size_t(kSortWarps) << (p.digit + 2), st, s);
     *order = s.out;
     s.ids = nullptr;
@@ -714,12 +715,12 @@ cudaError_t embed_bwd(const EmbedProblem& q, const int64_t* ids, const void* dY,
   const Plan p = plan_of(q);
   uint8_t* w8 = static_cast<uint8_t*>(ws);
   const uint2* order = nullptr;
-  const bool filled = q.tokens <= kOneBlockTokens && beta == 0.f;
-  const cudaError_t e = q.tokens <= kOneBlockTokens ? small_sort(q, p, ids, w8, filled ? dE : nullptr, &order, st) : p.rounds == 1 ? sort<1>(q, p, ids, w8, &order, st) : sort<kManyRounds>(q, p, ids, w8, &order, st);
+  const bool filled = q.tokens <= kOneBlockTokens && beta == 0.f, absent = beta != 1.f && !filled;
+  const cudaError_t e = q.tokens <= kOneBlockTokens ? small_sort(q, p, ids, w8, filled ? dE : nullptr, absent, &order, st) : p.rounds == 1 ? sort<1>(q, p, ids, w8, absent, &order, st) : sort<kManyRounds>(q, p, ids, w8, absent, &order, st);
   if (e != cudaSuccess) return e;
   if (q.bf16)
-    return q.grad_bf16 ? sums<__nv_bfloat16, __nv_bfloat16>(q, p, order, dY, dE, beta, filled, w8, st) : sums<__nv_bfloat16, float>(q, p, order, dY, dE, beta, filled, w8, st);
-  return q.grad_bf16 ? sums<float, __nv_bfloat16>(q, p, order, dY, dE, beta, filled, w8, st) : sums<float, float>(q, p, order, dY, dE, beta, filled, w8, st);
+    return q.grad_bf16 ? sums<__nv_bfloat16, __nv_bfloat16>(q, p, order, dY, dE, beta, absent, w8, st) : sums<__nv_bfloat16, float>(q, p, order, dY, dE, beta, absent, w8, st);
+  return q.grad_bf16 ? sums<float, __nv_bfloat16>(q, p, order, dY, dE, beta, absent, w8, st) : sums<float, float>(q, p, order, dY, dE, beta, absent, w8, st);
 }
 
 }  // namespace acx
