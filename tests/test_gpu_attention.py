@@ -116,6 +116,9 @@ CASES = {
     "own scale": dict(lengths=[300], heads=2, kv_heads=1, d=64, scale=0.02),
     "sharp scores": dict(lengths=[400], heads=2, kv_heads=1, d=64, size=5.0),
     "flat scores": dict(lengths=[900], heads=2, kv_heads=1, d=64, size=0.05),
+    # more documents and more tiles than the plan's block has threads and registers for
+    "1500 documents": dict(lengths=[i % 3 for i in range(1500)], heads=2, kv_heads=1, d=16, behind=3),
+    "4500 documents": dict(lengths=[1 + i % 3 for i in range(4500)], heads=2, kv_heads=2, d=8, causal=False, before=2),
     # enough heads for work items of 256 queries, and for a key tile's heads to be dealt in twos
     "many heads": dict(lengths=[700, 1000, 257], heads=28, kv_heads=4, d=64, before=11),
     "many heads 128": dict(lengths=[513, 900], heads=40, kv_heads=8, d=128, behind=5),
