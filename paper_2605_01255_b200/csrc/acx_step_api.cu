@@ -76,6 +76,7 @@ bool outputs_overlap(const acx_grad* list, int64_t count) {
 acx_status validate_grad(const acx_grad_desc* d, GradProblem* out) {
   if (!d || d->struct_size != sizeof(acx_grad_desc) || d->reserved != 0) return ACX_ERR_INVALID_ARG;
   if (d->tensors < 0 || d->tensors > (int64_t(1) << 24) || d->chunks < 0 || d->chunks > (int64_t(1) << 31)) return ACX_ERR_UNSUPPORTED_SHAPE;
+  if (d->tensors == 0 && d->chunks > 0) return ACX_ERR_INVALID_ARG;   // no list's: a plan is asked for only where there are tensors
   out->tensors = d->tensors;
   out->chunks = d->chunks;
   return ACX_OK;
