@@ -449,8 +449,10 @@ typedef struct acx_grad {
   const void* src;
   void* dst;
   int64_t n;
-  float weight;         /* >= 0: multiplies its sum of squares in the squared norm.  1 for a gradient; d_in / r for a factor A, whose
-                           ||A S^T||^2 is that many times ||A||^2 on average over the sketches (E[S^T S] = (d_in / r) I) */
+  float weight;         /* >= 0: multiplies its sum of squares in the squared norm.  1 for a gradient; (d_in + r + 1) / r for a factor A = dW S:
+                           ||A S^T||^2 = ||dW S S^T||^2 is that many times ||A||^2 on average over the sketches, as
+                           E[(S S^T)^2] = (d_in + r + 1) / r I and E[S S^T] = I.  (d_in / r, from E[S^T S] alone, would hold
+                           for an A that does not depend on S.) */
   int32_t src_dtype, dst_dtype;
   int32_t reserved;
 } acx_grad;

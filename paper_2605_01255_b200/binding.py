@@ -533,6 +533,11 @@ class GradList:
         self.desc, self.plan, self._tensors = desc, plan, tensors
 
 
+def grad_factor_weight(d_in: int, r: int) -> float:
+    """Weight of a gradient factor A = dW S in a norm: what ||A S^T||^2 is on average over the sketches, in units of ||A||^2."""
+    return (d_in + r + 1) / r
+
+
 def make_grad_list(tensors: Sequence[torch.Tensor], weights: Optional[Sequence[float]] = None, out: Optional[Sequence[torch.Tensor]] = None,
                    stream=None) -> GradList:
     """Contiguous fp32 or bf16 gradients of one device, their weights in the squared norm (None: 1) and where they go clipped (None: in

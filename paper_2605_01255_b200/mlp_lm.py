@@ -117,8 +117,8 @@ class MlpLm:
             self.table = B.make_embed_desc(m, d, s.vocab, bf, scale=d ** 0.5)
             self.ws_table = B.alloc_embed_workspace(self.table, B.ACX_OP_EMBED_BWD, self.dev)
         if s.max_norm > 0:
-            # a factor counts d_in / r times: what its gradient's norm is on average over the sketches
-            parts = [(a, self.w[l][k].shape[1] / s.r) for l in range(L) for k, a in self.factors[l].items()]
+            # a factor counts as often as its gradient A S^T does on average over the sketches
+            parts = [(a, B.grad_factor_weight(self.w[l][k].shape[1], s.r)) for l in range(L) for k, a in self.factors[l].items()]
             parts += [(t, 1.0) for ts in self.grads.values() for t in ts]
             self.clip = B.make_grad_list([t for t, _ in parts], [w for _, w in parts])
             self.norm, self.ws_clip = new(2, dt=f32), B.alloc_grad_workspace(self.clip)

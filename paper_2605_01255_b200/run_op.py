@@ -104,7 +104,7 @@ def _embed(m, d_in, d_out, r, tdt):
 
 def _grad_clip(m, d_in, d_out, r, tdt):
     factors = [torch.randn(d_out, r, device="cuda") for _ in range(24)]
-    grads = B.make_grad_list(factors, [d_in / r] * len(factors))
+    grads = B.make_grad_list(factors, [B.grad_factor_weight(d_in, r)] * len(factors))
     total, ws = torch.empty(2, device="cuda"), B.alloc_grad_workspace(grads)
     return lambda: B.acx_grad_clip(grads, 1.0, total, ws=ws)
 

@@ -1,0 +1,69 @@
+"""Attention, clipping and the training step where numbers end: scores of minus infinity and far beyond 2^24, saturated caps, values that
+are none where the mask hides them, short documents in long batches, steps whose norm is no number."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import attention as oa
+from paper_2605_01255_b200 import binding as B
+from paper_2605_01255_b200 import mlp_lm as M
+from test_gpu_step import reference, rel
+
+pytestmark = pytest.mark.gpu
+BF, NAN, INF = torch.bfloat16, float("nan"), float("inf")
+
+
+def offsets_of(*ends):
+    return torch.tensor([0, *ends], dtype=torch.int32, device="cuda")
+
+
+def inputs(T, H, K, d, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    return [torch.randn(T, h, d, generator=g).to(BF).cuda() for h in (H, K, K, H)]
+
+
+def run(desc, offsets, q, k, v, do, prefix=None, slopes=None):
+    """o, lse (tokens first), dq, dk, dv; outputs start as NaN."""
+    plan = B.alloc_attn_workspace(desc, B.ACX_OP_ATTN_PLAN)
+    B.acx_attn_plan(desc, offsets, plan, prefix=prefix)
+    o, lse = torch.full_like(q, NAN), torch.full((q.shape[1], q.shape[0]), NAN, device="cuda")
+    B.acx_attn_fwd(desc, q, k, v, plan, o, lse, slopes=slopes)
+    g = [torch.full_like(t, NAN) for t in (q, k, v)]
+    B.acx_attn_bwd(desc, q, k, v, plan, o, do, lse, *g, slopes=slopes, ws=B.alloc_attn_workspace(desc, B.ACX_OP_ATTN_BWD))
+    assert B.acx_last_device_status() == B.ACX_OK
+    return [o, lse.T.contiguous(), *g]
+
+
+# ------------------------------------------------------------------------------------------------------ the training step
+def test_step_against_autograd_with_the_weight_of_the_factors():
+    """The whole step, its gradients and what its clipping bounds; tolerances as for the step in test_gpu_step.py."""
+    s = M.Sizes(tokens=333, d=136, inter=264, vocab=1003, layers=2, r=32, alpha=0.8, max_norm=0.25, heads=6, kv_heads=2, head_dim=24, docs=4, tied=True)
+    model = M.MlpLm(s)
+    ids, y = M.synthetic_batch(s)
+    offsets = offsets_of(1, 130, 130, 300)      # one token, 129, none, 170; the last 33 tokens are padding
+    total = model.forward(ids, y, offsets=offsets)
+    dh0 = model.backward()
+    assert B.acx_last_device_status() == B.ACX_OK
+    loss, p = reference(model, ids, y, offsets)
+    norm, f = model.norm.double().tolist()
+    assert abs(float(total[0] / total[1]) - float(loss.detach())) <= 1e-2 * float(loss.detach())
+    tol = 6e-2
+    assert rel(dh0, p["h0"].grad) <= tol
+    assert 0 < f < 1 and abs(norm * f - s.max_norm) <= 1e-6 * s.max_norm
+    assert rel(model.grads["head"][0] / f, p["head"].grad) <= tol
+    for k in ("w_pre", "w_post", "gate"):
+        for a, b in zip(model.grads[k], p[k]):
+            assert rel(a / f, b.grad) <= tol, k
+    # the norm is that of what was clipped, a factor counted as A S^T is on average: every bf16 element off by 2^-8 at most, of its own size
+    square = lambda t: float(t.double().square().sum())  # noqa: E731
+    clipped = sum(square(t) for ts in model.grads.values() for t in ts)
+    clipped += sum((model.w[l][k].shape[1] + s.r + 1) / s.r * square(a) for l in range(s.layers) for k, a in model.factors[l].items())
+    assert abs(clipped ** 0.5 - s.max_norm) <= 2.0 ** -8 * s.max_norm
+    # |A|^2 is |dW|^2 on average.  One sketch: a standard deviation of sqrt(2 / r) = 25 % at most (dW of rank one), three of them.
+    for l, lw in enumerate(p["w"]):
+        for k, w in lw.items():
+            got = square(model.factors[l][k].double() / f) / square(w.grad)
+            assert 0.25 < got < 1.75, (l, k, got)
+
+
+SIZES = dict(tokens=256, d=128, inter=256, vocab=301, layers=2, r=32, heads=4, kv_heads=1, head_dim=32, docs=3, tied=True)

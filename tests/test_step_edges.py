@@ -19,6 +19,33 @@ def built():
     acx_build.build()
 
 
+@pytest.mark.parametrize("d_in,r", [(136, 32), (264, 32), (896, 64)])
+def test_weight_of_a_factor_is_what_its_gradient_has_on_average(d_in, r):
+    """A = dW S: ||A S^T||^2 over ||A||^2, over forty sketches.  For one row of dW and y = S^T x it is |y|^2 + chi^2 (d_in - 1 degrees) / r:
+    relative deviation sqrt(2 (d_in + r - 1)) / (d_in + r + 1), about sqrt(2 / (d_in + r)); four of them over sqrt(40)."""
+    dW = np.random.default_rng(0).normal(size=(5, d_in))
+    whole = factors = 0.0
+    for seed in range(40):
+        S = sk.sketch_for_dtype(seed, d_in, r, "bf16")
+        A = dW @ S
+        whole, factors = whole + ((A @ S.T) ** 2).sum(), factors + (A ** 2).sum()
+    assert abs(whole / factors / B.grad_factor_weight(d_in, r) - 1) <= 4 * (2 / (d_in + r) / 40) ** 0.5
+
+
+def test_the_step_counts_its_factors_so(monkeypatch):
+    lists = []
+    monkeypatch.setattr(B, "make_grad_list", lambda tensors, weights: lists.append((tensors, weights)))
+    monkeypatch.setattr(B, "alloc_grad_workspace", lambda grads: None)
+    s = M.Sizes(tokens=32, d=64, inter=128, vocab=100, layers=2, r=16, heads=2, kv_heads=1, head_dim=24, max_norm=1.0)
+    model = M.MlpLm(s, device="cpu")
+    (tensors, weights), = lists
+    of = {t.data_ptr(): w for t, w in zip(tensors, weights)}
+    for l in range(s.layers):
+        for k, d_in in (("gu", 64), ("dn", 128), ("qkv", 64), ("o", 48)):
+            assert of.pop(model.factors[l][k].data_ptr()) == (d_in + 17) / 16
+    assert set(of.values()) == {1.0} and len(of) == sum(len(t) for t in model.grads.values())
+
+
 def test_clipping_without_tensors_has_no_chunks():
     """A descriptor that no list has: its chunks would be read from a plan that nothing asked for."""
     d = B.acx_grad_desc(ctypes.sizeof(B.acx_grad_desc), 0, 0, 5)
