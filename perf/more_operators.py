@@ -118,8 +118,8 @@ def _gradients(case):
     d, kv, n, r = c["d"], c["kv"], c["inter"], c["r"]
     out = []
     for _ in range(c["layers"]):
-        # factors A (outputs x r) of q, k, v, o, gate, up, down: the squared norm of A S^T is d_in / r times A's on average
-        out += [(o * r, "f32", i / r) for o, i in ((d, d), (kv, d), (kv, d), (d, d), (n, d), (n, d), (d, n))]
+        # factors A (outputs x r) of q, k, v, o, gate, up, down: the squared norm of A S^T is (d_in + r + 1) / r times A's on average
+        out += [(o * r, "f32", (i + r + 1) / r) for o, i in ((d, d), (kv, d), (kv, d), (d, d), (n, d), (n, d), (d, n))]
         out += [(d, "f32", 1.0)] * 2
     return out + ([(c["vocab"] * d, "bf16", 1.0)] if c["vocab"] else [])
 
