@@ -478,7 +478,7 @@ ACX_API acx_status acx_grad_clip(const acx_grad_desc* desc, const void* plan, si
                                  size_t ws_bytes, void* cuda_stream);
 
 /* Synchronises the stream and returns ACX_ERR_TIMEOUT if any kernel on this device since the last call gave up on
- * a bounded wait (its outputs are then undefined), ACX_ERR_INVALID_ARG if one found a plan of another batch's sizes,
+ * a bounded wait (its outputs are then undefined), else ACX_ERR_INVALID_ARG if one found a plan of another batch's sizes,
  * ACX_ERR_CUDA on a CUDA error, else ACX_OK.  Clears the flag.  The
  * flag is one word per device: a kernel on any stream sets it, so the answer is about the device, not only about
  * `cuda_stream` (which is the stream that is synchronised first). */

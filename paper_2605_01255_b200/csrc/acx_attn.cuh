@@ -226,7 +226,8 @@ __device__ __forceinline__ void store_f32(float* at, const uint32_t (&v)[32], fl
 __device__ __forceinline__ bool plan_fits(const Params& p) {
   const int4 made = __ldcg(reinterpret_cast<const int4*>(p.plan) + 1);
   const bool fits = made.x == p.tokens && made.y == p.docs && made.z == p.causal;
-  if (!fits && blockIdx.x == 0 && threadIdx.x == 0) atomicExch(p.status, kDevBadInput);
+  // (a wait that ran out, here or in another kernel, weighs more: its word stays)
+  if (!fits && blockIdx.x == 0 && threadIdx.x == 0) atomicCAS(p.status, kDevOk, kDevBadInput);
   return fits;
 }
 

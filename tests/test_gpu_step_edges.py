@@ -34,6 +34,23 @@ def run(desc, offsets, q, k, v, do, prefix=None, slopes=None):
     return [o, lse.T.contiguous(), *g]
 
 
+# --------------------------------------------------------------------------------------------------------------- status
+def test_a_refused_plan_does_not_hide_a_wait_that_ran_out():
+    q, k, v, do = inputs(300, 2, 1, 64)
+    desc = B.make_attn_desc(300, 2, 1, 64, 2)
+    plan = B.alloc_attn_workspace(desc, B.ACX_OP_ATTN_PLAN)
+    o = torch.empty_like(q)
+    refused = lambda: B.acx_attn_fwd(desc, q, k, v, plan.zero_(), o)  # noqa: E731
+    assert B.acx_last_device_status() == B.ACX_OK
+    for calls in ((refused, 0), (0, refused), (refused, 0, refused)):
+        for call in calls:
+            call() if call else B.acx_debug_expired_wait(1_000_000)      # 1 ms on a barrier nobody signals
+        assert B.acx_last_device_status() == B.ACX_ERR_TIMEOUT
+        assert B.acx_last_device_status() == B.ACX_OK
+    refused()
+    assert B.acx_last_device_status() == B.ACX_ERR_INVALID_ARG
+
+
 # ------------------------------------------------------------------------------------------------------ the training step
 def test_step_against_autograd_with_the_weight_of_the_factors():
     """The whole step, its gradients and what its clipping bounds; tolerances as for the step in test_gpu_step.py."""
