@@ -453,7 +453,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
         // rows behind the document's end, of another document, change nothing of the others' roundings.)
         const bool above = row < t.end && !(mx <= m + 8.f);
         if (j == n - 1) {
-          m = mx;
+          m = max_nan(mx, -3.402823466e38f);   // (a tile whose scores are all minus infinity: weights of zero, and tiles to come may have others)
         } else if (__any_sync(0xFFFFFFFFu, above)) {
           ptx::tcgen05_fence_after_sync();
           const float m_new = above ? max_nan(m, mx) : m, f = above ? exp2_fast(m - m_new) : 1.f;

@@ -34,6 +34,39 @@ def run(desc, offsets, q, k, v, do, prefix=None, slopes=None):
     return [o, lse.T.contiguous(), *g]
 
 
+# ------------------------------------------------------------------------------------------ scores at the ends of the range
+@pytest.mark.parametrize("T,hidden", [(300, (100, 300)), (300, (128, 256)), (1000, (0, 990)), (700, (384, 700))])
+@pytest.mark.parametrize("d,slopes", [(64, False), (128, False), (64, True)])
+def test_keys_whose_scores_are_minus_infinity_have_no_weight(T, hidden, d, slopes):
+    """A mask written into a channel: the lowest bfloat16 times a query's 2 is beyond fp32.  Whole tiles of keys are such, the first that
+    is taken among them; what is left has the weights, the gradients and the sums it has without them."""
+    H, (n0, n1) = 2, hidden
+    q, k, v, do = inputs(T, H, 1, d)
+    keep = torch.ones(T, dtype=torch.bool, device="cuda")
+    keep[n0:n1] = False
+    q[:, :, 0] = 2.0
+    k[:, :, 0] = torch.where(keep, 0.0, torch.finfo(BF).min)[:, None].to(BF)
+    slope = torch.tensor([0.25, 0.01], device="cuda") if slopes else None
+    o, lse, dq, dk, dv = run(B.make_attn_desc(T, H, 1, d, causal=False), offsets_of(T), q, k, v, do, slopes=slope)
+    assert all(torch.isfinite(t).all() for t in (o, lse, dq, dk, dv))
+    assert not dk[~keep].any() and not dv[~keep].any()
+    pos = torch.arange(T, device="cuda").double()
+    for h in range(H):
+        Q, K, V, G = q[:, h].double(), k[keep, 0].double(), v[keep, 0].double(), do[:, h].double()
+        z = Q @ K.T * d ** -0.5
+        if slopes:
+            z = z - slope[h].double() * (pos[:, None] - pos[keep][None, :]).abs()
+        p = torch.softmax(z, 1)
+        # p rounded once and o once: 2^-8 of sum p |v| and of o; fp32 in between
+        assert ((o[:, h].double() - p @ V).abs() <= 2.0 ** -8 * 2.1 * (p @ V.abs()) + 1e-5).all()
+        assert ((lse[:, h].double() - torch.logsumexp(z, 1)).abs() <= 1e-4).all()
+        ds = p * (G @ V.T - ((G @ V.T) * p).sum(1, keepdim=True)) * d ** -0.5
+        # dS once, the output once, and delta off by what rounding o leaves of it: 2^-8 |dO| |o| of every p
+        lost = 2.0 ** -8 * 2 * (G.abs() * (p @ V.abs())).sum(1, keepdim=True)
+        err = 2.0 ** -8 * 1.1 * ds.abs() + p * lost * d ** -0.5
+        assert ((dq[:, h].double() - ds @ K).abs() <= 2.0 ** -8 * (ds @ K).abs() + err @ K.abs() + 1e-5).all()
+
+
 # --------------------------------------------------------------------------------------------------------------- status
 def test_a_refused_plan_does_not_hide_a_wait_that_ran_out():
     q, k, v, do = inputs(300, 2, 1, 64)
