@@ -414,7 +414,8 @@ ACX_API acx_status acx_attn_fwd(const acx_attn_desc* desc, const void* Q, int64_
 /* Gradients of the forward at Q, K, V (the same plan, slopes and descriptor; O and lse as it left them).
  *   dO [tokens][heads][head_dim] in;  dQ, dK, dV out, shaped as Q, K, V, none of them in the place of an input;  ws/ws_bytes:
  *   ACX_OP_ATTN_BWD.
- * The probabilities are taken from lse again, to 2^-22 |lse| relative: scores far beyond some 10^4 have no gradients of use.
+ * The probabilities are taken from lse again, to 2^-22 |lse| relative, and bounded by 1: gradients through scores far beyond some 10^4
+ * are of no use, but numbers.
  * Fixed summation order, no atomics: reproducible bits. */
 ACX_API acx_status acx_attn_bwd(const acx_attn_desc* desc, const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv,
                                 const float* slopes, const void* plan, size_t plan_bytes, const void* O, int64_t ldo, const void* dO, int64_t lddo,

@@ -44,6 +44,11 @@ constexpr int kRowWarp0 = 4, kRowWarps = 16, kThreads = 32 * (kRowWarp0 + kRowWa
 constexpr int kPanel = 32;        // columns of a tile that one warp takes
 constexpr int kPanels = kRows / kPanel;
 constexpr int kFewTokens = 512;
+// A probability 2^(x - lse) is at most 1, but x and lse are known to some 2^-22 of their size only: above this size (where that is
+// 2^-10) a probability is bounded.  Unbounded, one of scores of 1e8 was up to 2^9, one of 1e10 an infinity, which times a dO of zero
+// made every key's gradient NaN.  By row, not by warp: a row's bits do not depend on its neighbours.
+constexpr float kLargeLse = 4096.f;
+__device__ __forceinline__ float bounded_exponent(float x, float lse2) { return fabsf(lse2) > kLargeLse ? min_nan(x, 0.f) : x; }
 
 // ------------------------------------------------------------------------------------------------------------------ delta
 // delta[head][token] = sum of dO O over the head's columns.  Sixteen lanes per row.
@@ -388,6 +393,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         lse2 = live ? __ldcg(p.lse + at) * kLog2e : 0.f;
         delta = live ? __ldcg(p.delta + at) : 0.f;
       }
+      const bool large_row = !KEYS && __any_sync(0xFFFFFFFFu, fabsf(lse2) > kLargeLse);
       for (int h = w.head; ok && h < w.head + w.heads; ++h) {
         const float slope2 = BIAS ? __ldg(p.slopes + h) * kLog2e : 0.f;
         for (int i = 0; i < w.tiles; ++i, ++turns) {
@@ -412,8 +418,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           // dx/ds of the cap, as fp16: 2^-12 of it is little beside the rounding of dS
           __half2 slopes[CAP ? 16 : 1];
           uint32_t pk[16];
-          auto probabilities = [&](auto with_mask, auto is_small) {
-            constexpr bool kMask = decltype(with_mask)::value, kSmall = decltype(is_small)::value;
+          auto probabilities = [&](auto with_mask, auto is_small, auto is_large) {
+            constexpr bool kMask = decltype(with_mask)::value, kSmall = decltype(is_small)::value, kLarge = decltype(is_large)::value;
 #pragma unroll
             for (int i4 = 0; i4 < 8; ++i4) {
               float l[4] = {lse2, lse2, lse2, lse2};
@@ -433,6 +439,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                 };
                 x[0] = make_float2(at(0), at(1));
                 x[1] = make_float2(at(2), at(3));
+              }
+              if (kLarge) {
+                x[0] = make_float2(bounded_exponent(x[0].x, l[0]), bounded_exponent(x[0].y, l[1]));
+                x[1] = make_float2(bounded_exponent(x[1].x, l[2]), bounded_exponent(x[1].y, l[3]));
               }
 #pragma unroll
               for (int k = 0; k < 2; ++k) {
@@ -460,9 +470,13 @@ __global__ void __launch_bounds__(kThreads, 1)
               for (int k = 0; k < 32; ++k) s[k] = 0u;
             }
           };
-          if (masked) probabilities(std::true_type{}, std::false_type{});
-          else if (CAP && small_scores(p, s)) probabilities(std::false_type{}, std::true_type{});
-          else probabilities(std::false_type{}, std::false_type{});
+          constexpr std::true_type yes{};
+          constexpr std::false_type no{};
+          // (the mask's bounds hold for tiles without one too: one form for all that is large)
+          if (KEYS ? __any_sync(0xFFFFFFFFu, fabsf(vec[lane]) > kLargeLse) : large_row) probabilities(yes, no, yes);
+          else if (masked) probabilities(yes, no, no);
+          else if (CAP && small_scores(p, s)) probabilities(no, yes, no);
+          else probabilities(no, no, no);
           // P to shared memory: this row's 64 bytes of the panel's 64-column chunk
           if (!warp_wait(p_free, (turns & 1) ^ 1u, abort_flag)) { give_up(); ok = false; break; }
 #pragma unroll

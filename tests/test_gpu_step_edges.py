@@ -67,6 +67,41 @@ def test_keys_whose_scores_are_minus_infinity_have_no_weight(T, hidden, d, slope
         assert ((dq[:, h].double() - ds @ K).abs() <= 2.0 ** -8 * (ds @ K).abs() + err @ K.abs() + 1e-5).all()
 
 
+@pytest.mark.parametrize("size", [1e5, 1e8, 1e30])
+@pytest.mark.parametrize("d,cap,slopes,causal", [(64, 0.0, False, True), (128, 0.0, False, False), (64, 0.0, True, True), (64, 1e31, False, True)])
+def test_gradients_beside_scores_that_fp32_cannot_tell_apart(size, d, cap, slopes, causal):
+    """Queries whose scores are far beyond 2^24 have probabilities of no use in the backward pass, but of no more than 1: all gradients
+    are numbers, and where such queries have no gradient of their own, those of the keys are what the other queries make of them."""
+    T, H, n = 300, 2, 100
+    desc, offsets = B.make_attn_desc(T, H, 1, d, causal=causal, softcap=cap), offsets_of(T)
+    slope = torch.tensor([0.25, 0.01], device="cuda") if slopes else None
+    q, k, v, do = inputs(T, H, 1, d)
+    want = run(desc, offsets, q, k, v, torch.cat([torch.zeros_like(do[:n]), do[n:]]), slopes=slope)
+    g = torch.Generator().manual_seed(9)
+    q[:n] = (size * torch.randn(n, H, d, generator=g)).to(BF).cuda()
+    got = run(desc, offsets, q, k, v, do, slopes=slope)
+    assert all(torch.isfinite(t).all() for t in got)
+    do[:n] = 0
+    got = run(desc, offsets, q, k, v, do, slopes=slope)
+    assert all(torch.isfinite(t).all() for t in got) and not got[2][:n].any()
+    # the same sums: products of zero beside them
+    for a, b in zip(got[2:], want[2:]):
+        assert torch.equal(a[n:] if a is got[2] else a, b[n:] if b is want[2] else b)
+
+
+def test_keys_of_minus_1e30_have_finite_gradients():
+    T, H, d, n = 300, 2, 64, 100
+    desc, offsets = B.make_attn_desc(T, H, 1, d), offsets_of(T)
+    q, k, v, do = inputs(T, H, 1, d)
+    q[:], k[:n] = 1.0, -1e30
+    o, lse, dq, dk, dv = run(desc, offsets, q, k, v, do)
+    assert all(torch.isfinite(t).all() for t in (o, lse, dq, dk, dv))
+    do[:n] = 0                       # the queries that see nothing else
+    o, lse, dq, dk, dv = run(desc, offsets, q, k, v, do)
+    assert all(torch.isfinite(t).all() for t in (o, lse, dq, dk, dv))
+    assert not dq[:n].any() and not dk[:n].any() and not dv[:n].any()
+
+
 # --------------------------------------------------------------------------------------------------------------- status
 def test_a_refused_plan_does_not_hide_a_wait_that_ran_out():
     q, k, v, do = inputs(300, 2, 1, 64)
