@@ -407,7 +407,7 @@ ACX_API acx_status acx_attn_plan(const acx_attn_desc* desc, const int32_t* offse
  * Scores that the mask takes out may be anything.  Values of a document's own tokens have to be finite, though: a weight of zero
  * times a NaN or an infinity is a NaN, for any query within 127 tokens before such a one.
  * Scores and sums are fp32; the probabilities enter the second product rounded to bfloat16, as dS = p (dP - delta) does in the
- * backward; every output is rounded once. */
+ * backward (into dK of a document of up to 512 tokens as two bfloat16, to 2^-16); every output is rounded once. */
 ACX_API acx_status acx_attn_fwd(const acx_attn_desc* desc, const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv,
                                 const float* slopes, const void* plan, size_t plan_bytes, void* O, int64_t ldo, float* lse, void* cuda_stream);
 

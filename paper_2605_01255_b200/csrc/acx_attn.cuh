@@ -81,7 +81,6 @@ struct Params {
   int64_t lddq, lddk, lddv;
   float *dk_part, *dv_part;  // [part][tokens][kv_heads][d], or null: one part, written to dK and dV
   int parts, heads_per_part;
-  int two_parts;             // dS of the keys' launch as the sum of two bf16
 };
 
 __device__ __forceinline__ float2 unpack2(uint32_t v) { return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u)); }

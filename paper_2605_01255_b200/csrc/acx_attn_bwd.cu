@@ -23,8 +23,9 @@
 //
 // A query that sees one key only has p = 1 and no gradient through its scores: exactly zero, not the difference of two roundings.
 //
-// Of a few tokens (kFewTokens) dS goes into dK as two bf16 parts, the rounded one and what is left: nothing averages out between so few
-// queries, and a launch of that size is all latency.  Errors of dK 0.0023 to 0.0025 -> 0.0017, its own rounding; the backward of 256 tokens
+// Of a document of a few tokens (kFewTokens) dS goes into dK as two bf16 parts, the rounded one and what is left: nothing averages out between so few
+// queries.  It is the document that decides, not the batch: the same one has the same errors (and, where a group's heads are not dealt to
+// parts, the same bits) whatever stands beside it.  Errors of dK 0.0023 to 0.0025 -> 0.0017, its own rounding; the backward of 256 tokens
 // x 14 heads x 64 20.2 -> 20.5 us, 512 x 8 x 64 23.7 -> 24.7, but 2048 x 6 x 128 80 -> 85 and 8192 x 24 x 128 1323 -> 1434.
 //
 // Where a batch has few key tiles for the SMs a group's query heads are dealt to several work items, whose fp32 sums a last kernel adds
@@ -108,6 +109,9 @@ struct Smem {
   static constexpr int kBars = kExchange + (KEYS ? 0 : kPartBytes), kBytes = kBars + 256;
   static_assert(kBytes <= 232448, "shared memory of one CTA");
 };
+
+// Whether dS goes into dK in two parts.
+__device__ __forceinline__ bool two_parts(const Item& t) { return t.end - t.start <= kFewTokens; }
 
 // What one work item goes through.
 struct Unit {
@@ -308,7 +312,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!wait(ds_full, turns & 1)) break;
         ptx::tcgen05_fence_after_sync();
         rows_mma<HD, 16>(tmem_second, tmem_dp, t0_tiles + a.stage * T::kBytes, steps, d16, i > 0);
-        if (KEYS && p.two_parts) rows_mma<HD, 16>(tmem_second, tmem_dp + 16, t0_tiles + a.stage * T::kBytes, steps, d16, true);
+        if (KEYS && two_parts(w.t)) rows_mma<HD, 16>(tmem_second, tmem_dp + 16, t0_tiles + a.stage * T::kBytes, steps, d16, true);
         ptx::umma_commit_elected(t0_empty(a.stage));
         if (i == n - 1) ptx::umma_commit_elected(out_full);
         if (i + 1 < n) {
@@ -527,7 +531,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
           ptx::tmem_st_x16(dp_at, pk);
-          if (KEYS && p.two_parts) {   // what the rounding left
+          if (KEYS && two_parts(w.t)) {   // what the rounding left
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               const float2 l = q8::add2(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), neg2(unpack2(pk[i])));
@@ -744,7 +748,6 @@ cudaError_t attn_bwd(const AttnProblem& q, const AttnMatrix& Q, const AttnMatrix
   pk.items = reinterpret_cast<const Item*>(plan8 + at.keys);
   const unsigned grid_q = unsigned(std::min<int64_t>(at.tile_cap * q.heads, sm_count()));
   const unsigned grid_k = unsigned(std::min<int64_t>(at.tile_cap * q.kv_heads * kp.parts, sm_count()));
-  pk.two_parts = q.tokens <= kFewTokens;
   const bool cap = q.softcap > 0.f, bias = slopes != nullptr;
   e = q.d <= 64 ? launch_both<64>(cap, bias, m, p, grid_q, pk, grid_k, st) : launch_both<128>(cap, bias, m, p, grid_q, pk, grid_k, st);
   if (e != cudaSuccess || kp.parts == 1) return e;
