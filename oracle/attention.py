@@ -23,10 +23,12 @@ def seen(start, end, prefix_end, causal):
     return (i[None, :] <= i[:, None]) | (i[None, :] < prefix_end)
 
 
-def attention(q, k, v, offsets, *, causal=True, prefix=None, scale=None, softcap=0.0, slopes=None, do=None):
+def attention(q, k, v, offsets, *, causal=True, prefix=None, scale=None, softcap=0.0, slopes=None, do=None,
+              slope_error=(0.0, 2.0 ** -18)):
     """q [tokens, heads, d], k, v [tokens, kv_heads, d].  A dict of o, lse and, with do, dq, dk, dv; each with the largest error that
     the roundings of a bf16 implementation may make (`*_bound`): every stored value once, the probabilities and their gradients once
-    before they are multiplied (2^-8 of the value each), fp32 in between."""
+    before they are multiplied (2^-8 of the value each), fp32 in between.  slope_error: what the cap's slope may be off by, relatively
+    and absolutely."""
     q, k, v = (np.asarray(x, dtype=np.float64) for x in (q, k, v))
     T, H, d = q.shape
     group = H // k.shape[1]
@@ -73,7 +75,7 @@ def attention(q, k, v, offsets, *, causal=True, prefix=None, scale=None, softcap
             lost = (np.abs(G) * ob).sum(1, keepdims=True) + 2.0 ** -18 * (np.abs(G) @ np.abs(V).T + np.abs(delta))
             lost = p * lost * slope
             if softcap:
-                lost = lost + 2.0 ** -18 * p * np.abs(dp - delta) * scale     # 1 - tanh^2 is right to a few 2^-23, absolutely
+                lost = lost + p * np.abs(dp - delta) * (slope_error[0] * slope + slope_error[1] * scale)
             ds_err = (r + rel) * np.abs(ds) + lost
             single = mask.sum(1) == 1
             ds_err[single] = 0.0                          # the gradient of a softmax over one key is zero, exactly

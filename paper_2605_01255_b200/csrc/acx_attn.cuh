@@ -69,8 +69,8 @@ struct Params {
   const float* slopes;       // [heads], BIAS only
   float scale;
   float c;                   // scale log2(e): x = c s without a cap
-  float cap_in;              // scale / cap: the tanh's argument per unit of s
-  float cap_out;             // cap log2(e)
+  float cap_in;              // 2^7 scale / cap: the tanh's argument per unit of s
+  float cap_out;             // 2^-7 cap log2(e)
   float* lse;                // [heads][tokens], natural logarithm
   int* status;
   __nv_bfloat16* O;
@@ -112,39 +112,50 @@ __device__ __forceinline__ float rcp_fast(float x) {
   return y;
 }
 
-// tanh.  1 - 2 / (1 + e^2u) keeps about 2^-23 absolutely, which is too little near zero once a large cap multiplies it; up to 0.75
-// an odd polynomial, fitted to tanh(u) / u (relative error 1.4e-9 before rounding), takes over.  SMALL: all arguments are below that.
+// 2^7 tanh(2^-7 u), and tanh' in units of 2^-14: with t for the former the latter is 2^14 - t^2.  With r = 1 / (1 + e^2|v|), v = 2^-7 u, they are
+// 1 - 2 r and 4 r (1 - r): the latter keeps its digits where the tanh saturates (1 - tanh^2 loses them: 6 % at v = 8).  The former keeps
+// about 2^-23 absolutely, which is too little near zero once a large cap multiplies it; up to 0.75 an odd polynomial, fitted to
+// tanh(v) / v (relative error 1.2e-8 before rounding), takes over.  SMALL: all arguments are below that.
+constexpr float kTanhUnit = 128.f, kSlopeUnit = kTanhUnit * kTanhUnit;
 template <bool SMALL>
-__device__ __forceinline__ float tanh_of(float u) {
+__device__ __forceinline__ float tanh_of(float u, float* slope) {
+  constexpr float c1 = 1.f / kSlopeUnit, c2 = c1 * c1, c3 = c2 * c1, c4 = c3 * c1, c5 = c4 * c1, c6 = c5 * c1;
   const float q = u * u;
-  float t = fmaf(q, fmaf(q, fmaf(q, fmaf(q, fmaf(q, 1.7277066e-3f, -7.6394570e-3f), 2.1438753e-2f), -5.3887937e-2f), 0.13332610f), -0.33333308f);
+  float t = fmaf(q, fmaf(q, fmaf(q, fmaf(q, fmaf(q, 1.7277066e-3f * c6, -7.6394570e-3f * c5), 2.1438753e-2f * c4), -5.3887937e-2f * c3), 0.13332610f * c2),
+                 -0.33333308f * c1);
   t = fmaf(u * q, t, u);
-  if (SMALL) return t;
-  const float r = 1.f - 2.f * rcp_fast(1.f + exp2_fast(u * (2.f * kLog2e)));
-  return fabsf(u) < 0.75f ? t : r;
+  if (SMALL) {
+    if (slope) *slope = fmaf(-t, t, kSlopeUnit);
+    return t;
+  }
+  const float r = rcp_fast(1.f + exp2_fast(fabsf(u) * (2.f * kLog2e / kTanhUnit)));
+  if (slope) {
+    const float f = 4.f * kSlopeUnit * r;
+    *slope = fmaf(-f, r, f);
+  }
+  return fabsf(u) < 0.75f * kTanhUnit ? t : copysignf(fmaf(-2.f * kTanhUnit, r, kTanhUnit), u);
 }
 
-// x of a raw score s; `far` = query position - key position.  For CAP, *slope = d x / d s in units of c.
+// x of a raw score s; `far` = query position - key position.  For CAP, *slope = d x / d s in units of 2^-14 c.
 template <bool CAP, bool BIAS, bool SMALL>
 __device__ __forceinline__ float exponent(const Params& p, float s, float far, float slope2, float* slope = nullptr) {
   float x;
   if (CAP) {
-    const float t = tanh_of<SMALL>(s * p.cap_in);
-    x = t * p.cap_out;
-    if (slope) *slope = fmaf(-t, t, 1.f);
+    x = tanh_of<SMALL>(s * p.cap_in, slope) * p.cap_out;
   } else {
     x = s * p.c;
   }
   if (BIAS) x = fmaf(-slope2, fabsf(far), x);
   return x;
 }
-// Whether the tanh's polynomial alone does for a warp's scores.
+// Whether the tanh's polynomial alone does for the scores of a warp's rows inside the document (the slopes that the two forms give may
+// differ in their last bit, and other documents decide nothing here).
 template <int N>
-__device__ __forceinline__ bool small_scores(const Params& p, const uint32_t (&s)[N]) {
+__device__ __forceinline__ bool small_scores(const Params& p, const uint32_t (&s)[N], bool live) {
   float top = 0.f;
 #pragma unroll
   for (int i = 0; i < N; ++i) top = fmaxf(top, fabsf(__uint_as_float(s[i])));
-  return __all_sync(0xFFFFFFFFu, top * p.cap_in < 0.75f);
+  return __all_sync(0xFFFFFFFFu, !live || top * p.cap_in < 0.75f * kTanhUnit);
 }
 
 // A wait of a whole warp, which it leaves together: what follows (tensor memory loads and stores) has to be executed by converged

@@ -49,7 +49,11 @@ constexpr int kFewTokens = 512;
 // 2^-10) a probability is bounded.  Unbounded, one of scores of 1e8 was up to 2^9, one of 1e10 an infinity, which times a dO of zero
 // made every key's gradient NaN.  By row, not by warp: a row's bits do not depend on its neighbours.
 constexpr float kLargeLse = 4096.f;
-__device__ __forceinline__ float bounded_exponent(float x, float lse2) { return fabsf(lse2) > kLargeLse ? min_nan(x, 0.f) : x; }
+__device__ __forceinline__ float bounded_exponent(float x, float lse2, float top) { return fabsf(lse2) > kLargeLse ? min_nan(x, top) : x; }
+// With a cap the probabilities are 2^-14 of what they are and its slopes 2^14, as fp16: those from 2^-28 on have all digits of that (a score
+// of 10.4 caps), and their product is dS.  The exponents get -14 with lse; dV and the sums of p (dP - delta) are put right at their end.
+constexpr float kCapShift = 14.f;
+static_assert(kSlopeUnit == 16384.f, "2^kCapShift");
 
 // ------------------------------------------------------------------------------------------------------------------ delta
 // delta[head][token] = sum of dO O over the head's columns.  Sixteen lanes per row.
@@ -347,7 +351,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int k = 0; k < 4; ++k) {
               const int row = w.other0 + i * kRows + 32 * k + lane;
               const int64_t at = int64_t(h) * p.tokens + row;
-              a[k] = row < w.t.end ? __ldcg(p.lse + at) * kLog2e : 0.f;   // behind the document's end: masked
+              a[k] = row < w.t.end ? fmaf(__ldcg(p.lse + at), kLog2e, CAP ? kCapShift : 0.f) : 0.f;   // behind the document's end: masked
               b[k] = row < w.t.end ? __ldcg(p.delta + at) : 0.f;
             }
             if (!warp_wait(vec_empty(s.stage), s.phase ^ 1u, abort_flag)) { give_up(); ok = false; break; }
@@ -394,7 +398,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       float2 rest2 = make_float2(0.f, 0.f), kept2 = rest2;   // sums of p (dP - delta), and of what dS's rounding makes of them
       if (!KEYS) {
         const int64_t at = int64_t(w.head) * p.tokens + row;
-        lse2 = live ? __ldcg(p.lse + at) * kLog2e : 0.f;
+        lse2 = live ? fmaf(__ldcg(p.lse + at), kLog2e, CAP ? kCapShift : 0.f) : 0.f;
         delta = live ? __ldcg(p.delta + at) : 0.f;
       }
       const bool large_row = !KEYS && __any_sync(0xFFFFFFFFu, fabsf(lse2) > kLargeLse);
@@ -419,7 +423,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
           const bool masked = c0 < all_first || c0 + kPanel > all_last;
           const int lo = first - c0, hi = last - c0;
-          // dx/ds of the cap, as fp16: 2^-12 of it is little beside the rounding of dS
+          // dx/ds of the cap, as fp16: off by 2^-11 at most, beside the 2^-8 of dS
           __half2 slopes[CAP ? 16 : 1];
           uint32_t pk[16];
           auto probabilities = [&](auto with_mask, auto is_small, auto is_large) {
@@ -431,7 +435,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const float4 v = *reinterpret_cast<const float4*>(vec + 4 * i4);
                 l[0] = v.x; l[1] = v.y; l[2] = v.z; l[3] = v.w;
               }
-              float e[4], slope[4] = {1.f, 1.f, 1.f, 1.f};
+              float e[4], slope[4];
               auto score = [&](int k) { return make_float2(__uint_as_float(s[4 * i4 + k]), __uint_as_float(s[4 * i4 + k + 1])); };
               const float2 x01 = q8::fma2(score(0), q8::both(p.c), make_float2(-l[0], -l[1])),
                            x23 = q8::fma2(score(2), q8::both(p.c), make_float2(-l[2], -l[3]));
@@ -445,8 +449,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 x[1] = make_float2(at(2), at(3));
               }
               if (kLarge) {
-                x[0] = make_float2(bounded_exponent(x[0].x, l[0]), bounded_exponent(x[0].y, l[1]));
-                x[1] = make_float2(bounded_exponent(x[1].x, l[2]), bounded_exponent(x[1].y, l[3]));
+                constexpr float kTop = CAP ? -kCapShift : 0.f;
+                x[0] = make_float2(bounded_exponent(x[0].x, l[0], kTop), bounded_exponent(x[0].y, l[1], kTop));
+                x[1] = make_float2(bounded_exponent(x[1].x, l[2], kTop), bounded_exponent(x[1].y, l[3], kTop));
               }
 #pragma unroll
               for (int k = 0; k < 2; ++k) {
@@ -479,7 +484,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           // (the mask's bounds hold for tiles without one too: one form for all that is large)
           if (KEYS ? __any_sync(0xFFFFFFFFu, fabsf(vec[lane]) > kLargeLse) : large_row) probabilities(yes, no, yes);
           else if (masked) probabilities(yes, no, no);
-          else if (CAP && small_scores(p, s)) probabilities(no, yes, no);
+          else if (CAP && small_scores(p, s, live)) probabilities(no, yes, no);
           else probabilities(no, no, no);
           // P to shared memory: this row's 64 bytes of the panel's 64-column chunk
           if (!warp_wait(p_free, (turns & 1) ^ 1u, abort_flag)) { give_up(); ok = false; break; }
@@ -553,7 +558,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!KEYS) {
         // r of the row: the panels' parts, [0] + [2] and [1] + [3] first (room for two)
         float2 rest = make_float2(rest2.x + rest2.y, kept2.x + kept2.y);
-        if (CAP) rest.y += rest.x;
+        if (CAP) {
+          rest.x *= kSlopeUnit;
+          rest.y += rest.x;
+        }
         float2* part = reinterpret_cast<float2*>(gen + M::kExchange);
         if (!warp_wait(parts_free, (it & 1) ^ 1u, abort_flag)) { give_up(); break; }   // those of the item before have been read
         if (panel < 2) part[panel * kRows + r] = rest;
@@ -580,7 +588,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // panels 0 and 1 store dV's halves, 2 and 3 dK's
         const bool dk = panel >= 2;
         const int half = (panel & 1) * (HD / 2);
-        const float f = dk ? p.scale : 1.f;
+        const float f = dk ? p.scale : CAP ? kSlopeUnit : 1.f;
         float* part = dk ? p.dk_part : p.dv_part;
         if (part) part += ((int64_t(w.part) * p.tokens + row) * p.kv_heads + w.kv_head) * p.d;
         __nv_bfloat16* out = (dk ? p.dK + int64_t(row) * p.lddk : p.dV + int64_t(row) * p.lddv) + int64_t(w.kv_head) * p.d;

@@ -389,7 +389,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
                 s[c][i] = __float_as_uint(exponent<CAP, BIAS, decltype(is_small)::value>(p, __uint_as_float(s[c][i]),
                                                                                           float(row - k0) - float(32 * c + i), slope2));
           };
-          if (small_scores(p, s[0]) && small_scores(p, s[1]) && small_scores(p, s[2]) && small_scores(p, s[3])) capped(std::true_type{});
+          const bool live = row < t.end;
+          if (small_scores(p, s[0], live) && small_scores(p, s[1], live) && small_scores(p, s[2], live) && small_scores(p, s[3], live)) capped(std::true_type{});
           else capped(std::false_type{});
         } else if (BIAS) {
           const float2 c2 = q8::both(p.c);
@@ -570,8 +571,8 @@ Params common_params(const AttnProblem& q, const void* plan, const float* slopes
   p.slopes = slopes;
   p.scale = q.scale;
   p.c = q.scale * kLog2e;
-  p.cap_in = q.softcap > 0.f ? q.scale / q.softcap : 0.f;
-  p.cap_out = q.softcap * kLog2e;
+  p.cap_in = q.softcap > 0.f ? q.scale / q.softcap * kTanhUnit : 0.f;
+  p.cap_out = q.softcap * kLog2e / kTanhUnit;
   p.lse = lse;
   p.status = status;
   return p;

@@ -102,6 +102,29 @@ def test_keys_of_minus_1e30_have_finite_gradients():
     assert not dq[:n].any() and not dk[:n].any() and not dv[:n].any()
 
 
+# ------------------------------------------------------------------------------------------------------- saturated caps
+@pytest.mark.parametrize("d,alibi,causal", [(64, False, False), (128, False, True), (64, True, True)])
+@pytest.mark.parametrize("T", [200, 700])
+def test_gradients_through_a_saturated_cap(d, alibi, causal, T):
+    """Scores of 6.5 to 9.5 times the cap, either way: the cap's slope is 4 e^-2|u|, 1e-5 to 2e-8, and the gradients have its digits."""
+    H, cap, g = 2, 10.0, torch.Generator().manual_seed(T)
+    u = (6.5 + 3 * torch.rand(T, 1, 1, generator=g)) * torch.where(torch.rand(T, 1, 1, generator=g) < 0.5, 1.0, -1.0)
+    rnd = lambda h: torch.randn(T, h, d, generator=g)  # noqa: E731
+    q, k = (1 + 0.1 * rnd(H)).to(BF).cuda(), (cap * u * d ** -0.5 * (1 + 0.1 * rnd(1))).to(BF).cuda()
+    v, do = rnd(1).to(BF).cuda(), rnd(H).to(BF).cuda()
+    slopes = torch.tensor([0.05, 0.01], device="cuda") if alibi else None
+    got = dict(zip(("o", "lse", "dq", "dk", "dv"), run(B.make_attn_desc(T, H, 1, d, causal=causal, softcap=cap), offsets_of(T), q, k, v, do, slopes=slopes)))
+    n = lambda t: t.double().cpu().numpy()  # noqa: E731
+    # the slope's own error: half a step of fp16, 2^-11, and as much for fp32 scores, exponential and reciprocal (a score of 95 in
+    # fp32 sums is off by 2^-21 of that, twice as much over the cap in the slope: 2^-16.7); absolutely half a step of fp16 below its range, 2^-39
+    want = oa.attention(n(q), n(k), n(v), [0, T], causal=causal, softcap=cap, slopes=None if slopes is None else n(slopes), do=n(do),
+                        slope_error=(2.0 ** -10, 2.0 ** -39))
+    for name in ("o", "dq", "dk", "dv"):
+        off = np.abs(n(got[name]) - want[name]) - want[name + "_bound"]
+        assert off.max() <= 2.0 ** -22 * np.abs(want[name]).max(), (name, off.max(), np.abs(want[name]).max())
+        assert np.median(want[name + "_bound"]) <= 0.1 * np.abs(want[name]).max(), name      # a bound that says something
+
+
 # ------------------------------------------------------------------------------------------- short documents, long batches
 def test_dk_of_a_document_does_not_depend_on_the_batch():
     """One query head per key head (no parts to join): the same bits in a batch of 500 tokens, of 513 and of 4000."""
