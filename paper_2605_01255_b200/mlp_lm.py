@@ -12,12 +12,14 @@ straight into AdamW (`acx_reconstruct_adamw`), the head's and the vectors' are l
 With `heads` the block has attention over packed documents in front, a sub-block between two norms of its own:
     [Q | K | V] = y Wqkv^T  (factor kept, and Q, K, V),  a = attention within the documents (kept, with its lse),  b = a Wo^T  (factor kept).
 With `tied` the batch is word ids: h_0 = sqrt(d) Whead[ids], whose gradient is added to the head's.  With `max_norm` the gradients of
-all linears (as factors), of the vectors and of the head are clipped together before any weight is updated.
+all linears (as factors), of the vectors and of the head are clipped together before any weight is updated; a step whose norm is not a
+number (an infinity or a NaN among the gradients) is left out, weights, moments and step count as they were.
 
     python -m paper_2605_01255_b200.mlp_lm [steps] [full]     # a few steps on one synthetic batch: the loss falls; full: all of these
 """
 from __future__ import annotations
 
+import math
 import sys
 from dataclasses import dataclass, replace
 from typing import Dict, List
@@ -179,7 +181,8 @@ class MlpLm:
 
     def backward(self, lr: float = 0.0, **hyper) -> torch.Tensor:
         """Gradient of the mean loss with respect to h0; with lr > 0 every linear takes its AdamW step as soon as its factor is
-        known (after the last use of its weights in this pass), or, where gradients are clipped, once all of them are."""
+        known (after the last use of its weights in this pass), or, where gradients are clipped, once all of them are: the host then
+        waits for the norm, and a step whose norm is not a number is left out (in a graph's capture it cannot: every step is taken)."""
         s, n = self.s, self.s.inter
         clip = s.max_norm > 0
         B.acx_linear_ce_bwd(self.ce, self.y, self.head, self.targets, self.lse, self.dy, self.grads["head"][0], loss=self.loss,
@@ -215,6 +218,10 @@ class MlpLm:
             B.acx_embed_bwd(self.table, self.ids, dh0, self.grads["head"][0], beta=1.0, ws=self.ws_table)
         if clip:
             B.acx_grad_clip(self.clip, s.max_norm, self.norm, ws=self.ws_clip)
+            if lr > 0 and not (self.norm.is_cuda and torch.cuda.is_current_stream_capturing()):
+                norm, f = self.norm.tolist()
+                if not math.isfinite(norm) and not f < 1:      # (one beyond fp32 reads as infinity, but has its factor)
+                    return dh0
             for l in range(s.layers):
                 for kind in self.factors[l]:
                     self._update(l, kind, lr, hyper)

@@ -202,3 +202,49 @@ def test_step_against_autograd_with_the_weight_of_the_factors():
 
 
 SIZES = dict(tokens=256, d=128, inter=256, vocab=301, layers=2, r=32, heads=4, kv_heads=1, head_dim=32, docs=3, tied=True)
+
+
+def test_a_step_whose_norm_is_no_number_is_left_out():
+    s = M.Sizes(max_norm=1.0, **SIZES)
+    model = M.MlpLm(s)
+    ids, y = M.synthetic_batch(s)
+    keep = lambda: [t.clone() for l in range(s.layers) for k in model.w[l] for t in (model.w[l][k], model.master[l][k], *model.moments[l][k])]  # noqa: E731
+    before, good = keep(), float(model.head[0, 0])
+    model.head[ids[0], 0] = INF
+    model.forward(ids, y)
+    model.backward(lr=1e-3)
+    assert not np.isfinite(float(model.norm[0])) and float(model.norm[1]) == 1.0
+    assert model.step_no == 0 and all(torch.equal(a, b) for a, b in zip(keep(), before))
+    model.head[ids[0], 0] = good
+    model.forward(ids, y)
+    model.backward(lr=1e-3)
+    assert model.step_no == 1 and all(torch.isfinite(t).all() for t in keep())
+    assert not any(torch.equal(a, b) for a, b in zip(keep(), before))
+
+
+def test_a_clipped_step_can_be_captured():
+    s = M.Sizes(max_norm=1.0, **SIZES)
+    model = M.MlpLm(s)
+    ids, y = M.synthetic_batch(s)
+
+    def step():
+        model.forward(ids, y)
+        model.backward(lr=1e-3)
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    state = [t for lw, mw, mo in zip(model.w, model.master, model.moments) for k in lw for t in (lw[k], mw[k], *mo[k])]
+    keep = [t.clone() for t in state]
+    step()
+    want = [t.clone() for t in state]
+    for t, k in zip(state, keep):
+        t.copy_(k)
+    model.step_no = 1
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    graph.replay()
+    assert all(torch.equal(a, b) for a, b in zip(state, want))
+    assert B.acx_last_device_status() == B.ACX_OK

@@ -46,6 +46,25 @@ def test_the_step_counts_its_factors_so(monkeypatch):
     assert set(of.values()) == {1.0} and len(of) == sum(len(t) for t in model.grads.values())
 
 
+@pytest.mark.parametrize("norm,f,steps", [(0.5, 1.0, 1), (4.0, 0.25, 1), (float("inf"), 1e-40, 1), (float("inf"), 1.0, 0), (float("nan"), 1.0, 0)])
+def test_a_step_whose_norm_is_no_number_is_left_out(monkeypatch, norm, f, steps):
+    """(a norm beyond fp32 reads as infinity, but has a factor: those gradients are clipped like others)"""
+    monkeypatch.setattr(B, "make_grad_list", lambda tensors, weights: None)
+    monkeypatch.setattr(B, "alloc_grad_workspace", lambda grads: None)
+    model = M.MlpLm(M.Sizes(tokens=32, d=64, inter=128, vocab=100, layers=2, r=16, max_norm=1.0), device="cpu")
+    for name in ("acx_norm_join_fwd", "acx_linear_fwd", "acx_swiglu_fwd", "acx_linear_ce_fwd", "acx_linear_ce_bwd", "acx_norm_join_bwd",
+                 "acx_linear_bwd", "acx_swiglu_bwd"):
+        monkeypatch.setattr(B, name, lambda *a, **k: None)
+    monkeypatch.setattr(B, "acx_grad_clip", lambda grads, max_norm, total, ws: total.copy_(torch.tensor([norm, f])))
+    updates = []
+    monkeypatch.setattr(B, "acx_reconstruct_adamw", lambda *a, step, **k: updates.append(step))
+    model.forward(*M.synthetic_batch(model.s, device="cpu"))
+    model.backward()
+    assert not updates and model.step_no == 0
+    model.backward(lr=1e-3)
+    assert updates == steps * 4 * [1] and model.step_no == steps
+
+
 def test_clipping_without_tensors_has_no_chunks():
     """A descriptor that no list has: its chunks would be read from a plan that nothing asked for."""
     d = B.acx_grad_desc(ctypes.sizeof(B.acx_grad_desc), 0, 0, 5)
