@@ -403,9 +403,13 @@ ACX_API acx_status acx_attn_plan(const acx_attn_desc* desc, const int32_t* offse
                                  void* cuda_stream);
 
 /*   Q [tokens][heads][head_dim], K, V [tokens][kv_heads][head_dim] in;  slopes [heads] fp32 or NULL: no bias;
- *   O [tokens][heads][head_dim] out;  lse [heads][tokens] fp32, out, or NULL: log of the sum of exp(z), for the backward.
- * Scores that the mask takes out may be anything.  Values of a document's own tokens have to be finite, though: a weight of zero
- * times a NaN or an infinity is a NaN, for any query within 127 tokens before such a one.
+ *   O [tokens][heads][head_dim] out;  lse [heads][tokens] fp32, out, or NULL: log of the sum of exp(z), for the backward; neither in the
+ *   place of an input.
+ * Scores that the mask takes out may be anything, and a score of minus infinity is a weight of zero (a query that has no others has
+ * no softmax: NaN).  Values of a document's own tokens have to be finite, though: a weight of zero times a NaN or an infinity is a NaN.
+ * Tiles of 128 tokens count from the document's start, and a query takes whole tiles: up to its own, or where the prefix ends behind
+ * that, up to the one in which it ends (all of the document's where not causal).  A value of V in them that is not finite reaches it
+ * although the mask hides it.
  * Scores and sums are fp32; the probabilities enter the second product rounded to bfloat16, as dS = p (dP - delta) does in the
  * backward (into dK of a document of up to 512 tokens as two bfloat16, to 2^-16); every output is rounded once. */
 ACX_API acx_status acx_attn_fwd(const acx_attn_desc* desc, const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv,
@@ -416,6 +420,8 @@ ACX_API acx_status acx_attn_fwd(const acx_attn_desc* desc, const void* Q, int64_
  *   ACX_OP_ATTN_BWD.
  * The probabilities are taken from lse again, to 2^-22 |lse| relative, and bounded by 1: gradients through scores far beyond some 10^4
  * are of no use, but numbers.
+ * What is not finite reaches as far as in the forward: of K and V, dQ of the queries that take its tile; of Q, O, lse and dO, dK and dV
+ * of the keys whose own tile begins at or before that of such a query, or, where their tile begins inside the prefix, of all of those.
  * Fixed summation order, no atomics: reproducible bits. */
 ACX_API acx_status acx_attn_bwd(const acx_attn_desc* desc, const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv,
                                 const float* slopes, const void* plan, size_t plan_bytes, const void* O, int64_t ldo, const void* dO, int64_t lddo,

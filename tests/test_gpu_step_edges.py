@@ -125,6 +125,38 @@ def test_gradients_through_a_saturated_cap(d, alibi, causal, T):
         assert np.median(want[name + "_bound"]) <= 0.1 * np.abs(want[name]).max(), name      # a bound that says something
 
 
+# ----------------------------------------------------------------------------------- how far what is not a number reaches
+def test_values_that_are_no_numbers_reach_the_tiles_that_take_them():
+    """Tiles of 128 tokens count from the document's start.  A query takes those up to the prefix's end or its own, whichever is later; a
+    key takes queries from its own tile on, or from the document's start if its tile begins inside the prefix."""
+    T, H, d, s = 700, 2, 64, 37
+    end = s + 600
+    x = inputs(T, H, 1, d)
+    desc = B.make_attn_desc(T, H, 1, d, 2)
+    for prefix, bad in ((0, s + 132), (130, s + 260)):
+        args, kw = (desc, offsets_of(s, end)), dict(prefix=torch.tensor([0, prefix], dtype=torch.int32, device="cuda"))
+        want = run(*args, *x, **kw)
+        tile = s + (bad - s) // 128 * 128            # queries before this one take no tile with the bad key
+        for i in (1, 2):
+            y = [t.clone() for t in x]
+            y[i][bad] = NAN
+            got = run(*args, *y, **kw)
+            for a, b in zip(got[:3], want):
+                assert torch.equal(a[:tile], b[:tile]), (prefix, i)
+            assert torch.equal(got[3][:s], want[3][:s]) and torch.equal(got[3][end:], want[3][end:])
+        later = s + 256                              # tiles of keys that begin behind the bad query's and behind the prefix
+        for i in (0, 3):
+            y = [t.clone() for t in x]
+            y[i][s + 140] = INF
+            got = run(*args, *y, **kw)
+            assert torch.equal(got[3][later:], want[3][later:]) and torch.equal(got[4][later:], want[4][later:]), (prefix, i)
+    # what the text says of a prefix: a query takes the whole tile that the prefix ends in
+    y = [t.clone() for t in x]
+    y[2][s + 250] = NAN
+    o = run(*args, *y, **kw)[0]
+    assert torch.isnan(o[s:end]).all()
+
+
 # ------------------------------------------------------------------------------------------- short documents, long batches
 def test_dk_of_a_document_does_not_depend_on_the_batch():
     """One query head per key head (no parts to join): the same bits in a batch of 500 tokens, of 513 and of 4000."""
