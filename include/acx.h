@@ -379,7 +379,8 @@ ACX_API acx_status acx_linear_ce_bwd_loss(const acx_ce_desc* desc, const void* X
  * o_i = sum of p_ij v_j, p the softmax of z over the keys that i sees: those of its own document and, where causal, only the keys
  * j <= i and those of the document's prefix.
  *   head_dim a multiple of 8, 8 <= head_dim <= 128;  heads a multiple of kv_heads, at most 4096;  tokens <= 2^24 (0 is a no-op);
- *   docs >= 1;  scale > 0;  (tokens / 128 + docs) * heads <= 2^30. */
+ *   docs >= 1;  scale > 0;  scale, softcap and scale / softcap <= 2^104;  slopes finite, and as large as
+ *   leaves their products with the longest distance finite;  (tokens / 128 + docs) * heads <= 2^30. */
 typedef struct acx_attn_desc {
   uint32_t struct_size; /* sizeof(acx_attn_desc) */
   int32_t io_dtype;     /* ACX_BF16 */

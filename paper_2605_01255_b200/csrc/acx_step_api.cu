@@ -14,6 +14,9 @@ acx_status validate_attn(const acx_attn_desc* d, AttnProblem* out) {
   if (!d || d->struct_size != sizeof(acx_attn_desc)) return ACX_ERR_INVALID_ARG;
   if (d->io_dtype != ACX_BF16 || (d->causal != 0 && d->causal != 1)) return ACX_ERR_INVALID_ARG;
   if (!(d->scale > 0.f) || !std::isfinite(d->scale) || !(d->softcap >= 0.f) || !std::isfinite(d->softcap)) return ACX_ERR_INVALID_ARG;
+  // what the kernels take of them stays well inside fp32: scale log2(e), softcap log2(e), 2^7 scale / softcap, scale times a gradient
+  constexpr double kMost = 0x1p104;
+  if (d->scale > kMost || d->softcap > kMost || (d->softcap > 0.f && d->scale > kMost * d->softcap)) return ACX_ERR_INVALID_ARG;
   if (d->tokens < 0 || d->tokens > (int64_t(1) << 24) || d->docs < 1 || d->docs > (int64_t(1) << 24)) return ACX_ERR_UNSUPPORTED_SHAPE;
   if (d->heads < 1 || d->heads > 4096 || d->kv_heads < 1 || d->heads % d->kv_heads) return ACX_ERR_UNSUPPORTED_SHAPE;
   if (d->head_dim < 8 || d->head_dim > 128 || d->head_dim % 8) return ACX_ERR_UNSUPPORTED_SHAPE;

@@ -280,3 +280,18 @@ def test_a_clipped_step_can_be_captured():
     graph.replay()
     assert all(torch.equal(a, b) for a, b in zip(state, want))
     assert B.acx_last_device_status() == B.ACX_OK
+
+
+@pytest.mark.parametrize("scale,cap,size", [(2.0 ** 104, 0.0, 2.0 ** -104), (0.125, 2.0 ** 104, 1.0), (1.0, 2.0 ** -104, 1.0)])
+def test_scales_and_caps_at_their_limits(scale, cap, size):
+    """The largest scale on queries as small (so that scores are ordinary ones), a cap that does nothing, one that leaves no score: the
+    results are those of ordinary scales, and of a mean."""
+    T, H, d = 200, 2, 64
+    q, k, v, do = inputs(T, H, 1, d)
+    offsets = offsets_of(T)
+    got = run(B.make_attn_desc(T, H, 1, d, scale=scale, softcap=cap), offsets, q * size, k, v, do)
+    assert all(torch.isfinite(t).all() for t in got)
+    want = run(B.make_attn_desc(T, H, 1, d, scale=scale * size), offsets, torch.zeros_like(q) if cap == 2.0 ** -104 else q, k, v, do)
+    # a rounding more or less of the scores (2^-24 of some tens) turns a bf16 result over: one step, 2^-7, of few
+    for a, b in zip(got[:2], want[:2]):
+        assert ((a.double() - b.double()).abs() <= 2.0 ** -7 * b.double().abs() + 1e-4).all()

@@ -76,3 +76,15 @@ def test_clipping_without_tensors_has_no_chunks():
     assert L.acx_grad_plan(ctypes.byref(d), None, p(P), 1 << 30, None) == B.ACX_ERR_INVALID_ARG
     for op in (B.ACX_OP_GRAD_PLAN, B.ACX_OP_GRAD_CLIP):
         assert L.acx_grad_workspace_bytes(ctypes.byref(d), op) == 0
+
+
+@pytest.mark.parametrize("scale,cap,ok", [(0.125, 50.0, True), (0.125, 1e5, True), (2.0 ** 104, 0.0, True), (2.0 ** 105, 0.0, False), (2.0 ** 127, 0.0, False),
+                                          (3e38, 0.0, False), (0.125, 2.0 ** 104, True), (0.125, 2.0 ** 105, False), (0.125, 2.4e38, False),
+                                          (1.0, 2.0 ** -104, True), (1.0, 2.0 ** -105, False), (1e3, 1e-36, False), (1.0, 1e-45, False)])
+def test_scales_and_caps_beyond_what_fp32_holds(scale, cap, ok):
+    """The kernels take scale log2(e), cap log2(e) and 2^7 scale / cap, and scale times gradients: each has to be a number."""
+    d = B.make_attn_desc(256, 4, 2, 64, scale=scale, softcap=cap)
+    assert (B.acx_attn_workspace_bytes(d, B.ACX_OP_ATTN_PLAN) > 0) == ok
+    if not ok:
+        p = ctypes.c_void_p
+        assert B.lib().acx_attn_plan(ctypes.byref(d), p(P), None, p(P), 1 << 30, None) == B.ACX_ERR_INVALID_ARG
