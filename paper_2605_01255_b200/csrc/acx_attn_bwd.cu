@@ -12,7 +12,7 @@
 // together (errors of dQ 0.0029 relative to its size without it).  So dS is taken with the delta that O gives, r_i = sum of
 // p (dP - delta) summed in fp32 beside it, delta + r is what the launch for the keys uses, and dQ = scale (second - r' first) with
 // the sum r' of the dS as they were rounded: exact ones sum to zero, so r' is e and what the roundings leave of the keys' mean (errors
-// of dQ 0.00245 with r, 0.0023 with r', where the keys have a mean; the rounding of dS and of dQ themselves make 0.0023).
+// of dQ 0.00245 with r, 0.0022 to 0.0023 with r', where the keys have a mean; the rounding of dS and of dQ themselves make 0.0023).
 // The price of two launches is that S and dP are computed twice: eight products instead of five.  Measured: 8192 tokens x 24 heads (8
 // of keys) x 128, causal, 609 us for the queries and 709 for the keys, 1.25 PFLOP/s over the eight, 75 % of the rate of a large product (tensor
 // pipe 70 and 56 % busy); 2650 and 3180 cycles per tile of 128 x 128 where the products alone need 2048, the rest is rows' work in between.

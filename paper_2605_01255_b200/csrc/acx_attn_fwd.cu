@@ -14,7 +14,10 @@
 // What bounds it: per tile of 128 x 128 and d = 128 the tensor core needs 2 x 512 cycles and the 16384 exponentials 1024 cycles of
 // the special function units: both at once.  Measured: 8192 tokens x 24 heads (8 of keys) x 128, causal, 352 us, 1.17 PFLOP/s, 71 % of
 // the rate of a large product, tensor pipe 60 % busy and exponentials 61 %; 16384 x 32 x 8 x 64 with distances 1603 us, 0.69 PFLOP/s: half
-// the products per score, and the instructions around each exponential (bias, maximum, conversion, sum) fill the issue slots.
+// the products per score.  No unit is full: one document of 4096 x 32 x 8, d = 64 with distances has exponentials 58 %, issue slots 49 %, tensor
+// pipe 29 % (without 65, 38, 33; d = 128 58, 35, 58).  A scheduler has two rows' warps, which go through reading scores, maximum, exponentials
+// and storing one after the other; of the cycles between two instructions of a warp the largest parts are fixed latencies and scores
+// on their way from tensor memory.
 //
 // Roles (384 threads, one CTA per SM, persistent): warp 0 copies, warp 1 products and tensor memory, warps 4..7 and 8..11
 // the rows of the two halves, with 208 registers a thread (the first warpgroup's threads keep 88: 128 x 88 + 256 x 208 is what
@@ -162,7 +165,8 @@ static_assert(kBins == kPlanThreads, "one bin per thread");
 // ---------------------------------------------------------------------------------------------------------------- forward
 constexpr int kFwdThreads = 384;
 // Work items have 256 queries, whose halves take turns with the products; where that leaves SMs without an item they have 128, and one
-// half of the rows' warps has nothing to do (2048 tokens x 16 heads x 64, 128 items of 256: 30.2 us, 24.1 in items of 128; 3001 x 6 x
+// half of the rows' warps has nothing to do.  Items are counted from the batch's tokens; uneven documents make more of them, which the host does
+// not know (2048 tokens x 16 heads x 64, 128 items of 256: 30.2 us, 24.1 in items of 128; 3001 x 6 x
 // 72 with a cap 52.9 and 48.6; but 4096 x 14 x 64, 224 items: 54 and 70).
 template <int HD>
 struct FwdSmem {
