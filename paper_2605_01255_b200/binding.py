@@ -561,8 +561,11 @@ def make_grad_list(tensors: Sequence[torch.Tensor], weights: Optional[Sequence[f
     if dev.index != torch.cuda.current_device():
         raise ValueError("the gradients are on %s, the current device is cuda:%d" % (dev, torch.cuda.current_device()))
     plan = torch.empty(int(lib().acx_grad_workspace_bytes(ctypes.byref(desc), ACX_OP_GRAD_PLAN)), dtype=torch.uint8, device=dev)
+    current = torch.cuda.current_stream()
+    if stream is not None and stream != current:
+        stream.wait_stream(current)      # the plan's memory is the current stream's: what was there before may still be written
     _check(lib().acx_grad_plan(ctypes.byref(desc), items, ctypes.c_void_p(plan.data_ptr()), plan.numel(), _stream(stream)), "acx_grad_plan")
-    (stream or torch.cuda.current_stream()).synchronize()
+    (stream or current).synchronize()
     return GradList(desc, plan, (tensors, out))
 
 

@@ -295,3 +295,20 @@ def test_scales_and_caps_at_their_limits(scale, cap, size):
     # a rounding more or less of the scores (2^-24 of some tens) turns a bf16 result over: one step, 2^-7, of few
     for a, b in zip(got[:2], want[:2]):
         assert ((a.double() - b.double()).abs() <= 2.0 ** -7 * b.double().abs() + 1e-4).all()
+
+
+def test_a_list_made_on_another_stream_waits_for_the_memory_it_gets():
+    """The plan's memory comes from the current stream, where a kernel may still have to write what was there before."""
+    grads = [torch.ones(n, device="cuda") for n in (100, 70_000, 5)]
+    want = B.make_grad_list(grads).plan.clone()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        old = torch.empty(want.numel(), dtype=torch.uint8, device="cuda")
+        torch.cuda._sleep(20_000_000)                # some 10 ms of nothing, then the write
+        old.fill_(255)
+        del old
+        lst = B.make_grad_list(grads, stream=side)
+        torch.cuda.synchronize()
+        assert torch.equal(lst.plan, want)           # (before any call reads it)
+        del lst
